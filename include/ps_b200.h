@@ -591,6 +591,64 @@ int ps_planner_num_aggregators(ps_planner* pl, int* allocated_out, int* alive_ou
  * it has to wait for the next cycle. */
 int ps_planner_outlier_fits(double cycle, double now_in_cycle, double remaining_scheduled, double exec_time);
 
+/* ---------------------------------------------------------------------------
+ * Microscaled 4-bit operands: what a worker computes with between a pull and a
+ * push.  (The paper has no counterpart: it leaves the workers' arithmetic to the
+ * training framework.)  No ps_service is involved; the calls run on `stream` of
+ * the CURRENT device, allocate nothing and wait for nothing.
+ *
+ * Format: blocks of 32 consecutive elements of a row share the scale
+ * 2^(floor(log2(largest magnitude)) - 2), at least 2^-127; the quotients are E2M1
+ * numbers (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives), rounded to nearest,
+ * ties to the even code, saturating at 6.  A block that holds a NaN or an infinity
+ * reads back as NaN in all its places and makes every product it enters NaN.
+ * ------------------------------------------------------------------------- */
+
+/* One operand of rows x cols elements.  The caller owns both buffers (device,
+ * 16-byte aligned, sizes from ps_mx_sizes); their layout is the library's:
+ * codes = two per byte, rows of round_up(cols, 32)/2 bytes; scales = atoms of 128
+ * rows x 4 blocks in the order in which the tensor cores take them. */
+typedef struct {
+  void* codes;
+  void* scales;
+  long long rows, cols;
+} ps_mx;
+
+/* Bytes of the two buffers of an operand (either out pointer may be NULL).
+ * Errors: BAD_ARG (rows < 0, cols < 1, either 2^31 or more). */
+int ps_mx_sizes(long long rows, long long cols, size_t* code_bytes_out, size_t* scale_bytes_out);
+
+/* Quantises the matrix x (device; rows x cols of `dtype`, a ps_dtype; row stride
+ * `ld` elements, >= cols) along its rows into *q, along its columns into *qt, or
+ * both from one read of x.  *qt is the operand of the transposed matrix: its rows
+ * are x's columns (qt->rows == cols, qt->cols == rows), so it is what a product
+ * that sums over x's rows takes — of the three products of a layer's training step,
+ * y = x w^T, dx = dy w and dw = dy^T x, the last two need it.  q or qt may be NULL,
+ * not both.  rows = 0 is a no-op.
+ * Errors: BAD_ARG, ALIGN (x not aligned to its element, an operand's buffer not to
+ * 16 bytes), TOO_LARGE (2^31 tiles of 128 x 128), CUDA. */
+int ps_mx_quantize(const void* x, int dtype, long long rows, long long cols, long long ld, const ps_mx* q,
+                   const ps_mx* qt, void* stream);
+
+/* The values an operand stands for, as `dtype` (exact in either), row stride `ld`.
+ * Errors: BAD_ARG, ALIGN, TOO_LARGE, CUDA. */
+int ps_mx_dequantize(const ps_mx* q, int dtype, void* out, long long ld, void* stream);
+
+/* c[m][n] = sum_k a[m][k] * b[n][k] (c: a->rows x b->rows of `dtype`, row stride
+ * `ldc`), products exact, summed in binary32 by the tensor cores in an order that
+ * depends on the sizes only, rounded once to `dtype`.  a->cols must equal b->cols.
+ * No rows in a or b: a no-op.
+ * Errors: BAD_ARG, ALIGN, TOO_LARGE, CUDA. */
+int ps_mx_matmul(const ps_mx* a, const ps_mx* b, int dtype, void* c, long long ldc, void* stream);
+
+/* Waits for the current device and reports the product's status word: 0 = no
+ * fault; non-zero = a bounded wait inside a kernel expired (that launch's results
+ * are undefined). */
+int ps_mx_status(int* status_out);
+
+/* Text of the last CUDA error of a ps_mx_* or ps_clip_* call on this host thread. */
+const char* ps_op_last_error(void);
+
 const char* ps_strerror(int status);
 /* Text of the last CUDA error seen by this service ("" if none). */
 const char* ps_last_cuda_error(ps_service* svc);

@@ -50,6 +50,10 @@ class ps_chunk_info(C.Structure):
                 ("elem_count", C.c_ulonglong), ("num_workers", C.c_int), ("vector_path", C.c_int)]
 
 
+class ps_mx(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("rows", C.c_longlong), ("cols", C.c_longlong)]
+
+
 class PsError(RuntimeError):
     def __init__(self, status: int, where: str, detail: str = ""):
         self.status = status
@@ -134,6 +138,13 @@ _SIGNATURES = {
     "ps_peer_event_wait": (C.c_int, [C.c_void_p, C.c_void_p]),
     "ps_peer_event_destroy": (C.c_int, [C.c_void_p]),
     "ps_peer_copy_many": (C.c_int, [C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "ps_mx_sizes": (C.c_int, [C.c_longlong, C.c_longlong, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]),
+    "ps_mx_quantize": (C.c_int, [C.c_void_p, C.c_int, C.c_longlong, C.c_longlong, C.c_longlong, C.c_void_p, C.c_void_p,
+                                 C.c_void_p]),
+    "ps_mx_dequantize": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p, C.c_longlong, C.c_void_p]),
+    "ps_mx_matmul": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_longlong, C.c_void_p]),
+    "ps_mx_status": (C.c_int, [C.POINTER(C.c_int)]),
+    "ps_op_last_error": (C.c_char_p, []),
     "ps_strerror": (C.c_char_p, [C.c_int]),
     "ps_last_cuda_error": (C.c_char_p, [C.c_void_p]),
     "ps_version": (C.c_char_p, []),
@@ -619,6 +630,88 @@ def ps_peer_copy_many(dsts, srcs, nbytes, stream=None):
     """uint64 numpy arrays of destination and source addresses and of byte counts."""
     _check_peer(load().ps_peer_copy_many(len(dsts), dsts.ctypes.data, srcs.ctypes.data, nbytes.ctypes.data,
                                          _stream_ptr(stream)), "ps_peer_copy_many")
+
+
+# ---- operators that need no service ---------------------------------------------
+
+def _check_op(rc: int, where: str):
+    if rc != PS_OK:
+        raise PsError(rc, where, load().ps_op_last_error().decode() if rc == PS_ERR_CUDA else "")
+
+
+_DTYPES = {"torch.float32": PS_F32, "torch.bfloat16": PS_BF16}
+
+
+def _dtype(t, where: str) -> int:
+    d = _DTYPES.get(str(t.dtype))
+    if d is None:
+        raise PsError(PS_ERR_BAD_ARG, where, "%s is neither float32 nor bfloat16" % t.dtype)
+    return d
+
+
+def _matrix(t, where: str):
+    """(address, ps_dtype, row stride) of a 2-d device tensor whose rows are contiguous."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or not t.is_cuda:
+        raise PsError(PS_ERR_BAD_ARG, where, "a 2-d CUDA tensor with contiguous rows is wanted")
+    return t.data_ptr(), _dtype(t, where), max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+
+
+class MxTensor:
+    """A microscaled 4-bit operand of rows x cols elements and the two device
+    buffers that hold it (`codes` and `scales`, uint8, in the library's layout)."""
+
+    def __init__(self, rows: int, cols: int, device=None):
+        import torch
+        n, m = C.c_size_t(), C.c_size_t()
+        _check_op(load().ps_mx_sizes(rows, cols, C.byref(n), C.byref(m)), "ps_mx_sizes")
+        self.rows, self.cols = rows, cols
+        self.codes = torch.empty(n.value, dtype=torch.uint8, device=device or "cuda")
+        self.scales = torch.empty(m.value, dtype=torch.uint8, device=device or "cuda")
+        self._c = ps_mx(self.codes.data_ptr(), self.scales.data_ptr(), rows, cols)
+        self.ref = C.addressof(self._c)
+
+    @property
+    def shape(self):
+        return self.rows, self.cols
+
+
+def _mx_ref(q):
+    return None if q is None else q.ref
+
+
+def ps_mx_quantize(x, q=None, qt=None, stream=None):
+    """Quantises the device matrix x (float32 or bfloat16, any row stride) along
+    its rows into q and / or along its columns into qt (x's transpose)."""
+    where = "ps_mx_quantize"
+    ptr, dtype, ld = _matrix(x, where)
+    _check_op(load().ps_mx_quantize(ptr, dtype, x.shape[0], x.shape[1], ld, _mx_ref(q), _mx_ref(qt), _stream_ptr(stream)),
+              where)
+
+
+def ps_mx_dequantize(q, out, stream=None):
+    """Writes the values q stands for to the device matrix out, which it returns."""
+    where = "ps_mx_dequantize"
+    ptr, dtype, ld = _matrix(out, where)
+    if tuple(out.shape) != q.shape:
+        raise PsError(PS_ERR_BAD_ARG, where, "out is %s, the operand %s" % (tuple(out.shape), q.shape))
+    _check_op(load().ps_mx_dequantize(q.ref, dtype, ptr, ld, _stream_ptr(stream)), where)
+    return out
+
+
+def ps_mx_matmul(a, b, out, stream=None):
+    """out[m][n] = sum over k of a[m][k] * b[n][k]; returns out (float32 or bfloat16, any row stride)."""
+    where = "ps_mx_matmul"
+    ptr, dtype, ld = _matrix(out, where)
+    if out.shape[0] != a.rows or out.shape[1] != b.rows:
+        raise PsError(PS_ERR_BAD_ARG, where, "out is %s, the product %s" % (tuple(out.shape), (a.rows, b.rows)))
+    _check_op(load().ps_mx_matmul(a.ref, b.ref, dtype, ptr, ld, _stream_ptr(stream)), where)
+    return out
+
+
+def ps_mx_status() -> int:
+    v = C.c_int()
+    _check_op(load().ps_mx_status(C.byref(v)), "ps_mx_status")
+    return v.value
 
 
 def _bind(name):

@@ -1,0 +1,410 @@
+// Product of two microscaled 4-bit operands on the 5th-generation tensor cores:
+//     C[m][n] = sum_k A[m][k] * B[n][k],   fp32 accumulation, fp32 or bf16 result.
+//
+// tcgen05.mma of kind mxf4 takes E2M1 operands from shared memory and one E8M0
+// scale per 32 elements of either from tensor memory.  A CTA computes tiles of
+// 128 rows of one operand ("P") by BN rows of the other ("Q"), 256 elements of K
+// per pipeline stage: a stage is 128 and BN rows of 128 bytes (TMA, 128-byte
+// swizzle) and their atoms of scales (plain bulk copies; the quantiser stores
+// them in the order in which scale memory takes them).
+//   warp 0     one lane issues the copies
+//   warp 1     one lane copies the scales to tensor memory and issues the MMAs
+//   warps 2-5  read the accumulators and store the result
+// Where one operand has few rows (single tokens) it is Q and the other, usually
+// the weight, P, whichever of A and B that is: the MMA's 128 rows are then full
+// and what is left is reading P once.  Such a product has few tiles, so the CTAs
+// of a cluster share a tile's K and add their parts in rank order through
+// distributed shared memory: no workspace, no atomics, the same result each time.
+#pragma once
+
+#include <cuda.h>
+
+#include "ps_mx.cuh"
+
+namespace psb {
+
+constexpr int kMmThreads = 192;
+constexpr int kMmP = 128;                       // rows of P in a tile
+constexpr int kMmStageK = 256;                  // elements of K in a stage: 128 bytes of codes, 2 atoms of scales
+constexpr int kMmMaxStages = 8;
+constexpr int kMmSmem = 227 * 1024;
+
+template <int BN>
+struct MmCfg {
+  static constexpr int kQBlocks = (BN + 127) / 128;             // 128-row blocks of scales of Q
+  static constexpr int kBytesP = kMmP * 128, kBytesQ = BN * 128;
+  static constexpr int kBytesS = 2 * kMxAtom;                   // scales of one 128-row block in a stage
+  static constexpr int kStage = kBytesP + kBytesQ + kBytesS * (1 + kQBlocks);
+  static constexpr int kFit = (kMmSmem - 2048) / kStage;
+  static constexpr int kStages = kFit < kMmMaxStages ? kFit : kMmMaxStages;
+  static constexpr int kAcc = BN <= 128 ? 2 : 1;                // accumulators: two hide the epilogue; 256 columns leave room for one
+  static constexpr int kScaleCol = kAcc * BN;                   // tensor memory: accumulators, then two sets of scales
+  static constexpr int kScaleSet = 8 + 8 * kQBlocks;
+  static constexpr int kCols = kScaleCol + 2 * kScaleSet;
+  static constexpr int kAlloc = kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
+  static constexpr int kSmem = 1024 + kStages * kStage;
+  static_assert(kStages >= 3 && kCols <= 512 && kStage % 1024 == 0, "tile does not fit");
+};
+
+struct MmArgs {
+  const uint8_t* sp;                            // scales of P and Q
+  const uint8_t* sq;
+  void* c;
+  long long ldc;
+  long long rows_p, rows_q;
+  long long atoms;                              // atoms of scales per 128 rows
+  int stages_k;                                 // stages along K
+  int tiles_p, tiles_q;
+  int splits;                                   // CTAs (one cluster) per tile
+  int swap;                                     // 1: P is B, so a lane's row is a column of C
+  int out_f32;
+  int vec_ok;                                   // rows of C allow 128-bit stores
+  int* status;
+};
+
+constexpr long long kMmWaitCycles = 2000000000ll;     // about a second
+
+__device__ __forceinline__ unsigned int mm_smem(const void* p) {
+  return static_cast<unsigned int>(__cvta_generic_to_shared(p));
+}
+
+__device__ __forceinline__ bool mm_try_wait(unsigned int bar, unsigned int parity) {
+  unsigned int ok;
+  asm volatile(
+      "{\n\t"
+      ".reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t"
+      "}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+
+// Bounded wait: false if the limit ran out (the status word then says so and the launch's results are undefined).
+__device__ __forceinline__ bool mm_wait(unsigned int bar, unsigned int parity, int* status) {
+  if (mm_try_wait(bar, parity)) return true;
+  const long long t0 = clock64();
+  while (!mm_try_wait(bar, parity)) {
+    if (clock64() - t0 > kMmWaitCycles) {
+      atomicExch(status, 1);
+      return false;
+    }
+  }
+  return true;
+}
+
+__device__ __forceinline__ void mm_tma(unsigned int dst, const CUtensorMap* map, int x, int y, unsigned int bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(y), "r"(bar)
+      : "memory");
+}
+
+__device__ __forceinline__ void mm_bulk(unsigned int dst, const void* src, unsigned int bytes, unsigned int bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+               "l"(src), "r"(bytes), "r"(bar)
+               : "memory");
+}
+
+__device__ __forceinline__ void mm_commit(unsigned int bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+// Shared memory descriptors: rows of 128 bytes in 128-byte swizzle (8-row groups 1024 bytes apart), and an atom of
+// scales, 32 rows of 16 bytes (8-row groups 128 bytes apart, no swizzle).
+__device__ __forceinline__ unsigned long long mm_desc_codes(unsigned int addr) {
+  return (unsigned long long)((addr & 0x3ffffu) >> 4) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ unsigned long long mm_desc_scales(unsigned int addr) {
+  return (unsigned long long)((addr & 0x3ffffu) >> 4) | (1ull << 16) | (8ull << 32) | (1ull << 46);
+}
+
+__device__ __forceinline__ void mm_copy_scales(unsigned int tmem, unsigned int smem) {
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(mm_desc_scales(smem)) : "memory");
+}
+
+__device__ __forceinline__ void mm_mma(unsigned int d, unsigned long long a, unsigned long long b, unsigned int idesc,
+                                       unsigned int sa, unsigned int sb, bool accumulate) {
+  asm volatile(
+      "{\n\t"
+      ".reg .pred p;\n\t"
+      "setp.ne.u32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t"
+      "}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"((unsigned int)accumulate)
+      : "memory");
+}
+
+// 32 columns of this warp's 32 lanes.
+__device__ __forceinline__ void mm_load32(unsigned int tmem, float (&v)[32]) {
+  unsigned int* u = reinterpret_cast<unsigned int*>(v);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]),
+        "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15]), "=r"(u[16]),
+        "=r"(u[17]), "=r"(u[18]), "=r"(u[19]), "=r"(u[20]), "=r"(u[21]), "=r"(u[22]), "=r"(u[23]), "=r"(u[24]),
+        "=r"(u[25]), "=r"(u[26]), "=r"(u[27]), "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
+      : "r"(tmem));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void mm_load16(unsigned int tmem, float (&v)[16]) {
+  unsigned int* u = reinterpret_cast<unsigned int*>(v);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]),
+        "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15])
+      : "r"(tmem));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+template <int N>
+__device__ __forceinline__ void mm_load(unsigned int tmem, float (&v)[N]) {
+  if constexpr (N == 32) mm_load32(tmem, v);
+  else mm_load16(tmem, v);
+}
+
+__device__ __forceinline__ unsigned int mm_bf16x2(float lo, float hi) {
+  unsigned int r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+__device__ __forceinline__ void mm_store1(const MmArgs& a, long long m, long long n, float v) {
+  const size_t at = (size_t)m * (size_t)a.ldc + (size_t)n;
+  if (a.out_f32) static_cast<float*>(a.c)[at] = v;
+  else static_cast<unsigned short*>(a.c)[at] = (unsigned short)mm_bf16x2(v, 0.f);
+}
+
+// Stores N consecutive accumulators (rows q.. of Q) of P's row p.
+template <int N>
+__device__ __forceinline__ void mm_store(const MmArgs& a, long long p, long long q, const float (&v)[N]) {
+  if (p >= a.rows_p) return;
+  if (a.swap) {                                  // a warp's lanes are neighbours in C
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (q + i < a.rows_q) mm_store1(a, q + i, p, v[i]);
+  } else if (a.vec_ok && q + N <= a.rows_q) {
+    if (a.out_f32) {
+      float4* o = reinterpret_cast<float4*>(static_cast<float*>(a.c) + (size_t)p * (size_t)a.ldc + (size_t)q);
+#pragma unroll
+      for (int i = 0; i < N / 4; ++i) o[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+    } else {
+      uint4* o = reinterpret_cast<uint4*>(static_cast<unsigned short*>(a.c) + (size_t)p * (size_t)a.ldc + (size_t)q);
+#pragma unroll
+      for (int i = 0; i < N / 8; ++i)
+        o[i] = make_uint4(mm_bf16x2(v[8 * i], v[8 * i + 1]), mm_bf16x2(v[8 * i + 2], v[8 * i + 3]),
+                          mm_bf16x2(v[8 * i + 4], v[8 * i + 5]), mm_bf16x2(v[8 * i + 6], v[8 * i + 7]));
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (q + i < a.rows_q) mm_store1(a, p, q + i, v[i]);
+  }
+}
+
+// Tiles are walked in groups of 16 along P, so that the tiles in flight share rows of both operands in L2.
+__device__ __forceinline__ void mm_tile(const MmArgs& a, int tile, int* tp, int* tq) {
+  constexpr int kGroup = 16;
+  const int per = kGroup * a.tiles_q, g = tile / per, in = tile - g * per;
+  const int n = min(kGroup, a.tiles_p - g * kGroup);
+  *tq = in / n;
+  *tp = g * kGroup + in - *tq * n;
+}
+
+__device__ __forceinline__ void mm_cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+__device__ __forceinline__ float mm_remote(unsigned int addr, unsigned int rank) {
+  float v;
+  asm volatile(
+      "{\n\t"
+      ".reg .b32 r;\n\t"
+      "mapa.shared::cluster.u32 r, %1, %2;\n\t"
+      "ld.shared::cluster.f32 %0, [r];\n\t"
+      "}"
+      : "=f"(v)
+      : "r"(addr), "r"(rank)
+      : "memory");
+  return v;
+}
+
+template <int BN>
+__global__ void __launch_bounds__(kMmThreads, 1)
+ps_mx_matmul_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_q,
+                    const __grid_constant__ MmArgs args) {
+  using Cfg = MmCfg<BN>;
+  extern __shared__ unsigned char raw[];
+  __shared__ __align__(8) unsigned long long s_full[kMmMaxStages], s_empty[kMmMaxStages], s_acc_full[2], s_acc_empty[2];
+  __shared__ unsigned int s_tmem;
+  unsigned char* stages = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+  const unsigned int base = mm_smem(stages);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+  if (tid == 0) {
+    for (int s = 0; s < Cfg::kStages; ++s) {
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(mm_smem(&s_full[s])) : "memory");
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(mm_smem(&s_empty[s])) : "memory");
+    }
+    for (int b = 0; b < Cfg::kAcc; ++b) {
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(mm_smem(&s_acc_full[b])) : "memory");
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], 4;" ::"r"(mm_smem(&s_acc_empty[b])) : "memory");
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_p) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_q) : "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(mm_smem(&s_tmem)),
+                 "r"(Cfg::kAlloc)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const unsigned int tmem = s_tmem;
+  mx_pdl();
+
+  const int tiles = args.tiles_p * args.tiles_q;
+  const int rank = args.splits > 1 ? (int)(blockIdx.x % (unsigned)args.splits) : 0;
+  const int first = args.splits > 1 ? (int)(blockIdx.x / (unsigned)args.splits) : (int)blockIdx.x;
+  const int stride = args.splits > 1 ? tiles : (int)gridDim.x;      // a cluster computes one tile
+  const int k0 = (int)((long long)args.stages_k * rank / args.splits);
+  const int k1 = (int)((long long)args.stages_k * (rank + 1) / args.splits);
+
+  if (warp == 0) {
+    if (lane == 0) {
+      unsigned int it = 0;
+      bool ok = true;
+      for (int tile = first; ok && tile < tiles; tile += stride) {
+        int tp, tq;
+        mm_tile(args, tile, &tp, &tq);
+        const uint8_t* sp = args.sp + (size_t)tp * (size_t)args.atoms * kMxAtom;
+        const uint8_t* sq = args.sq + (size_t)tq * Cfg::kQBlocks * (size_t)args.atoms * kMxAtom;
+        // (the last tile of Q may have no second block of scales; its columns are never stored)
+        const int qb = min(Cfg::kQBlocks, (int)((args.rows_q - (long long)tq * BN + 127) >> 7));
+        const unsigned int bytes = Cfg::kBytesP + Cfg::kBytesQ + Cfg::kBytesS * (1 + qb);
+        for (int k = k0; k < k1; ++k, ++it) {
+          const unsigned int s = it % Cfg::kStages, use = it / Cfg::kStages;
+          if (use > 0 && !mm_wait(mm_smem(&s_empty[s]), (use - 1) & 1u, args.status)) { ok = false; break; }
+          const unsigned int bar = mm_smem(&s_full[s]), at = base + s * Cfg::kStage;
+          asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+          mm_tma(at, &map_p, k * 128, tp * kMmP, bar);
+          mm_tma(at + Cfg::kBytesP, &map_q, k * 128, tq * BN, bar);
+          const unsigned int sc = at + Cfg::kBytesP + Cfg::kBytesQ;
+          mm_bulk(sc, sp + (size_t)k * Cfg::kBytesS, Cfg::kBytesS, bar);
+          for (int b = 0; b < qb; ++b)
+            mm_bulk(sc + Cfg::kBytesS * (1 + b), sq + ((size_t)b * (size_t)args.atoms * kMxAtom + (size_t)k * Cfg::kBytesS),
+                    Cfg::kBytesS, bar);
+        }
+      }
+      if (!ok)                                        // an expired wait: let this CTA's own copies land
+        for (unsigned int s = 0; s < (unsigned)Cfg::kStages && s < it; ++s)
+          mm_wait(mm_smem(&s_full[s]), ((it - 1 - s) / Cfg::kStages) & 1u, args.status);
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (lane == 0) {
+      constexpr unsigned int kIdesc = (1u << 7) | (1u << 10) | ((unsigned)(BN >> 3) << 17) | (1u << 23) | (8u << 24);
+      unsigned int it = 0, n = 0;
+      bool ok = true;
+      for (int tile = first; ok && tile < tiles; tile += stride, ++n) {
+        const unsigned int buf = n % Cfg::kAcc, use = n / Cfg::kAcc;
+        if (use > 0 && !mm_wait(mm_smem(&s_acc_empty[buf]), (use - 1) & 1u, args.status)) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        for (int k = k0; k < k1; ++k, ++it) {
+          const unsigned int s = it % Cfg::kStages;
+          if (!mm_wait(mm_smem(&s_full[s]), (it / Cfg::kStages) & 1u, args.status)) { ok = false; break; }
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const unsigned int at = base + s * Cfg::kStage, sc = at + Cfg::kBytesP + Cfg::kBytesQ;
+          const unsigned int tp = tmem + Cfg::kScaleCol + (it & 1u) * Cfg::kScaleSet, tq = tp + 8;
+          // scales: atom j of P in 4 columns; atom j of Q's blocks side by side
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            mm_copy_scales(tp + j * 4, sc + j * kMxAtom);
+#pragma unroll
+            for (int b = 0; b < Cfg::kQBlocks; ++b)
+              mm_copy_scales(tq + (j * Cfg::kQBlocks + b) * 4, sc + Cfg::kBytesS * (1 + b) + j * kMxAtom);
+          }
+          const unsigned long long dp = mm_desc_codes(at), dq = mm_desc_codes(at + Cfg::kBytesP);
+          // four MMAs of 64 elements (32 bytes) each; an atom serves two, which name its lower or upper pair of scales
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const unsigned int id = kIdesc | ((unsigned)(i & 1) << 30) | ((unsigned)(i & 1) << 5);
+            mm_mma(tmem + buf * BN, dp + 2 * i, dq + 2 * i, id, tp + (i >> 1) * 4, tq + (i >> 1) * 4 * Cfg::kQBlocks,
+                   k > k0 || i > 0);
+          }
+          mm_commit(mm_smem(&s_empty[s]));
+        }
+        mm_commit(mm_smem(&s_acc_full[buf]));
+      }
+    }
+    __syncwarp();
+  } else {
+    const int quad = warp & 3;                        // the quarter of tensor memory's lanes this warp may read
+    unsigned int n = 0;
+    for (int tile = first; tile < tiles; tile += stride, ++n) {
+      const unsigned int buf = n % Cfg::kAcc;
+      if (!__all_sync(0xffffffffu, mm_wait(mm_smem(&s_acc_full[buf]), (n / Cfg::kAcc) & 1u, args.status))) break;
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      int tp, tq;
+      mm_tile(args, tile, &tp, &tq);
+      const int row = quad * 32 + lane;
+      const unsigned int acc = tmem + ((unsigned)(quad * 32) << 16) + buf * BN;
+      constexpr int kStep = BN < 32 ? BN : 32;
+      if (args.splits == 1) {
+#pragma unroll 1
+        for (int c = 0; c < BN; c += kStep) {
+          float v[kStep];
+          mm_load<kStep>(acc + c, v);
+          mm_store<kStep>(args, (long long)tp * kMmP + row, (long long)tq * BN + c, v);
+        }
+      } else {
+        // this CTA's part goes to its shared memory (the stages are no longer in use), in an order in which
+        // neither these stores nor the reads below meet in a bank
+        float* red = reinterpret_cast<float*>(stages);
+#pragma unroll 1
+        for (int c = 0; c < BN; c += kStep) {
+          float v[kStep];
+          mm_load<kStep>(acc + c, v);
+#pragma unroll
+          for (int i = 0; i < kStep; ++i) red[args.swap ? (c + i) * kMmP + row : row * (BN + 1) + c + i] = k1 > k0 ? v[i] : 0.f;
+        }
+      }
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane == 0)
+        asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(mm_smem(&s_acc_empty[buf])) : "memory");
+    }
+    __syncwarp();
+  }
+
+  if (args.splits > 1) {
+    mm_cluster_sync();
+    int tp, tq;
+    mm_tile(args, first, &tp, &tq);
+    const int total = kMmP * BN, e0 = total / args.splits * rank, e1 = rank + 1 == args.splits ? total : e0 + total / args.splits;
+    for (int e = e0 + tid; e < e1; e += kMmThreads) {
+      const int row = args.swap ? e % kMmP : e / BN, col = args.swap ? e / kMmP : e % BN;
+      const unsigned int at = base + 4u * (unsigned)(args.swap ? col * kMmP + row : row * (BN + 1) + col);
+      float sum = 0.f;
+      for (int r = 0; r < args.splits; ++r) sum += mm_remote(at, (unsigned)r);
+      const long long p = (long long)tp * kMmP + row, q = (long long)tq * BN + col;
+      if (p < args.rows_p && q < args.rows_q) mm_store1(args, args.swap ? q : p, args.swap ? p : q, sum);
+    }
+    mm_cluster_sync();                                // nobody leaves while its shared memory is being read
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  if (warp == 1)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(Cfg::kAlloc) : "memory");
+}
+
+}  // namespace psb

@@ -1,0 +1,303 @@
+"""Microscaled 4-bit operands: quantisation both ways, the values read back, and the product with
+its gradients, against plain numpy in 64 bits.  Quantisation is defined to the bit, so it is compared
+for equality; the product's tolerance is derived from the number of additions."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2204_03211_b200 import binding as B
+
+MAGS = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+
+
+def mx_ref(x):
+    """The values a matrix takes on in the format, blocks of 32 along its rows, in 64 bits (NaN blocks as NaN)."""
+    x = np.asarray(x, dtype=np.float64)
+    R, Cc = x.shape
+    full = np.zeros((R, -(-Cc // 32) * 32))
+    full[:, :Cc] = x
+    out = np.empty_like(full)
+    for r in range(R):
+        for b in range(0, full.shape[1], 32):
+            v = full[r, b:b + 32]
+            if not np.isfinite(v).all():
+                out[r, b:b + 32] = np.nan
+                continue
+            top = np.abs(v).max()
+            e = max(int(np.frexp(top)[1]) - 3, -127) if top else -127
+            a = np.abs(v) / 2.0 ** e
+            d = np.abs(a[:, None] - MAGS[None])
+            code = np.empty(32, dtype=int)
+            for i in range(32):
+                best = np.flatnonzero(d[i] == d[i].min())              # two at a tie: the even code
+                code[i] = next((k for k in best if k % 2 == 0), best[0])
+            out[r, b:b + 32] = np.copysign(MAGS[code], v) * 2.0 ** e
+    return out[:, :Cc]
+
+
+def as64(t):
+    return t.detach().float().cpu().numpy().astype(np.float64)
+
+
+def same(got, ref):
+    return np.array_equal(np.isnan(got), np.isnan(ref)) and np.array_equal(got[~np.isnan(ref)], ref[~np.isnan(ref)])
+
+
+def quantized(x, transposed=False):
+    r, c = x.shape
+    q = B.MxTensor(c, r) if transposed else B.MxTensor(r, c)
+    B.ps_mx_quantize(x, None if transposed else q, q if transposed else None)
+    return q
+
+
+def values(q, dtype=torch.float32):
+    return B.ps_mx_dequantize(q, torch.empty(q.rows, q.cols, device="cuda", dtype=dtype))
+
+
+def tricky(rows, cols, dtype, seed):
+    """Values over many binades: whole blocks of zeros, subnormal and huge blocks, every tie of the format, signed
+    zeros, and blocks with an infinity or a NaN."""
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(rows, cols, generator=g) * torch.exp2(torch.randint(-30, 30, (rows, 1), generator=g).float())
+    ties = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0, 7.0, 7.75, -0.25, -0.75, -2.5, -5.0, 0.0, -0.0])
+    for r in range(rows):
+        k = r % 9
+        if k == 1:
+            x[r] = 0
+        elif k == 2:
+            x[r] = ties[torch.randint(0, 16, (cols,), generator=g)]
+            x[r, ::32] = 4.5
+        elif k == 3:
+            x[r] *= 2.0 ** -130
+        elif k == 4:
+            x[r] = torch.sign(x[r]) * 3e38
+        elif k == 5:
+            x[r, cols // 2] = float("inf")
+        elif k == 6:
+            x[r, -1] = float("nan")
+        elif k == 7:
+            x[r] = torch.exp2(torch.randint(-8, 3, (cols,), generator=g).float())
+    return x.to(dtype).cuda()
+
+
+SHAPES = [(1, 1), (1, 31), (1, 32), (3, 33), (9, 64), (18, 127), (33, 129), (129, 40), (130, 257), (64, 1000)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,cols", SHAPES)
+def test_quantize_both_ways(rows, cols, dtype):
+    x = tricky(rows, cols, dtype, rows * 1000 + cols)
+    ref, ref_t = mx_ref(as64(x)), mx_ref(as64(x).T)
+    q, qt = B.MxTensor(rows, cols), B.MxTensor(cols, rows)
+    for t in (q.codes, q.scales, qt.codes, qt.scales):
+        t.fill_(0xFF)                       # padding has to be written, not found
+    B.ps_mx_quantize(x, q, qt)
+    for out in (torch.float32, torch.bfloat16):
+        assert same(as64(values(q, out)), ref)
+        assert same(as64(values(qt, out)), ref_t)
+    assert same(as64(values(quantized(x))), ref)
+    assert same(as64(values(quantized(x, True))), ref_t)
+    one, one_t = quantized(x), quantized(x, True)
+    assert torch.equal(one.codes, q.codes) and torch.equal(one_t.codes, qt.codes)
+
+
+@pytest.mark.gpu
+def test_quantize_strides_alignment_and_streams():
+    base = torch.randn(70, 301, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for dtype in (torch.float32, torch.bfloat16):
+        b = base.to(dtype)
+        side.wait_stream(torch.cuda.current_stream())
+        for off, width in ((0, 300), (1, 300), (3, 40), (8, 128)):
+            x = b[:, off:off + width]                   # row stride 301: no vector loads
+            q, qt = B.MxTensor(70, width), B.MxTensor(width, 70)
+            wide = torch.full((70, width + 5), 7.0, device="cuda", dtype=dtype)
+            side.wait_stream(torch.cuda.current_stream())
+            B.ps_mx_quantize(x, q, qt, side)
+            B.ps_mx_dequantize(q, wide[:, :width], side)
+            side.synchronize()
+            assert same(as64(wide[:, :width]), mx_ref(as64(x)))
+            assert (wide[:, width:] == 7.0).all()
+            assert same(as64(values(qt)), mx_ref(as64(x).T))
+
+
+def check_product(M, N, K, dtype, seed=0, scale=True):
+    g = torch.Generator().manual_seed(seed)
+    a = torch.randn(M, K, generator=g)
+    b = torch.randn(N, K, generator=g)
+    if scale:                               # blocks of very different size: additions do round
+        a *= torch.exp2(torch.randint(-12, 12, (M, 1), generator=g).float())
+        a[:, : K // 2] *= 2.0 ** 11
+        b[:, K // 3:] *= 2.0 ** -7
+    a, b = a.cuda(), b.cuda()
+    qa, qb = quantized(a), quantized(b)
+    va, vb = as64(values(qa)), as64(values(qb))
+    wide = torch.full((M, N + 3), 5.0, device="cuda", dtype=dtype)
+    out = wide[:, :N] if M % 2 else torch.full((M, N), 5.0, device="cuda", dtype=dtype)
+    B.ps_mx_matmul(qa, qb, out)
+    got, ref = as64(out), va @ vb.T
+    # K products, exact; each addition may lose one unit in the last of 24 bits of a partial sum, which is at
+    # most the sum of the magnitudes; a bf16 result is rounded once more, to 8 bits
+    bound = K * 2.0 ** -23 * (np.abs(va) @ np.abs(vb).T)
+    if dtype is torch.bfloat16:
+        bound = bound * (1 + 2.0 ** -8) + np.abs(ref) * 2.0 ** -8
+    assert (np.abs(got - ref) <= bound).all(), np.max(np.abs(got - ref) - bound)
+    assert (wide[:, N:] == 5.0).all()
+    assert B.ps_mx_status() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("M,N,K", [
+    (1, 1, 1), (1, 128, 32), (1, 1000, 2050), (2, 129, 256), (7, 5, 100), (16, 640, 512), (17, 300, 4096),
+    (64, 1024, 257), (65, 65, 65), (300, 1, 512), (257, 20, 4000), (128, 128, 128), (127, 129, 385), (500, 700, 1500),
+    (129, 2500, 64), (2500, 257, 511),
+])
+def test_product(M, N, K, dtype):
+    check_product(M, N, K, dtype, M * 7 + N * 3 + K)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,N,K", [(4000, 2817, 300), (2305, 4100, 1024), (20000, 250, 96)])
+def test_product_of_many_tiles(M, N, K):
+    check_product(M, N, K, torch.bfloat16)
+
+
+@pytest.mark.gpu
+def test_product_is_repeatable_and_poisons_only_its_rows():
+    a, b = torch.randn(70, 900, device="cuda"), torch.randn(200, 900, device="cuda")
+    a[3, 40] = float("nan")
+    b[11, 899] = float("inf")
+    qa, qb = quantized(a), quantized(b)
+    first = B.ps_mx_matmul(qa, qb, torch.empty(70, 200, device="cuda"))
+    for _ in range(3):
+        again = B.ps_mx_matmul(qa, qb, torch.empty(70, 200, device="cuda"))
+        assert torch.equal(first.view(torch.int32), again.view(torch.int32))
+    bad = torch.zeros(70, 200, dtype=torch.bool, device="cuda")
+    bad[3] = True
+    bad[:, 11] = True
+    assert torch.equal(first.isnan(), bad)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,K,N", [(1, 32, 64), (40, 64, 96), (130, 300, 70)])
+def test_gradients_of_a_layer(T, K, N):
+    """dx = dy w and dw = dy^T x: against the formula on the operands' values, and against differences of
+    sum(dy * y), which are exact because every value involved is one the format holds."""
+    g = torch.Generator().manual_seed(T)
+    grid = torch.tensor([-4.0, -3.0, -1.5, -0.5, 0.0, 1.0, 2.0, 3.0, 4.0])
+    draw = lambda r, c: grid[torch.randint(0, 9, (r, c), generator=g)]  # noqa: E731
+    x, w, dy = draw(T, K), draw(N, K), draw(T, N)
+    for t in (x, w, dy):
+        t[::32, :] = 4.0                    # every block along either direction has the scale 1
+        t[:, ::32] = 4.0
+    x, w, dy = x.cuda(), w.cuda(), dy.cuda()
+    out = lambda r, c: torch.empty(r, c, device="cuda")  # noqa: E731
+    dx = as64(B.ps_mx_matmul(quantized(dy), quantized(w, True), out(T, K)))
+    dw = as64(B.ps_mx_matmul(quantized(dy, True), quantized(x, True), out(N, K)))
+    assert np.array_equal(dx, as64(dy) @ as64(w))           # integers times a quarter: exact in binary32
+    assert np.array_equal(dw, as64(dy).T @ as64(x))
+    loss = lambda xx, ww: (as64(dy) * as64(B.ps_mx_matmul(quantized(xx), quantized(ww), out(T, N)))).sum()  # noqa: E731
+    at = loss(x, w)
+    for i, j in ((T - 1, K - 1), (T // 2, K // 3)):
+        if i % 32 and j % 32:
+            xx = x.clone()
+            xx[i, j] = 2.0 if float(x[i, j]) != 2.0 else 3.0
+            assert (loss(xx, w) - at) / float(xx[i, j] - x[i, j]) == dx[i, j]
+    for i, j in ((N - 1, K - 1), (N // 2, K // 3)):
+        if i % 32 and j % 32:
+            ww = w.clone()
+            ww[i, j] = 2.0 if float(w[i, j]) != 2.0 else 3.0
+            assert (loss(x, ww) - at) / float(ww[i, j] - w[i, j]) == dw[i, j]
+
+
+@pytest.mark.gpu
+def test_empty_products_and_stream_order():
+    assert B.ps_mx_matmul(B.MxTensor(0, 64), quantized(torch.ones(5, 64, device="cuda")),
+                          torch.empty(0, 5, device="cuda")).shape == (0, 5)
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        x = torch.randn(512, 2048, device="cuda")
+        w = torch.randn(512, 2048, device="cuda")
+        q, qw, y = B.MxTensor(512, 2048), B.MxTensor(512, 2048), torch.empty(512, 512, device="cuda")
+        outs = []
+        for k in range(8):                  # operands are overwritten while earlier products are still queued
+            B.ps_mx_quantize(x + k, q, stream=s)
+            B.ps_mx_quantize(w, qw, stream=s)
+            outs.append(B.ps_mx_matmul(q, qw, y, s).clone())
+        s.synchronize()
+        for k in range(8):
+            ref = B.ps_mx_matmul(quantized_on(x + k, s), qw, torch.empty_like(y), s)
+            s.synchronize()
+            assert torch.equal(outs[k], ref)
+
+
+def quantized_on(x, s):
+    q = B.MxTensor(*x.shape)
+    B.ps_mx_quantize(x, q, stream=s)
+    return q
+
+
+# ---- refusals: before any device call, so they need no GPU ------------------------------------------------
+
+def raw(rows, cols, codes=1 << 20, scales=1 << 21):
+    return B.ps_mx(codes, scales, rows, cols)
+
+
+def test_sizes():
+    n, m = C.c_size_t(), C.c_size_t()
+    lib = B.load()
+    for rows, cols, codes, scales in ((1, 1, 16, 1024), (128, 256, 128 * 128, 1024), (129, 257, 129 * 144, 4096),
+                                      (0, 64, 0, 0)):
+        assert lib.ps_mx_sizes(rows, cols, C.byref(n), C.byref(m)) == B.PS_OK
+        assert (n.value, m.value) == (codes, scales)
+    for rows, cols in ((-1, 4), (4, 0), (1 << 31, 4), (4, 1 << 31)):
+        assert lib.ps_mx_sizes(rows, cols, C.byref(n), C.byref(m)) == B.PS_ERR_BAD_ARG
+
+
+def test_refusals():
+    lib = B.load()
+    ref = C.byref
+    q = lambda *a, **k: ref(raw(*a, **k))  # noqa: E731
+    x = 1 << 22
+    bad, align = B.PS_ERR_BAD_ARG, B.PS_ERR_ALIGN
+    quant = lambda *a: lib.ps_mx_quantize(*a, None)  # noqa: E731
+    assert quant(x, 7, 4, 64, 64, q(4, 64), None) == bad              # type
+    assert quant(x, B.PS_F32, 4, 64, 64, None, None) == bad           # nothing wanted
+    assert quant(x, B.PS_F32, -1, 64, 64, q(4, 64), None) == bad
+    assert quant(x, B.PS_F32, 4, 0, 64, q(4, 64), None) == bad
+    assert quant(x, B.PS_F32, 4, 64, 63, q(4, 64), None) == bad       # stride shorter than a row
+    assert quant(None, B.PS_F32, 4, 64, 64, q(4, 64), None) == bad
+    assert quant(x, B.PS_F32, 4, 64, 64, q(4, 65), None) == bad       # shapes
+    assert quant(x, B.PS_F32, 4, 64, 64, None, q(4, 64)) == bad       # the transpose has x's columns as rows
+    assert quant(x, B.PS_F32, 4, 64, 64, q(4, 64, codes=0), None) == bad
+    assert quant(x + 2, B.PS_F32, 4, 64, 64, q(4, 64), None) == align
+    assert quant(x + 1, B.PS_BF16, 4, 64, 64, q(4, 64), None) == align
+    assert quant(x, B.PS_F32, 4, 64, 64, q(4, 64, codes=(1 << 20) + 8), None) == align
+    assert quant(x, B.PS_F32, 4, 64, 64, q(4, 64, scales=(1 << 20) + 4), None) == align
+    assert quant(None, B.PS_F32, 0, 64, 64, q(0, 64), None) == B.PS_OK
+    deq = lambda *a: lib.ps_mx_dequantize(*a, None)  # noqa: E731
+    assert deq(None, B.PS_F32, x, 64) == bad
+    assert deq(q(4, 64), 9, x, 64) == bad
+    assert deq(q(4, 64), B.PS_F32, x, 63) == bad
+    assert deq(q(4, 64), B.PS_F32, None, 64) == bad
+    assert deq(q(4, 64), B.PS_F32, x + 2, 64) == align
+    assert deq(q(0, 64), B.PS_F32, None, 64) == B.PS_OK
+    mul = lambda *a: lib.ps_mx_matmul(*a, None)  # noqa: E731
+    assert mul(q(4, 64), q(5, 96), B.PS_F32, x, 5) == bad             # contraction lengths
+    assert mul(q(4, 64), q(5, 64), B.PS_F32, x, 4) == bad             # stride shorter than a row
+    assert mul(q(4, 64), q(5, 64), 3, x, 5) == bad
+    assert mul(q(4, 64), None, B.PS_F32, x, 5) == bad
+    assert mul(q(4, 64), q(5, 64), B.PS_F32, None, 5) == bad
+    assert mul(q(4, 64), q(5, 64), B.PS_F32, x + 2, 5) == align
+    assert mul(q(0, 64), q(5, 64), B.PS_F32, None, 5) == B.PS_OK
+    assert lib.ps_mx_status(None) == bad
+
+
+def test_binding_refuses_wrong_tensors():
+    with pytest.raises(B.PsError):
+        B.ps_mx_quantize(torch.zeros(4, 64), B.MxTensor(4, 64, device="cpu"))
