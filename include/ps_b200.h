@@ -330,6 +330,35 @@ int ps_round_prepare(ps_service* svc, int n_push, const int* jobs, const int* bl
 int ps_round_run(ps_service* svc, int round, void* stream, const float** params_dev_ptrs_out);
 int ps_round_release(ps_service* svc, int round);
 
+/* Aggregation with the gradients clipped by their global norm.  (The paper trains
+ * with whatever optimizer the job brings; the transformer and LSTM jobs it and its
+ * successors co-locate are trained with clipped gradients, and the norm has to be
+ * taken over the sums, which only the service sees.)  As ps_aggregate, but for every
+ * job in `ready` (up to 64)
+ *     n = sqrt(sum of G*G over all listed blocks of the job)    summed in binary64
+ *     G = G * c,  c = min(1, max_norm / (n + 1e-6))             binary32
+ * before the optimizer step; G is the sum of the shards times grad_scale.  With
+ * c = 1 parameters and state get the same bits as from ps_aggregate.  A NaN among
+ * the gradients makes c NaN, an infinity makes it 0 (and 0 * infinity a NaN).
+ * max_norm > 0; +infinity asks for the norm alone.  norms_dev_out (device, may be
+ * NULL) receives one float per job in the order in which `ready` names them first.
+ * ps_block_stats reports the squared norm before clipping.  List a job's blocks in
+ * ONE call: each call takes its own norm.
+ * One cooperative launch on `stream` itself, also with PS_OPT_OVERLAP (rounds held
+ * back by PS_OPT_BATCH go out before it); PS_OPT_KERNEL and PS_OPT_PROFILE do not
+ * apply.  The first call, and one that lists more elements than any before, allocate
+ * 4 bytes of device memory per listed element and wait for the device.
+ * Errors: those of ps_aggregate; BAD_ARG (max_norm not above 0, norms_dev_out not
+ * aligned to 4 bytes), TOO_LARGE (more than 64 jobs). */
+int ps_aggregate_clipped(ps_service* svc, const ps_task* ready, int n_ready, float max_norm, float* norms_dev_out,
+                         void* stream);
+
+/* A run of a prepared round whose aggregate is ps_aggregate_clipped.  Runs with and
+ * without clipping of one round may alternate.  (A round prepared with
+ * PS_ROUND_INPUTS_COMPLETE is ordered after `stream` here, as without the flag.) */
+int ps_round_run_clipped(ps_service* svc, int round, float max_norm, float* norms_dev_out, void* stream,
+                         const float** params_dev_ptrs_out);
+
 /* Per-block statistics of the last aggregate (paper Section 3.1: profilers feed
  * the manager): squared norm of the aggregated gradient and the step counter.
  * Waits for the block's last aggregate to finish.  Either out pointer may be
@@ -391,7 +420,8 @@ int ps_launch_info(ps_service* svc, unsigned long long* launches_out, int* grid_
                    const char** kernel_name_out);
 
 /* Launch accounting per kernel variant (0 = persistent direct-load kernel,
- * 1 = small-launch kernel with the table in its parameters, 2 = bulk-copy ring):
+ * 1 = small-launch kernel with the table in its parameters, 2 = bulk-copy ring,
+ * 3 = clipped aggregates):
  * launches so far, the algorithmic bytes they covered (W shards read, parameters
  * and state read and written, dense semantics) and the kernel's name.
  * Errors: BAD_ARG (variant out of range). */
@@ -645,6 +675,39 @@ int ps_mx_matmul(const ps_mx* a, const ps_mx* b, int dtype, void* c, long long l
  * fault; non-zero = a bounded wait inside a kernel expired (that launch's results
  * are undefined). */
 int ps_mx_status(int* status_out);
+
+/* ---------------------------------------------------------------------------
+ * Global gradient norm over many tensors and clipping on the worker's side: a
+ * worker that clips its own gradient before it pushes it, or whose training
+ * framework wants the norm.
+ *     n = sqrt(sum over all tensors of x*x),  dst = src * min(1, max_norm / (n + 1e-6))
+ * No ps_service is involved.  A ps_clip remembers a list of tensors; the list of a
+ * training job does not change from step to step.
+ * ------------------------------------------------------------------------- */
+typedef struct ps_clip ps_clip; /* opaque */
+
+/* Remembers n tensors (host arrays of device pointers and element counts, copied):
+ * source i of src_dtype is written to destination i of dst_dtype, e.g. fp32
+ * gradients into a bf16 push buffer.  dsts[i] == srcs[i] clips in place (same dtype
+ * only); otherwise no destination may overlap a source.  Tensors that are 16-byte
+ * aligned on both sides take 128-bit accesses.  Empty tensors are allowed.
+ * Allocates a small table on `device`.  Errors: BAD_ARG, ALIGN, NOMEM, CUDA. */
+int ps_clip_create(ps_clip** out, int device, int n, const void* const* srcs, int src_dtype, void* const* dsts,
+                   int dst_dtype, const size_t* nelems);
+
+/* One cooperative launch on `stream`.  max_norm > 0; +infinity means factor 1 (the
+ * norm, and the copy where destinations are their own).  norm_dev_out (device
+ * float) may be NULL.  A factor of exactly 1 leaves tensors clipped in place
+ * untouched.  Non-finite norms: as for ps_aggregate_clipped.  Runs of one ps_clip
+ * must not overlap on the GPU: use one stream, or order the streams.
+ * Errors: BAD_HANDLE, BAD_ARG, ALIGN, CUDA. */
+int ps_clip_run(ps_clip* clip, float max_norm, float* norm_dev_out, void* stream);
+
+/* Waits for the device; non-zero: a bounded wait inside a run expired. */
+int ps_clip_status(ps_clip* clip, int* status_out);
+
+/* Frees the table; waits for runs that still use it. */
+int ps_clip_destroy(ps_clip* clip);
 
 /* Text of the last CUDA error of a ps_mx_* or ps_clip_* call on this host thread. */
 const char* ps_op_last_error(void);

@@ -138,6 +138,13 @@ _SIGNATURES = {
     "ps_peer_event_wait": (C.c_int, [C.c_void_p, C.c_void_p]),
     "ps_peer_event_destroy": (C.c_int, [C.c_void_p]),
     "ps_peer_copy_many": (C.c_int, [C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "ps_aggregate_clipped": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_float, C.c_void_p, C.c_void_p]),
+    "ps_round_run_clipped": (C.c_int, [C.c_void_p, C.c_int, C.c_float, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "ps_clip_create": (C.c_int, [C.POINTER(C.c_void_p), C.c_int, C.c_int, C.c_void_p, C.c_int, C.c_void_p, C.c_int,
+                                 C.c_void_p]),
+    "ps_clip_run": (C.c_int, [C.c_void_p, C.c_float, C.c_void_p, C.c_void_p]),
+    "ps_clip_status": (C.c_int, [C.c_void_p, C.POINTER(C.c_int)]),
+    "ps_clip_destroy": (C.c_int, [C.c_void_p]),
     "ps_mx_sizes": (C.c_int, [C.c_longlong, C.c_longlong, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]),
     "ps_mx_quantize": (C.c_int, [C.c_void_p, C.c_int, C.c_longlong, C.c_longlong, C.c_longlong, C.c_void_p, C.c_void_p,
                                  C.c_void_p]),
@@ -309,10 +316,25 @@ def ps_round_release(svc, round_id: int):
     _check(load().ps_round_release(svc, round_id), "ps_round_release", svc)
 
 
-def ps_launch_stats(svc):
-    """[{kernel, launches, bytes}] per kernel variant."""
+def ps_aggregate_clipped(svc, ready, max_norm: float, norms_out=None, stream=None):
+    """ps_aggregate with every listed job's gradients clipped by their global
+    norm; norms_out: optional float32 device tensor, one entry per job."""
+    tasks = ready if isinstance(ready, C.Array) else make_tasks(list(ready))
+    _check(load().ps_aggregate_clipped(svc, tasks, len(tasks), max_norm, _ptr(norms_out), _stream_ptr(stream)),
+           "ps_aggregate_clipped", svc)
+
+
+def ps_round_run_clipped(svc, round_id: int, max_norm: float, norms_out=None, stream=None, out=None):
+    """ps_round_run with the gradients clipped as by ps_aggregate_clipped."""
+    _check(load().ps_round_run_clipped(svc, round_id, max_norm, _ptr(norms_out), _stream_ptr(stream), _ptr(out)),
+           "ps_round_run_clipped", svc)
+    return out
+
+
+def ps_launch_stats(svc, variants: int = 3):
+    """[{kernel, launches, bytes}] per kernel variant (the fourth: clipped aggregates)."""
     res = []
-    for v in range(3):
+    for v in range(variants):
         n, b, name = C.c_ulonglong(), C.c_ulonglong(), C.c_char_p()
         _check(load().ps_launch_stats(svc, v, C.byref(n), C.byref(b), C.byref(name)), "ps_launch_stats", svc)
         res.append(dict(kernel=(name.value or b"").decode(), launches=n.value, bytes=b.value))
@@ -528,13 +550,15 @@ class Service:
 
     def view(self, ptr: int, nelem: int, device: int | None = None):
         """fp32 torch view of `nelem` elements of service-owned device memory
-        (for reading results in tests; no copy)."""
+        (for reading results; no copy).  The view keeps this Service object, and
+        with it the memory, alive; close() invalidates it."""
         import torch
 
         class _Mem:
             pass
 
         m = _Mem()
+        m.service = self
         m.__cuda_array_interface__ = {"shape": (nelem,), "typestr": "<f4", "data": (ptr, False), "version": 2}
         return torch.as_tensor(m, device="cuda" if device is None else "cuda:%d" % device)
 
@@ -656,6 +680,52 @@ def _matrix(t, where: str):
     return t.data_ptr(), _dtype(t, where), max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
 
 
+class Clip:
+    """A list of device tensors whose gradients are clipped together: sources
+    and, unless they are clipped in place, destinations (float32 or bfloat16,
+    contiguous, one type per side)."""
+
+    def __init__(self, srcs, dsts=None, device: int | None = None):
+        where = "ps_clip_create"
+        self.srcs, self.dsts = list(srcs), list(srcs if dsts is None else dsts)     # kept alive with the handle
+        if [t.numel() for t in self.srcs] != [t.numel() for t in self.dsts]:
+            raise PsError(PS_ERR_BAD_ARG, where, "sources and destinations differ in number or size")
+        for t in self.srcs + self.dsts:
+            if not t.is_cuda or not t.is_contiguous():
+                raise PsError(PS_ERR_BAD_ARG, where, "contiguous CUDA tensors are wanted")
+        types = [{_dtype(t, where) for t in ts} for ts in (self.srcs, self.dsts)]
+        if any(len(t) > 1 for t in types):
+            raise PsError(PS_ERR_BAD_ARG, where, "one dtype per side is wanted")
+        if device is None:
+            device = self.srcs[0].device.index if self.srcs else 0
+        n = len(self.srcs)
+        src, dst = ((C.c_void_p * n)(*[t.data_ptr() for t in ts]) for ts in (self.srcs, self.dsts))
+        h = C.c_void_p()
+        _check_op(load().ps_clip_create(C.byref(h), device, n, src, types[0].pop() if n else PS_F32, dst,
+                                        types[1].pop() if n else PS_F32,
+                                        (C.c_size_t * n)(*[t.numel() for t in self.srcs])), where)
+        self.handle = h.value
+
+    def run(self, max_norm: float, norm_out=None, stream=None):
+        _check_op(load().ps_clip_run(self.handle, max_norm, _ptr(norm_out), _stream_ptr(stream)), "ps_clip_run")
+
+    def status(self) -> int:
+        v = C.c_int()
+        _check_op(load().ps_clip_status(self.handle, C.byref(v)), "ps_clip_status")
+        return v.value
+
+    def close(self):
+        if getattr(self, "handle", None):
+            load().ps_clip_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
 class MxTensor:
     """A microscaled 4-bit operand of rows x cols elements and the two device
     buffers that hold it (`codes` and `scales`, uint8, in the library's layout)."""
@@ -725,7 +795,7 @@ def _bind(name):
     return method
 
 
-for _n in ("flush", "round", "round_prepare", "round_run", "round_release", "launch_stats", "registry_info", "register_job", "register_block", "push", "push_rows", "push_rows_batch", "push_batch", "push_host", "push_host_batch", "aggregate", "join", "pull", "pull_batch", "pull_host",
+for _n in ("flush", "round", "round_prepare", "round_run", "round_release", "round_run_clipped", "aggregate_clipped", "launch_stats", "registry_info", "register_job", "register_block", "push", "push_rows", "push_rows_batch", "push_batch", "push_host", "push_host_batch", "aggregate", "join", "pull", "pull_batch", "pull_host",
            "migrate_block", "migrate_blocks", "block_stats", "block_profile", "job_profile", "block_state", "plan", "set_option", "get_option", "arena_info",
            "launch_info", "device_status", "block_export", "block_import", "unregister_block", "arena_export", "block_location"):
     setattr(Service, _n, _bind(_n))

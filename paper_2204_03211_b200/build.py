@@ -16,7 +16,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libps_b200.so")
 SOURCES = [os.path.join(CSRC, "ps_service.cu"), os.path.join(CSRC, "ps_planner.cpp"), os.path.join(CSRC, "ps_peer.cpp"),
-           os.path.join(CSRC, "ps_mx.cu")]
+           os.path.join(CSRC, "ps_mx.cu"), os.path.join(CSRC, "ps_clip.cu")]
 
 
 def _deps():

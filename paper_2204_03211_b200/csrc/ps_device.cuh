@@ -6,4 +6,5 @@
 #include "ps_kernel_ldg.cuh"
 #include "ps_kernel_inline.cuh"
 #include "ps_kernel_bulk.cuh"
+#include "ps_kernel_clip.cuh"
 #include "ps_migrate.cuh"

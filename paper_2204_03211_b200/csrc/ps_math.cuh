@@ -12,10 +12,12 @@ struct Hp {
   float lr, mom, wd, b1, b2, omb1, omb2, eps, gs, ss_t, sbc2_t;
 };
 
+// OPT of a chunk body that only sums: "p" receives the scaled gradient, there is no state.
+constexpr int kSumOnly = 2;
+
+// The optimizer's step for a scaled gradient.
 template <int OPT>
-__device__ __forceinline__ void update_elem(const Hp& h, float G, float& p, float& s0, float& s1, double& sq) {
-  G = __fmul_rn(G, h.gs);
-  sq = fma((double)G, (double)G, sq);      // binary64: product exact, sum rounded once
+__device__ __forceinline__ void apply_elem(const Hp& h, float G, float& p, float& s0, float& s1) {
   const float d = __fadd_rn(G, __fmul_rn(h.wd, p));
   if (OPT == 0) {
     const float v = __fadd_rn(__fmul_rn(h.mom, s0), d);
@@ -29,6 +31,14 @@ __device__ __forceinline__ void update_elem(const Hp& h, float G, float& p, floa
     s1 = v;
     p = __fsub_rn(p, __fmul_rn(h.ss_t, __fdiv_rn(m, den)));
   }
+}
+
+template <int OPT>
+__device__ __forceinline__ void update_elem(const Hp& h, float G, float& p, float& s0, float& s1, double& sq) {
+  G = __fmul_rn(G, h.gs);
+  sq = fma((double)G, (double)G, sq);      // binary64: product exact, sum rounded once
+  if constexpr (OPT == kSumOnly) p = G;
+  else apply_elem<OPT>(h, G, p, s0, s1);
 }
 
 __device__ __forceinline__ float bf16_lo(unsigned int u) { return __uint_as_float(u << 16); }
@@ -85,7 +95,7 @@ __device__ __forceinline__ void update4(const Hp& h, const float4& G, float* p, 
   update_elem<OPT>(h, G.z, P.z, A.z, B.z, sq);
   update_elem<OPT>(h, G.w, P.w, A.w, B.w, sq);
   *reinterpret_cast<float4*>(p + e) = P;
-  *reinterpret_cast<float4*>(s0 + e) = A;
+  if (OPT != kSumOnly) *reinterpret_cast<float4*>(s0 + e) = A;
   if (OPT == 1) *reinterpret_cast<float4*>(s1 + e) = B;
 }
 
@@ -120,8 +130,8 @@ __device__ __forceinline__ void chunk_f32_vec(unsigned int tid, const Hp& h, con
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const size_t e = begin + 4 * (size_t)(i + u * NT);
-      pv[u] = *reinterpret_cast<const float4*>(p + e);
-      av[u] = *reinterpret_cast<const float4*>(s0 + e);
+      pv[u] = OPT != kSumOnly ? *reinterpret_cast<const float4*>(p + e) : make_float4(0, 0, 0, 0);
+      av[u] = OPT != kSumOnly ? *reinterpret_cast<const float4*>(s0 + e) : make_float4(0, 0, 0, 0);
       if (OPT == 1) bv[u] = *reinterpret_cast<const float4*>(s1 + e); else bv[u] = make_float4(0, 0, 0, 0);
     }
     if (pf_lane) {
@@ -130,8 +140,8 @@ __device__ __forceinline__ void chunk_f32_vec(unsigned int tid, const Hp& h, con
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           const size_t e = begin + 4 * (size_t)(i + (U + u) * NT);
-          prefetch_l2(p + e);
-          prefetch_l2(s0 + e);
+          if (OPT != kSumOnly) prefetch_l2(p + e);
+          if (OPT != kSumOnly) prefetch_l2(s0 + e);
           if (OPT == 1) prefetch_l2(s1 + e);
         }
         for (int w = 0; w <= kAheadF32 && w < W; ++w) {
@@ -172,9 +182,10 @@ __device__ __forceinline__ void chunk_f32_vec(unsigned int tid, const Hp& h, con
   // remaining groups, one per thread
   for (; i < nvec; i += NT) {
     const size_t e = begin + 4 * (size_t)i;
-    const float4 pv = *reinterpret_cast<const float4*>(p + e);
-    const float4 av = *reinterpret_cast<const float4*>(s0 + e);
-    const float4 bv = (OPT == 1) ? *reinterpret_cast<const float4*>(s1 + e) : make_float4(0, 0, 0, 0);
+    const float4 zero = make_float4(0, 0, 0, 0);
+    const float4 pv = OPT != kSumOnly ? *reinterpret_cast<const float4*>(p + e) : zero;
+    const float4 av = OPT != kSumOnly ? *reinterpret_cast<const float4*>(s0 + e) : zero;
+    const float4 bv = (OPT == 1) ? *reinterpret_cast<const float4*>(s1 + e) : zero;
     float4 acc = as_f4(ld_stream(static_cast<const float*>(ld_ptr(shards)) + e));
 #pragma unroll 4
     for (int w = 1; w < W; ++w) acc = add4(acc, ld_stream(static_cast<const float*>(ld_ptr(shards, w)) + e));
@@ -193,7 +204,7 @@ __device__ __forceinline__ void chunk_bf16_vec(unsigned int tid, const Hp& h, co
   const bool pf_lane = (tid & 7) == 0;      // shards: 8 lanes x 16 bytes = one line
   for (unsigned int i = tid; i < nvec; i += NT) {
     const size_t e = begin + 8 * (size_t)i;
-    if ((tid & 3) == 0) {                   // parameters and state: 4 lanes x 32 bytes = one line
+    if (OPT != kSumOnly && (tid & 3) == 0) {   // parameters and state: 4 lanes x 32 bytes = one line
       prefetch_l2(p + e);
       prefetch_l2(s0 + e);
       if (OPT == 1) prefetch_l2(s1 + e);
@@ -213,9 +224,13 @@ __device__ __forceinline__ void chunk_bf16_vec(unsigned int tid, const Hp& h, co
       add_bf16x2(acc[4], acc[5], t.z);
       add_bf16x2(acc[6], acc[7], t.w);
     }
-    const float4 p0 = *reinterpret_cast<const float4*>(p + e), p1 = *reinterpret_cast<const float4*>(p + e + 4);
-    const float4 a0 = *reinterpret_cast<const float4*>(s0 + e), a1 = *reinterpret_cast<const float4*>(s0 + e + 4);
-    float4 b0 = make_float4(0, 0, 0, 0), b1 = b0;
+    float4 p0 = make_float4(0, 0, 0, 0), p1 = p0, a0 = p0, a1 = p0, b0 = p0, b1 = p0;
+    if (OPT != kSumOnly) {
+      p0 = *reinterpret_cast<const float4*>(p + e);
+      p1 = *reinterpret_cast<const float4*>(p + e + 4);
+      a0 = *reinterpret_cast<const float4*>(s0 + e);
+      a1 = *reinterpret_cast<const float4*>(s0 + e + 4);
+    }
     if (OPT == 1) {
       b0 = *reinterpret_cast<const float4*>(s1 + e);
       b1 = *reinterpret_cast<const float4*>(s1 + e + 4);
@@ -242,10 +257,10 @@ __device__ __forceinline__ void chunk_scalar(unsigned int tid, const Hp& h, cons
       G = __ldcs(static_cast<const float*>(ld_ptr(shards)) + e);
       for (int w = 1; w < W; ++w) G = __fadd_rn(G, __ldcs(static_cast<const float*>(ld_ptr(shards, w)) + e));
     }
-    float P = p[e], A = s0[e], B = (OPT == 1) ? s1[e] : 0.f;
+    float P = OPT != kSumOnly ? p[e] : 0.f, A = OPT != kSumOnly ? s0[e] : 0.f, B = (OPT == 1) ? s1[e] : 0.f;
     update_elem<OPT>(h, G, P, A, B, sq);
     p[e] = P;
-    s0[e] = A;
+    if (OPT != kSumOnly) s0[e] = A;
     if (OPT == 1) s1[e] = B;
   }
 }

@@ -83,8 +83,9 @@ __device__ __forceinline__ void chunk_rows(unsigned int tid, const Hp& h, const 
           acc.x = __fadd_rn(acc.x, 0.f); acc.y = __fadd_rn(acc.y, 0.f);
           acc.z = __fadd_rn(acc.z, 0.f); acc.w = __fadd_rn(acc.w, 0.f);
         }
-        const float4 pv = *reinterpret_cast<const float4*>(p + e);
-        const float4 av = *reinterpret_cast<const float4*>(s0 + e);
+        const float4 z = make_float4(0, 0, 0, 0);
+        const float4 pv = OPT != kSumOnly ? *reinterpret_cast<const float4*>(p + e) : z;
+        const float4 av = OPT != kSumOnly ? *reinterpret_cast<const float4*>(s0 + e) : z;
         const float4 bv = (OPT == 1) ? *reinterpret_cast<const float4*>(s1 + e) : make_float4(0, 0, 0, 0);
         update4<OPT>(h, acc, p, s0, s1, e, pv, av, bv, sq);
       } else {
@@ -104,8 +105,10 @@ __device__ __forceinline__ void chunk_rows(unsigned int tid, const Hp& h, const 
           for (int q = 0; q < 8; ++q) acc[q] = __fadd_rn(acc[q], 0.f);
         }
         const float4 z = make_float4(0, 0, 0, 0);
-        const float4 p0 = *reinterpret_cast<const float4*>(p + e), p1 = *reinterpret_cast<const float4*>(p + e + 4);
-        const float4 a0 = *reinterpret_cast<const float4*>(s0 + e), a1 = *reinterpret_cast<const float4*>(s0 + e + 4);
+        const float4 p0 = OPT != kSumOnly ? *reinterpret_cast<const float4*>(p + e) : z;
+        const float4 p1 = OPT != kSumOnly ? *reinterpret_cast<const float4*>(p + e + 4) : z;
+        const float4 a0 = OPT != kSumOnly ? *reinterpret_cast<const float4*>(s0 + e) : z;
+        const float4 a1 = OPT != kSumOnly ? *reinterpret_cast<const float4*>(s0 + e + 4) : z;
         const float4 b0 = (OPT == 1) ? *reinterpret_cast<const float4*>(s1 + e) : z;
         const float4 b1 = (OPT == 1) ? *reinterpret_cast<const float4*>(s1 + e + 4) : z;
         update4<OPT>(h, make_float4(acc[0], acc[1], acc[2], acc[3]), p, s0, s1, e, p0, a0, b0, sq);

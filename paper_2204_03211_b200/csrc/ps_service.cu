@@ -117,9 +117,10 @@ struct Plan {                              // one built task table (host copy)
   unsigned int total_chunks = 0, chunk_elems = 0;
   bool has_sparse = false;                 // some task carries row-sparse shards (direct-load kernel only)
   unsigned long long algo_bytes = 0;       // algorithmic bytes of the launch (dense semantics)
+  size_t spool = 0;                        // clipped launches: elements of the buffer of kept sums
 };
 
-enum { kVarLdg = 0, kVarInline = 1, kVarBulk = 2, kVariants = 3 };
+enum { kVarLdg = 0, kVarInline = 1, kVarBulk = 2, kVarClip = 3, kVariants = 4 };
 
 // A round that recurs every iteration (ps_round_prepare): the caller's lists, what
 // they resolve to, and the packed task table of the last run.
@@ -135,6 +136,14 @@ struct Prepared {
   bool self_contained = false;             // the pushes are exactly the W shards of every ready block
   bool plan_ok = false;                    // `plan` can be reused after patching the step fields
   Plan plan;
+  bool clip_ok = false;                    // the same for the table of clipped runs
+  Plan clip_plan;
+};
+
+// What a clipped aggregate adds to an aggregate.
+struct ClipCall {
+  float max_norm;
+  float* norms_out;                        // device, one float per job of the ready list, or nullptr
 };
 
 }  // namespace psb
@@ -196,6 +205,14 @@ struct ps_service {
   bool mig_large_ok = true;                // the 28 KB kernel-parameter form of the migration kernel is accepted
   unsigned long long epoch = 0;            // bumped by whatever can invalidate a prepared round's table:
                                            // migration, import, unregistration, options
+  // clipped aggregates: the kept sums, the grid barrier, and the end of the last such launch (the next one uses the
+  // same buffer and barrier, on whatever stream)
+  float* clip_spool = nullptr;
+  size_t clip_spool_cap = 0;
+  GridBarrier* clip_bar = nullptr;
+  cudaEvent_t clip_done = nullptr;
+  bool clip_recorded = false;
+  int clip_ctas = 0;                       // CTAs of the clip kernels an SM holds
   int last_grid = 0, last_block = 0;
   const char* last_kernel = "none";
   std::string cuda_err;
@@ -650,6 +667,22 @@ int push_checked(ps_service* s, int job, int block, int worker, const void* ptr,
   return PS_OK;
 }
 
+// The launch in `slot` has taken the pushes of the blocks `idx`.
+void consume_pushes(ps_service* s, const std::vector<int>& idx, int slot, unsigned long long gen) {
+  for (int bi : idx) {
+    Block& b = s->blocks[bi];
+    b.step++;
+    std::fill(b.pushed.begin(), b.pushed.end(), nullptr);
+    std::fill(b.row_ids.begin(), b.row_ids.end(), nullptr);
+    std::fill(b.row_cnt.begin(), b.row_cnt.end(), 0u);
+    b.row_len = 0;
+    b.nsparse = 0;
+    b.npushed = 0;
+    b.last_slot = slot;
+    b.last_slot_gen = gen;
+  }
+}
+
 // Launches one aggregation kernel with an optional programmatic-serialization attribute.
 template <typename... KArgs, typename... Args>
 cudaError_t launch_kernel(void (*kernel)(KArgs...), int grid, int block, size_t smem, cudaStream_t stream,
@@ -754,6 +787,9 @@ int ps_destroy(ps_service* s) {
     if (s->status_dev) cudaFree(s->status_dev);
     if (s->exit_ctrs) cudaFree(s->exit_ctrs);
     if (s->done_host) cudaFreeHost(const_cast<unsigned long long*>(s->done_host));
+    if (s->clip_spool) cudaFree(s->clip_spool);
+    if (s->clip_bar) cudaFree(s->clip_bar);
+    if (s->clip_done) cudaEventDestroy(s->clip_done);
     if (s->copy_stream) cudaStreamDestroy(s->copy_stream);
     for (auto ws : s->work_streams) if (ws) cudaStreamDestroy(ws);
   }
@@ -1176,18 +1212,7 @@ static int launch_plan(ps_service* s, const std::vector<int>& idx, Plan& plan, c
   s->last_grid = grid;
   s->last_block = bulk ? kBulkThreads : kThreads;
   s->last_kernel = inl ? "inline" : bulk ? "bulk" : "ldg";
-  for (int bi : idx) {
-    Block& b = s->blocks[bi];
-    b.step++;
-    std::fill(b.pushed.begin(), b.pushed.end(), nullptr);
-    std::fill(b.row_ids.begin(), b.row_ids.end(), nullptr);
-    std::fill(b.row_cnt.begin(), b.row_cnt.end(), 0u);
-    b.row_len = 0;
-    b.nsparse = 0;
-    b.npushed = 0;
-    b.last_slot = slot_index;
-    b.last_slot_gen = sl->gen;
-  }
+  consume_pushes(s, idx, slot_index, sl->gen);
   return PS_OK;
 }
 
@@ -1243,6 +1268,209 @@ int launch_in_parts(ps_service* s, const std::vector<int>& idx, int parts) {
     if (rc) return rc;
   }
   return PS_OK;
+}
+
+// Builds the table of a clipped launch of the validated blocks `idx`: tasks in the caller's order, each with its cost
+// and its place in the buffer of kept sums.
+int build_clip_plan(ps_service* s, const std::vector<int>& idx, Plan* plan) {
+  const size_t n = idx.size();
+  plan->order = idx;
+  size_t nptr = 0, nsp = 0;
+  for (int bi : idx) {
+    const size_t W = (size_t)s->jobs[s->blocks[bi].job].d.num_workers;
+    nptr += W;
+    if (s->blocks[bi].nsparse) nsp += W;
+  }
+  const size_t tasks_off = sizeof(PsClipHdr);
+  const size_t costs_off = tasks_off + n * sizeof(PsTaskDev);
+  const size_t ptrs_off = costs_off + n * sizeof(PsClipCost);
+  const size_t sparse_off = (ptrs_off + nptr * sizeof(void*) + 15) / 16 * 16;
+  plan->bytes.assign(sparse_off + nsp * sizeof(PsSparseDev), 0);
+  plan->has_sparse = nsp > 0;
+  unsigned char* base = plan->bytes.data();
+  PsTaskDev* tasks = reinterpret_cast<PsTaskDev*>(base + tasks_off);
+  PsClipCost* costs = reinterpret_cast<PsClipCost*>(base + costs_off);
+  const void** ptrs = reinterpret_cast<const void**>(base + ptrs_off);
+  PsSparseDev* sp = reinterpret_cast<PsSparseDev*>(base + sparse_off);
+  std::vector<int> job_ids;                // in order of first appearance
+  unsigned long long cost = 0, spool = 0, units = 0;
+  size_t row = 0, sp_row = 0;
+  plan->algo_bytes = 0;
+  for (size_t i = 0; i < n; ++i) {
+    const Block& b = s->blocks[idx[i]];
+    const Job& j = s->jobs[b.job];
+    const int W = j.d.num_workers;
+    PsTaskDev& t = tasks[i];
+    t.p = blk_p(s, b);
+    t.s0 = blk_s0(s, b);
+    t.s1 = blk_s1(s, b);
+    t.nelem = b.nelem;
+    t.shard_row = (unsigned int)row;
+    t.t_first = ~0ull;
+    set_step_fields(j, b, &t);
+    t.job = b.job;
+    t.stat_idx = b.stat_idx;
+    t.vec_ok = 1;
+    for (int w = 0; w < W; ++w) {
+      ptrs[row + w] = b.pushed[w];
+      if (reinterpret_cast<uintptr_t>(b.pushed[w]) & 15u) t.vec_ok = 0;
+    }
+    unsigned int unit = kClipUnit;
+    if (b.nsparse) {
+      t.row_len = b.row_len;
+      t.sparse_row = (unsigned int)sp_row;
+      for (int w = 0; w < W; ++w) {
+        sp[sp_row + w].ids = b.row_ids[w];
+        sp[sp_row + w].n = b.row_cnt[w];
+      }
+      sp_row += W;
+      unit = std::max(1u, kClipUnit / b.row_len) * b.row_len;
+    }
+    const unsigned long long nunits = (b.nelem + unit - 1) / unit;
+    if (unit > (1u << 24) || nunits > 0xffffffffull) return PS_ERR_TOO_LARGE;
+    size_t slot = std::find(job_ids.begin(), job_ids.end(), b.job) - job_ids.begin();
+    if (slot == job_ids.size()) job_ids.push_back(b.job);
+    PsClipCost& k = costs[i];
+    k.start = cost;
+    k.unit = unit * (unsigned int)(bytes_per_elem(j) + 8);       // sums are written and read once
+    k.unit_elems = unit;
+    k.units = (unsigned int)nunits;
+    k.job_slot = (unsigned int)slot;
+    k.spool = spool;
+    cost += nunits * k.unit + kClipTaskCost;
+    spool += (b.nelem + 63) / 64 * 64;
+    units += nunits;
+    row += W;
+    plan->algo_bytes += b.nelem * bytes_per_elem(j);
+  }
+  if (job_ids.size() > (size_t)kClipMaxJobs) return PS_ERR_TOO_LARGE;
+  PsClipHdr* h = reinterpret_cast<PsClipHdr*>(base);
+  h->n_tasks = (unsigned int)n;
+  h->n_jobs = (unsigned int)job_ids.size();
+  h->tasks_off = (unsigned int)tasks_off;
+  h->costs_off = (unsigned int)costs_off;
+  h->ptrs_off = (unsigned int)ptrs_off;
+  h->sparse_off = (unsigned int)sparse_off;
+  h->cache_elems = kClipCache;
+  h->total_cost = cost;
+  plan->total_chunks = (unsigned int)std::min<unsigned long long>(units, 0xffffffffull);
+  plan->spool = spool;
+  return PS_OK;
+}
+
+// Device memory and launch limits of the clipped kernels, at the first such call and when the buffer has to grow.
+int ensure_clip(ps_service* s, size_t spool_elems) {
+  if (!s->clip_done) {
+    constexpr int kSmem = (int)(kClipCache * sizeof(float));
+    int a = 0, b = 0;
+    PS_CUDA(s, cudaFuncSetAttribute(ps_aggregate_clip_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
+    PS_CUDA(s, cudaFuncSetAttribute(ps_aggregate_clip_inline_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
+    PS_CUDA(s, cudaOccupancyMaxActiveBlocksPerMultiprocessor(&a, ps_aggregate_clip_kernel, kThreads, kSmem));
+    PS_CUDA(s, cudaOccupancyMaxActiveBlocksPerMultiprocessor(&b, ps_aggregate_clip_inline_kernel, kThreads, kSmem));
+    if (!s->clip_bar) PS_CUDA(s, cudaMalloc(&s->clip_bar, sizeof(GridBarrier)));
+    PS_CUDA(s, cudaMemset(s->clip_bar, 0, sizeof(GridBarrier)));
+    PS_CUDA(s, cudaStreamSynchronize(cudaStreamLegacy));
+    s->clip_ctas = std::max(1, std::min(a, b));
+    PS_CUDA(s, cudaEventCreateWithFlags(&s->clip_done, cudaEventDisableTiming));
+  }
+  if (spool_elems > s->clip_spool_cap) {
+    PS_CUDA(s, cudaDeviceSynchronize());
+    if (s->clip_spool) PS_CUDA(s, cudaFree(s->clip_spool));
+    s->clip_spool = nullptr;
+    s->clip_spool_cap = 0;
+    const cudaError_t e = cudaMalloc(&s->clip_spool, spool_elems * sizeof(float));
+    if (e != cudaSuccess) {
+      s->cuda_err = std::string("buffer of kept sums: ") + cudaGetErrorString(e);
+      cudaGetLastError();
+      return e == cudaErrorMemoryAllocation ? PS_ERR_NOMEM : PS_ERR_CUDA;
+    }
+    s->clip_spool_cap = spool_elems;
+  }
+  return PS_OK;
+}
+
+// Launches the clipped kernel for the table `plan` of the blocks `idx` on `stream` itself (device current).
+int launch_clip(ps_service* s, const std::vector<int>& idx, Plan& plan, const ClipCall& call, cudaStream_t stream) {
+  ++s->call_id;
+  int rc = ensure_clip(s, plan.spool);
+  if (rc) return rc;
+  PsClipHdr* h = reinterpret_cast<PsClipHdr*>(plan.bytes.data());
+  h->max_norm = call.max_norm;
+  // one CTA per four units (1024 elements, one vector per thread) up to what is resident at once
+  const int grid = (int)std::max<unsigned long long>(
+      1, std::min<unsigned long long>((plan.total_chunks + 3ull) / 4, (unsigned long long)s->num_sms * s->clip_ctas));
+  const size_t segs = (size_t)h->n_tasks + (size_t)grid;
+  const size_t parts = segs + (size_t)grid * h->n_jobs;
+  const bool inl = s->opt_inline && plan.bytes.size() <= kInlineBytes;
+  Slot* sl = nullptr;
+  rc = acquire_slot(s, inl ? 0 : plan.bytes.size(), parts + (segs + 1) / 2, &sl);
+  if (rc) return rc;
+  const int slot_index = (int)(sl - s->slots);
+  unsigned int waited = 0;
+  for (int bi : idx) {
+    rc = order_after_block(s, s->blocks[bi], stream, &waited);
+    if (rc) return rc;
+  }
+  if (s->clip_recorded) PS_CUDA(s, cudaStreamWaitEvent(stream, s->clip_done, 0));
+  const unsigned long long seq = s->launches + 1;
+  unsigned long long* done_word = s->done_dev + slot_index;
+  double* job_parts = sl->partials + segs;
+  unsigned int* seg_at = reinterpret_cast<unsigned int*>(sl->partials + parts);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3((unsigned)kThreads);
+  cfg.dynamicSmemBytes = kClipCache * sizeof(float);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeCooperative;
+  attr[0].val.cooperative = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  cudaError_t le;
+  if (inl) {
+    PsInlineTable tbl;
+    std::memcpy(tbl.bytes, plan.bytes.data(), plan.bytes.size());
+    le = cudaLaunchKernelEx(&cfg, ps_aggregate_clip_inline_kernel, tbl, (const PsJobDev*)s->jobs_dev, s->stats_dev,
+                            sl->partials, job_parts, seg_at, s->clip_spool, s->clip_bar, call.norms_out, s->status_dev,
+                            s->exit_ctrs + slot_index, done_word, seq);
+  } else {
+    std::memcpy(sl->host, plan.bytes.data(), plan.bytes.size());
+    PS_CUDA(s, cudaMemcpyAsync(sl->dev, sl->host, plan.bytes.size(), cudaMemcpyHostToDevice, s->copy_stream));
+    PS_CUDA(s, cudaEventRecord(sl->copied, s->copy_stream));
+    PS_CUDA(s, cudaStreamWaitEvent(stream, sl->copied, 0));
+    le = cudaLaunchKernelEx(&cfg, ps_aggregate_clip_kernel, (const unsigned char*)sl->dev, (const PsJobDev*)s->jobs_dev,
+                            s->stats_dev, sl->partials, job_parts, seg_at, s->clip_spool, s->clip_bar, call.norms_out,
+                            s->status_dev, s->exit_ctrs + slot_index, done_word, seq);
+  }
+  if (le != cudaSuccess) {
+    s->cuda_err = std::string("kernel launch: ") + cudaGetErrorString(le);
+    cudaGetLastError();
+    return PS_ERR_CUDA;
+  }
+  sl->seq = seq;
+  sl->gen = seq;
+  sl->signals = true;
+  sl->stream = stream;
+  sl->work_stream = -1;
+  sl->inflight = true;
+  sl->done_recorded = false;
+  PS_CUDA(s, cudaEventRecord(sl->done, stream));
+  sl->done_recorded = true;
+  PS_CUDA(s, cudaEventRecord(s->clip_done, stream));
+  s->clip_recorded = true;
+  s->next_slot = (s->next_slot + 1) % kSlots;
+  s->launches = seq;
+  s->var_launches[kVarClip]++;
+  s->var_bytes[kVarClip] += plan.algo_bytes;
+  s->last_grid = grid;
+  s->last_block = kThreads;
+  s->last_kernel = inl ? "clip_inline" : "clip";
+  consume_pushes(s, idx, slot_index, sl->gen);
+  return PS_OK;
+}
+
+bool bad_clip(float max_norm, const float* norms_out) {
+  return !(max_norm > 0.0f) || (reinterpret_cast<uintptr_t>(norms_out) & 3u);
 }
 
 // Sends out everything the batch holds (device made current here).
@@ -1338,6 +1566,23 @@ int ps_aggregate(ps_service* s, const ps_task* ready, int n_ready, void* stream_
   return submit_ready(s, s->idx, static_cast<cudaStream_t>(stream_), 0u, nullptr, false);
 }
 
+int ps_aggregate_clipped(ps_service* s, const ps_task* ready, int n_ready, float max_norm, float* norms_out,
+                         void* stream_) {
+  if (!alive(s)) return PS_ERR_BAD_HANDLE;
+  std::lock_guard<std::mutex> lk(s->mu);
+  if (bad_clip(max_norm, norms_out)) return PS_ERR_BAD_ARG;
+  int rc = validate_ready(s, ready, n_ready, &s->idx);
+  if (rc) return rc;
+  if (!has_device(s)) return PS_ERR_NO_DEVICE;
+  if (s->idx.empty()) return PS_OK;
+  rc = flush_batch(s);                     // earlier rounds first
+  if (rc) return rc;
+  PS_CUDA(s, cudaSetDevice(s->device));
+  rc = build_clip_plan(s, s->idx, &s->plan);
+  if (rc) return rc;
+  return launch_clip(s, s->idx, s->plan, ClipCall{max_norm, norms_out}, static_cast<cudaStream_t>(stream_));
+}
+
 static int push_batch_locked(ps_service* s, int n, const int* jobs, const int* blocks, const int* workers,
                              const void* const* ptrs);
 static void unpush_locked(ps_service* s, int n, const int* jobs, const int* blocks, const int* workers);
@@ -1369,7 +1614,7 @@ int ps_round(ps_service* s, int n_push, const int* jobs, const int* blocks, cons
 static int resolve_prepared(ps_service* s, Prepared& r) {
   const size_t n = r.jobs.size();
   r.push_bi.resize(n);
-  r.plan_ok = false;
+  r.plan_ok = r.clip_ok = false;
   for (size_t i = 0; i < n; ++i) {
     const int bi = find_block(s, r.jobs[i], r.block_ids[i]);
     if (bi < 0 || !r.ptrs[i]) return PS_ERR_BAD_ARG;
@@ -1444,9 +1689,8 @@ int ps_round_release(ps_service* s, int round) {
   return PS_OK;
 }
 
-int ps_round_run(ps_service* s, int round, void* stream_, const float** params_out) {
-  if (!alive(s)) return PS_ERR_BAD_HANDLE;
-  std::lock_guard<std::mutex> lk(s->mu);
+// A run of a prepared round; with `clip` its gradients are clipped by their global norm.
+static int round_run(ps_service* s, int round, const ClipCall* clip, void* stream_, const float** params_out) {
   if (round < 0 || round >= (int)s->prepared.size() || !s->prepared[round].live) return PS_ERR_BAD_ARG;
   Prepared& r = s->prepared[round];
   if (r.epoch != s->epoch) {
@@ -1480,20 +1724,36 @@ int ps_round_run(ps_service* s, int round, void* stream_, const float** params_o
     }
   if (!rc && !has_device(s)) rc = PS_ERR_NO_DEVICE;
   if (!rc && !r.idx.empty()) {
-    const bool reuse = r.self_contained && r.plan_ok;
+    const bool reuse = r.self_contained && (clip ? r.clip_ok : r.plan_ok);
+    Plan& plan = clip ? r.clip_plan : r.plan;
     if (reuse) {
       // same blocks, same places, same pointers as last time: only the step moves on
-      unsigned char* base = r.plan.bytes.data();
-      PsTaskDev* tasks = reinterpret_cast<PsTaskDev*>(base + reinterpret_cast<PsTableHdr*>(base)->tasks_off);
-      for (size_t i = 0; i < r.plan.order.size(); ++i) {
-        const Block& b = s->blocks[r.plan.order[i]];
+      unsigned char* base = plan.bytes.data();
+      PsTaskDev* tasks = reinterpret_cast<PsTaskDev*>(base + (clip ? reinterpret_cast<PsClipHdr*>(base)->tasks_off
+                                                                   : reinterpret_cast<PsTableHdr*>(base)->tasks_off));
+      for (size_t i = 0; i < plan.order.size(); ++i) {
+        const Block& b = s->blocks[plan.order[i]];
         set_step_fields(s->jobs[b.job], b, &tasks[i]);
       }
     }
     bool built = false;
-    rc = submit_ready(s, r.idx, static_cast<cudaStream_t>(stream_), r.flags, &r.plan, reuse, &built);
+    if (clip) {
+      rc = flush_batch(s);                 // earlier rounds first
+      if (!rc) {
+        const cudaError_t e = cudaSetDevice(s->device);
+        if (e != cudaSuccess) { s->cuda_err = cudaGetErrorString(e); rc = PS_ERR_CUDA; }
+      }
+      if (!rc && !reuse) {
+        rc = build_clip_plan(s, r.idx, &plan);
+        built = !rc;
+      }
+      if (!rc) rc = launch_clip(s, r.idx, plan, *clip, static_cast<cudaStream_t>(stream_));
+      if (!reuse) r.clip_ok = !rc && r.self_contained && built;
+    } else {
+      rc = submit_ready(s, r.idx, static_cast<cudaStream_t>(stream_), r.flags, &plan, reuse, &built);
+    }
     // the round's own table can be reused next time only if it was built for this round just now
-    if (!reuse) r.plan_ok = !rc && r.self_contained && built;
+    if (!clip && !reuse) r.plan_ok = !rc && r.self_contained && built;
   }
   if (rc) {
     for (size_t i = 0; i < done; ++i) {
@@ -1506,6 +1766,21 @@ int ps_round_run(ps_service* s, int round, void* stream_, const float** params_o
   if (params_out)
     for (size_t i = 0; i < r.idx.size(); ++i) params_out[i] = blk_p(s, s->blocks[r.idx[i]]);
   return PS_OK;
+}
+
+int ps_round_run(ps_service* s, int round, void* stream, const float** params_out) {
+  if (!alive(s)) return PS_ERR_BAD_HANDLE;
+  std::lock_guard<std::mutex> lk(s->mu);
+  return round_run(s, round, nullptr, stream, params_out);
+}
+
+int ps_round_run_clipped(ps_service* s, int round, float max_norm, float* norms_out, void* stream,
+                         const float** params_out) {
+  if (!alive(s)) return PS_ERR_BAD_HANDLE;
+  std::lock_guard<std::mutex> lk(s->mu);
+  if (bad_clip(max_norm, norms_out)) return PS_ERR_BAD_ARG;
+  const ClipCall call = {max_norm, norms_out};
+  return round_run(s, round, &call, stream, params_out);
 }
 
 int ps_join(ps_service* s, void* stream_) {
@@ -2083,7 +2358,7 @@ int ps_launch_stats(ps_service* s, int variant, unsigned long long* launches_out
   { int frc = flush_batch(s); if (frc) return frc; }    // held-back rounds go out first
   if (variant < 0 || variant >= kVariants) return PS_ERR_BAD_ARG;
   static const char* const names[kVariants] = {"ps_aggregate_ldg_kernel", "ps_aggregate_inline_kernel",
-                                               "ps_aggregate_bulk_kernel"};
+                                               "ps_aggregate_bulk_kernel", "ps_aggregate_clip_kernel"};
   if (launches_out) *launches_out = s->var_launches[variant];
   if (bytes_out) *bytes_out = s->var_bytes[variant];
   if (name_out) *name_out = names[variant];

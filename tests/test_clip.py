@@ -1,0 +1,498 @@
+"""Gradients clipped by their global norm: in the service's aggregate and on a worker's own tensors.
+
+The norm is checked against 64 bits.  Given the norm the kernel reports, every later operation is one
+binary32 rounding, so parameters, state and clipped tensors are compared for equality."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2204_03211_b200 import binding as B
+
+f32 = np.float32
+
+
+def factor(norm, max_norm):
+    if np.isinf(max_norm):
+        return f32(1)
+    with np.errstate(all="ignore"):
+        f = f32(max_norm) / (f32(norm) + f32(1e-6))
+    return f32(1) if f >= 1 else f
+
+
+def to_bf16(x):
+    return torch.from_numpy(np.ascontiguousarray(x)).to(torch.bfloat16)
+
+
+class Ref:
+    """One block: numpy in binary32, one rounding per operation."""
+
+    def __init__(self, hp, p):
+        self.hp, self.p = hp, p.copy()
+        self.s0, self.s1, self.t = np.zeros_like(p), np.zeros_like(p), 0
+
+    def scaled_sum(self, grads):
+        G = grads[0].astype(f32)
+        for g in grads[1:]:
+            G = G + g.astype(f32)
+        return G * f32(self.hp["grad_scale"])
+
+    def apply(self, G, c):
+        hp = self.hp
+        self.t += 1
+        d = G * c + f32(hp["weight_decay"]) * self.p
+        if hp["opt"] == B.PS_SGD:
+            self.s0 = f32(hp["momentum"]) * self.s0 + d
+            self.p = self.p - f32(hp["lr"]) * self.s0
+        else:
+            b1, b2 = f32(hp["beta1"]), f32(hp["beta2"])
+            self.s0 = b1 * self.s0 + (f32(1) - b1) * d
+            self.s1 = b2 * self.s1 + (f32(1) - b2) * (d * d)
+            ss = f32(float(f32(hp["lr"])) / (1.0 - float(b1) ** self.t))
+            sbc2 = f32(np.sqrt(1.0 - float(b2) ** self.t))
+            self.p = self.p - ss * (self.s0 / (np.sqrt(self.s1) / sbc2 + f32(hp["eps"])))
+
+
+def hparams(opt, dtype, W, grad_scale=1.0):
+    return dict(opt=opt, grad_dtype=dtype, num_workers=W, lr=0.05, momentum=0.9, weight_decay=1e-3, beta1=0.9, beta2=0.99,
+                eps=1e-8, grad_scale=grad_scale)
+
+
+class World:
+    """A service and the references of its blocks, fed the same gradients."""
+
+    def __init__(self, jobs, sizes, contexts=1, seed=0):
+        self.rng = np.random.default_rng(seed)
+        self.svc = B.Service(0, contexts, 3 * sum(4 * n + 4096 for s in sizes for n in s) + (1 << 20))
+        self.jobs, self.sizes, self.ref = jobs, sizes, {}
+        for j, (hp, ns) in enumerate(zip(jobs, sizes)):
+            assert self.svc.register_job(**hp) == j
+            for b, n in enumerate(ns):
+                p = self.rng.normal(0, 0.05, n).astype(f32)
+                self.svc.register_block(j, b, n, 0, p)
+                self.ref[j, b] = Ref(hp, p)
+        self.ready = list(self.ref)
+
+    def gradients(self, shift=0, spread=1e-2):
+        """Device shards and the same values on the host; shift > 0 leaves the shards unaligned."""
+        self.dev, self.host = {}, {}
+        for (j, b), r in self.ref.items():
+            for w in range(self.jobs[j]["num_workers"]):
+                g = torch.from_numpy(self.rng.normal(0, spread, len(r.p) + shift).astype(f32))
+                if self.jobs[j]["grad_dtype"] == B.PS_BF16:
+                    g = g.to(torch.bfloat16)
+                self.host[j, b, w] = g[shift:].float().numpy()
+                self.dev[j, b, w] = g.cuda()[shift:]
+
+    def push(self):
+        for (j, b, w), g in self.dev.items():
+            self.svc.push(j, b, w, g)
+
+    def sums(self):
+        return {k: r.scaled_sum([self.host[k[0], k[1], w] for w in range(r.hp["num_workers"])]) for k, r in self.ref.items()}
+
+    def check(self, max_norm, norms):
+        """norms: what the kernel reported, one per job.  Compares everything and advances the references."""
+        sums = self.sums()
+        for j in range(len(self.jobs)):
+            true = np.sqrt(sum((sums[k].astype(np.float64) ** 2).sum() for k in sums if k[0] == j))
+            # binary64 sums and square root, rounded once to 24 bits
+            assert abs(float(norms[j]) - true) <= 1.01 * 2.0 ** -24 * true
+            c = factor(norms[j], max_norm)
+            for (jj, b), r in self.ref.items():
+                if jj != j:
+                    continue
+                r.apply(sums[jj, b], c)
+                got = self.svc.view(self.svc.pull(jj, b), len(r.p)).cpu().numpy()
+                assert np.array_equal(got, r.p), (jj, b, np.flatnonzero(got != r.p)[:5])
+                a0, a1, _ = self.svc.block_state(jj, b)
+                assert np.array_equal(self.svc.view(a0, len(r.p)).cpu().numpy(), r.s0)
+                if a1:
+                    assert np.array_equal(self.svc.view(a1, len(r.p)).cpu().numpy(), r.s1)
+                sq, step = self.svc.block_stats(jj, b)
+                want = (sums[jj, b].astype(np.float64) ** 2).sum()
+                assert step == r.t and abs(sq - want) <= 1e-12 * want
+        assert self.svc.device_status() == 0
+
+
+TINY, MIXED = [1, 5, 33, 1024], [300_001, 7, 65536, 256, 255, 257, 1, 90_000]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("opt", [B.PS_SGD, B.PS_ADAM])
+@pytest.mark.parametrize("dtype", [B.PS_F32, B.PS_BF16])
+@pytest.mark.parametrize("W", [1, 2, 5])
+@pytest.mark.parametrize("sizes,inline", [(TINY, 1), (TINY, 0), (MIXED, 1)])
+def test_aggregate_clipped(opt, dtype, W, sizes, inline):
+    world = World([hparams(opt, dtype, W, 0.5)], [sizes], seed=W)
+    world.svc.set_option(B.PS_OPT_INLINE_TABLE, inline)
+    norms = torch.full((1,), -1.0, device="cuda")
+    for it, max_norm in enumerate((0.05, 1e4, 0.7)):
+        world.gradients(shift=it % 2)
+        world.push()
+        world.svc.aggregate_clipped(world.ready, max_norm, norms)
+        world.check(max_norm, norms.cpu().numpy())
+    world.svc.close()
+
+
+@pytest.mark.gpu
+def test_more_sums_than_shared_memory_holds():
+    """14 million elements: most sums go through the buffer; a second, smaller call uses it again."""
+    sizes = [9_000_001, 3, 4_999_999, 64]
+    world = World([hparams(B.PS_SGD, B.PS_F32, 2)], [sizes])
+    norms = torch.zeros(1, device="cuda")
+    for max_norm in (1.0, 2.0):
+        world.gradients()
+        world.push()
+        world.svc.aggregate_clipped(world.ready, max_norm, norms)
+        world.check(max_norm, norms.cpu().numpy())
+    world.svc.close()
+
+
+@pytest.mark.gpu
+def test_several_jobs_have_their_own_norms():
+    jobs = [hparams(B.PS_SGD, B.PS_F32, 16), hparams(B.PS_ADAM, B.PS_BF16, 2), hparams(B.PS_SGD, B.PS_BF16, 3, 2.0)]
+    world = World(jobs, [[5000, 120_001], [70_000, 9], [333] * 90])
+    world.gradients()
+    for j in (1, 2):
+        for k in world.dev:
+            if k[0] == j:
+                world.dev[k] *= 4 ** j
+                world.host[k] = world.host[k] * f32(4 ** j)
+    world.push()
+    norms = torch.zeros(3, device="cuda")
+    order = sorted(world.ready, key=lambda t: (-t[0], t[1]))       # job 2 is named first
+    world.svc.aggregate_clipped(order, 0.9, norms)
+    world.check(0.9, norms.cpu().numpy()[::-1])
+    world.svc.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kernel", [1, 2])
+def test_a_factor_of_one_changes_nothing(kernel):
+    """Norm below the limit, and an infinite limit: the same bits as ps_aggregate."""
+    jobs = [hparams(B.PS_SGD, B.PS_F32, 3), hparams(B.PS_ADAM, B.PS_BF16, 4)]
+    a, b = World(jobs, [MIXED, TINY], seed=5), World(jobs, [MIXED, TINY], seed=5)
+    b.svc.set_option(B.PS_OPT_KERNEL, kernel)
+    norms = torch.zeros(2, device="cuda")
+    for limit in (1e9, float("inf")):
+        a.gradients()
+        b.gradients()
+        a.push()
+        b.push()
+        a.svc.aggregate_clipped(a.ready, limit, norms)
+        b.svc.aggregate(b.ready)
+        a.check(limit, norms.cpu().numpy())
+        for k, r in a.ref.items():
+            n = len(r.p)
+            assert torch.equal(a.svc.view(a.svc.pull(*k), n), b.svc.view(b.svc.pull(*k), n))
+    a.svc.close()
+    b.svc.close()
+
+
+@pytest.mark.gpu
+def test_nonfinite_gradients():
+    for bad, want in ((float("nan"), "nan"), (float("inf"), "zero")):
+        world = World([hparams(B.PS_SGD, B.PS_F32, 2)], [[1000, 50]])
+        world.gradients()
+        world.dev[0, 0, 1][77] = bad
+        world.push()
+        norms = torch.zeros(1, device="cuda")
+        before = world.svc.view(world.svc.pull(0, 1), 50).cpu().numpy()
+        world.svc.aggregate_clipped(world.ready, 1.0, norms)
+        after0 = world.svc.view(world.svc.pull(0, 0), 1000).cpu().numpy()
+        after1 = world.svc.view(world.svc.pull(0, 1), 50).cpu().numpy()
+        if want == "nan":
+            assert np.isnan(norms.item()) and np.isnan(after0).all() and np.isnan(after1).all()
+        else:                                # the factor is 0: only weight decay moves the other elements
+            assert np.isinf(norms.item()) and np.isnan(after0[77]) and np.isfinite(np.delete(after0, 77)).all()
+            hp = world.jobs[0]
+            assert np.array_equal(after1, before - f32(hp["lr"]) * (f32(hp["weight_decay"]) * before))
+        world.svc.close()
+
+
+@pytest.mark.gpu
+def test_zero_gradients_are_not_scaled():
+    world = World([hparams(B.PS_SGD, B.PS_F32, 2)], [[3000]])
+    world.gradients()
+    for k in world.dev:
+        world.dev[k].zero_()
+        world.host[k][:] = 0
+    world.push()
+    norms = torch.full((1,), 9.0, device="cuda")
+    world.svc.aggregate_clipped(world.ready, 1.0, norms)
+    world.check(1.0, norms.cpu().numpy())
+    assert norms.item() == 0.0
+    world.svc.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [B.PS_F32, B.PS_BF16])
+@pytest.mark.parametrize("row_len", [8, 400])
+def test_row_sparse_shards(dtype, row_len):
+    rows, W = 700, 3
+    world = World([hparams(B.PS_SGD, dtype, W)], [[rows * row_len, 1000]])
+    world.gradients()
+    keep = []
+    for w in range(W):
+        ids = np.sort(world.rng.choice(rows, 40 + w, replace=False)).astype(np.int32)
+        full = world.dev[0, 0, w].view(rows, row_len)
+        world.host[0, 0, w] = np.where(np.isin(np.arange(rows), ids)[:, None],
+                                       world.host[0, 0, w].reshape(rows, row_len), f32(0)).reshape(-1)
+        if w == 1:                           # one dense worker among them
+            d = torch.from_numpy(world.host[0, 0, w]).to(full.dtype).cuda()
+            keep.append(d)
+            world.svc.push(0, 0, w, d)
+        else:
+            di = torch.from_numpy(ids).cuda()
+            v = full[di.long()].contiguous()
+            keep += [di, v]
+            world.svc.push_rows(0, 0, w, di, len(ids), row_len, v)
+        world.svc.push(0, 1, w, world.dev[0, 1, w])
+    norms = torch.zeros(1, device="cuda")
+    world.svc.aggregate_clipped(world.ready, 0.3, norms)
+    world.check(0.3, norms.cpu().numpy())
+    world.svc.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("overlap", [0, 1])
+def test_prepared_rounds_alternate_with_other_calls(overlap):
+    """Clipped and plain runs of one prepared round, a migration between them, and a second stream."""
+    world = World([hparams(B.PS_ADAM, B.PS_F32, 2)], [[40_000, 129]], contexts=2)
+    svc = world.svc
+    svc.set_option(B.PS_OPT_OVERLAP, overlap)
+    world.gradients()
+    dev = world.dev
+    keys = list(dev)
+    i32 = lambda k: np.array([x[k] for x in keys], np.int32)  # noqa: E731
+    rid = svc.round_prepare(i32(0), i32(1), i32(2), np.array([dev[k].data_ptr() for k in keys], np.uint64), world.ready)
+    norms = torch.zeros(1, device="cuda")
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for it in range(6):
+        s = streams[it % 2]
+        if it == 3:
+            svc.migrate_blocks(world.ready, 1, s)
+        if it % 3 == 1:
+            svc.round_run(rid, s)
+            svc.join(s)
+            torch.cuda.synchronize()
+            sums = world.sums()
+            for k, r in world.ref.items():
+                r.apply(sums[k], f32(1))
+        else:
+            svc.round_run_clipped(rid, 0.25, norms, s)
+            torch.cuda.synchronize()
+            world.check(0.25, norms.cpu().numpy())
+    for _ in range(4):                       # nothing waits in between: steps of one block follow one another
+        svc.round_run_clipped(rid, 0.25, norms, streams[0])
+        svc.round_run_clipped(rid, 0.25, norms, streams[1])
+    torch.cuda.synchronize()
+    sums, c = world.sums(), factor(norms.item(), 0.25)
+    for k, r in world.ref.items():
+        for _ in range(8):
+            r.apply(sums[k], c)
+        assert np.array_equal(svc.view(svc.pull(*k), len(r.p)).cpu().numpy(), r.p)
+    assert svc.launch_stats(4)[3]["launches"] == 12
+    svc.close()
+
+
+@pytest.mark.gpu
+def test_the_factor_is_the_gradients_scale_by_differences():
+    """Without momentum and weight decay the update is -lr * c(G) * G; its derivative along a direction D of the
+    gradients is compared with a difference quotient of the formula in 64 bits."""
+    n, lr, limit, h = 4096, 1.0, 0.5, 1e-3
+    rng = np.random.default_rng(3)
+    G, D = rng.normal(0, 1e-2, n).astype(f32), rng.normal(0, 1e-2, n).astype(f32)
+
+    def update(g):
+        svc = B.Service(0, 1, 1 << 20)
+        j = svc.register_job(opt=B.PS_SGD, num_workers=1, lr=lr)
+        svc.register_block(j, 0, n, 0)
+        d = torch.from_numpy(g.astype(f32)).cuda()
+        svc.push(j, 0, 0, d)
+        svc.aggregate_clipped([(j, 0)], limit)
+        torch.cuda.synchronize()
+        out = svc.view(svc.pull(j, 0), n).cpu().numpy().astype(np.float64)
+        svc.close()
+        return out
+
+    G64, D64 = G.astype(np.float64), D.astype(np.float64)
+    norm = np.sqrt((G64 ** 2).sum())
+    assert norm > limit
+    exact = -lr * limit / norm * (D64 - G64 * (G64 @ D64) / norm ** 2)     # d/dG of limit * G / |G|
+    quotient = (update(G + h * D) - update(G - h * D)) / (2 * h)
+    # inputs and outputs carry 2^-24 relative, divided by 2h; the quotient's own error is of order h^2
+    tol = (4 * 2.0 ** -24 / (2 * h) + 10 * h * h) * (np.abs(G64).max() + np.abs(D64).max())
+    assert np.abs(quotient - exact).max() <= tol
+
+
+# ---- a worker's own tensors ---------------------------------------------------------------------------
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("src,dst", [("f32", "f32"), ("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("sizes,shift", [([1], 0), ([7, 8, 2048, 2049, 1], 0), ([100_003, 64, 5], 1), ([3_000_000, 17], 0),
+                                         ([300] * 200, 0)])
+def test_clip_tensors(src, dst, sizes, shift):
+    g = torch.Generator().manual_seed(sum(sizes))
+    hosts = [(torch.randn(n, generator=g) * 0.1).to(DT[src]) for n in sizes]
+    srcs = [torch.cat([torch.zeros(shift, dtype=DT[src]), h]).cuda()[shift:] for h in hosts]
+    dsts = [torch.full((n + shift,), 3.0, device="cuda", dtype=DT[dst])[shift:] for n in sizes]
+    clip = B.Clip(srcs, dsts)
+    norm = torch.zeros(1, device="cuda")
+    true = np.sqrt(sum(float((h.double() ** 2).sum()) for h in hosts))
+    for limit in (0.2, 1e6, float("inf"), 0.05):
+        clip.run(limit, norm)
+        # eight squares are added with at most sixteen roundings of 2^-24, the rest in binary64; half of it reaches the root
+        assert abs(norm.item() - true) <= 9 * 2.0 ** -24 * true
+        c = torch.tensor(factor(norm.item(), limit))
+        for h, d in zip(hosts, dsts):
+            assert torch.equal((h.float() * c).to(DT[dst]), d.cpu())
+    assert clip.status() == 0
+    clip.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_clip_in_place(dt):
+    hosts = [(torch.randn(n) * 0.1).to(DT[dt]) for n in (5000, 1, 0, 70_001)]
+    dev = [h.clone().cuda() for h in hosts]
+    clip, norm = B.Clip(dev), torch.zeros(1, device="cuda")
+    clip.run(1e6, norm)
+    assert all(torch.equal(h, d.cpu()) for h, d in zip(hosts, dev))
+    clip.run(0.5, norm)
+    c = torch.tensor(factor(norm.item(), 0.5))
+    assert all(torch.equal((h.float() * c).to(DT[dt]), d.cpu()) for h, d in zip(hosts, dev))
+    clip.close()
+
+
+@pytest.mark.gpu
+def test_clip_extreme_values():
+    """Squares that leave binary32's range, both ways, and non-finite elements."""
+    norm = torch.zeros(1, device="cuda")
+    for v in (1e30, 1e-30):
+        x = torch.full((1000,), v, device="cuda")
+        clip = B.Clip([x], [torch.empty_like(x)])
+        clip.run(1.0, norm)
+        true = float(f32(v)) * np.sqrt(1000.0)
+        assert abs(norm.item() - true) <= 2.0 ** -23 * true
+        clip.close()
+    for bad in (float("nan"), float("inf")):
+        x = torch.ones(100, device="cuda")
+        x[50] = bad
+        out = torch.empty_like(x)
+        clip = B.Clip([x], [out])
+        clip.run(1.0, norm)
+        if np.isnan(bad):
+            assert np.isnan(norm.item()) and out.isnan().all()
+        else:
+            assert np.isinf(norm.item()) and out.isnan().sum() == 1 and (out[:50] == 0).all()
+        clip.close()
+    empty = B.Clip([torch.empty(0, device="cuda")])
+    norm.fill_(5)
+    empty.run(1.0, norm)
+    assert norm.item() == 0
+
+
+@pytest.mark.gpu
+def test_clip_on_streams():
+    a, b = torch.randn(1_000_000, device="cuda"), torch.randn(1_000_000, device="cuda")
+    out = [torch.empty_like(a) for _ in range(2)]
+    clips, norms = [B.Clip([a], [out[0]]), B.Clip([b], [out[1]])], torch.zeros(2, device="cuda")
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(20):
+        for k in range(2):
+            clips[k].run(1.0, norms[k:], streams[k])
+    torch.cuda.synchronize()
+    for k, t in enumerate((a, b)):
+        assert torch.equal(out[k].cpu(), t.cpu() * torch.tensor(factor(norms[k].item(), 1.0)))
+
+
+# ---- refusals: no GPU needed ----------------------------------------------------------------------------
+
+def test_aggregate_refusals():
+    svc = B.Service(B.PS_DEVICE_NONE, 1, 1 << 20)
+    lib = B.load()
+    j = svc.register_job(num_workers=2)
+    svc.register_block(j, 0, 100)
+    ready = B.make_tasks([(j, 0)])
+    call = lambda t, n, m, out=None: lib.ps_aggregate_clipped(svc.handle, t, n, m, out, None)  # noqa: E731
+    assert call(ready, 1, 1.0) == B.PS_ERR_NOT_READY
+    for w in range(2):
+        svc.push(j, 0, w, 4096)
+    for m in (0.0, -1.0, float("nan")):
+        assert call(ready, 1, m) == B.PS_ERR_BAD_ARG
+    assert call(ready, 1, 1.0, 2) == B.PS_ERR_BAD_ARG
+    assert call(B.make_tasks([(j, 3)]), 1, 1.0) == B.PS_ERR_BAD_ARG
+    assert call(B.make_tasks([(j, 0), (j, 0)]), 2, 1.0) == B.PS_ERR_DUPLICATE
+    assert call(None, 1, 1.0) == B.PS_ERR_BAD_ARG
+    assert call(ready, 1, 1.0) == B.PS_ERR_NO_DEVICE
+    assert lib.ps_aggregate_clipped(None, ready, 1, 1.0, None, None) == B.PS_ERR_BAD_HANDLE
+    assert lib.ps_round_run_clipped(svc.handle, 0, 1.0, None, None, None) == B.PS_ERR_BAD_ARG
+    rid = svc.round_prepare(None, None, None, None, [(j, 0)])
+    assert lib.ps_round_run_clipped(svc.handle, rid, 0.0, None, None, None) == B.PS_ERR_BAD_ARG
+    assert lib.ps_round_run_clipped(svc.handle, rid, 1.0, None, None, None) == B.PS_ERR_NO_DEVICE
+
+
+def test_clip_refusals():
+    lib = B.load()
+    h = C.c_void_p()
+    ptrs = lambda *a: (C.c_void_p * len(a))(*a)  # noqa: E731
+    ns = (C.c_size_t * 1)(10)
+    make = lambda *a: lib.ps_clip_create(C.byref(h), *a)  # noqa: E731
+    ok = ptrs(4096)
+    bad, align = B.PS_ERR_BAD_ARG, B.PS_ERR_ALIGN
+    assert lib.ps_clip_create(None, 0, 1, ok, 0, ok, 0, ns) == bad
+    assert make(-1, 1, ok, 0, ok, 0, ns) == bad
+    assert make(0, -1, ok, 0, ok, 0, ns) == bad
+    assert make(0, 1, None, 0, ok, 0, ns) == bad
+    assert make(0, 1, ok, 5, ok, 0, ns) == bad
+    assert make(0, 1, ok, 0, ok, 5, ns) == bad
+    assert make(0, 1, ptrs(None), 0, ok, 0, ns) == bad
+    assert make(0, 1, ok, 0, ok, 1, ns) == bad                   # in place, but of another type
+    assert make(0, 1, ptrs(4098), 0, ok, 0, ns) == align
+    assert make(0, 1, ok, 0, ptrs(4097), 1, ns) == align
+    assert lib.ps_clip_run(None, 1.0, None, None) == B.PS_ERR_BAD_HANDLE
+    assert lib.ps_clip_status(None, None) == B.PS_ERR_BAD_HANDLE
+    assert lib.ps_clip_destroy(None) == B.PS_ERR_BAD_HANDLE
+
+
+@pytest.mark.gpu
+def test_more_than_64_jobs_are_refused():
+    svc = B.Service(0, 1, 1 << 20)
+    grads = torch.ones(64, device="cuda")
+    for j in range(65):
+        svc.register_job(num_workers=1)
+        svc.register_block(j, 0, 64)
+        svc.push(j, 0, 0, grads)
+    with pytest.raises(B.PsError) as e:
+        svc.aggregate_clipped([(j, 0) for j in range(65)], 1.0)
+    assert e.value.status == B.PS_ERR_TOO_LARGE
+    norms = torch.zeros(64, device="cuda")
+    svc.aggregate_clipped([(j, 0) for j in range(64)], 1.0, norms)       # the pushes are still there
+    assert (norms == 8.0).all()
+    svc.close()
+
+
+@pytest.mark.gpu
+def test_a_view_keeps_its_service():
+    """A view of service-owned memory outlives the last other reference to the service."""
+    import gc
+    import weakref
+    svc = B.Service(0, 1, 1 << 20)
+    j = svc.register_job(num_workers=1)
+    svc.register_block(j, 0, 64)
+    view, seen = svc.view(svc.pull(j, 0), 64), weakref.ref(svc)
+    del svc
+    gc.collect()
+    assert seen() is not None                # checked on the host before the memory is read
+    assert (view == 0).all()
+    del view
+    gc.collect()
+    assert seen() is None
