@@ -663,21 +663,27 @@ def _check_op(rc: int, where: str):
         raise PsError(rc, where, load().ps_op_last_error().decode() if rc == PS_ERR_CUDA else "")
 
 
-_DTYPES = {"torch.float32": PS_F32, "torch.bfloat16": PS_BF16}
+_DTYPES = {}            # torch.dtype -> ps_dtype, filled at the first call (this module imports torch only where it is used)
 
 
 def _dtype(t, where: str) -> int:
-    d = _DTYPES.get(str(t.dtype))
+    d = _DTYPES.get(t.dtype)
     if d is None:
-        raise PsError(PS_ERR_BAD_ARG, where, "%s is neither float32 nor bfloat16" % t.dtype)
+        import torch
+        _DTYPES.update({torch.float32: PS_F32, torch.bfloat16: PS_BF16})
+        d = _DTYPES.get(t.dtype)
+        if d is None:
+            raise PsError(PS_ERR_BAD_ARG, where, "%s is neither float32 nor bfloat16" % t.dtype)
     return d
 
 
 def _matrix(t, where: str):
-    """(address, ps_dtype, row stride) of a 2-d device tensor whose rows are contiguous."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or not t.is_cuda:
+    """(address, ps_dtype, rows, columns, row stride) of a 2-d device tensor whose rows are contiguous."""
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 2 or not t.is_cuda or (strides[1] != 1 and shape[1] > 1):
         raise PsError(PS_ERR_BAD_ARG, where, "a 2-d CUDA tensor with contiguous rows is wanted")
-    return t.data_ptr(), _dtype(t, where), max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+    rows, cols = shape
+    return t.data_ptr(), _dtype(t, where), rows, cols, strides[0] if rows > 1 else cols
 
 
 class Clip:
@@ -745,36 +751,34 @@ class MxTensor:
         return self.rows, self.cols
 
 
-def _mx_ref(q):
-    return None if q is None else q.ref
-
-
 def ps_mx_quantize(x, q=None, qt=None, stream=None):
     """Quantises the device matrix x (float32 or bfloat16, any row stride) along
     its rows into q and / or along its columns into qt (x's transpose)."""
-    where = "ps_mx_quantize"
-    ptr, dtype, ld = _matrix(x, where)
-    _check_op(load().ps_mx_quantize(ptr, dtype, x.shape[0], x.shape[1], ld, _mx_ref(q), _mx_ref(qt), _stream_ptr(stream)),
-              where)
+    ptr, dtype, rows, cols, ld = _matrix(x, "ps_mx_quantize")
+    rc = load().ps_mx_quantize(ptr, dtype, rows, cols, ld, q and q.ref, qt and qt.ref, _stream_ptr(stream))
+    if rc:
+        _check_op(rc, "ps_mx_quantize")
 
 
 def ps_mx_dequantize(q, out, stream=None):
     """Writes the values q stands for to the device matrix out, which it returns."""
-    where = "ps_mx_dequantize"
-    ptr, dtype, ld = _matrix(out, where)
-    if tuple(out.shape) != q.shape:
-        raise PsError(PS_ERR_BAD_ARG, where, "out is %s, the operand %s" % (tuple(out.shape), q.shape))
-    _check_op(load().ps_mx_dequantize(q.ref, dtype, ptr, ld, _stream_ptr(stream)), where)
+    ptr, dtype, rows, cols, ld = _matrix(out, "ps_mx_dequantize")
+    if rows != q.rows or cols != q.cols:
+        raise PsError(PS_ERR_BAD_ARG, "ps_mx_dequantize", "out is %s, the operand %s" % ((rows, cols), q.shape))
+    rc = load().ps_mx_dequantize(q.ref, dtype, ptr, ld, _stream_ptr(stream))
+    if rc:
+        _check_op(rc, "ps_mx_dequantize")
     return out
 
 
 def ps_mx_matmul(a, b, out, stream=None):
     """out[m][n] = sum over k of a[m][k] * b[n][k]; returns out (float32 or bfloat16, any row stride)."""
-    where = "ps_mx_matmul"
-    ptr, dtype, ld = _matrix(out, where)
-    if out.shape[0] != a.rows or out.shape[1] != b.rows:
-        raise PsError(PS_ERR_BAD_ARG, where, "out is %s, the product %s" % (tuple(out.shape), (a.rows, b.rows)))
-    _check_op(load().ps_mx_matmul(a.ref, b.ref, dtype, ptr, ld, _stream_ptr(stream)), where)
+    ptr, dtype, rows, cols, ld = _matrix(out, "ps_mx_matmul")
+    if rows != a.rows or cols != b.rows:
+        raise PsError(PS_ERR_BAD_ARG, "ps_mx_matmul", "out is %s, the product %s" % ((rows, cols), (a.rows, b.rows)))
+    rc = load().ps_mx_matmul(a.ref, b.ref, dtype, ptr, ld, _stream_ptr(stream))
+    if rc:
+        _check_op(rc, "ps_mx_matmul")
     return out
 
 

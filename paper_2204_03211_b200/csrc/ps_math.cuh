@@ -10,10 +10,14 @@ namespace psb {
 
 struct Hp {
   float lr, mom, wd, b1, b2, omb1, omb2, eps, gs, ss_t, sbc2_t;
+  float clip;                              // clipping factor (OPT >= kClipped)
 };
 
-// OPT of a chunk body that only sums: "p" receives the scaled gradient, there is no state.
-constexpr int kSumOnly = 2;
+// What a chunk body does with a sum (its parameter OPT): the optimizer's step (PS_SGD, PS_ADAM); only keep the scaled
+// gradient, in "p"; only add up its square; the step for the scaled gradient times the clipping factor.
+constexpr int kSumOnly = 2, kNormOnly = 3, kClipped = 4;         // kClipped + optimizer
+__host__ __device__ constexpr bool updates(int opt) { return opt != kSumOnly && opt != kNormOnly; }
+__host__ __device__ constexpr bool has_s1(int opt) { return updates(opt) && (opt & 1); }
 
 // The optimizer's step for a scaled gradient.
 template <int OPT>
@@ -36,9 +40,13 @@ __device__ __forceinline__ void apply_elem(const Hp& h, float G, float& p, float
 template <int OPT>
 __device__ __forceinline__ void update_elem(const Hp& h, float G, float& p, float& s0, float& s1, double& sq) {
   G = __fmul_rn(G, h.gs);
-  sq = fma((double)G, (double)G, sq);      // binary64: product exact, sum rounded once
-  if constexpr (OPT == kSumOnly) p = G;
-  else apply_elem<OPT>(h, G, p, s0, s1);
+  if constexpr (OPT >= kClipped) {
+    apply_elem<OPT - kClipped>(h, __fmul_rn(G, h.clip), p, s0, s1);
+  } else {
+    sq = fma((double)G, (double)G, sq);    // binary64: product exact, sum rounded once
+    if constexpr (OPT == kSumOnly) p = G;
+    if constexpr (updates(OPT)) apply_elem<OPT>(h, G, p, s0, s1);
+  }
 }
 
 __device__ __forceinline__ float bf16_lo(unsigned int u) { return __uint_as_float(u << 16); }
@@ -94,9 +102,9 @@ __device__ __forceinline__ void update4(const Hp& h, const float4& G, float* p, 
   update_elem<OPT>(h, G.y, P.y, A.y, B.y, sq);
   update_elem<OPT>(h, G.z, P.z, A.z, B.z, sq);
   update_elem<OPT>(h, G.w, P.w, A.w, B.w, sq);
-  *reinterpret_cast<float4*>(p + e) = P;
-  if (OPT != kSumOnly) *reinterpret_cast<float4*>(s0 + e) = A;
-  if (OPT == 1) *reinterpret_cast<float4*>(s1 + e) = B;
+  if (OPT != kNormOnly) *reinterpret_cast<float4*>(p + e) = P;
+  if (updates(OPT)) *reinterpret_cast<float4*>(s0 + e) = A;
+  if (has_s1(OPT)) *reinterpret_cast<float4*>(s1 + e) = B;
 }
 
 // ---------------------------------------------------------------- chunk bodies
@@ -130,9 +138,9 @@ __device__ __forceinline__ void chunk_f32_vec(unsigned int tid, const Hp& h, con
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const size_t e = begin + 4 * (size_t)(i + u * NT);
-      pv[u] = OPT != kSumOnly ? *reinterpret_cast<const float4*>(p + e) : make_float4(0, 0, 0, 0);
-      av[u] = OPT != kSumOnly ? *reinterpret_cast<const float4*>(s0 + e) : make_float4(0, 0, 0, 0);
-      if (OPT == 1) bv[u] = *reinterpret_cast<const float4*>(s1 + e); else bv[u] = make_float4(0, 0, 0, 0);
+      pv[u] = updates(OPT) ? *reinterpret_cast<const float4*>(p + e) : make_float4(0, 0, 0, 0);
+      av[u] = updates(OPT) ? *reinterpret_cast<const float4*>(s0 + e) : make_float4(0, 0, 0, 0);
+      if (has_s1(OPT)) bv[u] = *reinterpret_cast<const float4*>(s1 + e); else bv[u] = make_float4(0, 0, 0, 0);
     }
     if (pf_lane) {
       if (W <= kNextTripMaxW && i + U * NT + (U - 1) * NT < nvec) {
@@ -140,9 +148,9 @@ __device__ __forceinline__ void chunk_f32_vec(unsigned int tid, const Hp& h, con
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           const size_t e = begin + 4 * (size_t)(i + (U + u) * NT);
-          if (OPT != kSumOnly) prefetch_l2(p + e);
-          if (OPT != kSumOnly) prefetch_l2(s0 + e);
-          if (OPT == 1) prefetch_l2(s1 + e);
+          if (updates(OPT)) prefetch_l2(p + e);
+          if (updates(OPT)) prefetch_l2(s0 + e);
+          if (has_s1(OPT)) prefetch_l2(s1 + e);
         }
         for (int w = 0; w <= kAheadF32 && w < W; ++w) {
           const float* g = static_cast<const float*>(ld_ptr(shards, w));
@@ -183,9 +191,9 @@ __device__ __forceinline__ void chunk_f32_vec(unsigned int tid, const Hp& h, con
   for (; i < nvec; i += NT) {
     const size_t e = begin + 4 * (size_t)i;
     const float4 zero = make_float4(0, 0, 0, 0);
-    const float4 pv = OPT != kSumOnly ? *reinterpret_cast<const float4*>(p + e) : zero;
-    const float4 av = OPT != kSumOnly ? *reinterpret_cast<const float4*>(s0 + e) : zero;
-    const float4 bv = (OPT == 1) ? *reinterpret_cast<const float4*>(s1 + e) : zero;
+    const float4 pv = updates(OPT) ? *reinterpret_cast<const float4*>(p + e) : zero;
+    const float4 av = updates(OPT) ? *reinterpret_cast<const float4*>(s0 + e) : zero;
+    const float4 bv = has_s1(OPT) ? *reinterpret_cast<const float4*>(s1 + e) : zero;
     float4 acc = as_f4(ld_stream(static_cast<const float*>(ld_ptr(shards)) + e));
 #pragma unroll 4
     for (int w = 1; w < W; ++w) acc = add4(acc, ld_stream(static_cast<const float*>(ld_ptr(shards, w)) + e));
@@ -204,19 +212,24 @@ __device__ __forceinline__ void chunk_bf16_vec(unsigned int tid, const Hp& h, co
   const bool pf_lane = (tid & 7) == 0;      // shards: 8 lanes x 16 bytes = one line
   for (unsigned int i = tid; i < nvec; i += NT) {
     const size_t e = begin + 8 * (size_t)i;
-    if (OPT != kSumOnly && (tid & 3) == 0) {   // parameters and state: 4 lanes x 32 bytes = one line
+    if (updates(OPT) && (tid & 3) == 0) {   // parameters and state: 4 lanes x 32 bytes = one line
       prefetch_l2(p + e);
       prefetch_l2(s0 + e);
-      if (OPT == 1) prefetch_l2(s1 + e);
+      if (has_s1(OPT)) prefetch_l2(s1 + e);
     }
-    if (pf_lane)
+    // a body that only reads, with few workers: the next trip's lines, else the next workers' of this trip
+    const bool next_trip = !updates(OPT) && W <= kNextTripMaxW;
+    if (pf_lane && next_trip && i + NT < nvec)
+      for (int w = 0; w < W; ++w)
+        prefetch_l2(static_cast<const unsigned short*>(ld_ptr(shards, w)) + e + 8 * (size_t)NT);
+    if (pf_lane && !(next_trip && i != tid))
       for (int w = 1; w <= kAheadBf16 && w < W; ++w)
         prefetch_l2(static_cast<const unsigned short*>(ld_ptr(shards, w)) + e);
     float acc[8];
     widen8(ld_stream(static_cast<const unsigned short*>(ld_ptr(shards)) + e), acc);
 #pragma unroll 4
     for (int w = 1; w < W; ++w) {
-      if (pf_lane && w + kAheadBf16 < W)
+      if (pf_lane && !next_trip && w + kAheadBf16 < W)
         prefetch_l2(static_cast<const unsigned short*>(ld_ptr(shards, w + kAheadBf16)) + e);
       const uint4 t = ld_stream(static_cast<const unsigned short*>(ld_ptr(shards, w)) + e);
       add_bf16x2(acc[0], acc[1], t.x);
@@ -225,13 +238,13 @@ __device__ __forceinline__ void chunk_bf16_vec(unsigned int tid, const Hp& h, co
       add_bf16x2(acc[6], acc[7], t.w);
     }
     float4 p0 = make_float4(0, 0, 0, 0), p1 = p0, a0 = p0, a1 = p0, b0 = p0, b1 = p0;
-    if (OPT != kSumOnly) {
+    if (updates(OPT)) {
       p0 = *reinterpret_cast<const float4*>(p + e);
       p1 = *reinterpret_cast<const float4*>(p + e + 4);
       a0 = *reinterpret_cast<const float4*>(s0 + e);
       a1 = *reinterpret_cast<const float4*>(s0 + e + 4);
     }
-    if (OPT == 1) {
+    if (has_s1(OPT)) {
       b0 = *reinterpret_cast<const float4*>(s1 + e);
       b1 = *reinterpret_cast<const float4*>(s1 + e + 4);
     }
@@ -257,11 +270,11 @@ __device__ __forceinline__ void chunk_scalar(unsigned int tid, const Hp& h, cons
       G = __ldcs(static_cast<const float*>(ld_ptr(shards)) + e);
       for (int w = 1; w < W; ++w) G = __fadd_rn(G, __ldcs(static_cast<const float*>(ld_ptr(shards, w)) + e));
     }
-    float P = OPT != kSumOnly ? p[e] : 0.f, A = OPT != kSumOnly ? s0[e] : 0.f, B = (OPT == 1) ? s1[e] : 0.f;
+    float P = updates(OPT) ? p[e] : 0.f, A = updates(OPT) ? s0[e] : 0.f, B = has_s1(OPT) ? s1[e] : 0.f;
     update_elem<OPT>(h, G, P, A, B, sq);
-    p[e] = P;
-    if (OPT != kSumOnly) s0[e] = A;
-    if (OPT == 1) s1[e] = B;
+    if (OPT != kNormOnly) p[e] = P;
+    if (updates(OPT)) s0[e] = A;
+    if (has_s1(OPT)) s1[e] = B;
   }
 }
 

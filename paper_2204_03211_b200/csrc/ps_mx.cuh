@@ -8,7 +8,8 @@
 // holds the quotients.  Scaling by a power of two is exact in binary32, so the
 // only rounding is the one to E2M1.  A block of zeros, and one whose scale would
 // fall below 2^-127, has the scale 2^-127; a block that holds an infinity or a
-// NaN has the scale byte 0xFF and reads back as NaN in all 32 places.
+// NaN has the scale byte 0xFF (its codes mean nothing) and reads back as NaN in all
+// 32 places.
 //
 // Codes: two per byte, the lower nibble first, rows of ceil(cols/32)*16 bytes
 // (padding elements are +0).  Scales: 512-byte atoms of 128 rows x 4 blocks, byte
@@ -42,16 +43,13 @@ struct MxOut {                               // one direction of a quantisation;
 
 // ------------------------------------------------------------------ arithmetic
 
-// Scale byte of a block from the bits of its largest magnitude (binary32).  NaNs compare above infinity.
-__device__ __forceinline__ unsigned int mx_scale_byte(unsigned int amax_bits) {
-  const unsigned int e = amax_bits >> 23;
+// Scale byte of a block from the exponent field of its largest magnitude (binary32 and bf16 have the same).
+__device__ __forceinline__ unsigned int mx_scale_byte(unsigned int e) {
   return e >= 255u ? 255u : e > 2u ? e - 2u : 0u;
 }
 
-// 2^-(scale) as a binary32 factor; 0 for a block that is not finite (its codes are zeros).
-__device__ __forceinline__ float mx_inverse(unsigned int sb) {
-  return __uint_as_float(sb == 255u ? 0u : (254u - sb) << 23);
-}
+// 1 / scale.  (For a block that is not finite this is not a power of two: its codes mean nothing, its scale is NaN.)
+__device__ __forceinline__ float mx_inverse(unsigned int sb) { return __uint_as_float((254u - sb) << 23); }
 
 // Eight values, already divided by their scale, as eight nibbles (v[0] lowest).
 __device__ __forceinline__ unsigned int mx_pack8(const float (&v)[8]) {
@@ -69,21 +67,41 @@ __device__ __forceinline__ unsigned int mx_pack8(const float (&v)[8]) {
   return r;
 }
 
-// Multiplies by the inverse scale.  A block that is not finite has the factor 0, and 0 * inf is a NaN, whose
-// conversion is unspecified here: its elements are replaced by zeros first.
-__device__ __forceinline__ unsigned int mx_codes8(const float (&x)[8], unsigned int sb) {
-  const float inv = mx_inverse(sb);
+__device__ __forceinline__ unsigned int mul_bf16x2(unsigned int a, unsigned int b) {
+  unsigned int r;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+// Eight bf16 values as codes.  The division by the scale is done on pairs: it is exact, or the quotient is below
+// 2^-126 and far below the smallest code's half.  inv: 1 / scale of the values' block(s), twice.
+__device__ __forceinline__ unsigned int mx_codes8(const unsigned int (&w)[4], unsigned int inv) {
   float v[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = sb == 255u ? 0.f : __fmul_rn(x[i], inv);
+  for (int i = 0; i < 4; ++i) {
+    const unsigned int q = mul_bf16x2(w[i], inv);
+    v[2 * i] = __uint_as_float(q << 16);
+    v[2 * i + 1] = __uint_as_float(q & 0xffff0000u);
+  }
   return mx_pack8(v);
 }
 
-__device__ __forceinline__ unsigned int abs_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+__device__ __forceinline__ unsigned int mx_codes8(const float (&x)[8], float inv) {
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(x[i], inv);
+  return mx_pack8(v);
+}
 
-__device__ __forceinline__ unsigned int max_u16x2(unsigned int a, unsigned int b) {
+// Largest magnitude, NaN if there is one; the result's sign bit means nothing.
+__device__ __forceinline__ float max_abs(float a, float b) {
+  float r;
+  asm("max.NaN.xorsign.abs.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ unsigned int max_abs_bf16x2(unsigned int a, unsigned int b) {
   unsigned int r;
-  asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
 
@@ -185,26 +203,24 @@ ps_mx_quantize_kernel(const typename MxIn<BF16>::T* __restrict__ x, long long ro
       }
     }
     if constexpr (ROWS) {
-      unsigned int amax;
+      unsigned int sb, q;
       if constexpr (BF16) {
-        v[0] = __uint_as_float(raw.x << 16); v[1] = __uint_as_float(raw.x & 0xffff0000u);
-        v[2] = __uint_as_float(raw.y << 16); v[3] = __uint_as_float(raw.y & 0xffff0000u);
-        v[4] = __uint_as_float(raw.z << 16); v[5] = __uint_as_float(raw.z & 0xffff0000u);
-        v[6] = __uint_as_float(raw.w << 16); v[7] = __uint_as_float(raw.w & 0xffff0000u);
-        unsigned int m = max_u16x2(max_u16x2(raw.x & 0x7fff7fffu, raw.y & 0x7fff7fffu),
-                                   max_u16x2(raw.z & 0x7fff7fffu, raw.w & 0x7fff7fffu));
-        amax = max(m & 0xffffu, m >> 16) << 16;
+        const unsigned int w[4] = {raw.x, raw.y, raw.z, raw.w};
+        unsigned int m = max_abs_bf16x2(max_abs_bf16x2(w[0], w[1]), max_abs_bf16x2(w[2], w[3]));
+        m = max_abs_bf16x2(m, __shfl_xor_sync(0xffffffffu, m, 1));
+        m = max_abs_bf16x2(m, __shfl_xor_sync(0xffffffffu, m, 2));
+        m = max_abs_bf16x2(m, m >> 16);
+        sb = mx_scale_byte((m >> 7) & 0xffu);
+        q = mx_codes8(w, ((254u - sb) << 7) * 0x10001u);
       } else {
-        amax = 0u;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) amax = max(amax, abs_bits(v[i]));
+        float m = max_abs(max_abs(max_abs(v[0], v[1]), max_abs(v[2], v[3])), max_abs(max_abs(v[4], v[5]), max_abs(v[6], v[7])));
+        m = max_abs(m, __shfl_xor_sync(0xffffffffu, m, 1));
+        m = max_abs(m, __shfl_xor_sync(0xffffffffu, m, 2));
+        sb = mx_scale_byte((__float_as_uint(m) >> 23) & 0xffu);
+        q = mx_codes8(v, mx_inverse(sb));
       }
-      amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-      amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-      const unsigned int sb = mx_scale_byte(amax);
       if (r < rows && (c & ~31ll) < cols) {
-        *reinterpret_cast<unsigned int*>(out.codes + (size_t)r * (size_t)mx_pitch(cols) + (size_t)(c >> 1)) =
-            mx_codes8(v, sb);
+        *reinterpret_cast<unsigned int*>(out.codes + (size_t)r * (size_t)mx_pitch(cols) + (size_t)(c >> 1)) = q;
         if ((g & 3) == 0) s_row[(tr & 31) * 16 + (tr >> 5) * 4 + (g >> 2)] = (unsigned char)sb;
       }
     }
@@ -216,16 +232,19 @@ ps_mx_quantize_kernel(const typename MxIn<BF16>::T* __restrict__ x, long long ro
     const bool any = r0 + rb * 32 < rows;
     if constexpr (BF16) {
       const int cw = (tid & 7) + (tid >> 5) * 8;              // word = pair of columns
-      unsigned int w[32], m = 0u;
+      unsigned int w[32];
 #pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        w[i] = tile[tile_word<kWords>(rb * 32 + i, cw)];
-        m = max_u16x2(m, w[i] & 0x7fff7fffu);
-      }
+      for (int i = 0; i < 32; ++i) w[i] = tile[tile_word<kWords>(rb * 32 + i, cw)];
+      unsigned int m = max_abs_bf16x2(w[0], w[1]);
+#pragma unroll
+      for (int i = 2; i < 32; ++i) m = max_abs_bf16x2(m, w[i]);
+      const unsigned int sb[2] = {mx_scale_byte((m >> 7) & 0xffu), mx_scale_byte((m >> 23) & 0xffu)};
+      const unsigned int inv = (((254u - sb[0]) << 7) & 0xffffu) | ((254u - sb[1]) << 23);
+#pragma unroll
+      for (int i = 0; i < 32; ++i) w[i] = mul_bf16x2(w[i], inv);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int tc = 2 * cw + h;
-        const unsigned int sb = mx_scale_byte((h ? m >> 16 : m & 0xffffu) << 16);
         uint4 q;
         unsigned int* qp = reinterpret_cast<unsigned int*>(&q);
 #pragma unroll
@@ -234,26 +253,26 @@ ps_mx_quantize_kernel(const typename MxIn<BF16>::T* __restrict__ x, long long ro
 #pragma unroll
           for (int i = 0; i < 8; ++i)
             v[i] = __uint_as_float(h ? w[k * 8 + i] & 0xffff0000u : w[k * 8 + i] << 16);
-          qp[k] = mx_codes8(v, sb);
+          qp[k] = mx_pack8(v);
         }
         if (any && c0 + tc < cols) {
           *reinterpret_cast<uint4*>(out_t.codes + (size_t)(c0 + tc) * (size_t)mx_pitch(rows) +
                                     (size_t)(r0 / 2 + rb * 16)) = q;
-          s_col[(tc & 31) * 16 + (tc >> 5) * 4 + rb] = (unsigned char)sb;
+          s_col[(tc & 31) * 16 + (tc >> 5) * 4 + rb] = (unsigned char)sb[h];
         }
       }
     } else {
 #pragma unroll 1
       for (int h = 0; h < 2; ++h) {
         const int tc = (tid & 7) + (tid >> 5) * 8 + h * 64;
-        float v[32];
-        unsigned int m = 0u;
+        float v[32], m = 0.f;
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
           v[i] = __uint_as_float(tile[tile_word<kWords>(rb * 32 + i, tc)]);
-          m = max(m, abs_bits(v[i]));
+          m = max_abs(m, v[i]);
         }
-        const unsigned int sb = mx_scale_byte(m);
+        const unsigned int sb = mx_scale_byte((__float_as_uint(m) >> 23) & 0xffu);
+        const float inv = mx_inverse(sb);
         uint4 q;
         unsigned int* qp = reinterpret_cast<unsigned int*>(&q);
 #pragma unroll
@@ -261,7 +280,7 @@ ps_mx_quantize_kernel(const typename MxIn<BF16>::T* __restrict__ x, long long ro
           float u[8];
 #pragma unroll
           for (int i = 0; i < 8; ++i) u[i] = v[k * 8 + i];
-          qp[k] = mx_codes8(u, sb);
+          qp[k] = mx_codes8(u, inv);
         }
         if (any && c0 + tc < cols) {
           *reinterpret_cast<uint4*>(out_t.codes + (size_t)(c0 + tc) * (size_t)mx_pitch(rows) +
@@ -291,12 +310,6 @@ ps_mx_quantize_kernel(const typename MxIn<BF16>::T* __restrict__ x, long long ro
 // is its value times 2^-126, subnormals included: two
 // exact multiplications (2^126, the scale) give the result without a conversion
 // instruction, which issue at a fraction of the rate.
-
-__device__ __forceinline__ unsigned int mul_bf16x2(unsigned int a, unsigned int b) {
-  unsigned int r;
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
 
 // Nibbles 2j and 2j+1 of w as a pair of bf16 values, unscaled.
 __device__ __forceinline__ unsigned int mx_pair(unsigned int w, int j) {

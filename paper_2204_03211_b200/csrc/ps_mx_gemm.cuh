@@ -220,18 +220,47 @@ __device__ __forceinline__ void mm_cluster_sync() {
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-__device__ __forceinline__ float mm_remote(unsigned int addr, unsigned int rank) {
-  float v;
-  asm volatile(
-      "{\n\t"
+// Four floats at `addr` of this CTA's layout, from the cluster's CTA `rank`.
+__device__ __forceinline__ float4 mm_remote4(unsigned int addr, unsigned int rank) {
+  float4 v;
+  asm("{\n\t"
       ".reg .b32 r;\n\t"
-      "mapa.shared::cluster.u32 r, %1, %2;\n\t"
-      "ld.shared::cluster.f32 %0, [r];\n\t"
+      "mapa.shared::cluster.u32 r, %4, %5;\n\t"
+      "ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [r];\n\t"
       "}"
-      : "=f"(v)
-      : "r"(addr), "r"(rank)
-      : "memory");
+      : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+      : "r"(addr), "r"(rank));
   return v;
+}
+
+// The sum over the cluster's parts in rank order: all loads are in flight together.
+template <int S>
+__device__ __forceinline__ float4 mm_sum_parts(unsigned int addr) {
+  float4 t[S];
+#pragma unroll
+  for (int r = 0; r < S; ++r) t[r] = mm_remote4(addr, (unsigned)r);
+#pragma unroll
+  for (int r = 1; r < S; ++r) {
+    t[0].x = __fadd_rn(t[0].x, t[r].x);
+    t[0].y = __fadd_rn(t[0].y, t[r].y);
+    t[0].z = __fadd_rn(t[0].z, t[r].z);
+    t[0].w = __fadd_rn(t[0].w, t[r].w);
+  }
+  return t[0];
+}
+
+// Stores four neighbours of C's row m, columns n..n+3 (n < limit).
+__device__ __forceinline__ void mm_store4(const MmArgs& a, long long m, long long n, long long limit, float4 v) {
+  if (a.vec_ok && n + 4 <= limit) {
+    const size_t at = (size_t)m * (size_t)a.ldc + (size_t)n;
+    if (a.out_f32) *reinterpret_cast<float4*>(static_cast<float*>(a.c) + at) = v;
+    else *reinterpret_cast<uint2*>(static_cast<unsigned short*>(a.c) + at) = make_uint2(mm_bf16x2(v.x, v.y), mm_bf16x2(v.z, v.w));
+  } else {
+    mm_store1(a, m, n, v.x);
+    if (n + 1 < limit) mm_store1(a, m, n + 1, v.y);
+    if (n + 2 < limit) mm_store1(a, m, n + 2, v.z);
+    if (n + 3 < limit) mm_store1(a, m, n + 3, v.w);
+  }
 }
 
 template <int BN>
@@ -374,7 +403,14 @@ ps_mx_matmul_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_cons
           float v[kStep];
           mm_load<kStep>(acc + c, v);
 #pragma unroll
-          for (int i = 0; i < kStep; ++i) red[args.swap ? (c + i) * kMmP + row : row * (BN + 1) + c + i] = k1 > k0 ? v[i] : 0.f;
+          for (int i = 0; i < kStep; i += 4) {
+            if (args.swap) {
+#pragma unroll
+              for (int q = 0; q < 4; ++q) red[(c + i + q) * kMmP + row] = v[i + q];
+            } else {
+              *reinterpret_cast<float4*>(red + row * (BN + 4) + c + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+            }
+          }
         }
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -389,14 +425,17 @@ ps_mx_matmul_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_cons
     mm_cluster_sync();
     int tp, tq;
     mm_tile(args, first, &tp, &tq);
-    const int total = kMmP * BN, e0 = total / args.splits * rank, e1 = rank + 1 == args.splits ? total : e0 + total / args.splits;
+    // groups of four neighbours in C; every CTA takes an equal share of them
+    const int total = kMmP * BN / 4, e0 = (int)((long long)total * rank / args.splits);
+    const int e1 = (int)((long long)total * (rank + 1) / args.splits);
     for (int e = e0 + tid; e < e1; e += kMmThreads) {
-      const int row = args.swap ? e % kMmP : e / BN, col = args.swap ? e / kMmP : e % BN;
-      const unsigned int at = base + 4u * (unsigned)(args.swap ? col * kMmP + row : row * (BN + 1) + col);
-      float sum = 0.f;
-      for (int r = 0; r < args.splits; ++r) sum += mm_remote(at, (unsigned)r);
+      const int row = args.swap ? e % (kMmP / 4) * 4 : e / (BN / 4), col = args.swap ? e / (kMmP / 4) : e % (BN / 4) * 4;
       const long long p = (long long)tp * kMmP + row, q = (long long)tq * BN + col;
-      if (p < args.rows_p && q < args.rows_q) mm_store1(args, args.swap ? q : p, args.swap ? p : q, sum);
+      if (p >= args.rows_p || q >= args.rows_q) continue;
+      const unsigned int at = base + 4u * (unsigned)(args.swap ? col * kMmP + row : row * (BN + 4) + col);
+      const float4 v = args.splits == 8 ? mm_sum_parts<8>(at) : args.splits == 4 ? mm_sum_parts<4>(at) : mm_sum_parts<2>(at);
+      if (args.swap) mm_store4(args, q, p, args.rows_p, v);
+      else mm_store4(args, p, q, args.rows_q, v);
     }
     mm_cluster_sync();                                // nobody leaves while its shared memory is being read
   }

@@ -84,9 +84,9 @@ __device__ __forceinline__ void chunk_rows(unsigned int tid, const Hp& h, const 
           acc.z = __fadd_rn(acc.z, 0.f); acc.w = __fadd_rn(acc.w, 0.f);
         }
         const float4 z = make_float4(0, 0, 0, 0);
-        const float4 pv = OPT != kSumOnly ? *reinterpret_cast<const float4*>(p + e) : z;
-        const float4 av = OPT != kSumOnly ? *reinterpret_cast<const float4*>(s0 + e) : z;
-        const float4 bv = (OPT == 1) ? *reinterpret_cast<const float4*>(s1 + e) : make_float4(0, 0, 0, 0);
+        const float4 pv = updates(OPT) ? *reinterpret_cast<const float4*>(p + e) : z;
+        const float4 av = updates(OPT) ? *reinterpret_cast<const float4*>(s0 + e) : z;
+        const float4 bv = has_s1(OPT) ? *reinterpret_cast<const float4*>(s1 + e) : make_float4(0, 0, 0, 0);
         update4<OPT>(h, acc, p, s0, s1, e, pv, av, bv, sq);
       } else {
         float acc[8];
@@ -105,12 +105,12 @@ __device__ __forceinline__ void chunk_rows(unsigned int tid, const Hp& h, const 
           for (int q = 0; q < 8; ++q) acc[q] = __fadd_rn(acc[q], 0.f);
         }
         const float4 z = make_float4(0, 0, 0, 0);
-        const float4 p0 = OPT != kSumOnly ? *reinterpret_cast<const float4*>(p + e) : z;
-        const float4 p1 = OPT != kSumOnly ? *reinterpret_cast<const float4*>(p + e + 4) : z;
-        const float4 a0 = OPT != kSumOnly ? *reinterpret_cast<const float4*>(s0 + e) : z;
-        const float4 a1 = OPT != kSumOnly ? *reinterpret_cast<const float4*>(s0 + e + 4) : z;
-        const float4 b0 = (OPT == 1) ? *reinterpret_cast<const float4*>(s1 + e) : z;
-        const float4 b1 = (OPT == 1) ? *reinterpret_cast<const float4*>(s1 + e + 4) : z;
+        const float4 p0 = updates(OPT) ? *reinterpret_cast<const float4*>(p + e) : z;
+        const float4 p1 = updates(OPT) ? *reinterpret_cast<const float4*>(p + e + 4) : z;
+        const float4 a0 = updates(OPT) ? *reinterpret_cast<const float4*>(s0 + e) : z;
+        const float4 a1 = updates(OPT) ? *reinterpret_cast<const float4*>(s0 + e + 4) : z;
+        const float4 b0 = has_s1(OPT) ? *reinterpret_cast<const float4*>(s1 + e) : z;
+        const float4 b1 = has_s1(OPT) ? *reinterpret_cast<const float4*>(s1 + e + 4) : z;
         update4<OPT>(h, make_float4(acc[0], acc[1], acc[2], acc[3]), p, s0, s1, e, p0, a0, b0, sq);
         update4<OPT>(h, make_float4(acc[4], acc[5], acc[6], acc[7]), p, s0, s1, e + 4, p1, a1, b1, sq);
       }

@@ -205,13 +205,13 @@ struct ps_service {
   bool mig_large_ok = true;                // the 28 KB kernel-parameter form of the migration kernel is accepted
   unsigned long long epoch = 0;            // bumped by whatever can invalidate a prepared round's table:
                                            // migration, import, unregistration, options
-  // clipped aggregates: the kept sums, the grid barrier, and the end of the last such launch (the next one uses the
-  // same buffer and barrier, on whatever stream)
+  // clipped aggregates: the kept sums, the grid barrier and counters, which one launch after the other uses, on
+  // whatever streams
   float* clip_spool = nullptr;
   size_t clip_spool_cap = 0;
-  GridBarrier* clip_bar = nullptr;
-  cudaEvent_t clip_done = nullptr;
-  bool clip_recorded = false;
+  ClipShared* clip_shared = nullptr;
+  int clip_slot = -1;                      // slot and number of the last clipped launch
+  unsigned long long clip_seq = 0;
   int clip_ctas = 0;                       // CTAs of the clip kernels an SM holds
   int last_grid = 0, last_block = 0;
   const char* last_kernel = "none";
@@ -788,8 +788,7 @@ int ps_destroy(ps_service* s) {
     if (s->exit_ctrs) cudaFree(s->exit_ctrs);
     if (s->done_host) cudaFreeHost(const_cast<unsigned long long*>(s->done_host));
     if (s->clip_spool) cudaFree(s->clip_spool);
-    if (s->clip_bar) cudaFree(s->clip_bar);
-    if (s->clip_done) cudaEventDestroy(s->clip_done);
+    if (s->clip_shared) cudaFree(s->clip_shared);
     if (s->copy_stream) cudaStreamDestroy(s->copy_stream);
     for (auto ws : s->work_streams) if (ws) cudaStreamDestroy(ws);
   }
@@ -1270,11 +1269,47 @@ int launch_in_parts(ps_service* s, const std::vector<int>& idx, int parts) {
   return PS_OK;
 }
 
-// Builds the table of a clipped launch of the validated blocks `idx`: tasks in the caller's order, each with its cost
-// and its place in the buffer of kept sums.
+// Elements per chunk of a clipped launch.  One whose sums fit into shared memory is cut into at most one chunk per CTA
+// (the smallest multiple of 64 that does it): 16 blocks of 65536 elements on 592 CTAs, for instance, become 592 chunks
+// of 1792 and not 512 of 2048.  A larger one gets about eight chunks per CTA: fewer leave the CTAs uneven at the
+// barrier, more cost their start-up and a longer sum of partial sums (six 512-wide layers, eight workers: chunks of
+// 4096, 8192 and 12288 elements 317, 307 and 314 us).
+unsigned int clip_chunk(ps_service* s, const std::vector<int>& idx, unsigned int grid) {
+  unsigned long long elems = 0;
+  for (int bi : idx) elems += s->blocks[bi].nelem;
+  auto chunks = [&](unsigned int ce) {
+    unsigned long long n = 0;
+    for (int bi : idx) n += (s->blocks[bi].nelem + ce - 1) / ce;
+    return n;
+  };
+  if (chunks(kClipSlot) <= grid) {
+    unsigned int lo = 4, hi = kClipSlot / 64;              // in units of 64 elements
+    while (lo < hi) {
+      const unsigned int mid = (lo + hi) / 2;
+      if (chunks(mid * 64) <= grid) hi = mid; else lo = mid + 1;
+    }
+    return lo * 64;
+  }
+  const unsigned long long want = (elems / (8ull * grid) + 1023) / 1024 * 1024;
+  return (unsigned int)std::min<unsigned long long>(kClipChunkMax, std::max<unsigned long long>(kClipChunkMin, want));
+}
+
+// Builds the table of a clipped launch of the validated blocks `idx`: tasks sorted by job, jobs in the order in which
+// the list names them first.
 int build_clip_plan(ps_service* s, const std::vector<int>& idx, Plan* plan) {
   const size_t n = idx.size();
-  plan->order = idx;
+  std::vector<int> job_ids;
+  for (int bi : idx)
+    if (std::find(job_ids.begin(), job_ids.end(), s->blocks[bi].job) == job_ids.end()) {
+      if (job_ids.size() == (size_t)kClipMaxJobs) return PS_ERR_TOO_LARGE;
+      job_ids.push_back(s->blocks[bi].job);
+    }
+  plan->order.clear();
+  if (job_ids.size() == 1) plan->order = idx;
+  else
+    for (int j : job_ids)
+      for (int bi : idx)
+        if (s->blocks[bi].job == j) plan->order.push_back(bi);
   size_t nptr = 0, nsp = 0;
   for (int bi : idx) {
     const size_t W = (size_t)s->jobs[s->blocks[bi].job].d.num_workers;
@@ -1282,22 +1317,24 @@ int build_clip_plan(ps_service* s, const std::vector<int>& idx, Plan* plan) {
     if (s->blocks[bi].nsparse) nsp += W;
   }
   const size_t tasks_off = sizeof(PsClipHdr);
-  const size_t costs_off = tasks_off + n * sizeof(PsTaskDev);
-  const size_t ptrs_off = costs_off + n * sizeof(PsClipCost);
+  const size_t starts_off = tasks_off + n * sizeof(PsTaskDev);
+  const size_t jobs_off = starts_off + n * sizeof(unsigned int);
+  const size_t ptrs_off = (jobs_off + (job_ids.size() + 1) * sizeof(unsigned int) + 15) / 16 * 16;
   const size_t sparse_off = (ptrs_off + nptr * sizeof(void*) + 15) / 16 * 16;
   plan->bytes.assign(sparse_off + nsp * sizeof(PsSparseDev), 0);
   plan->has_sparse = nsp > 0;
   unsigned char* base = plan->bytes.data();
   PsTaskDev* tasks = reinterpret_cast<PsTaskDev*>(base + tasks_off);
-  PsClipCost* costs = reinterpret_cast<PsClipCost*>(base + costs_off);
+  unsigned int* starts = reinterpret_cast<unsigned int*>(base + starts_off);
+  unsigned int* job_first = reinterpret_cast<unsigned int*>(base + jobs_off);
   const void** ptrs = reinterpret_cast<const void**>(base + ptrs_off);
   PsSparseDev* sp = reinterpret_cast<PsSparseDev*>(base + sparse_off);
-  std::vector<int> job_ids;                // in order of first appearance
-  unsigned long long cost = 0, spool = 0, units = 0;
-  size_t row = 0, sp_row = 0;
+  const unsigned int ce = clip_chunk(s, idx, (unsigned int)(s->num_sms * s->clip_ctas));
+  unsigned long long chunk = 0, spool = 0;
+  size_t row = 0, sp_row = 0, slot = 0;
   plan->algo_bytes = 0;
   for (size_t i = 0; i < n; ++i) {
-    const Block& b = s->blocks[idx[i]];
+    const Block& b = s->blocks[plan->order[i]];
     const Job& j = s->jobs[b.job];
     const int W = j.d.num_workers;
     PsTaskDev& t = tasks[i];
@@ -1306,7 +1343,6 @@ int build_clip_plan(ps_service* s, const std::vector<int>& idx, Plan* plan) {
     t.s1 = blk_s1(s, b);
     t.nelem = b.nelem;
     t.shard_row = (unsigned int)row;
-    t.t_first = ~0ull;
     set_step_fields(j, b, &t);
     t.job = b.job;
     t.stat_idx = b.stat_idx;
@@ -1315,64 +1351,67 @@ int build_clip_plan(ps_service* s, const std::vector<int>& idx, Plan* plan) {
       ptrs[row + w] = b.pushed[w];
       if (reinterpret_cast<uintptr_t>(b.pushed[w]) & 15u) t.vec_ok = 0;
     }
-    unsigned int unit = kClipUnit;
-    if (b.nsparse) {
+    t.chunk_elems = ce;
+    t.reread = !b.nsparse && t.vec_ok && W * j.grad_esize() <= kClipReread;
+    if (b.nsparse) {                       // chunks of whole rows
+      if (b.row_len > (1u << 30)) return PS_ERR_TOO_LARGE;
       t.row_len = b.row_len;
+      t.chunk_elems = std::max(1u, ce / b.row_len) * b.row_len;
       t.sparse_row = (unsigned int)sp_row;
       for (int w = 0; w < W; ++w) {
         sp[sp_row + w].ids = b.row_ids[w];
         sp[sp_row + w].n = b.row_cnt[w];
       }
       sp_row += W;
-      unit = std::max(1u, kClipUnit / b.row_len) * b.row_len;
     }
-    const unsigned long long nunits = (b.nelem + unit - 1) / unit;
-    if (unit > (1u << 24) || nunits > 0xffffffffull) return PS_ERR_TOO_LARGE;
-    size_t slot = std::find(job_ids.begin(), job_ids.end(), b.job) - job_ids.begin();
-    if (slot == job_ids.size()) job_ids.push_back(b.job);
-    PsClipCost& k = costs[i];
-    k.start = cost;
-    k.unit = unit * (unsigned int)(bytes_per_elem(j) + 8);       // sums are written and read once
-    k.unit_elems = unit;
-    k.units = (unsigned int)nunits;
-    k.job_slot = (unsigned int)slot;
-    k.spool = spool;
-    cost += nunits * k.unit + kClipTaskCost;
+    const unsigned long long nchunks = (b.nelem + t.chunk_elems - 1) / t.chunk_elems;
+    if (job_ids[slot] != b.job) ++slot;
+    if (i == 0 || s->blocks[plan->order[i - 1]].job != b.job) job_first[slot] = (unsigned int)chunk;
+    t.job_slot = (unsigned short)slot;
+    t.first_chunk = starts[i] = (unsigned int)chunk;
+    t.nchunks = (unsigned int)nchunks;
+    t.spool = spool;
+    chunk += nchunks;
+    if (chunk > 0x7ffffff0ull) return PS_ERR_BAD_ARG;
     spool += (b.nelem + 63) / 64 * 64;
-    units += nunits;
     row += W;
     plan->algo_bytes += b.nelem * bytes_per_elem(j);
   }
-  if (job_ids.size() > (size_t)kClipMaxJobs) return PS_ERR_TOO_LARGE;
+  job_first[job_ids.size()] = (unsigned int)chunk;
   PsClipHdr* h = reinterpret_cast<PsClipHdr*>(base);
   h->n_tasks = (unsigned int)n;
   h->n_jobs = (unsigned int)job_ids.size();
+  h->total_chunks = (unsigned int)chunk;
   h->tasks_off = (unsigned int)tasks_off;
-  h->costs_off = (unsigned int)costs_off;
+  h->starts_off = (unsigned int)starts_off;
+  h->jobs_off = (unsigned int)jobs_off;
   h->ptrs_off = (unsigned int)ptrs_off;
   h->sparse_off = (unsigned int)sparse_off;
-  h->cache_elems = kClipCache;
-  h->total_cost = cost;
-  plan->total_chunks = (unsigned int)std::min<unsigned long long>(units, 0xffffffffull);
+  plan->total_chunks = (unsigned int)chunk;
+  plan->chunk_elems = ce;
   plan->spool = spool;
   return PS_OK;
 }
 
-// Device memory and launch limits of the clipped kernels, at the first such call and when the buffer has to grow.
-int ensure_clip(ps_service* s, size_t spool_elems) {
-  if (!s->clip_done) {
-    constexpr int kSmem = (int)(kClipCache * sizeof(float));
+// Launch limits and device memory of the clipped kernels, at the first such call.
+int ensure_clip(ps_service* s) {
+  if (!s->clip_ctas) {
+    constexpr int kSmem = (int)(kClipSlot * sizeof(float));
     int a = 0, b = 0;
     PS_CUDA(s, cudaFuncSetAttribute(ps_aggregate_clip_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
     PS_CUDA(s, cudaFuncSetAttribute(ps_aggregate_clip_inline_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
     PS_CUDA(s, cudaOccupancyMaxActiveBlocksPerMultiprocessor(&a, ps_aggregate_clip_kernel, kThreads, kSmem));
     PS_CUDA(s, cudaOccupancyMaxActiveBlocksPerMultiprocessor(&b, ps_aggregate_clip_inline_kernel, kThreads, kSmem));
-    if (!s->clip_bar) PS_CUDA(s, cudaMalloc(&s->clip_bar, sizeof(GridBarrier)));
-    PS_CUDA(s, cudaMemset(s->clip_bar, 0, sizeof(GridBarrier)));
+    if (!s->clip_shared) PS_CUDA(s, cudaMalloc(&s->clip_shared, sizeof(ClipShared)));
+    PS_CUDA(s, cudaMemset(s->clip_shared, 0, sizeof(ClipShared)));
     PS_CUDA(s, cudaStreamSynchronize(cudaStreamLegacy));
     s->clip_ctas = std::max(1, std::min(a, b));
-    PS_CUDA(s, cudaEventCreateWithFlags(&s->clip_done, cudaEventDisableTiming));
   }
+  return PS_OK;
+}
+
+// The buffer of kept sums holds at least this many.
+int ensure_spool(ps_service* s, size_t spool_elems) {
   if (spool_elems > s->clip_spool_cap) {
     PS_CUDA(s, cudaDeviceSynchronize());
     if (s->clip_spool) PS_CUDA(s, cudaFree(s->clip_spool));
@@ -1392,34 +1431,34 @@ int ensure_clip(ps_service* s, size_t spool_elems) {
 // Launches the clipped kernel for the table `plan` of the blocks `idx` on `stream` itself (device current).
 int launch_clip(ps_service* s, const std::vector<int>& idx, Plan& plan, const ClipCall& call, cudaStream_t stream) {
   ++s->call_id;
-  int rc = ensure_clip(s, plan.spool);
+  int rc = ensure_spool(s, plan.spool);
   if (rc) return rc;
   PsClipHdr* h = reinterpret_cast<PsClipHdr*>(plan.bytes.data());
   h->max_norm = call.max_norm;
-  // one CTA per four units (1024 elements, one vector per thread) up to what is resident at once
-  const int grid = (int)std::max<unsigned long long>(
-      1, std::min<unsigned long long>((plan.total_chunks + 3ull) / 4, (unsigned long long)s->num_sms * s->clip_ctas));
-  const size_t segs = (size_t)h->n_tasks + (size_t)grid;
-  const size_t parts = segs + (size_t)grid * h->n_jobs;
+  const int grid = (int)std::min<unsigned long long>(plan.total_chunks, (unsigned long long)s->num_sms * s->clip_ctas);
   const bool inl = s->opt_inline && plan.bytes.size() <= kInlineBytes;
   Slot* sl = nullptr;
-  rc = acquire_slot(s, inl ? 0 : plan.bytes.size(), parts + (segs + 1) / 2, &sl);
+  rc = acquire_slot(s, inl ? 0 : plan.bytes.size(), plan.total_chunks, &sl);
   if (rc) return rc;
   const int slot_index = (int)(sl - s->slots);
   unsigned int waited = 0;
+  if (s->clip_slot >= 0) {                 // the last clipped launch uses the same memory
+    Slot& last = s->slots[s->clip_slot];
+    if (last.seq == s->clip_seq && !slot_finished(s, last)) {
+      PS_CUDA(s, cudaStreamWaitEvent(stream, last.done, 0));
+      waited = 1u << (unsigned)s->clip_slot;
+    }
+  }
   for (int bi : idx) {
     rc = order_after_block(s, s->blocks[bi], stream, &waited);
     if (rc) return rc;
   }
-  if (s->clip_recorded) PS_CUDA(s, cudaStreamWaitEvent(stream, s->clip_done, 0));
   const unsigned long long seq = s->launches + 1;
   unsigned long long* done_word = s->done_dev + slot_index;
-  double* job_parts = sl->partials + segs;
-  unsigned int* seg_at = reinterpret_cast<unsigned int*>(sl->partials + parts);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)grid);
   cfg.blockDim = dim3((unsigned)kThreads);
-  cfg.dynamicSmemBytes = kClipCache * sizeof(float);
+  cfg.dynamicSmemBytes = kClipSlot * sizeof(float);
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeCooperative;
@@ -1431,7 +1470,7 @@ int launch_clip(ps_service* s, const std::vector<int>& idx, Plan& plan, const Cl
     PsInlineTable tbl;
     std::memcpy(tbl.bytes, plan.bytes.data(), plan.bytes.size());
     le = cudaLaunchKernelEx(&cfg, ps_aggregate_clip_inline_kernel, tbl, (const PsJobDev*)s->jobs_dev, s->stats_dev,
-                            sl->partials, job_parts, seg_at, s->clip_spool, s->clip_bar, call.norms_out, s->status_dev,
+                            sl->partials, s->clip_spool, s->clip_shared, call.norms_out, s->status_dev,
                             s->exit_ctrs + slot_index, done_word, seq);
   } else {
     std::memcpy(sl->host, plan.bytes.data(), plan.bytes.size());
@@ -1439,8 +1478,8 @@ int launch_clip(ps_service* s, const std::vector<int>& idx, Plan& plan, const Cl
     PS_CUDA(s, cudaEventRecord(sl->copied, s->copy_stream));
     PS_CUDA(s, cudaStreamWaitEvent(stream, sl->copied, 0));
     le = cudaLaunchKernelEx(&cfg, ps_aggregate_clip_kernel, (const unsigned char*)sl->dev, (const PsJobDev*)s->jobs_dev,
-                            s->stats_dev, sl->partials, job_parts, seg_at, s->clip_spool, s->clip_bar, call.norms_out,
-                            s->status_dev, s->exit_ctrs + slot_index, done_word, seq);
+                            s->stats_dev, sl->partials, s->clip_spool, s->clip_shared, call.norms_out, s->status_dev,
+                            s->exit_ctrs + slot_index, done_word, seq);
   }
   if (le != cudaSuccess) {
     s->cuda_err = std::string("kernel launch: ") + cudaGetErrorString(le);
@@ -1456,8 +1495,8 @@ int launch_clip(ps_service* s, const std::vector<int>& idx, Plan& plan, const Cl
   sl->done_recorded = false;
   PS_CUDA(s, cudaEventRecord(sl->done, stream));
   sl->done_recorded = true;
-  PS_CUDA(s, cudaEventRecord(s->clip_done, stream));
-  s->clip_recorded = true;
+  s->clip_slot = slot_index;
+  s->clip_seq = seq;
   s->next_slot = (s->next_slot + 1) % kSlots;
   s->launches = seq;
   s->var_launches[kVarClip]++;
@@ -1578,7 +1617,8 @@ int ps_aggregate_clipped(ps_service* s, const ps_task* ready, int n_ready, float
   rc = flush_batch(s);                     // earlier rounds first
   if (rc) return rc;
   PS_CUDA(s, cudaSetDevice(s->device));
-  rc = build_clip_plan(s, s->idx, &s->plan);
+  rc = ensure_clip(s);
+  if (!rc) rc = build_clip_plan(s, s->idx, &s->plan);
   if (rc) return rc;
   return launch_clip(s, s->idx, s->plan, ClipCall{max_norm, norms_out}, static_cast<cudaStream_t>(stream_));
 }
@@ -1743,6 +1783,7 @@ static int round_run(ps_service* s, int round, const ClipCall* clip, void* strea
         const cudaError_t e = cudaSetDevice(s->device);
         if (e != cudaSuccess) { s->cuda_err = cudaGetErrorString(e); rc = PS_ERR_CUDA; }
       }
+      if (!rc) rc = ensure_clip(s);
       if (!rc && !reuse) {
         rc = build_clip_plan(s, r.idx, &plan);
         built = !rc;

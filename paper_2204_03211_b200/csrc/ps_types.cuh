@@ -39,12 +39,13 @@ struct __align__(16) PsTaskDev {       // 128 bytes, one per ready (job, block)
   unsigned int chunk_elems;            // elements per chunk of THIS task (multiple of 1024, or of row_len)
   unsigned int row_len;                // > 0: some shards of this task are row-sparse; elements per row
   unsigned int sparse_row;             // index of the task's first PsSparseDev entry (one per worker)
-  unsigned int _r2;
+  unsigned short job_slot;             // clipped launches: which of the launch's jobs
+  unsigned short reread;               // clipped launches: 1: the update reads the shards again
   // device-time profile of this task, filled only when the table asks for it
   unsigned long long busy_ns;          // sum over chunks of (chunk end - chunk start)      (uploaded as 0)
   unsigned long long t_first;          // earliest chunk start, %globaltimer ns             (uploaded as ~0)
   unsigned long long t_last;           // latest chunk end                                  (uploaded as 0)
-  unsigned long long _r3;
+  unsigned long long spool;            // clipped launches: where the task's sums start in the buffer
 };
 
 struct __align__(16) PsTableHdr {      // 48 bytes at the start of the table
