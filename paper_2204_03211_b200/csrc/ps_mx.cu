@@ -129,7 +129,7 @@ int quantize(const void* x, long long rows, long long cols, long long ld, MxOut 
   const long long nc = ROWS ? mx_atoms(cols) : (cols + 127) / 128, nr = COLS ? mx_atoms(rows) : (rows + 127) / 128;
   if (nc * nr > 0x7fffffffll) return PS_ERR_TOO_LARGE;
   const int vec_ok = !misaligned(x, 16) && (ld * (long long)sizeof(T)) % 16 == 0;
-  const size_t smem = COLS ? (size_t)kMxTile * kMxTile * sizeof(T) : 0;
+  const size_t smem = (size_t)kMxTile * kMxTile * sizeof(T);
   if (smem > 48 * 1024) {
     const cudaError_t e = cudaFuncSetAttribute(ps_mx_quantize_kernel<BF16, ROWS, COLS>,
                                                cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);

@@ -112,16 +112,17 @@ __device__ __forceinline__ void mx_pdl() {
 
 // ---------------------------------------------------------------- quantisation
 //
-// One CTA per 128 x 128 tile, i.e. one atom of scales in each direction.  Eight
-// elements per thread and step are read (128-bit loads where the row allows it);
-// along the rows a block then sits in four neighbouring lanes, whose maximum two
-// shuffles give, and is converted straight from registers.  For the columns the
-// tile goes through shared memory once: a thread takes one block of 32 rows of one
-// column (two columns of bf16, packed), so both directions cost one read of x.
-// The four row blocks of a column sit in one warp and are stored as 64 bytes; their
-// shared memory reads would meet in the same banks (a stride of 32 rows is a
-// multiple of 32 banks whatever the pitch), so the column index is permuted by the
-// row block.
+// One CTA per 128 x 128 tile, i.e. one atom of scales in each direction.  The tile
+// goes to shared memory with asynchronous 16-byte copies, all of them in flight at
+// once (read through registers, with a few loads in flight per thread, the kernel
+// waited for memory: 35 us for 8192 x 4096 bf16 both ways instead of 22.5); both
+// directions then cost one read of x.  Along the rows a block sits in four
+// neighbouring lanes (two shuffles give its maximum); along the columns a thread
+// takes one block of 32 rows of one column (a pair of columns of bf16) and reads it
+// twice, for the maximum and for the codes, which halves its registers.  The four
+// row blocks of a column sit in one warp and are stored as 64 bytes; their shared
+// memory reads would meet in the same banks (a stride of 32 rows is a multiple of 32
+// banks whatever the pitch), so the column index is permuted by the row block.
 
 constexpr int kQuantThreads = 256;
 
@@ -132,23 +133,23 @@ struct MxIn<false> { using T = float; };
 template <>
 struct MxIn<true> { using T = unsigned short; };
 
-template <bool BF16>
-__device__ __forceinline__ float mx_widen(typename MxIn<BF16>::T v) {
-  if constexpr (BF16) return __uint_as_float((unsigned int)v << 16);
-  else return v;
-}
-
 // Word of the tile in shared memory that holds column word c of row r.
 template <int WORDS>
 __device__ __forceinline__ int tile_word(int r, int c) { return r * WORDS + (c ^ (((r >> 5) & 3) << 3)); }
 
+__device__ __forceinline__ void copy16(unsigned int dst, const void* src, unsigned int bytes) {   // the rest is zeros
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+
 template <bool BF16, bool ROWS, bool COLS>
-__global__ void __launch_bounds__(kQuantThreads)
+__global__ void __launch_bounds__(kQuantThreads, BF16 ? 6 : 3)
 ps_mx_quantize_kernel(const typename MxIn<BF16>::T* __restrict__ x, long long rows, long long cols, long long ld,
                       int vec_ok, unsigned int col_tiles, MxOut out, MxOut out_t) {
   using T = typename MxIn<BF16>::T;
   constexpr int kWords = BF16 ? 64 : 128;                     // 32-bit words of a tile row
-  extern __shared__ unsigned int tile[];                      // COLS: 128 rows of kWords
+  constexpr int kPiece = 16 / sizeof(T);                      // elements of a copy
+  constexpr int kPieces = kMxTile / kPiece;                   // copies of a tile row
+  extern __shared__ __align__(16) unsigned int tile[];        // 128 rows of kWords
   __shared__ __align__(16) unsigned char s_row[kMxAtom], s_col[kMxAtom];
   const int tid = threadIdx.x;
   const long long rt = blockIdx.x / col_tiles, ct = blockIdx.x % col_tiles;
@@ -157,54 +158,49 @@ ps_mx_quantize_kernel(const typename MxIn<BF16>::T* __restrict__ x, long long ro
     if (ROWS) reinterpret_cast<unsigned int*>(s_row)[tid] = 0u;
     if (COLS) reinterpret_cast<unsigned int*>(s_col)[tid] = 0u;
   }
-  __syncthreads();
   mx_pdl();
 
-  // 16 lanes cover a row of the tile, 16 rows per step
-  const int g = tid & 15, rr = tid >> 4;
-  const long long c = c0 + g * 8;
-#pragma unroll 4
-  for (int step = 0; step < 8; ++step) {
-    const int tr = step * 16 + rr;
-    const long long r = r0 + tr;
-    float v[8];
-    uint4 raw = make_uint4(0, 0, 0, 0);
-    if (r < rows && c < cols) {
-      const T* p = x + (size_t)r * (size_t)ld + (size_t)c;
-      if (vec_ok && c + 8 <= cols) {
-        if constexpr (BF16) {
-          raw = *reinterpret_cast<const uint4*>(p);
-        } else {
-          const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-          v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-        }
+  {
+    constexpr int kStepRows = kQuantThreads / kPieces;
+    const int g = tid % kPieces, rr = tid / kPieces;
+    const long long c = c0 + g * kPiece;
+    const long long left = cols - c;                          // elements of this thread's pieces inside the matrix
+    const unsigned int n = left <= 0 ? 0u : left < kPiece ? (unsigned int)left : (unsigned int)kPiece;
+    const T* p = x + (size_t)(r0 + rr) * (size_t)ld + (size_t)c;
+#pragma unroll
+    for (int step = 0; step < kMxTile / kStepRows; ++step) {
+      const int tr = step * kStepRows + rr;
+      unsigned int* w = tile + tile_word<kWords>(tr, g * 4);
+      const unsigned int k = r0 + tr < rows ? n : 0u;
+      if (vec_ok) {
+        copy16((unsigned int)__cvta_generic_to_shared(w), k ? p : x, k * (unsigned int)sizeof(T));
       } else {
-        T t[8];
+        T t[kPiece];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) t[i] = c + i < cols ? p[i] : T(0);
-        if constexpr (BF16) {
-          raw = make_uint4(t[0] | (unsigned int)t[1] << 16, t[2] | (unsigned int)t[3] << 16,
-                           t[4] | (unsigned int)t[5] << 16, t[6] | (unsigned int)t[7] << 16);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = t[i];
-        }
+        for (int i = 0; i < kPiece; ++i) t[i] = (unsigned int)i < k ? p[i] : T(0);
+        if constexpr (BF16)
+          *reinterpret_cast<uint4*>(w) = make_uint4(t[0] | (unsigned int)t[1] << 16, t[2] | (unsigned int)t[3] << 16,
+                                                    t[4] | (unsigned int)t[5] << 16, t[6] | (unsigned int)t[7] << 16);
+        else
+          *reinterpret_cast<float4*>(w) = make_float4(t[0], t[1], t[2], t[3]);
       }
-    } else if constexpr (!BF16) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = 0.f;
+      p += (size_t)kStepRows * (size_t)ld;
     }
-    if constexpr (COLS) {
-      if constexpr (BF16) {
-        *reinterpret_cast<uint4*>(tile + tile_word<kWords>(tr, g * 4)) = raw;
-      } else {
-        *reinterpret_cast<float4*>(tile + tile_word<kWords>(tr, g * 8)) = make_float4(v[0], v[1], v[2], v[3]);
-        *reinterpret_cast<float4*>(tile + tile_word<kWords>(tr, g * 8 + 4)) = make_float4(v[4], v[5], v[6], v[7]);
-      }
-    }
-    if constexpr (ROWS) {
+    asm volatile("cp.async.wait_all;" ::: "memory");
+  }
+  __syncthreads();
+
+  if constexpr (ROWS) {
+    // 16 lanes cover a row of the tile, 16 rows per step
+    const int g = tid & 15, rr = tid >> 4;
+    const long long c = c0 + g * 8;
+    uint8_t* codes = out.codes + (size_t)(r0 + rr) * (size_t)mx_pitch(cols) + (size_t)(c >> 1);
+#pragma unroll 2
+    for (int step = 0; step < 8; ++step) {
+      const int tr = step * 16 + rr;
       unsigned int sb, q;
       if constexpr (BF16) {
+        const uint4 raw = *reinterpret_cast<const uint4*>(tile + tile_word<kWords>(tr, g * 4));
         const unsigned int w[4] = {raw.x, raw.y, raw.z, raw.w};
         unsigned int m = max_abs_bf16x2(max_abs_bf16x2(w[0], w[1]), max_abs_bf16x2(w[2], w[3]));
         m = max_abs_bf16x2(m, __shfl_xor_sync(0xffffffffu, m, 1));
@@ -213,51 +209,54 @@ ps_mx_quantize_kernel(const typename MxIn<BF16>::T* __restrict__ x, long long ro
         sb = mx_scale_byte((m >> 7) & 0xffu);
         q = mx_codes8(w, ((254u - sb) << 7) * 0x10001u);
       } else {
+        const float4 a = *reinterpret_cast<const float4*>(tile + tile_word<kWords>(tr, g * 8));
+        const float4 b = *reinterpret_cast<const float4*>(tile + tile_word<kWords>(tr, g * 8 + 4));
+        const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
         float m = max_abs(max_abs(max_abs(v[0], v[1]), max_abs(v[2], v[3])), max_abs(max_abs(v[4], v[5]), max_abs(v[6], v[7])));
         m = max_abs(m, __shfl_xor_sync(0xffffffffu, m, 1));
         m = max_abs(m, __shfl_xor_sync(0xffffffffu, m, 2));
         sb = mx_scale_byte((__float_as_uint(m) >> 23) & 0xffu);
         q = mx_codes8(v, mx_inverse(sb));
       }
-      if (r < rows && (c & ~31ll) < cols) {
-        *reinterpret_cast<unsigned int*>(out.codes + (size_t)r * (size_t)mx_pitch(cols) + (size_t)(c >> 1)) = q;
+      if (r0 + tr < rows && (c & ~31ll) < cols) {
+        *reinterpret_cast<unsigned int*>(codes) = q;
         if ((g & 3) == 0) s_row[(tr & 31) * 16 + (tr >> 5) * 4 + (g >> 2)] = (unsigned char)sb;
       }
+      codes += 16 * (size_t)mx_pitch(cols);
     }
   }
-  __syncthreads();
   if constexpr (COLS) {
     // thread: row block rb of one column (fp32) or of a pair of columns (bf16)
     const int rb = (tid >> 3) & 3;
     const bool any = r0 + rb * 32 < rows;
+    uint8_t* codes = out_t.codes + (size_t)(r0 / 2 + rb * 16);
     if constexpr (BF16) {
       const int cw = (tid & 7) + (tid >> 5) * 8;              // word = pair of columns
-      unsigned int w[32];
+      const unsigned int* w = tile + tile_word<kWords>(rb * 32, cw);    // (the permutation is the same in all 32 rows)
+      unsigned int m = 0u;
 #pragma unroll
-      for (int i = 0; i < 32; ++i) w[i] = tile[tile_word<kWords>(rb * 32 + i, cw)];
-      unsigned int m = max_abs_bf16x2(w[0], w[1]);
-#pragma unroll
-      for (int i = 2; i < 32; ++i) m = max_abs_bf16x2(m, w[i]);
+      for (int i = 0; i < 32; ++i) m = max_abs_bf16x2(m, w[i * kWords]);
       const unsigned int sb[2] = {mx_scale_byte((m >> 7) & 0xffu), mx_scale_byte((m >> 23) & 0xffu)};
       const unsigned int inv = (((254u - sb[0]) << 7) & 0xffffu) | ((254u - sb[1]) << 23);
+      unsigned int lo[4], hi[4];
 #pragma unroll
-      for (int i = 0; i < 32; ++i) w[i] = mul_bf16x2(w[i], inv);
+      for (int k = 0; k < 4; ++k) {
+        float a[8], b[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const unsigned int q = mul_bf16x2(w[(k * 8 + i) * kWords], inv);
+          a[i] = __uint_as_float(q << 16);
+          b[i] = __uint_as_float(q & 0xffff0000u);
+        }
+        lo[k] = mx_pack8(a);
+        hi[k] = mx_pack8(b);
+      }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int tc = 2 * cw + h;
-        uint4 q;
-        unsigned int* qp = reinterpret_cast<unsigned int*>(&q);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          float v[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            v[i] = __uint_as_float(h ? w[k * 8 + i] & 0xffff0000u : w[k * 8 + i] << 16);
-          qp[k] = mx_pack8(v);
-        }
         if (any && c0 + tc < cols) {
-          *reinterpret_cast<uint4*>(out_t.codes + (size_t)(c0 + tc) * (size_t)mx_pitch(rows) +
-                                    (size_t)(r0 / 2 + rb * 16)) = q;
+          *reinterpret_cast<uint4*>(codes + (size_t)(c0 + tc) * (size_t)mx_pitch(rows)) =
+              h ? make_uint4(hi[0], hi[1], hi[2], hi[3]) : make_uint4(lo[0], lo[1], lo[2], lo[3]);
           s_col[(tc & 31) * 16 + (tc >> 5) * 4 + rb] = (unsigned char)sb[h];
         }
       }
@@ -265,32 +264,28 @@ ps_mx_quantize_kernel(const typename MxIn<BF16>::T* __restrict__ x, long long ro
 #pragma unroll 1
       for (int h = 0; h < 2; ++h) {
         const int tc = (tid & 7) + (tid >> 5) * 8 + h * 64;
-        float v[32], m = 0.f;
+        const float* w = reinterpret_cast<const float*>(tile) + tile_word<kWords>(rb * 32, tc);
+        float m = 0.f;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          v[i] = __uint_as_float(tile[tile_word<kWords>(rb * 32 + i, tc)]);
-          m = max_abs(m, v[i]);
-        }
+        for (int i = 0; i < 32; ++i) m = max_abs(m, w[i * kWords]);
         const unsigned int sb = mx_scale_byte((__float_as_uint(m) >> 23) & 0xffu);
         const float inv = mx_inverse(sb);
-        uint4 q;
-        unsigned int* qp = reinterpret_cast<unsigned int*>(&q);
+        unsigned int q[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           float u[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) u[i] = v[k * 8 + i];
-          qp[k] = mx_codes8(u, inv);
+          for (int i = 0; i < 8; ++i) u[i] = w[(k * 8 + i) * kWords];
+          q[k] = mx_codes8(u, inv);
         }
         if (any && c0 + tc < cols) {
-          *reinterpret_cast<uint4*>(out_t.codes + (size_t)(c0 + tc) * (size_t)mx_pitch(rows) +
-                                    (size_t)(r0 / 2 + rb * 16)) = q;
+          *reinterpret_cast<uint4*>(codes + (size_t)(c0 + tc) * (size_t)mx_pitch(rows)) = make_uint4(q[0], q[1], q[2], q[3]);
           s_col[(tc & 31) * 16 + (tc >> 5) * 4 + rb] = (unsigned char)sb;
         }
       }
     }
-    __syncthreads();
   }
+  __syncthreads();
   // the atoms; tiles past the end exist to write the padding atoms' zeros
   if (tid < kMxAtom / 16) {
     if (ROWS && r0 < rows && ct < mx_atoms(cols))
