@@ -5,7 +5,7 @@
 #include <mutex>
 #include <string>
 
-#include "ps_mx_gemm.cuh"
+#include "ps_mx_pair.cuh"
 #include "ps_op.h"
 
 namespace psb {
@@ -71,7 +71,8 @@ int mx_device(const OpDevice& d, int** status) {
     if (e == cudaSuccess) e = allow_smem<16>();
     if (e == cudaSuccess) e = allow_smem<64>();
     if (e == cudaSuccess) e = allow_smem<128>();
-    if (e == cudaSuccess) e = allow_smem<256>();
+    if (e == cudaSuccess)
+      e = cudaFuncSetAttribute(ps_mx_matmul_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPairSmem);
     if (e == cudaSuccess && !g_encode) {
       void* fn = nullptr;
       cudaDriverEntryPointQueryResult q;
@@ -146,6 +147,30 @@ bool make_map(CUtensorMap* m, const ps_mx* q, int box_rows) {
   return g_encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, q->codes, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Atoms of scales, two (a stage's) at a time.
+bool make_scale_map(CUtensorMap* m, const ps_mx* q) {
+  const cuuint64_t dims[2] = {kMxAtom / 4, (cuuint64_t)((q->rows + 127) / 128 * mx_atoms(q->cols))};
+  const cuuint64_t strides[1] = {kMxAtom};
+  const cuuint32_t box[2] = {kMxAtom / 4, 2}, step[2] = {1, 1};
+  return g_encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, q->scales, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int matmul_pair(const ps_mx* a, const ps_mx* b, MmArgs args, const OpDevice& d, cudaStream_t stream) {
+  CUtensorMap ma, mb, msa, msb;
+  if (!make_map(&ma, a, 128) || !make_map(&mb, b, 128) || !make_scale_map(&msa, a) || !make_scale_map(&msb, b))
+    return op_cuda_error("tensor map", cudaErrorInvalidValue);
+  const long long tp = (a->rows + kPairTile - 1) / kPairTile, tq = (b->rows + kPairTile - 1) / kPairTile;
+  if (tp * tq > 0x3fffffffll || std::max(tp, tq) * 2 * args.atoms > 0x7fffffffll) return PS_ERR_TOO_LARGE;
+  args.tiles_p = (int)tp;
+  args.tiles_q = (int)tq;
+  // 256-bit stores where C's rows allow them
+  if (args.vec_ok && !misaligned(args.c, 32) && (args.ldc * (args.out_f32 ? 4 : 2)) % 32 == 0) args.vec_ok = 2;
+  const unsigned int grid = 2u * (unsigned)std::min<long long>(tp * tq, d.num_sms / 2);
+  return launch("4-bit product", ps_mx_matmul_pair_kernel, grid, kPairThreads, kPairSmem, 1, stream, ma, mb, msa, msb, args);
 }
 
 template <int BN>
@@ -253,9 +278,9 @@ int ps_mx_matmul(const ps_mx* a, const ps_mx* b, int dtype, void* c, long long l
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
   if (thin && q->rows <= 16) return matmul<16>(p, q, args, d, stream);
   if (thin) return matmul<64>(p, q, args, d, stream);
-  // wide tiles read each operand less often; they are taken once they fill the device
-  const long long wide = ((p->rows + 127) / 128) * ((q->rows + 255) / 256);
-  if (wide >= d.num_sms) return matmul<256>(p, q, args, d, stream);
+  // the pair's tiles read each operand less often; they are taken once they fill the device
+  const long long pairs = ((p->rows + 255) / 256) * ((q->rows + 255) / 256);
+  if (pairs >= d.num_sms / 2 - 12) return matmul_pair(p, q, args, d, stream);
   return matmul<128>(p, q, args, d, stream);
 }
 

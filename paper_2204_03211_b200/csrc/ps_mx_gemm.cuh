@@ -7,9 +7,14 @@
 // per pipeline stage: a stage is 128 and BN rows of 128 bytes (TMA, 128-byte
 // swizzle) and their atoms of scales (plain bulk copies; the quantiser stores
 // them in the order in which scale memory takes them).
-//   warp 0     one lane issues the copies
+//   warp 0     one lane issues the copies of codes
 //   warp 1     one lane copies the scales to tensor memory and issues the MMAs
 //   warps 2-5  read the accumulators and store the result
+//   warp 6     one lane issues the copies of scales
+// A stage is 512 cycles of MMA at most, and what a single lane issues for it is of
+// that order (a ready barrier alone costs about 100): the lanes are elected, which
+// lets their operands live in uniform registers, addresses advance by addition, and
+// the copies are spread over two warps.
 // Where one operand has few rows (single tokens) it is Q and the other, usually
 // the weight, P, whichever of A and B that is: the MMA's 128 rows are then full
 // and what is left is reading P once.  Such a product has few tiles, so the CTAs
@@ -23,7 +28,7 @@
 
 namespace psb {
 
-constexpr int kMmThreads = 192;
+constexpr int kMmThreads = 224;
 constexpr int kMmP = 128;                       // rows of P in a tile
 constexpr int kMmStageK = 256;                  // elements of K in a stage: 128 bytes of codes, 2 atoms of scales
 constexpr int kMmMaxStages = 8;
@@ -31,17 +36,17 @@ constexpr int kMmSmem = 227 * 1024;
 
 template <int BN>
 struct MmCfg {
-  static constexpr int kQBlocks = (BN + 127) / 128;             // 128-row blocks of scales of Q
   static constexpr int kBytesP = kMmP * 128, kBytesQ = BN * 128;
   static constexpr int kBytesS = 2 * kMxAtom;                   // scales of one 128-row block in a stage
-  static constexpr int kStage = kBytesP + kBytesQ + kBytesS * (1 + kQBlocks);
+  static constexpr int kStage = kBytesP + kBytesQ + 2 * kBytesS;
   static constexpr int kFit = (kMmSmem - 2048) / kStage;
   static constexpr int kStages = kFit < kMmMaxStages ? kFit : kMmMaxStages;
-  static constexpr int kAcc = BN <= 128 ? 2 : 1;                // accumulators: two hide the epilogue; 256 columns leave room for one
+  static constexpr int kAcc = 2;                                // accumulators: the second hides the epilogue
   static constexpr int kScaleCol = kAcc * BN;                   // tensor memory: accumulators, then two sets of scales
-  static constexpr int kScaleSet = 8 + 8 * kQBlocks;
+  static constexpr int kScaleSet = 16;
   static constexpr int kCols = kScaleCol + 2 * kScaleSet;
   static constexpr int kAlloc = kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
+  static_assert(BN <= 128, "one block of scales per operand");
   static constexpr int kSmem = 1024 + kStages * kStage;
   static_assert(kStages >= 3 && kCols <= 512 && kStage % 1024 == 0, "tile does not fit");
 };
@@ -66,6 +71,19 @@ constexpr long long kMmWaitCycles = 2000000000ll;     // about a second
 
 __device__ __forceinline__ unsigned int mm_smem(const void* p) {
   return static_cast<unsigned int>(__cvta_generic_to_shared(p));
+}
+
+// One lane of the (converged) warp; the compiler knows that it is one.
+__device__ __forceinline__ bool mm_elect() {
+  unsigned int p;
+  asm volatile(
+      "{\n\t"
+      ".reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t"
+      "}"
+      : "=r"(p));
+  return p != 0;
 }
 
 __device__ __forceinline__ bool mm_try_wait(unsigned int bar, unsigned int parity) {
@@ -112,6 +130,15 @@ __device__ __forceinline__ void mm_commit(unsigned int bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 
+// The stage that comes next, and the parity of its barriers.
+template <int STAGES>
+struct MmCursor {
+  unsigned int s = 0, parity = 0;
+  __device__ __forceinline__ void next() {
+    if (++s == STAGES) { s = 0; parity ^= 1u; }
+  }
+};
+
 // Shared memory descriptors: rows of 128 bytes in 128-byte swizzle (8-row groups 1024 bytes apart), and an atom of
 // scales, 32 rows of 16 bytes (8-row groups 128 bytes apart, no swizzle).
 __device__ __forceinline__ unsigned long long mm_desc_codes(unsigned int addr) {
@@ -121,8 +148,8 @@ __device__ __forceinline__ unsigned long long mm_desc_scales(unsigned int addr) 
   return (unsigned long long)((addr & 0x3ffffu) >> 4) | (1ull << 16) | (8ull << 32) | (1ull << 46);
 }
 
-__device__ __forceinline__ void mm_copy_scales(unsigned int tmem, unsigned int smem) {
-  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(mm_desc_scales(smem)) : "memory");
+__device__ __forceinline__ void mm_copy_scales(unsigned int tmem, unsigned long long desc) {
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
 }
 
 __device__ __forceinline__ void mm_mma(unsigned int d, unsigned long long a, unsigned long long b, unsigned int idesc,
@@ -273,11 +300,11 @@ ps_mx_matmul_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_cons
   __shared__ unsigned int s_tmem;
   unsigned char* stages = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   const unsigned int base = mm_smem(stages);
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
 
   if (tid == 0) {
     for (int s = 0; s < Cfg::kStages; ++s) {
-      asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(mm_smem(&s_full[s])) : "memory");
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], 2;" ::"r"(mm_smem(&s_full[s])) : "memory");
       asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(mm_smem(&s_empty[s])) : "memory");
     }
     for (int b = 0; b < Cfg::kAcc; ++b) {
@@ -307,71 +334,73 @@ ps_mx_matmul_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_cons
   const int k0 = (int)((long long)args.stages_k * rank / args.splits);
   const int k1 = (int)((long long)args.stages_k * (rank + 1) / args.splits);
 
-  if (warp == 0) {
-    if (lane == 0) {
-      unsigned int it = 0;
+  if (warp == 0 || warp == 6) {
+    // the two producers wait for a stage, arm its barrier with their own bytes and issue their copies
+    if (mm_elect()) {
+      MmCursor<Cfg::kStages> at;
+      unsigned int issued = 0;
       bool ok = true;
       for (int tile = first; ok && tile < tiles; tile += stride) {
         int tp, tq;
         mm_tile(args, tile, &tp, &tq);
-        const uint8_t* sp = args.sp + (size_t)tp * (size_t)args.atoms * kMxAtom;
-        const uint8_t* sq = args.sq + (size_t)tq * Cfg::kQBlocks * (size_t)args.atoms * kMxAtom;
-        // (the last tile of Q may have no second block of scales; its columns are never stored)
-        const int qb = min(Cfg::kQBlocks, (int)((args.rows_q - (long long)tq * BN + 127) >> 7));
-        const unsigned int bytes = Cfg::kBytesP + Cfg::kBytesQ + Cfg::kBytesS * (1 + qb);
-        for (int k = k0; k < k1; ++k, ++it) {
-          const unsigned int s = it % Cfg::kStages, use = it / Cfg::kStages;
-          if (use > 0 && !mm_wait(mm_smem(&s_empty[s]), (use - 1) & 1u, args.status)) { ok = false; break; }
-          const unsigned int bar = mm_smem(&s_full[s]), at = base + s * Cfg::kStage;
-          asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-          mm_tma(at, &map_p, k * 128, tp * kMmP, bar);
-          mm_tma(at + Cfg::kBytesP, &map_q, k * 128, tq * BN, bar);
-          const unsigned int sc = at + Cfg::kBytesP + Cfg::kBytesQ;
-          mm_bulk(sc, sp + (size_t)k * Cfg::kBytesS, Cfg::kBytesS, bar);
-          for (int b = 0; b < qb; ++b)
-            mm_bulk(sc + Cfg::kBytesS * (1 + b), sq + ((size_t)b * (size_t)args.atoms * kMxAtom + (size_t)k * Cfg::kBytesS),
-                    Cfg::kBytesS, bar);
+        if (warp == 0) {
+          for (int k = k0; k < k1; ++k, at.next(), ++issued) {
+            if (!mm_wait(mm_smem(&s_empty[0]) + 8 * at.s, at.parity ^ 1u, args.status)) { ok = false; break; }
+            const unsigned int bar = mm_smem(&s_full[0]) + 8 * at.s, dst = base + at.s * Cfg::kStage;
+            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "n"(Cfg::kBytesP + Cfg::kBytesQ)
+                         : "memory");
+            mm_tma(dst, &map_p, k * 128, tp * kMmP, bar);
+            mm_tma(dst + Cfg::kBytesP, &map_q, k * 128, tq * BN, bar);
+          }
+        } else {
+          const uint8_t* sp = args.sp + ((size_t)tp * (size_t)args.atoms + 2 * (size_t)k0) * kMxAtom;
+          const uint8_t* sq = args.sq + ((size_t)tq * (size_t)args.atoms + 2 * (size_t)k0) * kMxAtom;
+          for (int k = k0; k < k1; ++k, at.next(), ++issued, sp += Cfg::kBytesS, sq += Cfg::kBytesS) {
+            if (!mm_wait(mm_smem(&s_empty[0]) + 8 * at.s, at.parity ^ 1u, args.status)) { ok = false; break; }
+            const unsigned int bar = mm_smem(&s_full[0]) + 8 * at.s;
+            const unsigned int dst = base + at.s * Cfg::kStage + Cfg::kBytesP + Cfg::kBytesQ;
+            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "n"(2 * Cfg::kBytesS) : "memory");
+            mm_bulk(dst, sp, Cfg::kBytesS, bar);
+            mm_bulk(dst + Cfg::kBytesS, sq, Cfg::kBytesS, bar);
+          }
         }
       }
-      if (!ok)                                        // an expired wait: let this CTA's own copies land
-        for (unsigned int s = 0; s < (unsigned)Cfg::kStages && s < it; ++s)
-          mm_wait(mm_smem(&s_full[s]), ((it - 1 - s) / Cfg::kStages) & 1u, args.status);
+      if (!ok)                                        // an expired wait: let the copies in flight land
+        for (unsigned int s = 0; s < (unsigned)Cfg::kStages && s < issued; ++s)
+          mm_wait(mm_smem(&s_full[s]), ((issued - 1 - s) / Cfg::kStages) & 1u, args.status);
     }
     __syncwarp();
   } else if (warp == 1) {
-    if (lane == 0) {
+    if (mm_elect()) {
       constexpr unsigned int kIdesc = (1u << 7) | (1u << 10) | ((unsigned)(BN >> 3) << 17) | (1u << 23) | (8u << 24);
-      unsigned int it = 0, n = 0;
+      MmCursor<Cfg::kStages> at;
+      MmCursor<Cfg::kAcc> acc;
+      unsigned int set = 0;
       bool ok = true;
-      for (int tile = first; ok && tile < tiles; tile += stride, ++n) {
-        const unsigned int buf = n % Cfg::kAcc, use = n / Cfg::kAcc;
-        if (use > 0 && !mm_wait(mm_smem(&s_acc_empty[buf]), (use - 1) & 1u, args.status)) break;
+      for (int tile = first; ok && tile < tiles; tile += stride, acc.next()) {
+        if (!mm_wait(mm_smem(&s_acc_empty[0]) + 8 * acc.s, acc.parity ^ 1u, args.status)) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        for (int k = k0; k < k1; ++k, ++it) {
-          const unsigned int s = it % Cfg::kStages;
-          if (!mm_wait(mm_smem(&s_full[s]), (it / Cfg::kStages) & 1u, args.status)) { ok = false; break; }
+        const unsigned int d = tmem + acc.s * BN;
+        for (int k = k0; k < k1; ++k, at.next(), set ^= Cfg::kScaleSet) {
+          if (!mm_wait(mm_smem(&s_full[0]) + 8 * at.s, at.parity, args.status)) { ok = false; break; }
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          const unsigned int at = base + s * Cfg::kStage, sc = at + Cfg::kBytesP + Cfg::kBytesQ;
-          const unsigned int tp = tmem + Cfg::kScaleCol + (it & 1u) * Cfg::kScaleSet, tq = tp + 8;
-          // scales: atom j of P in 4 columns; atom j of Q's blocks side by side
+          const unsigned long long dp = mm_desc_codes(base + at.s * Cfg::kStage);
+          const unsigned long long ds = mm_desc_scales(base + at.s * Cfg::kStage + Cfg::kBytesP + Cfg::kBytesQ);
+          const unsigned int tp = tmem + Cfg::kScaleCol + set, tq = tp + 8;
+          // scales: atom j of P and of Q, four columns each (a descriptor counts in 16 bytes)
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            mm_copy_scales(tp + j * 4, sc + j * kMxAtom);
-#pragma unroll
-            for (int b = 0; b < Cfg::kQBlocks; ++b)
-              mm_copy_scales(tq + (j * Cfg::kQBlocks + b) * 4, sc + Cfg::kBytesS * (1 + b) + j * kMxAtom);
+            mm_copy_scales(tp + j * 4, ds + j * (kMxAtom / 16));
+            mm_copy_scales(tq + j * 4, ds + (Cfg::kBytesS + j * kMxAtom) / 16);
           }
-          const unsigned long long dp = mm_desc_codes(at), dq = mm_desc_codes(at + Cfg::kBytesP);
           // four MMAs of 64 elements (32 bytes) each; an atom serves two, which name its lower or upper pair of scales
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const unsigned int id = kIdesc | ((unsigned)(i & 1) << 30) | ((unsigned)(i & 1) << 5);
-            mm_mma(tmem + buf * BN, dp + 2 * i, dq + 2 * i, id, tp + (i >> 1) * 4, tq + (i >> 1) * 4 * Cfg::kQBlocks,
-                   k > k0 || i > 0);
-          }
-          mm_commit(mm_smem(&s_empty[s]));
+          for (int i = 0; i < 4; ++i)
+            mm_mma(d, dp + 2 * i, dp + Cfg::kBytesP / 16 + 2 * i, kIdesc | ((unsigned)(i & 1) << 30) | ((unsigned)(i & 1) << 5),
+                   tp + (i >> 1) * 4, tq + (i >> 1) * 4, k > k0 || i > 0);
+          mm_commit(mm_smem(&s_empty[0]) + 8 * at.s);
         }
-        mm_commit(mm_smem(&s_acc_full[buf]));
+        mm_commit(mm_smem(&s_acc_full[0]) + 8 * acc.s);
       }
     }
     __syncwarp();
