@@ -167,8 +167,6 @@ int matmul_pair(const ps_mx* a, const ps_mx* b, MmArgs args, const OpDevice& d, 
   if (tp * tq > 0x3fffffffll || std::max(tp, tq) * 2 * args.atoms > 0x7fffffffll) return PS_ERR_TOO_LARGE;
   args.tiles_p = (int)tp;
   args.tiles_q = (int)tq;
-  // 256-bit stores where C's rows allow them
-  if (args.vec_ok && !misaligned(args.c, 32) && (args.ldc * (args.out_f32 ? 4 : 2)) % 32 == 0) args.vec_ok = 2;
   const unsigned int grid = 2u * (unsigned)std::min<long long>(tp * tq, d.num_sms / 2);
   return launch("4-bit product", ps_mx_matmul_pair_kernel, grid, kPairThreads, kPairSmem, 1, stream, ma, mb, msa, msb, args);
 }

@@ -33,13 +33,14 @@ constexpr int kMmP = 128;                       // rows of P in a tile
 constexpr int kMmStageK = 256;                  // elements of K in a stage: 128 bytes of codes, 2 atoms of scales
 constexpr int kMmMaxStages = 8;
 constexpr int kMmSmem = 227 * 1024;
+constexpr int kMmStaging = 2048;                // bytes of an epilogue warp's staging for stores
 
 template <int BN>
 struct MmCfg {
   static constexpr int kBytesP = kMmP * 128, kBytesQ = BN * 128;
   static constexpr int kBytesS = 2 * kMxAtom;                   // scales of one 128-row block in a stage
   static constexpr int kStage = kBytesP + kBytesQ + 2 * kBytesS;
-  static constexpr int kFit = (kMmSmem - 2048) / kStage;
+  static constexpr int kFit = (kMmSmem - 2048 - 4 * kMmStaging) / kStage;  // four warps' staging beside the stages
   static constexpr int kStages = kFit < kMmMaxStages ? kFit : kMmMaxStages;
   static constexpr int kAcc = 2;                                // accumulators: the second hides the epilogue
   static constexpr int kScaleCol = kAcc * BN;                   // tensor memory: accumulators, then two sets of scales
@@ -47,7 +48,7 @@ struct MmCfg {
   static constexpr int kCols = kScaleCol + 2 * kScaleSet;
   static constexpr int kAlloc = kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
   static_assert(BN <= 128, "one block of scales per operand");
-  static constexpr int kSmem = 1024 + kStages * kStage;
+  static constexpr int kSmem = 1024 + kStages * kStage + 4 * kMmStaging;
   static_assert(kStages >= 3 && kCols <= 512 && kStage % 1024 == 0, "tile does not fit");
 };
 
@@ -164,8 +165,8 @@ __device__ __forceinline__ void mm_mma(unsigned int d, unsigned long long a, uns
       : "memory");
 }
 
-// 32 columns of this warp's 32 lanes.
-__device__ __forceinline__ void mm_load32(unsigned int tmem, float (&v)[32]) {
+// 32 or 16 columns of this warp's 32 lanes, without waiting for them.
+__device__ __forceinline__ void mm_load32(unsigned int tmem, float* v) {
   unsigned int* u = reinterpret_cast<unsigned int*>(v);
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
@@ -176,9 +177,8 @@ __device__ __forceinline__ void mm_load32(unsigned int tmem, float (&v)[32]) {
         "=r"(u[17]), "=r"(u[18]), "=r"(u[19]), "=r"(u[20]), "=r"(u[21]), "=r"(u[22]), "=r"(u[23]), "=r"(u[24]),
         "=r"(u[25]), "=r"(u[26]), "=r"(u[27]), "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
       : "r"(tmem));
-  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
-__device__ __forceinline__ void mm_load16(unsigned int tmem, float (&v)[16]) {
+__device__ __forceinline__ void mm_load16(unsigned int tmem, float* v) {
   unsigned int* u = reinterpret_cast<unsigned int*>(v);
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
@@ -186,12 +186,16 @@ __device__ __forceinline__ void mm_load16(unsigned int tmem, float (&v)[16]) {
       : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]),
         "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15])
       : "r"(tmem));
-  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 template <int N>
 __device__ __forceinline__ void mm_load(unsigned int tmem, float (&v)[N]) {
-  if constexpr (N == 32) mm_load32(tmem, v);
-  else mm_load16(tmem, v);
+  if constexpr (N == 16) {
+    mm_load16(tmem, v);
+  } else {
+#pragma unroll
+    for (int c = 0; c < N; c += 32) mm_load32(tmem + c, v + c);
+  }
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
 __device__ __forceinline__ unsigned int mm_bf16x2(float lo, float hi) {
@@ -206,31 +210,89 @@ __device__ __forceinline__ void mm_store1(const MmArgs& a, long long m, long lon
   else static_cast<unsigned short*>(a.c)[at] = (unsigned short)mm_bf16x2(v, 0.f);
 }
 
-// Stores N consecutive accumulators (rows q.. of Q) of P's row p.
-template <int N>
-__device__ __forceinline__ void mm_store(const MmArgs& a, long long p, long long q, const float (&v)[N]) {
-  if (p >= a.rows_p) return;
-  if (a.swap) {                                  // a warp's lanes are neighbours in C
+// A warp's 32 rows (m0.. of C) of COLS columns (n..), row `lane` in this lane's v, through 2 KB of shared memory, 16 rows
+// at a time: rows of up to 128 bytes in 16-byte pieces, permuted by the row so that neither side meets in a bank.
+// Stored straight from the registers, a warp's store touches 32 lines, and that was what products of short K waited for
+// (8192 x 4096 x 1024: 22.7 us, and 56 us where C's rows allow no wide stores, against 19.1 us).
+template <int COLS, bool F32>
+__device__ __forceinline__ void mm_store_rows_as(const MmArgs& a, unsigned char* buf, int lane, long long m0, long long n,
+                                                 long long rows, long long cols, const float* v) {
+  constexpr int kEs = F32 ? 4 : 2, kRow = COLS * kEs, kPieces = kRow / 16, kStep = 32 / kPieces;
+  static_assert(kRow <= 128 && 16 * kRow <= kMmStaging && (kPieces & (kPieces - 1)) == 0, "staging row");
+  const int live = (int)min(32ll, rows - m0);                 // rows of the warp inside C
+  const int live_cols = (int)min((long long)COLS, cols - n);
+  const bool wide = a.vec_ok && live_cols == COLS;
+  const int each = lane / kPieces, piece = lane % kPieces;
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (q + i < a.rows_q) mm_store1(a, q + i, p, v[i]);
-  } else if (a.vec_ok && q + N <= a.rows_q) {
-    if (a.out_f32) {
-      float4* o = reinterpret_cast<float4*>(static_cast<float*>(a.c) + (size_t)p * (size_t)a.ldc + (size_t)q);
+  for (int h = 0; h < 2; ++h) {
+    const int r0 = h * 16;
+    if ((lane >> 4) == h) {
+      uint4* mine = reinterpret_cast<uint4*>(buf + (lane & 15) * kRow);
 #pragma unroll
-      for (int i = 0; i < N / 4; ++i) o[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-    } else {
-      uint4* o = reinterpret_cast<uint4*>(static_cast<unsigned short*>(a.c) + (size_t)p * (size_t)a.ldc + (size_t)q);
-#pragma unroll
-      for (int i = 0; i < N / 8; ++i)
-        o[i] = make_uint4(mm_bf16x2(v[8 * i], v[8 * i + 1]), mm_bf16x2(v[8 * i + 2], v[8 * i + 3]),
-                          mm_bf16x2(v[8 * i + 4], v[8 * i + 5]), mm_bf16x2(v[8 * i + 6], v[8 * i + 7]));
+      for (int i = 0; i < kPieces; ++i) {
+        if constexpr (F32)
+          mine[i ^ (lane & (kPieces - 1))] = make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]),
+                                                        __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
+        else
+          mine[i ^ (lane & (kPieces - 1))] =
+              make_uint4(mm_bf16x2(v[8 * i], v[8 * i + 1]), mm_bf16x2(v[8 * i + 2], v[8 * i + 3]),
+                         mm_bf16x2(v[8 * i + 4], v[8 * i + 5]), mm_bf16x2(v[8 * i + 6], v[8 * i + 7]));
+      }
     }
-  } else {
+    __syncwarp();
+    if (wide) {
+      unsigned char* o = static_cast<unsigned char*>(a.c) + ((size_t)(m0 + r0 + each) * (size_t)a.ldc + (size_t)n) * kEs + piece * 16;
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (q + i < a.rows_q) mm_store1(a, p, q + i, v[i]);
+      for (int r = 0; r < 16; r += kStep) {
+        const int row = r + each;
+        const uint4 q = *reinterpret_cast<const uint4*>(buf + row * kRow + ((piece ^ (row & (kPieces - 1))) << 4));
+        if (r0 + row < live) *reinterpret_cast<uint4*>(o + (size_t)r * (size_t)a.ldc * kEs) = q;
+      }
+    } else {
+#pragma unroll 4
+      for (int r = 0; r < 16; ++r) {
+        const size_t at = (size_t)(m0 + r0 + r) * (size_t)a.ldc + (size_t)n;
+#pragma unroll
+        for (int c0 = 0; c0 < COLS; c0 += 32) {
+          const int c = c0 + lane;
+          if (r0 + r < live && c < live_cols) {
+            const unsigned char* e = buf + r * kRow + ((((c * kEs) >> 4) ^ (r & (kPieces - 1))) << 4) + ((c * kEs) & 15);
+            if constexpr (F32) static_cast<float*>(a.c)[at + c] = *reinterpret_cast<const float*>(e);
+            else static_cast<unsigned short*>(a.c)[at + c] = *reinterpret_cast<const unsigned short*>(e);
+          }
+        }
+      }
+    }
+    __syncwarp();
   }
+}
+
+// N accumulators (a multiple of 32, or 16) per lane.
+template <int N>
+__device__ __forceinline__ void mm_store_rows(const MmArgs& a, unsigned char* buf, int lane, long long m0, long long n,
+                                              long long rows, long long cols, const float* v) {
+  if (m0 >= rows) return;
+  if (a.out_f32) {
+    constexpr int kCols = N < 32 ? N : 32;
+#pragma unroll
+    for (int c = 0; c < N; c += kCols)
+      if (n + c < cols) mm_store_rows_as<kCols, true>(a, buf, lane, m0, n + c, rows, cols, v + c);
+  } else {
+    constexpr int kCols = N < 64 ? N : 64;
+#pragma unroll
+    for (int c = 0; c < N; c += kCols)
+      if (n + c < cols) mm_store_rows_as<kCols, false>(a, buf, lane, m0, n + c, rows, cols, v + c);
+  }
+}
+
+// Stores N consecutive accumulators (rows q.. of Q) of this lane's row p of P, where P is B: the warp's lanes are
+// neighbours in C.
+template <int N>
+__device__ __forceinline__ void mm_store_swapped(const MmArgs& a, long long p, long long q, const float (&v)[N]) {
+  if (p >= a.rows_p) return;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (q + i < a.rows_q) mm_store1(a, q + i, p, v[i]);
 }
 
 // Tiles are walked in groups of 16 along P, so that the tiles in flight share rows of both operands in L2.
@@ -405,6 +467,7 @@ ps_mx_matmul_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_cons
     }
     __syncwarp();
   } else {
+    unsigned char* staging = stages + Cfg::kStages * Cfg::kStage + (warp - 2) * kMmStaging;
     const int quad = warp & 3;                        // the quarter of tensor memory's lanes this warp may read
     unsigned int n = 0;
     for (int tile = first; tile < tiles; tile += stride, ++n) {
@@ -415,22 +478,15 @@ ps_mx_matmul_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_cons
       mm_tile(args, tile, &tp, &tq);
       const int row = quad * 32 + lane;
       const unsigned int acc = tmem + ((unsigned)(quad * 32) << 16) + buf * BN;
-      constexpr int kStep = BN < 32 ? BN : 32;
-      if (args.splits == 1) {
+      constexpr int kStep = BN < 64 ? BN : 64;
 #pragma unroll 1
-        for (int c = 0; c < BN; c += kStep) {
-          float v[kStep];
-          mm_load<kStep>(acc + c, v);
-          mm_store<kStep>(args, (long long)tp * kMmP + row, (long long)tq * BN + c, v);
-        }
-      } else {
-        // this CTA's part goes to its shared memory (the stages are no longer in use), in an order in which
-        // neither these stores nor the reads below meet in a bank
-        float* red = reinterpret_cast<float*>(stages);
-#pragma unroll 1
-        for (int c = 0; c < BN; c += kStep) {
-          float v[kStep];
-          mm_load<kStep>(acc + c, v);
+      for (int c = 0; c < BN; c += kStep) {
+        float v[kStep];
+        mm_load<kStep>(acc + c, v);
+        if (args.splits > 1) {
+          // this CTA's part goes to its shared memory (the stages are no longer in use), in an order in which neither
+          // these stores nor the reads below meet in a bank
+          float* red = reinterpret_cast<float*>(stages);
 #pragma unroll
           for (int i = 0; i < kStep; i += 4) {
             if (args.swap) {
@@ -440,6 +496,11 @@ ps_mx_matmul_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_cons
               *reinterpret_cast<float4*>(red + row * (BN + 4) + c + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
             }
           }
+        } else if (args.swap) {
+          mm_store_swapped<kStep>(args, (long long)tp * kMmP + row, (long long)tq * BN + c, v);
+        } else {
+          mm_store_rows<kStep>(args, staging, lane, (long long)tp * kMmP + quad * 32, (long long)tq * BN + c, args.rows_p,
+                               args.rows_q, v);
         }
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");

@@ -29,9 +29,15 @@ constexpr int kPairHalf = 128 * 128;                        // bytes of a CTA's 
 constexpr int kPairBytesS = 3 * 2 * kMxAtom;                // scales: its own 128 rows of A, all 256 of B
 constexpr int kPairStage = 2 * kPairHalf + kPairBytesS;
 constexpr int kPairStages = 6;
-constexpr int kPairSmem = 1024 + kPairStages * kPairStage;
+constexpr int kPairSmem = kPairStages * kPairStage + 8 * kMmStaging + 256;      // stages, staging for stores, barriers
 constexpr int kPairScaleCol = 256;                          // tensor memory: accumulators, then two sets of scales of 24 columns
-static_assert(kPairStage % 1024 == 0 && kPairSmem <= kMmSmem - 1024, "stages do not fit");
+static_assert(kPairStage % 1024 == 0 && kPairSmem <= kMmSmem, "stages do not fit");
+
+struct PairControl {
+  unsigned long long full[kPairStages], empty[kPairStages], acc_full, acc_empty;
+  unsigned int tmem;
+};
+static_assert(sizeof(PairControl) <= 256, "control block");
 
 // The address of this CTA's shared memory word in the pair's leader: the rank is one bit of a shared::cluster address.
 __device__ __forceinline__ unsigned int pair_leader(unsigned int addr) {
@@ -75,8 +81,11 @@ __device__ __forceinline__ bool pair_wait(unsigned int bar, unsigned int parity,
   return true;
 }
 
-__device__ __forceinline__ void pair_arrive(unsigned int bar) {       // an address of the cluster
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+// Arrives on a barrier of either CTA.  (Release at CTA scope, the default: what is handed over is tensor memory, whose
+// reads the tcgen05 fence before this orders.  At cluster scope the arrival waits for the warp's stores of the previous
+// tile, over a thousand cycles.)
+__device__ __forceinline__ void pair_arrive(unsigned int bar) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
 __device__ __forceinline__ void pair_commit(unsigned int bar) {       // arrives on both CTAs' barrier at this offset
@@ -105,64 +114,13 @@ __device__ __forceinline__ void pair_mma(unsigned int d, unsigned long long a, u
       : "memory");
 }
 
-// 32 columns, without waiting for them.
-__device__ __forceinline__ void pair_load32(unsigned int tmem, float* v) {
-  unsigned int* u = reinterpret_cast<unsigned int*>(v);
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]),
-        "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15]), "=r"(u[16]),
-        "=r"(u[17]), "=r"(u[18]), "=r"(u[19]), "=r"(u[20]), "=r"(u[21]), "=r"(u[22]), "=r"(u[23]), "=r"(u[24]),
-        "=r"(u[25]), "=r"(u[26]), "=r"(u[27]), "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
-      : "r"(tmem));
-}
-
-// A thread's 256 bits: one whole sector.
-__device__ __forceinline__ void store256(void* p, const unsigned int (&w)[8]) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
-               "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-               : "memory");
-}
-
-// 32 accumulators of row m, columns n..n+31.
-__device__ __forceinline__ void pair_store(const MmArgs& a, long long m, long long n, const float* v) {
-  if (m >= a.rows_p) return;
-  if (a.vec_ok > 1 && n + 32 <= a.rows_q) {
-    unsigned int w[8];
-    if (a.out_f32) {
-      float* o = static_cast<float*>(a.c) + (size_t)m * (size_t)a.ldc + (size_t)n;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-#pragma unroll
-        for (int q = 0; q < 8; ++q) w[q] = __float_as_uint(v[8 * i + q]);
-        store256(o + 8 * i, w);
-      }
-    } else {
-      unsigned short* o = static_cast<unsigned short*>(a.c) + (size_t)m * (size_t)a.ldc + (size_t)n;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-#pragma unroll
-        for (int q = 0; q < 8; ++q) w[q] = mm_bf16x2(v[16 * i + 2 * q], v[16 * i + 2 * q + 1]);
-        store256(o + 16 * i, w);
-      }
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 32; i += 4)
-      if (n + i < a.rows_q) mm_store4(a, m, n + i, a.rows_q, make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]));
-  }
-}
-
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 ps_mx_matmul_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                          const __grid_constant__ CUtensorMap map_sa, const __grid_constant__ CUtensorMap map_sb,
                          const __grid_constant__ MmArgs args) {
-  extern __shared__ unsigned char raw[];
-  __shared__ __align__(8) unsigned long long s_full[kPairStages], s_empty[kPairStages], s_acc_full, s_acc_empty;
-  __shared__ unsigned int s_tmem;
-  unsigned char* stages = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+  // (no static shared memory beside it: the stages start where the swizzle needs them to, at a multiple of 1024)
+  extern __shared__ __align__(1024) unsigned char stages[];
+  PairControl& ctl = *reinterpret_cast<PairControl*>(stages + kPairStages * kPairStage + 8 * kMmStaging);
   const unsigned int base = mm_smem(stages);
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   unsigned int rank;
@@ -170,11 +128,11 @@ ps_mx_matmul_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid
 
   if (tid == 0) {
     for (int s = 0; s < kPairStages; ++s) {
-      asm volatile("mbarrier.init.shared::cta.b64 [%0], 2;" ::"r"(mm_smem(&s_full[s])) : "memory");     // the leader's two producers
-      asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(mm_smem(&s_empty[s])) : "memory");
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], 2;" ::"r"(mm_smem(&ctl.full[s])) : "memory");     // the leader's two producers
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(mm_smem(&ctl.empty[s])) : "memory");
     }
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(mm_smem(&s_acc_full)) : "memory");
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], 16;" ::"r"(mm_smem(&s_acc_empty)) : "memory");    // 8 warps of each
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(mm_smem(&ctl.acc_full)) : "memory");
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], 16;" ::"r"(mm_smem(&ctl.acc_empty)) : "memory");    // 8 warps of each
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_b) : "memory");
@@ -182,14 +140,14 @@ ps_mx_matmul_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_sb) : "memory");
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(mm_smem(&s_tmem)) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(mm_smem(&ctl.tmem)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   mm_cluster_sync();                                      // both CTAs' barriers and tensor memory exist
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-  const unsigned int tmem = s_tmem;
+  const unsigned int tmem = ctl.tmem;
   mx_pdl();
 
   const int tiles = args.tiles_p * args.tiles_q, stride = (int)(gridDim.x / 2);
@@ -198,7 +156,7 @@ ps_mx_matmul_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid
   if (warp == 0 || warp == 10) {
     if (mm_elect()) {
       MmCursor<kPairStages> at;
-      const unsigned int full = pair_leader(mm_smem(&s_full[0]));
+      const unsigned int full = pair_leader(mm_smem(&ctl.full[0]));
       unsigned int issued = 0;
       bool ok = true;
       for (int tile = first; ok && tile < tiles; tile += stride) {
@@ -208,10 +166,10 @@ ps_mx_matmul_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid
         if (warp == 0) {
           const int row_a = tp * kPairTile + (int)rank * 128, row_b = tq * kPairTile + (int)rank * 128;
           for (int k = 0; k < nk; ++k, at.next(), ++issued) {
-            if (!mm_wait(mm_smem(&s_empty[0]) + 8 * at.s, at.parity ^ 1u, args.status)) { ok = false; break; }
+            if (!mm_wait(mm_smem(&ctl.empty[0]) + 8 * at.s, at.parity ^ 1u, args.status)) { ok = false; break; }
             const unsigned int dst = base + at.s * kPairStage, bar = full + 8 * at.s;
             if (rank == 0)
-              asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(mm_smem(&s_full[0]) + 8 * at.s),
+              asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(mm_smem(&ctl.full[0]) + 8 * at.s),
                            "n"(4 * kPairHalf)
                            : "memory");
             pair_tma(dst, &map_a, k * 128, row_a, bar);
@@ -221,10 +179,10 @@ ps_mx_matmul_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid
           // atoms of scales: 128-row block times atoms per block, two per stage (blocks that do not exist read as zeros)
           const int at_a = (int)((tp * 2 + (int)rank) * args.atoms), at_b = (int)(tq * 2 * args.atoms);
           for (int k = 0; k < nk; ++k, at.next(), ++issued) {
-            if (!mm_wait(mm_smem(&s_empty[0]) + 8 * at.s, at.parity ^ 1u, args.status)) { ok = false; break; }
+            if (!mm_wait(mm_smem(&ctl.empty[0]) + 8 * at.s, at.parity ^ 1u, args.status)) { ok = false; break; }
             const unsigned int dst = base + at.s * kPairStage + 2 * kPairHalf, bar = full + 8 * at.s;
             if (rank == 0)
-              asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(mm_smem(&s_full[0]) + 8 * at.s),
+              asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(mm_smem(&ctl.full[0]) + 8 * at.s),
                            "n"(2 * kPairBytesS)
                            : "memory");
             pair_tma(dst, &map_sa, 0, at_a + 2 * k, bar);
@@ -235,7 +193,7 @@ ps_mx_matmul_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid
       }
       if (!ok && rank == 0)                               // an expired wait: let the copies in flight land
         for (unsigned int s = 0; s < (unsigned)kPairStages && s < issued; ++s)
-          mm_wait(mm_smem(&s_full[s]), ((issued - 1 - s) / kPairStages) & 1u, args.status);
+          mm_wait(mm_smem(&ctl.full[s]), ((issued - 1 - s) / kPairStages) & 1u, args.status);
     }
     __syncwarp();
   } else if (warp == 1) {
@@ -245,10 +203,10 @@ ps_mx_matmul_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid
       unsigned int set = 0, acc_parity = 1;
       bool ok = true;
       for (int tile = first; ok && tile < tiles; tile += stride, acc_parity ^= 1u) {
-        if (!pair_wait(mm_smem(&s_acc_empty), acc_parity, args.status)) break;
+        if (!pair_wait(mm_smem(&ctl.acc_empty), acc_parity, args.status)) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         for (int k = 0; k < nk; ++k, at.next(), set ^= 32u) {
-          if (!pair_wait(mm_smem(&s_full[0]) + 8 * at.s, at.parity, args.status)) { ok = false; break; }
+          if (!pair_wait(mm_smem(&ctl.full[0]) + 8 * at.s, at.parity, args.status)) { ok = false; break; }
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const unsigned long long da = mm_desc_codes(base + at.s * kPairStage);
           const unsigned long long ds = mm_desc_scales(base + at.s * kPairStage + 2 * kPairHalf);
@@ -263,33 +221,31 @@ ps_mx_matmul_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid
           for (int i = 0; i < 4; ++i)
             pair_mma(tmem, da + 2 * i, da + kPairHalf / 16 + 2 * i, kIdesc | ((unsigned)(i & 1) << 30) | ((unsigned)(i & 1) << 5),
                      ta + (i >> 1) * 4, tb + (i >> 1) * 8, k > 0 || i > 0);
-          pair_commit(mm_smem(&s_empty[0]) + 8 * at.s);
+          pair_commit(mm_smem(&ctl.empty[0]) + 8 * at.s);
         }
-        pair_commit(mm_smem(&s_acc_full));
+        pair_commit(mm_smem(&ctl.acc_full));
       }
     }
     __syncwarp();
   } else {
     const int quad = warp & 3, half = (warp - 2) >> 2;
-    const unsigned int empty = pair_leader(mm_smem(&s_acc_empty));
+    unsigned char* staging = stages + kPairStages * kPairStage + (warp - 2) * kMmStaging;
+    const unsigned int empty = pair_leader(mm_smem(&ctl.acc_empty));
     const unsigned int acc = tmem + ((unsigned)(quad * 32) << 16) + half * 128;
     unsigned int n = 0;
     for (int tile = first; tile < tiles; tile += stride, ++n) {
-      if (!__all_sync(0xffffffffu, mm_wait(mm_smem(&s_acc_full), n & 1u, args.status))) break;
+      if (!__all_sync(0xffffffffu, mm_wait(mm_smem(&ctl.acc_full), n & 1u, args.status))) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       float v[128];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) pair_load32(acc + c * 32, v + c * 32);
-      asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+      mm_load<128>(acc, v);
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
       if (lane == 0) pair_arrive(empty);
       int tp, tq;
       mm_tile(args, tile, &tp, &tq);
-      const long long m = (long long)tp * kPairTile + rank * 128 + quad * 32 + lane;
+      const long long m = (long long)tp * kPairTile + rank * 128 + quad * 32;
       const long long q = (long long)tq * kPairTile + half * 128;
-#pragma unroll
-      for (int c = 0; c < 4; ++c) pair_store(args, m, q + c * 32, v + c * 32);
+      mm_store_rows<128>(args, staging, lane, m, q, args.rows_p, args.rows_q, v);
     }
     __syncwarp();
   }
