@@ -181,10 +181,13 @@ int matmul(const ps_mx* p, const ps_mx* q, MmArgs args, const OpDevice& d, cudaS
   args.tiles_p = (int)tp;
   args.tiles_q = (int)tq;
   const int tiles = (int)(tp * tq);
-  // few tiles: 2, 4 or 8 CTAs share a tile's K while that many CTAs fit and each keeps at least one stage
+  // few tiles: 2, 4 or 8 CTAs share a tile's K while that many CTAs fit and each keeps four stages; with fewer the sum
+  // of the parts costs more than it saves (1 x 4096 x 1024: 5.2 us as 4 x 1 stage, 3.8 us unsplit; 1 x 1024 x 4096:
+  // 4.7 us as 4 x 4 stages, 5.3 us as 2 x 8)
   args.splits = 1;
-  while (args.splits < 8 && tiles * args.splits * 2 <= d.num_sms && args.splits * 2 <= args.stages_k) args.splits *= 2;
-  const unsigned int grid = args.splits > 1 ? (unsigned)(tiles * args.splits) : (unsigned)std::min(tiles, d.num_sms);
+  const int room = d.num_sms * Cfg::kCtas;
+  while (args.splits < 8 && tiles * args.splits * 2 <= room && args.splits * 8 <= args.stages_k) args.splits *= 2;
+  const unsigned int grid = args.splits > 1 ? (unsigned)(tiles * args.splits) : (unsigned)std::min(tiles, room);
   return launch("4-bit product", ps_mx_matmul_kernel<BN>, grid, kMmThreads, Cfg::kSmem, args.splits, stream, mp, mq, args);
 }
 
@@ -279,6 +282,9 @@ int ps_mx_matmul(const ps_mx* a, const ps_mx* b, int dtype, void* c, long long l
   // the pair's tiles read each operand less often; they are taken once they fill the device
   const long long pairs = ((p->rows + 255) / 256) * ((q->rows + 255) / 256);
   if (pairs >= d.num_sms / 2 - 12) return matmul_pair(p, q, args, d, stream);
+  // tiles of 128 x 64, two CTAs on an SM, while those of 128 x 128 would leave half of the SMs without one
+  const long long tiles = ((p->rows + 127) / 128) * ((q->rows + 127) / 128);
+  if (tiles <= d.num_sms / 2) return matmul<64>(p, q, args, d, stream);
   return matmul<128>(p, q, args, d, stream);
 }
 

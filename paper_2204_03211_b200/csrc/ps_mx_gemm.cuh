@@ -35,12 +35,21 @@ constexpr int kMmMaxStages = 8;
 constexpr int kMmSmem = 227 * 1024;
 constexpr int kMmStaging = 2048;                // bytes of an epilogue warp's staging for stores
 
+struct MmControl {
+  unsigned long long full[kMmMaxStages], empty[kMmMaxStages], acc_full[2], acc_empty[2];
+  unsigned int tmem;
+};
+constexpr int kMmControl = 256;
+static_assert(sizeof(MmControl) <= kMmControl, "control block");
+
 template <int BN>
 struct MmCfg {
   static constexpr int kBytesP = kMmP * 128, kBytesQ = BN * 128;
   static constexpr int kBytesS = 2 * kMxAtom;                   // scales of one 128-row block in a stage
   static constexpr int kStage = kBytesP + kBytesQ + 2 * kBytesS;
-  static constexpr int kFit = (kMmSmem - 2048 - 4 * kMmStaging) / kStage;  // four warps' staging beside the stages
+  // Q of up to 64 rows: two CTAs share an SM, so that more tiles of P are on their way at once
+  static constexpr int kCtas = BN <= 64 ? 2 : 1;
+  static constexpr int kFit = ((kMmSmem + 1024) / kCtas - 1024 - kMmControl - 4 * kMmStaging) / kStage;
   static constexpr int kStages = kFit < kMmMaxStages ? kFit : kMmMaxStages;
   static constexpr int kAcc = 2;                                // accumulators: the second hides the epilogue
   static constexpr int kScaleCol = kAcc * BN;                   // tensor memory: accumulators, then two sets of scales
@@ -48,7 +57,7 @@ struct MmCfg {
   static constexpr int kCols = kScaleCol + 2 * kScaleSet;
   static constexpr int kAlloc = kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
   static_assert(BN <= 128, "one block of scales per operand");
-  static constexpr int kSmem = 1024 + kStages * kStage + 4 * kMmStaging;
+  static constexpr int kSmem = kStages * kStage + 4 * kMmStaging + kMmControl;
   static_assert(kStages >= 3 && kCols <= 512 && kStage % 1024 == 0, "tile does not fit");
 };
 
@@ -290,9 +299,19 @@ __device__ __forceinline__ void mm_store_rows(const MmArgs& a, unsigned char* bu
 template <int N>
 __device__ __forceinline__ void mm_store_swapped(const MmArgs& a, long long p, long long q, const float (&v)[N]) {
   if (p >= a.rows_p) return;
+  const int live = (int)min((long long)N, a.rows_q - q);
+  const size_t at = (size_t)q * (size_t)a.ldc + (size_t)p;
+  if (a.out_f32) {
+    float* o = static_cast<float*>(a.c) + at;
 #pragma unroll
-  for (int i = 0; i < N; ++i)
-    if (q + i < a.rows_q) mm_store1(a, q + i, p, v[i]);
+    for (int i = 0; i < N; ++i, o += a.ldc)
+      if (i < live) *o = v[i];
+  } else {
+    unsigned short* o = static_cast<unsigned short*>(a.c) + at;
+#pragma unroll
+    for (int i = 0; i < N; ++i, o += a.ldc)
+      if (i < live) *o = (unsigned short)mm_bf16x2(v[i], 0.f);
+  }
 }
 
 // Tiles are walked in groups of 16 along P, so that the tiles in flight share rows of both operands in L2.
@@ -353,32 +372,31 @@ __device__ __forceinline__ void mm_store4(const MmArgs& a, long long m, long lon
 }
 
 template <int BN>
-__global__ void __launch_bounds__(kMmThreads, 1)
+__global__ void __launch_bounds__(kMmThreads, MmCfg<BN>::kCtas)
 ps_mx_matmul_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_q,
                     const __grid_constant__ MmArgs args) {
   using Cfg = MmCfg<BN>;
-  extern __shared__ unsigned char raw[];
-  __shared__ __align__(8) unsigned long long s_full[kMmMaxStages], s_empty[kMmMaxStages], s_acc_full[2], s_acc_empty[2];
-  __shared__ unsigned int s_tmem;
-  unsigned char* stages = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+  // (no static shared memory beside it: the stages start where the swizzle needs them to, at a multiple of 1024)
+  extern __shared__ __align__(1024) unsigned char stages[];
+  MmControl& ctl = *reinterpret_cast<MmControl*>(stages + Cfg::kStages * Cfg::kStage + 4 * kMmStaging);
   const unsigned int base = mm_smem(stages);
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
 
   if (tid == 0) {
     for (int s = 0; s < Cfg::kStages; ++s) {
-      asm volatile("mbarrier.init.shared::cta.b64 [%0], 2;" ::"r"(mm_smem(&s_full[s])) : "memory");
-      asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(mm_smem(&s_empty[s])) : "memory");
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], 2;" ::"r"(mm_smem(&ctl.full[s])) : "memory");
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(mm_smem(&ctl.empty[s])) : "memory");
     }
     for (int b = 0; b < Cfg::kAcc; ++b) {
-      asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(mm_smem(&s_acc_full[b])) : "memory");
-      asm volatile("mbarrier.init.shared::cta.b64 [%0], 4;" ::"r"(mm_smem(&s_acc_empty[b])) : "memory");
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(mm_smem(&ctl.acc_full[b])) : "memory");
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], 4;" ::"r"(mm_smem(&ctl.acc_empty[b])) : "memory");
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_p) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_q) : "memory");
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(mm_smem(&s_tmem)),
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(mm_smem(&ctl.tmem)),
                  "r"(Cfg::kAlloc)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -386,7 +404,7 @@ ps_mx_matmul_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_cons
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-  const unsigned int tmem = s_tmem;
+  const unsigned int tmem = ctl.tmem;
   mx_pdl();
 
   const int tiles = args.tiles_p * args.tiles_q;
@@ -407,8 +425,8 @@ ps_mx_matmul_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_cons
         mm_tile(args, tile, &tp, &tq);
         if (warp == 0) {
           for (int k = k0; k < k1; ++k, at.next(), ++issued) {
-            if (!mm_wait(mm_smem(&s_empty[0]) + 8 * at.s, at.parity ^ 1u, args.status)) { ok = false; break; }
-            const unsigned int bar = mm_smem(&s_full[0]) + 8 * at.s, dst = base + at.s * Cfg::kStage;
+            if (!mm_wait(mm_smem(&ctl.empty[0]) + 8 * at.s, at.parity ^ 1u, args.status)) { ok = false; break; }
+            const unsigned int bar = mm_smem(&ctl.full[0]) + 8 * at.s, dst = base + at.s * Cfg::kStage;
             asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "n"(Cfg::kBytesP + Cfg::kBytesQ)
                          : "memory");
             mm_tma(dst, &map_p, k * 128, tp * kMmP, bar);
@@ -416,10 +434,10 @@ ps_mx_matmul_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_cons
           }
         } else {
           const uint8_t* sp = args.sp + ((size_t)tp * (size_t)args.atoms + 2 * (size_t)k0) * kMxAtom;
-          const uint8_t* sq = args.sq + ((size_t)tq * (size_t)args.atoms + 2 * (size_t)k0) * kMxAtom;
+          const uint8_t* sq = args.sq + ((size_t)(tq * BN / 128) * (size_t)args.atoms + 2 * (size_t)k0) * kMxAtom;
           for (int k = k0; k < k1; ++k, at.next(), ++issued, sp += Cfg::kBytesS, sq += Cfg::kBytesS) {
-            if (!mm_wait(mm_smem(&s_empty[0]) + 8 * at.s, at.parity ^ 1u, args.status)) { ok = false; break; }
-            const unsigned int bar = mm_smem(&s_full[0]) + 8 * at.s;
+            if (!mm_wait(mm_smem(&ctl.empty[0]) + 8 * at.s, at.parity ^ 1u, args.status)) { ok = false; break; }
+            const unsigned int bar = mm_smem(&ctl.full[0]) + 8 * at.s;
             const unsigned int dst = base + at.s * Cfg::kStage + Cfg::kBytesP + Cfg::kBytesQ;
             asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "n"(2 * Cfg::kBytesS) : "memory");
             mm_bulk(dst, sp, Cfg::kBytesS, bar);
@@ -429,7 +447,7 @@ ps_mx_matmul_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_cons
       }
       if (!ok)                                        // an expired wait: let the copies in flight land
         for (unsigned int s = 0; s < (unsigned)Cfg::kStages && s < issued; ++s)
-          mm_wait(mm_smem(&s_full[s]), ((issued - 1 - s) / Cfg::kStages) & 1u, args.status);
+          mm_wait(mm_smem(&ctl.full[s]), ((issued - 1 - s) / Cfg::kStages) & 1u, args.status);
     }
     __syncwarp();
   } else if (warp == 1) {
@@ -440,11 +458,14 @@ ps_mx_matmul_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_cons
       unsigned int set = 0;
       bool ok = true;
       for (int tile = first; ok && tile < tiles; tile += stride, acc.next()) {
-        if (!mm_wait(mm_smem(&s_acc_empty[0]) + 8 * acc.s, acc.parity ^ 1u, args.status)) break;
+        if (!mm_wait(mm_smem(&ctl.acc_empty[0]) + 8 * acc.s, acc.parity ^ 1u, args.status)) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const unsigned int d = tmem + acc.s * BN;
+        int tile_p, tile_q;
+        mm_tile(args, tile, &tile_p, &tile_q);
+        const unsigned int sub = (unsigned)(tile_q * BN % 128) / 32;       // where the tile's rows start in their block of scales
         for (int k = k0; k < k1; ++k, at.next(), set ^= Cfg::kScaleSet) {
-          if (!mm_wait(mm_smem(&s_full[0]) + 8 * at.s, at.parity, args.status)) { ok = false; break; }
+          if (!mm_wait(mm_smem(&ctl.full[0]) + 8 * at.s, at.parity, args.status)) { ok = false; break; }
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const unsigned long long dp = mm_desc_codes(base + at.s * Cfg::kStage);
           const unsigned long long ds = mm_desc_scales(base + at.s * Cfg::kStage + Cfg::kBytesP + Cfg::kBytesQ);
@@ -459,10 +480,10 @@ ps_mx_matmul_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_cons
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             mm_mma(d, dp + 2 * i, dp + Cfg::kBytesP / 16 + 2 * i, kIdesc | ((unsigned)(i & 1) << 30) | ((unsigned)(i & 1) << 5),
-                   tp + (i >> 1) * 4, tq + (i >> 1) * 4, k > k0 || i > 0);
-          mm_commit(mm_smem(&s_empty[0]) + 8 * at.s);
+                   tp + (i >> 1) * 4, tq + (i >> 1) * 4 + sub, k > k0 || i > 0);
+          mm_commit(mm_smem(&ctl.empty[0]) + 8 * at.s);
         }
-        mm_commit(mm_smem(&s_acc_full[0]) + 8 * acc.s);
+        mm_commit(mm_smem(&ctl.acc_full[0]) + 8 * acc.s);
       }
     }
     __syncwarp();
@@ -472,7 +493,7 @@ ps_mx_matmul_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_cons
     unsigned int n = 0;
     for (int tile = first; tile < tiles; tile += stride, ++n) {
       const unsigned int buf = n % Cfg::kAcc;
-      if (!__all_sync(0xffffffffu, mm_wait(mm_smem(&s_acc_full[buf]), (n / Cfg::kAcc) & 1u, args.status))) break;
+      if (!__all_sync(0xffffffffu, mm_wait(mm_smem(&ctl.acc_full[buf]), (n / Cfg::kAcc) & 1u, args.status))) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       int tp, tq;
       mm_tile(args, tile, &tp, &tq);
@@ -506,7 +527,7 @@ ps_mx_matmul_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_cons
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
       if (lane == 0)
-        asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(mm_smem(&s_acc_empty[buf])) : "memory");
+        asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(mm_smem(&ctl.acc_empty[buf])) : "memory");
     }
     __syncwarp();
   }
