@@ -689,8 +689,9 @@ typedef struct ps_clip ps_clip; /* opaque */
 /* Remembers n tensors (host arrays of device pointers and element counts, copied):
  * source i of src_dtype is written to destination i of dst_dtype, e.g. fp32
  * gradients into a bf16 push buffer.  dsts[i] == srcs[i] clips in place (same dtype
- * only); otherwise no destination may overlap a source.  Tensors that are 16-byte
- * aligned on both sides take 128-bit accesses.  Empty tensors are allowed.
+ * only); otherwise no destination may overlap a source.  Tensors aligned to eight
+ * elements on both sides (32 bytes of fp32, 16 of bf16) take wide accesses, others
+ * single ones with identical results.  Empty tensors are allowed.
  * Allocates a small table on `device`.  Errors: BAD_ARG, ALIGN, NOMEM, CUDA. */
 int ps_clip_create(ps_clip** out, int device, int n, const void* const* srcs, int src_dtype, void* const* dsts,
                    int dst_dtype, const size_t* nelems);
