@@ -241,7 +241,9 @@ int ps_mx_dequantize(const ps_mx* q, int dtype, void* out, long long ld, void* s
   if (misaligned(out, esize(dtype))) return PS_ERR_ALIGN;
   const long long nc = (q->cols + kDequantCols - 1) / kDequantCols, nr = (q->rows + kDequantRows - 1) / kDequantRows;
   if (nc * nr > 0x7fffffffll) return PS_ERR_TOO_LARGE;
-  const int vec_ok = !misaligned(out, 16) && (ld * (long long)esize(dtype)) % 16 == 0;
+  // 2: rows that allow 256-bit stores, 1: 128-bit ones
+  const long long row = ld * (long long)esize(dtype);
+  const int vec_ok = !misaligned(out, 32) && row % 32 == 0 ? 2 : !misaligned(out, 16) && row % 16 == 0;
   const uint8_t *codes = static_cast<const uint8_t*>(q->codes), *scales = static_cast<const uint8_t*>(q->scales);
   return launch("dequantise", dtype == PS_BF16 ? ps_mx_dequantize_kernel<true> : ps_mx_dequantize_kernel<false>,
                 (unsigned)(nc * nr), kDequantThreads, 0, 1, static_cast<cudaStream_t>(stream_), codes, scales, q->rows,

@@ -299,9 +299,9 @@ ps_mx_quantize_kernel(const typename MxIn<BF16>::T* __restrict__ x, long long ro
 
 // -------------------------------------------------------------- dequantisation
 //
-// A lane takes four bytes of codes (eight elements), a warp 256 columns of a row, so
-// that loads and stores are contiguous; a CTA takes 32 rows of such a strip.  A
-// nibble s eem placed as sign, exponent field 0..3 and top mantissa bit of a bf16
+// A lane takes eight bytes of codes (sixteen elements, half a block), a warp 512
+// columns of a row, so that a lane stores whole sectors; a CTA takes 32 rows of such a
+// strip.  A nibble s eem placed as sign, exponent field 0..3 and top mantissa bit of a bf16
 // is its value times 2^-126, subnormals included: two
 // exact multiplications (2^126, the scale) give the result without a conversion
 // instruction, which issue at a fraction of the rate.
@@ -319,7 +319,13 @@ __device__ __forceinline__ unsigned int mx_scale_pair(unsigned int sb) {
   return h | h << 16;
 }
 
-constexpr int kDequantThreads = 256, kDequantCols = 256, kDequantRows = 32;
+constexpr int kDequantThreads = 256, kDequantCols = 512, kDequantRows = 32;
+
+__device__ __forceinline__ void store_sector(void* p, const unsigned int* w) {       // 32 bytes, written once
+  asm volatile("st.global.cs.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+               "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
+}
 
 template <bool OUT_BF16>
 __global__ void __launch_bounds__(kDequantThreads)
@@ -328,15 +334,16 @@ ps_mx_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __rest
   mx_pdl();
   constexpr int kSteps = kDequantRows / (kDequantThreads / 32);
   const long long r0 = (long long)(blockIdx.x / col_tiles) * kDequantRows + (threadIdx.x >> 5);
-  const long long c = (long long)(blockIdx.x % col_tiles) * kDequantCols + (threadIdx.x & 31) * 8;
+  const long long c = (long long)(blockIdx.x % col_tiles) * kDequantCols + (threadIdx.x & 31) * 16;
   if (c >= cols) return;
   const size_t pitch = (size_t)mx_pitch(cols);
-  unsigned int w[kSteps], sb[kSteps];
+  uint2 w[kSteps];
+  unsigned int sb[kSteps];
 #pragma unroll
   for (int k = 0; k < kSteps; ++k) {
     const long long r = r0 + k * (kDequantThreads / 32);
     if (r < rows) {
-      w[k] = __ldcs(reinterpret_cast<const unsigned int*>(codes + (size_t)r * pitch + (size_t)(c >> 1)));
+      w[k] = __ldcs(reinterpret_cast<const uint2*>(codes + (size_t)r * pitch + (size_t)(c >> 1)));
       sb[k] = scales[mx_scale_at(r, c >> 5, mx_atoms(cols))];
     }
   }
@@ -345,30 +352,40 @@ ps_mx_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __rest
     const long long r = r0 + k * (kDequantThreads / 32);
     if (r >= rows) break;
     const unsigned int s = mx_scale_pair(sb[k]);
-    unsigned int v[4];
+    unsigned int v[8];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = mul_bf16x2(mx_pair(w[k], j), s);
+    for (int j = 0; j < 4; ++j) {
+      v[j] = mul_bf16x2(mx_pair(w[k].x, j), s);
+      v[4 + j] = mul_bf16x2(mx_pair(w[k].y, j), s);
+    }
     if constexpr (OUT_BF16) {
       unsigned short* o = static_cast<unsigned short*>(out) + (size_t)r * (size_t)ld + (size_t)c;
-      if (vec_ok && c + 8 <= cols) {
-        *reinterpret_cast<uint4*>(o) = make_uint4(v[0], v[1], v[2], v[3]);
+      if (vec_ok == 2 && c + 16 <= cols) {
+        store_sector(o, v);
+      } else if (vec_ok && c + 16 <= cols) {
+        reinterpret_cast<uint4*>(o)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<uint4*>(o)[1] = make_uint4(v[4], v[5], v[6], v[7]);
       } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < 16; ++i)
           if (c + i < cols) o[i] = (unsigned short)(i & 1 ? v[i >> 1] >> 16 : v[i >> 1] & 0xffffu);
       }
     } else {
       float* o = static_cast<float*>(out) + (size_t)r * (size_t)ld + (size_t)c;
-      float f[8];
+      unsigned int f[16];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(i & 1 ? v[i >> 1] & 0xffff0000u : v[i >> 1] << 16);
-      if (vec_ok && c + 8 <= cols) {
-        *reinterpret_cast<float4*>(o) = make_float4(f[0], f[1], f[2], f[3]);
-        *reinterpret_cast<float4*>(o + 4) = make_float4(f[4], f[5], f[6], f[7]);
+      for (int i = 0; i < 16; ++i) f[i] = i & 1 ? v[i >> 1] & 0xffff0000u : v[i >> 1] << 16;
+      if (vec_ok == 2 && c + 16 <= cols) {
+        store_sector(o, f);
+        store_sector(o + 8, f + 8);
+      } else if (vec_ok && c + 16 <= cols) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          reinterpret_cast<uint4*>(o)[i] = make_uint4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
       } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (c + i < cols) o[i] = f[i];
+        for (int i = 0; i < 16; ++i)
+          if (c + i < cols) o[i] = __uint_as_float(f[i]);
       }
     }
   }
