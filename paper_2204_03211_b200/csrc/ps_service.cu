@@ -617,7 +617,12 @@ Slot* pending_slot(ps_service* s, Block& b) {
 // wait for, so that a list of many blocks from one earlier launch costs one wait.
 // A launch that went to `stream` itself needs no wait: stream order covers it.
 int order_after_block(ps_service* s, Block& b, cudaStream_t stream, unsigned int* waited = nullptr) {
-  if (Slot* sl = pending_slot(s, b)) {
+  // (a slot this call has waited for already is not asked again: an unfinished launch's event would be queried once per
+  // block, half a microsecond each)
+  const bool known = waited && b.last_slot >= 0 && (*waited >> (unsigned)b.last_slot & 1u) &&
+                     s->slots[b.last_slot].gen == b.last_slot_gen;
+  Slot* sl = known ? nullptr : pending_slot(s, b);
+  if (sl) {
     const unsigned int bit = 1u << (unsigned)b.last_slot;
     // (a caller's stream handle may have been destroyed and handed out again, so only
     // the service's own streams are trusted to be the same stream when the handles match)
