@@ -349,7 +349,8 @@ int ps_round_release(ps_service* svc, int round);
  * apply.  The first call, and one that lists more elements than any before, allocate
  * 4 bytes of device memory per listed element and wait for the device.
  * Errors: those of ps_aggregate; BAD_ARG (max_norm not above 0, norms_dev_out not
- * aligned to 4 bytes), TOO_LARGE (more than 64 jobs). */
+ * aligned to 4 bytes), TOO_LARGE (more than 64 jobs, rows of more than 2^30 elements
+ * in a row-sparse push). */
 int ps_aggregate_clipped(ps_service* svc, const ps_task* ready, int n_ready, float max_norm, float* norms_dev_out,
                          void* stream);
 
@@ -645,7 +646,7 @@ typedef struct {
 } ps_mx;
 
 /* Bytes of the two buffers of an operand (either out pointer may be NULL).
- * Errors: BAD_ARG (rows < 0, cols < 1, either 2^31 or more). */
+ * Errors: BAD_ARG (rows < 0, cols < 1, either 2^30 or more). */
 int ps_mx_sizes(long long rows, long long cols, size_t* code_bytes_out, size_t* scale_bytes_out);
 
 /* Quantises the matrix x (device; rows x cols of `dtype`, a ps_dtype; row stride

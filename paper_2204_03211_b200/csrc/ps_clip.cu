@@ -13,8 +13,9 @@
 // elements stay in registers between the passes.
 //
 // Measured: 351 M fp32 elements into bf16 537 us (10 bytes per element, 6.55 TB/s;
-// the norm alone 209 us), bf16 into bf16 XXX us; 170 K elements in 37 tensors XXX us,
-// which is launch, barrier and four dependent trips to L2.
+// the norm alone 202 us, 7.0 TB/s), bf16 into bf16 345 us (6.1 TB/s), 8.4 M fp32 into
+// fp32 17 us, mostly out of L2; 170 K elements in 37 tensors 8.2 us a call, which is
+// launch, barrier and four dependent trips to L2.
 #include <algorithm>
 #include <cmath>
 #include <cstring>

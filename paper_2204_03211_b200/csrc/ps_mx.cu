@@ -92,7 +92,7 @@ bool bad_dtype(int t) { return t != PS_F32 && t != PS_BF16; }
 size_t esize(int t) { return t == PS_BF16 ? 2 : 4; }
 bool misaligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 
-constexpr long long kMxMaxDim = 1ll << 31;       // rows and columns of an operand (TMA coordinates are 32-bit)
+constexpr long long kMxMaxDim = 1ll << 30;       // rows and columns of an operand (TMA coordinates are 32-bit)
 
 int check_operand(const ps_mx* q) {
   if (!q || q->rows < 0 || q->cols < 1 || q->rows >= kMxMaxDim || q->cols >= kMxMaxDim) return PS_ERR_BAD_ARG;

@@ -26,7 +26,6 @@
 
 namespace psb {
 
-constexpr int kMxBlock = 32;                 // elements that share a scale
 constexpr int kMxTile = 128;                 // rows and columns of a quantiser tile: one atom of scales each way
 constexpr int kMxAtom = 512;                 // bytes of an atom
 

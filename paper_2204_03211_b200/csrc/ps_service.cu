@@ -1301,7 +1301,7 @@ unsigned int clip_chunk(ps_service* s, const std::vector<int>& idx, unsigned int
 
 // Builds the table of a clipped launch of the validated blocks `idx`: tasks sorted by job, jobs in the order in which
 // the list names them first.
-int build_clip_plan(ps_service* s, const std::vector<int>& idx, Plan* plan) {
+int build_clip_plan(ps_service* s, const std::vector<int>& idx, Plan* plan) try {
   const size_t n = idx.size();
   std::vector<int> job_ids;
   for (int bi : idx)
@@ -1396,6 +1396,8 @@ int build_clip_plan(ps_service* s, const std::vector<int>& idx, Plan* plan) {
   plan->chunk_elems = ce;
   plan->spool = spool;
   return PS_OK;
+} catch (const std::bad_alloc&) {
+  return PS_ERR_NOMEM;
 }
 
 // Launch limits and device memory of the clipped kernels, at the first such call.
@@ -1610,11 +1612,7 @@ int ps_aggregate(ps_service* s, const ps_task* ready, int n_ready, void* stream_
   return submit_ready(s, s->idx, static_cast<cudaStream_t>(stream_), 0u, nullptr, false);
 }
 
-int ps_aggregate_clipped(ps_service* s, const ps_task* ready, int n_ready, float max_norm, float* norms_out,
-                         void* stream_) {
-  if (!alive(s)) return PS_ERR_BAD_HANDLE;
-  std::lock_guard<std::mutex> lk(s->mu);
-  if (bad_clip(max_norm, norms_out)) return PS_ERR_BAD_ARG;
+static int aggregate_clipped(ps_service* s, const ps_task* ready, int n_ready, const ClipCall& call, cudaStream_t stream) {
   int rc = validate_ready(s, ready, n_ready, &s->idx);
   if (rc) return rc;
   if (!has_device(s)) return PS_ERR_NO_DEVICE;
@@ -1625,7 +1623,19 @@ int ps_aggregate_clipped(ps_service* s, const ps_task* ready, int n_ready, float
   rc = ensure_clip(s);
   if (!rc) rc = build_clip_plan(s, s->idx, &s->plan);
   if (rc) return rc;
-  return launch_clip(s, s->idx, s->plan, ClipCall{max_norm, norms_out}, static_cast<cudaStream_t>(stream_));
+  return launch_clip(s, s->idx, s->plan, call, stream);
+}
+
+int ps_aggregate_clipped(ps_service* s, const ps_task* ready, int n_ready, float max_norm, float* norms_out,
+                         void* stream) {
+  if (!alive(s)) return PS_ERR_BAD_HANDLE;
+  std::lock_guard<std::mutex> lk(s->mu);
+  if (bad_clip(max_norm, norms_out)) return PS_ERR_BAD_ARG;
+  try {                                    // (the table and its lists are vectors)
+    return aggregate_clipped(s, ready, n_ready, ClipCall{max_norm, norms_out}, static_cast<cudaStream_t>(stream));
+  } catch (const std::bad_alloc&) {
+    return PS_ERR_NOMEM;
+  }
 }
 
 static int push_batch_locked(ps_service* s, int n, const int* jobs, const int* blocks, const int* workers,
@@ -1826,7 +1836,11 @@ int ps_round_run_clipped(ps_service* s, int round, float max_norm, float* norms_
   std::lock_guard<std::mutex> lk(s->mu);
   if (bad_clip(max_norm, norms_out)) return PS_ERR_BAD_ARG;
   const ClipCall call = {max_norm, norms_out};
-  return round_run(s, round, &call, stream, params_out);
+  try {
+    return round_run(s, round, &call, stream, params_out);
+  } catch (const std::bad_alloc&) {        // the round could not be resolved: no push has been made
+    return PS_ERR_NOMEM;
+  }
 }
 
 int ps_join(ps_service* s, void* stream_) {
