@@ -1,7 +1,9 @@
 """ctypes binding of the C-ABI library (include/ps_b200.h).
 
 Argument marshalling only: every step of the aggregation path runs in the
-library's CUDA kernels.  The module-level functions carry the names of the C
+library's CUDA kernels.  The calls on 4-bit operands (ps_mx_quantize,
+ps_mx_dequantize, ps_mx_matmul), which run for a few microseconds, come from a
+small extension module instead of ctypes.  The module-level functions carry the names of the C
 entry points; `Service` is a thin object wrapper over the same calls.  If the
 shared library is missing or cannot be loaded the import of `load()` raises —
 there is no fallback of any kind.
@@ -168,8 +170,8 @@ def load():
             from . import build as _build
             _build.build()
         except Exception as e:      # noqa: BLE001
-            if not os.path.exists(LIB_PATH):
-                raise ImportError("%s is missing and could not be built (%s): run "
+            if not os.path.exists(LIB_PATH) or not os.path.exists(_build.OPS):
+                raise ImportError("%s or its Python extension is missing and could not be built (%s): run "
                                   "`python -m paper_2204_03211_b200.build`" % (LIB_PATH, e))
         lib = C.CDLL(LIB_PATH)
         for name, (res, args) in _SIGNATURES.items():
@@ -177,6 +179,16 @@ def load():
             fn.restype, fn.argtypes = res, args
         _lib = lib
     return _lib
+
+
+_FROM_OPS = ("ps_mx_quantize", "ps_mx_dequantize", "ps_mx_matmul", "MxTensor")
+
+
+def __getattr__(name):
+    if name in _FROM_OPS:
+        _load_ops()             # defines them
+        return globals()[name]
+    raise AttributeError("module %r has no attribute %r" % (__name__, name))
 
 
 def ps_strerror(status: int) -> str:
@@ -663,27 +675,55 @@ def _check_op(rc: int, where: str):
         raise PsError(rc, where, load().ps_op_last_error().decode() if rc == PS_ERR_CUDA else "")
 
 
-_DTYPES = {}            # torch.dtype -> ps_dtype, filled at the first call (this module imports torch only where it is used)
+_DTYPES = {}            # torch.dtype -> ps_dtype, filled by _load_ops()
 
 
 def _dtype(t, where: str) -> int:
+    if not _DTYPES:
+        _load_ops()
     d = _DTYPES.get(t.dtype)
     if d is None:
-        import torch
-        _DTYPES.update({torch.float32: PS_F32, torch.bfloat16: PS_BF16})
-        d = _DTYPES.get(t.dtype)
-        if d is None:
-            raise PsError(PS_ERR_BAD_ARG, where, "%s is neither float32 nor bfloat16" % t.dtype)
+        raise PsError(PS_ERR_BAD_ARG, where, "%s is neither float32 nor bfloat16" % t.dtype)
     return d
 
 
-def _matrix(t, where: str):
-    """(address, ps_dtype, rows, columns, row stride) of a 2-d device tensor whose rows are contiguous."""
-    shape, strides = t.shape, t.stride()
-    if len(shape) != 2 or not t.is_cuda or (strides[1] != 1 and shape[1] > 1):
-        raise PsError(PS_ERR_BAD_ARG, where, "a 2-d CUDA tensor with contiguous rows is wanted")
-    rows, cols = shape
-    return t.data_ptr(), _dtype(t, where), rows, cols, strides[0] if rows > 1 else cols
+def _raise_op(status: int, where: str, detail):
+    raise PsError(status, where, detail or (load().ps_op_last_error().decode() if status == PS_ERR_CUDA else ""))
+
+
+def _load_ops():
+    """Puts the extension's calls and the operand class into this module, at their
+    first use: nothing else here needs torch."""
+    import torch
+
+    load()
+
+    from . import _ops
+    _DTYPES.update({torch.float32: PS_F32, torch.bfloat16: PS_BF16})
+    _ops.setup(torch.float32, torch.bfloat16, _raise_op)
+
+    class MxTensor(_ops.Operand):
+        """A microscaled 4-bit operand of rows x cols elements and the two device
+        buffers that hold it (`codes` and `scales`, uint8, in the library's layout)."""
+
+        def __new__(cls, rows: int, cols: int, device=None):
+            return super().__new__(cls)
+
+        def __init__(self, rows: int, cols: int, device=None):
+            n, m = C.c_size_t(), C.c_size_t()
+            _check_op(load().ps_mx_sizes(rows, cols, C.byref(n), C.byref(m)), "ps_mx_sizes")
+            self.codes = torch.empty(n.value, dtype=torch.uint8, device=device or "cuda")
+            self.scales = torch.empty(m.value, dtype=torch.uint8, device=device or "cuda")
+            super().__init__(self.codes.data_ptr(), self.scales.data_ptr(), rows, cols)
+
+        @property
+        def shape(self):
+            return self.rows, self.cols
+
+    MxTensor.__qualname__ = "MxTensor"
+    for name in _FROM_OPS[:3]:
+        globals()[name] = getattr(_ops, name)
+    globals()["MxTensor"] = MxTensor
 
 
 class Clip:
@@ -730,56 +770,6 @@ class Clip:
             self.close()
         except Exception:
             pass
-
-
-class MxTensor:
-    """A microscaled 4-bit operand of rows x cols elements and the two device
-    buffers that hold it (`codes` and `scales`, uint8, in the library's layout)."""
-
-    def __init__(self, rows: int, cols: int, device=None):
-        import torch
-        n, m = C.c_size_t(), C.c_size_t()
-        _check_op(load().ps_mx_sizes(rows, cols, C.byref(n), C.byref(m)), "ps_mx_sizes")
-        self.rows, self.cols = rows, cols
-        self.codes = torch.empty(n.value, dtype=torch.uint8, device=device or "cuda")
-        self.scales = torch.empty(m.value, dtype=torch.uint8, device=device or "cuda")
-        self._c = ps_mx(self.codes.data_ptr(), self.scales.data_ptr(), rows, cols)
-        self.ref = C.addressof(self._c)
-
-    @property
-    def shape(self):
-        return self.rows, self.cols
-
-
-def ps_mx_quantize(x, q=None, qt=None, stream=None):
-    """Quantises the device matrix x (float32 or bfloat16, any row stride) along
-    its rows into q and / or along its columns into qt (x's transpose)."""
-    ptr, dtype, rows, cols, ld = _matrix(x, "ps_mx_quantize")
-    rc = load().ps_mx_quantize(ptr, dtype, rows, cols, ld, q and q.ref, qt and qt.ref, _stream_ptr(stream))
-    if rc:
-        _check_op(rc, "ps_mx_quantize")
-
-
-def ps_mx_dequantize(q, out, stream=None):
-    """Writes the values q stands for to the device matrix out, which it returns."""
-    ptr, dtype, rows, cols, ld = _matrix(out, "ps_mx_dequantize")
-    if rows != q.rows or cols != q.cols:
-        raise PsError(PS_ERR_BAD_ARG, "ps_mx_dequantize", "out is %s, the operand %s" % ((rows, cols), q.shape))
-    rc = load().ps_mx_dequantize(q.ref, dtype, ptr, ld, _stream_ptr(stream))
-    if rc:
-        _check_op(rc, "ps_mx_dequantize")
-    return out
-
-
-def ps_mx_matmul(a, b, out, stream=None):
-    """out[m][n] = sum over k of a[m][k] * b[n][k]; returns out (float32 or bfloat16, any row stride)."""
-    ptr, dtype, rows, cols, ld = _matrix(out, "ps_mx_matmul")
-    if rows != a.rows or cols != b.rows:
-        raise PsError(PS_ERR_BAD_ARG, "ps_mx_matmul", "out is %s, the product %s" % ((rows, cols), (a.rows, b.rows)))
-    rc = load().ps_mx_matmul(a.ref, b.ref, dtype, ptr, ld, _stream_ptr(stream))
-    if rc:
-        _check_op(rc, "ps_mx_matmul")
-    return out
 
 
 def ps_mx_status() -> int:

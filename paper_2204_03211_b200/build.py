@@ -2,19 +2,21 @@
 
     python -m paper_2204_03211_b200.build [--force] [--verbose]
 
-The library is rebuilt when any source under csrc/ or the public header is
-newer than the .so.  FMA contraction is disabled (--fmad=false) on top of the
+The library, and the small Python extension that calls it (csrc/ps_python.c, gcc),
+are rebuilt when any source under csrc/ or the public header is newer than them.  FMA contraction is disabled (--fmad=false) on top of the
 explicit round-to-nearest intrinsics in the kernels; fast-math is never used.
 """
 import glob
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libps_b200.so")
+OPS = os.path.join(HERE, "_ops" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = [os.path.join(CSRC, "ps_service.cu"), os.path.join(CSRC, "ps_planner.cpp"), os.path.join(CSRC, "ps_peer.cpp"),
            os.path.join(CSRC, "ps_mx.cu"), os.path.join(CSRC, "ps_clip.cu")]
 
@@ -33,16 +35,26 @@ def nvcc_command(verbose: bool = False):
     return cmd
 
 
-def build(force: bool = False, verbose: bool = False) -> str:
-    if not force and os.path.exists(LIB):
-        newest = max(os.path.getmtime(p) for p in _deps())
-        if os.path.getmtime(LIB) >= newest:
-            return LIB
-    res = subprocess.run(nvcc_command(verbose), capture_output=True, text=True)
+def ops_command():
+    return ["gcc", "-std=gnu11", "-O2", "-Wall", "-fPIC", "-shared", "-I", sysconfig.get_paths()["include"],
+            "-I", os.path.join(ROOT, "include"), "-o", OPS, os.path.join(CSRC, "ps_python.c"), "-L", HERE, "-lps_b200",
+            "-Wl,-rpath,$ORIGIN"]
+
+
+def _run(cmd, target: str, verbose: bool):
+    res = subprocess.run(cmd, capture_output=True, text=True)
     if verbose or res.returncode:
         sys.stderr.write(res.stdout + res.stderr)
     if res.returncode:
-        raise RuntimeError("nvcc failed building %s" % LIB)
+        raise RuntimeError("%s failed building %s" % (cmd[0], target))
+
+
+def build(force: bool = False, verbose: bool = False) -> str:
+    newest = max(os.path.getmtime(p) for p in _deps())
+    if force or not os.path.exists(LIB) or os.path.getmtime(LIB) < newest:
+        _run(nvcc_command(verbose), LIB, verbose)
+    if force or not os.path.exists(OPS) or os.path.getmtime(OPS) < newest:
+        _run(ops_command(), OPS, verbose)
     return LIB
 
 

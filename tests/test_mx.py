@@ -298,6 +298,40 @@ def test_refusals():
     assert lib.ps_mx_status(None) == bad
 
 
-def test_binding_refuses_wrong_tensors():
+def test_binding_refuses_wrong_arguments():
+    q = B.MxTensor(4, 64, device="cpu")
+    assert (q.rows, q.cols, q.shape) == (4, 64, (4, 64))
+    x = torch.zeros(4, 64)
+    with pytest.raises(B.PsError) as e:                          # not on a GPU
+        B.ps_mx_quantize(x, q)
+    assert e.value.status == B.PS_ERR_BAD_ARG
     with pytest.raises(B.PsError):
-        B.ps_mx_quantize(torch.zeros(4, 64), B.MxTensor(4, 64, device="cpu"))
+        B.ps_mx_dequantize(q, x)
+    with pytest.raises(B.PsError):
+        B.MxTensor(4, 0)
+    for call in (lambda: B.ps_mx_quantize(), lambda: B.ps_mx_quantize(x, x), lambda: B.ps_mx_quantize(x, q, None, None, 1),
+                 lambda: B.ps_mx_quantize(x, q, q=q), lambda: B.ps_mx_quantize(x, bias=q), lambda: B.ps_mx_matmul(q, q),
+                 lambda: B.ps_mx_matmul(q, "b", x), lambda: B.MxTensor()):
+        with pytest.raises(TypeError):
+            call()
+    with pytest.raises(AttributeError):
+        B.ps_mx_quantise
+
+
+@pytest.mark.gpu
+def test_binding_checks_shapes_and_types_and_takes_keywords():
+    x, q = torch.randn(8, 64, device="cuda"), B.MxTensor(8, 64)
+    qt = B.MxTensor(64, 8)
+    assert B.ps_mx_quantize(x, qt=qt, stream=torch.cuda.current_stream()) is None
+    B.ps_mx_quantize(x=x, q=q, stream=torch.cuda.current_stream().cuda_stream)
+    out = torch.empty(8, 8, device="cuda")
+    assert B.ps_mx_matmul(q, b=q, out=out) is out and out.equal(values(q) @ values(q).t())
+    for bad in (lambda: B.ps_mx_matmul(q, q, torch.empty(8, 9, device="cuda")), lambda: B.ps_mx_matmul(q, qt, out),
+                lambda: B.ps_mx_quantize(x, qt), lambda: B.ps_mx_quantize(x), lambda: B.ps_mx_quantize(x.double(), q),
+                lambda: B.ps_mx_quantize(x[0], q), lambda: B.ps_mx_quantize(x.t(), qt), lambda: B.ps_mx_dequantize(q, out),
+                lambda: B.ps_mx_quantize(x[:1].expand(8, 64), q)):
+        with pytest.raises(B.PsError) as e:
+            bad()
+        assert e.value.status == B.PS_ERR_BAD_ARG
+    with pytest.raises(AttributeError):
+        B.ps_mx_quantize(x, q, stream="main")
