@@ -137,7 +137,7 @@ int quantize(const void* x, long long rows, long long cols, long long ld, MxOut 
     if (e != cudaSuccess) return op_cuda_error("cudaFuncSetAttribute", e);
   }
   return launch("quantise", ps_mx_quantize_kernel<BF16, ROWS, COLS>, (unsigned)(nc * nr), kQuantThreads, smem, 1, stream,
-                static_cast<const T*>(x), rows, cols, ld, vec_ok, (unsigned)nc, out, out_t);
+                static_cast<const T*>(x), (int)rows, (int)cols, ld, vec_ok, (unsigned)nc, out, out_t);
 }
 
 bool make_map(CUtensorMap* m, const ps_mx* q, int box_rows) {

@@ -115,8 +115,8 @@ __device__ __forceinline__ void mx_pdl() {
 // goes to shared memory with asynchronous 16-byte copies, all of them in flight at
 // once (read through registers, with a few loads in flight per thread, the kernel
 // waited for memory: 35 us for 8192 x 4096 bf16 both ways instead of 22.5); both
-// directions then cost one read of x.  Along the rows a block sits in four
-// neighbouring lanes (two shuffles give its maximum); along the columns a thread
+// directions then cost one read of x.  Along the rows a block sits in two
+// neighbouring lanes (one shuffle gives its maximum); along the columns a thread
 // takes one block of 32 rows of one column (a pair of columns of bf16) and reads it
 // twice, for the maximum and for the codes, which halves its registers.  The four
 // row blocks of a column sit in one warp and are stored as 64 bytes; their shared
@@ -142,8 +142,8 @@ __device__ __forceinline__ void copy16(unsigned int dst, const void* src, unsign
 
 template <bool BF16, bool ROWS, bool COLS>
 __global__ void __launch_bounds__(kQuantThreads, BF16 ? 6 : 3)
-ps_mx_quantize_kernel(const typename MxIn<BF16>::T* __restrict__ x, long long rows, long long cols, long long ld,
-                      int vec_ok, unsigned int col_tiles, MxOut out, MxOut out_t) {
+ps_mx_quantize_kernel(const typename MxIn<BF16>::T* __restrict__ x, int rows, int cols, long long ld, int vec_ok,
+                      unsigned int col_tiles, MxOut out, MxOut out_t) {
   using T = typename MxIn<BF16>::T;
   constexpr int kWords = BF16 ? 64 : 128;                     // 32-bit words of a tile row
   constexpr int kPiece = 16 / sizeof(T);                      // elements of a copy
@@ -151,8 +151,9 @@ ps_mx_quantize_kernel(const typename MxIn<BF16>::T* __restrict__ x, long long ro
   extern __shared__ __align__(16) unsigned int tile[];        // 128 rows of kWords
   __shared__ __align__(16) unsigned char s_row[kMxAtom], s_col[kMxAtom];
   const int tid = threadIdx.x;
-  const long long rt = blockIdx.x / col_tiles, ct = blockIdx.x % col_tiles;
-  const long long r0 = rt * kMxTile, c0 = ct * kMxTile;
+  const int rt = (int)(blockIdx.x / col_tiles), ct = (int)(blockIdx.x % col_tiles);
+  const int r0 = rt * kMxTile, c0 = ct * kMxTile;            // (rows and columns stay below 2^30)
+  const unsigned int pitch = (unsigned int)mx_pitch(cols), pitch_t = (unsigned int)mx_pitch(rows);
   if (tid < kMxAtom / 4) {
     if (ROWS) reinterpret_cast<unsigned int*>(s_row)[tid] = 0u;
     if (COLS) reinterpret_cast<unsigned int*>(s_col)[tid] = 0u;
@@ -162,8 +163,8 @@ ps_mx_quantize_kernel(const typename MxIn<BF16>::T* __restrict__ x, long long ro
   {
     constexpr int kStepRows = kQuantThreads / kPieces;
     const int g = tid % kPieces, rr = tid / kPieces;
-    const long long c = c0 + g * kPiece;
-    const long long left = cols - c;                          // elements of this thread's pieces inside the matrix
+    const int c = c0 + g * kPiece;
+    const int left = cols - c;                                // elements of this thread's pieces inside the matrix
     const unsigned int n = left <= 0 ? 0u : left < kPiece ? (unsigned int)left : (unsigned int)kPiece;
     const T* p = x + (size_t)(r0 + rr) * (size_t)ld + (size_t)c;
 #pragma unroll
@@ -190,45 +191,58 @@ ps_mx_quantize_kernel(const typename MxIn<BF16>::T* __restrict__ x, long long ro
   __syncthreads();
 
   if constexpr (ROWS) {
-    // 16 lanes cover a row of the tile, 16 rows per step
-    const int g = tid & 15, rr = tid >> 4;
-    const long long c = c0 + g * 8;
-    uint8_t* codes = out.codes + (size_t)(r0 + rr) * (size_t)mx_pitch(cols) + (size_t)(c >> 1);
+    // 8 lanes of 16 elements cover a row of the tile, 32 rows per step; two neighbouring lanes hold a block
+    const int g = tid & 7, rr = tid >> 3;
+    const int c = c0 + g * 16, first = g >> 2;                // which half a lane reads first: eight lanes then meet in no bank
+    uint8_t* codes = out.codes + (size_t)(r0 + rr) * pitch + (size_t)(c >> 1);
 #pragma unroll 2
-    for (int step = 0; step < 8; ++step) {
-      const int tr = step * 16 + rr;
-      unsigned int sb, q;
+    for (int step = 0; step < 4; ++step) {
+      const int tr = step * 32 + rr;
+      unsigned int sb, q[2];
       if constexpr (BF16) {
-        const uint4 raw = *reinterpret_cast<const uint4*>(tile + tile_word<kWords>(tr, g * 4));
-        const unsigned int w[4] = {raw.x, raw.y, raw.z, raw.w};
-        unsigned int m = max_abs_bf16x2(max_abs_bf16x2(w[0], w[1]), max_abs_bf16x2(w[2], w[3]));
+        // (8 words: the permutation moves them together)
+        const uint4* p = reinterpret_cast<const uint4*>(tile + tile_word<kWords>(tr, g * 8));
+        const uint4 u0 = p[first], u1 = p[first ^ 1];
+        const unsigned int w0[4] = {u0.x, u0.y, u0.z, u0.w}, w1[4] = {u1.x, u1.y, u1.z, u1.w};
+        unsigned int m = max_abs_bf16x2(max_abs_bf16x2(max_abs_bf16x2(w0[0], w0[1]), max_abs_bf16x2(w0[2], w0[3])),
+                                        max_abs_bf16x2(max_abs_bf16x2(w1[0], w1[1]), max_abs_bf16x2(w1[2], w1[3])));
         m = max_abs_bf16x2(m, __shfl_xor_sync(0xffffffffu, m, 1));
-        m = max_abs_bf16x2(m, __shfl_xor_sync(0xffffffffu, m, 2));
         m = max_abs_bf16x2(m, m >> 16);
         sb = mx_scale_byte((m >> 7) & 0xffu);
-        q = mx_codes8(w, ((254u - sb) << 7) * 0x10001u);
+        const unsigned int inv = ((254u - sb) << 7) * 0x10001u;
+        q[0] = mx_codes8(w0, inv);
+        q[1] = mx_codes8(w1, inv);
       } else {
-        const float4 a = *reinterpret_cast<const float4*>(tile + tile_word<kWords>(tr, g * 8));
-        const float4 b = *reinterpret_cast<const float4*>(tile + tile_word<kWords>(tr, g * 8 + 4));
-        const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-        float m = max_abs(max_abs(max_abs(v[0], v[1]), max_abs(v[2], v[3])), max_abs(max_abs(v[4], v[5]), max_abs(v[6], v[7])));
+        // (halves of 8 elements, which the permutation moves apart, two 16-byte pieces each, in an order that also
+        // depends on the lane: the codes of the two pieces change places below)
+        const float4* p0 = reinterpret_cast<const float4*>(tile + tile_word<kWords>(tr, g * 16 + first * 8));
+        const float4* p1 = reinterpret_cast<const float4*>(tile + tile_word<kWords>(tr, g * 16 + (first ^ 1) * 8));
+        const int piece = (g >> 1) & 1;
+        const float4 a = p0[piece], b = p0[piece ^ 1], d = p1[piece], e = p1[piece ^ 1];
+        const float v0[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}, v1[8] = {d.x, d.y, d.z, d.w, e.x, e.y, e.z, e.w};
+        float m = max_abs(v0[0], v1[0]);
+#pragma unroll
+        for (int i = 1; i < 8; ++i) m = max_abs(m, max_abs(v0[i], v1[i]));
         m = max_abs(m, __shfl_xor_sync(0xffffffffu, m, 1));
-        m = max_abs(m, __shfl_xor_sync(0xffffffffu, m, 2));
         sb = mx_scale_byte((__float_as_uint(m) >> 23) & 0xffu);
-        q = mx_codes8(v, mx_inverse(sb));
+        const float inv = mx_inverse(sb);
+        q[0] = mx_codes8(v0, inv);
+        q[1] = mx_codes8(v1, inv);
+        q[0] = __funnelshift_l(q[0], q[0], 16 * piece);
+        q[1] = __funnelshift_l(q[1], q[1], 16 * piece);
       }
-      if (r0 + tr < rows && (c & ~31ll) < cols) {
-        *reinterpret_cast<unsigned int*>(codes) = q;
-        if ((g & 3) == 0) s_row[(tr & 31) * 16 + (tr >> 5) * 4 + (g >> 2)] = (unsigned char)sb;
+      if (r0 + tr < rows && (c & ~31) < cols) {
+        *reinterpret_cast<uint2*>(codes) = first ? make_uint2(q[1], q[0]) : make_uint2(q[0], q[1]);
+        if ((g & 1) == 0) s_row[(tr & 31) * 16 + (tr >> 5) * 4 + (g >> 1)] = (unsigned char)sb;
       }
-      codes += 16 * (size_t)mx_pitch(cols);
+      codes += 32 * (size_t)pitch;
     }
   }
   if constexpr (COLS) {
     // thread: row block rb of one column (fp32) or of a pair of columns (bf16)
     const int rb = (tid >> 3) & 3;
     const bool any = r0 + rb * 32 < rows;
-    uint8_t* codes = out_t.codes + (size_t)(r0 / 2 + rb * 16);
+    uint8_t* codes = out_t.codes + (r0 / 2 + rb * 16);
     if constexpr (BF16) {
       const int cw = (tid & 7) + (tid >> 5) * 8;              // word = pair of columns
       const unsigned int* w = tile + tile_word<kWords>(rb * 32, cw);    // (the permutation is the same in all 32 rows)
@@ -254,7 +268,7 @@ ps_mx_quantize_kernel(const typename MxIn<BF16>::T* __restrict__ x, long long ro
       for (int h = 0; h < 2; ++h) {
         const int tc = 2 * cw + h;
         if (any && c0 + tc < cols) {
-          *reinterpret_cast<uint4*>(codes + (size_t)(c0 + tc) * (size_t)mx_pitch(rows)) =
+          *reinterpret_cast<uint4*>(codes + (size_t)(c0 + tc) * pitch_t) =
               h ? make_uint4(hi[0], hi[1], hi[2], hi[3]) : make_uint4(lo[0], lo[1], lo[2], lo[3]);
           s_col[(tc & 31) * 16 + (tc >> 5) * 4 + rb] = (unsigned char)sb[h];
         }
@@ -278,7 +292,7 @@ ps_mx_quantize_kernel(const typename MxIn<BF16>::T* __restrict__ x, long long ro
           q[k] = mx_codes8(u, inv);
         }
         if (any && c0 + tc < cols) {
-          *reinterpret_cast<uint4*>(codes + (size_t)(c0 + tc) * (size_t)mx_pitch(rows)) = make_uint4(q[0], q[1], q[2], q[3]);
+          *reinterpret_cast<uint4*>(codes + (size_t)(c0 + tc) * pitch_t) = make_uint4(q[0], q[1], q[2], q[3]);
           s_col[(tc & 31) * 16 + (tc >> 5) * 4 + rb] = (unsigned char)sb;
         }
       }
@@ -288,10 +302,10 @@ ps_mx_quantize_kernel(const typename MxIn<BF16>::T* __restrict__ x, long long ro
   // the atoms; tiles past the end exist to write the padding atoms' zeros
   if (tid < kMxAtom / 16) {
     if (ROWS && r0 < rows && ct < mx_atoms(cols))
-      reinterpret_cast<uint4*>(out.scales + (size_t)(rt * mx_atoms(cols) + ct) * kMxAtom)[tid] =
+      reinterpret_cast<uint4*>(out.scales + (size_t)((long long)rt * mx_atoms(cols) + ct) * kMxAtom)[tid] =
           reinterpret_cast<const uint4*>(s_row)[tid];
     if (COLS && c0 < cols && rt < mx_atoms(rows))
-      reinterpret_cast<uint4*>(out_t.scales + (size_t)(ct * mx_atoms(rows) + rt) * kMxAtom)[tid] =
+      reinterpret_cast<uint4*>(out_t.scales + (size_t)((long long)ct * mx_atoms(rows) + rt) * kMxAtom)[tid] =
           reinterpret_cast<const uint4*>(s_col)[tid];
   }
 }
