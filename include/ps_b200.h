@@ -346,8 +346,11 @@ int ps_round_release(ps_service* svc, int round);
  * ONE call: each call takes its own norm.
  * One cooperative launch on `stream` itself, also with PS_OPT_OVERLAP (rounds held
  * back by PS_OPT_BATCH go out before it); PS_OPT_KERNEL and PS_OPT_PROFILE do not
- * apply.  The first call, and one that lists more elements than any before, allocate
- * 4 bytes of device memory per listed element and wait for the device.
+ * apply.  The first call allocates a little device memory; a call whose sums exceed
+ * the GPU's shared memory (about 7 million elements) keeps them in a buffer of 4 bytes
+ * per listed element, not counting blocks whose W shards take up to 8 bytes per
+ * element, which are read twice.  That buffer belongs to the service; a call that needs
+ * a larger one than any before waits for the device.
  * Errors: those of ps_aggregate; BAD_ARG (max_norm not above 0, norms_dev_out not
  * aligned to 4 bytes), TOO_LARGE (more than 64 jobs, rows of more than 2^30 elements
  * in a row-sparse push). */

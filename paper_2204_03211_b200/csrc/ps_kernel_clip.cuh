@@ -133,6 +133,16 @@ __device__ __forceinline__ unsigned int clip_find(const unsigned int* starts, un
   return lo;
 }
 
+// Where the sum of a chunk's element 0 is kept.  Of a task whose shards are read again only the last few elements of a
+// chunk are (from element `whole` on, fewer than eight): eight places per chunk.
+__device__ __forceinline__ float* clip_place(const PsTaskDev* T, unsigned int idx, unsigned int count, bool kept, float* cache,
+                                             float* spool) {
+  if (kept) return cache;
+  const unsigned int k = idx - T->first_chunk;
+  if (!T->reread) return spool + T->spool + (size_t)k * T->chunk_elems;
+  return spool + T->spool + 8 * (size_t)k - (count & ~7u);
+}
+
 // A job's chunk sums in a fixed order: thread t takes t, t + NT, ..., then the block adds its threads.
 template <int NT>
 __device__ __forceinline__ double clip_total(const double* parts, unsigned int n, unsigned int tid, double* red) {
@@ -189,7 +199,7 @@ __device__ __forceinline__ void clip_body(const unsigned char* table, const PsJo
     const size_t begin = (size_t)(idx - T->first_chunk) * T->chunk_elems;
     const unsigned int count = (unsigned int)min((unsigned long long)T->chunk_elems, T->nelem - begin);
     const bool kept = round == 0 && T->chunk_elems <= kClipSlot;
-    float* G_at = kept ? cache : spool + T->spool + begin;
+    float* G_at = clip_place(T, idx, count, kept, cache, spool);
     const void* const* shards = ptrs + T->shard_row;
     double sq = 0.0;
     unsigned int done = 0;
@@ -200,7 +210,7 @@ __device__ __forceinline__ void clip_body(const unsigned char* table, const PsJo
         sq = store ? clip_sum_vec<kSumOnly, true, kThreads>(tid, shards, J->W, J->gs, G_at, begin, done)
                    : clip_sum_vec<kNormOnly, true, kThreads>(tid, shards, J->W, J->gs, G_at, begin, done);
       } else {
-        done = count & ~3u;
+        done = store ? count & ~3u : count & ~7u;
         sq = store ? clip_sum_vec<kSumOnly, false, kThreads>(tid, shards, J->W, J->gs, G_at, begin, done)
                    : clip_sum_vec<kNormOnly, false, kThreads>(tid, shards, J->W, J->gs, G_at, begin, done);
       }
@@ -262,12 +272,12 @@ __device__ __forceinline__ void clip_body(const unsigned char* table, const PsJo
     const size_t begin = (size_t)(idx - T->first_chunk) * T->chunk_elems;
     const unsigned int count = (unsigned int)min((unsigned long long)T->chunk_elems, T->nelem - begin);
     const bool kept = own && T->chunk_elems <= kClipSlot;
-    const float* G_at = kept ? cache : spool + T->spool + begin;
+    const float* G_at = clip_place(T, idx, count, kept, cache, spool);
     const float factor = s_factor[T->job_slot];
     unsigned int done = 0;
     if (T->reread && !kept) {
       const void* const* shards = ptrs + T->shard_row;
-      done = count & (J->grad_dtype ? ~7u : ~3u);
+      done = count & ~7u;
       switch ((J->opt << 1) | J->grad_dtype) {
         case 0: clip_apply_shards<0, false, kThreads>(tid, J, T, factor, shards, begin, done); break;
         case 1: clip_apply_shards<0, true, kThreads>(tid, J, T, factor, shards, begin, done); break;

@@ -1335,7 +1335,7 @@ int build_clip_plan(ps_service* s, const std::vector<int>& idx, Plan* plan) try 
   const void** ptrs = reinterpret_cast<const void**>(base + ptrs_off);
   PsSparseDev* sp = reinterpret_cast<PsSparseDev*>(base + sparse_off);
   const unsigned int ce = clip_chunk(s, idx, (unsigned int)(s->num_sms * s->clip_ctas));
-  unsigned long long chunk = 0, spool = 0;
+  unsigned long long chunk = 0, spool = 0, unkept = 0;      // unkept: places of tasks whose chunks exceed shared memory
   size_t row = 0, sp_row = 0, slot = 0;
   plan->algo_bytes = 0;
   for (size_t i = 0; i < n; ++i) {
@@ -1378,7 +1378,9 @@ int build_clip_plan(ps_service* s, const std::vector<int>& idx, Plan* plan) try 
     t.spool = spool;
     chunk += nchunks;
     if (chunk > 0x7ffffff0ull) return PS_ERR_BAD_ARG;
-    spool += (b.nelem + 63) / 64 * 64;
+    const unsigned long long places = t.reread ? 8 * nchunks : (b.nelem + 63) / 64 * 64;
+    spool += places;
+    if (t.chunk_elems > kClipSlot) unkept += places;
     row += W;
     plan->algo_bytes += b.nelem * bytes_per_elem(j);
   }
@@ -1394,7 +1396,8 @@ int build_clip_plan(ps_service* s, const std::vector<int>& idx, Plan* plan) try 
   h->sparse_off = (unsigned int)sparse_off;
   plan->total_chunks = (unsigned int)chunk;
   plan->chunk_elems = ce;
-  plan->spool = spool;
+  // a launch with one chunk per CTA keeps every sum in shared memory
+  plan->spool = chunk <= (unsigned long long)s->num_sms * s->clip_ctas && !unkept ? 0 : spool;
   return PS_OK;
 } catch (const std::bad_alloc&) {
   return PS_ERR_NOMEM;

@@ -496,3 +496,20 @@ def test_a_view_keeps_its_service():
     del view
     gc.collect()
     assert seen() is None
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("opt,dtype,W,shift", [(B.PS_SGD, B.PS_F32, 3, 0), (B.PS_ADAM, B.PS_BF16, 4, 0), (B.PS_SGD, B.PS_BF16, 5, 0),
+                                               (B.PS_ADAM, B.PS_F32, 1, 0), (B.PS_SGD, B.PS_BF16, 2, 1)])
+def test_large_launches_keep_or_read_again(opt, dtype, W, shift):
+    """More elements than shared memory holds, chunks that end in fewer than a vector: shards of up to 8 bytes per
+    element are read again, others' sums are kept; unaligned ones take the scalar path throughout."""
+    world = World([hparams(opt, dtype, W)], [[8_000_003, 130_005, 7, 1]], seed=W)
+    norms = torch.zeros(1, device="cuda")
+    for limit in (0.5, 1e9):
+        world.gradients(shift=shift)
+        world.push()
+        world.svc.aggregate_clipped(world.ready, limit, norms)
+        world.check(limit, norms.cpu().numpy())
+    assert world.svc.launch_info()["kernel"] == "clip_inline"
+    world.svc.close()
