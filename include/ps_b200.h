@@ -348,8 +348,8 @@ int ps_round_release(ps_service* svc, int round);
  * back by PS_OPT_BATCH go out before it); PS_OPT_KERNEL and PS_OPT_PROFILE do not
  * apply.  The first call allocates a little device memory; a call whose sums exceed
  * the GPU's shared memory (about 7 million elements) keeps them in a buffer of 4 bytes
- * per listed element, not counting blocks whose W shards take up to 8 bytes per
- * element, which are read twice.  That buffer belongs to the service; a call that needs
+ * per listed element, not counting blocks whose W shards take at most 4 bytes per
+ * element (2 with Adam), which are read twice.  That buffer belongs to the service; a call that needs
  * a larger one than any before waits for the device.
  * Errors: those of ps_aggregate; BAD_ARG (max_norm not above 0, norms_dev_out not
  * aligned to 4 bytes), TOO_LARGE (more than 64 jobs, rows of more than 2^30 elements

@@ -1357,7 +1357,7 @@ int build_clip_plan(ps_service* s, const std::vector<int>& idx, Plan* plan) try 
       if (reinterpret_cast<uintptr_t>(b.pushed[w]) & 15u) t.vec_ok = 0;
     }
     t.chunk_elems = ce;
-    t.reread = !b.nsparse && t.vec_ok && W * j.grad_esize() <= kClipReread;
+    t.reread = !b.nsparse && t.vec_ok && W * j.grad_esize() <= (j.d.opt == PS_ADAM ? kClipRereadAdam : kClipRereadSgd);
     if (b.nsparse) {                       // chunks of whole rows
       if (b.row_len > (1u << 30)) return PS_ERR_TOO_LARGE;
       t.row_len = b.row_len;

@@ -499,11 +499,13 @@ def test_a_view_keeps_its_service():
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("opt,dtype,W,shift", [(B.PS_SGD, B.PS_F32, 3, 0), (B.PS_ADAM, B.PS_BF16, 4, 0), (B.PS_SGD, B.PS_BF16, 5, 0),
-                                               (B.PS_ADAM, B.PS_F32, 1, 0), (B.PS_SGD, B.PS_BF16, 2, 1)])
+@pytest.mark.parametrize("opt,dtype,W,shift", [
+    (B.PS_SGD, B.PS_F32, 3, 0), (B.PS_ADAM, B.PS_BF16, 4, 0), (B.PS_SGD, B.PS_BF16, 5, 0), (B.PS_ADAM, B.PS_F32, 1, 0),
+    (B.PS_SGD, B.PS_BF16, 2, 1), (B.PS_SGD, B.PS_F32, 1, 0), (B.PS_SGD, B.PS_BF16, 2, 0), (B.PS_ADAM, B.PS_BF16, 1, 0),
+])
 def test_large_launches_keep_or_read_again(opt, dtype, W, shift):
-    """More elements than shared memory holds, chunks that end in fewer than a vector: shards of up to 8 bytes per
-    element are read again, others' sums are kept; unaligned ones take the scalar path throughout."""
+    """More elements than shared memory holds, chunks that end in fewer than a vector: shards of few bytes per element
+    are read again, others' sums are kept; unaligned ones take the scalar path throughout."""
     world = World([hparams(opt, dtype, W)], [[8_000_003, 130_005, 7, 1]], seed=W)
     norms = torch.zeros(1, device="cuda")
     for limit in (0.5, 1e9):
