@@ -281,11 +281,12 @@ int ps_mx_matmul(const ps_mx* a, const ps_mx* b, int dtype, void* c, long long l
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
   if (thin && q->rows <= 16) return matmul<16>(p, q, args, d, stream);
   if (thin) return matmul<64>(p, q, args, d, stream);
-  // the pair's tiles read each operand less often; they are taken once they fill the device
-  const long long pairs = ((p->rows + 255) / 256) * ((q->rows + 255) / 256);
-  if (pairs >= d.num_sms / 2 - 12) return matmul_pair(p, q, args, d, stream);
-  // tiles of 128 x 64, two CTAs on an SM, while those of 128 x 128 would leave half of the SMs without one
+  // Up to one 128 x 128 tile per SM those tiles are taken, beyond that the pairs', which read each operand less often;
+  // where 128 x 128 would leave half of the SMs idle, 128 x 64, two CTAs on an SM.  Pairs | 128 x 128 | 128 x 64 in us:
+  // 2048 x 2048 x 4096 10.7 | 11.5 | 14.7, 1536 x 2048 x 4096 10.3 | 11.1 | 13.2, 1024 x 2048 x 4096 9.8 | 7.6 | 8.9,
+  // 1024 x 1024 x 4096 9.4 | 10.2 | 9.5, 1024 x 1024 x 512 5.2 | 4.6 | 4.4, 256 x 1024 x 512 5.1 | 4.5 | 3.8
   const long long tiles = ((p->rows + 127) / 128) * ((q->rows + 127) / 128);
+  if (tiles > d.num_sms) return matmul_pair(p, q, args, d, stream);
   if (tiles <= d.num_sms / 2) return matmul<64>(p, q, args, d, stream);
   return matmul<128>(p, q, args, d, stream);
 }

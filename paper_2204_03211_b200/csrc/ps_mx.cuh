@@ -114,7 +114,7 @@ __device__ __forceinline__ void mx_pdl() {
 // One CTA per 128 x 128 tile, i.e. one atom of scales in each direction.  The tile
 // goes to shared memory with asynchronous 16-byte copies, all of them in flight at
 // once (read through registers, with a few loads in flight per thread, the kernel
-// waited for memory: 35 us for 8192 x 4096 bf16 both ways instead of 22.5); both
+// waited for memory: 35 us for 8192 x 4096 bf16 both ways against 22.5 then); both
 // directions then cost one read of x.  Along the rows a block sits in two
 // neighbouring lanes (one shuffle gives its maximum); along the columns a thread
 // takes one block of 32 rows of one column (a pair of columns of bf16) and reads it
@@ -122,6 +122,10 @@ __device__ __forceinline__ void mx_pdl() {
 // row blocks of a column sit in one warp and are stored as 64 bytes; their shared
 // memory reads would meet in the same banks (a stride of 32 rows is a multiple of 32
 // banks whatever the pitch), so the column index is permuted by the row block.
+//
+// Measured on 8192 x 4096 bf16: rows 11.8 us (7.2 TB/s of values and codes), columns
+// 12.9 us, both 20.8 us (4.9 TB/s; issue slots 68 % busy, about 14 instructions per
+// element); fp32 both 31.6 us (5.4 TB/s).
 
 constexpr int kQuantThreads = 256;
 
@@ -314,10 +318,11 @@ ps_mx_quantize_kernel(const typename MxIn<BF16>::T* __restrict__ x, int rows, in
 //
 // A lane takes eight bytes of codes (sixteen elements, half a block), a warp 512
 // columns of a row, so that a lane stores whole sectors; a CTA takes 32 rows of such a
-// strip.  A nibble s eem placed as sign, exponent field 0..3 and top mantissa bit of a bf16
-// is its value times 2^-126, subnormals included: two
-// exact multiplications (2^126, the scale) give the result without a conversion
-// instruction, which issue at a fraction of the rate.
+// strip.  A nibble s eem placed as sign, exponent field 0..3 and top mantissa bit of a
+// bf16 is its value times 2^-126, subnormals included: two exact multiplications
+// (2^126, the scale) give the result without conversion instructions, which issue at a
+// fraction of the rate.  8192 x 4096 to bf16: 12.0 us, 7.1 TB/s of codes and values (with
+// eight elements per lane and 128-bit stores 15.3 us).
 
 // Nibbles 2j and 2j+1 of w as a pair of bf16 values, unscaled.
 __device__ __forceinline__ unsigned int mx_pair(unsigned int w, int j) {

@@ -20,6 +20,10 @@
 // and what is left is reading P once.  Such a product has few tiles, so the CTAs
 // of a cluster share a tile's K and add their parts in rank order through
 // distributed shared memory: no workspace, no atomics, the same result each time.
+//
+// Measured: 1 x 4096 x 1024 3.3 us, 8 x 4096 x 4096 5.5 us, 37 x 30522 x 1024 5.9 us with
+// the weight in L2 and 10 us cold (16.6 MB), 1000 x 256 x 300 3.8 us.  What is left is
+// latency: launch, the first copy, the MMAs of one tile, its store.
 #pragma once
 
 #include <cuda.h>
@@ -328,10 +332,11 @@ __device__ __forceinline__ void mm_cluster_sync() {
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// Four floats at `addr` of this CTA's layout, from the cluster's CTA `rank`.
+// Four floats at `addr` of this CTA's layout, from the cluster's CTA `rank`.  (volatile: not to be moved across the
+// cluster barriers)
 __device__ __forceinline__ float4 mm_remote4(unsigned int addr, unsigned int rank) {
   float4 v;
-  asm("{\n\t"
+  asm volatile("{\n\t"
       ".reg .b32 r;\n\t"
       "mapa.shared::cluster.u32 r, %4, %5;\n\t"
       "ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [r];\n\t"

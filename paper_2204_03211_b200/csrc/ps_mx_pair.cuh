@@ -1,15 +1,14 @@
 // Product of two microscaled 4-bit operands, large form: a pair of CTAs on two SMs
 // computes tiles of 256 rows of A by 256 rows of B (tcgen05 with cta_group::2).
 //
-// What bounds the one-CTA form on large operands is the traffic into shared memory:
-// at 128 x 256 a tile takes in 51 KB for every 512 cycles of MMA.  In the pair each
-// CTA loads its half of either operand, 35 KB for the same time, and the tensor cores
-// of both read both halves.  The leader (rank 0) issues the MMAs; both CTAs load their
-// own halves with their completion counted on the leader's barrier, which expects the
-// bytes of both (scales are copied by tensor map too, because only those copies can
-// signal the other CTA's barrier; the other CTA never arrives there itself: a remote
-// arrive with release semantics takes its thread 1400 cycles, nearly three stages).
-// Commits release the stages of both.
+// In the pair each CTA loads its half of either operand, 35 KB for every 512 cycles of
+// MMA (51 KB with 128 x 256 on one CTA), and the tensor cores of both read both
+// halves.  The leader (rank 0) issues the MMAs; both CTAs load their own halves with
+// their completion counted on the leader's barrier, which expects the bytes of both
+// (scales are copied by tensor map too, because only those copies can signal the other
+// CTA's barrier; the other CTA never arrives there itself: a remote arrive with release
+// semantics takes its thread 1400 cycles, nearly three stages).  Commits release the
+// stages of both.
 //   warp 0      one lane issues the copies of codes
 //   warp 1      leader only: scales to tensor memory, MMAs
 //   warp 10     one lane issues the copies of scales
@@ -17,6 +16,12 @@
 //               columns each, then release them and store while the next tile runs
 // 256 columns of accumulators and two sets of scales leave no room for a second set of
 // accumulators, so the release after the read is what lets the next tile start.
+//
+// Measured: 8192 x 4096 x 4096 49 us (5.6 PFLOP/s; on one CTA with 128 x 256 79.9 us),
+// 8192^3 178 us (6.2), 8192 x 4096 x 1024 20 us (3.5).  The tensor cores are busy 64 % of
+// the first: of 10000 cycles per tile 8192 are MMA and 1350 the wait for the accumulators
+// to be read; the rest is start, end and, under load, the power cap.  Short K is bound by
+// the stores of the result (3500 cycles per tile).
 #pragma once
 
 #include "ps_mx_gemm.cuh"
