@@ -162,9 +162,27 @@ def test_product(M, N, K, dtype):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("M,N,K", [(4000, 2817, 300), (2305, 4100, 1024), (20000, 250, 96)])
-def test_product_of_many_tiles(M, N, K):
-    check_product(M, N, K, torch.bfloat16)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("M,N,K", [(4000, 2817, 300), (2305, 4100, 1024), (20000, 250, 96), (1201, 1100, 600), (1024, 2048, 31),
+                                   (2049, 2304, 2600)])
+def test_product_of_many_tiles(M, N, K, dtype):
+    """Tiles of 128 x 128 and of CTA pairs, several per CTA, with edges in both directions."""
+    check_product(M, N, K, dtype)
+
+
+@pytest.mark.gpu
+def test_pairs_poison_only_what_they_should():
+    """A NaN in the last block of rows, and results that end inside a tile, in the pairs' tiles."""
+    a, b = torch.randn(2600, 320, device="cuda"), torch.randn(2500, 320, device="cuda")
+    a[2599, 319] = float("nan")
+    b[2499, 0] = float("-inf")
+    out = torch.full((2601, 2503), 3.0, device="cuda", dtype=torch.bfloat16)
+    B.ps_mx_matmul(quantized(a), quantized(b), out[:2600, :2500])
+    bad = torch.zeros(2600, 2500, dtype=torch.bool, device="cuda")
+    bad[2599] = True
+    bad[:, 2499] = True
+    assert torch.equal(out[:2600, :2500].isnan(), bad)
+    assert (out[2600] == 3.0).all() and (out[:, 2500:] == 3.0).all()
 
 
 @pytest.mark.gpu
