@@ -700,7 +700,7 @@ typedef struct ps_clip ps_clip; /* opaque */
 int ps_clip_create(ps_clip** out, int device, int n, const void* const* srcs, int src_dtype, void* const* dsts,
                    int dst_dtype, const size_t* nelems);
 
-/* One cooperative launch on `stream`.  max_norm > 0; +infinity means factor 1 (the
+/* One launch on `stream` (cooperative, except for short lists).  max_norm > 0; +infinity means factor 1 (the
  * norm, and the copy where destinations are their own).  norm_dev_out (device
  * float) may be NULL.  A factor of exactly 1 leaves tensors clipped in place
  * untouched.  Non-finite norms: as for ps_aggregate_clipped.  Runs of one ps_clip

@@ -400,6 +400,50 @@ def test_clip_extreme_values():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("src,dst,shift", [("f32", "f32", 0), ("bf16", "f32", 1), ("f32", "bf16", 0)])
+@pytest.mark.parametrize("units", [63, 64, 65, 127, 128, 129, 255, 256, 257, 296, 297])
+def test_clip_lists_around_the_limits_of_a_launch(units, src, dst, shift):
+    """Units of 2048 elements: a tensor of many with a ragged end, tensors of one unit, empty tensors between them."""
+    sizes = [5, 0, 2048 * (units - 4) - 3, 2048, 0, 2047, 1]
+    g = torch.Generator().manual_seed(units)
+    hosts = [torch.randn(n, generator=g).to(DT[src]) for n in sizes]
+    srcs = [torch.cat([torch.zeros(shift, dtype=DT[src]), h]).cuda()[shift:] for h in hosts]
+    dsts = [torch.full((n + shift,), 3.0, device="cuda", dtype=DT[dst])[shift:] for n in sizes]
+    true = np.sqrt(sum(float((h.double() ** 2).sum()) for h in hosts))
+    norm = torch.zeros(1, device="cuda")
+    clip = B.Clip(srcs, dsts)
+    clip.run(0.5, norm)
+    assert abs(norm.item() - true) <= 9 * 2.0 ** -24 * true
+    c = torch.tensor(factor(norm.item(), 0.5))
+    for h, d in zip(hosts, dsts):
+        assert torch.equal((h.float() * c).to(DT[dst]), d.cpu())
+    assert clip.status() == 0
+    clip.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [700, 40_000, 262_144])
+def test_clips_that_follow_one_another_read_what_the_one_before_wrote(n):
+    x = torch.randn(n) * 3
+    bufs = [x.clone().cuda()] + [torch.full((n,), 7.0, device="cuda") for _ in range(8)]
+    norms = torch.zeros(8, device="cuda")
+    clips = [B.Clip([bufs[k]], [bufs[k + 1]]) for k in range(8)]
+    for _ in range(20):
+        for k in range(8):
+            clips[k].run(64.0 / 2 ** k, norms[k:])
+        h = x
+        got = norms.cpu()
+        for k in range(8):
+            assert abs(got[k].item() - float(h.double().norm())) <= 9 * 2.0 ** -24 * float(h.double().norm())
+            h = h * torch.tensor(factor(got[k].item(), 64.0 / 2 ** k))
+            assert torch.equal(h, bufs[k + 1].cpu())
+        for b in bufs[1:]:
+            b.fill_(7.0)
+    for c in clips:
+        c.close()
+
+
+@pytest.mark.gpu
 def test_clip_on_streams():
     a, b = torch.randn(1_000_000, device="cuda"), torch.randn(1_000_000, device="cuda")
     out = [torch.empty_like(a) for _ in range(2)]
