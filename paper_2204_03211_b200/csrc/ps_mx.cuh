@@ -72,16 +72,26 @@ __device__ __forceinline__ unsigned int mul_bf16x2(unsigned int a, unsigned int 
   return r;
 }
 
-// Eight bf16 values as codes.  The division by the scale is done on pairs: it is exact, or the quotient is below
-// 2^-126 and far below the smallest code's half.  inv: 1 / scale of the values' block(s), twice.
+// The products of two pairs of bf16 values, in binary32: a mixed-precision fma unpacks and multiplies at once.  It adds
+// -0, which keeps the sign of a zero.  (A product of pairs, then unpacked, made both directions 22.0 instead of 20.4 us
+// for 8192 x 4096: the kernel is bound by the instructions it issues.)
+__device__ __forceinline__ void mx_divide(unsigned int w, unsigned int inv, float* lo, float* hi) {
+  asm("{\n\t"
+      ".reg .b16 a0, a1, s0, s1;\n\t"
+      "mov.b32 {a0, a1}, %2;\n\t"
+      "mov.b32 {s0, s1}, %3;\n\t"
+      "fma.rn.f32.bf16 %0, a0, s0, %4;\n\t"
+      "fma.rn.f32.bf16 %1, a1, s1, %4;\n\t"
+      "}"
+      : "=f"(*lo), "=f"(*hi)
+      : "r"(w), "r"(inv), "f"(-0.0f));
+}
+
+// Eight bf16 values as codes.  inv: 1 / scale of the values' block, twice.
 __device__ __forceinline__ unsigned int mx_codes8(const unsigned int (&w)[4], unsigned int inv) {
   float v[8];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const unsigned int q = mul_bf16x2(w[i], inv);
-    v[2 * i] = __uint_as_float(q << 16);
-    v[2 * i + 1] = __uint_as_float(q & 0xffff0000u);
-  }
+  for (int i = 0; i < 4; ++i) mx_divide(w[i], inv, &v[2 * i], &v[2 * i + 1]);
   return mx_pack8(v);
 }
 
@@ -123,9 +133,9 @@ __device__ __forceinline__ void mx_pdl() {
 // memory reads would meet in the same banks (a stride of 32 rows is a multiple of 32
 // banks whatever the pitch), so the column index is permuted by the row block.
 //
-// Measured on 8192 x 4096 bf16: rows 11.8 us (7.2 TB/s of values and codes), columns
-// 12.9 us, both 20.8 us (4.9 TB/s; issue slots 68 % busy, about 14 instructions per
-// element); fp32 both 31.6 us (5.4 TB/s).
+// Measured on 8192 x 4096 bf16, three matrices in rotation: rows 15.1 us (5.7 TB/s of
+// values and codes), columns 15.3 us, both 20.4 us (5.1 TB/s; bound by issue slots); fp32
+// both 32.3 us (5.3 TB/s).  Five CTAs per SM: with six the column pass spills (21.6 us).
 
 constexpr int kQuantThreads = 256;
 
@@ -145,7 +155,7 @@ __device__ __forceinline__ void copy16(unsigned int dst, const void* src, unsign
 }
 
 template <bool BF16, bool ROWS, bool COLS>
-__global__ void __launch_bounds__(kQuantThreads, BF16 ? 6 : 3)
+__global__ void __launch_bounds__(kQuantThreads, BF16 ? 5 : 3)
 ps_mx_quantize_kernel(const typename MxIn<BF16>::T* __restrict__ x, int rows, int cols, long long ld, int vec_ok,
                       unsigned int col_tiles, MxOut out, MxOut out_t) {
   using T = typename MxIn<BF16>::T;
@@ -261,9 +271,7 @@ ps_mx_quantize_kernel(const typename MxIn<BF16>::T* __restrict__ x, int rows, in
         float a[8], b[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const unsigned int q = mul_bf16x2(w[(k * 8 + i) * kWords], inv);
-          a[i] = __uint_as_float(q << 16);
-          b[i] = __uint_as_float(q & 0xffff0000u);
+          mx_divide(w[(k * 8 + i) * kWords], inv, &a[i], &b[i]);
         }
         lo[k] = mx_pack8(a);
         hi[k] = mx_pack8(b);
