@@ -704,7 +704,8 @@ def _load_ops():
 
     class MxTensor(_ops.Operand):
         """A microscaled 4-bit operand of rows x cols elements and the two device
-        buffers that hold it (`codes` and `scales`, uint8, in the library's layout)."""
+        buffers that hold it (`codes` and `scales`, uint8, in the library's layout).
+        The calls want their tensors and operands on the current device."""
 
         def __new__(cls, rows: int, cols: int, device=None):
             return super().__new__(cls)
@@ -714,7 +715,7 @@ def _load_ops():
             _check_op(load().ps_mx_sizes(rows, cols, C.byref(n), C.byref(m)), "ps_mx_sizes")
             self.codes = torch.empty(n.value, dtype=torch.uint8, device=device or "cuda")
             self.scales = torch.empty(m.value, dtype=torch.uint8, device=device or "cuda")
-            super().__init__(self.codes.data_ptr(), self.scales.data_ptr(), rows, cols)
+            super().__init__(self.codes.data_ptr(), self.scales.data_ptr(), rows, cols, self.codes.get_device())
 
         @property
         def shape(self):

@@ -2,7 +2,9 @@
  * the product of 4-bit operands, which for a single token run 2 to 5 us on the GPU.
  * Through ctypes such a call costs the host 4.1 us, half of it marshalling; here
  * about 2.7, the rest being the launch. Argument marshalling only, like the ctypes
- * binding beside it: every argument is checked here or by the library. */
+ * binding beside it: every argument is checked here or by the library. Where the
+ * buffers lie is checked here, because only here it is known: the library launches
+ * on the current device and takes addresses at their word. */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
@@ -12,22 +14,28 @@
 typedef struct {
   PyObject_HEAD
   ps_mx mx;
+  int device;                                                  /* of both buffers; -1: not on a GPU */
 } Operand;
 
 static PyTypeObject OperandType;
+/* (of the CUDA runtime that the library is linked to; through torch the lookup takes a quarter of a microsecond) */
+extern int cudaGetDevice(int* device);
+
 static PyObject *g_f32, *g_bf16, *g_fail;                      /* torch dtypes; what raises PsError */
-static PyObject *s_shape, *s_stride, *s_is_cuda, *s_data_ptr, *s_dtype, *s_cuda_stream;
+static PyObject *s_shape, *s_stride, *s_get_device, *s_data_ptr, *s_dtype, *s_cuda_stream;
 
 static int operand_init(PyObject* self, PyObject* args, PyObject* kw) {
-  static char* names[] = {"codes", "scales", "rows", "cols", NULL};
+  static char* names[] = {"codes", "scales", "rows", "cols", "device", NULL};
   unsigned long long codes, scales;
   long long rows, cols;
-  if (!PyArg_ParseTupleAndKeywords(args, kw, "KKLL", names, &codes, &scales, &rows, &cols)) return -1;
+  int device;
+  if (!PyArg_ParseTupleAndKeywords(args, kw, "KKLLi", names, &codes, &scales, &rows, &cols, &device)) return -1;
   ps_mx* m = &((Operand*)self)->mx;
   m->codes = (void*)(size_t)codes;
   m->scales = (void*)(size_t)scales;
   m->rows = rows;
   m->cols = cols;
+  ((Operand*)self)->device = device;
   return 0;
 }
 
@@ -54,7 +62,7 @@ static PyTypeObject OperandType = {
     PyVarObject_HEAD_INIT(NULL, 0).tp_name = "paper_2204_03211_b200._ops.Operand",
     .tp_basicsize = sizeof(Operand),
     .tp_flags = Py_TPFLAGS_DEFAULT | Py_TPFLAGS_BASETYPE,
-    .tp_doc = "A ps_mx: addresses of codes and scales, rows, cols.",
+    .tp_doc = "A ps_mx: addresses of codes and scales, rows, cols; and the device that both lie on (-1: none).",
     .tp_new = PyType_GenericNew,
     .tp_init = operand_init,
     .tp_getset = operand_fields,
@@ -72,23 +80,25 @@ static PyObject* fail(int status, const char* where, const char* detail) {
 
 typedef struct {
   void* ptr;
-  int dtype;
+  int dtype, device;
   long long rows, cols, ld;
 } Matrix;
 
 /* A 2-d CUDA tensor with contiguous rows.  0, or -1 with an exception set. */
 static int matrix(PyObject* t, Matrix* m, const char* where) {
-  PyObject *shape = NULL, *stride = NULL, *cuda = NULL, *ptr = NULL, *dtype = NULL;
+  PyObject *shape = NULL, *stride = NULL, *device = NULL, *ptr = NULL, *dtype = NULL;
   long long s0, s1;
   int ok = -1;
   shape = PyObject_GetAttr(t, s_shape);
   if (!shape) goto out;
   stride = PyObject_CallMethodNoArgs(t, s_stride);
-  cuda = stride ? PyObject_GetAttr(t, s_is_cuda) : NULL;
-  ptr = cuda ? PyObject_CallMethodNoArgs(t, s_data_ptr) : NULL;
+  device = stride ? PyObject_CallMethodNoArgs(t, s_get_device) : NULL;
+  ptr = device ? PyObject_CallMethodNoArgs(t, s_data_ptr) : NULL;
   dtype = ptr ? PyObject_GetAttr(t, s_dtype) : NULL;
   if (!dtype) goto out;
-  if (!PyTuple_Check(shape) || PyTuple_GET_SIZE(shape) != 2 || !PyTuple_Check(stride) || cuda != Py_True) {
+  m->device = (int)PyLong_AsLong(device);                      /* -1 for a tensor that is not on a GPU */
+  if (PyErr_Occurred()) goto out;
+  if (!PyTuple_Check(shape) || PyTuple_GET_SIZE(shape) != 2 || !PyTuple_Check(stride) || m->device < 0) {
     fail(PS_ERR_BAD_ARG, where, "a 2-d CUDA tensor with contiguous rows is wanted");
     goto out;
   }
@@ -115,7 +125,7 @@ static int matrix(PyObject* t, Matrix* m, const char* where) {
 out:
   Py_XDECREF(shape);
   Py_XDECREF(stride);
-  Py_XDECREF(cuda);
+  Py_XDECREF(device);
   Py_XDECREF(ptr);
   Py_XDECREF(dtype);
   return ok;
@@ -163,6 +173,23 @@ static int arguments(const char* where, PyObject* const* args, Py_ssize_t n, PyO
   return 0;
 }
 
+/* 0 if the matrix and the operands (NULL: none) lie on the current device, where the library launches; else -1 with an
+ * exception set. */
+static int placed(const Matrix* m, PyObject* a, PyObject* b, const char* where) {
+  PyObject* const ops[] = {a, b};
+  for (int i = 0; i < 2; ++i)
+    if (ops[i] && ops[i] != Py_None && ((Operand*)ops[i])->device != m->device) {
+      fail(PS_ERR_BAD_ARG, where, "the tensor and the operands are not all on one GPU");
+      return -1;
+    }
+  int current = -1;
+  if (cudaGetDevice(&current) || current != m->device) {
+    fail(PS_ERR_BAD_ARG, where, "the tensor and the operands are not on the current device");
+    return -1;
+  }
+  return 0;
+}
+
 /* NULL for None or a missing argument; sets *bad for what is no operand. */
 static const ps_mx* operand(PyObject* o, int* bad, const char* where) {
   if (!o || o == Py_None) return NULL;
@@ -185,7 +212,7 @@ static PyObject* py_quantize(PyObject* self, PyObject* const* args, Py_ssize_t n
   if (arguments(where, args, n, kwnames, names, 4, 1, a)) return NULL;
   const ps_mx* q = operand(a[1], &bad, where);
   const ps_mx* qt = bad ? NULL : operand(a[2], &bad, where);
-  if (bad || matrix(a[0], &x, where) || stream_of(a[3], &stream)) return NULL;
+  if (bad || matrix(a[0], &x, where) || stream_of(a[3], &stream) || placed(&x, a[1], a[2], where)) return NULL;
   Py_BEGIN_ALLOW_THREADS
   rc = ps_mx_quantize(x.ptr, x.dtype, x.rows, x.cols, x.ld, q, qt, stream);
   Py_END_ALLOW_THREADS
@@ -205,6 +232,7 @@ static PyObject* py_dequantize(PyObject* self, PyObject* const* args, Py_ssize_t
   const ps_mx* q = operand(a[0], &bad, where);
   if (bad || matrix(a[1], &o, where) || stream_of(a[2], &stream)) return NULL;
   if (!q || o.rows != q->rows || o.cols != q->cols) return fail(PS_ERR_BAD_ARG, where, "out and the operand differ in shape");
+  if (placed(&o, a[0], NULL, where)) return NULL;
   Py_BEGIN_ALLOW_THREADS
   rc = ps_mx_dequantize(q, o.dtype, o.ptr, o.ld, stream);
   Py_END_ALLOW_THREADS
@@ -227,6 +255,7 @@ static PyObject* py_matmul(PyObject* self, PyObject* const* args, Py_ssize_t n, 
   if (bad || matrix(v[2], &o, where) || stream_of(v[3], &stream)) return NULL;
   if (!a || !b || o.rows != a->rows || o.cols != b->rows)
     return fail(PS_ERR_BAD_ARG, where, "out is not of the product's shape");
+  if (placed(&o, v[0], v[1], where)) return NULL;
   Py_BEGIN_ALLOW_THREADS
   rc = ps_mx_matmul(a, b, o.dtype, o.ptr, o.ld, stream);
   Py_END_ALLOW_THREADS
@@ -263,8 +292,8 @@ static PyMethodDef methods[] = {
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ops", "Calls on 4-bit operands.", -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__ops(void) {
-  static const char* const texts[] = {"shape", "stride", "is_cuda", "data_ptr", "dtype", "cuda_stream"};
-  PyObject** const slots[] = {&s_shape, &s_stride, &s_is_cuda, &s_data_ptr, &s_dtype, &s_cuda_stream};
+  static const char* const texts[] = {"shape", "stride", "get_device", "data_ptr", "dtype", "cuda_stream"};
+  PyObject** const slots[] = {&s_shape, &s_stride, &s_get_device, &s_data_ptr, &s_dtype, &s_cuda_stream};
   for (int i = 0; i < 6; ++i)
     if (!(*slots[i] = PyUnicode_InternFromString(texts[i]))) return NULL;
   if (PyType_Ready(&OperandType) < 0) return NULL;

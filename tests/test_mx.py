@@ -353,3 +353,86 @@ def test_binding_checks_shapes_and_types_and_takes_keywords():
         assert e.value.status == B.PS_ERR_BAD_ARG
     with pytest.raises(AttributeError):
         B.ps_mx_quantize(x, q, stream="main")
+
+
+PLACES = r"""
+import ctypes, sys
+sys.path.insert(0, sys.argv[1])
+from paper_2204_03211_b200 import binding as B
+B.load()
+from paper_2204_03211_b200 import _ops
+
+
+class Tensor:
+    is_cuda, dtype = True, "f32"
+
+    def __init__(self, rows, cols, device):
+        self.shape, self.device = (rows, cols), device
+        self.is_cuda = device >= 0
+
+    def stride(self):
+        return self.shape[1], 1
+
+    def get_device(self):
+        return self.device
+
+    def data_ptr(self):
+        return 1 << 20
+
+
+def refused(call, *args):
+    try:
+        call(*args)
+    except B.PsError as e:
+        assert e.status == B.PS_ERR_BAD_ARG, e
+        return
+    raise AssertionError("launched")
+
+
+pretend = ctypes.CDLL(sys.argv[2])              # the current device is 0; launches are counted
+_ops.setup("f32", "bf16", B._raise_op)
+made = lambda r, c, d: _ops.Operand(1 << 21, 1 << 22, r, c, d)
+x, far = Tensor(8, 64, 0), Tensor(8, 64, 1)
+q, q_far, host = made(8, 64, 0), made(8, 64, 1), made(8, 64, -1)
+qt, qt_far, out, out_far = made(64, 8, 0), made(64, 8, 1), Tensor(8, 8, 0), Tensor(8, 8, 1)
+refused(_ops.ps_mx_quantize, x, host)
+refused(_ops.ps_mx_quantize, x, q_far)
+refused(_ops.ps_mx_quantize, x, q, qt_far)
+refused(_ops.ps_mx_quantize, x, None, qt_far)
+refused(_ops.ps_mx_quantize, far, q)
+refused(_ops.ps_mx_quantize, far, q_far)        # all on one GPU, but not on the current one
+refused(_ops.ps_mx_quantize, Tensor(8, 64, -1), host)
+refused(_ops.ps_mx_dequantize, host, x)
+refused(_ops.ps_mx_dequantize, q_far, x)
+refused(_ops.ps_mx_dequantize, q, far)
+refused(_ops.ps_mx_dequantize, q_far, far)
+refused(_ops.ps_mx_matmul, q, host, out)
+refused(_ops.ps_mx_matmul, host, q, out)
+refused(_ops.ps_mx_matmul, q, q_far, out)
+refused(_ops.ps_mx_matmul, q, q, out_far)
+refused(_ops.ps_mx_matmul, q_far, q_far, out_far)
+assert pretend.pretend_launches() == 0
+_ops.ps_mx_quantize(x, q, qt)
+_ops.ps_mx_dequantize(q, x)
+assert pretend.pretend_launches() == 2          # these are where they should be
+pretend.cudaSetDevice(1)
+_ops.ps_mx_quantize(far, q_far)
+refused(_ops.ps_mx_quantize, x, q)
+assert pretend.pretend_launches() == 3
+"""
+
+
+def test_buffers_off_the_current_device_are_refused(tmp_path):
+    """No kernel is launched on memory that the current device cannot reach: host buffers, another GPU's.  With made-up
+    addresses, on a runtime that only keeps count."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    B.MxTensor(1, 1, device="cpu")              # (builds and loads what the child uses)
+    pretend = str(tmp_path / "pretend.so")
+    subprocess.run(["gcc", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-o", pretend,
+                    os.path.join(root, "tests", "c", "pretend_cuda.c")], check=True)
+    run = subprocess.run([sys.executable, "-c", PLACES, root, pretend], env=dict(os.environ, LD_PRELOAD=pretend),
+                         capture_output=True, text=True)
+    assert run.returncode == 0, run.stderr
