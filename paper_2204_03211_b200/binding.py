@@ -222,16 +222,53 @@ def _ptr(x) -> int:
     return int(x)
 
 
+# What the library is not told and a check of its device outputs needs: a service's device, a prepared round's jobs.
+_SVC_DEVICE = {}        # handle -> device
+_ROUND_JOBS = {}        # (handle, round) -> jobs in its ready list
+
+
+def _floats_out(x, count: int, device, where: str) -> int:
+    """Address of the `count` floats a kernel writes to x: None, a raw address (the caller's word for it), or a
+    contiguous float32 tensor of at least that many on `device` (None: on any GPU)."""
+    if x is None or type(x) is int:
+        return x or 0
+    if hasattr(x, "get_device"):
+        on = x.get_device()
+        if on < 0 or (on != device and device is not None):
+            raise PsError(PS_ERR_BAD_ARG, where, "a tensor of norms is wanted on %s" % (
+                "a GPU" if device is None else "GPU %d" % device))
+        if _dtype(x, where) != PS_F32 or x.numel() < count or (count > 1 and not x.is_contiguous()):
+            raise PsError(PS_ERR_BAD_ARG, where, "%d contiguous float32 for the norms are wanted" % count)
+        return x.data_ptr()
+    if hasattr(x, "__index__") and not hasattr(x, "ctypes"):       # (a whole number of numpy's; not an array)
+        return int(x)
+    raise PsError(PS_ERR_BAD_ARG, where, "a tensor of norms is wanted on a GPU")
+
+
+def _job_count(tasks) -> int:
+    """Distinct jobs of a ps_task array."""
+    if len(tasks) < 2:
+        return len(tasks)
+    import numpy as np
+    jobs = np.frombuffer(tasks, np.int32)[::2]
+    return 1 if (jobs == jobs[0]).all() else len(np.unique(jobs))
+
+
 # ---- module-level functions with the C names --------------------------------
 
 def ps_create(device: int, num_contexts: int, arena_bytes_per_ctx: int) -> int:
     h = C.c_void_p()
     _check(load().ps_create(C.byref(h), device, num_contexts, arena_bytes_per_ctx), "ps_create")
+    if device >= 0:
+        _SVC_DEVICE[h.value] = device
     return h.value
 
 
 def ps_destroy(svc):
     _check(load().ps_destroy(svc), "ps_destroy")
+    _SVC_DEVICE.pop(svc, None)
+    for key in [k for k in _ROUND_JOBS if k[0] == svc]:
+        del _ROUND_JOBS[key]
 
 
 def ps_register_job(svc, opt=PS_SGD, grad_dtype=PS_F32, num_workers=1, lr=0.1, momentum=0.0, weight_decay=0.0,
@@ -316,6 +353,7 @@ def ps_round_prepare(svc, jobs, blocks, workers, ptrs, ready, flags: int = 0) ->
     out = C.c_int(-1)
     _check(load().ps_round_prepare(svc, n, _ptr(jobs), _ptr(blocks), _ptr(workers), _ptr(ptrs), tasks, len(tasks),
                                    flags, C.byref(out)), "ps_round_prepare", svc)
+    _ROUND_JOBS[svc, out.value] = _job_count(tasks)
     return out.value
 
 
@@ -326,20 +364,24 @@ def ps_round_run(svc, round_id: int, stream=None, out=None):
 
 def ps_round_release(svc, round_id: int):
     _check(load().ps_round_release(svc, round_id), "ps_round_release", svc)
+    _ROUND_JOBS.pop((svc, round_id), None)
 
 
 def ps_aggregate_clipped(svc, ready, max_norm: float, norms_out=None, stream=None):
     """ps_aggregate with every listed job's gradients clipped by their global
-    norm; norms_out: optional float32 device tensor, one entry per job."""
+    norm; norms_out: optional float32 tensor on the service's device, one entry
+    per job (or a device address)."""
+    where = "ps_aggregate_clipped"
     tasks = ready if isinstance(ready, C.Array) else make_tasks(list(ready))
-    _check(load().ps_aggregate_clipped(svc, tasks, len(tasks), max_norm, _ptr(norms_out), _stream_ptr(stream)),
-           "ps_aggregate_clipped", svc)
+    norms = norms_out if norms_out is None else _floats_out(norms_out, _job_count(tasks), _SVC_DEVICE.get(svc), where)
+    _check(load().ps_aggregate_clipped(svc, tasks, len(tasks), max_norm, norms, _stream_ptr(stream)), where, svc)
 
 
 def ps_round_run_clipped(svc, round_id: int, max_norm: float, norms_out=None, stream=None, out=None):
     """ps_round_run with the gradients clipped as by ps_aggregate_clipped."""
-    _check(load().ps_round_run_clipped(svc, round_id, max_norm, _ptr(norms_out), _stream_ptr(stream), _ptr(out)),
-           "ps_round_run_clipped", svc)
+    where = "ps_round_run_clipped"
+    norms = _floats_out(norms_out, _ROUND_JOBS.get((svc, round_id), 1), _SVC_DEVICE.get(svc), where)
+    _check(load().ps_round_run_clipped(svc, round_id, max_norm, norms, _stream_ptr(stream), _ptr(out)), where, svc)
     return out
 
 
@@ -745,6 +787,7 @@ class Clip:
             raise PsError(PS_ERR_BAD_ARG, where, "one dtype per side is wanted")
         if device is None:
             device = self.srcs[0].device.index if self.srcs else 0
+        self.device = device
         n = len(self.srcs)
         src, dst = ((C.c_void_p * n)(*[t.data_ptr() for t in ts]) for ts in (self.srcs, self.dsts))
         h = C.c_void_p()
@@ -754,7 +797,11 @@ class Clip:
         self.handle = h.value
 
     def run(self, max_norm: float, norm_out=None, stream=None):
-        _check_op(load().ps_clip_run(self.handle, max_norm, _ptr(norm_out), _stream_ptr(stream)), "ps_clip_run")
+        """norm_out: optional float32 tensor of one entry on the clip's device (or a device address)."""
+        norm = _floats_out(norm_out, 1, self.device, "ps_clip_run")
+        rc = _lib.ps_clip_run(self.handle, max_norm, norm, _stream_ptr(stream))
+        if rc != PS_OK:
+            _check_op(rc, "ps_clip_run")
 
     def status(self) -> int:
         v = C.c_int()

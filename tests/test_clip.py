@@ -559,3 +559,74 @@ def test_large_launches_keep_or_read_again(opt, dtype, W, shift):
         world.check(limit, norms.cpu().numpy())
     assert world.svc.launch_info()["kernel"] == "clip_inline"
     world.svc.close()
+
+
+class PretendFloats:
+    """What the binding asks a tensor of norms for; its address is never used, because every call has to be refused."""
+
+    def __init__(self, n, device=0, dtype=torch.float32, contiguous=True):
+        self.n, self.device, self.dtype, self.contiguous = n, device, dtype, contiguous
+
+    def get_device(self):
+        return self.device
+
+    def numel(self):
+        return self.n
+
+    def is_contiguous(self):
+        return self.contiguous
+
+    def data_ptr(self):
+        return 1 << 20
+
+
+def wrong_norms(n):
+    return [torch.zeros(n), np.zeros(n, f32), [0.0] * n, PretendFloats(n, device=-1), PretendFloats(n - 1),
+            PretendFloats(n, dtype=torch.float64), PretendFloats(n, dtype=torch.bfloat16)] + [
+                PretendFloats(n, contiguous=False)] * (n > 1)
+
+
+def test_norms_go_to_floats_on_the_gpu_only():
+    """A kernel writes one float per job: host memory, another type and too few entries would be writes out of place."""
+    svc = B.Service(B.PS_DEVICE_NONE, 1, 1 << 20)
+    every = []
+    for j in range(3):
+        assert svc.register_job(num_workers=1) == j
+        for b in range(2):
+            svc.register_block(j, b, 64)
+            svc.push(j, b, 0, 4096)
+            every.append((j, b))
+    B._SVC_DEVICE[svc.handle] = 0                # the tensors' device: nothing here gets as far as a launch
+    rid = svc.round_prepare(None, None, None, None, every)
+    one = svc.round_prepare(None, None, None, None, every[:2])
+    calls = [(3, lambda x: svc.aggregate_clipped(every, 1.0, x)), (3, lambda x: svc.aggregate_clipped(B.make_tasks(every), 1.0, x)),
+             (3, lambda x: svc.round_run_clipped(rid, 1.0, x)), (1, lambda x: svc.aggregate_clipped(every[:2], 1.0, x)),
+             (1, lambda x: svc.round_run_clipped(one, 1.0, x))]
+    for n, call in calls:
+        for x in wrong_norms(n) + [PretendFloats(n, device=1)]:
+            with pytest.raises(B.PsError) as e:
+                call(x)
+            assert e.value.status == B.PS_ERR_BAD_ARG
+        for x in (None, 4096, np.uint64(4096), PretendFloats(n), PretendFloats(n + 5)):
+            with pytest.raises(B.PsError) as e:
+                call(x)
+            assert e.value.status == B.PS_ERR_NO_DEVICE
+    svc.round_release(rid)
+    handle = svc.handle
+    assert [k for k in B._ROUND_JOBS if k[0] == handle] == [(handle, one)]
+    svc.close()
+    assert handle not in B._SVC_DEVICE and not [k for k in B._ROUND_JOBS if k[0] == handle]
+
+
+def test_a_clips_norm_goes_to_a_float_on_its_gpu_only():
+    B.load()
+    clip = B.Clip.__new__(B.Clip)                # no handle: the library refuses what the binding lets through
+    clip.handle, clip.device = None, 0
+    for x in wrong_norms(1) + [PretendFloats(1, device=1)]:
+        with pytest.raises(B.PsError) as e:
+            clip.run(1.0, x)
+        assert e.value.status == B.PS_ERR_BAD_ARG
+    for x in (None, 4096, PretendFloats(3)):
+        with pytest.raises(B.PsError) as e:
+            clip.run(1.0, x)
+        assert e.value.status == B.PS_ERR_BAD_HANDLE
