@@ -772,7 +772,7 @@ def _load_ops():
 class Clip:
     """A list of device tensors whose gradients are clipped together: sources
     and, unless they are clipped in place, destinations (float32 or bfloat16,
-    contiguous, one type per side)."""
+    contiguous, one type per side, all on one GPU)."""
 
     def __init__(self, srcs, dsts=None, device: int | None = None):
         where = "ps_clip_create"
@@ -780,13 +780,15 @@ class Clip:
         if [t.numel() for t in self.srcs] != [t.numel() for t in self.dsts]:
             raise PsError(PS_ERR_BAD_ARG, where, "sources and destinations differ in number or size")
         for t in self.srcs + self.dsts:
-            if not t.is_cuda or not t.is_contiguous():
+            if t.get_device() < 0 or not t.is_contiguous():
                 raise PsError(PS_ERR_BAD_ARG, where, "contiguous CUDA tensors are wanted")
         types = [{_dtype(t, where) for t in ts} for ts in (self.srcs, self.dsts)]
         if any(len(t) > 1 for t in types):
             raise PsError(PS_ERR_BAD_ARG, where, "one dtype per side is wanted")
         if device is None:
-            device = self.srcs[0].device.index if self.srcs else 0
+            device = self.srcs[0].get_device() if self.srcs else 0
+        if any(t.get_device() != device for t in self.srcs + self.dsts):
+            raise PsError(PS_ERR_BAD_ARG, where, "the tensors are not all on GPU %d" % device)
         self.device = device
         n = len(self.srcs)
         src, dst = ((C.c_void_p * n)(*[t.data_ptr() for t in ts]) for ts in (self.srcs, self.dsts))

@@ -630,3 +630,17 @@ def test_a_clips_norm_goes_to_a_float_on_its_gpu_only():
         with pytest.raises(B.PsError) as e:
             clip.run(1.0, x)
         assert e.value.status == B.PS_ERR_BAD_HANDLE
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="made-up addresses: only where there is no GPU")
+def test_a_clips_tensors_lie_on_one_gpu():
+    """One launch reads and writes them all; on a GPU that cannot reach one of them it would fault."""
+    here, far, host = PretendFloats(8), PretendFloats(8, device=1), PretendFloats(8, device=-1)
+    for t in (here, far, host):
+        t.is_cuda = True
+    for srcs, dsts, device in (([here, far], None, None), ([here], [far], None), ([far], [here], None), ([here], None, 1),
+                               ([here], [here], 1), ([here, here], [here, far], 0), ([host], None, None),
+                               ([torch.zeros(8)], None, None), ([here], [host], None)):
+        with pytest.raises(B.PsError) as e:
+            B.Clip(srcs, dsts, device)
+        assert e.value.status == B.PS_ERR_BAD_ARG
