@@ -686,7 +686,8 @@ int ps_mx_status(int* status_out);
  * framework wants the norm.
  *     n = sqrt(sum over all tensors of x*x),  dst = src * min(1, max_norm / (n + 1e-6))
  * No ps_service is involved.  A ps_clip remembers a list of tensors; the list of a
- * training job does not change from step to step.
+ * training job does not change from step to step.  The calls run on the device the
+ * list was made for and leave the calling thread's current device as it was.
  * ------------------------------------------------------------------------- */
 typedef struct ps_clip ps_clip; /* opaque */
 

@@ -459,7 +459,8 @@ int ps_clip_create(ps_clip** out, int device, int n, const void* const* srcs, in
   } catch (...) {
     return PS_ERR_NOMEM;
   }
-  cudaError_t e = cudaSetDevice(device);
+  DeviceScope on(device);
+  cudaError_t e = on.error;
   if (e != cudaSuccess) return op_cuda_error("cudaSetDevice", e);
   OpDevice d;
   int rc = op_device(&d);
@@ -525,7 +526,8 @@ int ps_clip_run(ps_clip* c, float max_norm, float* norm_out, void* stream_) {
   if (!alive(c)) return PS_ERR_BAD_HANDLE;
   if (!(max_norm > 0.0f)) return PS_ERR_BAD_ARG;
   if (reinterpret_cast<uintptr_t>(norm_out) & 3u) return PS_ERR_ALIGN;
-  cudaError_t e = cudaSetDevice(c->device);
+  DeviceScope on(c->device);
+  cudaError_t e = on.error;
   if (e != cudaSuccess) return op_cuda_error("cudaSetDevice", e);
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
   if (c->n == 0) {
@@ -563,7 +565,8 @@ int ps_clip_run(ps_clip* c, float max_norm, float* norm_out, void* stream_) {
 int ps_clip_status(ps_clip* c, int* status_out) {
   if (!alive(c)) return PS_ERR_BAD_HANDLE;
   if (!status_out) return PS_ERR_BAD_ARG;
-  cudaError_t e = cudaSetDevice(c->device);
+  DeviceScope on(c->device);
+  cudaError_t e = on.error;
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
   if (e == cudaSuccess) e = cudaMemcpy(status_out, c->mem + c->status_off, sizeof(int), cudaMemcpyDeviceToHost);
   return e == cudaSuccess ? PS_OK : op_cuda_error("ps_clip_status", e);
@@ -571,7 +574,8 @@ int ps_clip_status(ps_clip* c, int* status_out) {
 
 int ps_clip_destroy(ps_clip* c) {
   if (!alive(c)) return PS_ERR_BAD_HANDLE;
-  cudaError_t e = cudaSetDevice(c->device);
+  DeviceScope on(c->device);
+  cudaError_t e = on.error;
   if (e == cudaSuccess) e = cudaFree(c->mem);        // waits for launches that still use it
   c->magic = 0;
   delete c;

@@ -18,4 +18,26 @@ struct OpDevice {
 };
 int op_device(OpDevice* out);
 
+// Makes `device` current for a scope, and then what the calling thread had before: other calls launch on the current
+// device, and a handle on another one may be destroyed at any time (a garbage collector's).
+class DeviceScope {
+ public:
+  explicit DeviceScope(int device) {
+    int now = -1;
+    error = cudaGetDevice(&now);
+    if (error != cudaSuccess || now == device) return;
+    error = cudaSetDevice(device);
+    if (error == cudaSuccess) before_ = now;
+  }
+  ~DeviceScope() {
+    if (before_ >= 0) cudaSetDevice(before_);
+  }
+  DeviceScope(const DeviceScope&) = delete;
+  DeviceScope& operator=(const DeviceScope&) = delete;
+  cudaError_t error;
+
+ private:
+  int before_ = -1;
+};
+
 }  // namespace psb

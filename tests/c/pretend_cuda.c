@@ -4,9 +4,10 @@
 #include <stdlib.h>
 #include <string.h>
 
-static int current, launches;
+static int current, launches, launch_device = -1;
 
 int pretend_launches(void) { return launches; }
+int pretend_launch_device(void) { return launch_device; }      /* current at the last one */
 
 int cudaGetDevice(int* device) { *device = current; return 0; }
 int cudaSetDevice(int device) {
@@ -29,10 +30,12 @@ int cudaMalloc(void** p, size_t n) { *p = malloc(n ? n : 1); return *p ? 0 : 2; 
 int cudaFree(void* p) { free(p); return 0; }
 int cudaMemset(void* p, int v, size_t n) { memset(p, v, n); return 0; }
 int cudaMemcpy(void* d, const void* s, size_t n, int kind) { (void)kind; memcpy(d, s, n); return 0; }
+int cudaMemsetAsync(void* p, int v, size_t n, void* stream) { (void)p; (void)v; (void)n; (void)stream; return 0; }
 int cudaStreamSynchronize(void* stream) { (void)stream; return 0; }
 int cudaDeviceSynchronize(void) { return 0; }
 int cudaLaunchKernelExC(const void* config, const void* f, void** args) {
   (void)config; (void)f; (void)args;
   ++launches;
+  launch_device = current;
   return 0;
 }

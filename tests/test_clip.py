@@ -644,3 +644,49 @@ def test_a_clips_tensors_lie_on_one_gpu():
         with pytest.raises(B.PsError) as e:
             B.Clip(srcs, dsts, device)
         assert e.value.status == B.PS_ERR_BAD_ARG
+
+
+DEVICES = r"""
+import ctypes as C, sys
+sys.path.insert(0, sys.argv[1])
+from paper_2204_03211_b200 import binding as B
+lib, pretend = B.load(), C.CDLL(sys.argv[2])
+
+
+def current():
+    d = C.c_int(-1)
+    assert pretend.cudaGetDevice(C.byref(d)) == 0
+    return d.value
+
+
+for n in (1000, 10_000_000):                    # a short list, a long one
+    for mine in (0, 1):
+        assert pretend.cudaSetDevice(mine) == 0
+        h, st = C.c_void_p(), C.c_int(-1)
+        ptr, size, before = (C.c_void_p * 1)(1 << 20), (C.c_size_t * 1)(n), pretend.pretend_launches()
+        assert lib.ps_clip_create(C.byref(h), 1, 1, ptr, 0, ptr, 0, size) == 0 and current() == mine
+        assert lib.ps_clip_run(h, 1.0, None, None) == 0 and current() == mine
+        assert pretend.pretend_launches() == before + 1 and pretend.pretend_launch_device() == 1
+        assert lib.ps_clip_status(h, C.byref(st)) == 0 and st.value == 0 and current() == mine
+        assert lib.ps_clip_destroy(h) == 0 and current() == mine
+        assert lib.ps_clip_create(C.byref(h), 2, 1, ptr, 0, ptr, 0, size) == B.PS_ERR_CUDA and current() == mine
+        assert lib.ps_clip_create(C.byref(h), 1, 0, None, 0, None, 0, None) == 0
+        assert lib.ps_clip_run(h, 1.0, 1 << 20, None) == 0 and current() == mine
+        assert lib.ps_clip_destroy(h) == 0
+"""
+
+
+def test_clips_leave_the_current_device_alone(tmp_path):
+    """Other calls launch on the thread's current device: a clip on another one, or its collection, must not change it.
+    On a runtime of two made-up devices that only keeps count."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    B.load()
+    pretend = str(tmp_path / "pretend.so")
+    subprocess.run(["gcc", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-o", pretend,
+                    os.path.join(root, "tests", "c", "pretend_cuda.c")], check=True)
+    run = subprocess.run([sys.executable, "-c", DEVICES, root, pretend], env=dict(os.environ, LD_PRELOAD=pretend),
+                         capture_output=True, text=True)
+    assert run.returncode == 0, run.stderr
