@@ -120,10 +120,11 @@ enum {
                               a half each, on different streams, so that the tail of one overlaps the
                               start of the next.  Only a single round is cut this way; what was packed
                               from several rounds goes out as one launch.  0: one launch.  Same results. */
-  PS_OPT_WAIT_CYCLES = 11, /* bulk-copy kernel: how many SM clock cycles a warp waits for a ring stage
-                              before it gives up, records the failure in the status word
-                              (ps_device_status) and lets the launch end; default 4e9 (about 2 s).
-                              Results of a launch that gave up are undefined. */
+  PS_OPT_WAIT_CYCLES = 11, /* how many SM clock cycles a warp of the bulk-copy kernel waits for a ring
+                              stage, and a CTA of a clipped aggregate for the other CTAs, before it gives
+                              up, records the failure in the status word (ps_device_status) and lets the
+                              launch end; default 4e9 (about 2 s).  Results of a launch that gave up are
+                              undefined; those of later launches on other blocks are not. */
   PS_OPT_WORK_STREAMS = 9, /* with PS_OPT_OVERLAP: launches rotate over this many service-owned streams
                               (1..8, default 4) */
   PS_OPT_PROFILE = 5,      /* 1: aggregates record per-task device time (see ps_block_profile);

@@ -225,7 +225,7 @@ __device__ __forceinline__ bool clip_join(const ClipArgs& a, double sq, float* s
     for (int w = 1; w < kClipThreads / 32; ++w) v += s_red[w];
     __stcg(a.parts + c, v);
   }
-  if (!grid_barrier(a.bar)) {
+  if (!grid_barrier(a.bar, kGridWaitCycles, [] {})) {
     if (tid == 0) atomicExch(a.status, 1);
     return false;
   }

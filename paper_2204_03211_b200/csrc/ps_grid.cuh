@@ -12,9 +12,12 @@ struct GridBarrier {                     // device memory, zero before the first
 constexpr long long kGridWaitCycles = 4000000000ll;     // about two seconds
 
 // Every thread of every CTA calls this.  False (in all threads of the CTA) if the other CTAs did not arrive within
-// the limit; the launch is cooperative, so they are resident and do arrive.  The last CTA to arrive clears the count
-// and advances the generation, so launches of different sizes can use one barrier after the other.
-__device__ __forceinline__ bool grid_barrier(GridBarrier* b) {
+// `limit` cycles; the launch is cooperative, so they are resident and do arrive.  The last CTA to arrive clears the
+// count, calls `last` (one thread) and advances the generation, so launches of different sizes can use one barrier
+// after the other.  It is the one CTA that never waits: what the next launch has to find in order is put in order
+// there, whoever gave up waiting.
+template <typename F>
+__device__ __forceinline__ bool grid_barrier(GridBarrier* b, long long limit, F last) {
   __shared__ int s_ok;
   __syncthreads();
   if (threadIdx.x == 0) {
@@ -23,12 +26,13 @@ __device__ __forceinline__ bool grid_barrier(GridBarrier* b) {
     __threadfence();
     if (atomicAdd(&b->count, 1u) == gridDim.x - 1) {
       b->count = 0;
+      last();
       __threadfence();
       atomicAdd(&b->generation, 1u);
     } else {
       const long long t0 = clock64();
       while (*reinterpret_cast<volatile unsigned int*>(&b->generation) == mine) {
-        if (clock64() - t0 > kGridWaitCycles) { ok = false; break; }
+        if (clock64() - t0 > limit) { ok = false; break; }
       }
     }
     __threadfence();

@@ -43,12 +43,14 @@ struct __align__(16) PsClipHdr {               // 64 bytes at the start of the t
   unsigned int tasks_off, starts_off, ptrs_off, sparse_off;    // byte offsets from the table base
   unsigned int jobs_off;                       // first chunk of every job, and the end: n_jobs + 1 entries
   float max_norm;
-  unsigned int _r[6];
+  long long wait_cycles;                       // limit of the wait for the other CTAs
+  unsigned int _r[4];
 };
+static_assert(sizeof(PsClipHdr) == 64, "header");
 
 struct ClipShared {                            // device memory of the service, zero before the first launch
   GridBarrier bar;
-  unsigned int claim1, claim2;                 // chunks claimed beyond the fixed ones
+  unsigned int claim1, claim2;                 // chunks claimed beyond the fixed ones; cleared at the barrier
 };
 
 // ---- pass 1: sums of one chunk; the scaled sum of element begin + i goes to G[i] --------------------------
@@ -189,7 +191,6 @@ __device__ __forceinline__ void clip_body(const unsigned char* table, const PsJo
   __shared__ const void* s_rowsrc[kThreads / 32][32];
   const unsigned int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
-  if (c == 0 && tid == 0) sh->claim2 = 0;      // (used after the barrier only)
   for (unsigned int round = 0;; ++round) {
     __syncthreads();                           // the previous chunk's s_idx, s_task and s_red have been read
     if (warp == 0) {
@@ -248,11 +249,11 @@ __device__ __forceinline__ void clip_body(const unsigned char* table, const PsJo
     }
   }
 
-  if (!grid_barrier(&sh->bar)) {
+  // (claim1 for the next launch, claim2 for pass 2: by the last CTA to arrive, so also where others gave up waiting)
+  if (!grid_barrier(&sh->bar, hdr->wait_cycles, [sh] { sh->claim1 = sh->claim2 = 0; })) {
     if (tid == 0) atomicExch(status, 1);
     return;
   }
-  if (c == 0 && tid == 0) sh->claim1 = 0;      // for the next launch
   for (unsigned int j = 0; j < n_jobs; ++j) {
     const double v = clip_total<kThreads>(parts + job_first[j], job_first[j + 1] - job_first[j], tid, s_red);
     if (tid == 0) {

@@ -201,7 +201,7 @@ struct ps_service {
   long long opt_batch = 1;
   long long opt_split = 1;                 // large sets of ready blocks go out as a few overlapping launches
   std::vector<int> part;                   // scratch of launch_in_parts
-  long long opt_wait_cycles = 4000000000ll;   // bulk-copy kernel: limit of a wait inside the kernel (about 2 s)
+  long long opt_wait_cycles = 4000000000ll;   // limit of a wait inside the bulk-copy and the clipped kernel (about 2 s)
   bool mig_large_ok = true;                // the 28 KB kernel-parameter form of the migration kernel is accepted
   unsigned long long epoch = 0;            // bumped by whatever can invalidate a prepared round's table:
                                            // migration, import, unregistration, options
@@ -1445,6 +1445,7 @@ int launch_clip(ps_service* s, const std::vector<int>& idx, Plan& plan, const Cl
   if (rc) return rc;
   PsClipHdr* h = reinterpret_cast<PsClipHdr*>(plan.bytes.data());
   h->max_norm = call.max_norm;
+  h->wait_cycles = s->opt_wait_cycles;
   const int grid = (int)std::min<unsigned long long>(plan.total_chunks, (unsigned long long)s->num_sms * s->clip_ctas);
   const bool inl = s->opt_inline && plan.bytes.size() <= kInlineBytes;
   Slot* sl = nullptr;

@@ -690,3 +690,42 @@ def test_clips_leave_the_current_device_alone(tmp_path):
     run = subprocess.run([sys.executable, "-c", DEVICES, root, pretend], env=dict(os.environ, LD_PRELOAD=pretend),
                          capture_output=True, text=True)
     assert run.returncode == 0, run.stderr
+
+
+@pytest.mark.gpu
+def test_a_round_after_one_that_gave_up_waiting():
+    """With a limit of one cycle every CTA but the last gives up at the barrier and returns; the service reports it, and
+    the next round, on blocks that the failed ones did not touch, is like any other: nothing is left over in the counters
+    from which chunks are claimed (14 million elements: more chunks than CTAs)."""
+    import time
+    hp = hparams(B.PS_SGD, B.PS_F32, 2)
+    world = World([hp, hp], [[9_000_001, 4_999_999], [5_000_003, 8_999_997, 5]], seed=11)
+    svc, norms = world.svc, torch.zeros(1, device="cuda")
+    failed, sound = [k for k in world.ready if k[0] == 0], [k for k in world.ready if k[0] == 1]
+    keep = []                                # gradients that are in use until the launch has ended
+    for _ in range(3):
+        world.gradients()
+        for (j, b, w), g in world.dev.items():
+            if j == 0:
+                svc.push(j, b, w, g)
+        keep.append(world.dev)
+        torch.cuda.synchronize()
+        svc.set_option(B.PS_OPT_WAIT_CYCLES, 1)
+        t0 = time.perf_counter()
+        svc.aggregate_clipped(failed, 1.0, norms)
+        assert svc.device_status() != 0 and time.perf_counter() - t0 < 5.0
+    svc.set_option(B.PS_OPT_WAIT_CYCLES, 4_000_000_000)
+    world.ref = {k: world.ref[k] for k in sound}
+    world.jobs = [dict(hp, num_workers=2)] * 2
+    for limit in (0.5, 1e9):
+        world.gradients()
+        world.push()
+        svc.aggregate_clipped(sound, limit, norms)
+        torch.cuda.synchronize()
+        sums = world.sums()
+        true = np.sqrt(sum((v.astype(np.float64) ** 2).sum() for v in sums.values()))
+        assert abs(norms.item() - true) <= 1.01 * 2.0 ** -24 * true
+        for k, r in world.ref.items():
+            r.apply(sums[k], factor(norms.item(), limit))
+            assert np.array_equal(svc.view(svc.pull(*k), len(r.p)).cpu().numpy(), r.p)
+    svc.close()
