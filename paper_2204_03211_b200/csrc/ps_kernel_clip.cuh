@@ -184,7 +184,7 @@ __device__ __forceinline__ void clip_body(const unsigned char* table, const PsJo
   const unsigned int n_tasks = hdr->n_tasks, n_jobs = hdr->n_jobs, total = hdr->total_chunks;
   const unsigned int G = gridDim.x, c = blockIdx.x;          // (never more CTAs than chunks)
 
-  extern __shared__ float cache[];             // kClipSlot sums
+  extern __shared__ __align__(16) float cache[];       // kClipSlot sums, in vectors of four
   __shared__ double s_red[kThreads / 32];
   __shared__ float s_factor[kClipMaxJobs];
   __shared__ unsigned int s_idx, s_task;

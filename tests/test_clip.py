@@ -729,3 +729,20 @@ def test_a_round_after_one_that_gave_up_waiting():
             r.apply(sums[k], factor(norms.item(), limit))
             assert np.array_equal(svc.view(svc.pull(*k), len(r.p)).cpu().numpy(), r.p)
     svc.close()
+
+
+def test_dynamic_shared_memory_says_how_it_is_aligned():
+    """Every such array is accessed with 128-bit loads or copied to in bulk; an array of floats promises 4 bytes only, and
+    where it starts then depends on the static arrays in front of it."""
+    import glob
+    import os
+    import re
+    src = os.path.join(os.path.dirname(os.path.abspath(B.__file__)), "csrc")
+    found = [(os.path.basename(p), re.sub(r"\s+", " ", m)) for p in glob.glob(os.path.join(src, "*.cu*"))
+             for m in re.findall(r"extern __shared__[^;]*;", open(p).read())]
+    assert len(found) >= 5
+    for name, text in found:
+        if "unsigned char smem_raw[]" in text:       # bytes, whose kernel rounds their address up itself
+            continue
+        align = re.search(r"__align__\((\d+)\)", text)
+        assert align and int(align.group(1)) >= 16, (name, text)
