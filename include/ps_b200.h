@@ -686,7 +686,9 @@ int ps_mx_status(int* status_out);
  * worker that clips its own gradient before it pushes it, or whose training
  * framework wants the norm.
  *     n = sqrt(sum over all tensors of x*x),  dst = src * min(1, max_norm / (n + 1e-6))
- * No ps_service is involved.  A ps_clip remembers a list of tensors; the list of a
+ * The squares are exact and added in binary64; n is rounded once, to binary32: the float
+ * nearest to the true norm, unless that lies within 1/100 of a unit in the last place of
+ * the middle between two.  No ps_service is involved.  A ps_clip remembers a list of tensors; the list of a
  * training job does not change from step to step.  The calls run on the device the
  * list was made for and leave the calling thread's current device as it was.
  * ------------------------------------------------------------------------- */
@@ -697,7 +699,8 @@ typedef struct ps_clip ps_clip; /* opaque */
  * gradients into a bf16 push buffer.  dsts[i] == srcs[i] clips in place (same dtype
  * only); otherwise no destination may overlap a source.  Tensors aligned to eight
  * elements on both sides (32 bytes of fp32, 16 of bf16) take wide accesses, others
- * single ones with identical results.  Empty tensors are allowed.
+ * single ones, at two fifths of the speed; the order in which squares are added is the
+ * only difference.  Empty tensors are allowed.
  * Allocates a small table on `device`.  Errors: BAD_ARG, ALIGN, NOMEM, CUDA. */
 int ps_clip_create(ps_clip** out, int device, int n, const void* const* srcs, int src_dtype, void* const* dsts,
                    int dst_dtype, const size_t* nelems);

@@ -15,14 +15,23 @@
 // cluster of sixteen CTAs that keep their elements in registers between the passes: its
 // barrier is the hardware's, and a launch that is not cooperative overlaps its start and
 // the look at the list with the end of the stream's previous one.  Calls in a row take
-// 4.9 us on 1024 elements (host), 3.3 us on 65536, 4.7 on 262144, 7.0 on 524288; a
-// cooperative launch with one unit per CTA in registers took 6.0, 6.4, 7.2 and 8.2 us.
-// Above that sixteen SMs move too little.
+// 3.6 us on 1024 elements and on 65536, 5.0 on 262144, 7.6 on 524288; a cooperative
+// launch with one unit per CTA in registers took 6.0, 6.4, 7.2 and 8.2 us (with sums in
+// binary32, where this took 4.7 and 7.0 on the larger two).  Above that sixteen SMs move
+// too little.
 //
-// Measured: 351 M fp32 elements into bf16 537 us (10 bytes per element, 6.55 TB/s;
-// the norm alone 202 us, 7.0 TB/s), bf16 into bf16 345 us (6.1 TB/s), 8.4 M fp32 into
-// fp32 17 us, mostly out of L2; 170 K elements in 37 tensors 4.1 us a call, which is
-// launch, two dependent trips to L2 and the cluster's barriers.
+// Squares are added in binary64, where each is exact: added eight at a time in binary32,
+// the roundings of equal elements all point the same way, and the norm depended on how
+// its tensors are aligned.  That costs 3 % on the small list below, 7 to 10 % on a
+// quarter and half a million elements, up to 1 % on long lists.
+//
+// Measured, the 335 M elements of a 24-layer model: fp32 into bf16 544 us (10 bytes per
+// element in two passes, 6.2 TB/s), fp32 into fp32 678 us (5.9), bf16 into bf16 353 us
+// (5.7), the norm alone 202 us of fp32 (6.6 TB/s) and 109 of bf16 (6.1); 8.4 M fp32 into
+// fp32 17 us, mostly out of L2 (22.6 us with eight lists in rotation); 170 K elements in
+// 37 tensors 4.26 us a call, which is launch, two dependent trips to L2 and the cluster's
+// barriers.  Tensors that are not aligned to eight elements: 1416 us for the first of
+// these, 1375 for bf16, 11.3 us for 524288 elements.
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -115,26 +124,38 @@ __device__ __forceinline__ void store1(const ClipTensor& t, size_t e, float v) {
   else static_cast<float*>(t.dst)[e] = v;
 }
 
-// Sum of eight squares: in binary32 where neither overflow nor underflow can reach it (at most eight roundings, about
-// 3e-7 of one eighth-of-a-vector's share), else in binary64.  A conversion to binary64 issues at an eighth of the
-// rate of an addition, and one per element was what bounded the pass on bf16 gradients.
-__device__ __forceinline__ double squares8(const float (&v)[8]) {
-  float s = 0.f;
+// |x| in binary64, where its square is exact, without a conversion, which issues at a fraction of the rate of an
+// addition: exponent and mantissa are shifted into place, which is |x| times 2^-896, subnormals and zeros included, and
+// scaled.  Infinities and NaNs become numbers from 2^128 on, which no finite x reaches.
+__device__ __forceinline__ double widened(float x) {
+  const unsigned int u = __float_as_uint(x);
+  return __hiloint2double((int)((u & 0x7fffffffu) >> 3), (int)(u << 29)) * 0x1p896;
+}
+constexpr double kNotFinite = 0x1p256;            // a sum of their squares below it holds neither
+
+// Adds eight squares to four sums: binary64 throughout, the chains of dependent additions short.  Every fourth element
+// takes the conversion after all, which keeps both routes' units busy (bf16, 335 M elements, the norm alone: all by
+// conversion 112 us, none 109.4, every fourth 109.1).
+__device__ __forceinline__ void add_squares(const float (&v)[8], double (&acc)[4]) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) s = __fmaf_rn(v[i], v[i], s);
-  if (s > 1e-20f && s < 1e30f) return (double)s;
-  double d = 0.0;
+  for (int i = 0; i < 8; ++i) {
+    const double d = (i & 3) == 3 ? (double)v[i] : widened(v[i]);
+    acc[i & 3] = fma(d, d, acc[i & 3]);
+  }
+}
+__device__ __forceinline__ double sum4(const double (&a)[4]) { return (a[0] + a[1]) + (a[2] + a[3]); }
+// The same in binary32: what a sum that is not below kNotFinite stands for, infinity or NaN.
+__device__ __forceinline__ void add_squares32(const float (&v)[8], float& sq) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) d = fma((double)v[i], (double)v[i], d);
-  return d;
+  for (int i = 0; i < 8; ++i) sq = __fmaf_rn(v[i], v[i], sq);
 }
 
 // Squares of elements [b, whole) of one type, whole vectors; the loads of U vectors are in flight before the first is
-// used (the test for squares out of range, per vector, would otherwise keep them apart: 4.4 TB/s on bf16).
+// used.
 template <bool BF16, int U>
 __device__ __forceinline__ double squares(const void* src, size_t b, size_t whole) {
   constexpr size_t kStep = kClipThreads * 8;
-  double sq = 0.0;
+  double acc[4] = {0.0, 0.0, 0.0, 0.0};
   size_t i = b + threadIdx.x * 8;
   float v[8];
   for (; i + (U - 1) * kStep < whole; i += U * kStep) {
@@ -144,16 +165,25 @@ __device__ __forceinline__ double squares(const void* src, size_t b, size_t whol
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       r[u].widen(v);
-      sq += squares8(v);
+      add_squares(v, acc);
     }
   }
   for (; i < whole; i += kStep) {
     Raw8<BF16> r;
     r.load(src, i);
     r.widen(v);
-    sq += squares8(v);
+    add_squares(v, acc);
   }
-  return sq;
+  const double sq = sum4(acc);
+  if (sq < kNotFinite) return sq;
+  float s = 0.f;
+  for (i = b + threadIdx.x * 8; i < whole; i += kStep) {
+    Raw8<BF16> r;
+    r.load(src, i);
+    r.widen(v);
+    add_squares32(v, s);
+  }
+  return (double)s;
 }
 
 // The same elements times f, from the last one down.
@@ -266,6 +296,7 @@ ps_clip_short_kernel(const __grid_constant__ ClipArgs a) {
   const unsigned int mine = (tid / kUnitThreads) * kShortCtas + blockIdx.x;      // (the first units go to different CTAs)
   __shared__ double s_red[kShortThreads / 32], s_part;
   __shared__ float s_factor;
+  __shared__ bool s_again;
   __shared__ ClipUnit s_unit[kShortThreads / kUnitThreads][kRounds];
   pdl_launch_dependents();
   if (lane < kRounds && mine + lane * kShortStride < a.units) {                  // (the list does not change)
@@ -300,46 +331,63 @@ ps_clip_short_kernel(const __grid_constant__ ClipArgs a) {
       }
     }
   }
-  double sq = 0.0;
+  double acc[4] = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll
   for (int r = 0; r < kRounds; ++r) {
-    if (mine + r * kShortStride < a.units) sq += squares8(v[r]);
-    sq = fma((double)tail[r], (double)tail[r], sq);
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) sq += __shfl_down_sync(0xffffffffu, sq, o);
-  if ((tid & 31) == 0) s_red[tid >> 5] = sq;
-  __syncthreads();
-  if (tid < 32) {
-    double w = s_red[tid];
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) w += __shfl_down_sync(0xffffffffu, w, o);
-    if (tid == 0) s_part = w;
-  }
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-  if (tid == 0) {
-    double total = 0.0;
-    const unsigned int at = static_cast<unsigned int>(__cvta_generic_to_shared(&s_part));
-#pragma unroll
-    for (int c = 0; c < kShortCtas; ++c) {
-      double w;
-      asm volatile(
-          "{\n\t"
-          ".reg .b32 r;\n\t"
-          "mapa.shared::cluster.u32 r, %1, %2;\n\t"
-          "ld.shared::cluster.f64 %0, [r];\n\t"
-          "}"
-          : "=d"(w)
-          : "r"(at), "r"(c));
-      total += w;
+    if (mine + r * kShortStride < a.units) {
+      add_squares(v[r], acc);
+      const double d = widened(tail[r]);
+      acc[r] = fma(d, d, acc[r]);
     }
-    const float norm = (float)sqrt(total);
-    s_factor = clip_factor(norm, a.max_norm);
-    if (blockIdx.x == 0 && a.norm_out) *a.norm_out = norm;
   }
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");     // (nobody leaves while its part is being read)
-  __syncthreads();
+  double sq = sum4(acc);
+  for (bool again = false;; again = true) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sq += __shfl_down_sync(0xffffffffu, sq, o);
+    if ((tid & 31) == 0) s_red[tid >> 5] = sq;
+    __syncthreads();
+    if (tid < 32) {
+      double w = s_red[tid];
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) w += __shfl_down_sync(0xffffffffu, w, o);
+      if (tid == 0) s_part = w;
+    }
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (tid == 0) {
+      double total = 0.0;
+      const unsigned int at = static_cast<unsigned int>(__cvta_generic_to_shared(&s_part));
+#pragma unroll
+      for (int c = 0; c < kShortCtas; ++c) {
+        double w;
+        asm volatile(
+            "{\n\t"
+            ".reg .b32 r;\n\t"
+            "mapa.shared::cluster.u32 r, %1, %2;\n\t"
+            "ld.shared::cluster.f64 %0, [r];\n\t"
+            "}"
+            : "=d"(w)
+            : "r"(at), "r"(c));
+        total += w;
+      }
+      const float norm = (float)sqrt(total);
+      s_factor = clip_factor(norm, a.max_norm);
+      s_again = !again && !(total < kNotFinite);
+      if (blockIdx.x == 0 && a.norm_out) *a.norm_out = norm;
+    }
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");   // (nobody leaves while its part is being read)
+    __syncthreads();
+    if (!s_again) break;
+    // an infinity or a NaN, in whichever CTA: all of them have the same total and add up once more, to tell which
+    float s = 0.f;
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+      add_squares32(v[r], s);
+      s = __fmaf_rn(tail[r], tail[r], s);
+    }
+    sq = (double)s;
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  }
   const float f = s_factor;
 #pragma unroll
   for (int r = 0; r < kRounds; ++r) {

@@ -746,3 +746,45 @@ def test_dynamic_shared_memory_says_how_it_is_aligned():
             continue
         align = re.search(r"__align__\((\d+)\)", text)
         assert align and int(align.group(1)) >= 16, (name, text)
+
+
+def true_norm(hosts):
+    """The norm in 64 bits: squares of binary32 numbers are exact, math.fsum rounds their sum once."""
+    import math
+    return math.sqrt(math.fsum((np.concatenate([h.float().numpy() for h in hosts]).astype(np.float64) ** 2).tolist()))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("src", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [1, 7, 1000, 524_288, 524_289, 1_000_003])
+@pytest.mark.parametrize("values", ["0.000873832", "-3.3e37", "1.7e-42", "normal", "binades"])
+def test_the_norm_is_the_nearest_float(src, n, values):
+    """On both sides of the limit of short lists, aligned and not, with equal elements too, whose roundings would all
+    point the same way.
+
+    A thread adds at most a few thousand exact squares in binary64, the rest is a tree: a relative error of the sum below
+    2^-53 * 4096 = 2^-41, half of that in the root, which at 2^24 units per binade is less than 2^-17 of a unit in the
+    last place; the root's and the reference's own roundings (2^-52) are smaller still."""
+    g = torch.Generator().manual_seed(n)
+    if values == "normal":
+        h = torch.randn(n, generator=g) * 0.01
+    elif values == "binades":
+        h = torch.randn(n, generator=g) * torch.exp2(torch.randint(-60, 60, (n,), generator=g).float())
+    else:
+        h = torch.full((n,), float(values))
+    h = h.to(DT[src])
+    true, norms = true_norm([h]), []
+    for shift in (0, 1, 3):
+        x = torch.cat([torch.zeros(shift, dtype=DT[src]), h]).cuda()[shift:]
+        out, norm = torch.empty_like(x), torch.zeros(1, device="cuda")
+        clip = B.Clip([x], [out])
+        clip.run(0.05, norm)
+        got = norm.cpu().numpy()[0]
+        norms.append(got)
+        if true < float(np.finfo(f32).max):
+            assert abs(float(got) - true) <= (0.5 + 2.0 ** -10) * float(np.spacing(got)), (got, true)
+        else:
+            assert np.isinf(got)
+        assert torch.equal(out.cpu(), (h.float() * torch.tensor(factor(got, 0.05))).to(DT[src]))
+        clip.close()
+    assert max(norms) - min(norms) <= np.spacing(norms[0]) or np.isinf(norms).all()
