@@ -128,7 +128,8 @@ enum {
   PS_OPT_WORK_STREAMS = 9, /* with PS_OPT_OVERLAP: launches rotate over this many service-owned streams
                               (1..8, default 4) */
   PS_OPT_PROFILE = 5,      /* 1: aggregates record per-task device time (see ps_block_profile);
-                              costs a few atomics per chunk; direct-load kernel only; default 0 */
+                              costs a few atomics per chunk; direct-load kernels and clipped
+                              aggregates (both passes); default 0 */
   PS_OPT_KERNEL = 4        /* kernel variant: 0 = automatic (direct loads), 1 = direct loads,
                               2 = bulk-copy ring (shards staged through shared memory by the TMA
                               unit); results are identical except for the rounding of the
@@ -346,8 +347,7 @@ int ps_round_release(ps_service* svc, int round);
  * ps_block_stats reports the squared norm before clipping.  List a job's blocks in
  * ONE call: each call takes its own norm.
  * One cooperative launch on `stream` itself, also with PS_OPT_OVERLAP (rounds held
- * back by PS_OPT_BATCH go out before it); PS_OPT_KERNEL and PS_OPT_PROFILE do not
- * apply.  The first call allocates a little device memory; a call whose sums exceed
+ * back by PS_OPT_BATCH go out before it); PS_OPT_KERNEL does not apply.  The first call allocates a little device memory; a call whose sums exceed
  * the GPU's shared memory (about 7 million elements) keeps them in a buffer of 4 bytes
  * per listed element, not counting blocks whose W shards take at most 4 bytes per
  * element (2 with Adam), which are read twice.  That buffer belongs to the service; a call that needs

@@ -39,7 +39,8 @@ constexpr unsigned int kClipChunkMin = 8192, kClipChunkMax = 32768;   // element
 constexpr unsigned int kClipRereadSgd = 4, kClipRereadAdam = 2;
 
 struct __align__(16) PsClipHdr {               // 64 bytes at the start of the table
-  unsigned int n_tasks, n_jobs, total_chunks, _r0;
+  unsigned int n_tasks, n_jobs, total_chunks;
+  unsigned int profile;                        // 1: record per-task device time; the chunk sums are followed by two times each
   unsigned int tasks_off, starts_off, ptrs_off, sparse_off;    // byte offsets from the table base
   unsigned int jobs_off;                       // first chunk of every job, and the end: n_jobs + 1 entries
   float max_norm;
@@ -182,6 +183,8 @@ __device__ __forceinline__ void clip_body(const unsigned char* table, const PsJo
   const void* const* ptrs = reinterpret_cast<const void* const*>(table + hdr->ptrs_off);
   const PsSparseDev* sparse = reinterpret_cast<const PsSparseDev*>(table + hdr->sparse_off);
   const unsigned int n_tasks = hdr->n_tasks, n_jobs = hdr->n_jobs, total = hdr->total_chunks;
+  const bool profile = hdr->profile != 0;
+  unsigned long long* times = reinterpret_cast<unsigned long long*>(parts + total);      // pass 1: start and end of every chunk
   const unsigned int G = gridDim.x, c = blockIdx.x;          // (never more CTAs than chunks)
 
   extern __shared__ __align__(16) float cache[];       // kClipSlot sums, in vectors of four
@@ -191,6 +194,12 @@ __device__ __forceinline__ void clip_body(const unsigned char* table, const PsJo
   __shared__ const void* s_rowsrc[kThreads / 32][32];
   const unsigned int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
+  if (profile && tid == 0)                     // pass 2 adds to these
+    for (unsigned int t = c; t < n_tasks; t += G) {
+      PsStat* st = stats + tasks[t].stat_idx;
+      st->busy_ns = st->t_last = 0;
+      st->t_first = ~0ull;
+    }
   for (unsigned int round = 0;; ++round) {
     __syncthreads();                           // the previous chunk's s_idx, s_task and s_red have been read
     if (warp == 0) {
@@ -206,6 +215,7 @@ __device__ __forceinline__ void clip_body(const unsigned char* table, const PsJo
     __syncthreads();
     const unsigned int idx = s_idx;
     if (idx >= total) break;
+    if (profile && tid == 0) times[2 * (size_t)idx] = global_ns();
     const PsTaskDev* T = tasks + s_task;
     const PsJobDev* J = jobs + T->job;
     const size_t begin = (size_t)(idx - T->first_chunk) * T->chunk_elems;
@@ -246,6 +256,7 @@ __device__ __forceinline__ void clip_body(const unsigned char* table, const PsJo
 #pragma unroll
       for (int w = 1; w < kThreads / 32; ++w) v += s_red[w];
       __stcg(parts + idx, v);
+      if (profile) times[2 * (size_t)idx + 1] = global_ns();
     }
   }
 
@@ -279,6 +290,7 @@ __device__ __forceinline__ void clip_body(const unsigned char* table, const PsJo
     __syncthreads();
     const unsigned int idx = s_idx;
     own = idx < G;
+    const unsigned long long t_begin = profile && tid == 0 ? global_ns() : 0ull;
     const PsTaskDev* T = tasks + s_task;
     const PsJobDev* J = jobs + T->job;
     const size_t begin = (size_t)(idx - T->first_chunk) * T->chunk_elems;
@@ -298,6 +310,16 @@ __device__ __forceinline__ void clip_body(const unsigned char* table, const PsJo
       if (J->opt) clip_apply<1, kThreads>(tid, J, T, factor, G_at + done, begin + done, count - done);
       else clip_apply<0, kThreads>(tid, J, T, factor, G_at + done, begin + done, count - done);
     }
+    if (profile) {
+      __syncthreads();
+      if (tid == 0) {
+        PsStat* st = stats + T->stat_idx;
+        const unsigned long long t_end = global_ns(), first = __ldcg(times + 2 * (size_t)idx);
+        atomicAdd(&st->busy_ns, t_end - t_begin + (__ldcg(times + 2 * (size_t)idx + 1) - first));
+        atomicMin(&st->t_first, first);
+        atomicMax(&st->t_last, t_end);
+      }
+    }
   }
 
   // per-block statistics: a task's chunk sums in a fixed order, one CTA per task
@@ -305,11 +327,10 @@ __device__ __forceinline__ void clip_body(const unsigned char* table, const PsJo
     const PsTaskDev* T = tasks + t;
     const double v = clip_total<kThreads>(parts + T->first_chunk, T->nchunks, tid, s_red);
     if (tid == 0) {
-      PsStat st;
-      st.sqnorm = v;
-      st.step = T->step;
-      st.busy_ns = st.t_first = st.t_last = st._r0 = 0;
-      stats[T->stat_idx] = st;
+      PsStat* st = stats + T->stat_idx;
+      st->sqnorm = v;
+      st->step = T->step;
+      if (!profile) st->busy_ns = st->t_first = st->t_last = 0;
     }
   }
 }

@@ -1449,7 +1449,8 @@ int launch_clip(ps_service* s, const std::vector<int>& idx, Plan& plan, const Cl
   const int grid = (int)std::min<unsigned long long>(plan.total_chunks, (unsigned long long)s->num_sms * s->clip_ctas);
   const bool inl = s->opt_inline && plan.bytes.size() <= kInlineBytes;
   Slot* sl = nullptr;
-  rc = acquire_slot(s, inl ? 0 : plan.bytes.size(), plan.total_chunks, &sl);
+  h->profile = s->opt_profile ? 1u : 0u;
+  rc = acquire_slot(s, inl ? 0 : plan.bytes.size(), (size_t)plan.total_chunks * (h->profile ? 3 : 1), &sl);
   if (rc) return rc;
   const int slot_index = (int)(sl - s->slots);
   unsigned int waited = 0;

@@ -788,3 +788,37 @@ def test_the_norm_is_the_nearest_float(src, n, values):
         assert torch.equal(out.cpu(), (h.float() * torch.tensor(factor(got, 0.05))).to(DT[src]))
         clip.close()
     assert max(norms) - min(norms) <= np.spacing(norms[0]) or np.isinf(norms).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("sizes", [[1 << 20, 1 << 18, 4096, 3 << 20], [9_000_000, 1 << 18, 4096, 20_000_000]])
+def test_clipped_rounds_are_profiled(sizes):
+    """The device time that blocks are assigned by is recorded for clipped rounds too (with and without the buffer of kept
+    sums), and only when it is asked for; it changes no result."""
+    world = World([hparams(B.PS_SGD, B.PS_F32, 3)], [sizes], seed=4)
+    svc, norms = world.svc, torch.zeros(1, device="cuda")
+    for it, on in enumerate((0, 1, 1, 0)):
+        svc.set_option(B.PS_OPT_PROFILE, on)
+        world.gradients()
+        world.push()
+        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        torch.cuda.synchronize()
+        e0.record()
+        svc.aggregate_clipped(world.ready, 0.5, norms)
+        e1.record()
+        torch.cuda.synchronize()
+        wall = e0.elapsed_time(e1) * 1e3
+        prof = [svc.block_profile(*k) for k in world.ready]
+        if not on:
+            assert prof == [(0.0, 0.0)] * 4 and svc.job_profile(0) == (0.0, 0.0, 0)
+        else:
+            busy, span = [p[0] for p in prof], [p[1] for p in prof]
+            assert min(busy) > 0 and min(span) > 0
+            assert busy[3] > busy[0] > busy[1] > busy[2]            # ordered like the sizes
+            assert max(span) <= wall * 1.05 + 5.0                  # (the timer's resolution)
+            total, whole, n = svc.job_profile(0)
+            assert n == 4 and abs(total - sum(busy)) < 1e-6
+            assert total <= svc.launch_info()["grid"] * (wall * 1.05 + 5.0)
+            assert max(span) - 1e-6 <= whole <= wall * 1.05 + 5.0
+        world.check(0.5, norms.cpu().numpy())
+    svc.close()
