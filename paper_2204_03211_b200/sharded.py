@@ -94,7 +94,7 @@ class ShardedService:
     def __init__(self, rank: int, world: int, device: int, num_contexts: int = 1, arena_bytes: int = 1 << 30):
         self.rank, self.world, self.device = rank, world, device
         self.svc = B.Service(device, num_contexts, arena_bytes)
-        self.owner = {}
+        self.owner, self.split = {}, set()
 
     def close(self):
         self.svc.close()
@@ -104,6 +104,8 @@ class ShardedService:
 
     def set_owners(self, owner: dict):
         self.owner = dict(owner)
+        first = {}
+        self.split = {j for (j, _), r in self.owner.items() if first.setdefault(j, r) != r}     # jobs with several owners
 
     def owns(self, job: int, block: int) -> bool:
         return self.owner[(job, block)] == self.rank
@@ -130,6 +132,20 @@ class ShardedService:
         mine = self.owned(ready)
         if mine:
             self.svc.aggregate(mine, stream)
+        return len(mine)
+
+    def aggregate_clipped(self, ready, max_norm: float, norms_out=None, stream=None) -> int:
+        """`aggregate` with every job's gradients clipped by their global norm.  The
+        norm is taken over one service's blocks, so a job whose blocks have several
+        owners is refused on every rank: each would clip by the norm of its own
+        blocks.  norms_out: one float per owned job, in order."""
+        for j, _ in ready:
+            if j in self.split:
+                raise B.PsError(B.PS_ERR_BAD_ARG, "ShardedService.aggregate_clipped",
+                                "the blocks of job %d have several owners" % j)
+        mine = self.owned(ready)
+        if mine:
+            self.svc.aggregate_clipped(mine, max_norm, norms_out, stream)
         return len(mine)
 
     def pull(self, job: int, block: int) -> int:

@@ -399,3 +399,25 @@ def test_bench_replica_arm_two_ranks_on_one_device():
     assert abs(line["value"] - 2 * cfg.num_params / (line["ms_per_step"] * 1e-3)) <= 1e-6 * line["value"]
     assert line["gpu_launches"] == 20 * line["timed_region"]["blocks"] and line["cpu_baseline"] is None
     assert line["e2e"]["h2d_bytes_per_step"] == 4 * 4 * cfg.num_params
+
+
+def test_clipping_a_job_with_several_owners_is_refused():
+    """Every rank would clip by the norm of its own blocks; a job that one rank owns is clipped there."""
+    ready = [(j, b) for j in range(2) for b in range(3)]
+    for rank in range(2):
+        sh = sharded.ShardedService(rank, 2, B.PS_DEVICE_NONE, 1, 1 << 20)
+        sh.set_owners({(j, b): 0 if j == 0 else b % 2 for j, b in ready})
+        for j in range(2):
+            assert sh.register_job(num_workers=1) == j
+        for j, b in ready:
+            sh.register_block(j, b, 64)
+            sh.push(j, b, 0, 4096)
+        for tasks in (ready, ready[3:], [(1, 0), (1, 2)]):
+            with pytest.raises(B.PsError) as e:
+                sh.aggregate_clipped(tasks, 1.0)
+            assert e.value.status == B.PS_ERR_BAD_ARG and "job 1" in str(e.value)
+        called = []
+        sh.svc.aggregate_clipped = lambda *a: called.append(a)
+        assert sh.aggregate_clipped(ready[:3], 0.5, None, 7) == (3 if rank == 0 else 0)
+        assert called == ([(ready[:3], 0.5, None, 7)] if rank == 0 else [])
+        sh.close()
