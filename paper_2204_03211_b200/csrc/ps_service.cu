@@ -1761,60 +1761,64 @@ static int round_run(ps_service* s, int round, const ClipCall* clip, void* strea
   const size_t n = r.push_bi.size();
   size_t done = 0;
   int rc = PS_OK;
-  for (; done < n; ++done) {
-    Block& b = s->blocks[r.push_bi[done]];
-    const int w = r.workers[done];
-    if (b.queued) {                        // its previous aggregate is still held in the batch
-      rc = flush_batch(s);
-      if (rc) break;
-    }
-    if (b.pushed[w]) { rc = PS_ERR_DUPLICATE; break; }
-    if (b.nsparse > 0 && (reinterpret_cast<uintptr_t>(r.ptrs[done]) & 15u)) { rc = PS_ERR_ALIGN; break; }
-    b.pushed[w] = r.ptrs[done];
-    b.npushed++;
-  }
-  // the ready list
-  if (!rc)
-    for (int bi : r.idx) {
-      if (s->blocks[bi].queued) {          // listed again without new pushes: not ready once its aggregate is out
+  try {                                    // (a flush and a table allocate; pushes made are taken back whatever fails)
+    for (; done < n; ++done) {
+      Block& b = s->blocks[r.push_bi[done]];
+      const int w = r.workers[done];
+      if (b.queued) {                        // its previous aggregate is still held in the batch
         rc = flush_batch(s);
         if (rc) break;
       }
-      if (s->blocks[bi].npushed != s->jobs[s->blocks[bi].job].d.num_workers) { rc = PS_ERR_NOT_READY; break; }
+      if (b.pushed[w]) { rc = PS_ERR_DUPLICATE; break; }
+      if (b.nsparse > 0 && (reinterpret_cast<uintptr_t>(r.ptrs[done]) & 15u)) { rc = PS_ERR_ALIGN; break; }
+      b.pushed[w] = r.ptrs[done];
+      b.npushed++;
     }
-  if (!rc && !has_device(s)) rc = PS_ERR_NO_DEVICE;
-  if (!rc && !r.idx.empty()) {
-    const bool reuse = r.self_contained && (clip ? r.clip_ok : r.plan_ok);
-    Plan& plan = clip ? r.clip_plan : r.plan;
-    if (reuse) {
-      // same blocks, same places, same pointers as last time: only the step moves on
-      unsigned char* base = plan.bytes.data();
-      PsTaskDev* tasks = reinterpret_cast<PsTaskDev*>(base + (clip ? reinterpret_cast<PsClipHdr*>(base)->tasks_off
-                                                                   : reinterpret_cast<PsTableHdr*>(base)->tasks_off));
-      for (size_t i = 0; i < plan.order.size(); ++i) {
-        const Block& b = s->blocks[plan.order[i]];
-        set_step_fields(s->jobs[b.job], b, &tasks[i]);
+    // the ready list
+    if (!rc)
+      for (int bi : r.idx) {
+        if (s->blocks[bi].queued) {          // listed again without new pushes: not ready once its aggregate is out
+          rc = flush_batch(s);
+          if (rc) break;
+        }
+        if (s->blocks[bi].npushed != s->jobs[s->blocks[bi].job].d.num_workers) { rc = PS_ERR_NOT_READY; break; }
       }
+    if (!rc && !has_device(s)) rc = PS_ERR_NO_DEVICE;
+    if (!rc && !r.idx.empty()) {
+      const bool reuse = r.self_contained && (clip ? r.clip_ok : r.plan_ok);
+      Plan& plan = clip ? r.clip_plan : r.plan;
+      if (reuse) {
+        // same blocks, same places, same pointers as last time: only the step moves on
+        unsigned char* base = plan.bytes.data();
+        PsTaskDev* tasks = reinterpret_cast<PsTaskDev*>(base + (clip ? reinterpret_cast<PsClipHdr*>(base)->tasks_off
+                                                                     : reinterpret_cast<PsTableHdr*>(base)->tasks_off));
+        for (size_t i = 0; i < plan.order.size(); ++i) {
+          const Block& b = s->blocks[plan.order[i]];
+          set_step_fields(s->jobs[b.job], b, &tasks[i]);
+        }
+      }
+      bool built = false;
+      if (clip) {
+        rc = flush_batch(s);                 // earlier rounds first
+        if (!rc) {
+          const cudaError_t e = cudaSetDevice(s->device);
+          if (e != cudaSuccess) { s->cuda_err = cudaGetErrorString(e); rc = PS_ERR_CUDA; }
+        }
+        if (!rc) rc = ensure_clip(s);
+        if (!rc && !reuse) {
+          rc = build_clip_plan(s, r.idx, &plan);
+          built = !rc;
+        }
+        if (!rc) rc = launch_clip(s, r.idx, plan, *clip, static_cast<cudaStream_t>(stream_));
+        if (!reuse) r.clip_ok = !rc && r.self_contained && built;
+      } else {
+        rc = submit_ready(s, r.idx, static_cast<cudaStream_t>(stream_), r.flags, &plan, reuse, &built);
+      }
+      // the round's own table can be reused next time only if it was built for this round just now
+      if (!clip && !reuse) r.plan_ok = !rc && r.self_contained && built;
     }
-    bool built = false;
-    if (clip) {
-      rc = flush_batch(s);                 // earlier rounds first
-      if (!rc) {
-        const cudaError_t e = cudaSetDevice(s->device);
-        if (e != cudaSuccess) { s->cuda_err = cudaGetErrorString(e); rc = PS_ERR_CUDA; }
-      }
-      if (!rc) rc = ensure_clip(s);
-      if (!rc && !reuse) {
-        rc = build_clip_plan(s, r.idx, &plan);
-        built = !rc;
-      }
-      if (!rc) rc = launch_clip(s, r.idx, plan, *clip, static_cast<cudaStream_t>(stream_));
-      if (!reuse) r.clip_ok = !rc && r.self_contained && built;
-    } else {
-      rc = submit_ready(s, r.idx, static_cast<cudaStream_t>(stream_), r.flags, &plan, reuse, &built);
-    }
-    // the round's own table can be reused next time only if it was built for this round just now
-    if (!clip && !reuse) r.plan_ok = !rc && r.self_contained && built;
+  } catch (const std::bad_alloc&) {
+    rc = PS_ERR_NOMEM;
   }
   if (rc) {
     for (size_t i = 0; i < done; ++i) {
@@ -1843,7 +1847,7 @@ int ps_round_run_clipped(ps_service* s, int round, float max_norm, float* norms_
   const ClipCall call = {max_norm, norms_out};
   try {
     return round_run(s, round, &call, stream, params_out);
-  } catch (const std::bad_alloc&) {        // the round could not be resolved: no push has been made
+  } catch (const std::bad_alloc&) {        // the round could not be resolved
     return PS_ERR_NOMEM;
   }
 }

@@ -1,6 +1,6 @@
-/* A stand-in for the calls of the CUDA runtime that the operators without a service make, loaded in front of it
- * (LD_PRELOAD) where there is no GPU: two devices, memory on the host, launches that are only counted.  What the
- * host side does about devices can then be looked at. */
+/* A stand-in for the calls of the CUDA runtime that the library makes, loaded in front of it (LD_PRELOAD) where there is
+ * no GPU: two devices, memory on the host, launches that are only counted and, to whoever asks, have not finished.
+ * What the host side does can then be looked at. */
 #include <stdlib.h>
 #include <string.h>
 
@@ -33,6 +33,20 @@ int cudaMemcpy(void* d, const void* s, size_t n, int kind) { (void)kind; memcpy(
 int cudaMemsetAsync(void* p, int v, size_t n, void* stream) { (void)p; (void)v; (void)n; (void)stream; return 0; }
 int cudaStreamSynchronize(void* stream) { (void)stream; return 0; }
 int cudaDeviceSynchronize(void) { return 0; }
+int cudaStreamCreateWithFlags(void** stream, unsigned flags) { (void)flags; *stream = malloc(1); return 0; }
+int cudaStreamDestroy(void* stream) { free(stream); return 0; }
+int cudaStreamWaitEvent(void* stream, void* event, unsigned flags) { (void)stream; (void)event; (void)flags; return 0; }
+int cudaEventCreateWithFlags(void** event, unsigned flags) { (void)flags; *event = malloc(1); return 0; }
+int cudaEventDestroy(void* event) { free(event); return 0; }
+int cudaEventRecord(void* event, void* stream) { (void)event; (void)stream; return 0; }
+int cudaEventQuery(void* event) { (void)event; return 600; }   /* cudaErrorNotReady */
+int cudaEventSynchronize(void* event) { (void)event; return 0; }
+int cudaHostAlloc(void** p, size_t n, unsigned flags) { (void)flags; return cudaMalloc(p, n); }
+int cudaFreeHost(void* p) { free(p); return 0; }
+int cudaHostGetDevicePointer(void** d, void* h, unsigned flags) { (void)flags; *d = h; return 0; }
+int cudaMemcpyAsync(void* d, const void* s, size_t n, int kind, void* stream) { (void)stream; return cudaMemcpy(d, s, n, kind); }
+int cudaGetLastError(void) { return 0; }
+const char* cudaGetErrorString(int e) { (void)e; return "made up"; }
 int cudaLaunchKernelExC(const void* config, const void* f, void** args) {
   (void)config; (void)f; (void)args;
   ++launches;

@@ -822,3 +822,50 @@ def test_clipped_rounds_are_profiled(sizes):
             assert max(span) - 1e-6 <= whole <= wall * 1.05 + 5.0
         world.check(0.5, norms.cpu().numpy())
     svc.close()
+
+
+NOMEM = r"""
+import ctypes as C, sys
+import numpy as np
+sys.path.insert(0, sys.argv[1])
+from paper_2204_03211_b200 import binding as B
+lib, new = B.load(), C.CDLL(sys.argv[2])
+i32 = lambda *a: np.array(a, np.int32)
+failures = 0
+for k in range(1, 20):
+    svc = B.Service(0, 1, 1 << 20)
+    svc.set_option(B.PS_OPT_OVERLAP, 1)
+    rounds = []
+    for j in range(4):                          # two launches that run on, a round held back behind them, the one in question
+        svc.register_job(num_workers=1)
+        svc.register_block(j, 0, 64)
+        rounds.append(svc.round_prepare(i32(j), i32(0), i32(0), np.array([1 << 20], np.uint64), [(j, 0)], B.PS_ROUND_INPUTS_COMPLETE))
+    for r in rounds[:3]:
+        svc.round_run(r)
+    new.fail_new(k)
+    rc = lib.ps_round_run_clipped(svc.handle, rounds[3], 1.0, None, None, None)
+    new.fail_new(0)
+    assert rc in (B.PS_OK, B.PS_ERR_NOMEM), rc
+    failures += rc != B.PS_OK
+    svc.push(3, 0, 0, 1 << 20)                  # DUPLICATE if a failed call had left its push behind
+    svc.aggregate_clipped([(3, 0)], 1.0)
+    svc.close()
+assert failures >= 4 and rc == B.PS_OK, (failures, rc)      # (a sort does without its buffer; the last ones came after the call)
+"""
+
+
+def test_a_clipped_round_that_runs_out_of_memory_takes_its_pushes_back(tmp_path):
+    """Every allocation of a clipped round fails once, those of the held-back round that goes out before it included."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    B.load()
+    pretend, failing = str(tmp_path / "pretend.so"), str(tmp_path / "failing.so")
+    subprocess.run(["gcc", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-o", pretend,
+                    os.path.join(root, "tests", "c", "pretend_cuda.c")], check=True)
+    subprocess.run(["g++", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-o", failing,
+                    os.path.join(root, "tests", "c", "failing_new.cpp")], check=True)
+    run = subprocess.run([sys.executable, "-c", NOMEM, root, failing],
+                         env=dict(os.environ, LD_PRELOAD=pretend + ":" + failing), capture_output=True, text=True)
+    assert run.returncode == 0, run.stderr
