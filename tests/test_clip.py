@@ -787,7 +787,7 @@ def test_the_norm_is_the_nearest_float(src, n, values):
             assert np.isinf(got)
         assert torch.equal(out.cpu(), (h.float() * torch.tensor(factor(got, 0.05))).to(DT[src]))
         clip.close()
-    assert max(norms) - min(norms) <= np.spacing(norms[0]) or np.isinf(norms).all()
+    assert np.isinf(norms).all() or max(norms) - min(norms) <= np.spacing(norms[0])
 
 
 @pytest.mark.gpu
@@ -869,3 +869,63 @@ def test_a_clipped_round_that_runs_out_of_memory_takes_its_pushes_back(tmp_path)
     run = subprocess.run([sys.executable, "-c", NOMEM, root, failing],
                          env=dict(os.environ, LD_PRELOAD=pretend + ":" + failing), capture_output=True, text=True)
     assert run.returncode == 0, run.stderr
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shift", [0, 1])
+def test_a_tensor_of_more_than_two_to_the_31_elements(shift):
+    """Offsets past 32 bits on both sides: markers on either side of 2^31 and at the end, equal elements elsewhere, whose
+    sum of squares is known."""
+    n, v = (1 << 31) + 4099, 2.0 ** -10
+    x = torch.full((n + shift,), v, device="cuda", dtype=torch.bfloat16)[shift:]
+    at = [0, (1 << 31) - 1, 1 << 31, (1 << 31) + 2049, n - 1]
+    for k, i in enumerate(at):
+        x[i] = 8.0 * (k + 1)
+    out, norm = torch.zeros(n + shift, device="cuda", dtype=torch.bfloat16)[shift:], torch.zeros(1, device="cuda")
+    clip = B.Clip([x], [out])
+    clip.run(1.0, norm)
+    got = norm.cpu().numpy()[0]
+    true = np.sqrt((n - len(at)) * v * v + sum((8.0 * (k + 1)) ** 2 for k in range(len(at))))
+    # binary64 throughout (all squares here are multiples of 2^-20 and their sum is below 2^33: it is even exact)
+    assert abs(float(got) - true) <= (0.5 + 2.0 ** -10) * float(np.spacing(got))
+    c = torch.tensor(factor(got, 1.0))
+    for k, i in enumerate(at):
+        assert out[i].cpu() == (torch.tensor(8.0 * (k + 1)) * c).to(torch.bfloat16)
+        out[i] = (torch.tensor(v) * c).to(torch.bfloat16)
+    assert (out == (torch.tensor(v) * c).to(torch.bfloat16).item()).all()
+    clip.close()
+
+
+@pytest.mark.gpu
+def test_clips_from_several_host_threads():
+    """Handles are independent: one thread, stream and list each, results as on one thread."""
+    import threading
+    lists = [[torch.randn(n, device="cuda") for n in ns] for ns in ([100_000, 5], [700_000], [64] * 40, [3_000_001, 17])]
+    torch.cuda.synchronize()
+    errors = []
+
+    def work(k):
+        try:
+            torch.cuda.set_device(0)
+            stream, norm = torch.cuda.Stream(), torch.zeros(1, device="cuda")
+            outs = [torch.empty_like(t) for t in lists[k]]
+            torch.cuda.synchronize()
+            for it in range(30):
+                clip = B.Clip(lists[k], outs)
+                limit = 0.5 + it
+                clip.run(limit, norm, stream)
+                stream.synchronize()
+                c = torch.tensor(factor(norm.item(), limit))
+                true = true_norm([t.cpu() for t in lists[k]]) if it == 0 else true
+                assert abs(norm.item() - true) <= float(np.spacing(f32(norm.item())))
+                assert all(torch.equal(o.cpu(), t.cpu() * c) for o, t in zip(outs, lists[k]))
+                clip.close()
+        except Exception as e:      # noqa: BLE001
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(len(lists))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors

@@ -436,3 +436,99 @@ def test_buffers_off_the_current_device_are_refused(tmp_path):
     run = subprocess.run([sys.executable, "-c", PLACES, root, pretend], env=dict(os.environ, LD_PRELOAD=pretend),
                          capture_output=True, text=True)
     assert run.returncode == 0, run.stderr
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_row_strides_whose_offsets_pass_31_bits(dtype):
+    """The last rows of every matrix lie beyond 2^31 elements: the same bits as from packed ones."""
+    R, C, ld = 70_000, 96, 32_000
+    wide = torch.empty(R, ld, device="cuda", dtype=dtype)
+    x = wide[:, :C]
+    x.copy_(torch.randn(R, C, device="cuda"))
+    packed = x.contiguous()
+    q, qt, pq, pqt = B.MxTensor(R, C), B.MxTensor(C, R), B.MxTensor(R, C), B.MxTensor(C, R)
+    B.ps_mx_quantize(x, q, qt)
+    B.ps_mx_quantize(packed, pq, pqt)
+    for a, b in ((q, pq), (qt, pqt)):
+        assert torch.equal(a.codes, b.codes) and torch.equal(a.scales, b.scales)
+    B.ps_mx_dequantize(q, x)
+    assert torch.equal(x, B.ps_mx_dequantize(q, torch.empty_like(packed)))
+    for n in (5, 90):                       # few rows: one CTA per tile; more: CTA pairs
+        w = quantized(torch.randn(n, C, device="cuda"))
+        B.ps_mx_matmul(q, w, wide[:, :n])
+        assert torch.equal(wide[:, :n], B.ps_mx_matmul(q, w, torch.empty(R, n, device="cuda", dtype=dtype)))
+    del wide, x
+    long = torch.empty(16, 140_000_000, device="cuda", dtype=dtype)[:, :R]      # few rows far apart: the swapped product
+    w = quantized(torch.randn(16, C, device="cuda"))
+    B.ps_mx_matmul(w, q, long)
+    assert torch.equal(long, B.ps_mx_matmul(w, q, torch.empty(16, R, device="cuda", dtype=dtype)))
+    assert B.ps_mx_status() == 0
+
+
+@pytest.mark.gpu
+def test_operands_of_more_than_two_gigabytes():
+    """Codes of 2.1 GB in either direction, from rows that repeat every 1024: so do codes, values and products."""
+    period, times, C = 1024, 1024, 4128
+    rows = period * times + 5
+    base = torch.randn(period, C, device="cuda").bfloat16()
+    x = torch.empty(rows, C, device="cuda", dtype=torch.bfloat16)
+    x[:period * times].view(times, period, C)[:] = base
+    x[period * times:] = base[:5]
+    q, qt, bq, bqt = B.MxTensor(rows, C), B.MxTensor(C, rows), B.MxTensor(period, C), B.MxTensor(C, period)
+    B.ps_mx_quantize(x, q, qt)
+    B.ps_mx_quantize(base, bq, bqt)
+    assert q.codes.numel() > 1 << 31 and qt.codes.numel() > 1 << 31
+    codes, want = q.codes.view(rows, -1), bq.codes.view(period, -1)
+    assert (codes[:period * times].view(times, period, -1) == want).all() and torch.equal(codes[period * times:], want[:5])
+    t, want_t = qt.codes.view(C, -1), bqt.codes.view(C, -1)
+    for k in range(0, times, 128):
+        part = t[:, k * period // 2:(k + 128) * period // 2].reshape(C, 128, period // 2)
+        assert (part == want_t[:, None]).all()
+    w = quantized(torch.randn(16, C, device="cuda"))
+    y, small = torch.empty(rows, 16, device="cuda"), B.ps_mx_matmul(bq, w, torch.empty(period, 16, device="cuda"))
+    B.ps_mx_matmul(q, w, y)
+    # (the same sums in the same order, whatever the number of tiles, where K is not split: up to rounding otherwise)
+    assert (y[:period * times].view(times, period, 16) == y[:period]).all() and torch.equal(y[period * times:], y[:5])
+    # at most one unit in the last of 24 bits of a partial sum per addition
+    bound = C * 2.0 ** -23 * (values(bq).abs() @ values(w).abs().t())
+    assert ((y[:period] - small).abs() <= 2 * bound).all()
+    x.fill_(7.0)
+    B.ps_mx_dequantize(q, x)
+    assert (x[:period * times].view(times, period, C) == values(bq, torch.bfloat16)).all()
+    assert B.ps_mx_status() == 0
+
+
+@pytest.mark.gpu
+def test_calls_from_several_host_threads():
+    """One thread, stream and set of operands each; every result has the bits of the one-thread call."""
+    import threading
+    sizes = [(1, 1000, 512), (300, 256, 1000), (700, 900, 2048), (2100, 2500, 320)]
+    inputs = [(torch.randn(m, k, device="cuda"), torch.randn(n, k, device="cuda")) for m, n, k in sizes]
+    want = [B.ps_mx_matmul(quantized(a), quantized(b), torch.empty(a.shape[0], b.shape[0], device="cuda")) for a, b in inputs]
+    torch.cuda.synchronize()
+    errors = []
+
+    def work(i):
+        try:
+            torch.cuda.set_device(0)
+            a, b = inputs[i]
+            stream = torch.cuda.Stream()
+            qa, qb = B.MxTensor(*a.shape), B.MxTensor(*b.shape)
+            out = torch.zeros_like(want[i])
+            torch.cuda.synchronize()
+            for _ in range(50):
+                B.ps_mx_quantize(a, qa, stream=stream)
+                B.ps_mx_quantize(b, qb, stream=stream)
+                B.ps_mx_matmul(qa, qb, out, stream)
+                stream.synchronize()
+                assert torch.equal(out, want[i])
+        except Exception as e:      # noqa: BLE001
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(sizes))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors and B.ps_mx_status() == 0, errors
