@@ -347,11 +347,12 @@ int ps_round_release(ps_service* svc, int round);
  * ps_block_stats reports the squared norm before clipping.  List a job's blocks in
  * ONE call: each call takes its own norm.
  * One cooperative launch on `stream` itself, also with PS_OPT_OVERLAP (rounds held
- * back by PS_OPT_BATCH go out before it); PS_OPT_KERNEL does not apply.  The first call allocates a little device memory; a call whose sums exceed
- * the GPU's shared memory (about 7 million elements) keeps them in a buffer of 4 bytes
- * per listed element, not counting blocks whose W shards take at most 4 bytes per
- * element (2 with Adam), which are read twice.  That buffer belongs to the service; a call that needs
- * a larger one than any before waits for the device.
+ * back by PS_OPT_BATCH go out before it); PS_OPT_KERNEL does not apply.  The first call
+ * allocates a little device memory; a call whose sums exceed the GPU's shared memory
+ * (about 7 million elements) keeps them in a buffer of 4 bytes per listed element, not
+ * counting blocks whose W shards take at most 4 bytes per element (2 with Adam), which
+ * are read twice, from wherever they lie.  That buffer belongs to the service; a call
+ * that needs a larger one than any before waits for the device.
  * Errors: those of ps_aggregate; BAD_ARG (max_norm not above 0, norms_dev_out not
  * aligned to 4 bytes), TOO_LARGE (more than 64 jobs, rows of more than 2^30 elements
  * in a row-sparse push). */
@@ -649,7 +650,9 @@ typedef struct {
   long long rows, cols;
 } ps_mx;
 
-/* Bytes of the two buffers of an operand (either out pointer may be NULL).
+/* Bytes of the two buffers of an operand (either out pointer may be NULL).  An operand
+ * has at least one column: a product that sums over nothing, such as the weight gradient
+ * of an empty batch, is the caller's to fill with zeros.
  * Errors: BAD_ARG (rows < 0, cols < 1, either 2^30 or more). */
 int ps_mx_sizes(long long rows, long long cols, size_t* code_bytes_out, size_t* scale_bytes_out);
 

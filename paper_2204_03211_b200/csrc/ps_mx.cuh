@@ -74,7 +74,7 @@ __device__ __forceinline__ unsigned int mul_bf16x2(unsigned int a, unsigned int 
 
 // The products of two pairs of bf16 values, in binary32: a mixed-precision fma unpacks and multiplies at once.  It adds
 // -0, which keeps the sign of a zero.  (A product of pairs, then unpacked, made both directions 22.0 instead of 20.4 us
-// for 8192 x 4096: the kernel is bound by the instructions it issues.)
+// for 8192 x 4096.)
 __device__ __forceinline__ void mx_divide(unsigned int w, unsigned int inv, float* lo, float* hi) {
   asm("{\n\t"
       ".reg .b16 a0, a1, s0, s1;\n\t"
@@ -133,9 +133,12 @@ __device__ __forceinline__ void mx_pdl() {
 // memory reads would meet in the same banks (a stride of 32 rows is a multiple of 32
 // banks whatever the pitch), so the column index is permuted by the row block.
 //
-// Measured on 8192 x 4096 bf16, three matrices in rotation: rows 15.1 us (5.7 TB/s of
-// values and codes), columns 15.3 us, both 20.4 us (5.1 TB/s; bound by issue slots); fp32
-// both 32.3 us (5.3 TB/s).  Five CTAs per SM: with six the column pass spills (21.6 us).
+// Measured on 8192 x 4096 bf16, three matrices in rotation: rows 14.6 us (5.8 TB/s of
+// values and codes), columns 15.3 us, both 20.1 us (5.1 TB/s); fp32 25.4, 26.2 and 32.2 us
+// (5.3 TB/s).  Both at once keep 67 % of the issue slots busy, and the largest stall is
+// the wait for the tile.  Five CTAs per SM: with six the column pass spills (21.6 us).
+// Rows that are not 16-byte aligned go through registers, element by element: 8191 x 4095
+// both ways 35 us from bf16, 65 us from fp32.
 
 constexpr int kQuantThreads = 256;
 
@@ -329,8 +332,10 @@ ps_mx_quantize_kernel(const typename MxIn<BF16>::T* __restrict__ x, int rows, in
 // strip.  A nibble s eem placed as sign, exponent field 0..3 and top mantissa bit of a
 // bf16 is its value times 2^-126, subnormals included: two exact multiplications
 // (2^126, the scale) give the result without conversion instructions, which issue at a
-// fraction of the rate.  8192 x 4096 to bf16: 12.0 us, 7.1 TB/s of codes and values (with
-// eight elements per lane and 128-bit stores 15.3 us).
+// fraction of the rate.  8192 x 4096 to bf16, three matrices in rotation: 14.8 us, 5.7 TB/s
+// of codes and values; one again and again, out of L2 in part, 12.0 us (with eight elements
+// per lane and 128-bit stores 15.3 us).  Rows that allow no wide stores are written element
+// by element: 8191 x 4095 takes 197 us to bf16, 152 us to fp32.
 
 // Nibbles 2j and 2j+1 of w as a pair of bf16 values, unscaled.
 __device__ __forceinline__ unsigned int mx_pair(unsigned int w, int j) {

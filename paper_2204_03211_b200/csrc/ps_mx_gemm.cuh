@@ -21,9 +21,11 @@
 // of a cluster share a tile's K and add their parts in rank order through
 // distributed shared memory: no workspace, no atomics, the same result each time.
 //
-// Measured: 1 x 4096 x 1024 3.3 us, 8 x 4096 x 4096 5.5 us, 37 x 30522 x 1024 5.9 us with
-// the weight in L2 and 10 us cold (16.6 MB), 1000 x 256 x 300 3.8 us.  What is left is
-// latency: launch, the first copy, the MMAs of one tile, its store.
+// Measured, the weight in L2 | weights of 300 MB in rotation, calls in a row: 1 x 4096 x 1024
+// 3.3 | 3.9 us, 8 x 4096 x 4096 5.5 | 6.4, 37 x 30522 x 1024 5.9 | 6.7 (10 us alone with cold
+// caches), 16 x 8192 x 8192 7.4 | 10.3, 1 x 28672 x 8192 21.7 | 23.8 (5.2 TB/s of the weight);
+// 1000 x 256 x 300 3.8 us.  What is left of the shorter ones is latency: launch, the first
+// copy, the MMAs of one tile, its store.
 #pragma once
 
 #include <cuda.h>

@@ -21,7 +21,8 @@
 // 8192^3 178 us (6.2), 8192 x 4096 x 1024 20 us (3.5).  The tensor cores are busy 64 % of
 // the first: of 10000 cycles per tile 8192 are MMA and 1350 the wait for the accumulators
 // to be read; the rest is start, end and, under load, the power cap.  Short K is bound by
-// the stores of the result (3500 cycles per tile).
+// the stores of the result (3500 cycles per tile); so are fp32 results (8192 x 4096 x 4096
+// 61 us, 8192 x 4096 x 1024 31 us).
 #pragma once
 
 #include "ps_mx_gemm.cuh"
