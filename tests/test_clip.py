@@ -929,3 +929,32 @@ def test_clips_from_several_host_threads():
     for t in threads:
         t.join()
     assert not errors, errors
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("src", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [100, 65_537, 524_288, 600_001])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_infinities_and_nans_in_short_and_long_lists(src, n, shift):
+    """One of them at the start, at each place of a vector, in the tail: an infinity gives the factor 0, a NaN, also beside
+    an infinity, NaN throughout."""
+    h = torch.ones(n + shift, dtype=DT[src])
+    x, out, norm = h.cuda()[shift:], torch.empty(n + shift, device="cuda", dtype=DT[src])[shift:], torch.zeros(1, device="cuda")
+    clip = B.Clip([x, x[:0]], [out, out[:0]])
+    inf, nan = float("inf"), float("nan")
+    for at in [0, 1, 2, 3, 4, 7, n // 2, n - 1]:
+        for bad in (inf, -inf, nan):
+            x[at] = bad
+            clip.run(1.0, norm)
+            if np.isnan(bad):
+                assert norm.isnan().all() and out.isnan().all()
+            else:
+                assert norm.isposinf().all() and out[at].isnan() and out.isnan().sum() == 1 and (out == 0).sum() == n - 1
+                x[n - 1 - at] = nan
+                clip.run(1.0, norm)
+                assert norm.isnan().all() and out.isnan().all()
+                x[n - 1 - at] = 1.0
+            x[at] = 1.0
+    clip.run(1e9, norm)                      # and nothing of it is left
+    assert abs(norm.item() - n ** 0.5) <= 0.51 * float(np.spacing(f32(n ** 0.5))) and torch.equal(out, x)
+    clip.close()
