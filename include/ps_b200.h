@@ -722,7 +722,55 @@ int ps_clip_status(ps_clip* clip, int* status_out);
 /* Frees the table; waits for runs that still use it. */
 int ps_clip_destroy(ps_clip* clip);
 
-/* Text of the last CUDA error of a ps_mx_* or ps_clip_* call on this host thread. */
+/* ---------------------------------------------------------------------------
+ * Softmax cross entropy over a vocabulary: the last layer's loss of a worker that trains
+ * a language model, and the gradients of its input and its weight, without the tokens x
+ * vocab scores ever being stored.  (The paper has no counterpart: it leaves the workers'
+ * arithmetic to the training framework.)
+ *     s[t][v] = sum_d x[t][d] * w[v][d]          products exact, summed in binary32
+ *     lse[t] = log(sum_v exp(s[t][v])),  loss[t] = lse[t] - s[t][target[t]]
+ *     e[t][v] = g[t] * (exp(s[t][v] - lse[t]) - [v == target[t]]),  g[t] = scale * token_scale[t]
+ *     dx[t] = sum_v e[t][v] * w[v],  dw[v] = sum_t e[t][v] * x[t]
+ * x and w are bf16.  A token whose target lies outside [0, vocab) (-100, say) is ignored:
+ * its loss, lse and row of dx are zeros, and nothing of its row of x reaches dw, NaN
+ * included.  e is rounded to bf16, the sums over it are binary32.  A score that is a NaN or
+ * +infinity makes its token's loss and gradients NaN.
+ * The calls run on `stream` of the CURRENT device, allocate nothing and wait for nothing.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  const void* x;                 /* device, tokens x dim, row stride ldx elements */
+  long long ldx;
+  const void* w;                 /* device, vocab x dim, row stride ldw elements */
+  long long ldw;
+  const void* targets;           /* device, one whole number of target_bits (32 or 64) per token */
+  int target_bits;
+  long long tokens, vocab, dim;  /* tokens >= 0, vocab and dim >= 1, each below 2^30 */
+  void* workspace;               /* device, 256-byte aligned, the caller's; its contents mean nothing between calls */
+  size_t workspace_bytes;
+} ps_xent;
+
+/* Bytes of workspace that calls of at most `tokens` tokens need: where w's rows start on 16-byte boundaries (w
+ * 16-byte aligned, ldw a multiple of eight), and where they do not (w is then copied first).
+ * Errors: BAD_ARG. */
+int ps_xent_sizes(long long tokens, long long vocab, long long dim, size_t* bytes_out, size_t* bytes_unaligned_out);
+
+/* One float per token into loss and lse (device; either may be NULL).  No tokens: a no-op.
+ * Errors: BAD_ARG, ALIGN, NOMEM (workspace too small), TOO_LARGE (2^30 tiles of 256 x 256), CUDA. */
+int ps_xent_forward(const ps_xent* q, float* loss, float* lse, void* stream);
+
+/* Both gradients, from the lse of a ps_xent_forward of the same x, w and targets: dx (bf16)
+ * and dw (dw_dtype, a ps_dtype), with row strides in elements; either may be NULL.
+ * token_scale (device, one float per token) may be NULL, which stands for ones.  dx and dw
+ * are written, not added to; without tokens dw is zeros.  The order of every sum depends on the
+ * sizes only.  Errors: those of ps_xent_forward. */
+int ps_xent_backward(const ps_xent* q, const float* lse, float scale, const float* token_scale, void* dx, long long lddx,
+                     void* dw, int dw_dtype, long long lddw, void* stream);
+
+/* Waits for the current device and reports the status word of these calls' kernels: 0 = no
+ * fault; non-zero = a bounded wait inside a kernel expired (that call's results are undefined). */
+int ps_xent_status(int* status_out);
+
+/* Text of the last CUDA error of a ps_mx_*, ps_clip_* or ps_xent_* call on this host thread. */
 const char* ps_op_last_error(void);
 
 const char* ps_strerror(int status);

@@ -41,13 +41,29 @@ int op_device(OpDevice* out) {
   return PS_OK;
 }
 
+static EncodeTiled g_encode = nullptr;
+
+static cudaError_t find_encoder() {                  // (under g_op_mu)
+  if (g_encode) return cudaSuccess;
+  void* fn = nullptr;
+  cudaDriverEntryPointQueryResult q;
+  cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q);
+  if (e == cudaSuccess && (q != cudaDriverEntryPointSuccess || !fn)) e = cudaErrorNotSupported;
+  if (e == cudaSuccess) g_encode = reinterpret_cast<EncodeTiled>(fn);
+  return e;
+}
+
+int op_encoder(EncodeTiled* out) {
+  std::lock_guard<std::mutex> lk(g_op_mu);
+  const cudaError_t e = find_encoder();
+  if (e != cudaSuccess) return op_cuda_error("cuTensorMapEncodeTiled", e);
+  *out = g_encode;
+  return PS_OK;
+}
+
 namespace {
 
 static __device__ int g_mx_status;
-
-using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                 const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
 // Per device: the address of the status word, and that the product kernels may use their shared memory.
 struct MxDevice {
@@ -55,7 +71,6 @@ struct MxDevice {
   int* status = nullptr;
 };
 MxDevice g_mx_dev[kOpMaxDevices];
-EncodeTiled g_encode = nullptr;
 
 template <int BN>
 cudaError_t allow_smem() {
@@ -73,13 +88,7 @@ int mx_device(const OpDevice& d, int** status) {
     if (e == cudaSuccess) e = allow_smem<128>();
     if (e == cudaSuccess)
       e = cudaFuncSetAttribute(ps_mx_matmul_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPairSmem);
-    if (e == cudaSuccess && !g_encode) {
-      void* fn = nullptr;
-      cudaDriverEntryPointQueryResult q;
-      e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q);
-      if (e == cudaSuccess && (q != cudaDriverEntryPointSuccess || !fn)) e = cudaErrorNotSupported;
-      if (e == cudaSuccess) g_encode = reinterpret_cast<EncodeTiled>(fn);
-    }
+    if (e == cudaSuccess) e = find_encoder();
     if (e != cudaSuccess) return op_cuda_error("preparing the 4-bit product", e);
     m.status = static_cast<int*>(p);
     m.ready = true;
@@ -101,28 +110,6 @@ int check_operand(const ps_mx* q) {
   return PS_OK;
 }
 
-// A launch that may overlap its prologue with the tail of the stream's previous one (it waits for that launch to
-// complete before it touches memory), optionally in clusters.
-template <typename... KArgs, typename... Args>
-int launch(const char* what, void (*kernel)(KArgs...), unsigned int grid, int block, size_t smem, int cluster,
-           cudaStream_t stream, Args... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3((unsigned)block);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = (unsigned)cluster;
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = cluster > 1 ? 2 : 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
-  return e == cudaSuccess ? PS_OK : op_cuda_error(what, e);
-}
-
 template <bool BF16, bool ROWS, bool COLS>
 int quantize(const void* x, long long rows, long long cols, long long ld, MxOut out, MxOut out_t, cudaStream_t stream) {
   using T = typename MxIn<BF16>::T;
@@ -136,7 +123,7 @@ int quantize(const void* x, long long rows, long long cols, long long ld, MxOut 
                                                cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return op_cuda_error("cudaFuncSetAttribute", e);
   }
-  return launch("quantise", ps_mx_quantize_kernel<BF16, ROWS, COLS>, (unsigned)(nc * nr), kQuantThreads, smem, 1, stream,
+  return op_launch("quantise", ps_mx_quantize_kernel<BF16, ROWS, COLS>, (unsigned)(nc * nr), kQuantThreads, smem, 1, stream,
                 static_cast<const T*>(x), (int)rows, (int)cols, ld, vec_ok, (unsigned)nc, out, out_t);
 }
 
@@ -168,7 +155,7 @@ int matmul_pair(const ps_mx* a, const ps_mx* b, MmArgs args, const OpDevice& d, 
   args.tiles_p = (int)tp;
   args.tiles_q = (int)tq;
   const unsigned int grid = 2u * (unsigned)std::min<long long>(tp * tq, d.num_sms / 2);
-  return launch("4-bit product", ps_mx_matmul_pair_kernel, grid, kPairThreads, kPairSmem, 1, stream, ma, mb, msa, msb, args);
+  return op_launch("4-bit product", ps_mx_matmul_pair_kernel, grid, kPairThreads, kPairSmem, 1, stream, ma, mb, msa, msb, args);
 }
 
 template <int BN>
@@ -188,7 +175,7 @@ int matmul(const ps_mx* p, const ps_mx* q, MmArgs args, const OpDevice& d, cudaS
   const int room = d.num_sms * Cfg::kCtas;
   while (args.splits < 8 && tiles * args.splits * 2 <= room && args.splits * 8 <= args.stages_k) args.splits *= 2;
   const unsigned int grid = args.splits > 1 ? (unsigned)(tiles * args.splits) : (unsigned)std::min(tiles, room);
-  return launch("4-bit product", ps_mx_matmul_kernel<BN>, grid, kMmThreads, Cfg::kSmem, args.splits, stream, mp, mq, args);
+  return op_launch("4-bit product", ps_mx_matmul_kernel<BN>, grid, kMmThreads, Cfg::kSmem, args.splits, stream, mp, mq, args);
 }
 
 }  // namespace
@@ -245,7 +232,7 @@ int ps_mx_dequantize(const ps_mx* q, int dtype, void* out, long long ld, void* s
   const long long row = ld * (long long)esize(dtype);
   const int vec_ok = !misaligned(out, 32) && row % 32 == 0 ? 2 : !misaligned(out, 16) && row % 16 == 0;
   const uint8_t *codes = static_cast<const uint8_t*>(q->codes), *scales = static_cast<const uint8_t*>(q->scales);
-  return launch("dequantise", dtype == PS_BF16 ? ps_mx_dequantize_kernel<true> : ps_mx_dequantize_kernel<false>,
+  return op_launch("dequantise", dtype == PS_BF16 ? ps_mx_dequantize_kernel<true> : ps_mx_dequantize_kernel<false>,
                 (unsigned)(nc * nr), kDequantThreads, 0, 1, static_cast<cudaStream_t>(stream_), codes, scales, q->rows,
                 q->cols, out, ld, vec_ok, (unsigned)nc);
 }

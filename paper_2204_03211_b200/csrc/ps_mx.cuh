@@ -24,6 +24,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "ps_mma.cuh"
+
 namespace psb {
 
 constexpr int kMxTile = 128;                 // rows and columns of a quantiser tile: one atom of scales each way
@@ -114,11 +116,6 @@ __device__ __forceinline__ unsigned int max_abs_bf16x2(unsigned int a, unsigned 
   return r;
 }
 
-__device__ __forceinline__ void mx_pdl() {
-  asm volatile("griddepcontrol.launch_dependents;");
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-}
-
 // ---------------------------------------------------------------- quantisation
 //
 // One CTA per 128 x 128 tile, i.e. one atom of scales in each direction.  The tile
@@ -175,7 +172,7 @@ ps_mx_quantize_kernel(const typename MxIn<BF16>::T* __restrict__ x, int rows, in
     if (ROWS) reinterpret_cast<unsigned int*>(s_row)[tid] = 0u;
     if (COLS) reinterpret_cast<unsigned int*>(s_col)[tid] = 0u;
   }
-  mx_pdl();
+  mm_pdl();
 
   {
     constexpr int kStepRows = kQuantThreads / kPieces;
@@ -352,17 +349,11 @@ __device__ __forceinline__ unsigned int mx_scale_pair(unsigned int sb) {
 
 constexpr int kDequantThreads = 256, kDequantCols = 512, kDequantRows = 32;
 
-__device__ __forceinline__ void store_sector(void* p, const unsigned int* w) {       // 32 bytes, written once
-  asm volatile("st.global.cs.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
-               "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-               : "memory");
-}
-
 template <bool OUT_BF16>
 __global__ void __launch_bounds__(kDequantThreads)
 ps_mx_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, long long rows,
                         long long cols, void* __restrict__ out, long long ld, int vec_ok, unsigned int col_tiles) {
-  mx_pdl();
+  mm_pdl();
   constexpr int kSteps = kDequantRows / (kDequantThreads / 32);
   const long long r0 = (long long)(blockIdx.x / col_tiles) * kDequantRows + (threadIdx.x >> 5);
   const long long c = (long long)(blockIdx.x % col_tiles) * kDequantCols + (threadIdx.x & 31) * 16;

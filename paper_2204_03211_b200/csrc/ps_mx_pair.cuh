@@ -45,65 +45,6 @@ struct PairControl {
 };
 static_assert(sizeof(PairControl) <= 256, "control block");
 
-// The address of this CTA's shared memory word in the pair's leader: the rank is one bit of a shared::cluster address.
-__device__ __forceinline__ unsigned int pair_leader(unsigned int addr) {
-  unsigned int r;
-  asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
-  return r;
-}
-
-// A copy of this CTA whose bytes are counted on `bar`, a barrier of either CTA of the pair.
-__device__ __forceinline__ void pair_tma(unsigned int dst, const CUtensorMap* map, int x, int y, unsigned int bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
-          dst),
-      "l"(map), "r"(x), "r"(y), "r"(bar)
-      : "memory");
-}
-
-// mm_wait on a barrier that the other CTA arrives at.
-__device__ __forceinline__ bool pair_try_wait(unsigned int bar, unsigned int parity) {
-  unsigned int ok;
-  asm volatile(
-      "{\n\t"
-      ".reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t"
-      "}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-__device__ __forceinline__ bool pair_wait(unsigned int bar, unsigned int parity, int* status) {
-  if (pair_try_wait(bar, parity)) return true;
-  const long long t0 = clock64();
-  while (!pair_try_wait(bar, parity)) {
-    if (clock64() - t0 > kMmWaitCycles) {
-      atomicExch(status, 1);
-      return false;
-    }
-  }
-  return true;
-}
-
-// Arrives on a barrier of either CTA.  (Release at CTA scope, the default: what is handed over is tensor memory, whose
-// reads the tcgen05 fence before this orders.  At cluster scope the arrival waits for the warp's stores of the previous
-// tile, over a thousand cycles.)
-__device__ __forceinline__ void pair_arrive(unsigned int bar) {
-  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-
-__device__ __forceinline__ void pair_commit(unsigned int bar) {       // arrives on both CTAs' barrier at this offset
-  asm volatile(
-      "{\n\t"
-      ".reg .b16 m;\n\t"
-      "mov.b16 m, 3;\n\t"
-      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], m;\n\t"
-      "}" ::"r"(bar)
-      : "memory");
-}
-
 __device__ __forceinline__ void pair_copy_scales(unsigned int tmem, unsigned long long desc) {
   asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
 }
@@ -154,7 +95,7 @@ ps_mx_matmul_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid
   mm_cluster_sync();                                      // both CTAs' barriers and tensor memory exist
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const unsigned int tmem = ctl.tmem;
-  mx_pdl();
+  mm_pdl();
 
   const int tiles = args.tiles_p * args.tiles_q, stride = (int)(gridDim.x / 2);
   const int first = (int)(blockIdx.x / 2), nk = args.stages_k;

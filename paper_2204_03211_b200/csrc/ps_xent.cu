@@ -1,0 +1,304 @@
+// Host side of the cross entropy over a vocabulary (declarations and contracts: include/ps_b200.h).
+#include <algorithm>
+#include <cstdint>
+#include <cstring>
+#include <mutex>
+
+#include "ps_op.h"
+#include "ps_xent.cuh"
+
+namespace psb {
+namespace {
+
+static __device__ int g_xent_status;
+
+constexpr int kXeMaxDevices = 64;
+constexpr long long kXeMaxDim = 1ll << 30;       // (TMA coordinates are 32-bit)
+
+struct XeDevice {
+  bool ready = false;
+  int* status = nullptr;
+};
+std::mutex g_xent_mu;
+XeDevice g_xent_dev[kXeMaxDevices];
+
+int xent_device(const OpDevice& d, int** status) {
+  std::lock_guard<std::mutex> lk(g_xent_mu);
+  XeDevice& x = g_xent_dev[d.id];
+  if (!x.ready) {
+    void* p = nullptr;
+    cudaError_t e = cudaGetSymbolAddress(&p, g_xent_status);
+    if (e == cudaSuccess)
+      e = cudaFuncSetAttribute(ps_tc_kernel<XeOp>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcCfg<XeOp::kPlanes>::kSmem);
+    if (e != cudaSuccess) return op_cuda_error("preparing the cross entropy", e);
+    x.status = static_cast<int*>(p);
+    x.ready = true;
+  }
+  *status = x.status;
+  return PS_OK;
+}
+
+bool misaligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
+long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+
+// How the gradients' pass is cut, and where everything lies in the workspace.  It depends on the sizes alone, so that
+// ps_xent_sizes and the calls agree whatever device they run on.
+struct XePlan {
+  long long nparts, pitch, piece, pieces;
+  int slices;                            // per piece
+  size_t parts, score, xm, d[2], sums, w, end, end_unaligned;
+};
+
+// A piece of d: as many words as make 2^24 entries (32 MB), whole tiles, at least one.
+constexpr long long kXePieceEntries = 1ll << 24;
+constexpr int kXePairs = 74;             // CTA pairs that the cuts are made for
+constexpr int kXeMaxSlices = 64, kXeMinStages = 4;
+constexpr long long kXeSliceRows = 1ll << 14;    // slices x tokens, where there is more than one slice
+
+XePlan xent_plan(long long T, long long V, long long D) {
+  XePlan p;
+  p.nparts = ceil_div(V, 128);
+  p.pitch = ceil_div(D, 8) * 8;
+  const long long all = ceil_div(V, kTcTile) * kTcTile;
+  p.piece = std::min(all, std::max<long long>(1, kXePieceEntries / std::max(1ll, T) / kTcTile) * kTcTile);
+  p.pieces = ceil_div(V, p.piece);
+  // dx has few tiles, each as long as the piece has words: its words are shared out to slices until one is no longer
+  // than half of what a pair computes in a launch
+  const long long tm = ceil_div(T, kTcTile), td = ceil_div(D, kTcTile), tv = p.piece / kTcTile, nk = p.piece / kTcK;
+  const long long total = tm * tv * ceil_div(D, kTcK) + tm * td * nk + tv * td * ceil_div(T, kTcK);
+  const long long longest = std::max<long long>(kXeMinStages, total / kXePairs / 2);
+  const long long most = std::min<long long>(kXeMaxSlices, std::max(1ll, kXeSliceRows / std::max(1ll, T)));
+  p.slices = (int)std::min(most, std::max(1ll, ceil_div(nk, longest)));
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += round256(bytes);
+    return here;
+  };
+  p.xm = take((size_t)T * (size_t)p.pitch * 2);
+  const size_t shared = at;              // the losses' pass is done with its part before the gradients' pass begins
+  p.parts = take((size_t)T * (size_t)p.nparts * sizeof(float2));
+  p.score = take((size_t)T * sizeof(float));
+  const size_t forward = at;
+  at = shared;
+  for (int b = 0; b < 2; ++b) p.d[b] = take(b < p.pieces ? (size_t)T * (size_t)p.piece * 2 : 0);
+  p.sums = take(p.slices > 1 || p.pieces > 1 ? (size_t)p.slices * (size_t)T * (size_t)D * sizeof(float) : 0);
+  at = std::max(at, forward);
+  p.end = at;
+  p.w = take((size_t)V * (size_t)p.pitch * 2);
+  p.end_unaligned = at;
+  return p;
+}
+
+// What any call of at most T tokens needs (a smaller batch is cut into larger pieces and more slices).
+size_t xent_bytes(long long T, long long V, long long D, bool unaligned) {
+  const size_t pitch = (size_t)ceil_div(D, 8) * 8, all = (size_t)ceil_div(V, kTcTile) * kTcTile, t = (size_t)T;
+  const size_t x = round256(t * pitch * 2), w = unaligned ? round256((size_t)V * pitch * 2) : 0;
+  const size_t parts = round256(t * (size_t)ceil_div(V, 128) * sizeof(float2)) + round256(t * sizeof(float));
+  const size_t piece = std::max(std::min(t * all, (size_t)kXePieceEntries), t * kTcTile);
+  const size_t rows = std::max(t, std::min(t * kXeMaxSlices, (size_t)kXeSliceRows));
+  return std::max<size_t>(256, x + w + std::max(parts, 2 * round256(piece * 2) + round256(rows * (size_t)D * sizeof(float))));
+}
+
+bool make_map(EncodeTiled encode, CUtensorMap* m, const void* p, long long rows, long long cols, long long ld) {
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
+  const cuuint32_t box[2] = {64, 64}, step[2] = {1, 1};
+  return encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(p), dims, strides, box, step,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct XeCall {
+  const ps_xent* q;
+  XePlan plan;
+  OpDevice dev;
+  cudaStream_t stream;
+  char* ws;
+  bool copy_w;
+  XeArgs args;
+};
+
+bool rows_aligned(const void* p, long long ld) { return !misaligned(p, 16) && ld % 8 == 0; }
+
+int check(const ps_xent* q, XePlan* plan, bool* copy_w) {
+  if (!q || q->tokens < 0 || q->vocab < 1 || q->dim < 1 || q->tokens >= kXeMaxDim || q->vocab >= kXeMaxDim ||
+      q->dim >= kXeMaxDim || q->ldx < q->dim || q->ldw < q->dim || (q->target_bits != 32 && q->target_bits != 64))
+    return PS_ERR_BAD_ARG;
+  if (!q->w || !q->workspace || (q->tokens > 0 && (!q->x || !q->targets))) return PS_ERR_BAD_ARG;
+  if (misaligned(q->x, 2) || misaligned(q->w, 2) || misaligned(q->targets, q->target_bits / 8) || misaligned(q->workspace, 256))
+    return PS_ERR_ALIGN;
+  if (ceil_div(q->tokens, kTcTile) * ceil_div(q->vocab, kTcTile) > 0x3fffffffll ||
+      ceil_div(q->vocab, kTcTile) * ceil_div(q->dim, kTcTile) > 0x3fffffffll)
+    return PS_ERR_TOO_LARGE;
+  *plan = xent_plan(q->tokens, q->vocab, q->dim);
+  *copy_w = !rows_aligned(q->w, q->ldw);
+  if (q->workspace_bytes < (*copy_w ? plan->end_unaligned : plan->end)) return PS_ERR_NOMEM;
+  return PS_OK;
+}
+
+int copy_rows(const XeCall& c, const void* src, long long rows, long long ld, size_t to, bool mask) {
+  const long long units = rows * (c.plan.pitch / 8);
+  const unsigned grid = (unsigned)std::min<long long>(ceil_div(units, kXeCopyThreads), (long long)c.dev.num_sms * 16);
+  return op_launch("cross entropy", ps_xent_copy_kernel, grid, kXeCopyThreads, 0, 1, c.stream,
+                   static_cast<const unsigned short*>(src), rows, c.q->dim, ld, reinterpret_cast<unsigned short*>(c.ws + to),
+                   c.plan.pitch, mask ? c.q->targets : nullptr, c.q->target_bits == 64 ? 1 : 0, c.q->vocab,
+                   rows_aligned(src, ld) ? 1 : 0);
+}
+
+// What both passes set up.  use_copy: x is read from its masked copy.
+int begin(XeCall* c, const ps_xent* q, void* stream, bool backward) {
+  c->q = q;
+  c->stream = static_cast<cudaStream_t>(stream);
+  c->ws = static_cast<char*>(q->workspace);
+  int rc = op_device(&c->dev);
+  if (rc) return rc;
+  std::memset(&c->args, 0, sizeof c->args);
+  XeArgs& a = c->args;
+  rc = xent_device(c->dev, &a.status);
+  if (rc) return rc;
+  EncodeTiled encode;
+  rc = op_encoder(&encode);
+  if (rc) return rc;
+  a.T = q->tokens;
+  a.V = q->vocab;
+  a.D = q->dim;
+  a.targets = q->targets;
+  a.target64 = q->target_bits == 64;
+  const bool copy_x = backward || !rows_aligned(q->x, q->ldx);
+  const void* x = copy_x ? c->ws + c->plan.xm : q->x;
+  const void* w = c->copy_w ? c->ws + c->plan.w : q->w;
+  if (!make_map(encode, &a.x, x, a.T, a.D, copy_x ? c->plan.pitch : q->ldx) ||
+      !make_map(encode, &a.w, w, a.V, a.D, c->copy_w ? c->plan.pitch : q->ldw))
+    return op_cuda_error("tensor map", cudaErrorInvalidValue);
+  if (backward)
+    for (int b = 0; b < 2 && b < c->plan.pieces; ++b)
+      if (!make_map(encode, &a.d[b], c->ws + c->plan.d[b], a.T, c->plan.piece, c->plan.piece))
+        return op_cuda_error("tensor map", cudaErrorInvalidValue);
+  a.xm = a.x;
+  if (copy_x) rc = copy_rows(*c, q->x, q->tokens, q->ldx, c->plan.xm, backward);
+  if (!rc && c->copy_w) rc = copy_rows(*c, q->w, q->vocab, q->ldw, c->plan.w, false);
+  return rc;
+}
+
+// Launches the segments of c->args, the longest tiles first.
+int launch_segments(XeCall* c) {
+  XeArgs& a = c->args;
+  std::stable_sort(a.seg, a.seg + a.nseg, [](const XeSeg& p, const XeSeg& q) { return p.nk / p.slices > q.nk / q.slices; });
+  long long tiles = 0;
+  for (int i = 0; i < a.nseg; ++i) {
+    a.seg[i].first = (int)tiles;
+    tiles += (long long)a.seg[i].tiles_m * a.seg[i].tiles_n * a.seg[i].slices;
+  }
+  if (tiles > 0x3fffffffll) return PS_ERR_TOO_LARGE;
+  a.tiles = (int)tiles;
+  const unsigned grid = 2u * (unsigned)std::min<long long>(tiles, c->dev.num_sms / 2);
+  return op_launch("cross entropy", ps_tc_kernel<XeOp>, grid, kTcThreads, TcCfg<XeOp::kPlanes>::kSmem, 1, c->stream, a);
+}
+
+}  // namespace
+}  // namespace psb
+
+using namespace psb;
+
+extern "C" {
+
+int ps_xent_sizes(long long tokens, long long vocab, long long dim, size_t* bytes_out, size_t* bytes_unaligned_out) {
+  if (tokens < 0 || vocab < 1 || dim < 1 || tokens >= kXeMaxDim || vocab >= kXeMaxDim || dim >= kXeMaxDim) return PS_ERR_BAD_ARG;
+  if (bytes_out) *bytes_out = xent_bytes(tokens, vocab, dim, false);
+  if (bytes_unaligned_out) *bytes_unaligned_out = xent_bytes(tokens, vocab, dim, true);
+  return PS_OK;
+}
+
+int ps_xent_forward(const ps_xent* q, float* loss, float* lse, void* stream) {
+  XeCall c;
+  int rc = check(q, &c.plan, &c.copy_w);
+  if (rc) return rc;
+  if (q->tokens == 0) return PS_OK;
+  if (!loss && !lse) return PS_ERR_BAD_ARG;
+  if (misaligned(loss, 4) || misaligned(lse, 4)) return PS_ERR_ALIGN;
+  rc = begin(&c, q, stream, false);
+  if (rc) return rc;
+  XeArgs& a = c.args;
+  a.parts = reinterpret_cast<float2*>(c.ws + c.plan.parts);
+  a.nparts = (int)c.plan.nparts;
+  a.score = reinterpret_cast<float*>(c.ws + c.plan.score);
+  a.nseg = 1;
+  a.seg[0] = XeSeg{kXeStats, 0, (int)ceil_div(a.T, kTcTile), (int)ceil_div(a.V, kTcTile), 0, (int)ceil_div(a.D, kTcK), 1, 0, 0, 0};
+  rc = launch_segments(&c);
+  if (rc) return rc;
+  return op_launch("cross entropy", ps_xent_join_kernel, (unsigned)ceil_div(a.T, kXeJoinThreads / 32), kXeJoinThreads, 0, 1,
+                   c.stream, (const float2*)a.parts, a.nparts, (const float*)a.score, a.targets, a.target64, a.T, a.V, loss, lse);
+}
+
+int ps_xent_backward(const ps_xent* q, const float* lse, float scale, const float* token_scale, void* dx, long long lddx,
+                     void* dw, int dw_dtype, long long lddw, void* stream) {
+  XeCall c;
+  int rc = check(q, &c.plan, &c.copy_w);
+  if (rc) return rc;
+  if ((!dx && !dw) || (dw_dtype != PS_F32 && dw_dtype != PS_BF16) || (dx && lddx < q->dim) || (dw && lddw < q->dim))
+    return PS_ERR_BAD_ARG;
+  if (q->tokens > 0 && !lse) return PS_ERR_BAD_ARG;
+  const size_t es = dw_dtype == PS_F32 ? 4 : 2;
+  if (misaligned(lse, 4) || misaligned(token_scale, 4) || misaligned(dx, 2) || misaligned(dw, es)) return PS_ERR_ALIGN;
+  if (q->tokens == 0) {                  // a sum over nothing
+    if (!dw) return PS_OK;
+    const cudaError_t e = cudaMemset2DAsync(dw, (size_t)lddw * es, 0, (size_t)q->dim * es, (size_t)q->vocab,
+                                            static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? PS_OK : op_cuda_error("ps_xent_backward", e);
+  }
+  rc = begin(&c, q, stream, true);
+  if (rc) return rc;
+  XeArgs& a = c.args;
+  const XePlan& p = c.plan;
+  a.lse = lse;
+  a.weights = token_scale;
+  a.scale = scale;
+  for (int b = 0; b < 2; ++b) a.d_out[b] = reinterpret_cast<__nv_bfloat16*>(c.ws + p.d[b]);
+  a.piece = (int)p.piece;
+  a.dx_sums = reinterpret_cast<float*>(c.ws + p.sums);
+  a.dx = static_cast<__nv_bfloat16*>(dx);
+  a.dw = dw;
+  a.ld_dx = lddx;
+  a.ld_dw = lddw;
+  a.dw_f32 = dw_dtype == PS_F32;
+  a.dx_wide = !misaligned(dx, 32) && lddx * 2 % 32 == 0;
+  a.dw_wide = !misaligned(dw, 32) && lddw * (long long)es % 32 == 0;
+  const int tm = (int)ceil_div(a.T, kTcTile), td = (int)ceil_div(a.D, kTcTile);
+  int filled = 0;                        // slices of dx's sums that hold something
+  for (long long k = 0; k <= p.pieces; ++k) {
+    a.nseg = 0;
+    if (k < p.pieces) {
+      const long long v0 = k * p.piece, words = std::min(p.piece, a.V - v0);
+      a.seg[a.nseg++] = XeSeg{kXeProb, 0, tm, (int)ceil_div(words, kTcTile), (int)v0, (int)ceil_div(a.D, kTcK), 1, (int)(k & 1), 0, 0};
+    }
+    if (k > 0) {
+      const long long v0 = (k - 1) * p.piece, words = std::min(p.piece, a.V - v0);
+      const int nk = (int)ceil_div(words, kTcK), buf = (int)((k - 1) & 1);
+      if (dx) {
+        const int slices = std::min(p.slices, nk);       // (the last piece may be short; earlier ones filled all)
+        a.seg[a.nseg++] = XeSeg{kXeDx, 0, tm, td, (int)v0, nk, slices, buf, k == 1, k == p.pieces && p.slices == 1};
+        filled = std::max(filled, slices);
+      }
+      if (dw) a.seg[a.nseg++] = XeSeg{kXeDw, 0, (int)ceil_div(words, kTcTile), td, (int)v0, (int)ceil_div(a.T, kTcK), 1, buf, 0, 0};
+    }
+    rc = launch_segments(&c);
+    if (rc) return rc;
+  }
+  if (dx && p.slices > 1) {
+    const unsigned grid = (unsigned)std::min<long long>(ceil_div(a.T * a.D, kXeCopyThreads), (long long)c.dev.num_sms * 8);
+    rc = op_launch("cross entropy", ps_xent_slices_kernel, grid, kXeCopyThreads, 0, 1, c.stream, (const float*)a.dx_sums, filled,
+                   a.T, a.D, a.dx, a.ld_dx);
+  }
+  return rc;
+}
+
+int ps_xent_status(int* status_out) {
+  if (!status_out) return PS_ERR_BAD_ARG;
+  cudaError_t e = cudaDeviceSynchronize();
+  if (e == cudaSuccess) e = cudaMemcpyFromSymbol(status_out, g_xent_status, sizeof(int));
+  return e == cudaSuccess ? PS_OK : op_cuda_error("ps_xent_status", e);
+}
+
+}  // extern "C"
