@@ -723,6 +723,46 @@ int ps_clip_status(ps_clip* clip, int* status_out);
 int ps_clip_destroy(ps_clip* clip);
 
 /* ---------------------------------------------------------------------------
+ * Orthogonalised matrices: the direction of Muon's update, for a trainer that applies its own
+ * optimizer (jobs of the service have PS_MUON).  For each m x n matrix G of a list
+ *     X = G / (|G| + 1e-7)                        Frobenius norm, added in binary64
+ *     five times:  A = X X^T,  X = a X + (b A + c A A) X
+ *     (a, b, c) = (3.4445, -4.7750, 2.0315)
+ * which takes the singular values of G to about 1 (0.7 to 1.2) and leaves its singular vectors;
+ * with m > n the same of the transpose.  Sums are binary32.  bf16 results come from operands of
+ * 11 bits (X itself is kept to 22), fp32 results from operands of 22 bits, three products
+ * for one, at the precision of binary32 arithmetic.  A matrix with a NaN or an infinity gives NaNs;
+ * a matrix of zeros gives zeros.
+ * No ps_service is involved.  A ps_ortho remembers a list of matrices, which does not change from
+ * step to step, and holds a workspace of 8 bytes per element (and 4 or 8 for the square of each
+ * matrix's smaller side).  The calls run on the device the list was made for and leave the calling
+ * thread's current device as it was.
+ * ------------------------------------------------------------------------- */
+typedef struct ps_ortho ps_ortho; /* opaque */
+
+typedef struct {
+  void* data;                    /* device; sources are only read */
+  long long rows, cols, ld;      /* row stride in elements, >= cols */
+} ps_matrix;
+
+/* Remembers n matrices (host arrays, copied): source i of src_dtype gives destination i of
+ * dst_dtype.  Destinations must not overlap each other; a destination may be its own or another
+ * source, all sources are read before any result is written.  Empty matrices are allowed.  Waits until the
+ * tables are on the device.  Errors: BAD_ARG (shapes differ, ld < cols, NULL), ALIGN, TOO_LARGE, NOMEM, CUDA. */
+int ps_ortho_create(ps_ortho** out, int device, int n, const ps_matrix* srcs, int src_dtype, const ps_matrix* dsts,
+                    int dst_dtype);
+
+/* Three launches on `stream`, the last one cooperative.  Runs of one ps_ortho must not overlap on
+ * the GPU: use one stream, or order the streams.  Errors: BAD_HANDLE, CUDA. */
+int ps_ortho_run(ps_ortho* o, void* stream);
+
+/* Waits for the device; non-zero: a bounded wait inside a run expired. */
+int ps_ortho_status(ps_ortho* o, int* status_out);
+
+/* Frees the tables and the workspace; waits for runs that still use them. */
+int ps_ortho_destroy(ps_ortho* o);
+
+/* ---------------------------------------------------------------------------
  * Softmax cross entropy over a vocabulary: the last layer's loss of a worker that trains
  * a language model, and the gradients of its input and its weight, without the tokens x
  * vocab scores ever being stored.  (The paper has no counterpart: it leaves the workers'
@@ -770,7 +810,7 @@ int ps_xent_backward(const ps_xent* q, const float* lse, float scale, const floa
  * fault; non-zero = a bounded wait inside a kernel expired (that call's results are undefined). */
 int ps_xent_status(int* status_out);
 
-/* Text of the last CUDA error of a ps_mx_*, ps_clip_* or ps_xent_* call on this host thread. */
+/* Text of the last CUDA error of a ps_mx_*, ps_clip_*, ps_ortho_* or ps_xent_* call on this host thread. */
 const char* ps_op_last_error(void);
 
 const char* ps_strerror(int status);

@@ -56,6 +56,10 @@ class ps_mx(C.Structure):
     _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("rows", C.c_longlong), ("cols", C.c_longlong)]
 
 
+class ps_matrix(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("rows", C.c_longlong), ("cols", C.c_longlong), ("ld", C.c_longlong)]
+
+
 class ps_xent(C.Structure):
     _fields_ = [("x", C.c_void_p), ("ldx", C.c_longlong), ("w", C.c_void_p), ("ldw", C.c_longlong),
                 ("targets", C.c_void_p), ("target_bits", C.c_int), ("tokens", C.c_longlong), ("vocab", C.c_longlong),
@@ -159,6 +163,10 @@ _SIGNATURES = {
     "ps_mx_dequantize": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p, C.c_longlong, C.c_void_p]),
     "ps_mx_matmul": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_longlong, C.c_void_p]),
     "ps_mx_status": (C.c_int, [C.POINTER(C.c_int)]),
+    "ps_ortho_create": (C.c_int, [C.POINTER(C.c_void_p), C.c_int, C.c_int, C.c_void_p, C.c_int, C.c_void_p, C.c_int]),
+    "ps_ortho_run": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "ps_ortho_status": (C.c_int, [C.c_void_p, C.POINTER(C.c_int)]),
+    "ps_ortho_destroy": (C.c_int, [C.c_void_p]),
     "ps_xent_sizes": (C.c_int, [C.c_longlong, C.c_longlong, C.c_longlong, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]),
     "ps_xent_forward": (C.c_int, [C.POINTER(ps_xent), C.c_void_p, C.c_void_p, C.c_void_p]),
     "ps_xent_backward": (C.c_int, [C.POINTER(ps_xent), C.c_void_p, C.c_float, C.c_void_p, C.c_void_p, C.c_longlong,
@@ -824,6 +832,57 @@ class Clip:
     def close(self):
         if getattr(self, "handle", None):
             load().ps_clip_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Ortho:
+    """A list of matrices (2-D device tensors with contiguous rows, float32 or bfloat16, one type per side, all on one
+    GPU) and where their orthogonalised forms go; without destinations they replace the sources."""
+
+    def __init__(self, srcs, dsts=None, device: int | None = None):
+        where = "ps_ortho_create"
+        self.srcs, self.dsts = list(srcs), list(srcs if dsts is None else dsts)     # kept alive with the handle
+        if [tuple(t.shape) for t in self.srcs] != [tuple(t.shape) for t in self.dsts]:
+            raise PsError(PS_ERR_BAD_ARG, where, "sources and destinations differ in number or shape")
+        for t in self.srcs + self.dsts:
+            if t.get_device() < 0 or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (
+                    t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+                raise PsError(PS_ERR_BAD_ARG, where, "CUDA matrices with contiguous rows are wanted")
+        types = [{_dtype(t, where) for t in ts} for ts in (self.srcs, self.dsts)]
+        if any(len(t) > 1 for t in types):
+            raise PsError(PS_ERR_BAD_ARG, where, "one dtype per side is wanted")
+        if device is None:
+            device = self.srcs[0].get_device() if self.srcs else 0
+        if any(t.get_device() != device for t in self.srcs + self.dsts):
+            raise PsError(PS_ERR_BAD_ARG, where, "the matrices are not all on GPU %d" % device)
+        self.device = device
+        n = len(self.srcs)
+        src, dst = ((ps_matrix * n)(*[(t.data_ptr(), t.shape[0], t.shape[1], max(t.stride(0), t.shape[1])) for t in ts])
+                    for ts in (self.srcs, self.dsts))
+        h = C.c_void_p()
+        _check_op(load().ps_ortho_create(C.byref(h), device, n, src, types[0].pop() if n else PS_F32, dst,
+                                         types[1].pop() if n else PS_F32), where)
+        self.handle = h.value
+
+    def run(self, stream=None):
+        rc = _lib.ps_ortho_run(self.handle, _stream_ptr(stream))
+        if rc != PS_OK:
+            _check_op(rc, "ps_ortho_run")
+
+    def status(self) -> int:
+        v = C.c_int()
+        _check_op(load().ps_ortho_status(self.handle, C.byref(v)), "ps_ortho_status")
+        return v.value
+
+    def close(self):
+        if getattr(self, "handle", None):
+            load().ps_ortho_destroy(self.handle)
             self.handle = None
 
     def __del__(self):

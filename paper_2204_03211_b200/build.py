@@ -19,7 +19,7 @@ LIB = os.path.join(HERE, "libps_b200.so")
 OPS = os.path.join(HERE, "_ops" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = [os.path.join(CSRC, "ps_service.cu"), os.path.join(CSRC, "ps_planner.cpp"), os.path.join(CSRC, "ps_peer.cpp"),
            os.path.join(CSRC, "ps_mx.cu"), os.path.join(CSRC, "ps_clip.cu"),
-           os.path.join(CSRC, "ps_xent.cu")]
+           os.path.join(CSRC, "ps_ortho.cu"), os.path.join(CSRC, "ps_xent.cu")]
 
 
 def _deps():

@@ -111,6 +111,15 @@ __device__ __forceinline__ void mm_load32(unsigned int tmem, float* v) {
         "=r"(u[25]), "=r"(u[26]), "=r"(u[27]), "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
       : "r"(tmem));
 }
+__device__ __forceinline__ void mm_store16(unsigned int tmem, const float* v) {      // without waiting
+  const unsigned int* u = reinterpret_cast<const unsigned int*>(v);
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(tmem),
+      "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]),
+      "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15])
+      : "memory");
+}
 __device__ __forceinline__ void mm_load16(unsigned int tmem, float* v) {
   unsigned int* u = reinterpret_cast<unsigned int*>(v);
   asm volatile(

@@ -1,0 +1,411 @@
+// Host side of the orthogonalisation (declarations and contracts: include/ps_b200.h).
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <cstring>
+#include <mutex>
+#include <new>
+
+#include "ps_ortho.cuh"
+#include "ps_ortho.h"
+
+namespace psb {
+namespace {
+
+constexpr int kNsMaxDevices = 64;
+constexpr long long kNsMaxDim = 1ll << 30;       // (TMA coordinates are 32-bit)
+constexpr long long kNsMaxTiles = 1ll << 26;     // tiles and units of a list
+
+struct NsDevice {
+  bool ready = false;
+  int room[2][2];                        // by split and pair: tiles that are worked on together
+};
+std::mutex g_ns_mu;
+NsDevice g_ns_dev[kNsMaxDevices];
+
+// The four kernels: two planes or one, pairs of CTAs or single ones.
+struct NsKernel {
+  void (*fn)(NsArgs);
+  int smem, ctas;
+};
+template <int PLANES, bool PAIR>
+NsKernel kernel_as() {
+  return {ps_tc_kernel<NsOp<PLANES, PAIR>>, TcCfg<NsOp<PLANES, PAIR>>::kSmem, PAIR ? 2 : 1};
+}
+NsKernel kernel_of(bool split, bool pair) {
+  return split ? (pair ? kernel_as<2, true>() : kernel_as<2, false>()) : (pair ? kernel_as<1, true>() : kernel_as<1, false>());
+}
+
+int ns_device(bool split, bool pair, int* room) {
+  OpDevice d;
+  int rc = op_device(&d);
+  if (rc) return rc;
+  std::lock_guard<std::mutex> lk(g_ns_mu);
+  NsDevice& n = g_ns_dev[d.id];
+  if (!n.ready) {
+    for (int s = 0; s < 2; ++s)
+      for (int p = 0; p < 2; ++p) {
+        const NsKernel k = kernel_of(s, p);
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)k.ctas);
+        cfg.blockDim = dim3(kTcThreads);
+        cfg.dynamicSmemBytes = (size_t)k.smem;
+        int clusters = 0;
+        cudaError_t e = cudaFuncSetAttribute(k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, k.smem);
+        if (e == cudaSuccess) e = cudaOccupancyMaxActiveClusters(&clusters, k.fn, &cfg);
+        if (e != cudaSuccess) return op_cuda_error("preparing the orthogonalisation", e);
+        n.room[s][p] = std::max(1, std::min(clusters, d.num_sms / k.ctas));
+      }
+    n.ready = true;
+  }
+  *room = n.room[split][pair];
+  return PS_OK;
+}
+
+long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+bool empty(const NsItem& it) { return it.rows == 0 || it.cols == 0; }
+
+// Where a matrix's working memory lies.
+struct NsLayout {
+  long long m, n, pitch_x, pitch_e;
+  size_t x[2][2], e[2], f[2], d, fd, parts, end;
+  long long units;
+};
+
+NsLayout layout(const NsItem& it, bool split, size_t at) {
+  NsLayout l;
+  l.m = std::min(it.rows, it.cols);
+  l.n = std::max(it.rows, it.cols);
+  l.pitch_x = ceil_div(l.n, 64) * 64;
+  l.pitch_e = ceil_div(l.m, 64) * 64;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += round256(bytes);
+    return here;
+  };
+  const size_t x = (size_t)l.m * (size_t)l.pitch_x * 2, e = (size_t)l.m * (size_t)l.pitch_e * 2;
+  for (int b = 0; b < 2; ++b)
+    for (int p = 0; p < 2; ++p) l.x[b][p] = take(x);
+  for (int p = 0; p < 2; ++p) l.e[p] = take(p == 0 || split ? e : 0);
+  for (int p = 0; p < 2; ++p) l.f[p] = take(p == 0 || split ? e : 0);
+  const size_t d = (size_t)ceil_div(l.m, 256) * 256 * sizeof(float);      // (read by whole tiles)
+  l.d = take(d);
+  l.fd = take(d);
+  l.units = ceil_div(it.rows, kNsUnitRows) * ceil_div(it.cols, kNsUnitCols);
+  l.parts = take(it.parts ? 0 : (size_t)l.units * sizeof(double));
+  l.end = at;
+  return l;
+}
+
+// A plane by boxes: 64 x 64 as the products' operand (128-byte swizzle), or `rows` x 32 for the epilogues (64-byte swizzle).
+bool make_map(EncodeTiled encode, CUtensorMap* m, const void* p, long long rows, long long cols, long long pitch, int box_rows,
+              bool operand) {
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)pitch * 2};
+  const cuuint32_t box[2] = {operand ? 64u : 32u, (cuuint32_t)box_rows}, step[2] = {1, 1};
+  return encode(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void*>(p), dims, strides, box, step,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, operand ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Matrices whose products of one kind go out together: enough for this many tiles per pair, so that what a tile waits
+// for has long been done.
+constexpr long long kNsGroupTiles = 2 * 74;
+
+// Pairs of CTAs fetch half as much from L2 per product as single ones; single ones have four times as many tiles, and
+// their products are done in half the time.  Lists of more than this many 256 x 256 tiles take pairs.  Single | pairs,
+// bf16 results, us: 24 x 512 x 512 (96 tiles) 209 | 253, 36 x 512 x 2048 (576) 746 | 680, 24 x 1024 x 4096 (1536) 2779 | 2213.
+constexpr long long kNsPairsFrom = 200;
+
+}  // namespace
+
+size_t NsPlan::workspace(const std::vector<NsItem>& items, bool split) {
+  size_t at = 0;
+  long long tiles = 0, units = 0;
+  for (const NsItem& it : items) {
+    if (empty(it)) continue;
+    const NsLayout l = layout(it, split, at);
+    at = l.end;
+    const long long tm = ceil_div(l.m, 128), tn = ceil_div(l.n, 128);
+    if (tm > (1ll << 13) || tn > (1ll << 20)) return 0;
+    tiles += kNsSteps * (tm * (tm + 1) + tm * tn);
+    units += l.units;
+    if (tiles > kNsMaxTiles || units > kNsMaxTiles) return 0;
+  }
+  return std::max<size_t>(at, 256);
+}
+
+NsPlan::~NsPlan() {
+  if (mem_) cudaFree(mem_);              // (waits for launches that still use it)
+}
+
+int NsPlan::build(const std::vector<NsItem>& items, bool split, void* workspace) {
+  // Single CTAs with 128 x 128 where pairs would have few tiles.
+  long long large = 0;
+  for (const NsItem& it : items)
+    if (!empty(it)) large += ceil_div(it.rows, 256) * ceil_div(it.cols, 256);
+  pair_ = large > kNsPairsFrom;
+  const long long tile = pair_ ? 256 : 128;
+  int room = 0;
+  int rc = ns_device(split, pair_, &room);
+  if (rc) return rc;
+  EncodeTiled encode;
+  rc = op_encoder(&encode);
+  if (rc) return rc;
+  char* ws = static_cast<char*>(workspace);
+  std::vector<const NsItem*> live;
+  for (const NsItem& it : items)
+    if (!empty(it)) live.push_back(&it);
+  const size_t n = live.size();
+  if (n == 0) return PS_OK;
+  std::vector<CUtensorMap> maps(kNsMaps * n);
+  std::vector<NsMat> mats(n);
+  std::vector<NsTile> list;
+  std::vector<int2> units;
+  std::memset(mats.data(), 0, n * sizeof(NsMat));
+  std::memset(maps.data(), 0, maps.size() * sizeof(CUtensorMap));
+  size_t at = 0;
+  long long sym_tiles = 0;
+  for (size_t i = 0; i < n; ++i) {
+    const NsItem& it = *live[i];
+    const NsLayout l = layout(it, split, at);
+    at = l.end;
+    NsMat& M = mats[i];
+    auto half_at = [&](size_t o) { return reinterpret_cast<__half*>(ws + o); };
+    M.m = (int)l.m;
+    M.n = (int)l.n;
+    M.flip = it.rows > it.cols;
+    M.out = it.out;
+    M.pitch_x = l.pitch_x;
+    M.pitch_e = l.pitch_e;
+    bool ok = true;
+    CUtensorMap* map = &maps[kNsMaps * i];
+    auto plane = [&](int at_map, const void* p, long long cols, long long pitch) {
+      ok = ok && make_map(encode, map + at_map, p, l.m, cols, pitch, 64, true);
+      ok = ok && make_map(encode, map + kNsTall + at_map, p, l.m, cols, pitch, 128, false);
+    };
+    for (int b = 0; b < 2; ++b)
+      for (int p = 0; p < 2; ++p) {
+        M.x[b][p] = half_at(l.x[b][p]);
+        plane(2 * b + p, M.x[b][p], l.n, l.pitch_x);
+      }
+    for (int p = 0; p < (split ? 2 : 1); ++p) {
+      M.e[p] = half_at(l.e[p]);
+      M.f[p] = half_at(l.f[p]);
+      plane(4 + p, M.e[p], l.m, l.pitch_e);
+      plane(6 + p, M.f[p], l.m, l.pitch_e);
+      ok = ok && make_map(encode, map + kNsMirror + p, M.e[p], l.m, l.m, l.pitch_e, 32, false);
+      ok = ok && make_map(encode, map + kNsMirror + 2 + p, M.f[p], l.m, l.m, l.pitch_e, 32, false);
+    }
+    if (!ok) return op_cuda_error("tensor map", cudaErrorInvalidValue);
+    M.d = reinterpret_cast<float*>(ws + l.d);
+    M.fd = reinterpret_cast<float*>(ws + l.fd);
+    M.src = it.src;
+    M.ld_src = it.ld_src;
+    M.src_bf16 = it.src_bf16;
+    M.parts = it.parts ? it.parts : reinterpret_cast<double*>(ws + l.parts);
+    M.nparts = it.parts ? it.nparts : (int)l.units;
+    if (!it.parts) norms_ = true;
+    M.dst = it.dst;
+    M.ld_dst = it.ld_dst;
+    const size_t es = it.out == kNsOutBf16 ? 2 : 4;
+    M.wide = !M.flip && (reinterpret_cast<uintptr_t>(it.dst) & 31u) == 0 && it.ld_dst * (long long)es % 32 == 0;
+    M.decay = it.decay;
+    M.step = it.step;
+    // 2^kx: entries of X0 are about 1 / sqrt(m n)
+    int kx = (int)std::lround(0.5 * std::log2((double)l.m * (double)l.n));
+    kx = std::max(0, std::min(14, kx));
+    M.sx = std::ldexp(1.f, kx);
+    const int tm = (int)ceil_div(l.m, tile), tn = (int)ceil_div(l.n, tile);
+    for (int a = 0; a < tm; ++a) {
+      const int ctas = pair_ && l.m - a * tile > 128 ? 2 : 1;
+      M.parts_s += (a + 1) * ctas;
+      M.parts_x += tn * ctas;
+    }
+    sym_tiles += tm * (tm + 1) / 2;
+    for (long long u = 0; u < l.units; ++u) units.push_back(make_int2((int)i, (int)u));
+  }
+  // the tiles: matrices dealt to groups, a group's products one kind after the other
+  const size_t groups = (size_t)std::max<long long>(1, std::min<long long>((long long)n, sym_tiles / kNsGroupTiles));
+  for (size_t g = 0; g < groups; ++g)
+    for (int step = 0; step < kNsSteps; ++step)
+      for (int product = 0; product < 3; ++product)
+        for (size_t i = g; i < n; i += groups) {
+          const int tm = (int)ceil_div(mats[i].m, tile), tn = (int)ceil_div(mats[i].n, tile);
+          for (int a = 0; a < tm; ++a)
+            for (int b = 0; b < (product == 2 ? tn : a + 1); ++b)
+              list.push_back(NsTile{(int)i, (short)step, (short)product, a, b});
+        }
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = off;
+    off += round256(bytes);
+    return here;
+  };
+  const size_t maps_off = take(maps.size() * sizeof(CUtensorMap));
+  mats_off_ = take(n * sizeof(NsMat));
+  list_off_ = take(list.size() * sizeof(NsTile));
+  units_off_ = take(units.size() * sizeof(int2));
+  const size_t done_off = take(n * sizeof(unsigned int) * 32);         // a line each
+  status_off_ = take(sizeof(int));
+  void* mem = nullptr;
+  cudaError_t e = cudaMalloc(&mem, off);
+  if (e != cudaSuccess) return op_cuda_error("tables of the orthogonalisation", e);
+  mem_ = static_cast<unsigned char*>(mem);
+  for (size_t i = 0; i < n; ++i) {
+    mats[i].maps = reinterpret_cast<const CUtensorMap*>(mem_ + maps_off) + kNsMaps * i;
+    mats[i].done = reinterpret_cast<unsigned int*>(mem_ + done_off) + 32 * i;
+  }
+  auto put = [&](size_t o, const void* p, size_t bytes) {
+    if (e == cudaSuccess) e = cudaMemcpy(mem_ + o, p, bytes, cudaMemcpyHostToDevice);
+  };
+  put(maps_off, maps.data(), maps.size() * sizeof(CUtensorMap));
+  put(mats_off_, mats.data(), n * sizeof(NsMat));
+  put(list_off_, list.data(), list.size() * sizeof(NsTile));
+  put(units_off_, units.data(), units.size() * sizeof(int2));
+  if (e == cudaSuccess) e = cudaMemset(mem_ + done_off, 0, status_off_ + sizeof(int) - done_off);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(cudaStreamLegacy);   // before other streams use it
+  if (e != cudaSuccess) return op_cuda_error("tables of the orthogonalisation", e);
+  tiles_ = (int)list.size();
+  units_ = (int)units.size();
+  grid_ = (pair_ ? 2 : 1) * std::min(tiles_, room);
+  split_ = split;
+  return PS_OK;
+}
+
+int NsPlan::run(cudaStream_t stream, int* launches) const {
+  if (launches) *launches = 0;
+  if (!tiles_) return PS_OK;
+  const NsMat* mats = reinterpret_cast<const NsMat*>(mem_ + mats_off_);
+  const int2* units = reinterpret_cast<const int2*>(mem_ + units_off_);
+  int rc = PS_OK;
+  if (norms_) rc = op_launch("orthogonalisation", ps_ortho_norm_kernel, (unsigned)units_, kNsThreads, 0, 1, stream, mats, units);
+  if (!rc) rc = op_launch("orthogonalisation", ps_ortho_prepare_kernel, (unsigned)units_, kNsThreads, 0, 1, stream, mats, units);
+  if (rc) return rc;
+  NsArgs a;
+  a.status = reinterpret_cast<int*>(mem_ + status_off_);
+  a.mats = mats;
+  a.list = reinterpret_cast<const NsTile*>(mem_ + list_off_);
+  a.tiles = tiles_;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)grid_);
+  cfg.blockDim = dim3(kTcThreads);
+  const NsKernel kernel = kernel_of(split_, pair_);
+  cfg.dynamicSmemBytes = (size_t)kernel.smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeCooperative;           // tiles wait for tiles of other CTAs: all have to be running
+  attr[0].val.cooperative = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel.fn, a);
+  if (e != cudaSuccess) return op_cuda_error("orthogonalisation", e);
+  if (launches) *launches = norms_ ? 3 : 2;
+  return PS_OK;
+}
+
+int NsPlan::status(int* out) const {
+  *out = 0;
+  cudaError_t e = cudaDeviceSynchronize();
+  if (e == cudaSuccess && mem_) e = cudaMemcpy(out, mem_ + status_off_, sizeof(int), cudaMemcpyDeviceToHost);
+  return e == cudaSuccess ? PS_OK : op_cuda_error("status of the orthogonalisation", e);
+}
+
+constexpr uint32_t kOrthoMagic = 0x50534f32u;    // "PSO2"
+
+}  // namespace psb
+
+using namespace psb;
+
+struct ps_ortho {
+  uint32_t magic = kOrthoMagic;
+  int device = 0;
+  void* workspace = nullptr;
+  NsPlan plan;
+};
+
+namespace {
+bool alive(const ps_ortho* o) { return o && o->magic == kOrthoMagic; }
+bool misaligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
+}  // namespace
+
+extern "C" {
+
+int ps_ortho_create(ps_ortho** out, int device, int n, const ps_matrix* srcs, int src_dtype, const ps_matrix* dsts, int dst_dtype) {
+  if (!out) return PS_ERR_BAD_ARG;
+  *out = nullptr;
+  if (device < 0 || n < 0 || (n > 0 && (!srcs || !dsts))) return PS_ERR_BAD_ARG;
+  if ((src_dtype != PS_F32 && src_dtype != PS_BF16) || (dst_dtype != PS_F32 && dst_dtype != PS_BF16)) return PS_ERR_BAD_ARG;
+  ps_ortho* o = nullptr;
+  int rc = PS_OK;
+  try {
+    std::vector<NsItem> items((size_t)n);
+    for (int i = 0; i < n; ++i) {
+      const ps_matrix &s = srcs[i], &d = dsts[i];
+      if (s.rows < 0 || s.cols < 0 || s.rows >= kNsMaxDim || s.cols >= kNsMaxDim || d.rows != s.rows || d.cols != s.cols)
+        return PS_ERR_BAD_ARG;
+      if (s.rows == 0 || s.cols == 0) continue;
+      if (!s.data || !d.data || s.ld < s.cols || d.ld < d.cols) return PS_ERR_BAD_ARG;
+      if (misaligned(s.data, src_dtype == PS_BF16 ? 2 : 4) || misaligned(d.data, dst_dtype == PS_BF16 ? 2 : 4)) return PS_ERR_ALIGN;
+      NsItem& it = items[(size_t)i];
+      it.rows = s.rows;
+      it.cols = s.cols;
+      it.src = s.data;
+      it.ld_src = s.ld;
+      it.src_bf16 = src_dtype == PS_BF16;
+      it.dst = d.data;
+      it.ld_dst = d.ld;
+      it.out = dst_dtype == PS_BF16 ? kNsOutBf16 : kNsOutF32;
+    }
+    const bool split = dst_dtype == PS_F32;
+    const size_t bytes = NsPlan::workspace(items, split);
+    if (!bytes) return PS_ERR_TOO_LARGE;
+    DeviceScope on(device);
+    cudaError_t e = on.error;
+    if (e != cudaSuccess) return op_cuda_error("cudaSetDevice", e);
+    o = new ps_ortho();
+    o->device = device;
+    e = cudaMalloc(&o->workspace, bytes);
+    rc = e == cudaSuccess ? o->plan.build(items, split, o->workspace) : op_cuda_error("ps_ortho_create", e);
+    if (!rc) {
+      *out = o;
+      return PS_OK;
+    }
+  } catch (const std::bad_alloc&) {
+    rc = PS_ERR_NOMEM;
+  }
+  if (o) {
+    DeviceScope on(device);
+    if (o->workspace) cudaFree(o->workspace);
+    delete o;
+  }
+  return rc;
+}
+
+int ps_ortho_run(ps_ortho* o, void* stream) {
+  if (!alive(o)) return PS_ERR_BAD_HANDLE;
+  DeviceScope on(o->device);
+  if (on.error != cudaSuccess) return op_cuda_error("cudaSetDevice", on.error);
+  return o->plan.run(static_cast<cudaStream_t>(stream));
+}
+
+int ps_ortho_status(ps_ortho* o, int* status_out) {
+  if (!alive(o)) return PS_ERR_BAD_HANDLE;
+  if (!status_out) return PS_ERR_BAD_ARG;
+  DeviceScope on(o->device);
+  if (on.error != cudaSuccess) return op_cuda_error("cudaSetDevice", on.error);
+  return o->plan.status(status_out);
+}
+
+int ps_ortho_destroy(ps_ortho* o) {
+  if (!alive(o)) return PS_ERR_BAD_HANDLE;
+  DeviceScope on(o->device);
+  cudaError_t e = on.error;
+  if (e == cudaSuccess && o->workspace) e = cudaFree(o->workspace);      // waits for runs that still use it
+  o->magic = 0;
+  delete o;
+  return e == cudaSuccess ? PS_OK : op_cuda_error("ps_ortho_destroy", e);
+}
+
+}  // extern "C"

@@ -1,0 +1,483 @@
+// Orthogonalisation of matrices by five Newton-Schulz steps, the heart of Muon's update:
+//     X = G / (|G| + 1e-7)   (Frobenius norm),   five times:   A = X X^T,  B = b A + c A A,  X = a X + B X
+// for m x n matrices with m <= n; taller ones are worked on as their transposes.
+//
+// Three products per step and 15 per matrix, each needing the one before it, for a list of matrices at once.  All of
+// them run in ONE cooperative launch of the frame of ps_tc.cuh: every tile names the matrix and the product it belongs
+// to, tiles are listed step by step, and a tile waits until its matrix's earlier products are done (one counter per
+// matrix).  Every pair of CTAs takes its tiles in the list's order, so whatever a tile waits for is being worked on;
+// there is no barrier over the grid, and one matrix's wait is another one's work.  A and B are symmetric: only tiles on
+// and below the diagonal are computed, and stored twice.
+//
+// Arithmetic.  Operands are fp16 (11 bits) scaled by powers of two, sums are binary32.
+//  - The largest entries of A and B stand on their diagonals, and the last steps subtract them from a; they are
+//    kept apart in binary32 and enter in the epilogues (A A = E E + (d_i + d_j) E + d^2, and (a + f_i) X + F X), where E
+//    and F are what is off the diagonal.  One rounding of the whole B costs four times the error.
+//  - X is kept as high + low halves (22 bits).  Directions that the gradient hardly has grow by a^5 = 485, and with
+//    them whatever X was rounded to: with 11 bits a matrix of falling singular values comes out 2 % wrong.
+//  - Results in bf16 take one product, of the high halves: 5e-4 to 1e-3 of the result's norm (its own rounding is
+//    1.7e-3).  Results in binary32, and the service's update, also split E and F and take three (high x high, high x
+//    low, low x high): what is left is the rounding of the tensor cores' sums.
+// Scales: X by 2^kx (about sqrt(m n), at most 2^14: entries are at most 1.2), E by 2^14 (at most 1.5), F by 2^13 (at
+// most 2.9), so that nothing overflows fp16 and typical entries are far from its subnormal end.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "ps_tc.cuh"
+
+namespace psb {
+
+constexpr int kNsSteps = 5;
+constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
+constexpr double kNsEps = 1e-7;
+constexpr float kNsScaleE = 16384.f, kNsScaleF = 8192.f;
+
+constexpr int kNsMaps = 20, kNsTall = 8, kNsMirror = 16;
+
+enum { kNsOutF32 = 0, kNsOutBf16 = 1, kNsOutUpdate = 2 };
+
+struct NsMat {                           // one matrix, in its working orientation: m <= n
+  int m, n;
+  int flip;                              // 1: source and result are the transposes
+  int out;                               // kNsOut*
+  long long pitch_x, pitch_e;            // elements; multiples of 64
+  __half* x[2][2];                       // two buffers of two planes: a step reads one and writes the other
+  __half* e[2];                          // planes of what is off A's diagonal; the second where products are split
+  __half* f[2];                          // and off B's
+  float *d, *fd;                         // the diagonals
+  const CUtensorMap* maps;               // x[0], x[1], e, f, two planes each: as operands, by 128 x 32 (kNsTall), and e and
+                                         // f by 32 x 32 (kNsMirror)
+  const void* src;                       // rows x cols as the caller sees them
+  long long ld_src;
+  int src_bf16;
+  int nparts;
+  double* parts;                         // partial sums of squares
+  void* dst;
+  long long ld_dst;
+  int wide;                              // rows of dst allow 256-bit accesses
+  float decay, step;                     // kNsOutUpdate: dst = dst * decay - step * O
+  float sx;                              // 2^kx
+  int parts_s, parts_x;                  // what `done` counts in a symmetric product and in the last one
+  unsigned int* done;                    // CTAs' finished parts of tiles (those that have rows of the matrix)
+};
+
+struct NsTile {                          // one tile of the list
+  int mat;
+  short step, product;                   // product 0: A, 1: B, 2: X
+  int ti, tj;
+};
+
+struct NsArgs {
+  int* status;
+  const NsMat* mats;
+  const NsTile* list;
+  int tiles;
+};
+
+// Two values as high and low halves: fp16 numbers whose sums they are (to 22 bits).
+__device__ __forceinline__ void ns_split2(float a, float b, unsigned int& hi, unsigned int& lo) {
+  const __half2 h = __floats2half2_rn(a, b);
+  const float2 f = __half22float2(h);
+  const __half2 l = __floats2half2_rn(a - f.x, b - f.y);
+  hi = *reinterpret_cast<const unsigned int*>(&h);
+  lo = *reinterpret_cast<const unsigned int*>(&l);
+}
+__device__ __forceinline__ void ns_split(float v, __half& hi, __half& lo) {
+  hi = __float2half_rn(v);
+  lo = __float2half_rn(v - __half2float(hi));
+}
+__device__ __forceinline__ float2 ns_widen(unsigned int u) { return __half22float2(*reinterpret_cast<const __half2*>(&u)); }
+
+template <int PLANES, bool PAIR>
+struct NsOp {
+  static constexpr bool kPair = PAIR;
+  static constexpr int kPlanes = PLANES, kType = 0, kTile = PAIR ? 256 : 128, kColumns = kTile / 2;
+  static constexpr int kSlots = 2, kStages = PLANES == 2 ? 2 : 4;
+  static constexpr int kSegment = PLANES == 1 ? 0 : PAIR ? 4 : 2;
+  using Args = NsArgs;
+
+  static __device__ __forceinline__ int tiles(const NsArgs& a) { return a.tiles; }
+
+  using Item = NsTile;
+
+  static __device__ __forceinline__ Item item(const NsArgs& a, int index, int tiles) { return a.list[min(index, tiles - 1)]; }
+
+  static __device__ __forceinline__ int stages(const NsArgs& a, const NsTile& at) {
+    const NsMat& M = a.mats[at.mat];
+    return ((at.product == 0 ? M.n : M.m) + kTcK - 1) / kTcK;
+  }
+
+  // A tile waits for its matrix's earlier products.
+  static __device__ __forceinline__ void tile(const NsArgs& a, const NsTile& at, TcTile* t) {
+    const NsMat& M = a.mats[at.mat];
+    t->ready = M.done;
+    t->need = (unsigned)(at.step * (2 * M.parts_s + M.parts_x) + at.product * M.parts_s);
+    t->a_row = at.ti * kTile;
+    t->b_row = at.tj * kTile;
+    t->a_k = t->b_k = 0;
+    t->a_mn = 0;
+    t->b_mn = at.product == 2;           // X's rows are k there
+    const CUtensorMap* x = M.maps + 2 * (at.step & 1);
+    t->a = at.product == 0 ? x : at.product == 1 ? M.maps + 4 : M.maps + 6;
+    t->b = at.product == 1 ? M.maps + 4 : x;
+    t->nk = stages(a, at);
+  }
+
+  // ---- slots: 128 rows by 32 columns of E (product 1) or X (product 2) go in, of E, F or X come out.  Symmetric results
+  // of tiles off the diagonal also go out mirrored: from the slot's second plane, or, where both planes are results,
+  // from a slot of their own.
+
+  static __device__ __forceinline__ int width(const NsMat& M, const NsTile& at) { return at.product == 2 ? M.n : M.m; }
+  static __device__ __forceinline__ bool mirrored(const NsTile& at) { return at.product < 2 && at.ti != at.tj; }
+  static __device__ __forceinline__ int per_chunk(const NsTile& at) { return PLANES == 2 && mirrored(at) ? 2 : 1; }
+
+  static __device__ __forceinline__ int entries(const NsArgs& a, const NsTile& at, int rank, int half) {
+    const NsMat& M = a.mats[at.mat];
+    const int left = width(M, at) - (at.tj * kTile + half * kColumns);
+    if (left <= 0 || at.ti * kTile + rank * 128 >= M.m) return 0;
+    return min(kColumns / 32, (left + 31) / 32) * per_chunk(at);
+  }
+
+  static __device__ __forceinline__ void load(const NsArgs& a, const NsTile& at, int rank, int half, int entry, unsigned int slot,
+                                              unsigned int vectors, unsigned int bar) {
+    const NsMat& M = a.mats[at.mat];
+    const int per = per_chunk(at), c = entry / per * 32, i0 = at.ti * kTile + rank * 128, j0 = at.tj * kTile + half * kColumns;
+    if (at.product == 0 || entry % per) {                // nothing to read
+      tc_arrive(bar);
+      return;
+    }
+    const int planes = at.product == 1 ? PLANES : 2;
+    const unsigned int first = entry == 0 ? (at.product == 1 ? 512 + 4 * kColumns : 512) : 0;
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(planes * kTcPlane + first) : "memory");
+    if (entry == 0) {                                    // the diagonal at the rows, and at the columns
+      mm_bulk(vectors, (at.product == 1 ? M.d : M.fd) + i0, 512, bar);
+      if (at.product == 1) mm_bulk(vectors + 512, M.d + j0, 4 * kColumns, bar);
+    }
+    const CUtensorMap* map = M.maps + kNsTall + (at.product == 1 ? 4 : 2 * (at.step & 1));
+    for (int p = 0; p < planes; ++p) mm_tma(slot + p * kTcPlane, map + p, j0 + c, i0, bar);
+  }
+
+  static __device__ __forceinline__ void store(const NsArgs& a, const NsTile& at, int rank, int half, int entry, unsigned int slot) {
+    const NsMat& M = a.mats[at.mat];
+    if (at.product == 2 && at.step == kNsSteps - 1) return;                  // (results go out from registers)
+    const int per = per_chunk(at), c = entry / per * 32, i0 = at.ti * kTile + rank * 128, j = at.tj * kTile + half * kColumns + c;
+    const bool direct = entry % per == 0, mirror = mirrored(at) && (PLANES == 1 || !direct);
+    if (direct) {
+      const CUtensorMap* map = M.maps + kNsTall + (at.product == 0 ? 4 : at.product == 1 ? 6 : 2 * ((at.step & 1) ^ 1));
+      for (int p = 0; p < (at.product == 2 ? 2 : PLANES); ++p) tc_store(map + p, j, i0, slot + p * kTcPlane);
+    }
+    if (mirror) {
+      const CUtensorMap* map = M.maps + kNsMirror + 2 * at.product;
+      for (int p = 0; p < PLANES; ++p)
+        for (int q = 0; q < 4; ++q)
+          if (i0 + 32 * q < M.m) tc_store(map + p, i0 + 32 * q, j, slot + (PLANES == 1 ? kTcPlane : p * kTcPlane) + q * (kTcPlane / 4));
+    }
+  }
+
+  static __device__ __forceinline__ void done(const NsArgs& a, const NsTile& at, int rank) {
+    if (at.product == 2 && at.step == kNsSteps - 1) return;                  // (nobody waits for results)
+    if (at.ti * kTile + rank * 128 >= a.mats[at.mat].m) return;              // (would count before the tile is done)
+    asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(a.mats[at.mat].done) : "memory");
+  }
+
+  struct Epilogue {
+    const NsTile& at;
+    const NsMat& M;
+    TcWarp& w;
+    MmCursor<kSlots>& slot;
+    int i, j0, width_;                   // this lane's row; the warp's first column, and where the columns end
+    bool live, last;
+
+    __device__ __forceinline__ Epilogue(const NsArgs& a, const NsTile& item, TcWarp& warp, MmCursor<kSlots>& cursor)
+        : at(item), M(a.mats[item.mat]), w(warp), slot(cursor) {}
+
+    __device__ __forceinline__ void begin() {
+      const int i0 = at.ti * kTile + w.row;
+      i = i0 + w.lane;
+      j0 = at.tj * kTile + w.col;
+      width_ = width(M, at);
+      live = (i0 & ~127) < M.m;                            // (as entries(): the CTA's rows hold something)
+      last = at.step == kNsSteps - 1;
+    }
+
+    __device__ __forceinline__ uint4* piece(int p, int k) {
+      return reinterpret_cast<uint4*>(w.slots + slot.s * kTcSlot + p * kTcPlane + tc_piece_at((w.row & 127) + w.lane, k));
+    }
+
+    __device__ __forceinline__ void wait_staged() { mm_wait(w.staged + 8 * slot.s, slot.parity, w.status); }
+
+    // The warp's part of the slot may go out.
+    __device__ __forceinline__ void hand_over() {
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (w.lane == 0) tc_arrive(w.filled + 8 * slot.s);
+      slot.next();
+    }
+
+    // This lane's row of both planes: v as high and low halves.
+    __device__ __forceinline__ void put(const float (&v)[32], bool low) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        unsigned int hi[4], lo[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) ns_split2(v[8 * k + 2 * q], v[8 * k + 2 * q + 1], hi[q], lo[q]);
+        *piece(0, k) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        if (low) *piece(1, k) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+      }
+    }
+
+    // The same down a column: the mirrored 32 x 32, high or low halves.
+    __device__ __forceinline__ void put_mirrored(const float (&v)[32], int p, bool low) {
+      unsigned char* base = w.slots + slot.s * kTcSlot + p * kTcPlane + ((w.row & 127) >> 5) * (kTcPlane / 4) + (w.lane & 7) * 2;
+#pragma unroll
+      for (int k = 0; k < 32; k += 2) {
+        unsigned int hi, lo;
+        ns_split2(v[k], v[k + 1], hi, lo);
+        const unsigned int u = low ? lo : hi;
+        *reinterpret_cast<unsigned short*>(base + tc_piece_at(k, w.lane >> 3)) = (unsigned short)(u & 0xffffu);
+        *reinterpret_cast<unsigned short*>(base + tc_piece_at(k + 1, w.lane >> 3)) = (unsigned short)(u >> 16);
+      }
+    }
+
+    // Off-diagonal entries of a symmetric matrix, already scaled, and where they mirror.
+    __device__ __forceinline__ void put_symmetric(const float (&v)[32]) {
+      put(v, PLANES == 2);
+      if (PLANES == 1 && mirrored(at)) put_mirrored(v, 1, false);
+      hand_over();
+      if (PLANES == 2 && mirrored(at)) {
+        wait_staged();
+        put_mirrored(v, 0, false);
+        put_mirrored(v, 1, true);
+        hand_over();
+      }
+    }
+
+    __device__ __forceinline__ void columns(float (&v)[32], int c) {
+      const int j = j0 + c;
+      if (!live || j >= width_) return;
+      wait_staged();
+      if (at.product == 0) gram(v, j);
+      else if (at.product == 1) poly(v, j, c);
+      else apply(v, j);
+    }
+
+    __device__ __forceinline__ void gram(float (&v)[32], int j) {
+      const float s = kNsScaleE / (M.sx * M.sx);         // (powers of two)
+#pragma unroll
+      for (int k = 0; k < 32; ++k) v[k] *= s;
+      if (at.ti == at.tj) {
+        const int k0 = i - j;
+        float diagonal = 0.f;
+#pragma unroll
+        for (int k = 0; k < 32; ++k) {
+          diagonal = k == k0 ? v[k] : diagonal;
+          v[k] = k == k0 ? 0.f : v[k];
+        }
+        if (k0 >= 0 && k0 < 32 && i < M.m) M.d[i] = diagonal * (1.f / kNsScaleE);
+      }
+      put_symmetric(v);
+    }
+
+    __device__ __forceinline__ void poly(float (&v)[32], int j, int c) {
+      constexpr float kInvE = 1.f / kNsScaleE;
+      const float di = w.vectors[(w.row & 127) + w.lane];
+      const float* d = w.vectors + 128 + c;
+      const int k0 = at.ti == at.tj ? i - j : -1;
+      float diagonal = 0.f;
+#pragma unroll
+      for (int k = 0; k < 32; k += 8) {
+        const uint4 h4 = *piece(0, k >> 3);
+        uint4 l4 = make_uint4(0, 0, 0, 0);
+        if constexpr (PLANES == 2) l4 = *piece(1, k >> 3);
+        const float4 d0 = *reinterpret_cast<const float4*>(d + k), d1 = *reinterpret_cast<const float4*>(d + k + 4);
+        const float dj[8] = {d0.x, d0.y, d0.z, d0.w, d1.x, d1.y, d1.z, d1.w};
+        const unsigned int h[4] = {h4.x, h4.y, h4.z, h4.w}, l[4] = {l4.x, l4.y, l4.z, l4.w};
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const float2 h2 = ns_widen(h[q >> 1]), l2 = ns_widen(l[q >> 1]);
+          float e = q & 1 ? h2.y : h2.x;
+          if constexpr (PLANES == 2) e += q & 1 ? l2.y : l2.x;
+          // (b e + c (sum + (d_i + d_j) e)) 2^13 for e and sum scaled by 2^14 and 2^28
+          const float sum = v[k + q];
+          diagonal = k + q == k0 ? sum : diagonal;
+          const float g = fmaf(kNsC * kNsScaleF * kInvE, di + dj[q], kNsB * kNsScaleF * kInvE);
+          v[k + q] = k + q == k0 ? 0.f : fmaf(g, e, sum * (kNsC * kNsScaleF * kInvE * kInvE));
+        }
+      }
+      if (k0 >= 0 && k0 < 32 && i < M.m) M.fd[i] = fmaf(kNsC, fmaf(di, di, diagonal * (kInvE * kInvE)), kNsB * di);
+      if (mirrored(at)) __syncwarp();                    // all have read the slot before others' columns are written there
+      put_symmetric(v);
+    }
+
+    __device__ __forceinline__ void apply(float (&v)[32], int j) {
+      constexpr float kInvF = 1.f / kNsScaleF;
+      const float t = kNsA + w.vectors[(w.row & 127) + w.lane];
+#pragma unroll
+      for (int k = 0; k < 32; k += 8) {
+        const uint4 h4 = *piece(0, k >> 3), l4 = *piece(1, k >> 3);
+        const unsigned int h[4] = {h4.x, h4.y, h4.z, h4.w}, l[4] = {l4.x, l4.y, l4.z, l4.w};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float2 h2 = ns_widen(h[q]), l2 = ns_widen(l[q]);
+          v[k + 2 * q] = fmaf(t, h2.x + l2.x, v[k + 2 * q] * kInvF);
+          v[k + 2 * q + 1] = fmaf(t, h2.y + l2.y, v[k + 2 * q + 1] * kInvF);
+        }
+      }
+      if (!last) {
+        put(v, true);                                    // (a lane overwrites what it has read itself)
+        hand_over();
+        return;
+      }
+      hand_over();
+      if (i < M.m) result(v, j);
+    }
+
+    // O: along a row of dst, or down a column, where the warp's lanes are neighbours.
+    __device__ __forceinline__ void result(float (&v)[32], int j) {
+      const float s = 1.f / M.sx;
+      const int count = min(32, M.n - j);
+#pragma unroll
+      for (int k = 0; k < 32; ++k) v[k] *= s;
+      const long long step = M.flip ? M.ld_dst : 1;
+      const size_t at0 = M.flip ? (size_t)j * (size_t)M.ld_dst + (size_t)i : (size_t)i * (size_t)M.ld_dst + (size_t)j;
+      if (M.out == kNsOutBf16) {
+        __nv_bfloat16* p = static_cast<__nv_bfloat16*>(M.dst) + at0;
+        if (M.wide && count >= 32) {
+          unsigned int u[16];
+#pragma unroll
+          for (int k = 0; k < 16; ++k) u[k] = mm_bf16x2(v[2 * k], v[2 * k + 1]);
+          store_sector(p, u);
+          store_sector(p + 16, u + 8);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 32; ++k)
+            if (k < count) p[k * step] = __float2bfloat16_rn(v[k]);
+        }
+        return;
+      }
+      float* p = static_cast<float*>(M.dst) + at0;
+      const bool update = M.out == kNsOutUpdate;
+      const float decay = M.decay, rate = M.step;
+      if (M.wide && count >= 32) {
+        if (update) {
+#pragma unroll
+          for (int k = 0; k < 32; k += 4) {
+            const float4 q = *reinterpret_cast<const float4*>(p + k);
+            v[k] = q.x * decay - rate * v[k];
+            v[k + 1] = q.y * decay - rate * v[k + 1];
+            v[k + 2] = q.z * decay - rate * v[k + 2];
+            v[k + 3] = q.w * decay - rate * v[k + 3];
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < 32; k += 8) store_sector(p + k, reinterpret_cast<const unsigned int*>(v) + k);
+      } else if (update) {
+#pragma unroll
+        for (int k = 0; k < 32; ++k)
+          if (k < count) p[k * step] = p[k * step] * decay - rate * v[k];
+      } else {
+#pragma unroll
+        for (int k = 0; k < 32; ++k)
+          if (k < count) p[k * step] = v[k];
+      }
+    }
+
+    __device__ __forceinline__ void end() {}
+  };
+};
+
+// ---- before the products: the norm, and X in its working form ---------------------------------------------
+
+constexpr int kNsThreads = 256;
+constexpr int kNsUnitRows = 64, kNsUnitCols = 256;       // of the source
+
+__device__ __forceinline__ float ns_source(const NsMat& M, size_t at) {
+  return M.src_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(M.src)[at]) : static_cast<const float*>(M.src)[at];
+}
+
+__device__ __forceinline__ double ns_block_sum(double v) {
+  __shared__ double red[kNsThreads / 32];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_down_sync(0xffffffffu, v, o);
+  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
+  __syncthreads();
+  v = red[0];
+#pragma unroll
+  for (int w = 1; w < kNsThreads / 32; ++w) v += red[w];
+  return v;
+}
+
+// One unit's sum of squares, in binary64.
+__global__ void __launch_bounds__(kNsThreads)
+ps_ortho_norm_kernel(const NsMat* __restrict__ mats, const int2* __restrict__ units) {
+  mm_pdl();
+  const int2 u = units[blockIdx.x];                      // matrix, unit within it
+  const NsMat& M = mats[u.x];
+  const int rows = M.flip ? M.n : M.m, cols = M.flip ? M.m : M.n;
+  const int across = (cols + kNsUnitCols - 1) / kNsUnitCols;
+  const int r0 = u.y / across * kNsUnitRows, c = u.y % across * kNsUnitCols + (int)threadIdx.x;
+  double s = 0.0;
+  if (c < cols) {
+    const int end = min(rows, r0 + kNsUnitRows);
+#pragma unroll 8
+    for (int r = r0; r < end; ++r) {
+      const double x = (double)ns_source(M, (size_t)r * (size_t)M.ld_src + (size_t)c);
+      s += x * x;
+    }
+  }
+  s = ns_block_sum(s);
+  if (threadIdx.x == 0) M.parts[u.y] = s;
+}
+
+// One unit of X, scaled, as two planes.
+__global__ void __launch_bounds__(kNsThreads)
+ps_ortho_prepare_kernel(const NsMat* __restrict__ mats, const int2* __restrict__ units) {
+  __shared__ float tile[64][65];
+  mm_pdl();
+  const int2 u = units[blockIdx.x];
+  const NsMat& M = mats[u.x];
+  double total = 0.0;
+  for (int k = (int)threadIdx.x; k < M.nparts; k += kNsThreads) total += M.parts[k];
+  total = ns_block_sum(total);
+  const float scale = (float)((double)M.sx / (sqrt(total) + kNsEps));
+  if (u.y == 0 && threadIdx.x == 0) *M.done = 0;
+  const int rows = M.flip ? M.n : M.m, cols = M.flip ? M.m : M.n;
+  const int across = (cols + kNsUnitCols - 1) / kNsUnitCols;
+  const int r0 = u.y / across * kNsUnitRows, c0 = u.y % across * kNsUnitCols;
+  if (!M.flip) {
+    const int c = c0 + (int)threadIdx.x;
+    if (c >= cols) return;
+    const int end = min(rows, r0 + kNsUnitRows);
+#pragma unroll 8
+    for (int r = r0; r < end; ++r) {
+      __half hi, lo;
+      ns_split(ns_source(M, (size_t)r * (size_t)M.ld_src + (size_t)c) * scale, hi, lo);
+      const size_t o = (size_t)r * (size_t)M.pitch_x + (size_t)c;
+      M.x[0][0][o] = hi;
+      M.x[0][1][o] = lo;
+    }
+    return;
+  }
+  const int x = (int)threadIdx.x & 63, y = (int)threadIdx.x >> 6;
+  for (int part = 0; part < kNsUnitCols; part += 64) {
+    if (c0 + part >= cols) break;                        // (the same for the whole CTA)
+    __syncthreads();
+#pragma unroll 4
+    for (int r = y; r < 64; r += kNsThreads / 64)
+      if (r0 + r < rows && c0 + part + x < cols) tile[r][x] = ns_source(M, (size_t)(r0 + r) * (size_t)M.ld_src + (size_t)(c0 + part + x));
+    __syncthreads();
+#pragma unroll 4
+    for (int r = y; r < 64; r += kNsThreads / 64) {
+      if (c0 + part + r < cols && r0 + x < rows) {
+        __half hi, lo;
+        ns_split(tile[x][r] * scale, hi, lo);
+        const size_t o = (size_t)(c0 + part + r) * (size_t)M.pitch_x + (size_t)(r0 + x);
+        M.x[0][0][o] = hi;
+        M.x[0][1][o] = lo;
+      }
+    }
+  }
+}
+
+}  // namespace psb

@@ -1,0 +1,47 @@
+// Orthogonalisation of a list of matrices, as the list's handle (ps_ortho.cu) and the service (ps_service.cu) use it.
+#pragma once
+
+#include <cuda_runtime.h>
+
+#include <vector>
+
+#include "ps_op.h"
+
+namespace psb {
+
+struct NsItem {                          // one matrix, rows x cols with strides in elements
+  long long rows = 0, cols = 0;
+  const void* src = nullptr;
+  long long ld_src = 0;
+  bool src_bf16 = false;
+  void* dst = nullptr;
+  long long ld_dst = 0;
+  int out = 0;                           // kNsOut*
+  float decay = 1.f, step = 1.f;         // kNsOutUpdate: dst = dst * decay - step * O
+  double* parts = nullptr;               // partial sums of src's squares that are there already; nullptr: computed here
+  int nparts = 0;
+};
+
+// The device tables of one list.  The workspace is its owner's; runs that share one must not overlap on the GPU.
+class NsPlan {
+ public:
+  ~NsPlan();
+  NsPlan() = default;
+  NsPlan(const NsPlan&) = delete;
+  NsPlan& operator=(const NsPlan&) = delete;
+
+  // Bytes of workspace that a list needs; split: three products of halves (binary32 results).  0: too large a list.
+  static size_t workspace(const std::vector<NsItem>& items, bool split);
+  // Makes the tables for the current device and waits until they are there.  Throws std::bad_alloc only.
+  int build(const std::vector<NsItem>& items, bool split, void* workspace);
+  int run(cudaStream_t stream, int* launches = nullptr) const;
+  int status(int* out) const;            // waits for the device
+
+ private:
+  unsigned char* mem_ = nullptr;
+  size_t mats_off_ = 0, list_off_ = 0, units_off_ = 0, status_off_ = 0;
+  int tiles_ = 0, units_ = 0, grid_ = 0;
+  bool split_ = false, pair_ = false, norms_ = false;
+};
+
+}  // namespace psb

@@ -29,7 +29,7 @@ int xent_device(const OpDevice& d, int** status) {
     void* p = nullptr;
     cudaError_t e = cudaGetSymbolAddress(&p, g_xent_status);
     if (e == cudaSuccess)
-      e = cudaFuncSetAttribute(ps_tc_kernel<XeOp>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcCfg<XeOp::kPlanes>::kSmem);
+      e = cudaFuncSetAttribute(ps_tc_kernel<XeOp>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcCfg<XeOp>::kSmem);
     if (e != cudaSuccess) return op_cuda_error("preparing the cross entropy", e);
     x.status = static_cast<int*>(p);
     x.ready = true;
@@ -60,12 +60,12 @@ XePlan xent_plan(long long T, long long V, long long D) {
   XePlan p;
   p.nparts = ceil_div(V, 128);
   p.pitch = ceil_div(D, 8) * 8;
-  const long long all = ceil_div(V, kTcTile) * kTcTile;
-  p.piece = std::min(all, std::max<long long>(1, kXePieceEntries / std::max(1ll, T) / kTcTile) * kTcTile);
+  const long long all = ceil_div(V, kXeTile) * kXeTile;
+  p.piece = std::min(all, std::max<long long>(1, kXePieceEntries / std::max(1ll, T) / kXeTile) * kXeTile);
   p.pieces = ceil_div(V, p.piece);
   // dx has few tiles, each as long as the piece has words: its words are shared out to slices until one is no longer
   // than half of what a pair computes in a launch
-  const long long tm = ceil_div(T, kTcTile), td = ceil_div(D, kTcTile), tv = p.piece / kTcTile, nk = p.piece / kTcK;
+  const long long tm = ceil_div(T, kXeTile), td = ceil_div(D, kXeTile), tv = p.piece / kXeTile, nk = p.piece / kTcK;
   const long long total = tm * tv * ceil_div(D, kTcK) + tm * td * nk + tv * td * ceil_div(T, kTcK);
   const long long longest = std::max<long long>(kXeMinStages, total / kXePairs / 2);
   const long long most = std::min<long long>(kXeMaxSlices, std::max(1ll, kXeSliceRows / std::max(1ll, T)));
@@ -93,10 +93,10 @@ XePlan xent_plan(long long T, long long V, long long D) {
 
 // What any call of at most T tokens needs (a smaller batch is cut into larger pieces and more slices).
 size_t xent_bytes(long long T, long long V, long long D, bool unaligned) {
-  const size_t pitch = (size_t)ceil_div(D, 8) * 8, all = (size_t)ceil_div(V, kTcTile) * kTcTile, t = (size_t)T;
+  const size_t pitch = (size_t)ceil_div(D, 8) * 8, all = (size_t)ceil_div(V, kXeTile) * kXeTile, t = (size_t)T;
   const size_t x = round256(t * pitch * 2), w = unaligned ? round256((size_t)V * pitch * 2) : 0;
   const size_t parts = round256(t * (size_t)ceil_div(V, 128) * sizeof(float2)) + round256(t * sizeof(float));
-  const size_t piece = std::max(std::min(t * all, (size_t)kXePieceEntries), t * kTcTile);
+  const size_t piece = std::max(std::min(t * all, (size_t)kXePieceEntries), t * kXeTile);
   const size_t rows = std::max(t, std::min(t * kXeMaxSlices, (size_t)kXeSliceRows));
   return std::max<size_t>(256, x + w + std::max(parts, 2 * round256(piece * 2) + round256(rows * (size_t)D * sizeof(float))));
 }
@@ -129,8 +129,8 @@ int check(const ps_xent* q, XePlan* plan, bool* copy_w) {
   if (!q->w || !q->workspace || (q->tokens > 0 && (!q->x || !q->targets))) return PS_ERR_BAD_ARG;
   if (misaligned(q->x, 2) || misaligned(q->w, 2) || misaligned(q->targets, q->target_bits / 8) || misaligned(q->workspace, 256))
     return PS_ERR_ALIGN;
-  if (ceil_div(q->tokens, kTcTile) * ceil_div(q->vocab, kTcTile) > 0x3fffffffll ||
-      ceil_div(q->vocab, kTcTile) * ceil_div(q->dim, kTcTile) > 0x3fffffffll)
+  if (ceil_div(q->tokens, kXeTile) * ceil_div(q->vocab, kXeTile) > 0x3fffffffll ||
+      ceil_div(q->vocab, kXeTile) * ceil_div(q->dim, kXeTile) > 0x3fffffffll)
     return PS_ERR_TOO_LARGE;
   *plan = xent_plan(q->tokens, q->vocab, q->dim);
   *copy_w = !rows_aligned(q->w, q->ldw);
@@ -194,7 +194,7 @@ int launch_segments(XeCall* c) {
   if (tiles > 0x3fffffffll) return PS_ERR_TOO_LARGE;
   a.tiles = (int)tiles;
   const unsigned grid = 2u * (unsigned)std::min<long long>(tiles, c->dev.num_sms / 2);
-  return op_launch("cross entropy", ps_tc_kernel<XeOp>, grid, kTcThreads, TcCfg<XeOp::kPlanes>::kSmem, 1, c->stream, a);
+  return op_launch("cross entropy", ps_tc_kernel<XeOp>, grid, kTcThreads, TcCfg<XeOp>::kSmem, 1, c->stream, a);
 }
 
 }  // namespace
@@ -225,7 +225,7 @@ int ps_xent_forward(const ps_xent* q, float* loss, float* lse, void* stream) {
   a.nparts = (int)c.plan.nparts;
   a.score = reinterpret_cast<float*>(c.ws + c.plan.score);
   a.nseg = 1;
-  a.seg[0] = XeSeg{kXeStats, 0, (int)ceil_div(a.T, kTcTile), (int)ceil_div(a.V, kTcTile), 0, (int)ceil_div(a.D, kTcK), 1, 0, 0, 0};
+  a.seg[0] = XeSeg{kXeStats, 0, (int)ceil_div(a.T, kXeTile), (int)ceil_div(a.V, kXeTile), 0, (int)ceil_div(a.D, kTcK), 1, 0, 0, 0};
   rc = launch_segments(&c);
   if (rc) return rc;
   return op_launch("cross entropy", ps_xent_join_kernel, (unsigned)ceil_div(a.T, kXeJoinThreads / 32), kXeJoinThreads, 0, 1,
@@ -265,13 +265,13 @@ int ps_xent_backward(const ps_xent* q, const float* lse, float scale, const floa
   a.dw_f32 = dw_dtype == PS_F32;
   a.dx_wide = !misaligned(dx, 32) && lddx * 2 % 32 == 0;
   a.dw_wide = !misaligned(dw, 32) && lddw * (long long)es % 32 == 0;
-  const int tm = (int)ceil_div(a.T, kTcTile), td = (int)ceil_div(a.D, kTcTile);
+  const int tm = (int)ceil_div(a.T, kXeTile), td = (int)ceil_div(a.D, kXeTile);
   int filled = 0;                        // slices of dx's sums that hold something
   for (long long k = 0; k <= p.pieces; ++k) {
     a.nseg = 0;
     if (k < p.pieces) {
       const long long v0 = k * p.piece, words = std::min(p.piece, a.V - v0);
-      a.seg[a.nseg++] = XeSeg{kXeProb, 0, tm, (int)ceil_div(words, kTcTile), (int)v0, (int)ceil_div(a.D, kTcK), 1, (int)(k & 1), 0, 0};
+      a.seg[a.nseg++] = XeSeg{kXeProb, 0, tm, (int)ceil_div(words, kXeTile), (int)v0, (int)ceil_div(a.D, kTcK), 1, (int)(k & 1), 0, 0};
     }
     if (k > 0) {
       const long long v0 = (k - 1) * p.piece, words = std::min(p.piece, a.V - v0);
@@ -281,7 +281,7 @@ int ps_xent_backward(const ps_xent* q, const float* lse, float scale, const floa
         a.seg[a.nseg++] = XeSeg{kXeDx, 0, tm, td, (int)v0, nk, slices, buf, k == 1, k == p.pieces && p.slices == 1};
         filled = std::max(filled, slices);
       }
-      if (dw) a.seg[a.nseg++] = XeSeg{kXeDw, 0, (int)ceil_div(words, kTcTile), td, (int)v0, (int)ceil_div(a.T, kTcK), 1, buf, 0, 0};
+      if (dw) a.seg[a.nseg++] = XeSeg{kXeDw, 0, (int)ceil_div(words, kXeTile), td, (int)v0, (int)ceil_div(a.T, kTcK), 1, buf, 0, 0};
     }
     rc = launch_segments(&c);
     if (rc) return rc;

@@ -18,6 +18,8 @@
 
 namespace psb {
 
+constexpr int kXeTile = 256;
+
 enum { kXeStats = 0, kXeProb = 1, kXeDx = 2, kXeDw = 3 };
 
 struct XeSeg {                           // a launch's tiles of one kind, tiles_m x tiles_n (x slices)
@@ -94,10 +96,12 @@ __device__ __forceinline__ void xe_store_f32(float* o, const float* v, int live,
 }
 
 struct XeOp {
-  static constexpr int kPlanes = 1, kType = 1;
+  static constexpr bool kPair = true;
+  static constexpr int kPlanes = 1, kType = 1, kStages = 6, kSlots = 0, kSegment = 0;
   using Args = XeArgs;
 
   struct At { const XeSeg* seg; int m, n, slice; };
+  using Item = int;
 
   static __device__ __forceinline__ At locate(const XeArgs& a, int index) {
     At at;
@@ -118,14 +122,15 @@ struct XeOp {
   }
 
   static __device__ __forceinline__ int tiles(const XeArgs& a) { return a.tiles; }
+  static __device__ __forceinline__ Item item(const XeArgs&, int index, int) { return index; }
 
   static __device__ __forceinline__ void tile(const XeArgs& a, int index, TcTile* t) {
     const At at = locate(a, index);
     const XeSeg& s = *at.seg;
     t->ready = nullptr;
     t->need = 0;
-    t->a_row = at.m * kTcTile;
-    t->b_row = at.n * kTcTile;
+    t->a_row = at.m * kXeTile;
+    t->b_row = at.n * kXeTile;
     t->a_k = t->b_k = 0;
     t->nk = s.nk;
     t->a_mn = t->b_mn = 0;
@@ -150,18 +155,18 @@ struct XeOp {
 
   struct Epilogue {
     const XeArgs& a;
+    const TcWarp& w;
     const At at;
     long long row, word;                 // this lane's row; the target (kXeStats, kXeProb: relative to the tile's first column)
     float m, s, g;
-    int col0;
     bool counts;                         // the row's token has a target
 
-    __device__ __forceinline__ Epilogue(const XeArgs& args, int index) : a(args), at(locate(args, index)) {}
+    __device__ __forceinline__ Epilogue(const XeArgs& args, int index, const TcWarp& warp, MmCursor<1>&)
+        : a(args), w(warp), at(locate(args, index)) {}
 
-    __device__ __forceinline__ void begin(int r, int c, int) {
+    __device__ __forceinline__ void begin() {
       const int kind = at.seg->kind;
-      row = (long long)at.m * kTcTile + r;
-      col0 = c;
+      row = (long long)at.m * kXeTile + w.row + w.lane;
       if (kind <= kXeProb) {
         word = -1;
         m = __int_as_float(0xff800000);
@@ -170,7 +175,7 @@ struct XeOp {
         if (row < a.T) {
           const long long v = xe_target(a.targets, a.target64, row);
           counts = v >= 0 && v < a.V;
-          if (counts) word = v - (at.seg->v0 + (long long)at.n * kTcTile);
+          if (counts) word = v - (at.seg->v0 + (long long)at.n * kXeTile);
           if (kind == kXeProb && counts) {
             m = a.lse[row];
             g = a.weights ? a.scale * a.weights[row] : a.scale;
@@ -180,6 +185,7 @@ struct XeOp {
     }
 
     __device__ __forceinline__ void columns(float (&v)[32], int c) {
+      c += w.col;
       switch (at.seg->kind) {
         case kXeStats: stats(v, c); break;
         case kXeProb: prob(v, c); break;
@@ -189,7 +195,7 @@ struct XeOp {
     }
 
     __device__ __forceinline__ void stats(float (&v)[32], int c) {
-      const long long left = a.V - ((long long)at.n * kTcTile + c);
+      const long long left = a.V - ((long long)at.n * kXeTile + c);
       if (left < 32) {
 #pragma unroll
         for (int i = 0; i < 32; ++i)
@@ -197,9 +203,10 @@ struct XeOp {
       }
       const long long in = word - c;
       if (in >= 0 && in < 32) {
+        float score = 0.f;
 #pragma unroll
-        for (int i = 0; i < 32; ++i)
-          if (i == (int)in) a.score[row] = v[i];
+        for (int i = 0; i < 32; ++i) score = i == (int)in ? v[i] : score;
+        a.score[row] = score;
       }
       float t[8];
 #pragma unroll
@@ -222,7 +229,7 @@ struct XeOp {
     }
 
     __device__ __forceinline__ void prob(float (&v)[32], int c) {
-      const long long v0 = (long long)at.n * kTcTile + c;             // column in the piece
+      const long long v0 = (long long)at.n * kXeTile + c;             // column in the piece
       if (row >= a.T) return;
 #pragma unroll
       for (int i = 0; i < 32; ++i) v[i] = g * xe_exp2((v[i] - m) * kLog2e);
@@ -230,7 +237,7 @@ struct XeOp {
       if (in >= 0 && in < 32) {
 #pragma unroll
         for (int i = 0; i < 32; ++i)
-          if (i == (int)in) v[i] -= g;
+          v[i] -= i == (int)in ? g : 0.f;
       }
       // zeros past the vocabulary, and in the rows of ignored tokens whatever x holds there
       const long long live = counts ? a.V - (at.seg->v0 + v0) : 0;
@@ -243,7 +250,7 @@ struct XeOp {
     }
 
     __device__ __forceinline__ void dx(float (&v)[32], int c) {
-      const long long col = (long long)at.n * kTcTile + c;
+      const long long col = (long long)at.n * kXeTile + c;
       const int live = (int)min(32ll, a.D - col);
       if (row >= a.T || live <= 0) return;
       float* sums = a.dx_sums + ((size_t)at.slice * (size_t)a.T + (size_t)row) * (size_t)a.D + (size_t)col;
@@ -269,7 +276,7 @@ struct XeOp {
     }
 
     __device__ __forceinline__ void dw(float (&v)[32], int c) {
-      const long long col = (long long)at.n * kTcTile + c, out = at.seg->v0 + row;
+      const long long col = (long long)at.n * kXeTile + c, out = at.seg->v0 + row;
       const int live = (int)min(32ll, a.D - col);
       if (out >= a.V || live <= 0) return;
       const size_t o = (size_t)out * (size_t)a.ld_dw + (size_t)col;
@@ -277,9 +284,9 @@ struct XeOp {
       else xe_store_bf16(static_cast<__nv_bfloat16*>(a.dw) + o, v, live, a.dw_wide != 0);
     }
 
-    __device__ __forceinline__ void end(int) {
+    __device__ __forceinline__ void end() {
       if (at.seg->kind == kXeStats && row < a.T) {
-        const long long part = (long long)at.n * 2 + (col0 >> 7);
+        const long long part = (long long)at.n * 2 + (w.col >> 7);
         if (part < a.nparts) a.parts[(size_t)row * (size_t)a.nparts + (size_t)part] = make_float2(m, s);
       }
     }
