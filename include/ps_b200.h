@@ -33,6 +33,11 @@
  * Every operation is one IEEE-754 binary32 round-to-nearest operation with no
  * fused multiply-add; bf16 gradients are widened exactly.  The per-block
  * statistic is sum_i G*G in binary64.
+ *     MUON: v' = mom * v[i] + G;  u = G + mom * v';  O = u orthogonalised (see
+ *           ps_ortho below; the block is a matrix, ps_register_matrix)
+ *           p' = p[i] * (1 - lr*wd) - lr * update_scale * O[i]
+ * The products inside O are the tensor cores', of operands of 22 bits: O agrees with
+ * binary32 arithmetic to its rounding, not bit for bit, and is the same every time.
  */
 #ifndef PS_B200_H
 #define PS_B200_H
@@ -45,7 +50,7 @@ extern "C" {
 
 typedef struct ps_service ps_service; /* opaque */
 
-typedef enum { PS_SGD = 0, PS_ADAM = 1 } ps_opt;
+typedef enum { PS_SGD = 0, PS_ADAM = 1, PS_MUON = 2 } ps_opt;
 typedef enum { PS_F32 = 0, PS_BF16 = 1 } ps_dtype; /* gradient type; parameters and state are fp32 */
 
 typedef enum {
@@ -161,9 +166,29 @@ int ps_register_job(ps_service* svc, const ps_job_desc* desc, int* job_out);
  * paper's Appendix A.  `init_params_or_null` may be a host or a device pointer
  * to nelem floats (copied before return) or NULL (zeros).  Optimizer state
  * starts at zero and the step counter at 0.  Synchronous.
- * Errors: BAD_ARG, DUPLICATE, NOMEM, CUDA. */
+ * Errors: BAD_ARG (also for a PS_MUON job: ps_register_matrix), DUPLICATE, NOMEM, CUDA. */
 int ps_register_block(ps_service* svc, int job, int block, size_t nelem, int ctx,
                       const float* init_params_or_null);
+
+/* Registers block `block` of a PS_MUON job, a matrix of rows x cols parameters, row after
+ * row (every block of such a job is one; vectors and embeddings belong to a job with another
+ * optimizer).  update_scale multiplies lr for this block: 0.2 * sqrt(max(rows, cols))
+ * gives the update the size of Adam's, sqrt(max(1, rows / cols)) is the other common choice.
+ * Of the job's description lr, momentum, weight_decay (decoupled), grad_scale and the gradients'
+ * type and workers apply.  Otherwise as ps_register_block, whose pushes, pulls, migration,
+ * export and statistics apply unchanged; not for these blocks are ps_push_rows,
+ * ps_aggregate_clipped and ps_aggregate_block_noalloc (BAD_ARG).
+ * The aggregates of PS_MUON blocks run on the caller's stream itself, also with
+ * PS_OPT_OVERLAP, and are not held back; they are ordered after one another.  A list with
+ * blocks of such jobs and of others goes out as two launches.  The first aggregate of a set of
+ * blocks that are aggregated together makes its tables and, if it needs more than any before, the
+ * workspace (about 12 bytes per element and 16 for the square of each matrix's smaller side), and
+ * waits for the device; the tables of the last 64 sets are kept.  ps_block_profile covers the sum
+ * of the shards, not the orthogonalisation.
+ * Errors: those of ps_register_block; BAD_ARG (not a PS_MUON job, rows or cols below 1 or above
+ * 2^20, update_scale not finite), TOO_LARGE. */
+int ps_register_matrix(ps_service* svc, int job, int block, long long rows, long long cols, int ctx,
+                       const float* init_params_or_null, float update_scale);
 
 /* Push (paper Section 4, Appendix A): records worker `worker`'s gradient shard
  * for (job, block).  Zero-copy: `grad_dev_ptr` is a device pointer to nelem
@@ -427,7 +452,7 @@ int ps_launch_info(ps_service* svc, unsigned long long* launches_out, int* grid_
 
 /* Launch accounting per kernel variant (0 = persistent direct-load kernel,
  * 1 = small-launch kernel with the table in its parameters, 2 = bulk-copy ring,
- * 3 = clipped aggregates):
+ * 3 = clipped aggregates, 4 = aggregates of PS_MUON blocks, counted once each):
  * launches so far, the algorithmic bytes they covered (W shards read, parameters
  * and state read and written, dense semantics) and the kernel's name.
  * Errors: BAD_ARG (variant out of range). */
@@ -773,7 +798,8 @@ int ps_ortho_destroy(ps_ortho* o);
  *     dx[t] = sum_v e[t][v] * w[v],  dw[v] = sum_t e[t][v] * x[t]
  * x and w are bf16.  A token whose target lies outside [0, vocab) (-100, say) is ignored:
  * its loss, lse and row of dx are zeros, and nothing of its row of x reaches dw, NaN
- * included.  e is rounded to bf16, the sums over it are binary32.  A score that is a NaN or
+ * included.  exp(s - lse) - [...] is rounded to bf16, the sums over it are binary32; token_scale
+ * is applied to dx's sums, and for dw to x, rounded to bf16.  A score that is a NaN or
  * +infinity makes its token's loss and gradients NaN.
  * The calls run on `stream` of the CURRENT device, allocate nothing and wait for nothing.
  * ------------------------------------------------------------------------- */
@@ -789,9 +815,9 @@ typedef struct {
   size_t workspace_bytes;
 } ps_xent;
 
-/* Bytes of workspace that calls of at most `tokens` tokens need: where w's rows start on 16-byte boundaries (w
- * 16-byte aligned, ldw a multiple of eight), and where they do not (w is then copied first).
- * Errors: BAD_ARG. */
+/* Bytes of workspace that calls of at most `tokens` tokens need: where the rows of x and w start
+ * on 16-byte boundaries (base 16-byte aligned, stride a multiple of eight), and where either's do
+ * not (they are then copied first).  Errors: BAD_ARG. */
 int ps_xent_sizes(long long tokens, long long vocab, long long dim, size_t* bytes_out, size_t* bytes_unaligned_out);
 
 /* One float per token into loss and lse (device; either may be NULL).  No tokens: a no-op.

@@ -16,7 +16,7 @@ import os
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libps_b200.so")
 
-PS_SGD, PS_ADAM = 0, 1
+PS_SGD, PS_ADAM, PS_MUON = 0, 1, 2
 PS_F32, PS_BF16 = 0, 1
 PS_OK = 0
 PS_ERR_BAD_HANDLE, PS_ERR_BAD_ARG, PS_ERR_DUPLICATE, PS_ERR_NOT_READY = -1, -2, -3, -4
@@ -80,6 +80,8 @@ _SIGNATURES = {
     "ps_destroy": (C.c_int, [C.c_void_p]),
     "ps_register_job": (C.c_int, [C.c_void_p, C.POINTER(ps_job_desc), C.POINTER(C.c_int)]),
     "ps_register_block": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_size_t, C.c_int, C.c_void_p]),
+    "ps_register_matrix": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_longlong, C.c_longlong, C.c_int, C.c_void_p,
+                                     C.c_float]),
     "ps_push": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p]),
     "ps_push_rows": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int, C.c_int, C.c_void_p]),
     "ps_push_rows_batch": (C.c_int, [C.c_void_p, C.c_int] + [C.c_void_p] * 7),
@@ -302,6 +304,15 @@ def ps_register_block(svc, job: int, block: int, nelem: int, ctx: int = 0, init_
     _check(load().ps_register_block(svc, job, block, nelem, ctx, _ptr(init_params)), "ps_register_block", svc)
 
 
+def ps_register_matrix(svc, job: int, block: int, rows: int, cols: int, ctx: int = 0, init_params=None,
+                       update_scale: float | None = None):
+    """A block of a PS_MUON job.  update_scale: default 0.2 * sqrt(max(rows, cols))."""
+    if update_scale is None:
+        update_scale = 0.2 * max(rows, cols, 0) ** 0.5
+    _check(load().ps_register_matrix(svc, job, block, rows, cols, ctx, _ptr(init_params), update_scale),
+           "ps_register_matrix", svc)
+
+
 def ps_push(svc, job: int, block: int, worker: int, grad):
     _check(load().ps_push(svc, job, block, worker, _ptr(grad)), "ps_push", svc)
 
@@ -405,7 +416,7 @@ def ps_round_run_clipped(svc, round_id: int, max_norm: float, norms_out=None, st
 
 
 def ps_launch_stats(svc, variants: int = 3):
-    """[{kernel, launches, bytes}] per kernel variant (the fourth: clipped aggregates)."""
+    """[{kernel, launches, bytes}] per kernel variant (the fourth: clipped aggregates, the fifth: PS_MUON)."""
     res = []
     for v in range(variants):
         n, b, name = C.c_ulonglong(), C.c_ulonglong(), C.c_char_p()
@@ -893,7 +904,7 @@ class Ortho:
 
 
 def ps_xent_sizes(tokens: int, vocab: int, dim: int):
-    """Bytes of workspace: (rows of the weight on 16-byte boundaries, rows that are not)."""
+    """Bytes of workspace: (rows of x and w on 16-byte boundaries, rows that are not)."""
     a, b = C.c_size_t(), C.c_size_t()
     _check_op(load().ps_xent_sizes(tokens, vocab, dim, C.byref(a), C.byref(b)), "ps_xent_sizes")
     return a.value, b.value
@@ -908,8 +919,8 @@ def ps_xent_status() -> int:
 class CrossEntropy:
     """Losses and gradients of up to `tokens` tokens over a vocabulary (ps_xent_*), with the workspace they need.
     x is tokens x dim and w vocab x dim (bfloat16, any row stride), targets int32 or int64; all tensors on this
-    object's device, which has to be the current one.  `aligned`: whether w's rows start on 16-byte boundaries
-    (default: whether rows of dim elements do).  Calls of one object must not overlap on the GPU."""
+    object's device, which has to be the current one.  `aligned`: whether x's and w's rows start on 16-byte
+    boundaries (default: whether rows of dim elements do).  Calls of one object must not overlap on the GPU."""
 
     def __init__(self, tokens: int, vocab: int, dim: int, device=None, aligned: bool | None = None):
         import torch
@@ -995,7 +1006,7 @@ def _bind(name):
     return method
 
 
-for _n in ("flush", "round", "round_prepare", "round_run", "round_release", "round_run_clipped", "aggregate_clipped", "launch_stats", "registry_info", "register_job", "register_block", "push", "push_rows", "push_rows_batch", "push_batch", "push_host", "push_host_batch", "aggregate", "join", "pull", "pull_batch", "pull_host",
+for _n in ("flush", "round", "round_prepare", "round_run", "round_release", "round_run_clipped", "aggregate_clipped", "launch_stats", "registry_info", "register_job", "register_block", "register_matrix", "push", "push_rows", "push_rows_batch", "push_batch", "push_host", "push_host_batch", "aggregate", "join", "pull", "pull_batch", "pull_host",
            "migrate_block", "migrate_blocks", "block_stats", "block_profile", "job_profile", "block_state", "plan", "set_option", "get_option", "arena_info",
            "launch_info", "device_status", "block_export", "block_import", "unregister_block", "arena_export", "block_location"):
     setattr(Service, _n, _bind(_n))

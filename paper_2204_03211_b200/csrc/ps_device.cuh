@@ -7,4 +7,5 @@
 #include "ps_kernel_inline.cuh"
 #include "ps_kernel_bulk.cuh"
 #include "ps_kernel_clip.cuh"
+#include "ps_kernel_muon.cuh"
 #include "ps_migrate.cuh"

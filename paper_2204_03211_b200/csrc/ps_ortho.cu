@@ -140,7 +140,7 @@ NsPlan::~NsPlan() {
   if (mem_) cudaFree(mem_);              // (waits for launches that still use it)
 }
 
-int NsPlan::build(const std::vector<NsItem>& items, bool split, void* workspace) {
+int NsPlan::build(const std::vector<NsItem>& items, bool split, void* workspace, int* status) {
   // Single CTAs with 128 x 128 where pairs would have few tiles.
   long long large = 0;
   for (const NsItem& it : items)
@@ -213,10 +213,6 @@ int NsPlan::build(const std::vector<NsItem>& items, bool split, void* workspace)
     M.wide = !M.flip && (reinterpret_cast<uintptr_t>(it.dst) & 31u) == 0 && it.ld_dst * (long long)es % 32 == 0;
     M.decay = it.decay;
     M.step = it.step;
-    // 2^kx: entries of X0 are about 1 / sqrt(m n)
-    int kx = (int)std::lround(0.5 * std::log2((double)l.m * (double)l.n));
-    kx = std::max(0, std::min(14, kx));
-    M.sx = std::ldexp(1.f, kx);
     const int tm = (int)ceil_div(l.m, tile), tn = (int)ceil_div(l.n, tile);
     for (int a = 0; a < tm; ++a) {
       const int ctas = pair_ && l.m - a * tile > 128 ? 2 : 1;
@@ -248,7 +244,7 @@ int NsPlan::build(const std::vector<NsItem>& items, bool split, void* workspace)
   list_off_ = take(list.size() * sizeof(NsTile));
   units_off_ = take(units.size() * sizeof(int2));
   const size_t done_off = take(n * sizeof(unsigned int) * 32);         // a line each
-  status_off_ = take(sizeof(int));
+  const size_t status_off = take(sizeof(int));
   void* mem = nullptr;
   cudaError_t e = cudaMalloc(&mem, off);
   if (e != cudaSuccess) return op_cuda_error("tables of the orthogonalisation", e);
@@ -264,9 +260,10 @@ int NsPlan::build(const std::vector<NsItem>& items, bool split, void* workspace)
   put(mats_off_, mats.data(), n * sizeof(NsMat));
   put(list_off_, list.data(), list.size() * sizeof(NsTile));
   put(units_off_, units.data(), units.size() * sizeof(int2));
-  if (e == cudaSuccess) e = cudaMemset(mem_ + done_off, 0, status_off_ + sizeof(int) - done_off);
+  if (e == cudaSuccess) e = cudaMemset(mem_ + done_off, 0, status_off + sizeof(int) - done_off);
   if (e == cudaSuccess) e = cudaStreamSynchronize(cudaStreamLegacy);   // before other streams use it
   if (e != cudaSuccess) return op_cuda_error("tables of the orthogonalisation", e);
+  status_ = status ? status : reinterpret_cast<int*>(mem_ + status_off);
   tiles_ = (int)list.size();
   units_ = (int)units.size();
   grid_ = (pair_ ? 2 : 1) * std::min(tiles_, room);
@@ -284,7 +281,7 @@ int NsPlan::run(cudaStream_t stream, int* launches) const {
   if (!rc) rc = op_launch("orthogonalisation", ps_ortho_prepare_kernel, (unsigned)units_, kNsThreads, 0, 1, stream, mats, units);
   if (rc) return rc;
   NsArgs a;
-  a.status = reinterpret_cast<int*>(mem_ + status_off_);
+  a.status = status_;
   a.mats = mats;
   a.list = reinterpret_cast<const NsTile*>(mem_ + list_off_);
   a.tiles = tiles_;
@@ -308,7 +305,7 @@ int NsPlan::run(cudaStream_t stream, int* launches) const {
 int NsPlan::status(int* out) const {
   *out = 0;
   cudaError_t e = cudaDeviceSynchronize();
-  if (e == cudaSuccess && mem_) e = cudaMemcpy(out, mem_ + status_off_, sizeof(int), cudaMemcpyDeviceToHost);
+  if (e == cudaSuccess && status_) e = cudaMemcpy(out, status_, sizeof(int), cudaMemcpyDeviceToHost);
   return e == cudaSuccess ? PS_OK : op_cuda_error("status of the orthogonalisation", e);
 }
 

@@ -18,12 +18,14 @@
 //  - Results in bf16 take one product, of the high halves: 5e-4 to 1e-3 of the result's norm (its own rounding is
 //    1.7e-3).  Results in binary32, and the service's update, also split E and F and take three (high x high, high x
 //    low, low x high): what is left is the rounding of the tensor cores' sums.
-// Scales: X by 2^kx (about sqrt(m n), at most 2^14: entries are at most 1.2), E by 2^14 (at most 1.5), F by 2^13 (at
-// most 2.9), so that nothing overflows fp16 and typical entries are far from its subnormal end.
+// Scales: X by 2^15 (singular values, and so entries, are at most 1.21), E by 2^15 (at most 1.47), F by 2^14 (at most
+// 2.9): the largest powers of two that overflow nothing, because small entries beside large ones lose bits at fp16's
+// subnormal end.
 #pragma once
 
 #include <cuda_fp16.h>
 
+#include "ps_ortho.h"
 #include "ps_tc.cuh"
 
 namespace psb {
@@ -31,11 +33,9 @@ namespace psb {
 constexpr int kNsSteps = 5;
 constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
 constexpr double kNsEps = 1e-7;
-constexpr float kNsScaleE = 16384.f, kNsScaleF = 8192.f;
+constexpr float kNsScaleX = 32768.f, kNsScaleE = 32768.f, kNsScaleF = 16384.f;
 
 constexpr int kNsMaps = 20, kNsTall = 8, kNsMirror = 16;
-
-enum { kNsOutF32 = 0, kNsOutBf16 = 1, kNsOutUpdate = 2 };
 
 struct NsMat {                           // one matrix, in its working orientation: m <= n
   int m, n;
@@ -57,7 +57,6 @@ struct NsMat {                           // one matrix, in its working orientati
   long long ld_dst;
   int wide;                              // rows of dst allow 256-bit accesses
   float decay, step;                     // kNsOutUpdate: dst = dst * decay - step * O
-  float sx;                              // 2^kx
   int parts_s, parts_x;                  // what `done` counts in a symmetric product and in the last one
   unsigned int* done;                    // CTAs' finished parts of tiles (those that have rows of the matrix)
 };
@@ -263,7 +262,7 @@ struct NsOp {
     }
 
     __device__ __forceinline__ void gram(float (&v)[32], int j) {
-      const float s = kNsScaleE / (M.sx * M.sx);         // (powers of two)
+      constexpr float s = kNsScaleE / (kNsScaleX * kNsScaleX);
 #pragma unroll
       for (int k = 0; k < 32; ++k) v[k] *= s;
       if (at.ti == at.tj) {
@@ -298,7 +297,7 @@ struct NsOp {
           const float2 h2 = ns_widen(h[q >> 1]), l2 = ns_widen(l[q >> 1]);
           float e = q & 1 ? h2.y : h2.x;
           if constexpr (PLANES == 2) e += q & 1 ? l2.y : l2.x;
-          // (b e + c (sum + (d_i + d_j) e)) 2^13 for e and sum scaled by 2^14 and 2^28
+          // (b e + c (sum + (d_i + d_j) e)) in F's scale, e and sum in E's and its square
           const float sum = v[k + q];
           diagonal = k + q == k0 ? sum : diagonal;
           const float g = fmaf(kNsC * kNsScaleF * kInvE, di + dj[q], kNsB * kNsScaleF * kInvE);
@@ -335,7 +334,7 @@ struct NsOp {
 
     // O: along a row of dst, or down a column, where the warp's lanes are neighbours.
     __device__ __forceinline__ void result(float (&v)[32], int j) {
-      const float s = 1.f / M.sx;
+      constexpr float s = 1.f / kNsScaleX;
       const int count = min(32, M.n - j);
 #pragma unroll
       for (int k = 0; k < 32; ++k) v[k] *= s;
@@ -440,7 +439,7 @@ ps_ortho_prepare_kernel(const NsMat* __restrict__ mats, const int2* __restrict__
   double total = 0.0;
   for (int k = (int)threadIdx.x; k < M.nparts; k += kNsThreads) total += M.parts[k];
   total = ns_block_sum(total);
-  const float scale = (float)((double)M.sx / (sqrt(total) + kNsEps));
+  const float scale = (float)((double)kNsScaleX / (sqrt(total) + kNsEps));
   if (u.y == 0 && threadIdx.x == 0) *M.done = 0;
   const int rows = M.flip ? M.n : M.m, cols = M.flip ? M.m : M.n;
   const int across = (cols + kNsUnitCols - 1) / kNsUnitCols;

@@ -9,6 +9,8 @@
 
 namespace psb {
 
+enum { kNsOutF32 = 0, kNsOutBf16 = 1, kNsOutUpdate = 2 };
+
 struct NsItem {                          // one matrix, rows x cols with strides in elements
   long long rows = 0, cols = 0;
   const void* src = nullptr;
@@ -16,7 +18,7 @@ struct NsItem {                          // one matrix, rows x cols with strides
   bool src_bf16 = false;
   void* dst = nullptr;
   long long ld_dst = 0;
-  int out = 0;                           // kNsOut*
+  int out = kNsOutF32;
   float decay = 1.f, step = 1.f;         // kNsOutUpdate: dst = dst * decay - step * O
   double* parts = nullptr;               // partial sums of src's squares that are there already; nullptr: computed here
   int nparts = 0;
@@ -32,14 +34,16 @@ class NsPlan {
 
   // Bytes of workspace that a list needs; split: three products of halves (binary32 results).  0: too large a list.
   static size_t workspace(const std::vector<NsItem>& items, bool split);
-  // Makes the tables for the current device and waits until they are there.  Throws std::bad_alloc only.
-  int build(const std::vector<NsItem>& items, bool split, void* workspace);
+  // Makes the tables for the current device and waits until they are there.  Throws std::bad_alloc only.  `status`: the
+  // device word in which a bounded wait that ran out is noted; nullptr: one of its own.
+  int build(const std::vector<NsItem>& items, bool split, void* workspace, int* status = nullptr);
   int run(cudaStream_t stream, int* launches = nullptr) const;
   int status(int* out) const;            // waits for the device
 
  private:
   unsigned char* mem_ = nullptr;
-  size_t mats_off_ = 0, list_off_ = 0, units_off_ = 0, status_off_ = 0;
+  int* status_ = nullptr;
+  size_t mats_off_ = 0, list_off_ = 0, units_off_ = 0;
   int tiles_ = 0, units_ = 0, grid_ = 0;
   bool split_ = false, pair_ = false, norms_ = false;
 };

@@ -19,6 +19,7 @@
 #include <cstdint>
 #include <cstdio>
 #include <cstring>
+#include <memory>
 #include <mutex>
 #include <new>
 #include <string>
@@ -26,6 +27,7 @@
 
 #include "arena.h"
 #include "ps_device.cuh"
+#include "ps_ortho.h"
 
 namespace psb {
 
@@ -34,6 +36,7 @@ constexpr int kSlots = 16;                 // task tables in flight
 constexpr int kInlineGridFactor = 4;         // an inline launch has at most this many CTAs per resident slot
 constexpr int kWorkStreams = 8;             // overlap mode: launches rotate over this many streams
 constexpr unsigned int kMaxChunk = 1u << 20;
+constexpr long long kMuonMaxDim = 1ll << 20;   // rows and columns of a PS_MUON block (products of 2^40 stay below the block limit)
 
 struct Job {
   ps_job_desc d;
@@ -49,6 +52,8 @@ struct Job {
 struct Block {
   int job = 0, id = 0;
   size_t nelem = 0;
+  long long rows = 0, cols = 0;            // blocks of PS_MUON jobs: rows x cols = nelem
+  float update_scale = 0.f;
   int ctx = 0;
   size_t off = 0, bytes = 0;               // one arena range: p | s0 | s1
   size_t sec = 0;                          // byte stride between p, s0, s1
@@ -120,7 +125,7 @@ struct Plan {                              // one built task table (host copy)
   size_t spool = 0;                        // clipped launches: elements of the buffer of kept sums
 };
 
-enum { kVarLdg = 0, kVarInline = 1, kVarBulk = 2, kVarClip = 3, kVariants = 4 };
+enum { kVarLdg = 0, kVarInline = 1, kVarBulk = 2, kVarClip = 3, kVarMuon = 4, kVariants = 5 };
 
 // A round that recurs every iteration (ps_round_prepare): the caller's lists, what
 // they resolve to, and the packed task table of the last run.
@@ -139,6 +144,17 @@ struct Prepared {
   bool clip_ok = false;                    // the same for the table of clipped runs
   Plan clip_plan;
 };
+
+// The tables of the orthogonalisation for one set of PS_MUON blocks that are aggregated together.
+struct MuonSet {
+  std::vector<int> idx;                    // the set
+  unsigned long long epoch = 0;            // where its blocks lie, and how they are cut into chunks
+  unsigned long long used = 0;             // the aggregate that used it last
+  std::vector<size_t> u_off;               // per task of the table, floats from the workspace's start
+  size_t parts_off = 0;                    // bytes
+  NsPlan plan;
+};
+constexpr size_t kMuonSets = 64;           // sets whose tables are kept
 
 // What a clipped aggregate adds to an aggregate.
 struct ClipCall {
@@ -213,6 +229,13 @@ struct ps_service {
   int clip_slot = -1;                      // slot and number of the last clipped launch
   unsigned long long clip_seq = 0;
   int clip_ctas = 0;                       // CTAs of the clip kernels an SM holds
+  // PS_MUON aggregates: one after the other, on whatever streams, they use one workspace
+  char* muon_ws = nullptr;
+  size_t muon_ws_cap = 0;
+  std::vector<std::unique_ptr<MuonSet>> muon_sets;
+  int muon_slot = -1;                      // slot and number of the last one
+  unsigned long long muon_seq = 0;
+  std::vector<int> idx_muon, idx_other;    // scratch: a ready list by kind
   int last_grid = 0, last_block = 0;
   const char* last_kernel = "none";
   std::string cuda_err;
@@ -794,6 +817,8 @@ int ps_destroy(ps_service* s) {
     if (s->done_host) cudaFreeHost(const_cast<unsigned long long*>(s->done_host));
     if (s->clip_spool) cudaFree(s->clip_spool);
     if (s->clip_shared) cudaFree(s->clip_shared);
+    s->muon_sets.clear();
+    if (s->muon_ws) cudaFree(s->muon_ws);
     if (s->copy_stream) cudaStreamDestroy(s->copy_stream);
     for (auto ws : s->work_streams) if (ws) cudaStreamDestroy(ws);
   }
@@ -806,7 +831,7 @@ int ps_register_job(ps_service* s, const ps_job_desc* d, int* job_out) {
   if (!alive(s)) return PS_ERR_BAD_HANDLE;
   std::lock_guard<std::mutex> lk(s->mu);
   if (!d || !job_out) return PS_ERR_BAD_ARG;
-  if (d->opt != PS_SGD && d->opt != PS_ADAM) return PS_ERR_BAD_ARG;
+  if (d->opt != PS_SGD && d->opt != PS_ADAM && d->opt != PS_MUON) return PS_ERR_BAD_ARG;
   if (d->grad_dtype != PS_F32 && d->grad_dtype != PS_BF16) return PS_ERR_BAD_ARG;
   if (d->num_workers < 1 || d->num_workers > PS_MAX_WORKERS) return PS_ERR_BAD_ARG;
   const int id = (int)s->jobs.size();
@@ -832,9 +857,39 @@ int ps_register_job(ps_service* s, const ps_job_desc* d, int* job_out) {
   return PS_OK;
 }
 
+static int register_locked(ps_service* s, int job, int block, size_t nelem, int ctx, const float* init);
+
 int ps_register_block(ps_service* s, int job, int block, size_t nelem, int ctx, const float* init) {
   if (!alive(s)) return PS_ERR_BAD_HANDLE;
   std::lock_guard<std::mutex> lk(s->mu);
+  if (job < 0 || job >= (int)s->jobs.size() || s->jobs[job].d.opt == PS_MUON) return PS_ERR_BAD_ARG;
+  return register_locked(s, job, block, nelem, ctx, init);
+}
+
+int ps_register_matrix(ps_service* s, int job, int block, long long rows, long long cols, int ctx, const float* init,
+                       float update_scale) {
+  if (!alive(s)) return PS_ERR_BAD_HANDLE;
+  std::lock_guard<std::mutex> lk(s->mu);
+  if (job < 0 || job >= (int)s->jobs.size() || s->jobs[job].d.opt != PS_MUON) return PS_ERR_BAD_ARG;
+  if (rows < 1 || cols < 1 || rows > kMuonMaxDim || cols > kMuonMaxDim || !(std::fabs(update_scale) <= 3.4e38f)) return PS_ERR_BAD_ARG;
+  try {
+    NsItem one;                            // (a matrix that no aggregate could work on is refused here)
+    one.rows = rows;
+    one.cols = cols;
+    if (!NsPlan::workspace({one}, true)) return PS_ERR_TOO_LARGE;
+  } catch (const std::bad_alloc&) {
+    return PS_ERR_NOMEM;
+  }
+  const int rc = register_locked(s, job, block, (size_t)rows * (size_t)cols, ctx, init);
+  if (rc) return rc;
+  Block& b = s->blocks[s->jobs[job].block_of_id[block]];
+  b.rows = rows;
+  b.cols = cols;
+  b.update_scale = update_scale;
+  return PS_OK;
+}
+
+static int register_locked(ps_service* s, int job, int block, size_t nelem, int ctx, const float* init) {
   if (job < 0 || job >= (int)s->jobs.size() || block < 0 || block >= (1 << 26)) return PS_ERR_BAD_ARG;
   if (nelem == 0 || nelem > ((size_t)1 << 40) || ctx < 0 || ctx >= (int)s->ctxs.size()) return PS_ERR_BAD_ARG;
   Job& j = s->jobs[job];
@@ -933,6 +988,7 @@ static int push_rows_locked(ps_service* s, int job, int block, int worker, const
   if (bi < 0 || !row_ids || !values || n_rows < 0 || row_len <= 0) return PS_ERR_BAD_ARG;
   Block& b = s->blocks[bi];
   const Job& j = s->jobs[b.job];
+  if (j.d.opt == PS_MUON) return PS_ERR_BAD_ARG;
   if (worker < 0 || worker >= j.d.num_workers || j.d.num_workers > kRowsMaxWorkers) return PS_ERR_BAD_ARG;
   if (b.nelem % (size_t)row_len != 0 || (size_t)n_rows > b.nelem / (size_t)row_len) return PS_ERR_BAD_ARG;
   if (b.row_len != 0 && b.row_len != (unsigned int)row_len) return PS_ERR_BAD_ARG;
@@ -1305,6 +1361,8 @@ int build_clip_plan(ps_service* s, const std::vector<int>& idx, Plan* plan) try 
   const size_t n = idx.size();
   std::vector<int> job_ids;
   for (int bi : idx)
+    if (s->jobs[s->blocks[bi].job].d.opt == PS_MUON) return PS_ERR_BAD_ARG;
+  for (int bi : idx)
     if (std::find(job_ids.begin(), job_ids.end(), s->blocks[bi].job) == job_ids.end()) {
       if (job_ids.size() == (size_t)kClipMaxJobs) return PS_ERR_TOO_LARGE;
       job_ids.push_back(s->blocks[bi].job);
@@ -1520,6 +1578,146 @@ int launch_clip(ps_service* s, const std::vector<int>& idx, Plan& plan, const Cl
   return PS_OK;
 }
 
+// The tables for the set of PS_MUON blocks of `plan`, kept from aggregate to aggregate, and the workspace they need.
+int muon_set(ps_service* s, const Plan& plan, MuonSet** out) {
+  const unsigned char* base = plan.bytes.data();
+  const PsTaskDev* tasks = reinterpret_cast<const PsTaskDev*>(base + reinterpret_cast<const PsTableHdr*>(base)->tasks_off);
+  const unsigned long long now = s->launches + 1;
+  for (auto& m : s->muon_sets)
+    if (m->epoch == s->epoch && m->idx == plan.order) {
+      m->used = now;
+      *out = m.get();
+      return PS_OK;
+    }
+  const size_t n = plan.order.size();
+  auto m = std::make_unique<MuonSet>();
+  m->idx = plan.order;
+  m->epoch = s->epoch;
+  m->used = now;
+  size_t at = 0;
+  for (size_t i = 0; i < n; ++i) {
+    m->u_off.push_back(at / sizeof(float));
+    at += Arena::round_up(s->blocks[plan.order[i]].nelem * sizeof(float));
+  }
+  m->parts_off = at;
+  at += Arena::round_up((size_t)plan.total_chunks * sizeof(double));
+  std::vector<NsItem> items(n);
+  for (size_t i = 0; i < n; ++i) {
+    items[i].rows = s->blocks[plan.order[i]].rows;
+    items[i].cols = s->blocks[plan.order[i]].cols;
+    items[i].parts = reinterpret_cast<double*>(1);       // (not the library's to find room for)
+  }
+  const size_t ns = NsPlan::workspace(items, true);
+  if (!ns) return PS_ERR_TOO_LARGE;
+  if (at + ns > s->muon_ws_cap) {
+    PS_CUDA(s, cudaDeviceSynchronize());
+    s->muon_sets.clear();                  // (their tables name the old workspace)
+    if (s->muon_ws) PS_CUDA(s, cudaFree(s->muon_ws));
+    s->muon_ws = nullptr;
+    s->muon_ws_cap = 0;
+    const cudaError_t e = cudaMalloc(&s->muon_ws, at + ns);
+    if (e != cudaSuccess) {
+      s->muon_ws = nullptr;
+      s->cuda_err = std::string("workspace of PS_MUON aggregates: ") + cudaGetErrorString(e);
+      cudaGetLastError();
+      return e == cudaErrorMemoryAllocation ? PS_ERR_NOMEM : PS_ERR_CUDA;
+    }
+    s->muon_ws_cap = at + ns;
+  }
+  for (size_t i = 0; i < n; ++i) {
+    const Block& b = s->blocks[plan.order[i]];
+    const ps_job_desc& d = s->jobs[b.job].d;
+    NsItem& it = items[i];
+    it.src = reinterpret_cast<float*>(s->muon_ws) + m->u_off[i];
+    it.ld_src = it.ld_dst = b.cols;
+    it.parts = reinterpret_cast<double*>(s->muon_ws + m->parts_off) + tasks[i].first_chunk;
+    it.nparts = (int)tasks[i].nchunks;
+    it.dst = blk_p(s, b);
+    it.out = kNsOutUpdate;
+    it.decay = (float)(1.0 - (double)d.lr * (double)d.weight_decay);
+    it.step = (float)((double)d.lr * (double)b.update_scale);
+  }
+  const int rc = m->plan.build(items, true, s->muon_ws + at, s->status_dev);
+  if (rc) {
+    if (rc == PS_ERR_CUDA) s->cuda_err = ps_op_last_error();
+    return rc;
+  }
+  if (s->muon_sets.size() >= kMuonSets) {  // the one that has not been used for longest, or whose blocks have moved
+    size_t old = 0;
+    for (size_t k = 1; k < s->muon_sets.size(); ++k) {
+      const MuonSet &a = *s->muon_sets[k], &b = *s->muon_sets[old];
+      if ((a.epoch != s->epoch) != (b.epoch != s->epoch) ? a.epoch != s->epoch : a.used < b.used) old = k;
+    }
+    s->muon_sets.erase(s->muon_sets.begin() + (long)old);      // (freeing its tables waits for the device)
+  }
+  s->muon_sets.push_back(std::move(m));
+  *out = s->muon_sets.back().get();
+  return PS_OK;
+}
+
+// Launches the aggregate of the PS_MUON blocks `idx` (table `plan`, tables `set`) on `stream` itself (device current).
+int launch_muon(ps_service* s, const std::vector<int>& idx, Plan& plan, const MuonSet& set, cudaStream_t stream) {
+  ++s->call_id;
+  unsigned char* base = plan.bytes.data();
+  PsTaskDev* tasks = reinterpret_cast<PsTaskDev*>(base + reinterpret_cast<PsTableHdr*>(base)->tasks_off);
+  for (size_t i = 0; i < plan.order.size(); ++i) tasks[i].p = reinterpret_cast<float*>(s->muon_ws) + set.u_off[i];
+  Slot* sl = nullptr;
+  int rc = acquire_slot(s, plan.bytes.size(), (size_t)plan.total_chunks, &sl);
+  if (rc) return rc;
+  const int slot_index = (int)(sl - s->slots);
+  unsigned int waited = 0;
+  if (s->muon_slot >= 0) {                 // the last such aggregate uses the same workspace
+    Slot& last = s->slots[s->muon_slot];
+    if (last.seq == s->muon_seq && !slot_finished(s, last)) {
+      PS_CUDA(s, cudaStreamWaitEvent(stream, last.done, 0));
+      waited = 1u << (unsigned)s->muon_slot;
+    }
+  }
+  for (int bi : idx) {
+    rc = order_after_block(s, s->blocks[bi], stream, &waited);
+    if (rc) return rc;
+  }
+  const unsigned long long seq = s->launches + 1;
+  std::memcpy(sl->host, plan.bytes.data(), plan.bytes.size());
+  PS_CUDA(s, cudaMemcpyAsync(sl->dev, sl->host, plan.bytes.size(), cudaMemcpyHostToDevice, s->copy_stream));
+  PS_CUDA(s, cudaEventRecord(sl->copied, s->copy_stream));
+  PS_CUDA(s, cudaStreamWaitEvent(stream, sl->copied, 0));
+  const int grid = (int)std::min<unsigned long long>(plan.total_chunks, (unsigned long long)s->num_sms * 4u);
+  const cudaError_t le = launch_kernel(ps_aggregate_muon_kernel, grid, kThreads, 0, stream, false, sl->dev,
+                                       (const PsJobDev*)s->jobs_dev, s->stats_dev, sl->partials,
+                                       reinterpret_cast<double*>(s->muon_ws + set.parts_off));
+  if (le != cudaSuccess) {
+    s->cuda_err = std::string("kernel launch: ") + cudaGetErrorString(le);
+    cudaGetLastError();
+    return PS_ERR_CUDA;
+  }
+  rc = set.plan.run(stream);
+  if (rc) {
+    s->cuda_err = ps_op_last_error();
+    return rc;
+  }
+  sl->seq = seq;
+  sl->gen = seq;
+  sl->signals = false;                     // (finished when the orthogonalisation is: the event says so)
+  sl->stream = stream;
+  sl->work_stream = -1;
+  sl->inflight = true;
+  sl->done_recorded = false;
+  PS_CUDA(s, cudaEventRecord(sl->done, stream));
+  sl->done_recorded = true;
+  s->muon_slot = slot_index;
+  s->muon_seq = seq;
+  s->next_slot = (s->next_slot + 1) % kSlots;
+  s->launches = seq;
+  s->var_launches[kVarMuon]++;
+  s->var_bytes[kVarMuon] += plan.algo_bytes;
+  s->last_grid = grid;
+  s->last_block = kThreads;
+  s->last_kernel = "muon";
+  consume_pushes(s, idx, slot_index, sl->gen);
+  return PS_OK;
+}
+
 bool bad_clip(float max_norm, const float* norms_out) {
   return !(max_norm > 0.0f) || (reinterpret_cast<uintptr_t>(norms_out) & 3u);
 }
@@ -1553,6 +1751,28 @@ int flush_batch(ps_service* s) {
 
 extern "C" {
 
+// A ready list with blocks of PS_MUON jobs: the others go out as one launch as ever, without being held back, the PS_MUON
+// blocks together on `stream` itself.
+static int submit_muon(ps_service* s, const std::vector<int>& idx, cudaStream_t stream, unsigned int flags) try {
+  int rc = flush_batch(s);                 // earlier rounds first
+  if (rc) return rc;
+  PS_CUDA(s, cudaSetDevice(s->device));
+  s->idx_muon.clear();
+  s->idx_other.clear();
+  for (int bi : idx) (s->jobs[s->blocks[bi].job].d.opt == PS_MUON ? s->idx_muon : s->idx_other).push_back(bi);
+  Plan muon;
+  MuonSet* set = nullptr;
+  rc = build_plan(s, s->idx_muon, &muon);
+  if (!rc) rc = muon_set(s, muon, &set);   // what may fail for want of memory comes before the first launch
+  if (!rc && !s->idx_other.empty()) {
+    rc = build_plan(s, s->idx_other, &s->plan);
+    if (!rc) rc = launch_plan(s, s->idx_other, s->plan, stream, flags);
+  }
+  return rc ? rc : launch_muon(s, s->idx_muon, muon, *set, stream);
+} catch (const std::bad_alloc&) {
+  return PS_ERR_NOMEM;
+}
+
 // The validated, ready blocks `idx` are to be aggregated.  Packing over time: with
 // PS_OPT_OVERLAP and PS_OPT_BATCH, tasks whose inputs are complete are held back while at
 // least kBatchDepth launches are still running and go out together with whatever becomes
@@ -1562,6 +1782,8 @@ extern "C" {
 // already built for exactly `idx`, used when the launch goes out alone.
 static int submit_ready(ps_service* s, const std::vector<int>& idx, cudaStream_t stream, unsigned int flags,
                         Plan* own, bool own_ok, bool* own_built = nullptr) {
+  for (int bi : idx)
+    if (s->jobs[s->blocks[bi].job].d.opt == PS_MUON) return submit_muon(s, idx, stream, flags);
   const bool can_wait = s->opt_overlap && s->opt_batch && (flags & PS_ROUND_INPUTS_COMPLETE);
   if (!can_wait) {
     int rc = flush_batch(s);          // earlier rounds first: launches keep their order per block
@@ -2427,7 +2649,8 @@ int ps_launch_stats(ps_service* s, int variant, unsigned long long* launches_out
   { int frc = flush_batch(s); if (frc) return frc; }    // held-back rounds go out first
   if (variant < 0 || variant >= kVariants) return PS_ERR_BAD_ARG;
   static const char* const names[kVariants] = {"ps_aggregate_ldg_kernel", "ps_aggregate_inline_kernel",
-                                               "ps_aggregate_bulk_kernel", "ps_aggregate_clip_kernel"};
+                                               "ps_aggregate_bulk_kernel", "ps_aggregate_clip_kernel",
+                                               "ps_aggregate_muon_kernel"};
   if (launches_out) *launches_out = s->var_launches[variant];
   if (bytes_out) *bytes_out = s->var_bytes[variant];
   if (name_out) *name_out = names[variant];

@@ -47,7 +47,7 @@ size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 struct XePlan {
   long long nparts, pitch, piece, pieces;
   int slices;                            // per piece
-  size_t parts, score, xm, d[2], sums, w, end, end_unaligned;
+  size_t parts, score, xm, d[2], sums, x, w, end, end_unaligned;
 };
 
 // A piece of d: as many words as make 2^24 entries (32 MB), whole tiles, at least one.
@@ -86,6 +86,7 @@ XePlan xent_plan(long long T, long long V, long long D) {
   p.sums = take(p.slices > 1 || p.pieces > 1 ? (size_t)p.slices * (size_t)T * (size_t)D * sizeof(float) : 0);
   at = std::max(at, forward);
   p.end = at;
+  p.x = take((size_t)T * (size_t)p.pitch * 2);
   p.w = take((size_t)V * (size_t)p.pitch * 2);
   p.end_unaligned = at;
   return p;
@@ -94,7 +95,7 @@ XePlan xent_plan(long long T, long long V, long long D) {
 // What any call of at most T tokens needs (a smaller batch is cut into larger pieces and more slices).
 size_t xent_bytes(long long T, long long V, long long D, bool unaligned) {
   const size_t pitch = (size_t)ceil_div(D, 8) * 8, all = (size_t)ceil_div(V, kXeTile) * kXeTile, t = (size_t)T;
-  const size_t x = round256(t * pitch * 2), w = unaligned ? round256((size_t)V * pitch * 2) : 0;
+  const size_t x = (unaligned ? 2 : 1) * round256(t * pitch * 2), w = unaligned ? round256((size_t)V * pitch * 2) : 0;
   const size_t parts = round256(t * (size_t)ceil_div(V, 128) * sizeof(float2)) + round256(t * sizeof(float));
   const size_t piece = std::max(std::min(t * all, (size_t)kXePieceEntries), t * kXeTile);
   const size_t rows = std::max(t, std::min(t * kXeMaxSlices, (size_t)kXeSliceRows));
@@ -116,13 +117,13 @@ struct XeCall {
   OpDevice dev;
   cudaStream_t stream;
   char* ws;
-  bool copy_w;
+  bool copy_x, copy_w;                   // rows that no tensor map can walk are copied first
   XeArgs args;
 };
 
 bool rows_aligned(const void* p, long long ld) { return !misaligned(p, 16) && ld % 8 == 0; }
 
-int check(const ps_xent* q, XePlan* plan, bool* copy_w) {
+int check(const ps_xent* q, XeCall* c) {
   if (!q || q->tokens < 0 || q->vocab < 1 || q->dim < 1 || q->tokens >= kXeMaxDim || q->vocab >= kXeMaxDim ||
       q->dim >= kXeMaxDim || q->ldx < q->dim || q->ldw < q->dim || (q->target_bits != 32 && q->target_bits != 64))
     return PS_ERR_BAD_ARG;
@@ -132,24 +133,27 @@ int check(const ps_xent* q, XePlan* plan, bool* copy_w) {
   if (ceil_div(q->tokens, kXeTile) * ceil_div(q->vocab, kXeTile) > 0x3fffffffll ||
       ceil_div(q->vocab, kXeTile) * ceil_div(q->dim, kXeTile) > 0x3fffffffll)
     return PS_ERR_TOO_LARGE;
-  *plan = xent_plan(q->tokens, q->vocab, q->dim);
-  *copy_w = !rows_aligned(q->w, q->ldw);
-  if (q->workspace_bytes < (*copy_w ? plan->end_unaligned : plan->end)) return PS_ERR_NOMEM;
+  c->q = q;
+  c->plan = xent_plan(q->tokens, q->vocab, q->dim);
+  c->copy_w = !rows_aligned(q->w, q->ldw);
+  c->copy_x = q->tokens > 0 && !rows_aligned(q->x, q->ldx);
+  if (q->workspace_bytes < (c->copy_w || c->copy_x ? c->plan.end_unaligned : c->plan.end)) return PS_ERR_NOMEM;
   return PS_OK;
 }
 
-int copy_rows(const XeCall& c, const void* src, long long rows, long long ld, size_t to, bool mask) {
+int copy_rows(const XeCall& c, const void* src, long long rows, long long ld, size_t to, bool mask, const float* weights) {
   const long long units = rows * (c.plan.pitch / 8);
   const unsigned grid = (unsigned)std::min<long long>(ceil_div(units, kXeCopyThreads), (long long)c.dev.num_sms * 16);
   return op_launch("cross entropy", ps_xent_copy_kernel, grid, kXeCopyThreads, 0, 1, c.stream,
                    static_cast<const unsigned short*>(src), rows, c.q->dim, ld, reinterpret_cast<unsigned short*>(c.ws + to),
                    c.plan.pitch, mask ? c.q->targets : nullptr, c.q->target_bits == 64 ? 1 : 0, c.q->vocab,
-                   rows_aligned(src, ld) ? 1 : 0);
+                   weights, rows_aligned(src, ld) ? 1 : 0);
 }
 
-// What both passes set up.  use_copy: x is read from its masked copy.
-int begin(XeCall* c, const ps_xent* q, void* stream, bool backward) {
-  c->q = q;
+// What both passes set up.
+int begin(XeCall* c, void* stream, bool backward, const float* weights) {
+  const ps_xent* q = c->q;
+  const XePlan& p = c->plan;
   c->stream = static_cast<cudaStream_t>(stream);
   c->ws = static_cast<char*>(q->workspace);
   int rc = op_device(&c->dev);
@@ -166,19 +170,16 @@ int begin(XeCall* c, const ps_xent* q, void* stream, bool backward) {
   a.D = q->dim;
   a.targets = q->targets;
   a.target64 = q->target_bits == 64;
-  const bool copy_x = backward || !rows_aligned(q->x, q->ldx);
-  const void* x = copy_x ? c->ws + c->plan.xm : q->x;
-  const void* w = c->copy_w ? c->ws + c->plan.w : q->w;
-  if (!make_map(encode, &a.x, x, a.T, a.D, copy_x ? c->plan.pitch : q->ldx) ||
-      !make_map(encode, &a.w, w, a.V, a.D, c->copy_w ? c->plan.pitch : q->ldw))
-    return op_cuda_error("tensor map", cudaErrorInvalidValue);
-  if (backward)
-    for (int b = 0; b < 2 && b < c->plan.pieces; ++b)
-      if (!make_map(encode, &a.d[b], c->ws + c->plan.d[b], a.T, c->plan.piece, c->plan.piece))
-        return op_cuda_error("tensor map", cudaErrorInvalidValue);
-  a.xm = a.x;
-  if (copy_x) rc = copy_rows(*c, q->x, q->tokens, q->ldx, c->plan.xm, backward);
-  if (!rc && c->copy_w) rc = copy_rows(*c, q->w, q->vocab, q->ldw, c->plan.w, false);
+  bool ok = c->copy_x ? make_map(encode, &a.x, c->ws + p.x, a.T, a.D, p.pitch) : make_map(encode, &a.x, q->x, a.T, a.D, q->ldx);
+  ok = ok && (c->copy_w ? make_map(encode, &a.w, c->ws + p.w, a.V, a.D, p.pitch) : make_map(encode, &a.w, q->w, a.V, a.D, q->ldw));
+  if (backward) {
+    ok = ok && make_map(encode, &a.xm, c->ws + p.xm, a.T, a.D, p.pitch);
+    for (int b = 0; b < 2 && b < p.pieces; ++b) ok = ok && make_map(encode, &a.d[b], c->ws + p.d[b], a.T, p.piece, p.piece);
+  }
+  if (!ok) return op_cuda_error("tensor map", cudaErrorInvalidValue);
+  if (c->copy_x) rc = copy_rows(*c, q->x, q->tokens, q->ldx, p.x, false, nullptr);
+  if (!rc && c->copy_w) rc = copy_rows(*c, q->w, q->vocab, q->ldw, p.w, false, nullptr);
+  if (!rc && backward) rc = copy_rows(*c, q->x, q->tokens, q->ldx, p.xm, true, weights);
   return rc;
 }
 
@@ -213,12 +214,12 @@ int ps_xent_sizes(long long tokens, long long vocab, long long dim, size_t* byte
 
 int ps_xent_forward(const ps_xent* q, float* loss, float* lse, void* stream) {
   XeCall c;
-  int rc = check(q, &c.plan, &c.copy_w);
+  int rc = check(q, &c);
   if (rc) return rc;
   if (q->tokens == 0) return PS_OK;
   if (!loss && !lse) return PS_ERR_BAD_ARG;
   if (misaligned(loss, 4) || misaligned(lse, 4)) return PS_ERR_ALIGN;
-  rc = begin(&c, q, stream, false);
+  rc = begin(&c, stream, false, nullptr);
   if (rc) return rc;
   XeArgs& a = c.args;
   a.parts = reinterpret_cast<float2*>(c.ws + c.plan.parts);
@@ -235,7 +236,7 @@ int ps_xent_forward(const ps_xent* q, float* loss, float* lse, void* stream) {
 int ps_xent_backward(const ps_xent* q, const float* lse, float scale, const float* token_scale, void* dx, long long lddx,
                      void* dw, int dw_dtype, long long lddw, void* stream) {
   XeCall c;
-  int rc = check(q, &c.plan, &c.copy_w);
+  int rc = check(q, &c);
   if (rc) return rc;
   if ((!dx && !dw) || (dw_dtype != PS_F32 && dw_dtype != PS_BF16) || (dx && lddx < q->dim) || (dw && lddw < q->dim))
     return PS_ERR_BAD_ARG;
@@ -248,7 +249,7 @@ int ps_xent_backward(const ps_xent* q, const float* lse, float scale, const floa
                                             static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? PS_OK : op_cuda_error("ps_xent_backward", e);
   }
-  rc = begin(&c, q, stream, true);
+  rc = begin(&c, stream, true, dw ? token_scale : nullptr);
   if (rc) return rc;
   XeArgs& a = c.args;
   const XePlan& p = c.plan;
@@ -289,7 +290,7 @@ int ps_xent_backward(const ps_xent* q, const float* lse, float scale, const floa
   if (dx && p.slices > 1) {
     const unsigned grid = (unsigned)std::min<long long>(ceil_div(a.T * a.D, kXeCopyThreads), (long long)c.dev.num_sms * 8);
     rc = op_launch("cross entropy", ps_xent_slices_kernel, grid, kXeCopyThreads, 0, 1, c.stream, (const float*)a.dx_sums, filled,
-                   a.T, a.D, a.dx, a.ld_dx);
+                   a.T, a.D, a.targets, a.target64, a.V, a.weights, a.scale, a.dx, a.ld_dx);
   }
   return rc;
 }

@@ -9,9 +9,12 @@
 // so that what each launch ends with is covered by work that does not depend on it.  A piece of d takes about 32 MB
 // and so stays in L2 between its writing and its reading.
 //
-// Roundings: products of bf16 values are exact and summed in binary32; maxima, sums, lse and losses are binary32; d is
-// rounded to bf16 (it is an operand, and x and w are bf16, which one MMA wants of both): 2^-9 of each entry, which is
-// below the rounding of the bf16 gradients.
+// Roundings: products of bf16 values are exact and summed in binary32; maxima, sums, lse and losses are binary32.  What is
+// stored of d is exp(s - lse) - [v = target], rounded to bf16 (it is an operand, and x and w are bf16, which one MMA wants
+// of both): at most 2^-8 of each entry, of either sign, and none where it matters most, at the target of an unlikely word,
+// whose -1 is exact.  The factor g_t stays out of it, because its own rounding would be the same for all of a token's
+// entries (a mean over 7680 tokens came out 3.5e-3 wrong): scale enters in the epilogues, token_scale there for dx and in
+// the copy of x for dw.
 #pragma once
 
 #include "ps_tc.cuh"
@@ -34,7 +37,7 @@ struct XeSeg {                           // a launch's tiles of one kind, tiles_
 constexpr int kXeMaxSegs = 3;
 
 struct XeArgs {
-  CUtensorMap x, xm, w, d[2];            // xm: x with the rows of ignored tokens zeroed
+  CUtensorMap x, xm, w, d[2];            // xm: token_scale * x, the rows of ignored tokens zeroed
   int* status;
   int nseg, tiles;
   XeSeg seg[kXeMaxSegs];
@@ -60,6 +63,13 @@ struct XeArgs {
 
 __device__ __forceinline__ long long xe_target(const void* targets, int is64, long long t) {
   return is64 ? static_cast<const long long*>(targets)[t] : (long long)static_cast<const int*>(targets)[t];
+}
+
+// g_t; zero for an ignored token, whatever token_scale holds there.
+__device__ __forceinline__ float xe_factor(const void* targets, int is64, long long V, const float* weights, float scale, long long t) {
+  const long long v = xe_target(targets, is64, t);
+  if (v < 0 || v >= V) return 0.f;
+  return weights ? scale * weights[t] : scale;
 }
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -158,7 +168,7 @@ struct XeOp {
     const TcWarp& w;
     const At at;
     long long row, word;                 // this lane's row; the target (kXeStats, kXeProb: relative to the tile's first column)
-    float m, s, g;
+    float m, s, g;                       // g: kXeDx: the factor of the row's gradient
     bool counts;                         // the row's token has a target
 
     __device__ __forceinline__ Epilogue(const XeArgs& args, int index, const TcWarp& warp, MmCursor<1>&)
@@ -167,21 +177,24 @@ struct XeOp {
     __device__ __forceinline__ void begin() {
       const int kind = at.seg->kind;
       row = (long long)at.m * kXeTile + w.row + w.lane;
+      g = a.scale;
+      if (kind == kXeDx && row < a.T) g = factor(a, row);
       if (kind <= kXeProb) {
         word = -1;
         m = __int_as_float(0xff800000);
-        s = g = 0.f;
+        s = 0.f;
         counts = false;
         if (row < a.T) {
           const long long v = xe_target(a.targets, a.target64, row);
           counts = v >= 0 && v < a.V;
           if (counts) word = v - (at.seg->v0 + (long long)at.n * kXeTile);
-          if (kind == kXeProb && counts) {
-            m = a.lse[row];
-            g = a.weights ? a.scale * a.weights[row] : a.scale;
-          }
+          if (kind == kXeProb && counts) m = a.lse[row];
         }
       }
+    }
+
+    static __device__ __forceinline__ float factor(const XeArgs& a, long long row) {
+      return xe_factor(a.targets, a.target64, a.V, a.weights, a.scale, row);
     }
 
     __device__ __forceinline__ void columns(float (&v)[32], int c) {
@@ -232,12 +245,12 @@ struct XeOp {
       const long long v0 = (long long)at.n * kXeTile + c;             // column in the piece
       if (row >= a.T) return;
 #pragma unroll
-      for (int i = 0; i < 32; ++i) v[i] = g * xe_exp2((v[i] - m) * kLog2e);
+      for (int i = 0; i < 32; ++i) v[i] = xe_exp2((v[i] - m) * kLog2e);
       const long long in = word - c;
       if (in >= 0 && in < 32) {
 #pragma unroll
         for (int i = 0; i < 32; ++i)
-          v[i] -= i == (int)in ? g : 0.f;
+          v[i] -= i == (int)in ? 1.f : 0.f;
       }
       // zeros past the vocabulary, and in the rows of ignored tokens whatever x holds there
       const long long live = counts ? a.V - (at.seg->v0 + v0) : 0;
@@ -271,8 +284,13 @@ struct XeOp {
             if (i < live) v[i] += __ldcg(sums + i);
         }
       }
-      if (at.seg->finish) xe_store_bf16(a.dx + (size_t)row * (size_t)a.ld_dx + (size_t)col, v, live, a.dx_wide != 0);
-      else xe_store_f32(sums, v, live, wide);
+      if (at.seg->finish) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] *= g;
+        xe_store_bf16(a.dx + (size_t)row * (size_t)a.ld_dx + (size_t)col, v, live, a.dx_wide != 0);
+      } else {
+        xe_store_f32(sums, v, live, wide);
+      }
     }
 
     __device__ __forceinline__ void dw(float (&v)[32], int c) {
@@ -280,6 +298,8 @@ struct XeOp {
       const int live = (int)min(32ll, a.D - col);
       if (out >= a.V || live <= 0) return;
       const size_t o = (size_t)out * (size_t)a.ld_dw + (size_t)col;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) v[i] *= a.scale;
       if (a.dw_f32) xe_store_f32(static_cast<float*>(a.dw) + o, v, live, a.dw_wide != 0);
       else xe_store_bf16(static_cast<__nv_bfloat16*>(a.dw) + o, v, live, a.dw_wide != 0);
     }
@@ -335,13 +355,14 @@ ps_xent_join_kernel(const float2* __restrict__ parts, int nparts, const float* _
   }
 }
 
-// Copies a matrix of bf16 into rows of `pitch` elements (a multiple of eight; the rest zeros), the rows of ignored tokens
-// as zeros (targets != nullptr): what padded places of a batch hold, NaN or not, does not reach the gradients.
+// Copies a matrix of bf16 into rows of `pitch` elements (a multiple of eight; the rest zeros).  With targets the rows of
+// ignored tokens become zeros, so that what padded places of a batch hold, NaN or not, does not reach the gradients, and
+// the others are multiplied by their weight.
 constexpr int kXeCopyThreads = 256;
 __global__ void __launch_bounds__(kXeCopyThreads)
 ps_xent_copy_kernel(const unsigned short* __restrict__ src, long long rows, long long cols, long long ld,
                     unsigned short* __restrict__ dst, long long pitch, const void* __restrict__ targets, int target64,
-                    long long V, int wide) {
+                    long long V, const float* __restrict__ weights, int wide) {
   mm_pdl();
   const long long per = pitch / 8, total = rows * per;
   for (long long i = (long long)blockIdx.x * kXeCopyThreads + threadIdx.x; i < total; i += (long long)gridDim.x * kXeCopyThreads) {
@@ -362,6 +383,12 @@ ps_xent_copy_kernel(const unsigned short* __restrict__ src, long long rows, long
         for (int k = 0; k < 8; ++k) u[k] = c + k < cols ? p[k] : 0;
         q = make_uint4(u[0] | u[1] << 16, u[2] | u[3] << 16, u[4] | u[5] << 16, u[6] | u[7] << 16);
       }
+      if (weights) {
+        const float g = weights[r];
+        unsigned int* u = &q.x;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) u[k] = mm_bf16x2(__uint_as_float(u[k] << 16) * g, __uint_as_float(u[k] & 0xffff0000u) * g);
+      }
     }
     *reinterpret_cast<uint4*>(dst + (size_t)r * (size_t)pitch + (size_t)c) = q;
   }
@@ -369,7 +396,8 @@ ps_xent_copy_kernel(const unsigned short* __restrict__ src, long long rows, long
 
 // dx = sum over the slices, in order.
 __global__ void __launch_bounds__(kXeCopyThreads)
-ps_xent_slices_kernel(const float* __restrict__ sums, int slices, long long T, long long D, __nv_bfloat16* __restrict__ dx,
+ps_xent_slices_kernel(const float* __restrict__ sums, int slices, long long T, long long D, const void* __restrict__ targets,
+                      int target64, long long V, const float* __restrict__ weights, float scale, __nv_bfloat16* __restrict__ dx,
                       long long ld) {
   mm_pdl();
   const long long n = T * D;
@@ -378,7 +406,7 @@ ps_xent_slices_kernel(const float* __restrict__ sums, int slices, long long T, l
 #pragma unroll 8
     for (int k = 1; k < slices; ++k) v += sums[(size_t)k * (size_t)n + (size_t)i];
     const long long r = i / D;
-    dx[(size_t)r * (size_t)ld + (size_t)(i - r * D)] = __float2bfloat16_rn(v);
+    dx[(size_t)r * (size_t)ld + (size_t)(i - r * D)] = __float2bfloat16_rn(v * xe_factor(targets, target64, V, weights, scale, r));
   }
 }
 

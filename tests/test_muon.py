@@ -1,0 +1,324 @@
+"""PS_MUON jobs of the service: sums, momentum and the orthogonalised update.
+
+The sum, the momentum and the statistics are defined to the bit (binary32, worker order) and compared for equality.  The
+update comes from the orthogonalisation: the parameters may be off by lr * update_scale times what test_ortho.py allows
+an fp32 result (a bound on the Frobenius norm), plus three roundings of a parameter."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2204_03211_b200 import binding as B
+from test_ortho import off, steps
+
+gpu = pytest.mark.gpu
+LR, MOM, WD = 0.02, 0.95, 0.1
+
+
+class World:
+    """One PS_MUON job and what its blocks should hold, in 64 bits from binary32 momentum."""
+
+    def __init__(self, shapes, W=3, dtype=B.PS_F32, grad_scale=1.0, contexts=1, seed=0, svc=None, scales=None):
+        self.gen = torch.Generator(device="cuda").manual_seed(seed)
+        self.shapes, self.W, self.dtype, self.gs = shapes, W, dtype, grad_scale
+        self.svc = svc or B.Service(0, contexts, (1 << 22) + sum(8 * r * c for r, c in shapes))
+        self.job = self.svc.register_job(opt=B.PS_MUON, grad_dtype=dtype, num_workers=W, lr=LR, momentum=MOM, weight_decay=WD,
+                                         grad_scale=grad_scale)
+        self.scales = scales or [0.2 * max(s) ** 0.5 for s in shapes]
+        self.p, self.v = [], []
+        for b, s in enumerate(shapes):
+            p = self.rand(s) * 0.05
+            self.svc.register_matrix(self.job, b, *s, 0, p, None if scales is None else scales[b])
+            self.p.append(p.double())
+            self.v.append(torch.zeros(s, device="cuda"))
+        self.tol = [0.0] * len(shapes)
+        self.keep = []
+
+    def rand(self, s):
+        return torch.randn(s, device="cuda", generator=self.gen)
+
+    def shards(self, b, off_by=0):
+        n = self.shapes[b][0] * self.shapes[b][1]
+        t = torch.float32 if self.dtype == B.PS_F32 else torch.bfloat16
+        out = []
+        for _ in range(self.W):
+            flat = torch.empty(n + off_by, device="cuda", dtype=t)[off_by:]
+            flat.copy_((self.rand((n,)) * 1e-2).to(t))
+            out.append(flat)
+        return out
+
+    def expect(self, b, shards):
+        """One aggregate of block b: what its state has to be, and the norm of the sum."""
+        g = shards[0].float()
+        for s in shards[1:]:
+            g = g + s.float()                               # binary32, worker order
+        g = (g * np.float32(self.gs)).view(self.shapes[b])
+        m = np.float32(MOM)
+        v = self.v[b] * m + g
+        u = g + v * m
+        self.v[b] = v
+        o = steps(u)
+        rate = float(np.float32(float(np.float32(LR)) * float(np.float32(self.scales[b]))))
+        decay = float(np.float32(1.0 - float(np.float32(LR)) * float(np.float32(WD))))
+        self.p[b] = self.p[b] * decay - rate * o
+        self.tol[b] = self.tol[b] * decay + rate * (4 * off(steps(u, torch.float32), o) + 2.0 ** -17) * float(o.norm()) + \
+            3 * 2.0 ** -24 * float(self.p[b].norm())
+        return float(g.double().square().sum())
+
+    def push(self, b, shards):
+        self.keep.append(shards)
+        for w in reversed(range(self.W)):
+            self.svc.push(self.job, b, w, shards[w])
+
+    def step(self, blocks=None, off_by=0, stream=None, extra=()):
+        blocks = list(range(len(self.shapes))) if blocks is None else blocks
+        sq = {}
+        for b in blocks:
+            s = self.shards(b, off_by)
+            self.push(b, s)
+            sq[b] = self.expect(b, s)
+        torch.cuda.synchronize()
+        self.svc.aggregate([(self.job, b) for b in blocks] + list(extra), stream)
+        return sq
+
+    def check(self, steps_done=None, sq=None):
+        torch.cuda.synchronize()
+        assert self.svc.device_status() == 0
+        for b, s in enumerate(self.shapes):
+            n = s[0] * s[1]
+            p = self.svc.view(self.svc.pull(self.job, b), n).view(s)
+            v = self.svc.view(self.svc.block_state(self.job, b)[0], n).view(s)
+            assert torch.equal(v, self.v[b]), "momentum of block %d" % b
+            far = float((p.double() - self.p[b]).norm())
+            assert far <= self.tol[b] + 1e-12, "block %d: off by %.3g, allowed %.3g" % (b, far, self.tol[b])
+            if steps_done is not None:
+                got, step = self.svc.block_stats(self.job, b)
+                assert step == (steps_done[b] if isinstance(steps_done, list) else steps_done)
+                if sq and b in sq:
+                    assert abs(got - sq[b]) <= 1e-9 * sq[b]
+
+
+@gpu
+@pytest.mark.parametrize("W,dtype,gs,off_by", [(1, B.PS_F32, 1.0, 0), (4, B.PS_F32, 0.25, 0), (3, B.PS_BF16, 1.0, 0),
+                                               (2, B.PS_F32, 1.0, 1), (5, B.PS_BF16, 0.5, 3), (40, B.PS_BF16, 1.0, 0)])
+def test_rounds(W, dtype, gs, off_by):
+    """Every kind of matrix, several iterations, aligned and unaligned shards."""
+    w = World([(64, 64), (1, 200), (200, 1), (130, 257), (300, 70), (128, 512), (1, 1)], W, dtype, gs)
+    for t in range(3):
+        sq = w.step(off_by=off_by)
+    w.check(3, sq)
+
+
+@gpu
+def test_large_blocks():
+    w = World([(1024, 1024), (1024, 2048), (2048, 520)] * 3, 2)
+    for t in range(2):
+        w.step()
+    w.check(2)
+
+
+@gpu
+def test_subsets_and_update_scales():
+    """Blocks that become ready in changing groups: tables of several sets, the same workspace."""
+    w = World([(96, 200), (64, 64), (300, 100), (40, 40)], 2, scales=[1.0, 0.0, -0.5, 2.0])
+    done = [0] * 4
+    for group in ([0, 1], [2], [3, 0], [0, 1], [1, 2, 3], [2], [0, 1, 2, 3], [3]):
+        w.step(group)
+        for b in group:
+            done[b] += 1
+    w.check(done)
+
+
+@gpu
+def test_more_sets_than_are_kept():
+    w = World([(8, 8)] * 12, 1)
+    done = [0] * 12
+    for k in range(80):                                     # 66 different pairs
+        group = sorted({k % 12, (k * 5 + 1 + k // 12) % 12})
+        w.step(group)
+        for b in group:
+            done[b] += 1
+    w.check(done)
+
+
+@gpu
+@pytest.mark.parametrize("overlap", [0, 1])
+def test_beside_other_jobs(overlap):
+    """One list with blocks of PS_MUON, SGD and Adam jobs: the others get what they get alone, to the bit."""
+    svc, alone = B.Service(0, 1, 1 << 26), B.Service(0, 1, 1 << 26)
+    svc.set_option(B.PS_OPT_OVERLAP, overlap)
+    w = World([(100, 60), (64, 256)], 2, svc=svc)
+    kinds = [dict(opt=B.PS_SGD, lr=0.1, momentum=0.9, weight_decay=1e-4), dict(opt=B.PS_ADAM, lr=1e-3)]
+    jobs = [(svc.register_job(num_workers=2, **k), alone.register_job(num_workers=2, **k)) for k in kinds]
+    init = torch.randn(5000, device="cuda")
+    for a, b in jobs:
+        svc.register_block(a, 0, 5000, 0, init)
+        alone.register_block(b, 0, 5000, 0, init)
+    for t in range(3):
+        grads = [[torch.randn(5000, device="cuda") for _ in range(2)] for _ in jobs]
+        for (a, b), gs in zip(jobs, grads):
+            for k, g in enumerate(gs):
+                svc.push(a, 0, k, g)
+                alone.push(b, 0, k, g)
+        w.step(extra=[(a, 0) for a, _ in jobs])
+        alone.aggregate([(b, 0) for _, b in jobs])
+        svc.join()
+        torch.cuda.synchronize()
+    w.check(3)
+    for a, b in jobs:
+        assert torch.equal(svc.view(svc.pull(a, 0), 5000), alone.view(alone.pull(b, 0), 5000))
+    kinds = {v["kernel"]: v["launches"] for v in svc.launch_stats(5)}
+    assert kinds["ps_aggregate_muon_kernel"] == 3
+
+
+@gpu
+@pytest.mark.parametrize("flags", [0, B.PS_ROUND_INPUTS_COMPLETE])
+def test_prepared_rounds_and_streams(flags):
+    """Rounds replayed on changing streams without waiting in between: they follow one another by themselves."""
+    w = World([(150, 90), (64, 300)], 3)
+    w.svc.set_option(B.PS_OPT_OVERLAP, 1)
+    bufs = [w.shards(b) for b in range(2)]
+    blocks = np.repeat(np.arange(2, dtype=np.int32), 3)
+    ranks = np.tile(np.arange(3, dtype=np.int32), 2)
+    ptrs = np.array([bufs[b][r].data_ptr() for b, r in zip(blocks, ranks)], np.uint64)
+    rnd = w.svc.round_prepare(np.full(6, w.job, np.int32), blocks, ranks, ptrs, [(w.job, 0), (w.job, 1)], flags)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    for t in range(7):
+        for b in range(2):
+            w.expect(b, bufs[b])
+        w.svc.round_run(rnd, streams[t % 3])
+    w.check(7)
+    out = np.zeros(2, np.uint64)
+    w.svc.round_run(rnd, None, out)
+    for b in range(2):
+        w.expect(b, bufs[b])
+    assert list(out) == [w.svc.pull(w.job, b) for b in range(2)]
+    w.check(8)
+
+
+@gpu
+def test_migration_and_unregistration():
+    w = World([(64, 100), (120, 50), (33, 77)], 2, contexts=2)
+    w.step()
+    w.svc.migrate_blocks([(w.job, 0), (w.job, 2)], 1)
+    w.step()
+    w.svc.migrate_block(w.job, 0, 0)
+    w.step()
+    w.check(3)
+    # to another service and back, with momentum and step
+    other = World([(120, 50)], 2)
+    n, step = w.svc.block_export(w.job, 1)
+    lane = torch.empty(n, device="cuda", dtype=torch.uint8)
+    w.svc.block_export(w.job, 1, lane, n)
+    torch.cuda.synchronize()
+    other.svc.block_import(other.job, 0, lane, n, step)
+    other.p[0], other.v[0], other.tol[0] = w.p[1], w.v[1], w.tol[1]
+    other.step()
+    other.check(4)
+    w.svc.unregister_block(w.job, 1)
+    w.svc.register_matrix(w.job, 1, 50, 20)
+    w.shapes[1], w.scales[1] = (50, 20), 0.2 * 50 ** 0.5
+    w.p[1], w.v[1], w.tol[1] = torch.zeros(50, 20, device="cuda", dtype=torch.float64), torch.zeros(50, 20, device="cuda"), 0.0
+    w.step()
+    w.check([4, 1, 4])
+
+
+@gpu
+def test_push_from_host_memory_and_profile():
+    w = World([(48, 80)], 2)
+    w.svc.set_option(B.PS_OPT_PROFILE, 1)
+    s = w.shards(0)
+    host = [x.cpu() for x in s]
+    for k, h in enumerate(host):
+        w.svc.push_host(w.job, 0, k, h)
+    w.svc.aggregate([(w.job, 0)])
+    w.expect(0, s)
+    w.check(1)
+    busy, span = w.svc.block_profile(w.job, 0)
+    assert busy > 0 and span > 0
+
+
+@gpu
+def test_not_finite_gradients_stay_in_their_block():
+    w = World([(40, 40), (64, 30)], 1)
+    bad = torch.zeros(1600, device="cuda")
+    bad[7] = float("inf")
+    good = w.shards(1)
+    w.svc.push(w.job, 0, 0, bad)
+    w.push(1, good)
+    w.expect(1, good)
+    w.svc.aggregate([(w.job, 0), (w.job, 1)])
+    torch.cuda.synchronize()
+    assert w.svc.device_status() == 0
+    assert w.svc.view(w.svc.pull(w.job, 0), 1600).isnan().all()
+    p = w.svc.view(w.svc.pull(w.job, 1), 64 * 30).view(64, 30)
+    assert float((p.double() - w.p[1]).norm()) <= w.tol[1]
+
+
+@gpu
+def test_a_failed_call_changes_nothing():
+    w = World([(40, 40), (64, 30)], 2)
+    s = w.shards(0)
+    w.push(0, s)
+    for ready, status in (([(w.job, 0), (w.job, 1)], B.PS_ERR_NOT_READY), ([(w.job, 0), (w.job, 0)], B.PS_ERR_DUPLICATE)):
+        with pytest.raises(B.PsError) as e:
+            w.svc.aggregate(ready)
+        assert e.value.status == status
+    with pytest.raises(B.PsError) as e:
+        w.svc.aggregate_clipped([(w.job, 0)], 1.0)
+    assert e.value.status == B.PS_ERR_BAD_ARG
+    w.expect(0, s)
+    w.svc.aggregate([(w.job, 0)])
+    w.check([1, 0])
+
+
+def planning():
+    s = B.Service(B.PS_DEVICE_NONE, 1, 1 << 24)
+    return s, s.register_job(opt=B.PS_MUON, num_workers=2)
+
+
+def refused(status, call, *a):
+    with pytest.raises(B.PsError) as e:
+        call(*a)
+    assert e.value.status == status
+
+
+def test_registration_refuses():
+    s, j = planning()
+    sgd = s.register_job(opt=B.PS_SGD, num_workers=2)
+    bad = B.PS_ERR_BAD_ARG
+    refused(bad, s.register_block, j, 0, 100)
+    refused(bad, s.register_matrix, sgd, 0, 10, 10)
+    refused(bad, s.register_matrix, 9, 0, 10, 10)
+    for rows, cols in ((0, 5), (5, 0), (-1, 5), ((1 << 20) + 1, 1)):
+        refused(bad, s.register_matrix, j, 0, rows, cols)
+    for scale in (float("nan"), float("inf")):
+        refused(bad, s.register_matrix, j, 0, 4, 4, 0, None, scale)
+    refused(bad, s.register_matrix, j, 0, 4, 4, 1)
+    refused(B.PS_ERR_NOMEM, s.register_matrix, j, 0, 4096, 4096)
+    s.register_matrix(j, 0, 30, 40)
+    refused(B.PS_ERR_DUPLICATE, s.register_matrix, j, 0, 30, 40)
+    refused(bad, s.register_job, 3)
+
+
+def test_planning_knows_matrices():
+    """Arena ranges, pushes, readiness and the chunk table work without a device; computing does not."""
+    s, j = planning()
+    s.register_matrix(j, 0, 300, 100)
+    s.register_matrix(j, 1, 7, 9)
+    assert s.arena_info(0)[0] == 2 * (120_064 + 256)         # parameters and momentum
+    for b in range(2):
+        for w in range(2):
+            s.push(j, b, w, 4096 * (1 + b * 2 + w))
+    refused(B.PS_ERR_BAD_ARG, s.push_rows, j, 0, 0, 4096, 1, 100, 4096)
+    plan = s.plan([(j, 0), (j, 1)])
+    assert sum(c.elem_count for c in plan) == 30_063
+    refused(B.PS_ERR_NO_DEVICE, s.aggregate, [(j, 0), (j, 1)])
+    refused(B.PS_ERR_NO_DEVICE, s.aggregate_clipped, [(j, 0)], 1.0)
+    n, step = s.block_export(j, 0)
+    assert n == 2 * 120_064 and step == 0
+
+
+def test_noalloc_refuses():
+    d = B.ps_job_desc(B.PS_MUON, B.PS_F32, 1, 0.1, 0.9, 0, 0, 0, 0, 1)
+    refused(B.PS_ERR_BAD_ARG, B.ps_aggregate_block_noalloc, d, 1, 16, 4096, 8192, None, [4096])
