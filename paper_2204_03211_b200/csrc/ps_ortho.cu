@@ -6,8 +6,8 @@
 #include <mutex>
 #include <new>
 
-#include "ps_ortho.cuh"
 #include "ps_ortho.h"
+#include "ps_ortho_small.cuh"
 
 namespace psb {
 namespace {
@@ -56,6 +56,9 @@ int ns_device(bool split, bool pair, int* room) {
         if (e != cudaSuccess) return op_cuda_error("preparing the orthogonalisation", e);
         n.room[s][p] = std::max(1, std::min(clusters, d.num_sms / k.ctas));
       }
+    cudaError_t e = cudaFuncSetAttribute(ps_ortho_small_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSoSmem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(ps_ortho_small_kernel<2>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSoSmem);
+    if (e != cudaSuccess) return op_cuda_error("preparing the orthogonalisation", e);
     n.ready = true;
   }
   *room = n.room[split][pair];
@@ -120,7 +123,44 @@ constexpr long long kNsPairsFrom = 200;
 
 }  // namespace
 
+// A list of small matrices only stays in shared memory: CTAs per matrix, 0 for other lists.  There one matrix may be done
+// before another is read, so a result that lies where another matrix comes from takes the general form, which reads all
+// sources first.
+static int small_ctas(const std::vector<NsItem>& items) {
+  struct Range { uintptr_t first, end; int of; };
+  std::vector<Range> srcs;
+  long long widest = 0;
+  uintptr_t longest = 0;
+  auto range = [](const void* p, long long ld, const NsItem& it, size_t es, int of) {
+    const uintptr_t first = reinterpret_cast<uintptr_t>(p);
+    return Range{first, first + ((size_t)(it.rows - 1) * (size_t)ld + (size_t)it.cols) * es, of};
+  };
+  for (size_t i = 0; i < items.size(); ++i) {
+    const NsItem& it = items[i];
+    if (empty(it)) continue;
+    if (std::min(it.rows, it.cols) > kSoRows || std::max(it.rows, it.cols) > kSoCtas * kSoCols) return 0;
+    widest = std::max(widest, std::max(it.rows, it.cols));
+    srcs.push_back(range(it.src, it.ld_src, it, it.src_bf16 ? 2 : 4, (int)i));
+    longest = std::max(longest, srcs.back().end - srcs.back().first);
+  }
+  if (srcs.empty()) return 0;
+  std::sort(srcs.begin(), srcs.end(), [](const Range& a, const Range& b) { return a.first < b.first; });
+  for (size_t i = 0; i < items.size(); ++i) {
+    const NsItem& it = items[i];
+    if (empty(it) || !it.dst) continue;
+    const Range d = range(it.dst, it.ld_dst, it, it.out == kNsOutBf16 ? 2 : 4, (int)i);
+    const uintptr_t reach = d.first > longest ? d.first - longest : 0;       // (only sources that start from here on can overlap)
+    auto s = std::lower_bound(srcs.begin(), srcs.end(), reach, [](const Range& a, uintptr_t v) { return a.first < v; });
+    for (; s != srcs.end() && s->first < d.end; ++s)
+      if (s->of != d.of && s->end > d.first) return 0;
+  }
+  int ctas = 1;
+  while (ctas * kSoCols < widest) ctas *= 2;
+  return ctas;
+}
+
 size_t NsPlan::workspace(const std::vector<NsItem>& items, bool split) {
+  if (small_ctas(items)) return 256;
   size_t at = 0;
   long long tiles = 0, units = 0;
   for (const NsItem& it : items) {
@@ -141,7 +181,8 @@ NsPlan::~NsPlan() {
 }
 
 int NsPlan::build(const std::vector<NsItem>& items, bool split, void* workspace, int* status) {
-  // Single CTAs with 128 x 128 where pairs would have few tiles.
+  small_ = small_ctas(items);
+  // single CTAs with 128 x 128 where pairs would have few tiles
   long long large = 0;
   for (const NsItem& it : items)
     if (!empty(it)) large += ceil_div(it.rows, 256) * ceil_div(it.cols, 256);
@@ -159,7 +200,7 @@ int NsPlan::build(const std::vector<NsItem>& items, bool split, void* workspace,
     if (!empty(it)) live.push_back(&it);
   const size_t n = live.size();
   if (n == 0) return PS_OK;
-  std::vector<CUtensorMap> maps(kNsMaps * n);
+  std::vector<CUtensorMap> maps(small_ ? 0 : kNsMaps * n);
   std::vector<NsMat> mats(n);
   std::vector<NsTile> list;
   std::vector<int2> units;
@@ -169,14 +210,24 @@ int NsPlan::build(const std::vector<NsItem>& items, bool split, void* workspace,
   long long sym_tiles = 0;
   for (size_t i = 0; i < n; ++i) {
     const NsItem& it = *live[i];
-    const NsLayout l = layout(it, split, at);
-    at = l.end;
     NsMat& M = mats[i];
-    auto half_at = [&](size_t o) { return reinterpret_cast<__half*>(ws + o); };
-    M.m = (int)l.m;
-    M.n = (int)l.n;
+    M.m = (int)std::min(it.rows, it.cols);
+    M.n = (int)std::max(it.rows, it.cols);
     M.flip = it.rows > it.cols;
     M.out = it.out;
+    M.src = it.src;
+    M.ld_src = it.ld_src;
+    M.src_bf16 = it.src_bf16;
+    M.dst = it.dst;
+    M.ld_dst = it.ld_dst;
+    const size_t es = it.out == kNsOutBf16 ? 2 : 4;
+    M.wide = !M.flip && (reinterpret_cast<uintptr_t>(it.dst) & 31u) == 0 && it.ld_dst * (long long)es % 32 == 0;
+    M.decay = it.decay;
+    M.step = it.step;
+    if (small_) continue;
+    const NsLayout l = layout(it, split, at);
+    at = l.end;
+    auto half_at = [&](size_t o) { return reinterpret_cast<__half*>(ws + o); };
     M.pitch_x = l.pitch_x;
     M.pitch_e = l.pitch_e;
     bool ok = true;
@@ -201,18 +252,9 @@ int NsPlan::build(const std::vector<NsItem>& items, bool split, void* workspace,
     if (!ok) return op_cuda_error("tensor map", cudaErrorInvalidValue);
     M.d = reinterpret_cast<float*>(ws + l.d);
     M.fd = reinterpret_cast<float*>(ws + l.fd);
-    M.src = it.src;
-    M.ld_src = it.ld_src;
-    M.src_bf16 = it.src_bf16;
     M.parts = it.parts ? it.parts : reinterpret_cast<double*>(ws + l.parts);
     M.nparts = it.parts ? it.nparts : (int)l.units;
     if (!it.parts) norms_ = true;
-    M.dst = it.dst;
-    M.ld_dst = it.ld_dst;
-    const size_t es = it.out == kNsOutBf16 ? 2 : 4;
-    M.wide = !M.flip && (reinterpret_cast<uintptr_t>(it.dst) & 31u) == 0 && it.ld_dst * (long long)es % 32 == 0;
-    M.decay = it.decay;
-    M.step = it.step;
     const int tm = (int)ceil_div(l.m, tile), tn = (int)ceil_div(l.n, tile);
     for (int a = 0; a < tm; ++a) {
       const int ctas = pair_ && l.m - a * tile > 128 ? 2 : 1;
@@ -224,7 +266,7 @@ int NsPlan::build(const std::vector<NsItem>& items, bool split, void* workspace,
   }
   // the tiles: matrices dealt to groups, a group's products one kind after the other
   const size_t groups = (size_t)std::max<long long>(1, std::min<long long>((long long)n, sym_tiles / kNsGroupTiles));
-  for (size_t g = 0; g < groups; ++g)
+  for (size_t g = 0; !small_ && g < groups; ++g)
     for (int step = 0; step < kNsSteps; ++step)
       for (int product = 0; product < 3; ++product)
         for (size_t i = g; i < n; i += groups) {
@@ -254,7 +296,7 @@ int NsPlan::build(const std::vector<NsItem>& items, bool split, void* workspace,
     mats[i].done = reinterpret_cast<unsigned int*>(mem_ + done_off) + 32 * i;
   }
   auto put = [&](size_t o, const void* p, size_t bytes) {
-    if (e == cudaSuccess) e = cudaMemcpy(mem_ + o, p, bytes, cudaMemcpyHostToDevice);
+    if (e == cudaSuccess && bytes) e = cudaMemcpy(mem_ + o, p, bytes, cudaMemcpyHostToDevice);
   };
   put(maps_off, maps.data(), maps.size() * sizeof(CUtensorMap));
   put(mats_off_, mats.data(), n * sizeof(NsMat));
@@ -264,6 +306,7 @@ int NsPlan::build(const std::vector<NsItem>& items, bool split, void* workspace,
   if (e == cudaSuccess) e = cudaStreamSynchronize(cudaStreamLegacy);   // before other streams use it
   if (e != cudaSuccess) return op_cuda_error("tables of the orthogonalisation", e);
   status_ = status ? status : reinterpret_cast<int*>(mem_ + status_off);
+  count_ = (int)n;
   tiles_ = (int)list.size();
   units_ = (int)units.size();
   grid_ = (pair_ ? 2 : 1) * std::min(tiles_, room);
@@ -273,9 +316,14 @@ int NsPlan::build(const std::vector<NsItem>& items, bool split, void* workspace,
 
 int NsPlan::run(cudaStream_t stream, int* launches) const {
   if (launches) *launches = 0;
-  if (!tiles_) return PS_OK;
+  if (!count_) return PS_OK;
   const NsMat* mats = reinterpret_cast<const NsMat*>(mem_ + mats_off_);
   const int2* units = reinterpret_cast<const int2*>(mem_ + units_off_);
+  if (small_) {
+    if (launches) *launches = 1;
+    return op_launch("orthogonalisation", split_ ? ps_ortho_small_kernel<2> : ps_ortho_small_kernel<1>, (unsigned)(count_ * small_),
+                     kSoThreads, kSoSmem, small_, stream, SoArgs{mats, status_, small_});
+  }
   int rc = PS_OK;
   if (norms_) rc = op_launch("orthogonalisation", ps_ortho_norm_kernel, (unsigned)units_, kNsThreads, 0, 1, stream, mats, units);
   if (!rc) rc = op_launch("orthogonalisation", ps_ortho_prepare_kernel, (unsigned)units_, kNsThreads, 0, 1, stream, mats, units);

@@ -88,6 +88,56 @@ __device__ __forceinline__ void ns_split(float v, __half& hi, __half& lo) {
 }
 __device__ __forceinline__ float2 ns_widen(unsigned int u) { return __half22float2(*reinterpret_cast<const __half2*>(&u)); }
 
+// The last step's result, scaled, of this lane's row: along a row of dst, or down a column, where the warp's lanes are
+// neighbours.// (i: row, j: first column, `count` of them)
+__device__ __forceinline__ void ns_result(const NsMat& M, float (&v)[32], int i, int j, int count) {
+  constexpr float s = 1.f / kNsScaleX;
+#pragma unroll
+  for (int k = 0; k < 32; ++k) v[k] *= s;
+  const long long step = M.flip ? M.ld_dst : 1;
+  const size_t at0 = M.flip ? (size_t)j * (size_t)M.ld_dst + (size_t)i : (size_t)i * (size_t)M.ld_dst + (size_t)j;
+  if (M.out == kNsOutBf16) {
+    __nv_bfloat16* p = static_cast<__nv_bfloat16*>(M.dst) + at0;
+    if (M.wide && count >= 32) {
+      unsigned int u[16];
+#pragma unroll
+      for (int k = 0; k < 16; ++k) u[k] = mm_bf16x2(v[2 * k], v[2 * k + 1]);
+      store_sector(p, u);
+      store_sector(p + 16, u + 8);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 32; ++k)
+        if (k < count) p[k * step] = __float2bfloat16_rn(v[k]);
+    }
+    return;
+  }
+  float* p = static_cast<float*>(M.dst) + at0;
+  const bool update = M.out == kNsOutUpdate;
+  const float decay = M.decay, rate = M.step;
+  if (M.wide && count >= 32) {
+    if (update) {
+#pragma unroll
+      for (int k = 0; k < 32; k += 4) {
+        const float4 q = *reinterpret_cast<const float4*>(p + k);
+        v[k] = q.x * decay - rate * v[k];
+        v[k + 1] = q.y * decay - rate * v[k + 1];
+        v[k + 2] = q.z * decay - rate * v[k + 2];
+        v[k + 3] = q.w * decay - rate * v[k + 3];
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 32; k += 8) store_sector(p + k, reinterpret_cast<const unsigned int*>(v) + k);
+  } else if (update) {
+#pragma unroll
+    for (int k = 0; k < 32; ++k)
+      if (k < count) p[k * step] = p[k * step] * decay - rate * v[k];
+  } else {
+#pragma unroll
+    for (int k = 0; k < 32; ++k)
+      if (k < count) p[k * step] = v[k];
+  }
+}
+
 template <int PLANES, bool PAIR>
 struct NsOp {
   static constexpr bool kPair = PAIR;
@@ -329,57 +379,7 @@ struct NsOp {
         return;
       }
       hand_over();
-      if (i < M.m) result(v, j);
-    }
-
-    // O: along a row of dst, or down a column, where the warp's lanes are neighbours.
-    __device__ __forceinline__ void result(float (&v)[32], int j) {
-      constexpr float s = 1.f / kNsScaleX;
-      const int count = min(32, M.n - j);
-#pragma unroll
-      for (int k = 0; k < 32; ++k) v[k] *= s;
-      const long long step = M.flip ? M.ld_dst : 1;
-      const size_t at0 = M.flip ? (size_t)j * (size_t)M.ld_dst + (size_t)i : (size_t)i * (size_t)M.ld_dst + (size_t)j;
-      if (M.out == kNsOutBf16) {
-        __nv_bfloat16* p = static_cast<__nv_bfloat16*>(M.dst) + at0;
-        if (M.wide && count >= 32) {
-          unsigned int u[16];
-#pragma unroll
-          for (int k = 0; k < 16; ++k) u[k] = mm_bf16x2(v[2 * k], v[2 * k + 1]);
-          store_sector(p, u);
-          store_sector(p + 16, u + 8);
-        } else {
-#pragma unroll
-          for (int k = 0; k < 32; ++k)
-            if (k < count) p[k * step] = __float2bfloat16_rn(v[k]);
-        }
-        return;
-      }
-      float* p = static_cast<float*>(M.dst) + at0;
-      const bool update = M.out == kNsOutUpdate;
-      const float decay = M.decay, rate = M.step;
-      if (M.wide && count >= 32) {
-        if (update) {
-#pragma unroll
-          for (int k = 0; k < 32; k += 4) {
-            const float4 q = *reinterpret_cast<const float4*>(p + k);
-            v[k] = q.x * decay - rate * v[k];
-            v[k + 1] = q.y * decay - rate * v[k + 1];
-            v[k + 2] = q.z * decay - rate * v[k + 2];
-            v[k + 3] = q.w * decay - rate * v[k + 3];
-          }
-        }
-#pragma unroll
-        for (int k = 0; k < 32; k += 8) store_sector(p + k, reinterpret_cast<const unsigned int*>(v) + k);
-      } else if (update) {
-#pragma unroll
-        for (int k = 0; k < 32; ++k)
-          if (k < count) p[k * step] = p[k * step] * decay - rate * v[k];
-      } else {
-#pragma unroll
-        for (int k = 0; k < 32; ++k)
-          if (k < count) p[k * step] = v[k];
-      }
+      if (i < M.m) ns_result(M, v, i, j, min(32, M.n - j));
     }
 
     __device__ __forceinline__ void end() {}

@@ -72,7 +72,8 @@ def check(x, out):
 
 
 SHAPES = [(1, 1), (1, 50), (50, 1), (2, 3), (16, 16), (31, 33), (64, 64), (65, 200), (128, 128), (129, 127), (300, 300),
-          (128, 1000), (777, 300), (257, 513), (600, 130)]
+          (128, 1000), (777, 300), (257, 513), (600, 130),
+          (100, 2048), (2048, 77), (16, 300), (128, 257), (1, 1025), (100, 2049), (512, 128)]
 
 
 @gpu
@@ -93,9 +94,11 @@ def test_shapes(rows, cols, kind):
 @gpu
 @pytest.mark.parametrize("dst", [F32, BF])
 def test_a_list_of_many_shapes(dst):
-    """Pairs of CTAs (enough large tiles) and single ones, matrices of one tile next to matrices of many, empty ones."""
+    """Pairs of CTAs (enough large tiles) and single ones, matrices of one tile next to matrices of many, empty ones; and a
+    list of small ones only, which clusters of CTAs keep in shared memory."""
+    tiny = [(3, 700), (64, 64), (0, 9), (128, 384), (1100, 90), (17, 1), (128, 128)] * 30
     small = [(5, 7), (0, 4), (200, 40), (128, 384), (3, 0), (130, 130), (64, 64)]
-    for shapes in (small, small + [(512, 2100)] * 12, [(1100, 700)] * 15 + [(260, 30)]):
+    for shapes in (tiny, small, small + [(512, 2100)] * 12, [(1100, 700)] * 15 + [(260, 30)]):
         xs = [matrix(r, c, "normal" if k % 2 else "decaying", k) for k, (r, c) in enumerate(shapes)]
         outs = [torch.full((r, c), 9.0, device="cuda", dtype=dst) for r, c in shapes]
         o = B.Ortho(xs, outs)
