@@ -154,8 +154,11 @@ static int small_ctas(const std::vector<NsItem>& items) {
     for (; s != srcs.end() && s->first < d.end; ++s)
       if (s->of != d.of && s->end > d.first) return 0;
   }
-  int ctas = 1;
-  while (ctas * kSoCols < widest) ctas *= 2;
+  // One CTA where it can hold a matrix.  Else 128 columns each rather than 256: what every CTA does for itself gets shorter,
+  // adding up A does not get longer (128 x 512: MEASURE)
+  if (widest <= kSoCols) return 1;
+  int ctas = 2;
+  while (ctas < kSoCtas && ctas * (kSoCols / 2) < widest) ctas *= 2;
   return ctas;
 }
 

@@ -74,12 +74,27 @@ struct NsArgs {
   int tiles;
 };
 
+// c + a and c - a for the lower and the upper of two fp16 numbers: mixed-precision additions widen as they add.
+__device__ __forceinline__ float2 ns_add(unsigned int a, float2 c) {
+  float2 r;
+  asm("{\n\t"
+      ".reg .b16 l, h;\n\t"
+      "mov.b32 {l, h}, %2;\n\t"
+      "add.rn.f32.f16 %0, l, %3;\n\t"
+      "add.rn.f32.f16 %1, h, %4;\n\t"
+      "}"
+      : "=f"(r.x), "=f"(r.y)
+      : "r"(a), "f"(c.x), "f"(c.y));
+  return r;
+}
+__device__ __forceinline__ float2 ns_sub(unsigned int a, float2 c) { return ns_add(a ^ 0x80008000u, c); }
+
 // Two values as high and low halves: fp16 numbers whose sums they are (to 22 bits).
 __device__ __forceinline__ void ns_split2(float a, float b, unsigned int& hi, unsigned int& lo) {
   const __half2 h = __floats2half2_rn(a, b);
-  const float2 f = __half22float2(h);
-  const __half2 l = __floats2half2_rn(a - f.x, b - f.y);
   hi = *reinterpret_cast<const unsigned int*>(&h);
+  const float2 r = ns_sub(hi, make_float2(a, b));
+  const __half2 l = __floats2half2_rn(r.x, r.y);
   lo = *reinterpret_cast<const unsigned int*>(&l);
 }
 __device__ __forceinline__ void ns_split(float v, __half& hi, __half& lo) {
@@ -344,9 +359,8 @@ struct NsOp {
         const unsigned int h[4] = {h4.x, h4.y, h4.z, h4.w}, l[4] = {l4.x, l4.y, l4.z, l4.w};
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-          const float2 h2 = ns_widen(h[q >> 1]), l2 = ns_widen(l[q >> 1]);
-          float e = q & 1 ? h2.y : h2.x;
-          if constexpr (PLANES == 2) e += q & 1 ? l2.y : l2.x;
+          const float2 e2 = PLANES == 2 ? ns_add(l[q >> 1], ns_widen(h[q >> 1])) : ns_widen(h[q >> 1]);
+          const float e = q & 1 ? e2.y : e2.x;
           // (b e + c (sum + (d_i + d_j) e)) in F's scale, e and sum in E's and its square
           const float sum = v[k + q];
           diagonal = k + q == k0 ? sum : diagonal;
@@ -368,9 +382,9 @@ struct NsOp {
         const unsigned int h[4] = {h4.x, h4.y, h4.z, h4.w}, l[4] = {l4.x, l4.y, l4.z, l4.w};
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const float2 h2 = ns_widen(h[q]), l2 = ns_widen(l[q]);
-          v[k + 2 * q] = fmaf(t, h2.x + l2.x, v[k + 2 * q] * kInvF);
-          v[k + 2 * q + 1] = fmaf(t, h2.y + l2.y, v[k + 2 * q + 1] * kInvF);
+          const float2 x = ns_add(l[q], ns_widen(h[q]));
+          v[k + 2 * q] = fmaf(t, x.x, v[k + 2 * q] * kInvF);
+          v[k + 2 * q + 1] = fmaf(t, x.y, v[k + 2 * q + 1] * kInvF);
         }
       }
       if (!last) {

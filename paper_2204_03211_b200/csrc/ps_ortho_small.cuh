@@ -26,7 +26,8 @@ struct SoControl {
   unsigned long long bar;
   double norm[kSoCtas];
   double red[kSoThreads / 32];
-  float d[kSoRows], fd[kSoRows];
+  alignas(16) float d[kSoRows];
+  float fd[kSoRows];
   unsigned int tmem;
 };
 constexpr int kSoSmem = kSoX + kSoE + 2048;
@@ -78,20 +79,51 @@ ps_ortho_small_kernel(const __grid_constant__ SoArgs args) {
   mm_pdl();
 
   // ---- norm, and X0 as two planes (rows from m on and columns from `cols` on are zeros)
+  // (pieces of eight columns of a row; neighbouring lanes take neighbours along the source's rows)
   const bool flip = M.flip != 0;
-  auto source = [&](int r, int c) {                      // X[r][c0 + c]
+  const int pieces = (cols + 7) / 8, units = m * pieces;
+  const bool vec = !flip && (M.ld_src & 7) == 0 && (reinterpret_cast<uintptr_t>(M.src) & 31u) == 0;
+  auto fetch = [&](int u, float (&v)[8], int& r, int& piece) {
+    r = flip ? u % m : u / pieces;
+    piece = flip ? u / m : u - r * pieces;
+    const int c = piece * 8, live = min(8, cols - c);
     const size_t at = flip ? (size_t)(c0 + c) * (size_t)M.ld_src + (size_t)r : (size_t)r * (size_t)M.ld_src + (size_t)(c0 + c);
-    return ns_source(M, at);
-  };
-  // lanes run along the source's rows
-  const int fast = flip ? m : cols, slow = flip ? cols : m;
-  double sq = 0.0;
-  for (int s = warp; s < slow; s += kSoThreads / 32)
-#pragma unroll 4
-    for (int f = lane; f < fast; f += 32) {
-      const double v = (double)(flip ? source(f, s) : source(s, f));
-      sq = fma(v, v, sq);
+    const size_t next = flip ? (size_t)M.ld_src : 1;
+    if (vec && live == 8) {
+      if (M.src_bf16) {
+        const uint4 q = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(M.src) + at);
+        const unsigned int w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(k & 1 ? w[k >> 1] & 0xffff0000u : w[k >> 1] << 16);
+      } else {
+        const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(M.src) + at);
+        const float4 x = q[0], y = q[1];
+        v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+        v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+      }
+    } else if (M.src_bf16) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        v[k] = k < live ? __bfloat162float(static_cast<const __nv_bfloat16*>(M.src)[at + k * next]) : 0.f;
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = k < live ? static_cast<const float*>(M.src)[at + k * next] : 0.f;
     }
+  };
+  constexpr int kBatch = 4;                              // pieces in flight per thread
+  double sq = 0.0;
+  for (int u0 = tid; u0 < units; u0 += kBatch * kSoThreads) {
+    float v[kBatch][8];
+    int r, piece;
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k)
+      if (u0 + k * kSoThreads < units) fetch(u0 + k * kSoThreads, v[k], r, piece);
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k)
+      if (u0 + k * kSoThreads < units)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) sq = fma((double)v[k][q], (double)v[k][q], sq);
+  }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sq += __shfl_down_sync(0xffffffffu, sq, o);
   if (lane == 0) ctl.red[warp] = sq;
@@ -111,16 +143,23 @@ ps_ortho_small_kernel(const __grid_constant__ SoArgs args) {
   for (int k = 1; k < ctas; ++k) total += ctl.norm[k];
   const float scale = (float)((double)kNsScaleX / (sqrt(total) + kNsEps));
   const unsigned int lo_at = (unsigned int)(blocks * kSoBlock);     // the low plane follows the high one
-  for (int s = warp; s < slow; s += kSoThreads / 32)
-#pragma unroll 4
-    for (int f = lane; f < fast; f += 32) {
-      const int r = flip ? f : s, c = flip ? s : f;
-      __half hi, lo;
-      ns_split(source(r, c) * scale, hi, lo);
-      unsigned char* p = xs + so_piece(r, c >> 3) + (c & 7) * 2;
-      *reinterpret_cast<__half*>(p) = hi;
-      *reinterpret_cast<__half*>(p + lo_at) = lo;
-    }
+  for (int u0 = tid; u0 < units; u0 += kBatch * kSoThreads) {
+    float v[kBatch][8];
+    int r[kBatch], piece[kBatch];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k)
+      if (u0 + k * kSoThreads < units) fetch(u0 + k * kSoThreads, v[k], r[k], piece[k]);
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k)
+      if (u0 + k * kSoThreads < units) {
+        unsigned int hi[4], lo[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) ns_split2(v[k][2 * q] * scale, v[k][2 * q + 1] * scale, hi[q], lo[q]);
+        unsigned char* p = xs + so_piece(r[k], piece[k]);
+        *reinterpret_cast<uint4*>(p) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        *reinterpret_cast<uint4*>(p + lo_at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+      }
+  }
   asm volatile("fence.proxy.async;" ::: "memory");
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
@@ -129,29 +168,38 @@ ps_ortho_small_kernel(const __grid_constant__ SoArgs args) {
   const unsigned int xa = mm_smem(xs), ea = mm_smem(es), bar = mm_smem(&ctl.bar);
   const unsigned int mine = tmem + ((unsigned)((warp & 3) * 32) << 16);
   const int row = (warp & 3) * 32 + lane, part = warp >> 2;        // part: which 32 of 128 columns
+  const bool busy = (warp & 3) * 32 < m;                 // (the other rows stay zeros)
   unsigned int parity = 0;
 
-  // All products of one kind, by one thread: D (+)= A B^T over `steps` times 16 of k.  The strides of a step, and of every
-  // fourth one where k runs along rows of 64 elements.
+  // All products of one kind, by one elected lane: D = A B^T over k in [k0, k1), in units of 16.  Addresses advance by 32
+  // bytes along rows of 64 elements and by a block after them, or by 16 rows where k runs down the columns.
+  const bool issuer = warp == 0 && mm_elect();
   auto products = [&](unsigned int d, unsigned int a, unsigned int a_lo, unsigned int b, unsigned int b_lo, bool b_mn, int k0, int k1,
                       int cols_b) {
     const unsigned int idesc = (1u << 4) | ((unsigned)b_mn << 16) | ((unsigned)(cols_b >> 3) << 17) | (8u << 24);
-    auto desc = [&](unsigned int base, int k, bool mn) {
-      const unsigned int at = base + (mn ? (unsigned)k * 2048u : (unsigned)(k >> 2) * kSoBlock + (unsigned)(k & 3) * 32u);
-      return (unsigned long long)((at & 0x3ffffu) >> 4) | ((unsigned long long)(mn ? kSoBlock / 16 : 1) << 16) | (64ull << 32) |
-             (1ull << 46) | (2ull << 61);
-    };
+    const unsigned long long flags = (64ull << 32) | (1ull << 46) | (2ull << 61);
+    const unsigned long long da = (unsigned long long)((a & 0x3ffffu) >> 4) | (1ull << 16) | flags;
+    const unsigned long long db =
+        (unsigned long long)((b & 0x3ffffu) >> 4) | ((unsigned long long)(b_mn ? kSoBlock / 16 : 1) << 16) | flags;
+    const unsigned int step = b_mn ? 128u : 2u, block = b_mn ? 512u : kSoBlock / 16;
+    const unsigned int al = a_lo / 16, bl = b_lo / 16;
     bool more = false;
-    if (PLANES == 2)
-      for (int k = k0; k < k1; ++k) {
-        tc_mma<false>(d, desc(a, k, false), desc(b + b_lo, k, b_mn), idesc, more);
-        tc_mma<false>(d, desc(a + a_lo, k, false), desc(b, k, b_mn), idesc, true);
-        more = true;
+#pragma unroll
+    for (int pass = PLANES == 2 ? 0 : 1; pass < 2; ++pass)
+      for (int kb = k0 / 4; kb * 4 < k1; ++kb) {
+        const unsigned long long pa = da + (unsigned)kb * (kSoBlock / 16), pb = db + (unsigned)kb * block;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (kb * 4 + i >= k1) break;
+          if (pass == 0) {
+            tc_mma<false>(d, pa + i * 2, pb + i * step + bl, idesc, more);
+            tc_mma<false>(d, pa + i * 2 + al, pb + i * step, idesc, true);
+          } else {
+            tc_mma<false>(d, pa + i * 2, pb + i * step, idesc, more);
+          }
+          more = true;
+        }
       }
-    for (int k = k0; k < k1; ++k) {
-      tc_mma<false>(d, desc(a, k, false), desc(b, k, b_mn), idesc, more);
-      more = true;
-    }
   };
   // The sums are there (a wait that runs out is noted; the steps go on, so that a cluster's CTAs stay together).
   auto finished = [&] {
@@ -181,10 +229,10 @@ ps_ortho_small_kernel(const __grid_constant__ SoArgs args) {
   };
 
   const int ksteps_m = mp / 16;
-  const int ksteps_n = blocks * 4, half = ksteps_n > 8 ? ksteps_n / 2 : ksteps_n;
+  const int ksteps_n = blocks * 4, half = blocks > 2 ? blocks / 2 * 4 : ksteps_n;
   for (int step = 0; step < kNsSteps; ++step) {
     // ---- A = X X^T, over this CTA's columns in two parts
-    if (tid == 0) {
+    if (issuer) {
       if (blocks > 0) {
         products(tmem, xa, lo_at, xa, lo_at, false, 0, half, mp);
         if (half < ksteps_n) products(tmem + 128, xa, lo_at, xa, lo_at, false, half, ksteps_n, mp);
@@ -195,7 +243,7 @@ ps_ortho_small_kernel(const __grid_constant__ SoArgs args) {
     {
       constexpr float s = kNsScaleE / (kNsScaleX * kNsScaleX);
       float v[32];
-      if (part * 32 < mp) {
+      if (part * 32 < mp && busy) {
         if (blocks > 0) mm_load<32>(mine + part * 32, v);
         else
 #pragma unroll
@@ -224,7 +272,7 @@ ps_ortho_small_kernel(const __grid_constant__ SoArgs args) {
           v[k] = k == k0 ? 0.f : v[k];
         }
         if (k0 >= 0 && k0 < 32) ctl.d[row] = diagonal * (1.f / kNsScaleE);
-        put_e(v);
+        if (step == 0 || (busy && part * 32 < mp)) put_e(v);      // (what is zero stays zero)
       } else {
 #pragma unroll
         for (int k = 0; k < 32; k += 4)
@@ -284,12 +332,12 @@ ps_ortho_small_kernel(const __grid_constant__ SoArgs args) {
     handed_over();
 
     // ---- B, of which F is what is off the diagonal, in E's place (every CTA of a cluster for itself)
-    if (tid == 0) {
+    if (issuer) {
       products(tmem, ea, 2 * kSoBlock, ea, 2 * kSoBlock, false, 0, ksteps_m, mp);
       mm_commit(bar);
     }
     finished();
-    if (part * 32 < mp) {
+    if (part * 32 < mp && busy) {
       constexpr float kInvE = 1.f / kNsScaleE;
       float v[32];
       mm_load<32>(mine + part * 32, v);
@@ -307,14 +355,15 @@ ps_ortho_small_kernel(const __grid_constant__ SoArgs args) {
         uint4 l4 = make_uint4(0, 0, 0, 0);
         if (PLANES == 2) l4 = *reinterpret_cast<const uint4*>(p + 2 * kSoBlock);
         const unsigned int h[4] = {h4.x, h4.y, h4.z, h4.w}, l[4] = {l4.x, l4.y, l4.z, l4.w};
+        const float4 d0 = *reinterpret_cast<const float4*>(ctl.d + part * 32 + k), d1 = *reinterpret_cast<const float4*>(ctl.d + part * 32 + k + 4);
+        const float dj[8] = {d0.x, d0.y, d0.z, d0.w, d1.x, d1.y, d1.z, d1.w};
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-          const float2 h2 = ns_widen(h[q >> 1]), l2 = ns_widen(l[q >> 1]);
-          float e = q & 1 ? h2.y : h2.x;
-          if (PLANES == 2) e += q & 1 ? l2.y : l2.x;
+          const float2 e2 = PLANES == 2 ? ns_add(l[q >> 1], ns_widen(h[q >> 1])) : ns_widen(h[q >> 1]);
+          const float e = q & 1 ? e2.y : e2.x;
           const float sum = v[k + q];
           diagonal = k + q == k0 ? sum : diagonal;
-          const float g = fmaf(kNsC * kNsScaleF * kInvE, di + ctl.d[part * 32 + k + q], kNsB * kNsScaleF * kInvE);
+          const float g = fmaf(kNsC * kNsScaleF * kInvE, di + dj[q], kNsB * kNsScaleF * kInvE);
           v[k + q] = k + q == k0 ? 0.f : fmaf(g, e, sum * (kNsC * kNsScaleF * kInvE * kInvE));
         }
       }
@@ -327,7 +376,7 @@ ps_ortho_small_kernel(const __grid_constant__ SoArgs args) {
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 
     // ---- X = (a + f) X + F X, in X's place
-    if (tid == 0) {
+    if (issuer) {
       if (blocks > 0) products(tmem, ea, 2 * kSoBlock, xa, lo_at, true, 0, ksteps_m, np);
       mm_commit(bar);
     }
@@ -335,29 +384,38 @@ ps_ortho_small_kernel(const __grid_constant__ SoArgs args) {
     const bool last = step == kNsSteps - 1;
     const float t = row < m ? kNsA + ctl.fd[row] : 0.f;
 #pragma unroll 1
-    for (int c = part * 32; c < np; c += 128) {
+    for (int c = part * 32; c < np && busy; c += 128) {
       constexpr float kInvF = 1.f / kNsScaleF;
       float v[32];
       mm_load<32>(mine + c, v);
+      uint4 h4[4], l4[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        unsigned char* p = xs + so_piece(row, c / 8 + k);
-        const uint4 h4 = *reinterpret_cast<const uint4*>(p), l4 = *reinterpret_cast<const uint4*>(p + lo_at);
-        const unsigned int h[4] = {h4.x, h4.y, h4.z, h4.w}, l[4] = {l4.x, l4.y, l4.z, l4.w};
-        unsigned int hi[4], lo[4];
+        const unsigned char* p = xs + so_piece(row, c / 8 + k);
+        h4[k] = *reinterpret_cast<const uint4*>(p);
+        l4[k] = *reinterpret_cast<const uint4*>(p + lo_at);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        unsigned int h[4] = {h4[k].x, h4[k].y, h4[k].z, h4[k].w}, l[4] = {l4[k].x, l4[k].y, l4[k].z, l4[k].w};
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const float2 h2 = ns_widen(h[q]), l2 = ns_widen(l[q]);
+          const float2 x = ns_add(l[q], ns_widen(h[q]));
           float &a = v[8 * k + 2 * q], &b = v[8 * k + 2 * q + 1];
-          a = fmaf(t, h2.x + l2.x, a * kInvF);
-          b = fmaf(t, h2.y + l2.y, b * kInvF);
-          ns_split2(a, b, hi[q], lo[q]);
+          a = fmaf(t, x.x, a * kInvF);
+          b = fmaf(t, x.y, b * kInvF);
+          ns_split2(a, b, h[q], l[q]);
         }
-        if (!last) {
-          *reinterpret_cast<uint4*>(p) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-          *reinterpret_cast<uint4*>(p + lo_at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-        }
+        h4[k] = make_uint4(h[0], h[1], h[2], h[3]);
+        l4[k] = make_uint4(l[0], l[1], l[2], l[3]);
       }
+      if (!last)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          unsigned char* p = xs + so_piece(row, c / 8 + k);
+          *reinterpret_cast<uint4*>(p) = h4[k];
+          *reinterpret_cast<uint4*>(p + lo_at) = l4[k];
+        }
       if (last && row < m && c < cols) ns_result(M, v, row, c0 + c, min(32, cols - c));
     }
     asm volatile("fence.proxy.async;" ::: "memory");
