@@ -155,7 +155,7 @@ __device__ __forceinline__ void ns_result(const NsMat& M, float (&v)[32], int i,
 
 template <int PLANES, bool PAIR>
 struct NsOp {
-  static constexpr bool kPair = PAIR;
+  static constexpr bool kPair = PAIR, kSide = false;
   static constexpr int kPlanes = PLANES, kType = 0, kTile = PAIR ? 256 : 128, kColumns = kTile / 2;
   static constexpr int kSlots = 2, kStages = PLANES == 2 ? 2 : 4;
   static constexpr int kSegment = PLANES == 1 ? 0 : PAIR ? 4 : 2;
@@ -409,6 +409,29 @@ __device__ __forceinline__ float ns_source(const NsMat& M, size_t at) {
   return M.src_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(M.src)[at]) : static_cast<const float*>(M.src)[at];
 }
 
+// Eight neighbours of a source row, `live` of them inside it (the rest zeros).  vec: 16-byte aligned pieces.
+__device__ __forceinline__ void ns_fetch8(const NsMat& M, size_t at, int live, bool vec, float (&v)[8]) {
+  if (vec && live >= 8) {
+    if (M.src_bf16) {
+      const uint4 q = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(M.src) + at);
+      const unsigned int w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(k & 1 ? w[k >> 1] & 0xffff0000u : w[k >> 1] << 16);
+    } else {
+      const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(M.src) + at);
+      const float4 x = q[0], y = q[1];
+      v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+      v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = k < live ? ns_source(M, at + k) : 0.f;
+  }
+}
+__device__ __forceinline__ bool ns_vec(const NsMat& M) {
+  return (M.ld_src & 7) == 0 && (reinterpret_cast<uintptr_t>(M.src) & 15u) == 0;
+}
+
 __device__ __forceinline__ double ns_block_sum(double v) {
   __shared__ double red[kNsThreads / 32];
 #pragma unroll
@@ -421,6 +444,25 @@ __device__ __forceinline__ double ns_block_sum(double v) {
   return v;
 }
 
+// The unit's pieces of eight columns, four at a time in flight per thread: f(row, column, values).
+template <typename F>
+__device__ __forceinline__ void ns_each_piece(const NsMat& M, int r0, int c0, int rows, int cols, F f) {
+  constexpr int kPieces = kNsUnitCols / 8, kBatch = 4, kRows = kNsThreads / kPieces;
+  const bool vec = ns_vec(M);
+  const int c = c0 + ((int)threadIdx.x % kPieces) * 8, first = (int)threadIdx.x / kPieces, live = cols - c;
+  if (live <= 0) return;
+#pragma unroll 1
+  for (int r = first; r < kNsUnitRows; r += kBatch * kRows) {
+    float v[kBatch][8];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k)
+      if (r0 + r + k * kRows < rows) ns_fetch8(M, (size_t)(r0 + r + k * kRows) * (size_t)M.ld_src + (size_t)c, live, vec, v[k]);
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k)
+      if (r0 + r + k * kRows < rows) f(r0 + r + k * kRows, c, v[k]);
+  }
+}
+
 // One unit's sum of squares, in binary64.
 __global__ void __launch_bounds__(kNsThreads)
 ps_ortho_norm_kernel(const NsMat* __restrict__ mats, const int2* __restrict__ units) {
@@ -429,18 +471,23 @@ ps_ortho_norm_kernel(const NsMat* __restrict__ mats, const int2* __restrict__ un
   const NsMat& M = mats[u.x];
   const int rows = M.flip ? M.n : M.m, cols = M.flip ? M.m : M.n;
   const int across = (cols + kNsUnitCols - 1) / kNsUnitCols;
-  const int r0 = u.y / across * kNsUnitRows, c = u.y % across * kNsUnitCols + (int)threadIdx.x;
   double s = 0.0;
-  if (c < cols) {
-    const int end = min(rows, r0 + kNsUnitRows);
-#pragma unroll 8
-    for (int r = r0; r < end; ++r) {
-      const double x = (double)ns_source(M, (size_t)r * (size_t)M.ld_src + (size_t)c);
-      s += x * x;
-    }
-  }
+  ns_each_piece(M, u.y / across * kNsUnitRows, u.y % across * kNsUnitCols, rows, cols, [&](int, int, const float (&v)[8]) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s = fma((double)v[k], (double)v[k], s);
+  });
   s = ns_block_sum(s);
   if (threadIdx.x == 0) M.parts[u.y] = s;
+}
+
+// Eight values of a row of X as pieces of both planes; up to seven of them may lie behind the row's end, in its padding.
+__device__ __forceinline__ void ns_put8(const NsMat& M, int r, int c, const float (&v)[8], float scale) {
+  unsigned int hi[4], lo[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) ns_split2(v[2 * q] * scale, v[2 * q + 1] * scale, hi[q], lo[q]);
+  const size_t o = (size_t)r * (size_t)M.pitch_x + (size_t)c;
+  *reinterpret_cast<uint4*>(M.x[0][0] + o) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+  *reinterpret_cast<uint4*>(M.x[0][1] + o) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
 }
 
 // One unit of X, scaled, as two planes.
@@ -459,35 +506,38 @@ ps_ortho_prepare_kernel(const NsMat* __restrict__ mats, const int2* __restrict__
   const int across = (cols + kNsUnitCols - 1) / kNsUnitCols;
   const int r0 = u.y / across * kNsUnitRows, c0 = u.y % across * kNsUnitCols;
   if (!M.flip) {
-    const int c = c0 + (int)threadIdx.x;
-    if (c >= cols) return;
-    const int end = min(rows, r0 + kNsUnitRows);
-#pragma unroll 8
-    for (int r = r0; r < end; ++r) {
-      __half hi, lo;
-      ns_split(ns_source(M, (size_t)r * (size_t)M.ld_src + (size_t)c) * scale, hi, lo);
-      const size_t o = (size_t)r * (size_t)M.pitch_x + (size_t)c;
-      M.x[0][0][o] = hi;
-      M.x[0][1][o] = lo;
-    }
+    ns_each_piece(M, r0, c0, rows, cols, [&](int r, int c, const float (&v)[8]) { ns_put8(M, r, c, v, scale); });
     return;
   }
-  const int x = (int)threadIdx.x & 63, y = (int)threadIdx.x >> 6;
+  // transposed, 64 x 64 at a time: pieces along the source's rows in, along its columns out
+  const bool vec = ns_vec(M);
+  const int piece = (int)threadIdx.x & 7, line = (int)threadIdx.x >> 3;
   for (int part = 0; part < kNsUnitCols; part += 64) {
-    if (c0 + part >= cols) break;                        // (the same for the whole CTA)
+    const int c = c0 + part;
+    if (c >= cols) break;                                // (the same for the whole CTA)
+    float v[2][8];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int r = r0 + line + 32 * k, live = min(8, cols - (c + piece * 8));
+      if (r < rows && live > 0) ns_fetch8(M, (size_t)r * (size_t)M.ld_src + (size_t)(c + piece * 8), live, vec, v[k]);
+      else
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[k][q] = 0.f;
+    }
     __syncthreads();
-#pragma unroll 4
-    for (int r = y; r < 64; r += kNsThreads / 64)
-      if (r0 + r < rows && c0 + part + x < cols) tile[r][x] = ns_source(M, (size_t)(r0 + r) * (size_t)M.ld_src + (size_t)(c0 + part + x));
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int q = 0; q < 8; ++q) tile[line + 32 * k][piece * 8 + q] = v[k][q];
     __syncthreads();
-#pragma unroll 4
-    for (int r = y; r < 64; r += kNsThreads / 64) {
-      if (c0 + part + r < cols && r0 + x < rows) {
-        __half hi, lo;
-        ns_split(tile[x][r] * scale, hi, lo);
-        const size_t o = (size_t)(c0 + part + r) * (size_t)M.pitch_x + (size_t)(r0 + x);
-        M.x[0][0][o] = hi;
-        M.x[0][1][o] = lo;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int x = line + 32 * k;                       // row of X in the tile
+      if (c + x < cols && r0 + piece * 8 < rows) {
+        float w[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) w[q] = tile[piece * 8 + q][x];
+        ns_put8(M, c + x, r0 + piece * 8, w, scale);
       }
     }
   }

@@ -174,6 +174,7 @@ struct TcWarp {
 //   tiles(args); Item item(args, index), what the roles need to know of a tile, read one tile ahead; tile(args, item, TcTile*)
 //   Epilogue(args, item, TcWarp&, cursor): begin() before the sums are there, columns(32 sums of this lane's row, their
 //   place among the warp's columns), end()
+//   kSide (without slots): warps 2 and 3 do side(args, thread, threads)
 // and with slots
 //   entries(args, item, rank, half), how many slots the half's columns pass through; load(args, item, rank, half, entry,
 //   slot, vectors, barrier), which arrives; store(args, item, rank, half, entry, slot); done(args, item, rank)
@@ -366,6 +367,9 @@ ps_tc_kernel(const __grid_constant__ typename Op::Args args) {
             for (unsigned int s = 0; s < (unsigned)Op::kSlots; ++s)
               mm_wait(staged + h * kHalf + 8 * s, s < at[h].s ? at[h].parity : at[h].parity ^ 1u, args.status);
       }
+      __syncwarp();
+    } else if constexpr (Op::kSide) {
+      Op::side(args, (int)blockIdx.x * 64 + (warp - 2) * 32 + lane, (int)gridDim.x * 64);
       __syncwarp();
     }
   } else {

@@ -50,10 +50,10 @@ struct XePlan {
   size_t parts, score, xm, d[2], sums, x, w, end, end_unaligned;
 };
 
-// A piece of d: as many words as make 2^24 entries (32 MB), whole tiles, at least one.
-constexpr long long kXePieceEntries = 1ll << 24;
+// A piece of d: as many words as make 5 x 2^22 entries (40 MB), whole tiles, at least one.
+constexpr long long kXePieceEntries = 5ll << 22;
 constexpr int kXePairs = 74;             // CTA pairs that the cuts are made for
-constexpr int kXeMaxSlices = 64, kXeMinStages = 4;
+constexpr int kXeMaxSlices = 64, kXeMinStages = 16;
 constexpr long long kXeSliceRows = 1ll << 14;    // slices x tokens, where there is more than one slice
 
 XePlan xent_plan(long long T, long long V, long long D) {
@@ -61,15 +61,17 @@ XePlan xent_plan(long long T, long long V, long long D) {
   p.nparts = ceil_div(V, 128);
   p.pitch = ceil_div(D, 8) * 8;
   const long long all = ceil_div(V, kXeTile) * kXeTile;
-  p.piece = std::min(all, std::max<long long>(1, kXePieceEntries / std::max(1ll, T) / kXeTile) * kXeTile);
+  // (equal pieces: a short last one would leave the launches around it half empty)
+  const long long most_words = std::min(all, std::max<long long>(1, kXePieceEntries / std::max(1ll, T) / kXeTile) * kXeTile);
+  p.piece = ceil_div(ceil_div(V, ceil_div(V, most_words)), kXeTile) * kXeTile;
   p.pieces = ceil_div(V, p.piece);
   // dx has few tiles, each as long as the piece has words: its words are shared out to slices until one is no longer
   // than half of what a pair computes in a launch
   const long long tm = ceil_div(T, kXeTile), td = ceil_div(D, kXeTile), tv = p.piece / kXeTile, nk = p.piece / kTcK;
   const long long total = tm * tv * ceil_div(D, kTcK) + tm * td * nk + tv * td * ceil_div(T, kTcK);
   const long long longest = std::max<long long>(kXeMinStages, total / kXePairs / 2);
-  const long long most = std::min<long long>(kXeMaxSlices, std::max(1ll, kXeSliceRows / std::max(1ll, T)));
-  p.slices = (int)std::min(most, std::max(1ll, ceil_div(nk, longest)));
+  const long long most_slices = std::min<long long>(kXeMaxSlices, std::max(1ll, kXeSliceRows / std::max(1ll, T)));
+  p.slices = (int)std::min(most_slices, std::max(1ll, ceil_div(nk, longest)));
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t here = at;
@@ -141,17 +143,20 @@ int check(const ps_xent* q, XeCall* c) {
   return PS_OK;
 }
 
-int copy_rows(const XeCall& c, const void* src, long long rows, long long ld, size_t to, bool mask, const float* weights) {
+XeCopy copy_of(const XeCall& c, const void* src, long long rows, long long ld, size_t to, bool mask, const float* weights) {
+  return XeCopy{static_cast<const unsigned short*>(src), reinterpret_cast<unsigned short*>(c.ws + to), rows, c.q->dim, ld, c.plan.pitch,
+                mask ? c.q->targets : nullptr, c.q->target_bits == 64 ? 1 : 0, rows_aligned(src, ld) ? 1 : 0, c.q->vocab, weights};
+}
+
+int copy_rows(const XeCall& c, const void* src, long long rows, long long ld, size_t to) {
   const long long units = rows * (c.plan.pitch / 8);
-  const unsigned grid = (unsigned)std::min<long long>(ceil_div(units, kXeCopyThreads), (long long)c.dev.num_sms * 16);
+  const unsigned grid = (unsigned)std::min<long long>(ceil_div(units, kXeCopyThreads), (long long)c.dev.num_sms * 8);
   return op_launch("cross entropy", ps_xent_copy_kernel, grid, kXeCopyThreads, 0, 1, c.stream,
-                   static_cast<const unsigned short*>(src), rows, c.q->dim, ld, reinterpret_cast<unsigned short*>(c.ws + to),
-                   c.plan.pitch, mask ? c.q->targets : nullptr, c.q->target_bits == 64 ? 1 : 0, c.q->vocab,
-                   weights, rows_aligned(src, ld) ? 1 : 0);
+                   copy_of(c, src, rows, ld, to, false, nullptr));
 }
 
 // What both passes set up.
-int begin(XeCall* c, void* stream, bool backward, const float* weights) {
+int begin(XeCall* c, void* stream, bool backward) {
   const ps_xent* q = c->q;
   const XePlan& p = c->plan;
   c->stream = static_cast<cudaStream_t>(stream);
@@ -177,9 +182,8 @@ int begin(XeCall* c, void* stream, bool backward, const float* weights) {
     for (int b = 0; b < 2 && b < p.pieces; ++b) ok = ok && make_map(encode, &a.d[b], c->ws + p.d[b], a.T, p.piece, p.piece);
   }
   if (!ok) return op_cuda_error("tensor map", cudaErrorInvalidValue);
-  if (c->copy_x) rc = copy_rows(*c, q->x, q->tokens, q->ldx, p.x, false, nullptr);
-  if (!rc && c->copy_w) rc = copy_rows(*c, q->w, q->vocab, q->ldw, p.w, false, nullptr);
-  if (!rc && backward) rc = copy_rows(*c, q->x, q->tokens, q->ldx, p.xm, true, weights);
+  if (c->copy_x) rc = copy_rows(*c, q->x, q->tokens, q->ldx, p.x);
+  if (!rc && c->copy_w) rc = copy_rows(*c, q->w, q->vocab, q->ldw, p.w);
   return rc;
 }
 
@@ -219,7 +223,7 @@ int ps_xent_forward(const ps_xent* q, float* loss, float* lse, void* stream) {
   if (q->tokens == 0) return PS_OK;
   if (!loss && !lse) return PS_ERR_BAD_ARG;
   if (misaligned(loss, 4) || misaligned(lse, 4)) return PS_ERR_ALIGN;
-  rc = begin(&c, stream, false, nullptr);
+  rc = begin(&c, stream, false);
   if (rc) return rc;
   XeArgs& a = c.args;
   a.parts = reinterpret_cast<float2*>(c.ws + c.plan.parts);
@@ -249,7 +253,7 @@ int ps_xent_backward(const ps_xent* q, const float* lse, float scale, const floa
                                             static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? PS_OK : op_cuda_error("ps_xent_backward", e);
   }
-  rc = begin(&c, stream, true, dw ? token_scale : nullptr);
+  rc = begin(&c, stream, true);
   if (rc) return rc;
   XeArgs& a = c.args;
   const XePlan& p = c.plan;
@@ -270,6 +274,8 @@ int ps_xent_backward(const ps_xent* q, const float* lse, float scale, const floa
   int filled = 0;                        // slices of dx's sums that hold something
   for (long long k = 0; k <= p.pieces; ++k) {
     a.nseg = 0;
+    a.side = XeCopy();
+    if (k == 0 && dw) a.side = copy_of(c, q->x, q->tokens, q->ldx, p.xm, true, token_scale);
     if (k < p.pieces) {
       const long long v0 = k * p.piece, words = std::min(p.piece, a.V - v0);
       a.seg[a.nseg++] = XeSeg{kXeProb, 0, tm, (int)ceil_div(words, kXeTile), (int)v0, (int)ceil_div(a.D, kTcK), 1, (int)(k & 1), 0, 0};
@@ -288,9 +294,10 @@ int ps_xent_backward(const ps_xent* q, const float* lse, float scale, const floa
     if (rc) return rc;
   }
   if (dx && p.slices > 1) {
-    const unsigned grid = (unsigned)std::min<long long>(ceil_div(a.T * a.D, kXeCopyThreads), (long long)c.dev.num_sms * 8);
+    const unsigned grid = (unsigned)std::min<long long>(a.T, (long long)c.dev.num_sms * 16);
+    const bool wide = a.D % 4 == 0 && !misaligned(dx, 8) && lddx % 4 == 0;
     rc = op_launch("cross entropy", ps_xent_slices_kernel, grid, kXeCopyThreads, 0, 1, c.stream, (const float*)a.dx_sums, filled,
-                   a.T, a.D, a.targets, a.target64, a.V, a.weights, a.scale, a.dx, a.ld_dx);
+                   a.T, a.D, a.targets, a.target64, a.V, a.weights, a.scale, a.dx, a.ld_dx, wide ? 1 : 0);
   }
   return rc;
 }

@@ -36,6 +36,59 @@ struct XeSeg {                           // a launch's tiles of one kind, tiles_
 };
 constexpr int kXeMaxSegs = 3;
 
+// Copies a matrix of bf16 into rows of `pitch` elements (a multiple of eight; the rest zeros).  With targets the rows of
+// ignored tokens become zeros, so that what padded places of a batch hold, NaN or not, does not reach the gradients, and
+// the others are multiplied by their weight.
+struct XeCopy {
+  const unsigned short* src;             // nullptr: nothing to copy
+  unsigned short* dst;
+  long long rows, cols, ld, pitch;
+  const void* targets;
+  int target64;
+  int wide;                              // rows of src allow 128-bit loads
+  long long V;
+  const float* weights;
+};
+
+__device__ __forceinline__ long long xe_target(const void* targets, int is64, long long t) {
+  return is64 ? static_cast<const long long*>(targets)[t] : (long long)static_cast<const int*>(targets)[t];
+}
+
+// Pieces of eight elements first, first + stride, ...
+__device__ __forceinline__ void xe_copy(const XeCopy& c, long long first, long long stride) {
+  const unsigned int per = (unsigned int)(c.pitch / 8);
+  const long long total = c.rows * per;
+#pragma unroll 4
+  for (long long i = first; i < total; i += stride) {
+    const long long r = i / per, col = (i - r * per) * 8;
+    uint4 q = make_uint4(0, 0, 0, 0);
+    bool keep = true;
+    if (c.targets) {
+      const long long t = xe_target(c.targets, c.target64, r);
+      keep = t >= 0 && t < c.V;
+    }
+    if (keep) {
+      const unsigned short* p = c.src + (size_t)r * (size_t)c.ld + (size_t)col;
+      if (c.wide && col + 8 <= c.cols) {
+        q = *reinterpret_cast<const uint4*>(p);
+      } else {
+        unsigned int u[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) u[k] = col + k < c.cols ? p[k] : 0;
+        q = make_uint4(u[0] | u[1] << 16, u[2] | u[3] << 16, u[4] | u[5] << 16, u[6] | u[7] << 16);
+      }
+      if (c.weights) {
+        const float g = c.weights[r];
+        unsigned int u[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) u[k] = mm_bf16x2(__uint_as_float(u[k] << 16) * g, __uint_as_float(u[k] & 0xffff0000u) * g);
+        q = make_uint4(u[0], u[1], u[2], u[3]);
+      }
+    }
+    *reinterpret_cast<uint4*>(c.dst + (size_t)r * (size_t)c.pitch + (size_t)col) = q;
+  }
+}
+
 struct XeArgs {
   CUtensorMap x, xm, w, d[2];            // xm: token_scale * x, the rows of ignored tokens zeroed
   int* status;
@@ -59,11 +112,8 @@ struct XeArgs {
   void* dw;
   long long ld_dx, ld_dw;
   int dw_f32, dx_wide, dw_wide;          // wide: rows allow 256-bit stores
+  XeCopy side;                           // done by warps that have nothing else to do: xm, needed from the next launch on
 };
-
-__device__ __forceinline__ long long xe_target(const void* targets, int is64, long long t) {
-  return is64 ? static_cast<const long long*>(targets)[t] : (long long)static_cast<const int*>(targets)[t];
-}
 
 // g_t; zero for an ignored token, whatever token_scale holds there.
 __device__ __forceinline__ float xe_factor(const void* targets, int is64, long long V, const float* weights, float scale, long long t) {
@@ -108,6 +158,7 @@ __device__ __forceinline__ void xe_store_f32(float* o, const float* v, int live,
 struct XeOp {
   static constexpr bool kPair = true;
   static constexpr int kPlanes = 1, kType = 1, kStages = 6, kSlots = 0, kSegment = 0;
+  static constexpr bool kSide = true;
   using Args = XeArgs;
 
   struct At { const XeSeg* seg; int m, n, slice; };
@@ -133,6 +184,9 @@ struct XeOp {
 
   static __device__ __forceinline__ int tiles(const XeArgs& a) { return a.tiles; }
   static __device__ __forceinline__ Item item(const XeArgs&, int index, int) { return index; }
+  static __device__ __forceinline__ void side(const XeArgs& a, int thread, int threads) {
+    if (a.side.src) xe_copy(a.side, thread, threads);
+  }
 
   static __device__ __forceinline__ void tile(const XeArgs& a, int index, TcTile* t) {
     const At at = locate(a, index);
@@ -355,58 +409,45 @@ ps_xent_join_kernel(const float2* __restrict__ parts, int nparts, const float* _
   }
 }
 
-// Copies a matrix of bf16 into rows of `pitch` elements (a multiple of eight; the rest zeros).  With targets the rows of
-// ignored tokens become zeros, so that what padded places of a batch hold, NaN or not, does not reach the gradients, and
-// the others are multiplied by their weight.
 constexpr int kXeCopyThreads = 256;
 __global__ void __launch_bounds__(kXeCopyThreads)
-ps_xent_copy_kernel(const unsigned short* __restrict__ src, long long rows, long long cols, long long ld,
-                    unsigned short* __restrict__ dst, long long pitch, const void* __restrict__ targets, int target64,
-                    long long V, const float* __restrict__ weights, int wide) {
+ps_xent_copy_kernel(const __grid_constant__ XeCopy c) {
   mm_pdl();
-  const long long per = pitch / 8, total = rows * per;
-  for (long long i = (long long)blockIdx.x * kXeCopyThreads + threadIdx.x; i < total; i += (long long)gridDim.x * kXeCopyThreads) {
-    const long long r = i / per, c = (i - r * per) * 8;
-    uint4 q = make_uint4(0, 0, 0, 0);
-    bool keep = true;
-    if (targets) {
-      const long long t = xe_target(targets, target64, r);
-      keep = t >= 0 && t < V;
-    }
-    if (keep) {
-      const unsigned short* p = src + (size_t)r * (size_t)ld + (size_t)c;
-      if (wide && c + 8 <= cols) {
-        q = *reinterpret_cast<const uint4*>(p);
-      } else {
-        unsigned int u[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) u[k] = c + k < cols ? p[k] : 0;
-        q = make_uint4(u[0] | u[1] << 16, u[2] | u[3] << 16, u[4] | u[5] << 16, u[6] | u[7] << 16);
-      }
-      if (weights) {
-        const float g = weights[r];
-        unsigned int* u = &q.x;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) u[k] = mm_bf16x2(__uint_as_float(u[k] << 16) * g, __uint_as_float(u[k] & 0xffff0000u) * g);
-      }
-    }
-    *reinterpret_cast<uint4*>(dst + (size_t)r * (size_t)pitch + (size_t)c) = q;
-  }
+  xe_copy(c, (long long)blockIdx.x * kXeCopyThreads + threadIdx.x, (long long)gridDim.x * kXeCopyThreads);
 }
 
-// dx = sum over the slices, in order.
+// dx = sum over the slices, in order: a CTA per row, four columns per thread where rows allow it.
 __global__ void __launch_bounds__(kXeCopyThreads)
 ps_xent_slices_kernel(const float* __restrict__ sums, int slices, long long T, long long D, const void* __restrict__ targets,
                       int target64, long long V, const float* __restrict__ weights, float scale, __nv_bfloat16* __restrict__ dx,
-                      long long ld) {
+                      long long ld, int wide) {
   mm_pdl();
-  const long long n = T * D;
-  for (long long i = (long long)blockIdx.x * kXeCopyThreads + threadIdx.x; i < n; i += (long long)gridDim.x * kXeCopyThreads) {
-    float v = sums[i];
+  const size_t n = (size_t)T * (size_t)D;
+  for (long long r = blockIdx.x; r < T; r += gridDim.x) {
+    const float g = xe_factor(targets, target64, V, weights, scale, r);
+    const float* p = sums + (size_t)r * (size_t)D;
+    __nv_bfloat16* o = dx + (size_t)r * (size_t)ld;
+    if (wide) {
+      for (long long c = 4 * threadIdx.x; c < D; c += 4 * kXeCopyThreads) {
+        float4 v = *reinterpret_cast<const float4*>(p + c);
 #pragma unroll 8
-    for (int k = 1; k < slices; ++k) v += sums[(size_t)k * (size_t)n + (size_t)i];
-    const long long r = i / D;
-    dx[(size_t)r * (size_t)ld + (size_t)(i - r * D)] = __float2bfloat16_rn(v * xe_factor(targets, target64, V, weights, scale, r));
+        for (int k = 1; k < slices; ++k) {
+          const float4 q = *reinterpret_cast<const float4*>(p + (size_t)k * n + c);
+          v.x += q.x;
+          v.y += q.y;
+          v.z += q.z;
+          v.w += q.w;
+        }
+        *reinterpret_cast<uint2*>(o + c) = make_uint2(mm_bf16x2(v.x * g, v.y * g), mm_bf16x2(v.z * g, v.w * g));
+      }
+    } else {
+      for (long long c = threadIdx.x; c < D; c += kXeCopyThreads) {
+        float v = p[c];
+#pragma unroll 8
+        for (int k = 1; k < slices; ++k) v += p[(size_t)k * n + c];
+        o[c] = __float2bfloat16_rn(v * g);
+      }
+    }
   }
 }
 
