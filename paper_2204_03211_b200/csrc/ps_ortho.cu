@@ -101,14 +101,14 @@ NsLayout layout(const NsItem& it, bool split, size_t at) {
   return l;
 }
 
-// A plane by boxes: 64 x 64 as the products' operand (128-byte swizzle), or `rows` x 32 for the epilogues (64-byte swizzle).
+// A plane by boxes of `rows` x `cols`, rows of 128 bytes in 128-byte swizzle or of 64 in 64-byte swizzle.
 bool make_map(EncodeTiled encode, CUtensorMap* m, const void* p, long long rows, long long cols, long long pitch, int box_rows,
-              bool operand) {
+              int box_cols) {
   const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
   const cuuint64_t strides[1] = {(cuuint64_t)pitch * 2};
-  const cuuint32_t box[2] = {operand ? 64u : 32u, (cuuint32_t)box_rows}, step[2] = {1, 1};
+  const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, step[2] = {1, 1};
   return encode(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void*>(p), dims, strides, box, step,
-                CU_TENSOR_MAP_INTERLEAVE_NONE, operand ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -155,7 +155,7 @@ static int small_ctas(const std::vector<NsItem>& items) {
       if (s->of != d.of && s->end > d.first) return 0;
   }
   // One CTA where it can hold a matrix.  Else 128 columns each rather than 256: what every CTA does for itself gets shorter,
-  // adding up A does not get longer (128 x 512: MEASURE)
+  // adding up A does not get longer (four of 128 x 512: 81 us on two CTAs each, 66 on four)
   if (widest <= kSoCols) return 1;
   int ctas = 2;
   while (ctas < kSoCtas && ctas * (kSoCols / 2) < widest) ctas *= 2;
@@ -172,7 +172,7 @@ size_t NsPlan::workspace(const std::vector<NsItem>& items, bool split) {
     at = l.end;
     const long long tm = ceil_div(l.m, 128), tn = ceil_div(l.n, 128);
     if (tm > (1ll << 13) || tn > (1ll << 20)) return 0;
-    tiles += kNsSteps * (tm * (tm + 1) + tm * tn);
+    tiles += kNsSteps * (2 * tm * tm + tm * tn);
     units += l.units;
     if (tiles > kNsMaxTiles || units > kNsMaxTiles) return 0;
   }
@@ -210,7 +210,14 @@ int NsPlan::build(const std::vector<NsItem>& items, bool split, void* workspace,
   std::memset(mats.data(), 0, n * sizeof(NsMat));
   std::memset(maps.data(), 0, maps.size() * sizeof(CUtensorMap));
   size_t at = 0;
-  long long sym_tiles = 0;
+  long long sym_tiles = 0, square_tiles = 0;
+  for (const NsItem* it : live) {
+    const long long tm = ceil_div(std::min(it->rows, it->cols), tile);
+    square_tiles += tm * tm;
+  }
+  // Few tiles: all of them have a CTA anyway, and storing a tile twice takes an epilogue 4 us longer (3 x 777 x 300 to
+  // fp32: 215 us mirrored, 187 us not)
+  const bool mirror = square_tiles > room;
   for (size_t i = 0; i < n; ++i) {
     const NsItem& it = *live[i];
     NsMat& M = mats[i];
@@ -235,22 +242,26 @@ int NsPlan::build(const std::vector<NsItem>& items, bool split, void* workspace,
     M.pitch_e = l.pitch_e;
     bool ok = true;
     CUtensorMap* map = &maps[kNsMaps * i];
-    auto plane = [&](int at_map, const void* p, long long cols, long long pitch) {
-      ok = ok && make_map(encode, map + at_map, p, l.m, cols, pitch, 64, true);
-      ok = ok && make_map(encode, map + kNsTall + at_map, p, l.m, cols, pitch, 128, false);
+    auto plane = [&](int at_map, const void* p, long long cols, long long pitch, int box_rows, int box_cols) {
+      ok = ok && make_map(encode, map + at_map, p, l.m, cols, pitch, box_rows, box_cols);
     };
     for (int b = 0; b < 2; ++b)
       for (int p = 0; p < 2; ++p) {
         M.x[b][p] = half_at(l.x[b][p]);
-        plane(2 * b + p, M.x[b][p], l.n, l.pitch_x);
+        plane(2 * b + p, M.x[b][p], l.n, l.pitch_x, split ? 32 : 64, 64);
+        plane(kNsTall + 2 * b + p, M.x[b][p], l.n, l.pitch_x, 128, 32);
       }
     for (int p = 0; p < (split ? 2 : 1); ++p) {
       M.e[p] = half_at(l.e[p]);
       M.f[p] = half_at(l.f[p]);
-      plane(4 + p, M.e[p], l.m, l.pitch_e);
-      plane(6 + p, M.f[p], l.m, l.pitch_e);
-      ok = ok && make_map(encode, map + kNsMirror + p, M.e[p], l.m, l.m, l.pitch_e, 32, false);
-      ok = ok && make_map(encode, map + kNsMirror + 2 + p, M.f[p], l.m, l.m, l.pitch_e, 32, false);
+      if (!split) {
+        plane(4, M.e[p], l.m, l.pitch_e, 64, 64);
+        plane(6, M.f[p], l.m, l.pitch_e, 64, 64);
+      }
+      plane(kNsTall + 4 + p, M.e[p], l.m, l.pitch_e, 128, 32);
+      plane(kNsTall + 6 + p, M.f[p], l.m, l.pitch_e, 128, 32);
+      plane(kNsMirror + p, M.e[p], l.m, l.pitch_e, 32, 32);
+      plane(kNsMirror + 2 + p, M.f[p], l.m, l.pitch_e, 32, 32);
     }
     if (!ok) return op_cuda_error("tensor map", cudaErrorInvalidValue);
     M.d = reinterpret_cast<float*>(ws + l.d);
@@ -259,12 +270,13 @@ int NsPlan::build(const std::vector<NsItem>& items, bool split, void* workspace,
     M.nparts = it.parts ? it.nparts : (int)l.units;
     if (!it.parts) norms_ = true;
     const int tm = (int)ceil_div(l.m, tile), tn = (int)ceil_div(l.n, tile);
+    M.mirror = mirror;
     for (int a = 0; a < tm; ++a) {
       const int ctas = pair_ && l.m - a * tile > 128 ? 2 : 1;
-      M.parts_s += (a + 1) * ctas;
+      M.parts_s += (mirror ? a + 1 : tm) * ctas;
       M.parts_x += tn * ctas;
     }
-    sym_tiles += tm * (tm + 1) / 2;
+    sym_tiles += mirror ? tm * (tm + 1) / 2 : tm * tm;
     for (long long u = 0; u < l.units; ++u) units.push_back(make_int2((int)i, (int)u));
   }
   // the tiles: matrices dealt to groups, a group's products one kind after the other
@@ -275,7 +287,7 @@ int NsPlan::build(const std::vector<NsItem>& items, bool split, void* workspace,
         for (size_t i = g; i < n; i += groups) {
           const int tm = (int)ceil_div(mats[i].m, tile), tn = (int)ceil_div(mats[i].n, tile);
           for (int a = 0; a < tm; ++a)
-            for (int b = 0; b < (product == 2 ? tn : a + 1); ++b)
+            for (int b = 0; b < (product == 2 ? tn : mirror ? a + 1 : tm); ++b)
               list.push_back(NsTile{(int)i, (short)step, (short)product, a, b});
         }
   size_t off = 0;

@@ -6,8 +6,8 @@
 // them run in ONE cooperative launch of the frame of ps_tc.cuh: every tile names the matrix and the product it belongs
 // to, tiles are listed step by step, and a tile waits until its matrix's earlier products are done (one counter per
 // matrix).  Every pair of CTAs takes its tiles in the list's order, so whatever a tile waits for is being worked on;
-// there is no barrier over the grid, and one matrix's wait is another one's work.  A and B are symmetric: only tiles on
-// and below the diagonal are computed, and stored twice.
+// there is no barrier over the grid, and one matrix's wait is another one's work.  A and B are symmetric: where the tiles
+// outnumber the CTAs only those on and below the diagonal are computed, and stored twice.
 //
 // Arithmetic.  Operands are fp16 (11 bits) scaled by powers of two, sums are binary32.
 //  - The largest entries of A and B stand on their diagonals, and the last steps subtract them from a; they are
@@ -40,14 +40,17 @@ constexpr int kNsMaps = 20, kNsTall = 8, kNsMirror = 16;
 struct NsMat {                           // one matrix, in its working orientation: m <= n
   int m, n;
   int flip;                              // 1: source and result are the transposes
+  int mirror;                            // 1: symmetric products compute the lower tiles and store them twice
   int out;                               // kNsOut*
   long long pitch_x, pitch_e;            // elements; multiples of 64
   __half* x[2][2];                       // two buffers of two planes: a step reads one and writes the other
   __half* e[2];                          // planes of what is off A's diagonal; the second where products are split
   __half* f[2];                          // and off B's
   float *d, *fd;                         // the diagonals
-  const CUtensorMap* maps;               // x[0], x[1], e, f, two planes each: as operands, by 128 x 32 (kNsTall), and e and
-                                         // f by 32 x 32 (kNsMirror)
+  // Two planes each: x[0], x[1], e, f by 64 x 64 (one product: operands) or x[0], x[1] by 32 x 64 (three: transposed
+  // operands); x[0], x[1], e, f by 128 x 32 (kNsTall: the epilogues', and three products' operands); e, f by 32 x 32
+  // (kNsMirror).
+  const CUtensorMap* maps;
   const void* src;                       // rows x cols as the caller sees them
   long long ld_src;
   int src_bf16;
@@ -157,8 +160,10 @@ template <int PLANES, bool PAIR>
 struct NsOp {
   static constexpr bool kPair = PAIR, kSide = false;
   static constexpr int kPlanes = PLANES, kType = 0, kTile = PAIR ? 256 : 128, kColumns = kTile / 2;
-  static constexpr int kSlots = 2, kStages = PLANES == 2 ? 2 : 4;
-  static constexpr int kSegment = PLANES == 1 ? 0 : PAIR ? 4 : 2;
+  // Three products of a stage take three times as long as one, so they need short stages to have enough of them (long |
+  // short: 24 x 1024 x 4096 to fp32 4.86 | 4.44 ms); a single one is slowed by 64-byte rows (to bf16 2.46 | 2.63 ms).
+  static constexpr int kSlots = 2, kK = PLANES == 2 ? 32 : 64, kStages = 4;
+  static constexpr int kSegment = PLANES == 1 ? 0 : PAIR ? 8 : 4;
   using Args = NsArgs;
 
   static __device__ __forceinline__ int tiles(const NsArgs& a) { return a.tiles; }
@@ -169,7 +174,7 @@ struct NsOp {
 
   static __device__ __forceinline__ int stages(const NsArgs& a, const NsTile& at) {
     const NsMat& M = a.mats[at.mat];
-    return ((at.product == 0 ? M.n : M.m) + kTcK - 1) / kTcK;
+    return ((at.product == 0 ? M.n : M.m) + kK - 1) / kK;
   }
 
   // A tile waits for its matrix's earlier products.
@@ -182,9 +187,9 @@ struct NsOp {
     t->a_k = t->b_k = 0;
     t->a_mn = 0;
     t->b_mn = at.product == 2;           // X's rows are k there
-    const CUtensorMap* x = M.maps + 2 * (at.step & 1);
-    t->a = at.product == 0 ? x : at.product == 1 ? M.maps + 4 : M.maps + 6;
-    t->b = at.product == 1 ? M.maps + 4 : x;
+    const CUtensorMap *rows = M.maps + (kK == 32 ? kNsTall : 0), *x = rows + 2 * (at.step & 1), *e = rows + 4;
+    t->a = at.product == 0 ? x : at.product == 1 ? e : e + 2;
+    t->b = at.product == 0 ? x : at.product == 1 ? e : M.maps + 2 * (at.step & 1);
     t->nk = stages(a, at);
   }
 
@@ -193,20 +198,20 @@ struct NsOp {
   // from a slot of their own.
 
   static __device__ __forceinline__ int width(const NsMat& M, const NsTile& at) { return at.product == 2 ? M.n : M.m; }
-  static __device__ __forceinline__ bool mirrored(const NsTile& at) { return at.product < 2 && at.ti != at.tj; }
-  static __device__ __forceinline__ int per_chunk(const NsTile& at) { return PLANES == 2 && mirrored(at) ? 2 : 1; }
+  static __device__ __forceinline__ bool mirrored(const NsMat& M, const NsTile& at) { return M.mirror && at.product < 2 && at.ti != at.tj; }
+  static __device__ __forceinline__ int per_chunk(const NsMat& M, const NsTile& at) { return PLANES == 2 && mirrored(M, at) ? 2 : 1; }
 
   static __device__ __forceinline__ int entries(const NsArgs& a, const NsTile& at, int rank, int half) {
     const NsMat& M = a.mats[at.mat];
     const int left = width(M, at) - (at.tj * kTile + half * kColumns);
     if (left <= 0 || at.ti * kTile + rank * 128 >= M.m) return 0;
-    return min(kColumns / 32, (left + 31) / 32) * per_chunk(at);
+    return min(kColumns / 32, (left + 31) / 32) * per_chunk(M, at);
   }
 
   static __device__ __forceinline__ void load(const NsArgs& a, const NsTile& at, int rank, int half, int entry, unsigned int slot,
                                               unsigned int vectors, unsigned int bar) {
     const NsMat& M = a.mats[at.mat];
-    const int per = per_chunk(at), c = entry / per * 32, i0 = at.ti * kTile + rank * 128, j0 = at.tj * kTile + half * kColumns;
+    const int per = per_chunk(M, at), c = entry / per * 32, i0 = at.ti * kTile + rank * 128, j0 = at.tj * kTile + half * kColumns;
     if (at.product == 0 || entry % per) {                // nothing to read
       tc_arrive(bar);
       return;
@@ -225,8 +230,8 @@ struct NsOp {
   static __device__ __forceinline__ void store(const NsArgs& a, const NsTile& at, int rank, int half, int entry, unsigned int slot) {
     const NsMat& M = a.mats[at.mat];
     if (at.product == 2 && at.step == kNsSteps - 1) return;                  // (results go out from registers)
-    const int per = per_chunk(at), c = entry / per * 32, i0 = at.ti * kTile + rank * 128, j = at.tj * kTile + half * kColumns + c;
-    const bool direct = entry % per == 0, mirror = mirrored(at) && (PLANES == 1 || !direct);
+    const int per = per_chunk(M, at), c = entry / per * 32, i0 = at.ti * kTile + rank * 128, j = at.tj * kTile + half * kColumns + c;
+    const bool direct = entry % per == 0, mirror = mirrored(M, at) && (PLANES == 1 || !direct);
     if (direct) {
       const CUtensorMap* map = M.maps + kNsTall + (at.product == 0 ? 4 : at.product == 1 ? 6 : 2 * ((at.step & 1) ^ 1));
       for (int p = 0; p < (at.product == 2 ? 2 : PLANES); ++p) tc_store(map + p, j, i0, slot + p * kTcPlane);
@@ -307,9 +312,9 @@ struct NsOp {
     // Off-diagonal entries of a symmetric matrix, already scaled, and where they mirror.
     __device__ __forceinline__ void put_symmetric(const float (&v)[32]) {
       put(v, PLANES == 2);
-      if (PLANES == 1 && mirrored(at)) put_mirrored(v, 1, false);
+      if (PLANES == 1 && mirrored(M, at)) put_mirrored(v, 1, false);
       hand_over();
-      if (PLANES == 2 && mirrored(at)) {
+      if (PLANES == 2 && mirrored(M, at)) {
         wait_staged();
         put_mirrored(v, 0, false);
         put_mirrored(v, 1, true);
@@ -369,7 +374,7 @@ struct NsOp {
         }
       }
       if (k0 >= 0 && k0 < 32 && i < M.m) M.fd[i] = fmaf(kNsC, fmaf(di, di, diagonal * (kInvE * kInvE)), kNsB * di);
-      if (mirrored(at)) __syncwarp();                    // all have read the slot before others' columns are written there
+      if (mirrored(M, at)) __syncwarp();                    // all have read the slot before others' columns are written there
       put_symmetric(v);
     }
 

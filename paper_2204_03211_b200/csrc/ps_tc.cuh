@@ -4,14 +4,16 @@
 //     acc[i][j] = sum over k of A[i][k] * B[j][k],
 // and an operator `Op` says which tiles there are, where their operands lie, and what becomes of the sums.
 //
-// Operands are fetched as boxes of 64 rows by 64 columns (8 KB, rows of 128 bytes, 128-byte swizzle).  One box shape
-// serves both orders: where k runs along a row of the tensor ("K-major") a stage takes two boxes one below the other,
-// where it runs down the columns (transposed operands, as both gradients of a product need) two boxes side by side, and
-// the MMA's descriptors say which.  So no tensor is ever transposed in memory for a product.
-//
-// A stage is 64 elements of k: 16 KB per operand and CTA.  Operands may consist of two planes (value = high + low, see
-// Op::kPlanes): a stage then holds both and feeds three products, high x high, high x low and low x high, so what is
-// fetched from L2 per product is 2/3 of one plane's.
+// k may run along the rows of an operand's tensor ("K-major") or down its columns (transposed operands, as both gradients
+// of a product need): the boxes that are fetched and the MMA's descriptors say which, so no tensor is ever transposed in
+// memory for a product.  A stage is 64 or 32 elements of k (Op::kK), 16 or 8 KB per operand, plane and CTA:
+//   64  boxes of 64 rows by 64 columns, rows of 128 bytes in 128-byte swizzle, two one below the other (K-major) or side
+//       by side
+//   32  one box of 128 rows by 32 columns, rows of 64 bytes in 64-byte swizzle (K-major), or two of 32 rows by 64 columns
+//       in 128-byte swizzle side by side
+// Short stages keep more copies in flight in the same shared memory: one is worked on, the others are on their way.
+// Operands may consist of two planes (value = high + low, see Op::kPlanes): a stage then holds both and feeds three
+// products, high x high, high x low and low x high, so what is fetched from L2 per product is 2/3 of one plane's.
 //   warp 0     one lane issues the copies (each CTA its half, counted on the leader's barrier)
 //   warp 1     leader: one lane issues the MMAs
 //   warps 4-11 read the accumulators, two warps per quarter of the lanes, half of the columns each
@@ -29,10 +31,7 @@
 namespace psb {
 
 constexpr int kTcThreads = 384;
-constexpr int kTcK = 64;                                    // elements of k in a stage
-constexpr int kTcBox = 64 * 128;                            // bytes of a box
-constexpr int kTcOperand = 2 * kTcBox;                      // a CTA's 128 rows of one plane of one operand
-constexpr int kTcMaxStages = 6;
+constexpr int kTcMaxStages = 10;
 constexpr int kTcWarps = 8;                                 // epilogue warps
 
 constexpr int kTcMaxSlots = 4;
@@ -52,7 +51,8 @@ constexpr int kTcVector = 1024;                             // two vectors of 12
 
 template <typename Op>
 struct TcCfg {
-  static constexpr int kStage = 2 * Op::kPlanes * kTcOperand;
+  static constexpr int kOperand = 128 * Op::kK * 2;         // a CTA's 128 rows of one plane of one operand
+  static constexpr int kStage = 2 * Op::kPlanes * kOperand;
   static constexpr int kStages = Op::kStages;
   static constexpr int kSlotsAt = kStages * kStage, kVectorsAt = kSlotsAt + 2 * Op::kSlots * kTcSlot;
   // Vectors of a half's tiles, in turn.  A tile's are fetched when the slot of its first entry is free; with as many sets
@@ -75,11 +75,13 @@ struct TcTile {
   unsigned int need;
 };
 
-// Strides of the MMA's view of an operand in shared memory, in units of 16 bytes: between 64-row boxes (only where k runs
-// down the columns) and between groups of eight rows of 128 bytes.
+// The MMA's view of an operand in shared memory.  Strides in units of 16 bytes: between boxes of 64 columns (only where k
+// runs down them) and between groups of eight rows.
+template <int K>
 __device__ __forceinline__ unsigned long long tc_desc(unsigned int addr, int mn) {
-  const unsigned long long lead = mn ? kTcBox / 16 : 1;
-  return (unsigned long long)((addr & 0x3ffffu) >> 4) | (lead << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+  const unsigned long long at = (unsigned long long)((addr & 0x3ffffu) >> 4) | (1ull << 46);
+  if (mn) return at | ((unsigned long long)(K * 128 / 16) << 16) | (64ull << 32) | (2ull << 61);
+  return at | (1ull << 16) | (K == 64 ? (64ull << 32) | (2ull << 61) : (32ull << 32) | (4ull << 61));
 }
 
 template <bool PAIR>
@@ -116,15 +118,19 @@ __device__ __forceinline__ void tc_commit(unsigned int bar) {
   else mm_commit(bar);
 }
 
-// This CTA's 128 rows of an operand, 64 elements of k.
-template <bool PAIR>
+// This CTA's 128 rows of an operand, K elements of k.
+template <bool PAIR, int K>
 __device__ __forceinline__ void tc_fetch(unsigned int dst, const CUtensorMap* map, int mn, int row, int k, unsigned int bar) {
-  if constexpr (PAIR) {
-    pair_tma(dst, map, mn ? row : k, mn ? k : row, bar);
-    pair_tma(dst + kTcBox, map, mn ? row + 64 : k, mn ? k : row + 64, bar);
+  auto box = [&](unsigned int at, int x, int y) {
+    if constexpr (PAIR) pair_tma(at, map, x, y, bar);
+    else mm_tma(at, map, x, y, bar);
+  };
+  if (mn) {
+    box(dst, row, k);
+    box(dst + K * 128, row + 64, k);
   } else {
-    mm_tma(dst, map, mn ? row : k, mn ? k : row, bar);
-    mm_tma(dst + kTcBox, map, mn ? row + 64 : k, mn ? k : row + 64, bar);
+    box(dst, k, row);
+    if constexpr (K == 64) box(dst + 64 * 128, k, row + 64);
   }
 }
 
@@ -169,7 +175,7 @@ struct TcWarp {
 };
 
 // Op:
-//   kPair; kPlanes; kStages; kType (0 fp16, 1 bf16); kSegment (0, or: after so many stages the sums are taken over into
+//   kPair; kPlanes; kK; kStages; kType (0 fp16, 1 bf16); kSegment (0, or: after so many stages the sums are taken over into
 //   registers); kSlots; Args with `int* status`
 //   tiles(args); Item item(args, index), what the roles need to know of a tile, read one tile ahead; tile(args, item, TcTile*)
 //   Epilogue(args, item, TcWarp&, cursor): begin() before the sums are there, columns(32 sums of this lane's row, their
@@ -255,9 +261,9 @@ ps_tc_kernel(const __grid_constant__ typename Op::Args args) {
                          "n"(kCtas * Cfg::kStage)
                          : "memory");
 #pragma unroll
-          for (int p = 0; p < Op::kPlanes; ++p, dst += kTcOperand) tc_fetch<kPair>(dst, t.a + p, t.a_mn, row_a, t.a_k + k * kTcK, bar);
+          for (int p = 0; p < Op::kPlanes; ++p, dst += Cfg::kOperand) tc_fetch<kPair, Op::kK>(dst, t.a + p, t.a_mn, row_a, t.a_k + k * Op::kK, bar);
 #pragma unroll
-          for (int p = 0; p < Op::kPlanes; ++p, dst += kTcOperand) tc_fetch<kPair>(dst, t.b + p, t.b_mn, row_b, t.b_k + k * kTcK, bar);
+          for (int p = 0; p < Op::kPlanes; ++p, dst += Cfg::kOperand) tc_fetch<kPair, Op::kK>(dst, t.b + p, t.b_mn, row_b, t.b_k + k * Op::kK, bar);
         }
       }
       if (!ok && rank == 0)                               // an expired wait: let the copies in flight land
@@ -289,20 +295,20 @@ ps_tc_kernel(const __grid_constant__ typename Op::Args args) {
           for (int k = k0; k < k1; ++k, at.next()) {
             if (!tc_wait<kPair>(mm_smem(&ctl.full[0]) + 8 * at.s, at.parity, args.status)) { ok = false; break; }
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const unsigned long long da = tc_desc(base + at.s * Cfg::kStage, t.a_mn);
-            const unsigned long long db = tc_desc(base + at.s * Cfg::kStage + Op::kPlanes * kTcOperand, t.b_mn);
+            const unsigned long long da = tc_desc<Op::kK>(base + at.s * Cfg::kStage, t.a_mn);
+            const unsigned long long db = tc_desc<Op::kK>(base + at.s * Cfg::kStage + Op::kPlanes * Cfg::kOperand, t.b_mn);
             bool more = k > k0;
             if constexpr (Op::kPlanes == 2) {             // the small products first, while the sums are small
 #pragma unroll
-              for (int i = 0; i < kTcK / 16; ++i) {
+              for (int i = 0; i < Op::kK / 16; ++i) {
                 const unsigned long long a = da + i * step_a, b = db + i * step_b;
-                tc_mma<kPair>(d, a, b + kTcOperand / 16, idesc, more || i > 0);
-                tc_mma<kPair>(d, a + kTcOperand / 16, b, idesc, true);
+                tc_mma<kPair>(d, a, b + Cfg::kOperand / 16, idesc, more || i > 0);
+                tc_mma<kPair>(d, a + Cfg::kOperand / 16, b, idesc, true);
               }
               more = true;
             }
 #pragma unroll
-            for (int i = 0; i < kTcK / 16; ++i) tc_mma<kPair>(d, da + i * step_a, db + i * step_b, idesc, more || i > 0);
+            for (int i = 0; i < Op::kK / 16; ++i) tc_mma<kPair>(d, da + i * step_a, db + i * step_b, idesc, more || i > 0);
             tc_commit<kPair>(mm_smem(&ctl.empty[0]) + 8 * at.s);
           }
           tc_commit<kPair>(mm_smem(&ctl.acc_full[0]) + 8 * acc.s);

@@ -67,8 +67,8 @@ XePlan xent_plan(long long T, long long V, long long D) {
   p.pieces = ceil_div(V, p.piece);
   // dx has few tiles, each as long as the piece has words: its words are shared out to slices until one is no longer
   // than half of what a pair computes in a launch
-  const long long tm = ceil_div(T, kXeTile), td = ceil_div(D, kXeTile), tv = p.piece / kXeTile, nk = p.piece / kTcK;
-  const long long total = tm * tv * ceil_div(D, kTcK) + tm * td * nk + tv * td * ceil_div(T, kTcK);
+  const long long tm = ceil_div(T, kXeTile), td = ceil_div(D, kXeTile), tv = p.piece / kXeTile, nk = p.piece / kXeK;
+  const long long total = tm * tv * ceil_div(D, kXeK) + tm * td * nk + tv * td * ceil_div(T, kXeK);
   const long long longest = std::max<long long>(kXeMinStages, total / kXePairs / 2);
   const long long most_slices = std::min<long long>(kXeMaxSlices, std::max(1ll, kXeSliceRows / std::max(1ll, T)));
   p.slices = (int)std::min(most_slices, std::max(1ll, ceil_div(nk, longest)));
@@ -230,7 +230,7 @@ int ps_xent_forward(const ps_xent* q, float* loss, float* lse, void* stream) {
   a.nparts = (int)c.plan.nparts;
   a.score = reinterpret_cast<float*>(c.ws + c.plan.score);
   a.nseg = 1;
-  a.seg[0] = XeSeg{kXeStats, 0, (int)ceil_div(a.T, kXeTile), (int)ceil_div(a.V, kXeTile), 0, (int)ceil_div(a.D, kTcK), 1, 0, 0, 0};
+  a.seg[0] = XeSeg{kXeStats, 0, (int)ceil_div(a.T, kXeTile), (int)ceil_div(a.V, kXeTile), 0, (int)ceil_div(a.D, kXeK), 1, 0, 0, 0};
   rc = launch_segments(&c);
   if (rc) return rc;
   return op_launch("cross entropy", ps_xent_join_kernel, (unsigned)ceil_div(a.T, kXeJoinThreads / 32), kXeJoinThreads, 0, 1,
@@ -278,17 +278,17 @@ int ps_xent_backward(const ps_xent* q, const float* lse, float scale, const floa
     if (k == 0 && dw) a.side = copy_of(c, q->x, q->tokens, q->ldx, p.xm, true, token_scale);
     if (k < p.pieces) {
       const long long v0 = k * p.piece, words = std::min(p.piece, a.V - v0);
-      a.seg[a.nseg++] = XeSeg{kXeProb, 0, tm, (int)ceil_div(words, kXeTile), (int)v0, (int)ceil_div(a.D, kTcK), 1, (int)(k & 1), 0, 0};
+      a.seg[a.nseg++] = XeSeg{kXeProb, 0, tm, (int)ceil_div(words, kXeTile), (int)v0, (int)ceil_div(a.D, kXeK), 1, (int)(k & 1), 0, 0};
     }
     if (k > 0) {
       const long long v0 = (k - 1) * p.piece, words = std::min(p.piece, a.V - v0);
-      const int nk = (int)ceil_div(words, kTcK), buf = (int)((k - 1) & 1);
+      const int nk = (int)ceil_div(words, kXeK), buf = (int)((k - 1) & 1);
       if (dx) {
         const int slices = std::min(p.slices, nk);       // (the last piece may be short; earlier ones filled all)
         a.seg[a.nseg++] = XeSeg{kXeDx, 0, tm, td, (int)v0, nk, slices, buf, k == 1, k == p.pieces && p.slices == 1};
         filled = std::max(filled, slices);
       }
-      if (dw) a.seg[a.nseg++] = XeSeg{kXeDw, 0, (int)ceil_div(words, kXeTile), td, (int)v0, (int)ceil_div(a.T, kTcK), 1, buf, 0, 0};
+      if (dw) a.seg[a.nseg++] = XeSeg{kXeDw, 0, (int)ceil_div(words, kXeTile), td, (int)v0, (int)ceil_div(a.T, kXeK), 1, buf, 0, 0};
     }
     rc = launch_segments(&c);
     if (rc) return rc;

@@ -21,7 +21,7 @@
 
 namespace psb {
 
-constexpr int kXeTile = 256;
+constexpr int kXeTile = 256, kXeK = 64;
 
 enum { kXeStats = 0, kXeProb = 1, kXeDx = 2, kXeDw = 3 };
 
@@ -157,7 +157,7 @@ __device__ __forceinline__ void xe_store_f32(float* o, const float* v, int live,
 
 struct XeOp {
   static constexpr bool kPair = true;
-  static constexpr int kPlanes = 1, kType = 1, kStages = 6, kSlots = 0, kSegment = 0;
+  static constexpr int kPlanes = 1, kType = 1, kK = kXeK, kStages = 6, kSlots = 0, kSegment = 0;
   static constexpr bool kSide = true;
   using Args = XeArgs;
 
@@ -207,8 +207,8 @@ struct XeOp {
       t->a = &a.d[s.buf];
       t->b = &a.w;
       t->b_mn = 1;
-      t->a_k = k0 * kTcK;
-      t->b_k = s.v0 + k0 * kTcK;
+      t->a_k = k0 * kXeK;
+      t->b_k = s.v0 + k0 * kXeK;
       t->nk = k1 - k0;
     } else {                             // words x width, over the tokens
       t->a = &a.d[s.buf];
