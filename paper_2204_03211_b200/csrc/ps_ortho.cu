@@ -3,8 +3,10 @@
 #include <cmath>
 #include <cstdint>
 #include <cstring>
+#include <functional>
 #include <mutex>
 #include <new>
+#include <utility>
 
 #include "ps_ortho.h"
 #include "ps_ortho_small.cuh"
@@ -116,6 +118,9 @@ bool make_map(EncodeTiled encode, CUtensorMap* m, const void* p, long long rows,
 // for has long been done.
 constexpr long long kNsGroupTiles = 2 * 74;
 
+// What a tile costs besides its products, in elements of k.
+constexpr long long kNsTileCost = 256;
+
 // Pairs of CTAs fetch half as much from L2 per product as single ones; single ones have four times as many tiles, and
 // their products are done in half the time.  Lists of more than this many 256 x 256 tiles take pairs.  Single | pairs,
 // bf16 results, us: 24 x 512 x 512 (96 tiles) 209 | 253, 36 x 512 x 2048 (576) 746 | 680, 24 x 1024 x 4096 (1536) 2779 | 2213.
@@ -206,6 +211,7 @@ int NsPlan::build(const std::vector<NsItem>& items, bool split, void* workspace,
   std::vector<CUtensorMap> maps(small_ ? 0 : kNsMaps * n);
   std::vector<NsMat> mats(n);
   std::vector<NsTile> list;
+  std::vector<int> begin, owner;
   std::vector<int2> units;
   std::memset(mats.data(), 0, n * sizeof(NsMat));
   std::memset(maps.data(), 0, maps.size() * sizeof(CUtensorMap));
@@ -290,6 +296,28 @@ int NsPlan::build(const std::vector<NsItem>& items, bool split, void* workspace,
             for (int b = 0; b < (product == 2 ? tn : mirror ? a + 1 : tm); ++b)
               list.push_back(NsTile{(int)i, (short)step, (short)product, a, b});
         }
+  // each tile to the CTA (or pair) that has least to do so far, every CTA's in the order of all
+  if (!small_) {
+    const int workers = (int)std::min<size_t>(list.size(), (size_t)room);
+    using Load = std::pair<long long, int>;
+    std::vector<Load> loads;
+    for (int w = 0; w < workers; ++w) loads.push_back(Load(0, w));
+    begin.assign((size_t)workers + 1, 0);
+    for (const NsTile& t : list) {       // (a heap of loads: least first)
+      std::pop_heap(loads.begin(), loads.end(), std::greater<Load>());
+      Load& l = loads.back();
+      owner.push_back(l.second);
+      ++begin[(size_t)l.second + 1];
+      l.first += (t.product == 0 ? mats[(size_t)t.mat].n : mats[(size_t)t.mat].m) + kNsTileCost;
+      std::push_heap(loads.begin(), loads.end(), std::greater<Load>());
+    }
+    for (int w = 0; w < workers; ++w) begin[(size_t)w + 1] += begin[(size_t)w];
+    std::vector<NsTile> dealt(list.size());
+    std::vector<int> at_worker(begin.begin(), begin.end() - 1);
+    for (size_t t = 0; t < list.size(); ++t) dealt[(size_t)at_worker[(size_t)owner[t]]++] = list[t];
+    list.swap(dealt);
+    grid_ = workers * (pair_ ? 2 : 1);
+  }
   size_t off = 0;
   auto take = [&](size_t bytes) {
     const size_t here = off;
@@ -299,6 +327,7 @@ int NsPlan::build(const std::vector<NsItem>& items, bool split, void* workspace,
   const size_t maps_off = take(maps.size() * sizeof(CUtensorMap));
   mats_off_ = take(n * sizeof(NsMat));
   list_off_ = take(list.size() * sizeof(NsTile));
+  begin_off_ = take(begin.size() * sizeof(int));
   units_off_ = take(units.size() * sizeof(int2));
   const size_t done_off = take(n * sizeof(unsigned int) * 32);         // a line each
   const size_t status_off = take(sizeof(int));
@@ -316,15 +345,14 @@ int NsPlan::build(const std::vector<NsItem>& items, bool split, void* workspace,
   put(maps_off, maps.data(), maps.size() * sizeof(CUtensorMap));
   put(mats_off_, mats.data(), n * sizeof(NsMat));
   put(list_off_, list.data(), list.size() * sizeof(NsTile));
+  put(begin_off_, begin.data(), begin.size() * sizeof(int));
   put(units_off_, units.data(), units.size() * sizeof(int2));
   if (e == cudaSuccess) e = cudaMemset(mem_ + done_off, 0, status_off + sizeof(int) - done_off);
   if (e == cudaSuccess) e = cudaStreamSynchronize(cudaStreamLegacy);   // before other streams use it
   if (e != cudaSuccess) return op_cuda_error("tables of the orthogonalisation", e);
   status_ = status ? status : reinterpret_cast<int*>(mem_ + status_off);
   count_ = (int)n;
-  tiles_ = (int)list.size();
   units_ = (int)units.size();
-  grid_ = (pair_ ? 2 : 1) * std::min(tiles_, room);
   split_ = split;
   return PS_OK;
 }
@@ -347,7 +375,7 @@ int NsPlan::run(cudaStream_t stream, int* launches) const {
   a.status = status_;
   a.mats = mats;
   a.list = reinterpret_cast<const NsTile*>(mem_ + list_off_);
-  a.tiles = tiles_;
+  a.begin = reinterpret_cast<const int*>(mem_ + begin_off_);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)grid_);
   cfg.blockDim = dim3(kTcThreads);

@@ -5,7 +5,8 @@
 // Three products per step and 15 per matrix, each needing the one before it, for a list of matrices at once.  All of
 // them run in ONE cooperative launch of the frame of ps_tc.cuh: every tile names the matrix and the product it belongs
 // to, tiles are listed step by step, and a tile waits until its matrix's earlier products are done (one counter per
-// matrix).  Every pair of CTAs takes its tiles in the list's order, so whatever a tile waits for is being worked on;
+// matrix).  The host deals the tiles out, each to the CTA that has least to do so far, and every CTA works on its own in
+// the order of all: the first unfinished tile of all is always the next one of its CTA, so every wait ends;
 // there is no barrier over the grid, and one matrix's wait is another one's work.  A and B are symmetric: where the tiles
 // outnumber the CTAs only those on and below the diagonal are computed, and stored twice.
 //
@@ -73,8 +74,8 @@ struct NsTile {                          // one tile of the list
 struct NsArgs {
   int* status;
   const NsMat* mats;
-  const NsTile* list;
-  int tiles;
+  const NsTile* list;                    // CTA after CTA (or pair), each with its tiles in their common order
+  const int* begin;                      // where each one's start, and the end
 };
 
 // c + a and c - a for the lower and the upper of two fp16 numbers: mixed-precision additions widen as they add.
@@ -166,11 +167,15 @@ struct NsOp {
   static constexpr int kSegment = PLANES == 1 ? 0 : PAIR ? 8 : 4;
   using Args = NsArgs;
 
-  static __device__ __forceinline__ int tiles(const NsArgs& a) { return a.tiles; }
+  static __device__ __forceinline__ void tiles(const NsArgs& a, int mine, int, int* first, int* end, int* stride) {
+    *first = a.begin[mine];
+    *end = a.begin[mine + 1];
+    *stride = 1;
+  }
 
   using Item = NsTile;
 
-  static __device__ __forceinline__ Item item(const NsArgs& a, int index, int tiles) { return a.list[min(index, tiles - 1)]; }
+  static __device__ __forceinline__ Item item(const NsArgs& a, int index, int tiles) { return a.list[max(0, min(index, tiles - 1))]; }
 
   static __device__ __forceinline__ int stages(const NsArgs& a, const NsTile& at) {
     const NsMat& M = a.mats[at.mat];

@@ -43,8 +43,8 @@ class NsPlan {
  private:
   unsigned char* mem_ = nullptr;
   int* status_ = nullptr;
-  size_t mats_off_ = 0, list_off_ = 0, units_off_ = 0;
-  int count_ = 0, tiles_ = 0, units_ = 0, grid_ = 0;
+  size_t mats_off_ = 0, list_off_ = 0, begin_off_ = 0, units_off_ = 0;
+  int count_ = 0, units_ = 0, grid_ = 0;
   int small_ = 0;                        // > 0: in shared memory, with so many CTAs per matrix
   bool split_ = false, pair_ = false, norms_ = false;
 };

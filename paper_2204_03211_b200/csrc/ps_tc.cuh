@@ -177,7 +177,7 @@ struct TcWarp {
 // Op:
 //   kPair; kPlanes; kK; kStages; kType (0 fp16, 1 bf16); kSegment (0, or: after so many stages the sums are taken over into
 //   registers); kSlots; Args with `int* status`
-//   tiles(args); Item item(args, index), what the roles need to know of a tile, read one tile ahead; tile(args, item, TcTile*)
+//   tiles(args, this CTA or pair, their number, first, end, stride); Item item(args, index), what the roles need to know of a tile, read one tile ahead; tile(args, item, TcTile*)
 //   Epilogue(args, item, TcWarp&, cursor): begin() before the sums are there, columns(32 sums of this lane's row, their
 //   place among the warp's columns), end()
 //   kSide (without slots): warps 2 and 3 do side(args, thread, threads)
@@ -231,7 +231,8 @@ ps_tc_kernel(const __grid_constant__ typename Op::Args args) {
   const unsigned int tmem = ctl.tmem;
   mm_pdl();
 
-  const int tiles = Op::tiles(args), stride = (int)(gridDim.x / kCtas), first = (int)(blockIdx.x / kCtas);
+  int first, tiles, stride;                               // this CTA's (pair's) tiles: first, first + stride, ... below `tiles`
+  Op::tiles(args, (int)(blockIdx.x / kCtas), (int)(gridDim.x / kCtas), &first, &tiles, &stride);
 
   // Taking sums over into registers needs more of them than a third of the file per warpgroup: 128 x (40 + 2 x 232) is
   // what the 384 threads were launched with (168 each).

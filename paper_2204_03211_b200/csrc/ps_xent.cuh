@@ -182,7 +182,11 @@ struct XeOp {
     return at;
   }
 
-  static __device__ __forceinline__ int tiles(const XeArgs& a) { return a.tiles; }
+  static __device__ __forceinline__ void tiles(const XeArgs& a, int mine, int all, int* first, int* end, int* stride) {
+    *first = mine;
+    *end = a.tiles;
+    *stride = all;
+  }
   static __device__ __forceinline__ Item item(const XeArgs&, int index, int) { return index; }
   static __device__ __forceinline__ void side(const XeArgs& a, int thread, int threads) {
     if (a.side.src) xe_copy(a.side, thread, threads);
