@@ -767,13 +767,14 @@ typedef struct ps_ortho ps_ortho; /* opaque */
 
 typedef struct {
   void* data;                    /* device; sources are only read */
-  long long rows, cols, ld;      /* row stride in elements, >= cols */
+  long long rows, cols, ld;      /* 0..2^24 each; row stride in elements, >= cols */
 } ps_matrix;
 
 /* Remembers n matrices (host arrays, copied): source i of src_dtype gives destination i of
  * dst_dtype.  Destinations must not overlap each other; a destination may be its own or another
  * source, all sources are read before any result is written.  Empty matrices are allowed.  Waits until the
- * tables are on the device.  Errors: BAD_ARG (shapes differ, ld < cols, NULL), ALIGN, TOO_LARGE, NOMEM, CUDA. */
+ * tables are on the device.  Errors: BAD_ARG (shapes differ, ld < cols, NULL, two destinations that start at the
+ * same address), ALIGN, TOO_LARGE, NOMEM, CUDA. */
 int ps_ortho_create(ps_ortho** out, int device, int n, const ps_matrix* srcs, int src_dtype, const ps_matrix* dsts,
                     int dst_dtype);
 
@@ -801,6 +802,7 @@ int ps_ortho_destroy(ps_ortho* o);
  * included.  exp(s - lse) - [...] is rounded to bf16, the sums over it are binary32; token_scale
  * is applied to dx's sums, and for dw to x, rounded to bf16.  A score that is a NaN or
  * +infinity makes its token's loss and gradients NaN.
+ * dx and dw must not overlap the inputs or each other.
  * The calls run on `stream` of the CURRENT device, allocate nothing and wait for nothing.
  * ------------------------------------------------------------------------- */
 typedef struct {
@@ -810,7 +812,7 @@ typedef struct {
   long long ldw;
   const void* targets;           /* device, one whole number of target_bits (32 or 64) per token */
   int target_bits;
-  long long tokens, vocab, dim;  /* tokens >= 0, vocab and dim >= 1, each below 2^30 */
+  long long tokens, vocab, dim;  /* 0..2^26, 1..2^30, 1..2^24 */
   void* workspace;               /* device, 256-byte aligned, the caller's; its contents mean nothing between calls */
   size_t workspace_bytes;
 } ps_xent;

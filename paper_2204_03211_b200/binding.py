@@ -931,6 +931,7 @@ class CrossEntropy:
                                      dtype=torch.uint8, device=device or "cuda")
         self.device = self.workspace.get_device()
         self._types = {torch.int32: 32, torch.int64: 64}
+        self._current = torch.cuda.current_device
         self._bf16, self._f32, self._empty = torch.bfloat16, torch.float32, torch.empty
 
     def _bad(self, where, text):
@@ -952,6 +953,8 @@ class CrossEntropy:
 
     def _args(self, x, w, targets, where):
         n = x.shape[0] if x.dim() == 2 else -1
+        if self._current() != self.device:
+            self._bad(where, "GPU %d is not the current device" % self.device)
         if n > self.tokens:
             self._bad(where, "%d tokens, made for %d" % (n, self.tokens))
         ldx, ldw = self._matrix(x, n, (self._bf16,), where, "x"), self._matrix(w, self.vocab, (self._bf16,), where, "w")

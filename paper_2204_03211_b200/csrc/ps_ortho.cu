@@ -15,7 +15,7 @@ namespace psb {
 namespace {
 
 constexpr int kNsMaxDevices = 64;
-constexpr long long kNsMaxDim = 1ll << 30;       // (TMA coordinates are 32-bit)
+constexpr long long kNsMaxDim = 1ll << 24;       // (a tile of the longest product takes 0.3 s, bounded waits a second)
 constexpr long long kNsMaxTiles = 1ll << 26;     // tiles and units of a list
 
 struct NsDevice {
@@ -431,7 +431,7 @@ int ps_ortho_create(ps_ortho** out, int device, int n, const ps_matrix* srcs, in
     std::vector<NsItem> items((size_t)n);
     for (int i = 0; i < n; ++i) {
       const ps_matrix &s = srcs[i], &d = dsts[i];
-      if (s.rows < 0 || s.cols < 0 || s.rows >= kNsMaxDim || s.cols >= kNsMaxDim || d.rows != s.rows || d.cols != s.cols)
+      if (s.rows < 0 || s.cols < 0 || s.rows > kNsMaxDim || s.cols > kNsMaxDim || d.rows != s.rows || d.cols != s.cols)
         return PS_ERR_BAD_ARG;
       if (s.rows == 0 || s.cols == 0) continue;
       if (!s.data || !d.data || s.ld < s.cols || d.ld < d.cols) return PS_ERR_BAD_ARG;
@@ -449,6 +449,11 @@ int ps_ortho_create(ps_ortho** out, int device, int n, const ps_matrix* srcs, in
     const bool split = dst_dtype == PS_F32;
     const size_t bytes = NsPlan::workspace(items, split);
     if (!bytes) return PS_ERR_TOO_LARGE;
+    std::vector<const void*> to;
+    for (const NsItem& it : items)
+      if (it.dst) to.push_back(it.dst);
+    std::sort(to.begin(), to.end());
+    if (std::adjacent_find(to.begin(), to.end()) != to.end()) return PS_ERR_BAD_ARG;
     DeviceScope on(device);
     cudaError_t e = on.error;
     if (e != cudaSuccess) return op_cuda_error("cudaSetDevice", e);

@@ -13,7 +13,9 @@ namespace {
 static __device__ int g_xent_status;
 
 constexpr int kXeMaxDevices = 64;
-constexpr long long kXeMaxDim = 1ll << 30;       // (TMA coordinates are 32-bit)
+// (A tile sums over the tokens, the width or a piece of the words: 0.3 s for the longest, where bounded waits are a second.
+// TMA coordinates are 32-bit.)
+constexpr long long kXeMaxTokens = 1ll << 26, kXeMaxWidth = 1ll << 24, kXeMaxWords = 1ll << 30;
 
 struct XeDevice {
   bool ready = false;
@@ -126,8 +128,8 @@ struct XeCall {
 bool rows_aligned(const void* p, long long ld) { return !misaligned(p, 16) && ld % 8 == 0; }
 
 int check(const ps_xent* q, XeCall* c) {
-  if (!q || q->tokens < 0 || q->vocab < 1 || q->dim < 1 || q->tokens >= kXeMaxDim || q->vocab >= kXeMaxDim ||
-      q->dim >= kXeMaxDim || q->ldx < q->dim || q->ldw < q->dim || (q->target_bits != 32 && q->target_bits != 64))
+  if (!q || q->tokens < 0 || q->vocab < 1 || q->dim < 1 || q->tokens > kXeMaxTokens || q->vocab > kXeMaxWords ||
+      q->dim > kXeMaxWidth || q->ldx < q->dim || q->ldw < q->dim || (q->target_bits != 32 && q->target_bits != 64))
     return PS_ERR_BAD_ARG;
   if (!q->w || !q->workspace || (q->tokens > 0 && (!q->x || !q->targets))) return PS_ERR_BAD_ARG;
   if (misaligned(q->x, 2) || misaligned(q->w, 2) || misaligned(q->targets, q->target_bits / 8) || misaligned(q->workspace, 256))
@@ -210,7 +212,7 @@ using namespace psb;
 extern "C" {
 
 int ps_xent_sizes(long long tokens, long long vocab, long long dim, size_t* bytes_out, size_t* bytes_unaligned_out) {
-  if (tokens < 0 || vocab < 1 || dim < 1 || tokens >= kXeMaxDim || vocab >= kXeMaxDim || dim >= kXeMaxDim) return PS_ERR_BAD_ARG;
+  if (tokens < 0 || vocab < 1 || dim < 1 || tokens > kXeMaxTokens || vocab > kXeMaxWords || dim > kXeMaxWidth) return PS_ERR_BAD_ARG;
   if (bytes_out) *bytes_out = xent_bytes(tokens, vocab, dim, false);
   if (bytes_unaligned_out) *bytes_unaligned_out = xent_bytes(tokens, vocab, dim, true);
   return PS_OK;

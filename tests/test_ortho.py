@@ -127,6 +127,33 @@ def test_large_matrix_in_pairs():
 
 
 @gpu
+def test_offsets_past_2_31():
+    """Rows 2^23 elements apart: the last one starts past the 2^31st element of either tensor."""
+    m, n, ld = 300, 520, 1 << 23
+    base, to = torch.empty(m, ld, device="cuda"), torch.empty(m, ld, device="cuda", dtype=BF)
+    for rows, cols in ((m, n), (m, 100)):                   # the general form, and the small one
+        x, out = base[:rows, :cols], to[:rows, :cols]
+        x.copy_(matrix(rows, cols, "normal"))
+        o = B.Ortho([x], [out])
+        o.run()
+        assert o.status() == 0
+        check(x, out)
+
+
+@gpu
+def test_long_rows():
+    """Sums over 200 000 elements, and as many columns of a result."""
+    for rows, cols in ((3, 200_000), (140, 100_000), (100_000, 140)):
+        x = matrix(rows, cols, "normal")
+        for dst in (F32, BF):
+            out = torch.empty(rows, cols, device="cuda", dtype=dst)
+            o = B.Ortho([x], [out])
+            o.run()
+            assert o.status() == 0
+            check(x, out)
+
+
+@gpu
 def test_rows_of_wider_tensors_and_in_place():
     base = torch.randn(90, 300, device="cuda")
     wide = torch.full((90, 200), 5.0, device="cuda")
@@ -214,7 +241,9 @@ def test_refusals():
     bad = B.PS_ERR_BAD_ARG
     assert create(src=(0, 4, 8, 8)) == create(dst=(0, 4, 8, 8)) == create(src=(4096, 4, 8, 7)) == create(dst=(8192, 4, 8, 7)) == bad
     assert create(dst=(8192, 8, 4, 8)) == create(src=(4096, -1, 8, 8)) == create(st=2) == create(dt=-1) == create(device=-1) == bad
-    assert create(n=-1) == create(src=(4096, 1 << 30, 8, 8), dst=(8192, 1 << 30, 8, 8)) == bad
+    assert create(n=-1) == create(src=(4096, (1 << 24) + 1, 8, 8), dst=(8192, (1 << 24) + 1, 8, 8)) == bad
+    s, d = (B.ps_matrix * 2)((4096, 4, 8, 8), (4096, 4, 8, 8)), (B.ps_matrix * 2)((8192, 4, 8, 8), (8192, 4, 8, 8))
+    assert lib.ps_ortho_create(C.byref(h), 0, 2, s, B.PS_F32, d, B.PS_F32) == bad          # two results in one place
     assert create(src=(4098, 4, 8, 8)) == create(dst=(8193, 4, 8, 8), dt=B.PS_BF16) == B.PS_ERR_ALIGN
     big = (1 << 21, 1 << 21, 1 << 21)
     assert create(src=(4096, *big), dst=(8192, *big)) == B.PS_ERR_TOO_LARGE

@@ -199,6 +199,57 @@ def test_large_scores():
 
 
 @gpu
+@pytest.mark.parametrize("T,V,D", [(70_000, 300, 32_768), (300, 70_000, 32_768)])
+def test_offsets_past_2_31(T, V, D):
+    """Operands and results of 2.3 G elements: rows at both ends and around the 2^31st element against the formula."""
+    x = torch.empty(T, D, device="cuda", dtype=BF)
+    w = torch.empty(V, D, device="cuda", dtype=BF)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    for m in (x, w):
+        for r in range(0, m.shape[0], 4096):
+            m[r:r + 4096] = torch.randn(m[r:r + 4096].shape, device="cuda", generator=g)
+    w *= 0.01
+    t = torch.randint(0, V, (T,), device="cuda", generator=g)
+    ce = B.CrossEntropy(T, V, D)
+    loss, lse = ce.forward(x, w, t)
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    ce.backward(x, w, t, lse, dx, dw)
+    torch.cuda.synchronize()
+    assert B.ps_xent_status() == 0
+    edge = 2 ** 31 // D
+    rows = [r for r in (0, 1, edge - 1, edge, edge + 1, T - 1) if r < T]
+    words = [v for v in (0, edge - 1, edge, edge + 1, V - 1) if v < V]
+
+    def scores(rs):                                         # in 64 bits, a part of the width at a time
+        return sum(x[rs, c:c + 2048].double() @ w[:, c:c + 2048].double().t() for c in range(0, D, 2048))
+
+    for r in rows:
+        s = scores([r])[0]
+        l = torch.logsumexp(s, 0)
+        ds = 2 * D * 2.0 ** -24 * float((x[r].double().abs()[None] @ w[:1000].double().abs().t()).max()) * 4
+        assert abs(float(lse[r]) - float(l)) <= ds + 1e-5
+        assert abs(float(loss[r]) - float(l - s[t[r]])) <= 2 * ds + 1e-5
+        e = torch.exp(s - l)
+        e[t[r]] -= 1
+        cols = [0, 5, D - 1]
+        ref = e @ w[:, cols].double()
+        tol = 2.0 ** -8 * (e.abs() @ w[:, cols].double().abs()) + 2.0 ** -8 * ref.abs() + ds
+        assert bool(((dx[r, cols].double() - ref).abs() <= tol).all())
+    if T <= 1000:                                           # (dw needs the scores of all tokens)
+        s = scores(list(range(T)))
+        e = torch.exp(s - torch.logsumexp(s, 1)[:, None])
+        e[torch.arange(T), t] -= 1
+    else:
+        e = torch.cat([(lambda s: torch.exp(s - torch.logsumexp(s, 1)[:, None]))(scores(list(range(a, min(T, a + 5000)))))
+                       for a in range(0, T, 5000)])
+        e[torch.arange(T), t] -= 1
+    cols = [0, 5, D - 1]
+    ref = e[:, words].t() @ x[:, cols].double()
+    tol = 2.0 ** -7 * (e[:, words].abs().t() @ x[:, cols].double().abs()) + 2.0 ** -8 * ref.abs()
+    assert bool(((dw[words][:, cols].double() - ref).abs() <= tol).all())
+
+
+@gpu
 def test_no_tokens():
     ce = B.CrossEntropy(0, 90, 24)
     x, w = torch.empty(0, 24, device="cuda", dtype=BF), torch.randn(90, 24, device="cuda").to(BF)
@@ -289,13 +340,14 @@ def made_up(**kw):
 
 @pytest.mark.parametrize("kw,status", [
     (dict(tokens=-1), B.PS_ERR_BAD_ARG), (dict(vocab=0), B.PS_ERR_BAD_ARG), (dict(dim=0), B.PS_ERR_BAD_ARG),
-    (dict(tokens=1 << 30), B.PS_ERR_BAD_ARG), (dict(ldx=63), B.PS_ERR_BAD_ARG), (dict(ldw=10), B.PS_ERR_BAD_ARG),
+    (dict(tokens=(1 << 26) + 1), B.PS_ERR_BAD_ARG), (dict(vocab=(1 << 30) + 1), B.PS_ERR_BAD_ARG),
+    (dict(dim=(1 << 24) + 1, ldx=1 << 25, ldw=1 << 25), B.PS_ERR_BAD_ARG), (dict(ldx=63), B.PS_ERR_BAD_ARG), (dict(ldw=10), B.PS_ERR_BAD_ARG),
     (dict(target_bits=16), B.PS_ERR_BAD_ARG), (dict(x=0), B.PS_ERR_BAD_ARG), (dict(w=0), B.PS_ERR_BAD_ARG),
     (dict(targets=0), B.PS_ERR_BAD_ARG), (dict(workspace=0), B.PS_ERR_BAD_ARG), (dict(x=(1 << 20) + 1), B.PS_ERR_ALIGN),
     (dict(w=(1 << 21) + 1), B.PS_ERR_ALIGN), (dict(targets=(1 << 22) + 4), B.PS_ERR_ALIGN),
     (dict(workspace=(1 << 24) + 128), B.PS_ERR_ALIGN), (dict(workspace_bytes=1000), B.PS_ERR_NOMEM),
     (dict(ldw=68, workspace_bytes=1000), B.PS_ERR_NOMEM),
-    (dict(tokens=(1 << 30) - 1, vocab=(1 << 30) - 1, workspace_bytes=1 << 62), B.PS_ERR_TOO_LARGE)])
+    (dict(tokens=1 << 26, vocab=1 << 30, workspace_bytes=1 << 62), B.PS_ERR_TOO_LARGE)])
 def test_refusals(kw, status):
     lib, q = B.load(), made_up(**kw)
     assert lib.ps_xent_forward(C.byref(q), 1 << 23, 1 << 23, None) == status
