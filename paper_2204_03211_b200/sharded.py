@@ -116,6 +116,13 @@ class ShardedService:
         self.svc.register_block(job, block, nelem, ctx, init)
         return True
 
+    def register_matrix(self, job: int, block: int, rows: int, cols: int, ctx: int = 0, init=None, update_scale=None) -> bool:
+        """Block of a PS_MUON job.  Such an update is a block's own, so a job's blocks may have several owners."""
+        if not self.owns(job, block):
+            return False
+        self.svc.register_matrix(job, block, rows, cols, ctx, init, update_scale)
+        return True
+
     def push(self, job: int, block: int, worker: int, ptr) -> bool:
         """`ptr`: the shard's address in THIS process (a mapped peer address or a
         local one)."""

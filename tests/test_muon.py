@@ -322,3 +322,14 @@ def test_planning_knows_matrices():
 def test_noalloc_refuses():
     d = B.ps_job_desc(B.PS_MUON, B.PS_F32, 1, 0.1, 0.9, 0, 0, 0, 0, 1)
     refused(B.PS_ERR_BAD_ARG, B.ps_aggregate_block_noalloc, d, 1, 16, 4096, 8192, None, [4096])
+
+
+def test_sharded_service_registers_what_it_owns():
+    from paper_2204_03211_b200 import sharded
+    sh = sharded.ShardedService(1, 2, B.PS_DEVICE_NONE, 1, 1 << 20)
+    j = sh.register_job(opt=B.PS_MUON, grad_dtype=B.PS_F32, num_workers=1, lr=0.1, momentum=0.9, weight_decay=0.0)
+    sh.set_owners({(j, 0): 0, (j, 1): 1})
+    assert not sh.register_matrix(j, 0, 8, 4) and sh.register_matrix(j, 1, 4, 8)
+    assert sh.svc.arena_info(0)[0] == 2 * 256
+    refused(B.PS_ERR_BAD_ARG, sh.register_block, j, 1, 32)
+    sh.close()
