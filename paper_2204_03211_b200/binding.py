@@ -202,7 +202,7 @@ def load():
     return _lib
 
 
-_FROM_OPS = ("ps_mx_quantize", "ps_mx_dequantize", "ps_mx_matmul", "MxTensor")
+_FROM_OPS = ("ps_mx_quantize", "ps_mx_dequantize", "ps_mx_matmul", "MxTensor", "CrossEntropy")
 
 
 def __getattr__(name):
@@ -773,6 +773,7 @@ def _load_ops():
     from . import _ops
     _DTYPES.update({torch.float32: PS_F32, torch.bfloat16: PS_BF16})
     _ops.setup(torch.float32, torch.bfloat16, _raise_op)
+    _ops.setup_targets(torch.int32, torch.int64)
 
     class MxTensor(_ops.Operand):
         """A microscaled 4-bit operand of rows x cols elements and the two device
@@ -793,10 +794,43 @@ def _load_ops():
         def shape(self):
             return self.rows, self.cols
 
+    class CrossEntropy(_ops.Loss):
+        """Losses and gradients of up to `tokens` tokens over a vocabulary (ps_xent_*), with the workspace they need.
+        x is tokens x dim and w vocab x dim (bfloat16, any row stride), targets int32 or int64; all tensors on this
+        object's device, which has to be the current one.  `aligned`: whether x's and w's rows start on 16-byte
+        boundaries (default: whether rows of dim elements do).  Calls of one object must not overlap on the GPU."""
+
+        def __new__(cls, tokens: int, vocab: int, dim: int, device=None, aligned: bool | None = None):
+            return super().__new__(cls)
+
+        def __init__(self, tokens: int, vocab: int, dim: int, device=None, aligned: bool | None = None):
+            sizes = ps_xent_sizes(tokens, vocab, dim)
+            self.tokens, self.vocab, self.dim = tokens, vocab, dim
+            self.workspace = torch.empty(sizes[0 if (dim % 8 == 0 if aligned is None else aligned) else 1],
+                                         dtype=torch.uint8, device=device or "cuda")
+            self.device = self.workspace.get_device()
+            super().__init__(tokens, vocab, dim, self.workspace.data_ptr(), self.workspace.numel(), self.device)
+
+        def forward(self, x, w, targets, loss=None, lse=None, stream=None):
+            """Returns (loss, lse): one float32 per token, in the tensors given or in new ones."""
+            if loss is None:
+                loss = torch.empty(len(x), dtype=torch.float32, device=x.device)
+            if lse is None:
+                lse = torch.empty(len(x), dtype=torch.float32, device=x.device)
+            self._forward(x, w, targets, loss, lse, stream)
+            return loss, lse
+
+        def backward(self, x, w, targets, lse, dx=None, dw=None, scale: float = 1.0, token_scale=None, stream=None):
+            """dx (bfloat16) and dw (bfloat16 or float32), either of them None: the gradients of
+            sum(scale * token_scale * loss), written to the tensors given."""
+            self._backward(x, w, targets, lse, dx, dw, scale, token_scale, stream)
+            return dx, dw
+
     MxTensor.__qualname__ = "MxTensor"
+    CrossEntropy.__qualname__ = "CrossEntropy"
     for name in _FROM_OPS[:3]:
         globals()[name] = getattr(_ops, name)
-    globals()["MxTensor"] = MxTensor
+    globals()["MxTensor"], globals()["CrossEntropy"] = MxTensor, CrossEntropy
 
 
 class Clip:
@@ -914,82 +948,6 @@ def ps_xent_status() -> int:
     v = C.c_int()
     _check_op(load().ps_xent_status(C.byref(v)), "ps_xent_status")
     return v.value
-
-
-class CrossEntropy:
-    """Losses and gradients of up to `tokens` tokens over a vocabulary (ps_xent_*), with the workspace they need.
-    x is tokens x dim and w vocab x dim (bfloat16, any row stride), targets int32 or int64; all tensors on this
-    object's device, which has to be the current one.  `aligned`: whether x's and w's rows start on 16-byte
-    boundaries (default: whether rows of dim elements do).  Calls of one object must not overlap on the GPU."""
-
-    def __init__(self, tokens: int, vocab: int, dim: int, device=None, aligned: bool | None = None):
-        import torch
-
-        sizes = ps_xent_sizes(tokens, vocab, dim)
-        self.tokens, self.vocab, self.dim = tokens, vocab, dim
-        self.workspace = torch.empty(sizes[0 if (dim % 8 == 0 if aligned is None else aligned) else 1],
-                                     dtype=torch.uint8, device=device or "cuda")
-        self.device = self.workspace.get_device()
-        self._types = {torch.int32: 32, torch.int64: 64}
-        self._current = torch.cuda.current_device
-        self._bf16, self._f32, self._empty = torch.bfloat16, torch.float32, torch.empty
-
-    def _bad(self, where, text):
-        raise PsError(PS_ERR_BAD_ARG, where, text)
-
-    def _matrix(self, t, rows, dtypes, where, name):
-        if t.get_device() != self.device or t.dtype not in dtypes or t.dim() != 2 or tuple(t.shape) != (rows, self.dim) or (
-                self.dim > 1 and t.stride(1) != 1):
-            self._bad(where, "%s: a %d x %d matrix of %s with contiguous rows is wanted on GPU %d" % (
-                name, rows, self.dim, " or ".join(str(d)[6:] for d in dtypes), self.device))
-        return t.stride(0) if rows > 1 else max(t.stride(0), self.dim)
-
-    def _floats(self, t, n, where, name):
-        if t is None:
-            return None
-        if t.get_device() != self.device or t.dtype != self._f32 or t.numel() != n or not t.is_contiguous():
-            self._bad(where, "%s: %d contiguous float32 are wanted on GPU %d" % (name, n, self.device))
-        return t.data_ptr()
-
-    def _args(self, x, w, targets, where):
-        n = x.shape[0] if x.dim() == 2 else -1
-        if self._current() != self.device:
-            self._bad(where, "GPU %d is not the current device" % self.device)
-        if n > self.tokens:
-            self._bad(where, "%d tokens, made for %d" % (n, self.tokens))
-        ldx, ldw = self._matrix(x, n, (self._bf16,), where, "x"), self._matrix(w, self.vocab, (self._bf16,), where, "w")
-        bits = self._types.get(targets.dtype)
-        if bits is None or targets.get_device() != self.device or targets.numel() != n or not targets.is_contiguous():
-            self._bad(where, "targets: %d contiguous int32 or int64 are wanted on GPU %d" % (n, self.device))
-        ws = self.workspace
-        return n, ps_xent(x.data_ptr(), ldx, w.data_ptr(), ldw, targets.data_ptr(), bits, n, self.vocab, self.dim,
-                          ws.data_ptr(), ws.numel())
-
-    def forward(self, x, w, targets, loss=None, lse=None, stream=None):
-        """Returns (loss, lse): one float32 per token, in the tensors given or in new ones."""
-        where = "ps_xent_forward"
-        n, q = self._args(x, w, targets, where)
-        loss = self._empty(n, dtype=self._f32, device=x.device) if loss is None else loss
-        lse = self._empty(n, dtype=self._f32, device=x.device) if lse is None else lse
-        rc = _lib.ps_xent_forward(C.byref(q), self._floats(loss, n, where, "loss"), self._floats(lse, n, where, "lse"),
-                                  _stream_ptr(stream))
-        if rc != PS_OK:
-            _check_op(rc, where)
-        return loss, lse
-
-    def backward(self, x, w, targets, lse, dx=None, dw=None, scale: float = 1.0, token_scale=None, stream=None):
-        """dx (bfloat16) and dw (bfloat16 or float32), either of them None: the gradients of
-        sum(scale * token_scale * loss), written to the tensors given."""
-        where = "ps_xent_backward"
-        n, q = self._args(x, w, targets, where)
-        lddx = 0 if dx is None else self._matrix(dx, n, (self._bf16,), where, "dx")
-        lddw = 0 if dw is None else self._matrix(dw, self.vocab, (self._bf16, self._f32), where, "dw")
-        rc = _lib.ps_xent_backward(C.byref(q), self._floats(lse, n, where, "lse"), scale,
-                                   self._floats(token_scale, n, where, "token_scale"), _ptr(dx), lddx, _ptr(dw),
-                                   PS_F32 if dw is not None and dw.dtype == self._f32 else PS_BF16, lddw, _stream_ptr(stream))
-        if rc != PS_OK:
-            _check_op(rc, where)
-        return dx, dw
 
 
 def ps_mx_status() -> int:

@@ -1,7 +1,8 @@
 /* Python face of the calls whose cost is the call: quantisation, its inverse and
- * the product of 4-bit operands, which for a single token run 2 to 5 us on the GPU.
- * Through ctypes such a call costs the host 4.1 us, half of it marshalling; here
- * about 2.7, the rest being the launch. Argument marshalling only, like the ctypes
+ * the product of 4-bit operands, which for a single token run 2 to 5 us on the GPU,
+ * and the loss over a vocabulary with its gradients. Through ctypes a quantisation
+ * costs the host 4.1 us, half of it marshalling; here about 2.7, the rest being the
+ * launch (loss and gradients: 22 us, here 15). Argument marshalling only, like the ctypes
  * binding beside it: every argument is checked here or by the library. Where the
  * buffers lie is checked here, because only here it is known: the library launches
  * on the current device and takes addresses at their word. */
@@ -21,8 +22,8 @@ static PyTypeObject OperandType;
 /* (of the CUDA runtime that the library is linked to; through torch the lookup takes a quarter of a microsecond) */
 extern int cudaGetDevice(int* device);
 
-static PyObject *g_f32, *g_bf16, *g_fail;                      /* torch dtypes; what raises PsError */
-static PyObject *s_shape, *s_stride, *s_get_device, *s_data_ptr, *s_dtype, *s_cuda_stream;
+static PyObject *g_f32, *g_bf16, *g_i32, *g_i64, *g_fail;      /* torch dtypes; what raises PsError */
+static PyObject *s_shape, *s_stride, *s_get_device, *s_data_ptr, *s_dtype, *s_cuda_stream, *s_numel, *s_is_contiguous;
 
 static int operand_init(PyObject* self, PyObject* args, PyObject* kw) {
   static char* names[] = {"codes", "scales", "rows", "cols", "device", NULL};
@@ -81,7 +82,7 @@ static PyObject* fail(int status, const char* where, const char* detail) {
 typedef struct {
   void* ptr;
   int dtype, device;
-  long long rows, cols, ld;
+  long long rows, cols, ld, stride;                            /* stride: the tensor's own, also where there is one row */
 } Matrix;
 
 /* A 2-d CUDA tensor with contiguous rows.  0, or -1 with an exception set. */
@@ -113,6 +114,7 @@ static int matrix(PyObject* t, Matrix* m, const char* where) {
     goto out;
   }
   m->ld = m->rows > 1 ? s0 : m->cols;
+  m->stride = s0;
   if (dtype == g_f32) {
     m->dtype = PS_F32;
   } else if (dtype == g_bf16) {
@@ -264,6 +266,172 @@ static PyObject* py_matmul(PyObject* self, PyObject* const* args, Py_ssize_t n, 
   return v[2];
 }
 
+/* ---- the loss over a vocabulary: sizes, workspace and device of a CrossEntropy, which derives from it ---- */
+typedef struct {
+  PyObject_HEAD
+  long long tokens, vocab, dim;
+  void* workspace;
+  size_t bytes;
+  int device;
+} Loss;
+
+static int loss_init(PyObject* self, PyObject* args, PyObject* kw) {
+  static char* names[] = {"tokens", "vocab", "dim", "workspace", "bytes", "device", NULL};
+  unsigned long long workspace, bytes;
+  Loss* l = (Loss*)self;
+  if (!PyArg_ParseTupleAndKeywords(args, kw, "LLLKKi", names, &l->tokens, &l->vocab, &l->dim, &workspace, &bytes, &l->device))
+    return -1;
+  l->workspace = (void*)(size_t)workspace;
+  l->bytes = (size_t)bytes;
+  return 0;
+}
+
+/* A tensor of `rows` x dim with one of two types, on the loss's device; its rows' distance in m->ld. */
+static int loss_matrix(const Loss* l, PyObject* t, Matrix* m, long long rows, int f32_too, const char* where, const char* text) {
+  if (matrix(t, m, where)) return -1;
+  if (m->device != l->device || m->rows != rows || m->cols != l->dim || (m->dtype != PS_BF16 && !f32_too)) {
+    fail(PS_ERR_BAD_ARG, where, text);
+    return -1;
+  }
+  /* (of one row the tensor's own stride counts too: it may keep the alignment that dim alone has not) */
+  m->ld = rows > 1 || m->stride > l->dim ? m->stride : l->dim;
+  return 0;
+}
+
+/* n contiguous elements of dtype a or b (NULL: none) on the loss's device: the address, and which type. None: NULL. */
+static int loss_vector(const Loss* l, PyObject* t, long long n, PyObject* a, PyObject* b, void** out, int* second,
+                       const char* where, const char* text) {
+  PyObject *device = NULL, *count = NULL, *dense = NULL, *ptr = NULL, *dtype = NULL;
+  int ok = -1;
+  *out = NULL;
+  if (!t || t == Py_None) return 0;
+  device = PyObject_CallMethodNoArgs(t, s_get_device);
+  count = device ? PyObject_CallMethodNoArgs(t, s_numel) : NULL;
+  dense = count ? PyObject_CallMethodNoArgs(t, s_is_contiguous) : NULL;
+  ptr = dense ? PyObject_CallMethodNoArgs(t, s_data_ptr) : NULL;
+  dtype = ptr ? PyObject_GetAttr(t, s_dtype) : NULL;
+  if (!dtype) goto out;
+  const long on = PyLong_AsLong(device);
+  const long long have = PyLong_AsLongLong(count);
+  *out = PyLong_AsVoidPtr(ptr);
+  if (PyErr_Occurred()) goto out;
+  if (on != l->device || have != n || dense != Py_True || (dtype != a && (!b || dtype != b))) {
+    fail(PS_ERR_BAD_ARG, where, text);
+    goto out;
+  }
+  if (second) *second = dtype == b;
+  ok = 0;
+out:
+  Py_XDECREF(device);
+  Py_XDECREF(count);
+  Py_XDECREF(dense);
+  Py_XDECREF(ptr);
+  Py_XDECREF(dtype);
+  return ok;
+}
+
+/* What both calls are given: x, w, targets. */
+static int loss_inputs(const Loss* l, PyObject* const* a, ps_xent* q, const char* where) {
+  Matrix x, w;
+  void* targets;
+  int wide = 0, current = -1;
+  if (cudaGetDevice(&current) || current != l->device) {
+    fail(PS_ERR_BAD_ARG, where, "the tensors' device is not the current one");
+    return -1;
+  }
+  if (matrix(a[0], &x, where)) return -1;
+  if (x.rows > l->tokens) {
+    fail(PS_ERR_BAD_ARG, where, "more tokens than this object was made for");
+    return -1;
+  }
+  if (loss_matrix(l, a[0], &x, x.rows, 0, where, "x: tokens x dim bfloat16 are wanted, on this object's device") ||
+      loss_matrix(l, a[1], &w, l->vocab, 0, where, "w: vocab x dim bfloat16 are wanted, on this object's device"))
+    return -1;
+  if (a[2] == Py_None) {
+    fail(PS_ERR_BAD_ARG, where, "targets are wanted");
+    return -1;
+  }
+  if (loss_vector(l, a[2], x.rows, g_i32, g_i64, &targets, &wide, where,
+                  "targets: one contiguous int32 or int64 per token is wanted, on this object's device"))
+    return -1;
+  q->x = x.ptr;
+  q->ldx = x.ld;
+  q->w = w.ptr;
+  q->ldw = w.ld;
+  q->targets = targets;
+  q->target_bits = wide ? 64 : 32;
+  q->tokens = x.rows;
+  q->vocab = l->vocab;
+  q->dim = l->dim;
+  q->workspace = l->workspace;
+  q->workspace_bytes = l->bytes;
+  return 0;
+}
+
+static PyObject* loss_forward(PyObject* self, PyObject* const* args, Py_ssize_t n, PyObject* kwnames) {
+  static const char* const names[] = {"x", "w", "targets", "loss", "lse", "stream"};
+  static const char where[] = "ps_xent_forward", text[] = "loss, lse: one contiguous float32 per token is wanted, on this object's device";
+  const Loss* l = (const Loss*)self;
+  PyObject* a[6];
+  ps_xent q;
+  void *stream, *loss, *lse;
+  int rc;
+  if (arguments(where, args, n, kwnames, names, 6, 3, a) || loss_inputs(l, a, &q, where) ||
+      loss_vector(l, a[3], q.tokens, g_f32, NULL, &loss, NULL, where, text) ||
+      loss_vector(l, a[4], q.tokens, g_f32, NULL, &lse, NULL, where, text) || stream_of(a[5], &stream))
+    return NULL;
+  Py_BEGIN_ALLOW_THREADS
+  rc = ps_xent_forward(&q, (float*)loss, (float*)lse, stream);
+  Py_END_ALLOW_THREADS
+  if (rc) return fail(rc, where, NULL);
+  Py_RETURN_NONE;
+}
+
+static PyObject* loss_backward(PyObject* self, PyObject* const* args, Py_ssize_t n, PyObject* kwnames) {
+  static const char* const names[] = {"x", "w", "targets", "lse", "dx", "dw", "scale", "token_scale", "stream"};
+  static const char where[] = "ps_xent_backward";
+  const Loss* l = (const Loss*)self;
+  PyObject* a[9];
+  Matrix dx = {0}, dw = {0};
+  ps_xent q;
+  void *stream, *lse, *weights;
+  double scale = 1.0;
+  int rc;
+  if (arguments(where, args, n, kwnames, names, 9, 4, a) || loss_inputs(l, a, &q, where) ||
+      loss_vector(l, a[3], q.tokens, g_f32, NULL, &lse, NULL, where, "lse: one contiguous float32 per token is wanted, on this object's device") ||
+      loss_vector(l, a[7], q.tokens, g_f32, NULL, &weights, NULL, where,
+                  "token_scale: one contiguous float32 per token is wanted, on this object's device") ||
+      stream_of(a[8], &stream))
+    return NULL;
+  if (a[6] && (scale = PyFloat_AsDouble(a[6])) == -1.0 && PyErr_Occurred()) return NULL;
+  if (a[4] && a[4] != Py_None && loss_matrix(l, a[4], &dx, q.tokens, 0, where, "dx: tokens x dim bfloat16 are wanted, on this object's device"))
+    return NULL;
+  if (a[5] && a[5] != Py_None &&
+      loss_matrix(l, a[5], &dw, l->vocab, 1, where, "dw: vocab x dim bfloat16 or float32 are wanted, on this object's device"))
+    return NULL;
+  Py_BEGIN_ALLOW_THREADS
+  rc = ps_xent_backward(&q, (const float*)lse, (float)scale, (const float*)weights, dx.ptr, dx.ld, dw.ptr,
+                        dw.ptr ? dw.dtype : PS_BF16, dw.ld, stream);
+  Py_END_ALLOW_THREADS
+  if (rc) return fail(rc, where, NULL);
+  Py_RETURN_NONE;
+}
+
+static PyMethodDef loss_methods[] = {
+    {"_forward", (PyCFunction)(void (*)(void))loss_forward, METH_FASTCALL | METH_KEYWORDS, "losses into the tensors given"},
+    {"_backward", (PyCFunction)(void (*)(void))loss_backward, METH_FASTCALL | METH_KEYWORDS, "gradients into the tensors given"},
+    {NULL, NULL, 0, NULL}};
+
+static PyTypeObject LossType = {
+    PyVarObject_HEAD_INIT(NULL, 0).tp_name = "paper_2204_03211_b200._ops.Loss",
+    .tp_basicsize = sizeof(Loss),
+    .tp_flags = Py_TPFLAGS_DEFAULT | Py_TPFLAGS_BASETYPE,
+    .tp_doc = "Sizes, workspace and device of a CrossEntropy.",
+    .tp_new = PyType_GenericNew,
+    .tp_init = loss_init,
+    .tp_methods = loss_methods,
+};
+
 /* setup(float32, bfloat16, raiser): the objects that the calls compare with and report through. */
 static PyObject* py_setup(PyObject* self, PyObject* const* args, Py_ssize_t n) {
   (void)self;
@@ -277,6 +445,18 @@ static PyObject* py_setup(PyObject* self, PyObject* const* args, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
+/* setup_targets(int32, int64): the types that targets may have. */
+static PyObject* py_setup_targets(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+  (void)self;
+  if (n != 2) {
+    PyErr_SetString(PyExc_TypeError, "setup_targets(int32, int64)");
+    return NULL;
+  }
+  Py_XSETREF(g_i32, Py_NewRef(args[0]));
+  Py_XSETREF(g_i64, Py_NewRef(args[1]));
+  Py_RETURN_NONE;
+}
+
 static PyMethodDef methods[] = {
     {"ps_mx_quantize", (PyCFunction)(void (*)(void))py_quantize, METH_FASTCALL | METH_KEYWORDS,
      "ps_mx_quantize(x, q=None, qt=None, stream=None)\n\nQuantises the device matrix x (float32 or bfloat16, any row stride)\n"
@@ -287,21 +467,20 @@ static PyMethodDef methods[] = {
      "ps_mx_matmul(a, b, out, stream=None)\n\nout[m][n] = sum over k of a[m][k] * b[n][k]; returns out (float32 or\n"
      "bfloat16, any row stride)."},
     {"setup", (PyCFunction)(void (*)(void))py_setup, METH_FASTCALL, "setup(float32, bfloat16, raiser)"},
+    {"setup_targets", (PyCFunction)(void (*)(void))py_setup_targets, METH_FASTCALL, "setup_targets(int32, int64)"},
     {NULL, NULL, 0, NULL}};
 
-static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ops", "Calls on 4-bit operands.", -1, methods, NULL, NULL, NULL, NULL};
+static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ops", "Calls whose cost is the call.", -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__ops(void) {
-  static const char* const texts[] = {"shape", "stride", "get_device", "data_ptr", "dtype", "cuda_stream"};
-  PyObject** const slots[] = {&s_shape, &s_stride, &s_get_device, &s_data_ptr, &s_dtype, &s_cuda_stream};
-  for (int i = 0; i < 6; ++i)
+  static const char* const texts[] = {"shape", "stride", "get_device", "data_ptr", "dtype", "cuda_stream", "numel", "is_contiguous"};
+  PyObject** const slots[] = {&s_shape, &s_stride, &s_get_device, &s_data_ptr, &s_dtype, &s_cuda_stream, &s_numel, &s_is_contiguous};
+  for (int i = 0; i < 8; ++i)
     if (!(*slots[i] = PyUnicode_InternFromString(texts[i]))) return NULL;
-  if (PyType_Ready(&OperandType) < 0) return NULL;
+  if (PyType_Ready(&OperandType) < 0 || PyType_Ready(&LossType) < 0) return NULL;
   PyObject* m = PyModule_Create(&module);
   if (!m) return NULL;
-  Py_INCREF(&OperandType);
-  if (PyModule_AddObject(m, "Operand", (PyObject*)&OperandType) < 0) {
-    Py_DECREF(&OperandType);
+  if (PyModule_AddObjectRef(m, "Operand", (PyObject*)&OperandType) < 0 || PyModule_AddObjectRef(m, "Loss", (PyObject*)&LossType) < 0) {
     Py_DECREF(m);
     return NULL;
   }

@@ -35,6 +35,7 @@ constexpr int kTcMaxStages = 10;
 constexpr int kTcWarps = 8;                                 // epilogue warps
 
 constexpr int kTcMaxSlots = 4;
+constexpr int kTcSideThreads = 64;                          // of a CTA, for work beside the tiles
 
 struct TcControl {
   unsigned long long full[kTcMaxStages], empty[kTcMaxStages], acc_full[2], acc_empty[2];
@@ -376,7 +377,7 @@ ps_tc_kernel(const __grid_constant__ typename Op::Args args) {
       }
       __syncwarp();
     } else if constexpr (Op::kSide) {
-      Op::side(args, (int)blockIdx.x * 64 + (warp - 2) * 32 + lane, (int)gridDim.x * 64);
+      Op::side(args, (int)blockIdx.x * kTcSideThreads + (warp - 2) * 32 + lane, (int)gridDim.x * kTcSideThreads);
       __syncwarp();
     }
   } else {

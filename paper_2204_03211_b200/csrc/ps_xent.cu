@@ -48,8 +48,8 @@ size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 // ps_xent_sizes and the calls agree whatever device they run on.
 struct XePlan {
   long long nparts, pitch, piece, pieces;
-  int slices;                            // per piece
-  size_t parts, score, xm, d[2], sums, x, w, end, end_unaligned;
+  int slices, dw_slices;                 // of dx, per piece; of dw
+  size_t parts, score, xm, d[2], sums, dw_sums, x, w, end, end_unaligned;
 };
 
 // A piece of d: as many words as make 5 x 2^22 entries (40 MB), whole tiles, at least one.
@@ -57,6 +57,7 @@ constexpr long long kXePieceEntries = 5ll << 22;
 constexpr int kXePairs = 74;             // CTA pairs that the cuts are made for
 constexpr int kXeMaxSlices = 64, kXeMinStages = 16;
 constexpr long long kXeSliceRows = 1ll << 14;    // slices x tokens, where there is more than one slice
+constexpr long long kXeDwSliceRows = 1ll << 12;  // slices x words, the same for dw
 
 XePlan xent_plan(long long T, long long V, long long D) {
   XePlan p;
@@ -74,6 +75,10 @@ XePlan xent_plan(long long T, long long V, long long D) {
   const long long longest = std::max<long long>(kXeMinStages, total / kXePairs / 2);
   const long long most_slices = std::min<long long>(kXeMaxSlices, std::max(1ll, kXeSliceRows / std::max(1ll, T)));
   p.slices = (int)std::min(most_slices, std::max(1ll, ceil_div(nk, longest)));
+  // Few words: dw has few tiles, as long as there are tokens, which are shared out in the same way (6144 x 256 x 272, loss
+  // and gradients: 58 us with one slice, 41 with six)
+  const long long most_dw = std::min<long long>(kXeMaxSlices, std::max(1ll, kXeDwSliceRows / V));
+  p.dw_slices = p.pieces == 1 ? (int)std::min(most_dw, std::max(1ll, ceil_div(ceil_div(T, kXeK), longest))) : 1;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t here = at;
@@ -87,7 +92,8 @@ XePlan xent_plan(long long T, long long V, long long D) {
   const size_t forward = at;
   at = shared;
   for (int b = 0; b < 2; ++b) p.d[b] = take(b < p.pieces ? (size_t)T * (size_t)p.piece * 2 : 0);
-  p.sums = take(p.slices > 1 || p.pieces > 1 ? (size_t)p.slices * (size_t)T * (size_t)D * sizeof(float) : 0);
+  p.sums = take(p.slices > 1 || p.pieces > 1 ? (size_t)p.slices * (size_t)T * (size_t)p.pitch * sizeof(float) : 0);
+  p.dw_sums = take(p.dw_slices > 1 ? (size_t)p.dw_slices * (size_t)V * (size_t)p.pitch * sizeof(float) : 0);
   at = std::max(at, forward);
   p.end = at;
   p.x = take((size_t)T * (size_t)p.pitch * 2);
@@ -103,7 +109,9 @@ size_t xent_bytes(long long T, long long V, long long D, bool unaligned) {
   const size_t parts = round256(t * (size_t)ceil_div(V, 128) * sizeof(float2)) + round256(t * sizeof(float));
   const size_t piece = std::max(std::min(t * all, (size_t)kXePieceEntries), t * kXeTile);
   const size_t rows = std::max(t, std::min(t * kXeMaxSlices, (size_t)kXeSliceRows));
-  return std::max<size_t>(256, x + w + std::max(parts, 2 * round256(piece * 2) + round256(rows * (size_t)D * sizeof(float))));
+  const size_t dw_rows = 2 * V <= kXeDwSliceRows ? (size_t)std::min(V * kXeMaxSlices, kXeDwSliceRows) : 0;
+  return std::max<size_t>(256, x + w + std::max(parts, 2 * round256(piece * 2) + round256(rows * pitch * sizeof(float)) +
+                                                           round256(dw_rows * pitch * sizeof(float))));
 }
 
 bool make_map(EncodeTiled encode, CUtensorMap* m, const void* p, long long rows, long long cols, long long ld) {
@@ -124,6 +132,11 @@ struct XeCall {
   bool copy_x, copy_w;                   // rows that no tensor map can walk are copied first
   XeArgs args;
 };
+
+int row_alignment(const void* p, long long bytes) {
+  const uintptr_t bits = reinterpret_cast<uintptr_t>(p) | (uintptr_t)bytes;
+  return bits % 32 == 0 ? 32 : bits % 16 == 0 ? 16 : 1;
+}
 
 bool rows_aligned(const void* p, long long ld) { return !misaligned(p, 16) && ld % 8 == 0; }
 
@@ -150,11 +163,15 @@ XeCopy copy_of(const XeCall& c, const void* src, long long rows, long long ld, s
                 mask ? c.q->targets : nullptr, c.q->target_bits == 64 ? 1 : 0, rows_aligned(src, ld) ? 1 : 0, c.q->vocab, weights};
 }
 
-int copy_rows(const XeCall& c, const void* src, long long rows, long long ld, size_t to) {
-  const long long units = rows * (c.plan.pitch / 8);
+// Rows that no tensor map can walk, into the workspace.
+int copy_rows(const XeCall& c) {
+  const ps_xent* q = c.q;
+  XeCopy x = XeCopy(), w = XeCopy();
+  if (c.copy_x) x = copy_of(c, q->x, q->tokens, q->ldx, c.plan.x, false, nullptr);
+  if (c.copy_w) w = copy_of(c, q->w, q->vocab, q->ldw, c.plan.w, false, nullptr);
+  const long long units = std::max(x.rows, w.rows) * (c.plan.pitch / 8);
   const unsigned grid = (unsigned)std::min<long long>(ceil_div(units, kXeCopyThreads), (long long)c.dev.num_sms * 8);
-  return op_launch("cross entropy", ps_xent_copy_kernel, grid, kXeCopyThreads, 0, 1, c.stream,
-                   copy_of(c, src, rows, ld, to, false, nullptr));
+  return op_launch("cross entropy", ps_xent_copy_kernel, grid, kXeCopyThreads, 0, 1, c.stream, x, w);
 }
 
 // What both passes set up.
@@ -184,9 +201,12 @@ int begin(XeCall* c, void* stream, bool backward) {
     for (int b = 0; b < 2 && b < p.pieces; ++b) ok = ok && make_map(encode, &a.d[b], c->ws + p.d[b], a.T, p.piece, p.piece);
   }
   if (!ok) return op_cuda_error("tensor map", cudaErrorInvalidValue);
-  if (c->copy_x) rc = copy_rows(*c, q->x, q->tokens, q->ldx, p.x);
-  if (!rc && c->copy_w) rc = copy_rows(*c, q->w, q->vocab, q->ldw, p.w);
-  return rc;
+  return c->copy_x || c->copy_w ? copy_rows(*c) : PS_OK;
+}
+
+int add_slices(const XeCall& c, const XeSum& q) {
+  const unsigned grid = (unsigned)std::min<long long>(ceil_div(q.rows * (q.pitch / 4), kXeCopyThreads), (long long)c.dev.num_sms * 16);
+  return op_launch("cross entropy", ps_xent_slices_kernel, grid, kXeCopyThreads, 0, 1, c.stream, q);
 }
 
 // Launches the segments of c->args, the longest tiles first.
@@ -200,7 +220,10 @@ int launch_segments(XeCall* c) {
   }
   if (tiles > 0x3fffffffll) return PS_ERR_TOO_LARGE;
   a.tiles = (int)tiles;
-  const unsigned grid = 2u * (unsigned)std::min<long long>(tiles, c->dev.num_sms / 2);
+  // (pairs beyond the tiles only copy, four pieces per thread: x of 192 x 1256 for one word tile 72 us with one pair, 39
+  // with 59)
+  const long long copies = a.side.src ? ceil_div(a.side.rows * (a.side.pitch / 8), kTcSideThreads * 2 * 4) : 0;
+  const unsigned grid = 2u * (unsigned)std::min<long long>(std::max(tiles, copies), c->dev.num_sms / 2);
   return op_launch("cross entropy", ps_tc_kernel<XeOp>, grid, kTcThreads, TcCfg<XeOp>::kSmem, 1, c->stream, a);
 }
 
@@ -270,10 +293,13 @@ int ps_xent_backward(const ps_xent* q, const float* lse, float scale, const floa
   a.ld_dx = lddx;
   a.ld_dw = lddw;
   a.dw_f32 = dw_dtype == PS_F32;
-  a.dx_wide = !misaligned(dx, 32) && lddx * 2 % 32 == 0;
-  a.dw_wide = !misaligned(dw, 32) && lddw * (long long)es % 32 == 0;
+  a.dx_align = row_alignment(dx, lddx * 2);
+  a.dw_align = row_alignment(dw, lddw * (long long)es);
+  a.pitch = (int)p.pitch;
+  a.dw_sums = reinterpret_cast<float*>(c.ws + p.dw_sums);
   const int tm = (int)ceil_div(a.T, kXeTile), td = (int)ceil_div(a.D, kXeTile);
   int filled = 0;                        // slices of dx's sums that hold something
+  const int dw_slices = std::min<int>(p.dw_slices, (int)ceil_div(a.T, kXeK));
   for (long long k = 0; k <= p.pieces; ++k) {
     a.nseg = 0;
     a.side = XeCopy();
@@ -290,17 +316,17 @@ int ps_xent_backward(const ps_xent* q, const float* lse, float scale, const floa
         a.seg[a.nseg++] = XeSeg{kXeDx, 0, tm, td, (int)v0, nk, slices, buf, k == 1, k == p.pieces && p.slices == 1};
         filled = std::max(filled, slices);
       }
-      if (dw) a.seg[a.nseg++] = XeSeg{kXeDw, 0, (int)ceil_div(words, kXeTile), td, (int)v0, (int)ceil_div(a.T, kXeK), 1, buf, 0, 0};
+      if (dw) a.seg[a.nseg++] = XeSeg{kXeDw, 0, (int)ceil_div(words, kXeTile), td, (int)v0, (int)ceil_div(a.T, kXeK), dw_slices, buf, 0, 0};
     }
     rc = launch_segments(&c);
     if (rc) return rc;
   }
-  if (dx && p.slices > 1) {
-    const unsigned grid = (unsigned)std::min<long long>(a.T, (long long)c.dev.num_sms * 16);
-    const bool wide = a.D % 4 == 0 && !misaligned(dx, 8) && lddx % 4 == 0;
-    rc = op_launch("cross entropy", ps_xent_slices_kernel, grid, kXeCopyThreads, 0, 1, c.stream, (const float*)a.dx_sums, filled,
-                   a.T, a.D, a.targets, a.target64, a.V, a.weights, a.scale, a.dx, a.ld_dx, wide ? 1 : 0);
-  }
+  if (dx && p.slices > 1)
+    rc = add_slices(c, XeSum{a.dx_sums, filled, a.pitch, a.T, a.D, lddx, dx, 0, !misaligned(dx, 8) && a.D % 4 == 0 && lddx % 4 == 0, scale,
+                             a.targets, a.target64, a.V, token_scale});
+  if (!rc && dw && dw_slices > 1)
+    rc = add_slices(c, XeSum{a.dw_sums, dw_slices, a.pitch, a.V, a.D, lddw, dw, a.dw_f32,
+                             !misaligned(dw, 4 * es) && a.D % 4 == 0 && lddw % 4 == 0, scale, nullptr, 0, 0, nullptr});
   return rc;
 }
 

@@ -29,7 +29,7 @@ struct XeSeg {                           // a launch's tiles of one kind, tiles_
   int kind, first, tiles_m, tiles_n;
   int v0;                                // first word of the piece
   int nk;                                // stages along k, over all slices
-  int slices;                            // kXeDx: the piece's words are shared out; each slice has sums of its own
+  int slices;                            // kXeDx, kXeDw: the words or tokens are shared out; each slice has sums of its own
   int buf;                               // which of the two pieces of d
   int start;                             // kXeDx: 1: the sums start here (else they are added to what is there)
   int finish;                            // kXeDx: 1: store dx itself
@@ -54,6 +54,22 @@ __device__ __forceinline__ long long xe_target(const void* targets, int is64, lo
   return is64 ? static_cast<const long long*>(targets)[t] : (long long)static_cast<const int*>(targets)[t];
 }
 
+// Eight elements at p, which lie at least eight from their row's start and sixteen from its end: two aligned loads and a
+// shift by whole elements (element by element, w of 25600 x 1021 and both gradients for 128 tokens took 155 us, so 141).
+__device__ __forceinline__ uint4 xe_shifted(const unsigned short* p) {
+  const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+  const uint4* base = reinterpret_cast<const uint4*>(at & ~(uintptr_t)15);
+  const uint4 a = base[0], b = base[1];
+  unsigned int u[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+  for (int k = 0; k < 6; ++k) u[k] = at & 8 ? u[k + 2] : u[k];
+#pragma unroll
+  for (int k = 0; k < 5; ++k) u[k] = at & 4 ? u[k + 1] : u[k];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) u[k] = at & 2 ? __funnelshift_r(u[k], u[k + 1], 16) : u[k];
+  return make_uint4(u[0], u[1], u[2], u[3]);
+}
+
 // Pieces of eight elements first, first + stride, ...
 __device__ __forceinline__ void xe_copy(const XeCopy& c, long long first, long long stride) {
   const unsigned int per = (unsigned int)(c.pitch / 8);
@@ -71,6 +87,8 @@ __device__ __forceinline__ void xe_copy(const XeCopy& c, long long first, long l
       const unsigned short* p = c.src + (size_t)r * (size_t)c.ld + (size_t)col;
       if (c.wide && col + 8 <= c.cols) {
         q = *reinterpret_cast<const uint4*>(p);
+      } else if (col >= 8 && col + 16 <= c.cols) {
+        q = xe_shifted(p);
       } else {
         unsigned int u[8];
 #pragma unroll
@@ -107,11 +125,13 @@ struct XeArgs {
   float scale;
   __nv_bfloat16* d_out[2];               // T x piece
   int piece;
-  float* dx_sums;                        // slices x T x D
+  float* dx_sums;                        // slices x T x pitch
+  float* dw_sums;                        // slices x V x pitch, where there is more than one
+  int pitch;                             // D, rounded up to a multiple of eight
   __nv_bfloat16* dx;
   void* dw;
   long long ld_dx, ld_dw;
-  int dw_f32, dx_wide, dw_wide;          // wide: rows allow 256-bit stores
+  int dw_f32, dx_align, dw_align;        // align: bytes on whose multiples all rows start, at most 32
   XeCopy side;                           // done by warps that have nothing else to do: xm, needed from the next launch on
 };
 
@@ -130,29 +150,48 @@ __device__ __forceinline__ float xe_exp2(float x) {      // (an argument that is
   return r;
 }
 
-// 32 values of one row as bf16 or binary32, `live` of them inside the row.
-__device__ __forceinline__ void xe_store_bf16(__nv_bfloat16* o, const float* v, int live, bool wide) {
-  if (wide && live >= 32) {
-    unsigned int u[16];
+// A warp's 32 rows of 32 columns, a row per lane, as bf16 or binary32.  Rows from `rows` and columns from `cols` on are not
+// there.  What all rows allow: 32-byte stores, 16-byte stores, or single elements.  Those are stored along the rows, after
+// an exchange between the lanes: element by element down the columns every store touches 32 sectors (two tokens, 23680 x
+// 952, loss and gradients: 270 us, so 77).
+template <typename T>
+__device__ __forceinline__ void xe_store(T* first, long long ld, float (&v)[32], int lane, int rows, int cols, int align) {
+  static_assert(sizeof(T) == 2 || sizeof(T) == 4, "bf16 or binary32");
+  constexpr int kWords = 8 * sizeof(T);                   // of 32 bits
+  if (align >= 16 && cols >= 32) {
+    if (lane >= rows) return;
+    T* o = first + (size_t)lane * (size_t)ld;
+    unsigned int u[kWords];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) u[i] = mm_bf16x2(v[2 * i], v[2 * i + 1]);
-    store_sector(o, u);
-    store_sector(o + 16, u + 8);
-  } else {
+    for (int i = 0; i < kWords; ++i) u[i] = sizeof(T) == 4 ? __float_as_uint(v[i & 31]) : mm_bf16x2(v[(2 * i) & 31], v[(2 * i + 1) & 31]);
+    if (align >= 32)
+#pragma unroll
+      for (int i = 0; i < kWords; i += 8) store_sector(reinterpret_cast<unsigned int*>(o) + i, u + i);
+    else
+#pragma unroll
+      for (int i = 0; i < kWords; i += 4)
+        *reinterpret_cast<uint4*>(reinterpret_cast<unsigned int*>(o) + i) = make_uint4(u[i], u[i + 1], u[i + 2], u[i + 3]);
+    return;
+  }
+  // v[i] becomes what lane i holds for this lane's column
+#pragma unroll
+  for (int k = 16; k >= 1; k >>= 1) {
+    const bool upper = (lane & k) != 0;
 #pragma unroll
     for (int i = 0; i < 32; ++i)
-      if (i < live) o[i] = __float2bfloat16_rn(v[i]);
+      if ((i & k) == 0) {
+        const float got = __shfl_xor_sync(0xffffffffu, upper ? v[i] : v[i | k], k);
+        v[i] = upper ? got : v[i];
+        v[i | k] = upper ? v[i | k] : got;
+      }
   }
-}
-__device__ __forceinline__ void xe_store_f32(float* o, const float* v, int live, bool wide) {
-  if (wide && live >= 32) {
+  if (lane >= cols) return;
 #pragma unroll
-    for (int i = 0; i < 32; i += 8) store_sector(o + i, reinterpret_cast<const unsigned int*>(v) + i);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 32; ++i)
-      if (i < live) o[i] = v[i];
-  }
+  for (int i = 0; i < 32; ++i)
+    if (i < rows) {
+      if constexpr (sizeof(T) == 4) first[(size_t)i * (size_t)ld + lane] = v[i];
+      else first[(size_t)i * (size_t)ld + lane] = __float2bfloat16_rn(v[i]);
+    }
 }
 
 struct XeOp {
@@ -206,18 +245,20 @@ struct XeOp {
       t->a = &a.x;
       t->b = &a.w;
       t->b_row += s.v0;
-    } else if (s.kind == kXeDx) {        // tokens x width, over (a slice of) the piece's words
-      const int k0 = (int)((long long)s.nk * at.slice / s.slices), k1 = (int)((long long)s.nk * (at.slice + 1) / s.slices);
-      t->a = &a.d[s.buf];
+      return;
+    }
+    // over (a slice of) the piece's words, or the tokens
+    const int k0 = (int)((long long)s.nk * at.slice / s.slices), k1 = (int)((long long)s.nk * (at.slice + 1) / s.slices);
+    t->nk = k1 - k0;
+    t->a = &a.d[s.buf];
+    t->b_mn = 1;
+    t->a_k = t->b_k = k0 * kXeK;
+    if (s.kind == kXeDx) {               // tokens x width
       t->b = &a.w;
-      t->b_mn = 1;
-      t->a_k = k0 * kXeK;
-      t->b_k = s.v0 + k0 * kXeK;
-      t->nk = k1 - k0;
-    } else {                             // words x width, over the tokens
-      t->a = &a.d[s.buf];
+      t->b_k += s.v0;
+    } else {                             // words x width
       t->b = &a.xm;
-      t->a_mn = t->b_mn = 1;
+      t->a_mn = 1;
     }
   }
 
@@ -317,49 +358,59 @@ struct XeOp {
         for (int i = 0; i < 32; ++i)
           if (i >= live) v[i] = 0.f;
       }
-      xe_store_bf16(a.d_out[at.seg->buf] + (size_t)row * (size_t)a.piece + (size_t)v0, v, 32, true);
+      unsigned int u[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) u[i] = mm_bf16x2(v[2 * i], v[2 * i + 1]);
+      __nv_bfloat16* o = a.d_out[at.seg->buf] + (size_t)row * (size_t)a.piece + (size_t)v0;
+      store_sector(o, u);
+      store_sector(o + 16, u + 8);
     }
 
     __device__ __forceinline__ void dx(float (&v)[32], int c) {
-      const long long col = (long long)at.n * kXeTile + c;
-      const int live = (int)min(32ll, a.D - col);
-      if (row >= a.T || live <= 0) return;
-      float* sums = a.dx_sums + ((size_t)at.slice * (size_t)a.T + (size_t)row) * (size_t)a.D + (size_t)col;
-      const bool wide = (a.D & 7) == 0;
+      const long long col = (long long)at.n * kXeTile + c, row0 = row - w.lane;
+      const int rows = (int)min(32ll, a.T - row0), cols = (int)min(32ll, a.D - col);
+      if (rows <= 0 || cols <= 0) return;
+      // (sums lie in rows of whole groups of eight; past D they are sums of zeros)
+      float* sums = a.dx_sums + ((size_t)at.slice * (size_t)a.T + (size_t)row) * (size_t)a.pitch + (size_t)col;
+      const int live = w.lane < rows ? cols : 0;
       if (!at.seg->start) {
-        if (wide && live >= 32) {
 #pragma unroll
-          for (int i = 0; i < 32; i += 4) {
+        for (int i = 0; i < 32; i += 4)
+          if (i < live) {
             const float4 q = __ldcg(reinterpret_cast<const float4*>(sums + i));
             v[i] += q.x;
             v[i + 1] += q.y;
             v[i + 2] += q.z;
             v[i + 3] += q.w;
           }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 32; ++i)
-            if (i < live) v[i] += __ldcg(sums + i);
-        }
       }
       if (at.seg->finish) {
 #pragma unroll
         for (int i = 0; i < 32; ++i) v[i] *= g;
-        xe_store_bf16(a.dx + (size_t)row * (size_t)a.ld_dx + (size_t)col, v, live, a.dx_wide != 0);
+        xe_store(a.dx + (size_t)row0 * (size_t)a.ld_dx + (size_t)col, a.ld_dx, v, w.lane, rows, cols, a.dx_align);
       } else {
-        xe_store_f32(sums, v, live, wide);
+#pragma unroll
+        for (int i = 0; i < 32; i += 8)
+          if (i < live) store_sector(sums + i, reinterpret_cast<const unsigned int*>(v) + i);
       }
     }
 
     __device__ __forceinline__ void dw(float (&v)[32], int c) {
-      const long long col = (long long)at.n * kXeTile + c, out = at.seg->v0 + row;
-      const int live = (int)min(32ll, a.D - col);
-      if (out >= a.V || live <= 0) return;
+      const long long col = (long long)at.n * kXeTile + c, out = at.seg->v0 + row - w.lane;
+      const int rows = (int)min(32ll, a.V - out), cols = (int)min(32ll, a.D - col);
+      if (rows <= 0 || cols <= 0) return;
+      if (at.seg->slices > 1) {
+        float* sums = a.dw_sums + ((size_t)at.slice * (size_t)a.V + (size_t)out + w.lane) * (size_t)a.pitch + (size_t)col;
+#pragma unroll
+        for (int i = 0; i < 32; i += 8)
+          if (i < cols && w.lane < rows) store_sector(sums + i, reinterpret_cast<const unsigned int*>(v) + i);
+        return;
+      }
       const size_t o = (size_t)out * (size_t)a.ld_dw + (size_t)col;
 #pragma unroll
       for (int i = 0; i < 32; ++i) v[i] *= a.scale;
-      if (a.dw_f32) xe_store_f32(static_cast<float*>(a.dw) + o, v, live, a.dw_wide != 0);
-      else xe_store_bf16(static_cast<__nv_bfloat16*>(a.dw) + o, v, live, a.dw_wide != 0);
+      if (a.dw_f32) xe_store(static_cast<float*>(a.dw) + o, a.ld_dw, v, w.lane, rows, cols, a.dw_align);
+      else xe_store(static_cast<__nv_bfloat16*>(a.dw) + o, a.ld_dw, v, w.lane, rows, cols, a.dw_align);
     }
 
     __device__ __forceinline__ void end() {
@@ -415,42 +466,64 @@ ps_xent_join_kernel(const float2* __restrict__ parts, int nparts, const float* _
 
 constexpr int kXeCopyThreads = 256;
 __global__ void __launch_bounds__(kXeCopyThreads)
-ps_xent_copy_kernel(const __grid_constant__ XeCopy c) {
+ps_xent_copy_kernel(const __grid_constant__ XeCopy x, const __grid_constant__ XeCopy w) {
   mm_pdl();
-  xe_copy(c, (long long)blockIdx.x * kXeCopyThreads + threadIdx.x, (long long)gridDim.x * kXeCopyThreads);
+  const long long first = (long long)blockIdx.x * kXeCopyThreads + threadIdx.x, stride = (long long)gridDim.x * kXeCopyThreads;
+  if (x.src) xe_copy(x, first, stride);
+  if (w.src) xe_copy(w, first, stride);
 }
 
-// dx = sum over the slices, in order: a CTA per row, four columns per thread where rows allow it.
+// One gradient as the sum over its slices, in order: four columns of a row per thread.  dx's rows have factors of their
+// own (targets not NULL).
+struct XeSum {
+  const float* sums;                     // slices x rows x pitch
+  int slices, pitch;
+  long long rows, cols, ld;
+  void* out;
+  int f32, wide;                         // wide: rows allow stores of four
+  float scale;
+  const void* targets;
+  int target64;
+  long long V;
+  const float* weights;
+};
+
 __global__ void __launch_bounds__(kXeCopyThreads)
-ps_xent_slices_kernel(const float* __restrict__ sums, int slices, long long T, long long D, const void* __restrict__ targets,
-                      int target64, long long V, const float* __restrict__ weights, float scale, __nv_bfloat16* __restrict__ dx,
-                      long long ld, int wide) {
+ps_xent_slices_kernel(const __grid_constant__ XeSum q) {
   mm_pdl();
-  const size_t n = (size_t)T * (size_t)D;
-  for (long long r = blockIdx.x; r < T; r += gridDim.x) {
-    const float g = xe_factor(targets, target64, V, weights, scale, r);
-    const float* p = sums + (size_t)r * (size_t)D;
-    __nv_bfloat16* o = dx + (size_t)r * (size_t)ld;
-    if (wide) {
-      for (long long c = 4 * threadIdx.x; c < D; c += 4 * kXeCopyThreads) {
-        float4 v = *reinterpret_cast<const float4*>(p + c);
+  const unsigned int per = (unsigned int)q.pitch / 4;
+  const size_t n = (size_t)q.rows * (size_t)q.pitch;
+  const long long units = q.rows * per, stride = (long long)gridDim.x * kXeCopyThreads;
+  for (long long i = (long long)blockIdx.x * kXeCopyThreads + threadIdx.x; i < units; i += stride) {
+    const long long r = i / per, c = (i - r * per) * 4;
+    if (c >= q.cols) continue;
+    const float g = q.targets ? xe_factor(q.targets, q.target64, q.V, q.weights, q.scale, r) : q.scale;
+    const float* p = q.sums + (size_t)r * (size_t)q.pitch + (size_t)c;
+    float4 v = *reinterpret_cast<const float4*>(p);
 #pragma unroll 8
-        for (int k = 1; k < slices; ++k) {
-          const float4 q = *reinterpret_cast<const float4*>(p + (size_t)k * n + c);
-          v.x += q.x;
-          v.y += q.y;
-          v.z += q.z;
-          v.w += q.w;
-        }
-        *reinterpret_cast<uint2*>(o + c) = make_uint2(mm_bf16x2(v.x * g, v.y * g), mm_bf16x2(v.z * g, v.w * g));
-      }
+    for (int k = 1; k < q.slices; ++k) {
+      const float4 t = *reinterpret_cast<const float4*>(p + (size_t)k * n);
+      v.x += t.x;
+      v.y += t.y;
+      v.z += t.z;
+      v.w += t.w;
+    }
+    const float e[4] = {v.x * g, v.y * g, v.z * g, v.w * g};
+    const size_t o = (size_t)r * (size_t)q.ld + (size_t)c;
+    if (q.f32) {
+      float* out = static_cast<float*>(q.out) + o;
+      if (q.wide) *reinterpret_cast<float4*>(out) = make_float4(e[0], e[1], e[2], e[3]);
+      else
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (c + k < q.cols) out[k] = e[k];
     } else {
-      for (long long c = threadIdx.x; c < D; c += kXeCopyThreads) {
-        float v = p[c];
-#pragma unroll 8
-        for (int k = 1; k < slices; ++k) v += p[(size_t)k * n + c];
-        o[c] = __float2bfloat16_rn(v * g);
-      }
+      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(q.out) + o;
+      if (q.wide) *reinterpret_cast<uint2*>(out) = make_uint2(mm_bf16x2(e[0], e[1]), mm_bf16x2(e[2], e[3]));
+      else
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (c + k < q.cols) out[k] = __float2bfloat16_rn(e[k]);
     }
   }
 }

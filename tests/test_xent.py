@@ -116,6 +116,21 @@ def test_few_tokens_many_words_share_out_the_vocabulary():
 
 
 @gpu
+@pytest.mark.parametrize("T,V,D,kw", [(6000, 250, 72, {}), (3000, 100, 40, dict(dw_dtype=F32)), (2100, 300, 37, {}),
+                                      (2500, 64, 24, dict(made_for=9000, pad=3, token_scale=True)), (1100, 1, 8, {})])
+def test_many_tokens_few_words_share_out_the_tokens(T, V, D, kw):
+    run(T, V, D, **kw)
+
+
+@gpu
+@pytest.mark.parametrize("dw_dtype", [BF, F32])
+@pytest.mark.parametrize("D", [1, 8, 24, 33, 36, 40, 62, 264])
+def test_rows_of_results_on_any_boundary(D, dw_dtype):
+    """Results are stored 32 bytes, 16 bytes or an element at a time, the last along the rows."""
+    run(270, 300, D, dw_dtype=dw_dtype)
+
+
+@gpu
 def test_gradient_against_differences():
     """Directional derivatives of the 64-bit loss, by central differences in 64 bits."""
     T, V, D = 50, 300, 48
