@@ -760,7 +760,7 @@ int ps_clip_destroy(ps_clip* clip);
  * a matrix of zeros gives zeros.
  * No ps_service is involved.  A ps_ortho remembers a list of matrices, which does not change from
  * step to step, and holds a workspace of 8 bytes per element (and 4 or 8 for the square of each
- * matrix's smaller side).  The calls run on the device the list was made for and leave the calling
+ * matrix's smaller side) unless its runs are one launch.  The calls run on the device the list was made for and leave the calling
  * thread's current device as it was.
  * ------------------------------------------------------------------------- */
 typedef struct ps_ortho ps_ortho; /* opaque */
@@ -778,7 +778,9 @@ typedef struct {
 int ps_ortho_create(ps_ortho** out, int device, int n, const ps_matrix* srcs, int src_dtype, const ps_matrix* dsts,
                     int dst_dtype);
 
-/* Three launches on `stream`, the last one cooperative.  Runs of one ps_ortho must not overlap on
+/* One launch on `stream` where every matrix has at most 128 rows (or columns) and 4096 columns (or rows;
+ * above 2048 for up to 14 matrices) and no destination lies in another's source, else three, the last
+ * one cooperative.  Runs of one ps_ortho must not overlap on
  * the GPU: use one stream, or order the streams.  Errors: BAD_HANDLE, CUDA. */
 int ps_ortho_run(ps_ortho* o, void* stream);
 

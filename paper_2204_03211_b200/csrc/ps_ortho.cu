@@ -60,6 +60,8 @@ int ns_device(bool split, bool pair, int* room) {
       }
     cudaError_t e = cudaFuncSetAttribute(ps_ortho_small_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSoSmem);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(ps_ortho_small_kernel<2>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSoSmem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(ps_ortho_small_kernel<1>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(ps_ortho_small_kernel<2>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e != cudaSuccess) return op_cuda_error("preparing the orthogonalisation", e);
     n.ready = true;
   }
@@ -114,17 +116,35 @@ bool make_map(EncodeTiled encode, CUtensorMap* m, const void* p, long long rows,
                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Matrices whose products of one kind go out together: enough for this many tiles per pair, so that what a tile waits
-// for has long been done.
+// Matrices whose products of one kind go out together: as many as a workspace of 128 MB holds, which L2 keeps, or, where
+// that is fewer, as have this many tiles, so that what a tile waits for has long been done.  (One group of 200 of 192 x 192 instead of
+// four, to fp32: 644 and 347 us; half as many groups for 24 layers 1024 wide, 4.3 GB: 16.4 and 17.8 ms.)
 constexpr long long kNsGroupTiles = 2 * 74;
+constexpr int kNsGroupBytesLog = 27;
 
 // What a tile costs besides its products, in elements of k.
 constexpr long long kNsTileCost = 256;
 
-// Pairs of CTAs fetch half as much from L2 per product as single ones; single ones have four times as many tiles, and
-// their products are done in half the time.  Lists of more than this many 256 x 256 tiles take pairs.  Single | pairs,
-// bf16 results, us: 24 x 512 x 512 (96 tiles) 209 | 253, 36 x 512 x 2048 (576) 746 | 680, 24 x 1024 x 4096 (1536) 2779 | 2213.
-constexpr long long kNsPairsFrom = 200;
+// Pairs of CTAs (256 x 256 tiles) fetch half as much from L2 per product as single ones (128 x 128), which waste less where
+// sides are not multiples of 256, and share out what there is more evenly.  Pairs are taken where they compute at most
+// 1.2 times as much, every pair has a tile even of A, and there are more than 200 in all.  Single | pairs, us:
+//   to fp32  20 x 1024 x 1024 1385 | 1152, 200 x 192 x 192 350 | 306, 32 x 200 x 2571 525 | 606, 16 x 640 x 2560 983 | 1066
+//   to bf16  24 x 1024 x 4096 2779 | 2213, 24 x 512 x 512 209 | 253, 96 x 300 x 300 323 | 425
+constexpr long long kNsPairs = 74, kNsPairsFrom = 200;
+bool take_pairs(const std::vector<NsItem>& items) {
+  long long rows = 0, square = 0, all[2] = {0, 0};
+  for (const NsItem& it : items) {
+    if (empty(it)) continue;
+    const long long m = std::min(it.rows, it.cols), n = std::max(it.rows, it.cols);
+    rows += ceil_div(m, 256) * ceil_div(n, 256);
+    square += ceil_div(m, 256) * ceil_div(m, 256);
+    for (int p = 0; p < 2; ++p) {
+      const long long tm = ceil_div(m, 128 << p), tn = ceil_div(n, 128 << p);
+      all[p] += 2 * tm * tm + tm * tn;
+    }
+  }
+  return rows > kNsPairsFrom && square >= kNsPairs && 5 * 4 * all[1] <= 6 * all[0];
+}
 
 }  // namespace
 
@@ -160,10 +180,13 @@ static int small_ctas(const std::vector<NsItem>& items) {
       if (s->of != d.of && s->end > d.first) return 0;
   }
   // One CTA where it can hold a matrix.  Else 128 columns each rather than 256: what every CTA does for itself gets shorter,
-  // adding up A does not get longer (four of 128 x 512: 81 us on two CTAs each, 66 on four)
+  // adding up A does not get longer (four of 128 x 512: 81 us on two CTAs each, 66 on four).  Seven clusters of sixteen run
+  // at a time; for more than two turns the general form is as fast or faster (12 | 16 | 32 of 128 x 4096 to bf16: 155 | 232 |
+  // 389 us here, 191 | 218 | 341 there), and for 2048 columns clusters of eight (20 to fp32: 193 us, on sixteen 258).
   if (widest <= kSoCols) return 1;
+  if (widest > kSoCtas / 2 * kSoCols) return srcs.size() <= 14 ? kSoCtas : 0;
   int ctas = 2;
-  while (ctas < kSoCtas && ctas * (kSoCols / 2) < widest) ctas *= 2;
+  while (ctas < kSoCtas / 2 && ctas * (kSoCols / 2) < widest) ctas *= 2;
   return ctas;
 }
 
@@ -190,11 +213,7 @@ NsPlan::~NsPlan() {
 
 int NsPlan::build(const std::vector<NsItem>& items, bool split, void* workspace, int* status) {
   small_ = small_ctas(items);
-  // single CTAs with 128 x 128 where pairs would have few tiles
-  long long large = 0;
-  for (const NsItem& it : items)
-    if (!empty(it)) large += ceil_div(it.rows, 256) * ceil_div(it.cols, 256);
-  pair_ = large > kNsPairsFrom;
+  pair_ = take_pairs(items);
   const long long tile = pair_ ? 256 : 128;
   int room = 0;
   int rc = ns_device(split, pair_, &room);
@@ -286,7 +305,7 @@ int NsPlan::build(const std::vector<NsItem>& items, bool split, void* workspace,
     for (long long u = 0; u < l.units; ++u) units.push_back(make_int2((int)i, (int)u));
   }
   // the tiles: matrices dealt to groups, a group's products one kind after the other
-  const size_t groups = (size_t)std::max<long long>(1, std::min<long long>((long long)n, sym_tiles / kNsGroupTiles));
+  const size_t groups = std::max<size_t>(1, std::min({n, (size_t)(sym_tiles / kNsGroupTiles), at >> kNsGroupBytesLog}));
   for (size_t g = 0; !small_ && g < groups; ++g)
     for (int step = 0; step < kNsSteps; ++step)
       for (int product = 0; product < 3; ++product)

@@ -107,33 +107,28 @@ __device__ __forceinline__ void ns_split(float v, __half& hi, __half& lo) {
 }
 __device__ __forceinline__ float2 ns_widen(unsigned int u) { return __half22float2(*reinterpret_cast<const __half2*>(&u)); }
 
-// The last step's result, scaled, of this lane's row: along a row of dst, or down a column, where the warp's lanes are
-// neighbours.// (i: row, j: first column, `count` of them)
-__device__ __forceinline__ void ns_result(const NsMat& M, float (&v)[32], int i, int j, int count) {
+// The last step's result, scaled: a warp's rows i0 ... and columns j ..., `cols` of them, a row per lane.  Where dst's rows
+// allow it a lane stores along its row; else the warp's lanes store neighbours, down the columns of a dst that lies the
+// other way, or along the rows after an exchange.
+__device__ __forceinline__ void ns_result(const NsMat& M, float (&v)[32], int i0, int lane, int j, int cols) {
   constexpr float s = 1.f / kNsScaleX;
+  const bool update = M.out == kNsOutUpdate;
+  const float decay = M.decay, rate = M.step;
 #pragma unroll
   for (int k = 0; k < 32; ++k) v[k] *= s;
-  const long long step = M.flip ? M.ld_dst : 1;
-  const size_t at0 = M.flip ? (size_t)j * (size_t)M.ld_dst + (size_t)i : (size_t)i * (size_t)M.ld_dst + (size_t)j;
-  if (M.out == kNsOutBf16) {
-    __nv_bfloat16* p = static_cast<__nv_bfloat16*>(M.dst) + at0;
-    if (M.wide && count >= 32) {
+  if (M.wide && cols >= 32) {
+    if (i0 + lane >= M.m) return;
+    const size_t at = (size_t)(i0 + lane) * (size_t)M.ld_dst + (size_t)j;
+    if (M.out == kNsOutBf16) {
+      __nv_bfloat16* p = static_cast<__nv_bfloat16*>(M.dst) + at;
       unsigned int u[16];
 #pragma unroll
       for (int k = 0; k < 16; ++k) u[k] = mm_bf16x2(v[2 * k], v[2 * k + 1]);
       store_sector(p, u);
       store_sector(p + 16, u + 8);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 32; ++k)
-        if (k < count) p[k * step] = __float2bfloat16_rn(v[k]);
+      return;
     }
-    return;
-  }
-  float* p = static_cast<float*>(M.dst) + at0;
-  const bool update = M.out == kNsOutUpdate;
-  const float decay = M.decay, rate = M.step;
-  if (M.wide && count >= 32) {
+    float* p = static_cast<float*>(M.dst) + at;
     if (update) {
 #pragma unroll
       for (int k = 0; k < 32; k += 4) {
@@ -146,15 +141,35 @@ __device__ __forceinline__ void ns_result(const NsMat& M, float (&v)[32], int i,
     }
 #pragma unroll
     for (int k = 0; k < 32; k += 8) store_sector(p + k, reinterpret_cast<const unsigned int*>(v) + k);
-  } else if (update) {
-#pragma unroll
-    for (int k = 0; k < 32; ++k)
-      if (k < count) p[k * step] = p[k * step] * decay - rate * v[k];
-  } else {
-#pragma unroll
-    for (int k = 0; k < 32; ++k)
-      if (k < count) p[k * step] = v[k];
+    return;
   }
+  if (!M.flip) tc_exchange(v, lane);
+  const int rows = min(32, M.m - i0), count = M.flip ? cols : rows;
+  if (lane >= (M.flip ? rows : cols)) return;
+  const size_t ld = (size_t)M.ld_dst, at = (M.flip ? (size_t)j * ld + (size_t)i0 : (size_t)i0 * ld + (size_t)j) + (size_t)lane;
+  if (M.out == kNsOutBf16) {
+    __nv_bfloat16* p = static_cast<__nv_bfloat16*>(M.dst) + at;
+#pragma unroll
+    for (int k = 0; k < 32; ++k)
+      if (k < count) p[k * ld] = __float2bfloat16_rn(v[k]);
+    return;
+  }
+  float* p = static_cast<float*>(M.dst) + at;
+  if (update) {                          // (sixteen loads before the first store: a round of two layers 36 wide 102 us, so 64)
+#pragma unroll
+    for (int h = 0; h < 32; h += 16) {
+      float q[16];
+#pragma unroll
+      for (int k = 0; k < 16; ++k) q[k] = h + k < count ? p[(h + k) * ld] : 0.f;
+#pragma unroll
+      for (int k = 0; k < 16; ++k)
+        if (h + k < count) p[(h + k) * ld] = q[k] * decay - rate * v[h + k];
+    }
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 32; ++k)
+    if (k < count) p[k * ld] = v[k];
 }
 
 template <int PLANES, bool PAIR>
@@ -403,7 +418,7 @@ struct NsOp {
         return;
       }
       hand_over();
-      if (i < M.m) ns_result(M, v, i, j, min(32, M.n - j));
+      if (i - w.lane < M.m) ns_result(M, v, i - w.lane, w.lane, j, min(32, M.n - j));
     }
 
     __device__ __forceinline__ void end() {}

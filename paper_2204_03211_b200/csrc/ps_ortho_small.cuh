@@ -1,10 +1,10 @@
-// Orthogonalisation of small matrices (up to 128 by 2048): all five steps in shared memory.
+// Orthogonalisation of small matrices (up to 128 by 4096): all five steps in shared memory.
 //
 // In the general form (ps_ortho.cuh) a product of a small matrix is one tile, and what takes time is handing it from one
 // tile to the next through L2: 6 to 8 us, fifteen times.  Here a CTA keeps 128 rows by up to 256 columns of X (two
 // halves, 128 KB) and A or B (two halves, 64 KB) in shared memory, in the swizzled layout in which the tensor cores take
 // operands: X is an operand along its rows in X X^T and across them in B X, from the same bytes.  Wider matrices are cut
-// into columns over a cluster of 2, 4 or 8 CTAs; only A is a sum over all of them, which they add up through each
+// into columns over a cluster of 2 to 16 CTAs; only A is a sum over all of them, which they add up through each
 // other's shared memory, a share of the rows each, in rank order.  One launch does it all: norm, scaling, steps, result.
 //
 // Sixteen warps read the sums (row = lane, 32 columns at a time); thread 0 issues the products.  Arithmetic as in
@@ -20,7 +20,7 @@ namespace psb {
 
 constexpr int kSoThreads = 512;
 constexpr int kSoRows = 128, kSoCols = 256;              // of a CTA's part of X
-constexpr int kSoCtas = 8;
+constexpr int kSoCtas = 16;
 constexpr int kSoBlock = kSoRows * 128;                  // bytes of 128 rows by 64 columns of one plane
 constexpr int kSoX = 2 * (kSoCols / 64) * kSoBlock, kSoE = 4 * kSoBlock;
 
@@ -38,7 +38,7 @@ static_assert(sizeof(SoControl) <= 2048 && kSoSmem <= 227 * 1024, "does not fit"
 struct SoArgs {
   const NsMat* mats;
   int* status;
-  int ctas;                                              // of a cluster: 1, 2, 4 or 8
+  int ctas;                                              // of a cluster: 1, 2, 4, 8 or 16
 };
 
 // Byte offset of 16-byte piece `piece` (8 columns) of a row, in planes of 64-column blocks.
@@ -233,35 +233,44 @@ ps_ortho_small_kernel(const __grid_constant__ SoArgs args) {
   // The sum of the cluster's parts of A, in rank order, as E: a share of the rows per CTA, which hands them to all.  Whatever
   // the number of CTAs a thread reads eight pieces of four columns, all of them before it adds (one after the other: 4 of 128 x 512 to fp32 65.8 us, so 64.3).
   auto add_up = [&](auto number) {
-    constexpr int kCtas = decltype(number)::value, kUnits = 8 / kCtas, kRows = kSoRows / kCtas;
-    static_assert(kRows * 32 == kUnits * kSoThreads, "groups of four columns per thread");
+    constexpr int kCtas = decltype(number)::value, kUnits = kCtas < 8 ? 8 / kCtas : 1, kRows = kSoRows / kCtas;
+    const bool adds = kRows * 32 == kUnits * kSoThreads || tid < kRows * 32;      // (sixteen CTAs: half of the threads)
     constexpr float s = kNsScaleE / (kNsScaleX * kNsScaleX);
-    float4 q[kUnits][kCtas];
+    constexpr int kAtOnce = kCtas < 8 ? kCtas : 8;
+    float4 sum[kUnits] = {};
     mm_cluster_sync();                                   // all parts can be read
 #pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
-      const int e = tid + u * kSoThreads;
-      const unsigned int at = ea + so_float4(rank * kRows + e / 32, e & 31);
+    for (int k0 = 0; k0 < kCtas; k0 += kAtOnce) {
+      float4 q[kUnits][kAtOnce];
 #pragma unroll
-      for (int k = 0; k < kCtas; ++k)
-        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                     : "=f"(q[u][k].x), "=f"(q[u][k].y), "=f"(q[u][k].z), "=f"(q[u][k].w)
-                     : "r"(so_peer(at, k)));
-    }
+      for (int u = 0; u < kUnits; ++u) {
+        if (!adds) break;
+        const int e = tid + u * kSoThreads;
+        const unsigned int at = ea + so_float4(rank * kRows + e / 32, e & 31);
 #pragma unroll
-    for (int u = 0; u < kUnits; ++u)
-#pragma unroll
-      for (int k = 1; k < kCtas; ++k) {
-        q[u][0].x = __fadd_rn(q[u][0].x, q[u][k].x);
-        q[u][0].y = __fadd_rn(q[u][0].y, q[u][k].y);
-        q[u][0].z = __fadd_rn(q[u][0].z, q[u][k].z);
-        q[u][0].w = __fadd_rn(q[u][0].w, q[u][k].w);
+        for (int k = 0; k < kAtOnce; ++k)
+          asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                       : "=f"(q[u][k].x), "=f"(q[u][k].y), "=f"(q[u][k].z), "=f"(q[u][k].w)
+                       : "r"(so_peer(at, k0 + k)));
       }
+#pragma unroll
+      for (int u = 0; u < kUnits; ++u) {
+        if (!adds) break;
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+          sum[u].x = __fadd_rn(sum[u].x, q[u][k].x);
+          sum[u].y = __fadd_rn(sum[u].y, q[u][k].y);
+          sum[u].z = __fadd_rn(sum[u].z, q[u][k].z);
+          sum[u].w = __fadd_rn(sum[u].w, q[u][k].w);
+        }
+      }
+    }
     mm_cluster_sync();                                   // all parts have been read: their place is E's again
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
+      if (!adds) break;
       const int e = tid + u * kSoThreads, r = rank * kRows + e / 32, c = (e & 31) * 4;
-      float a[4] = {q[u][0].x * s, q[u][0].y * s, q[u][0].z * s, q[u][0].w * s};
+      float a[4] = {sum[u].x * s, sum[u].y * s, sum[u].z * s, sum[u].w * s};
       float diagonal = 0.f;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
@@ -336,7 +345,8 @@ ps_ortho_small_kernel(const __grid_constant__ SoArgs args) {
           *reinterpret_cast<float4*>(es + so_float4(row, part * 8 + k / 4)) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
         if (ctas == 2) add_up(std::integral_constant<int, 2>());
         else if (ctas == 4) add_up(std::integral_constant<int, 4>());
-        else add_up(std::integral_constant<int, 8>());
+        else if (ctas == 8) add_up(std::integral_constant<int, 8>());
+        else add_up(std::integral_constant<int, 16>());
       }
     }
     handed_over();
@@ -426,7 +436,7 @@ ps_ortho_small_kernel(const __grid_constant__ SoArgs args) {
           *reinterpret_cast<uint4*>(p) = h4[k];
           *reinterpret_cast<uint4*>(p + lo_at) = l4[k];
         }
-      if (last && row < m && c < cols) ns_result(M, v, row, c0 + c, min(32, cols - c));
+      if (last && c < cols) ns_result(M, v, row - lane, lane, c0 + c, min(32, cols - c));
     }
     asm volatile("fence.proxy.async;" ::: "memory");
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");

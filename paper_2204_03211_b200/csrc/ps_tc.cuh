@@ -166,6 +166,21 @@ __device__ __forceinline__ void tc_arrive(unsigned int bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
+// A warp's 32 x 32 values, a row per lane, become a column per lane: v[i] what lane i held for this lane's column.
+__device__ __forceinline__ void tc_exchange(float (&v)[32], int lane) {
+#pragma unroll
+  for (int k = 16; k >= 1; k >>= 1) {
+    const bool upper = (lane & k) != 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      if ((i & k) == 0) {
+        const float got = __shfl_xor_sync(0xffffffffu, upper ? v[i] : v[i | k], k);
+        v[i] = upper ? got : v[i];
+        v[i | k] = upper ? v[i | k] : got;
+      }
+  }
+}
+
 // What an epilogue warp knows of its place, and its walk over the slots.
 struct TcWarp {
   unsigned char* slots;                  // of the warp's half

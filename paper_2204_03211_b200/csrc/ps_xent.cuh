@@ -173,18 +173,7 @@ __device__ __forceinline__ void xe_store(T* first, long long ld, float (&v)[32],
         *reinterpret_cast<uint4*>(reinterpret_cast<unsigned int*>(o) + i) = make_uint4(u[i], u[i + 1], u[i + 2], u[i + 3]);
     return;
   }
-  // v[i] becomes what lane i holds for this lane's column
-#pragma unroll
-  for (int k = 16; k >= 1; k >>= 1) {
-    const bool upper = (lane & k) != 0;
-#pragma unroll
-    for (int i = 0; i < 32; ++i)
-      if ((i & k) == 0) {
-        const float got = __shfl_xor_sync(0xffffffffu, upper ? v[i] : v[i | k], k);
-        v[i] = upper ? got : v[i];
-        v[i | k] = upper ? v[i | k] : got;
-      }
-  }
+  tc_exchange(v, lane);
   if (lane >= cols) return;
 #pragma unroll
   for (int i = 0; i < 32; ++i)

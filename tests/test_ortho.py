@@ -114,6 +114,20 @@ def test_a_list_of_many_shapes(dst):
 
 
 @gpu
+@pytest.mark.parametrize("rows,cols,count", [(100, 4096, 3), (4095, 64, 2), (33, 2500, 14), (33, 2500, 15), (128, 4097, 1)])
+def test_rows_of_thousands(rows, cols, count):
+    """Up to 4096 columns one cluster of sixteen CTAs holds a matrix; longer lists, and wider ones, take the general form."""
+    xs = [matrix(rows, cols, "normal", k) for k in range(count)]
+    for dst in (F32, BF):
+        outs = [torch.full((rows, cols), 9.0, device="cuda", dtype=dst) for _ in xs]
+        o = B.Ortho(xs, outs)
+        o.run()
+        assert o.status() == 0
+        for x, out in ((xs[0], outs[0]), (xs[-1], outs[-1])):
+            check(x, out)
+
+
+@gpu
 def test_large_matrix_in_pairs():
     xs = [matrix(1024, 4096, "decaying", 3), matrix(4000, 1030, "normal", 4), matrix(2048, 2048, "normal", 5)] * 2
     for dst in (F32, BF):
