@@ -50,7 +50,7 @@ int ns_device(bool split, bool pair, int* room) {
         const NsKernel k = kernel_of(s, p);
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)k.ctas);
-        cfg.blockDim = dim3(kTcThreads);
+        cfg.blockDim = dim3(TcCfg<NsOp<1, false>>::kThreads);
         cfg.dynamicSmemBytes = (size_t)k.smem;
         int clusters = 0;
         cudaError_t e = cudaFuncSetAttribute(k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, k.smem);
@@ -397,7 +397,7 @@ int NsPlan::run(cudaStream_t stream, int* launches) const {
   a.begin = reinterpret_cast<const int*>(mem_ + begin_off_);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)grid_);
-  cfg.blockDim = dim3(kTcThreads);
+  cfg.blockDim = dim3(TcCfg<NsOp<1, false>>::kThreads);
   const NsKernel kernel = kernel_of(split_, pair_);
   cfg.dynamicSmemBytes = (size_t)kernel.smem;
   cfg.stream = stream;

@@ -175,6 +175,7 @@ __device__ __forceinline__ void ns_result(const NsMat& M, float (&v)[32], int i0
 template <int PLANES, bool PAIR>
 struct NsOp {
   static constexpr bool kPair = PAIR, kSide = false;
+  static constexpr int kWarps = 8;
   static constexpr int kPlanes = PLANES, kType = 0, kTile = PAIR ? 256 : 128, kColumns = kTile / 2;
   // Three products of a stage take three times as long as one, so they need short stages to have enough of them (long |
   // short: 24 x 1024 x 4096 to fp32 4.86 | 4.44 ms); a single one is slowed by 64-byte rows (to bf16 2.46 | 2.63 ms).

@@ -16,7 +16,8 @@
 // products, high x high, high x low and low x high, so what is fetched from L2 per product is 2/3 of one plane's.
 //   warp 0     one lane issues the copies (each CTA its half, counted on the leader's barrier)
 //   warp 1     leader: one lane issues the MMAs
-//   warps 4-11 read the accumulators, two warps per quarter of the lanes, half of the columns each
+//   warps 4-   (Op::kWarps: eight or sixteen) read the accumulators, two or four warps per quarter of the lanes, which
+//              share the columns
 //   warps 2-3  for operators whose epilogue reads and writes 16-bit tiles (Op::kSlots > 0): one lane per half of the
 //              columns fetches, and stores, 128 rows by 32 columns at a time through a ring of slots in shared memory.
 //              An epilogue that did its own copies spent four fifths of its time waiting for them.
@@ -30,9 +31,7 @@
 
 namespace psb {
 
-constexpr int kTcThreads = 384;
 constexpr int kTcMaxStages = 10;
-constexpr int kTcWarps = 8;                                 // epilogue warps
 
 constexpr int kTcMaxSlots = 4;
 constexpr int kTcSideThreads = 64;                          // of a CTA, for work beside the tiles
@@ -52,6 +51,7 @@ constexpr int kTcVector = 1024;                             // two vectors of 12
 
 template <typename Op>
 struct TcCfg {
+  static constexpr int kThreads = 128 + 32 * Op::kWarps;
   static constexpr int kOperand = 128 * Op::kK * 2;         // a CTA's 128 rows of one plane of one operand
   static constexpr int kStage = 2 * Op::kPlanes * kOperand;
   static constexpr int kStages = Op::kStages;
@@ -191,7 +191,7 @@ struct TcWarp {
 };
 
 // Op:
-//   kPair; kPlanes; kK; kStages; kType (0 fp16, 1 bf16); kSegment (0, or: after so many stages the sums are taken over into
+//   kPair; kWarps; kPlanes; kK; kStages; kType (0 fp16, 1 bf16); kSegment (0, or: after so many stages the sums are taken over into
 //   registers); kSlots; Args with `int* status`
 //   tiles(args, this CTA or pair, their number, first, end, stride); Item item(args, index), what the roles need to know of a tile, read one tile ahead; tile(args, item, TcTile*)
 //   Epilogue(args, item, TcWarp&, cursor): begin() before the sums are there, columns(32 sums of this lane's row, their
@@ -201,7 +201,7 @@ struct TcWarp {
 //   entries(args, item, rank, half), how many slots the half's columns pass through; load(args, item, rank, half, entry,
 //   slot, vectors, barrier), which arrives; store(args, item, rank, half, entry, slot); done(args, item, rank)
 template <typename Op>
-__global__ void __cluster_dims__(Op::kPair ? 2 : 1, 1, 1) __launch_bounds__(kTcThreads, 1)
+__global__ void __cluster_dims__(Op::kPair ? 2 : 1, 1, 1) __launch_bounds__(TcCfg<Op>::kThreads, 1)
 ps_tc_kernel(const __grid_constant__ typename Op::Args args) {
   using Cfg = TcCfg<Op>;
   // (no static shared memory beside it: the stages start where the swizzle needs them to, at a multiple of 1024)
@@ -210,7 +210,7 @@ ps_tc_kernel(const __grid_constant__ typename Op::Args args) {
   const unsigned int base = mm_smem(stages);
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   constexpr bool kPair = Op::kPair;
-  constexpr int kCtas = kPair ? 2 : 1, kTile = kCtas * 128, kColumns = kTile / 2;       // a tile's rows; a warp's columns
+  constexpr int kCtas = kPair ? 2 : 1, kTile = kCtas * 128, kColumns = kTile / (Op::kWarps / 4);       // a tile's rows; a warp's columns
   unsigned int rank = 0;
   if constexpr (kPair) asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
 
@@ -221,12 +221,12 @@ ps_tc_kernel(const __grid_constant__ typename Op::Args args) {
     }
     for (int b = 0; b < 2; ++b) {
       asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(mm_smem(&ctl.acc_full[b])) : "memory");
-      asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(mm_smem(&ctl.acc_empty[b])), "n"(kCtas * kTcWarps) : "memory");
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(mm_smem(&ctl.acc_empty[b])), "n"(kCtas * Op::kWarps) : "memory");
     }
     for (int h = 0; h < 2; ++h)
       for (int b = 0; b < Op::kSlots; ++b) {
         asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(mm_smem(&ctl.staged[h][b])) : "memory");
-        asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(mm_smem(&ctl.filled[h][b])), "n"(kTcWarps / 2) : "memory");
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(mm_smem(&ctl.filled[h][b])), "n"(Op::kWarps / 2) : "memory");
         asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(mm_smem(&ctl.freed[h][b])) : "memory");
       }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");

@@ -30,8 +30,8 @@ int xent_device(const OpDevice& d, int** status) {
   if (!x.ready) {
     void* p = nullptr;
     cudaError_t e = cudaGetSymbolAddress(&p, g_xent_status);
-    if (e == cudaSuccess)
-      e = cudaFuncSetAttribute(ps_tc_kernel<XeOp>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcCfg<XeOp>::kSmem);
+    for (const auto kernel : {ps_tc_kernel<XeOp<8>>, ps_tc_kernel<XeOp<16>>})
+      if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, TcCfg<XeOp<8>>::kSmem);
     if (e != cudaSuccess) return op_cuda_error("preparing the cross entropy", e);
     x.status = static_cast<int*>(p);
     x.ready = true;
@@ -61,7 +61,7 @@ constexpr long long kXeDwSliceRows = 1ll << 12;  // slices x words, the same for
 
 XePlan xent_plan(long long T, long long V, long long D) {
   XePlan p;
-  p.nparts = ceil_div(V, 128);
+  p.nparts = ceil_div(V, kXeTile / (xe_warps(D) / 4));
   p.pitch = ceil_div(D, 8) * 8;
   const long long all = ceil_div(V, kXeTile) * kXeTile;
   // (equal pieces: a short last one would leave the launches around it half empty)
@@ -106,7 +106,7 @@ XePlan xent_plan(long long T, long long V, long long D) {
 size_t xent_bytes(long long T, long long V, long long D, bool unaligned) {
   const size_t pitch = (size_t)ceil_div(D, 8) * 8, all = (size_t)ceil_div(V, kXeTile) * kXeTile, t = (size_t)T;
   const size_t x = (unaligned ? 2 : 1) * round256(t * pitch * 2), w = unaligned ? round256((size_t)V * pitch * 2) : 0;
-  const size_t parts = round256(t * (size_t)ceil_div(V, 128) * sizeof(float2)) + round256(t * sizeof(float));
+  const size_t parts = round256(t * (size_t)ceil_div(V, 64) * sizeof(float2)) + round256(t * sizeof(float));
   const size_t piece = std::max(std::min(t * all, (size_t)kXePieceEntries), t * kXeTile);
   const size_t rows = std::max(t, std::min(t * kXeMaxSlices, (size_t)kXeSliceRows));
   const size_t dw_rows = 2 * V <= kXeDwSliceRows ? (size_t)std::min(V * kXeMaxSlices, kXeDwSliceRows) : 0;
@@ -224,7 +224,9 @@ int launch_segments(XeCall* c) {
   // with 59)
   const long long copies = a.side.src ? ceil_div(a.side.rows * (a.side.pitch / 8), kTcSideThreads * 2 * 4) : 0;
   const unsigned grid = 2u * (unsigned)std::min<long long>(std::max(tiles, copies), c->dev.num_sms / 2);
-  return op_launch("cross entropy", ps_tc_kernel<XeOp>, grid, kTcThreads, TcCfg<XeOp>::kSmem, 1, c->stream, a);
+  const bool many = xe_warps(a.D) == 16;
+  return op_launch("cross entropy", many ? ps_tc_kernel<XeOp<16>> : ps_tc_kernel<XeOp<8>>, grid,
+                   many ? TcCfg<XeOp<16>>::kThreads : TcCfg<XeOp<8>>::kThreads, TcCfg<XeOp<8>>::kSmem, 1, c->stream, a);
 }
 
 }  // namespace

@@ -3,7 +3,7 @@
 //     d_tv = g_t (exp(s_tv - lse_t) - [v = target(t)]),  dx = d w,  dw = d^T x
 //
 // All four products run in the frame of ps_tc.cuh.  The losses' pass keeps of every 256 x 256 tile of scores one
-// maximum and one sum of exponentials per row and 128 columns, which a small kernel joins.  The gradients' pass walks
+// maximum and one sum of exponentials per row and warp (128 or 64 columns), which a small kernel joins.  The gradients' pass walks
 // the vocabulary in pieces: the scores of a piece are computed again, turned into d (bf16) and stored; the next launch
 // reads them twice, along the rows for dx and down the columns for dw, and computes the following piece's d beside it,
 // so that what each launch ends with is covered by work that does not depend on it.  A piece of d takes about 32 MB
@@ -116,7 +116,7 @@ struct XeArgs {
   const void* targets;
   int target64;
   // losses' pass
-  float2* parts;                         // (maximum, sum of exp(s - maximum)) per row and 128 columns, rows of nparts
+  float2* parts;                         // (maximum, sum of exp(s - maximum)) per row and warp's columns, rows of nparts
   int nparts;
   float* score;                          // s_t,target(t)
   // gradients' pass
@@ -183,8 +183,17 @@ __device__ __forceinline__ void xe_store(T* first, long long ld, float (&v)[32],
     }
 }
 
+// Epilogue warps.  A tile's MMAs take 512 cycles per 64 elements of the width, the epilogue of a tile of scores 8800 with
+// eight warps, which mostly wait for one another's results; sixteen are done sooner, but get in the way of the MMAs where
+// those are what takes longest.  Eight | sixteen, us: losses of 4096 x 30000 x 128 120 | 100, losses and gradients of
+// 3968 x 7658 x 512 188 | 169, losses of 1000 x 30522 x 1024 47.2 | 49.6.
+constexpr long long kXeManyWarpsBelow = 768;
+inline int xe_warps(long long D) { return D < kXeManyWarpsBelow ? 16 : 8; }
+
+template <int WARPS>
 struct XeOp {
   static constexpr bool kPair = true;
+  static constexpr int kWarps = WARPS;
   static constexpr int kPlanes = 1, kType = 1, kK = kXeK, kStages = 6, kSlots = 0, kSegment = 0;
   static constexpr bool kSide = true;
   using Args = XeArgs;
@@ -404,7 +413,8 @@ struct XeOp {
 
     __device__ __forceinline__ void end() {
       if (at.seg->kind == kXeStats && row < a.T) {
-        const long long part = (long long)at.n * 2 + (w.col >> 7);
+        constexpr int kColumns = kXeTile / (WARPS / 4);
+        const long long part = (long long)at.n * (kXeTile / kColumns) + w.col / kColumns;
         if (part < a.nparts) a.parts[(size_t)row * (size_t)a.nparts + (size_t)part] = make_float2(m, s);
       }
     }
@@ -425,14 +435,19 @@ ps_xent_join_kernel(const float2* __restrict__ parts, int nparts, const float* _
   const float2* p = parts + (size_t)row * (size_t)nparts;
   float m = __int_as_float(0xff800000), s = 0.f;
   if (counts)
-    for (int i = lane; i < nparts; i += 32) {
-      const float2 q = p[i];
-      const float top = fmaxf(m, q.x);
-      if (top == __int_as_float(0xff800000)) {
-        s += q.y;                                         // (zeros, or NaN)
-      } else {
-        s = s * xe_exp2((m - top) * kLog2e) + q.y * xe_exp2((q.x - top) * kLog2e);
-        m = top;
+    for (int i = lane; i < nparts; i += 4 * 32) {
+      float2 q[4];                                        // (loads before what depends on them)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) q[k] = i + 32 * k < nparts ? p[i + 32 * k] : make_float2(__int_as_float(0xff800000), 0.f);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float top = fmaxf(m, q[k].x);
+        if (top == __int_as_float(0xff800000)) {
+          s += q[k].y;                                    // (zeros, or NaN)
+        } else {
+          s = s * xe_exp2((m - top) * kLog2e) + q[k].y * xe_exp2((q[k].x - top) * kLog2e);
+          m = top;
+        }
       }
     }
 #pragma unroll

@@ -131,6 +131,13 @@ def test_rows_of_results_on_any_boundary(D, dw_dtype):
 
 
 @gpu
+@pytest.mark.parametrize("T,V,D", [(70, 300, 767), (300, 700, 768), (33, 130, 1000), (600, 1, 1030)])
+def test_widths_around_the_change_of_warps(T, V, D):
+    """From 768 on eight warps read a tile's sums, below sixteen."""
+    run(T, V, D)
+
+
+@gpu
 def test_gradient_against_differences():
     """Directional derivatives of the 64-bit loss, by central differences in 64 bits."""
     T, V, D = 50, 300, 48
