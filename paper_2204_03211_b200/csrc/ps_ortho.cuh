@@ -10,6 +10,10 @@
 // there is no barrier over the grid, and one matrix's wait is another one's work.  A and B are symmetric: where the tiles
 // outnumber the CTAs only those on and below the diagonal are computed, and stored twice.
 //
+// Measured: 24 of 1024 x 4096 to bf16 1.85 ms cool (1 PFLOP/s, tensor cores 65 % busy; X in two halves, 400 MB, comes from
+// HBM for every product, 6.4 GB in all), 2.2 ms in a row under the power cap, to fp32 4.4 to 4.8 ms; 24 of 512 x 512 to bf16
+// 165 us and 3 of 777 x 300 to fp32 187 us, bound by the latency of fifteen products in a row.
+//
 // Arithmetic.  Operands are fp16 (11 bits) scaled by powers of two, sums are binary32.
 //  - The largest entries of A and B stand on their diagonals, and the last steps subtract them from a; they are
 //    kept apart in binary32 and enter in the epilogues (A A = E E + (d_i + d_j) E + d^2, and (a + f_i) X + F X), where E

@@ -7,6 +7,10 @@
 // into columns over a cluster of 2 to 16 CTAs; only A is a sum over all of them, which they add up through each
 // other's shared memory, a share of the rows each, in rank order.  One launch does it all: norm, scaling, steps, result.
 //
+// Measured to fp32 | bf16: 8 of 64 x 256 46 | 32 us (general form 120), 4 of 128 x 512 64 | 48, 4 of 128 x 2048 95 | 69,
+// 4 of 128 x 4096 106 | 78 (general form 290 | 154).  Bound by the chain: 7.7 us per step on one CTA, of which 1.6 are the
+// MMAs of X X^T and 2 the epilogue of X; over a cluster 4 us more for adding up A.
+//
 // Sixteen warps read the sums (row = lane, 32 columns at a time); thread 0 issues the products.  Arithmetic as in
 // ps_ortho.cuh, with the small products of a pair of halves first and the long sums of A in two parts, so that few of
 // the tensor cores' cut-off additions meet large sums.
