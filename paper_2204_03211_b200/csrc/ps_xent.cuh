@@ -10,8 +10,8 @@
 // 40 MB and so stays in L2 between its writing and its reading.
 //
 // Bound by the tensor cores, and in a row by power, where the width is 1024 and more: losses of 8192 x 30522 x 1024 in 318 us
-// (1.6 PFLOP/s), both gradients in 1317 us (three products of 2 T V D, 1.17 PFLOP/s); by the epilogues of the scores below
-// (2048 x 33278 x 512: 67 us and 200 us); by its launches where everything is small (37 x 500 x 64: 22 us for four).
+// (1.6 PFLOP/s), both gradients in 1317 us (three products of 2 T V D, 1.17 PFLOP/s); by the epilogues of the scores and
+// the ends of launches below (2048 x 33278 x 512: 67 us and 200 us); by its launches where everything is small (37 x 500 x 64: 21 us for four).
 //
 // Roundings: products of bf16 values are exact and summed in binary32; maxima, sums, lse and losses are binary32.  What is
 // stored of d is exp(s - lse) - [v = target], rounded to bf16 (it is an operand, and x and w are bf16, which one MMA wants
