@@ -180,7 +180,10 @@ int ps_register_block(ps_service* svc, int job, int block, size_t nelem, int ctx
  * ps_aggregate_clipped and ps_aggregate_block_noalloc (BAD_ARG).
  * The aggregates of PS_MUON blocks run on the caller's stream itself, also with
  * PS_OPT_OVERLAP, and are not held back; they are ordered after one another.  A list with
- * blocks of such jobs and of others goes out as two launches.  The first aggregate of a set of
+ * blocks of such jobs and of others goes out as two launches, the others' first, when everything that may fail for want
+ * of memory has been done for both.  Should CUDA refuse a later launch of the call after all (PS_ERR_CUDA), the blocks of
+ * those before it are aggregated and their pushes consumed; PS_MUON blocks whose sums went out and whose orthogonalisation
+ * did not have their new momentum and step, and their old parameters.  The first aggregate of a set of
  * blocks that are aggregated together makes its tables and, if it needs more than any before, the
  * workspace (about 12 bytes per element and 16 for the square of each matrix's smaller side), and
  * waits for the device; the tables of the last 64 sets are kept.  ps_block_profile covers the sum

@@ -595,8 +595,9 @@ int wait_slot(ps_service* s, Slot& sl) {
   return PS_OK;
 }
 
-int acquire_slot(ps_service* s, size_t table_bytes, size_t nchunks, Slot** out) {
-  Slot& sl = s->slots[s->next_slot];
+// ahead: not the next launch's slot but the one of a launch after it, whose memory is wanted before that one goes out.
+int acquire_slot(ps_service* s, size_t table_bytes, size_t nchunks, Slot** out, int ahead = 0) {
+  Slot& sl = s->slots[(s->next_slot + ahead) % kSlots];
   int rc = wait_slot(s, sl);
   if (rc) return rc;
   if (!sl.done) PS_CUDA(s, cudaEventCreateWithFlags(&sl.done, cudaEventDisableTiming));
@@ -709,6 +710,15 @@ void consume_pushes(ps_service* s, const std::vector<int>& idx, int slot, unsign
     b.last_slot = slot;
     b.last_slot_gen = gen;
   }
+}
+
+// A kernel that could not be launched: its table may still be on its way from the slot's host memory, which the next
+// launch may write.
+int launch_failed(ps_service* s, cudaError_t e) {
+  s->cuda_err = std::string("kernel launch: ") + cudaGetErrorString(e);
+  cudaGetLastError();
+  cudaStreamSynchronize(s->copy_stream);
+  return PS_ERR_CUDA;
 }
 
 // Launches one aggregation kernel with an optional programmatic-serialization attribute.
@@ -1016,6 +1026,7 @@ static int push_rows_locked(ps_service* s, int job, int block, int worker, const
 static void unpush_locked(ps_service* s, int n, const int* jobs, const int* blocks, const int* workers) {
   for (int i = 0; i < n; ++i) {
     Block& b = s->blocks[find_block(s, jobs[i], blocks[i])];
+    if (!b.pushed[workers[i]]) continue;   // (consumed by a launch that went out before another failed)
     b.pushed[workers[i]] = nullptr;
     b.npushed--;
   }
@@ -1240,11 +1251,7 @@ static int launch_plan(ps_service* s, const std::vector<int>& idx, Plan& plan, c
       le = launch_kernel(ps_aggregate_ldg_kernel, grid, kThreads, 0, run, false, sl->dev,
                          (const PsJobDev*)s->jobs_dev, s->stats_dev, sl->partials, done_word, seq);
   }
-  if (le != cudaSuccess) {
-    s->cuda_err = std::string("kernel launch: ") + cudaGetErrorString(le);
-    cudaGetLastError();
-    return PS_ERR_CUDA;
-  }
+  if (le != cudaSuccess) return launch_failed(s, le);
   sl->seq = seq;
   sl->gen = seq;                           // what a block remembers of its last launch (unique per launch)
   sl->signals = true;
@@ -1258,8 +1265,9 @@ static int launch_plan(ps_service* s, const std::vector<int>& idx, Plan& plan, c
   // small rounds took 0.32 to 0.49 ms from run to run, against a steady 0.40 ms with the
   // records.  Completion is still learnt from the kernels' completion words where the host
   // only needs to know, not to order streams.)
-  PS_CUDA(s, cudaEventRecord(sl->done, run));
-  sl->done_recorded = true;
+  // (launched is launched: should the record fail, the call says so, and the pushes are consumed)
+  const cudaError_t re = cudaEventRecord(sl->done, run);
+  sl->done_recorded = re == cudaSuccess;
   if (ws >= 0) {
     s->ws_last_slot[ws] = slot_index;
     s->ws_last_seq[ws] = seq;
@@ -1273,6 +1281,7 @@ static int launch_plan(ps_service* s, const std::vector<int>& idx, Plan& plan, c
   s->last_block = bulk ? kBulkThreads : kThreads;
   s->last_kernel = inl ? "inline" : bulk ? "bulk" : "ldg";
   consume_pushes(s, idx, slot_index, sl->gen);
+  PS_CUDA(s, re);
   return PS_OK;
 }
 
@@ -1515,6 +1524,8 @@ int launch_clip(ps_service* s, const std::vector<int>& idx, Plan& plan, const Cl
   if (s->clip_slot >= 0) {                 // the last clipped launch uses the same memory
     Slot& last = s->slots[s->clip_slot];
     if (last.seq == s->clip_seq && !slot_finished(s, last)) {
+      rc = ensure_done_event(s, last);
+      if (rc) return rc;
       PS_CUDA(s, cudaStreamWaitEvent(stream, last.done, 0));
       waited = 1u << (unsigned)s->clip_slot;
     }
@@ -1551,20 +1562,15 @@ int launch_clip(ps_service* s, const std::vector<int>& idx, Plan& plan, const Cl
                             s->stats_dev, sl->partials, s->clip_spool, s->clip_shared, call.norms_out, s->status_dev,
                             s->exit_ctrs + slot_index, done_word, seq);
   }
-  if (le != cudaSuccess) {
-    s->cuda_err = std::string("kernel launch: ") + cudaGetErrorString(le);
-    cudaGetLastError();
-    return PS_ERR_CUDA;
-  }
+  if (le != cudaSuccess) return launch_failed(s, le);
   sl->seq = seq;
   sl->gen = seq;
   sl->signals = true;
   sl->stream = stream;
   sl->work_stream = -1;
   sl->inflight = true;
-  sl->done_recorded = false;
-  PS_CUDA(s, cudaEventRecord(sl->done, stream));
-  sl->done_recorded = true;
+  const cudaError_t re = cudaEventRecord(sl->done, stream);
+  sl->done_recorded = re == cudaSuccess;
   s->clip_slot = slot_index;
   s->clip_seq = seq;
   s->next_slot = (s->next_slot + 1) % kSlots;
@@ -1575,6 +1581,7 @@ int launch_clip(ps_service* s, const std::vector<int>& idx, Plan& plan, const Cl
   s->last_block = kThreads;
   s->last_kernel = inl ? "clip_inline" : "clip";
   consume_pushes(s, idx, slot_index, sl->gen);
+  PS_CUDA(s, re);
   return PS_OK;
 }
 
@@ -1655,47 +1662,46 @@ int muon_set(ps_service* s, const Plan& plan, MuonSet** out) {
   return PS_OK;
 }
 
-// Launches the aggregate of the PS_MUON blocks `idx` (table `plan`, tables `set`) on `stream` itself (device current).
-int launch_muon(ps_service* s, const std::vector<int>& idx, Plan& plan, const MuonSet& set, cudaStream_t stream) {
+// Everything that the aggregate of the PS_MUON blocks `idx` (table `plan`, tables `set`) on `stream` waits for (device
+// current).
+int order_muon(ps_service* s, const std::vector<int>& idx, Plan& plan, const MuonSet& set, cudaStream_t stream) {
   ++s->call_id;
   unsigned char* base = plan.bytes.data();
   PsTaskDev* tasks = reinterpret_cast<PsTaskDev*>(base + reinterpret_cast<PsTableHdr*>(base)->tasks_off);
   for (size_t i = 0; i < plan.order.size(); ++i) tasks[i].p = reinterpret_cast<float*>(s->muon_ws) + set.u_off[i];
-  Slot* sl = nullptr;
-  int rc = acquire_slot(s, plan.bytes.size(), (size_t)plan.total_chunks, &sl);
-  if (rc) return rc;
-  const int slot_index = (int)(sl - s->slots);
   unsigned int waited = 0;
   if (s->muon_slot >= 0) {                 // the last such aggregate uses the same workspace
     Slot& last = s->slots[s->muon_slot];
     if (last.seq == s->muon_seq && !slot_finished(s, last)) {
+      const int rc = ensure_done_event(s, last);
+      if (rc) return rc;
       PS_CUDA(s, cudaStreamWaitEvent(stream, last.done, 0));
       waited = 1u << (unsigned)s->muon_slot;
     }
   }
   for (int bi : idx) {
-    rc = order_after_block(s, s->blocks[bi], stream, &waited);
+    const int rc = order_after_block(s, s->blocks[bi], stream, &waited);
     if (rc) return rc;
   }
+  return PS_OK;
+}
+
+// Launches that aggregate with the slot that is now the next one (acquired before).
+int launch_muon(ps_service* s, const std::vector<int>& idx, const Plan& plan, const MuonSet& set, cudaStream_t stream) {
+  const int slot_index = s->next_slot;
+  Slot* sl = &s->slots[slot_index];
   const unsigned long long seq = s->launches + 1;
   std::memcpy(sl->host, plan.bytes.data(), plan.bytes.size());
-  PS_CUDA(s, cudaMemcpyAsync(sl->dev, sl->host, plan.bytes.size(), cudaMemcpyHostToDevice, s->copy_stream));
-  PS_CUDA(s, cudaEventRecord(sl->copied, s->copy_stream));
-  PS_CUDA(s, cudaStreamWaitEvent(stream, sl->copied, 0));
+  cudaError_t ce = cudaMemcpyAsync(sl->dev, sl->host, plan.bytes.size(), cudaMemcpyHostToDevice, s->copy_stream);
+  if (ce == cudaSuccess) ce = cudaEventRecord(sl->copied, s->copy_stream);
+  if (ce == cudaSuccess) ce = cudaStreamWaitEvent(stream, sl->copied, 0);
+  if (ce != cudaSuccess) return launch_failed(s, ce);
   const int grid = (int)std::min<unsigned long long>(plan.total_chunks, (unsigned long long)s->num_sms * 4u);
   const cudaError_t le = launch_kernel(ps_aggregate_muon_kernel, grid, kThreads, 0, stream, false, sl->dev,
                                        (const PsJobDev*)s->jobs_dev, s->stats_dev, sl->partials,
                                        reinterpret_cast<double*>(s->muon_ws + set.parts_off));
-  if (le != cudaSuccess) {
-    s->cuda_err = std::string("kernel launch: ") + cudaGetErrorString(le);
-    cudaGetLastError();
-    return PS_ERR_CUDA;
-  }
-  rc = set.plan.run(stream);
-  if (rc) {
-    s->cuda_err = ps_op_last_error();
-    return rc;
-  }
+  if (le != cudaSuccess) return launch_failed(s, le);
+  // From here on momentum moves: the pushes are consumed whatever becomes of the orthogonalisation's launches.
   sl->seq = seq;
   sl->gen = seq;
   sl->signals = false;                     // (finished when the orthogonalisation is: the event says so)
@@ -1703,8 +1709,6 @@ int launch_muon(ps_service* s, const std::vector<int>& idx, Plan& plan, const Mu
   sl->work_stream = -1;
   sl->inflight = true;
   sl->done_recorded = false;
-  PS_CUDA(s, cudaEventRecord(sl->done, stream));
-  sl->done_recorded = true;
   s->muon_slot = slot_index;
   s->muon_seq = seq;
   s->next_slot = (s->next_slot + 1) % kSlots;
@@ -1715,7 +1719,11 @@ int launch_muon(ps_service* s, const std::vector<int>& idx, Plan& plan, const Mu
   s->last_block = kThreads;
   s->last_kernel = "muon";
   consume_pushes(s, idx, slot_index, sl->gen);
-  return PS_OK;
+  const int rc = set.plan.run(stream);
+  ce = cudaEventRecord(sl->done, stream);
+  sl->done_recorded = ce == cudaSuccess;
+  if (rc || ce != cudaSuccess) s->cuda_err = rc ? ps_op_last_error() : cudaGetErrorString(ce);
+  return rc || ce != cudaSuccess ? PS_ERR_CUDA : PS_OK;
 }
 
 bool bad_clip(float max_norm, const float* norms_out) {
@@ -1763,8 +1771,13 @@ static int submit_muon(ps_service* s, const std::vector<int>& idx, cudaStream_t 
   Plan muon;
   MuonSet* set = nullptr;
   rc = build_plan(s, s->idx_muon, &muon);
-  if (!rc) rc = muon_set(s, muon, &set);   // what may fail for want of memory comes before the first launch
-  if (!rc && !s->idx_other.empty()) {
+  if (!rc) rc = muon_set(s, muon, &set);
+  // What may fail for want of memory, and all waiting, comes before the first launch.
+  const bool others = !s->idx_other.empty();
+  Slot* sl = nullptr;
+  if (!rc) rc = acquire_slot(s, muon.bytes.size(), (size_t)muon.total_chunks, &sl, others ? 1 : 0);
+  if (!rc) rc = order_muon(s, s->idx_muon, muon, *set, stream);
+  if (!rc && others) {
     rc = build_plan(s, s->idx_other, &s->plan);
     if (!rc) rc = launch_plan(s, s->idx_other, s->plan, stream, flags);
   }
@@ -2043,8 +2056,9 @@ static int round_run(ps_service* s, int round, const ClipCall* clip, void* strea
     rc = PS_ERR_NOMEM;
   }
   if (rc) {
-    for (size_t i = 0; i < done; ++i) {
+    for (size_t i = 0; i < done; ++i) {    // (a launch that went out before another failed has consumed its own)
       Block& b = s->blocks[r.push_bi[i]];
+      if (!b.pushed[r.workers[i]]) continue;
       b.pushed[r.workers[i]] = nullptr;
       b.npushed--;
     }

@@ -333,3 +333,98 @@ def test_sharded_service_registers_what_it_owns():
     assert sh.svc.arena_info(0)[0] == 2 * 256
     refused(B.PS_ERR_BAD_ARG, sh.register_block, j, 1, 32)
     sh.close()
+
+FAILURES = r"""
+import ctypes as C, sys
+import numpy as np
+sys.path.insert(0, sys.argv[1])
+from paper_2204_03211_b200 import binding as B
+B.load()
+fake = C.CDLL(sys.argv[2])
+fake.last_copy_from.restype = C.c_void_p
+SIDES = [int(n) for n in sys.argv[3].split(",")]
+i32 = lambda *a: np.array(a, np.int32)
+at = 1 << 20
+
+
+def world():
+    svc = B.Service(0, 1, 1 << 22)
+    svc.register_job(opt=B.PS_MUON, num_workers=2)
+    svc.register_job(opt=B.PS_SGD, num_workers=2)
+    for b, n in enumerate(SIDES):
+        svc.register_matrix(0, b, n, n)
+    svc.register_block(1, 0, 5000)
+    ready = [(0, b) for b in range(len(SIDES))] + [(1, 0)]
+    pushes = [(j, b, w) for j, b in ready for w in range(2)]
+    return svc, ready, [i32(*c) for c in zip(*pushes)], np.full(len(pushes), at, np.uint64)
+
+
+def steps(svc, ready):
+    return [svc.block_export(j, b)[1] for j, b in ready]
+
+
+def call(how, svc, ready, lists, ptrs):
+    if how == "aggregate":
+        svc.aggregate(ready)
+    elif how == "round":
+        svc.round(*lists, ptrs, ready)
+    else:
+        svc.round_run(svc.round_prepare(*lists, ptrs, ready))
+
+
+for how in ("aggregate", "round", "prepared"):
+    k, kinds = 0, set()
+    while True:
+        k += 1
+        svc, ready, lists, ptrs = world()
+        if how == "aggregate":
+            svc.push_batch(*lists, ptrs)
+        before = fake.launches_seen()
+        fake.fail_cuda(k)
+        status = B.PS_OK
+        try:
+            call(how, svc, ready, lists, ptrs)
+        except B.PsError as e:
+            status = e.status
+        failed = fake.calls_seen() >= k
+        fake.fail_cuda(0)
+        launched, table, done = fake.launches_seen() - before, fake.last_copy_from(), steps(svc, ready)
+        if not failed:
+            assert status == B.PS_OK and done == [1] * len(ready), (how, k, status, done)
+            break
+        assert status in (B.PS_ERR_NOMEM, B.PS_ERR_CUDA), (how, k, status)
+        kinds.add((status, launched))
+        # what went out has taken its pushes: the other job's launch is first, then the sums
+        assert done == [int(launched >= 2)] * len(SIDES) + [int(launched >= 1)], (how, k, launched, done)
+        if status == B.PS_ERR_NOMEM:
+            assert launched == 0, (how, k, launched)
+        # what did not is as it was, and everybody can go on
+        if how == "aggregate":
+            missing = [i for i, (j, b) in enumerate(zip(lists[0], lists[1])) if done[ready.index((j, b))]]
+            svc.push_batch(*[c[missing] for c in lists], ptrs[missing])
+        call(how, svc, ready, lists, ptrs)
+        assert steps(svc, ready) == [d + 1 for d in done], (how, k)
+        if launched >= 2:                       # the sums may still read their table
+            assert fake.last_copy_from() != table, (how, k)
+        svc.close()
+    assert {n for _, n in kinds} >= {0, 1, 2} and (B.PS_ERR_NOMEM, 0) in kinds and k > 10, (how, k, kinds)
+"""
+
+
+@pytest.mark.parametrize("sides", ["40,64", "40,200"])
+def test_what_fails_half_way_leaves_every_block_usable(tmp_path, sides):
+    """One list with blocks of two jobs, small matrices and larger ones; every call of the CUDA runtime that can fail does,
+    once.  Pushes are consumed by what was launched and by nothing else, and no launch's table is written again too early."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    B.load()
+    libs = []
+    for name in ("failing_cuda", "pretend_cuda"):
+        libs.append(str(tmp_path / (name + ".so")))
+        subprocess.run(["gcc", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-o", libs[-1],
+                        os.path.join(root, "tests", "c", name + ".c"), "-ldl"], check=True)
+    run = subprocess.run([sys.executable, "-c", FAILURES, root, libs[0], sides],
+                         env=dict(os.environ, LD_PRELOAD=":".join(libs)), capture_output=True, text=True)
+    assert run.returncode == 0, run.stderr
