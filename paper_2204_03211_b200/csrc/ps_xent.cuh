@@ -139,11 +139,14 @@ struct XeArgs {
   XeCopy side;                           // done by warps that have nothing else to do: xm, needed from the next launch on
 };
 
-// g_t; zero for an ignored token, whatever token_scale holds there.
-__device__ __forceinline__ float xe_factor(const void* targets, int is64, long long V, const float* weights, float scale, long long t) {
+// Whether token t has a target, and g_t if it has.  An ignored one's row of dx is zeros by choice and not as a product:
+// the sums of its zero entries with a row of w that holds an infinity are NaN.
+__device__ __forceinline__ bool xe_factor(const void* targets, int is64, long long V, const float* weights, float scale, long long t,
+                                          float* g) {
   const long long v = xe_target(targets, is64, t);
-  if (v < 0 || v >= V) return 0.f;
-  return weights ? scale * weights[t] : scale;
+  if (v < 0 || v >= V) return false;
+  *g = weights ? scale * weights[t] : scale;
+  return true;
 }
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -269,8 +272,8 @@ struct XeOp {
     const TcWarp& w;
     const At at;
     long long row, word;                 // this lane's row; the target (kXeStats, kXeProb: relative to the tile's first column)
-    float m, s, g;                       // g: kXeDx: the factor of the row's gradient
-    bool counts;                         // the row's token has a target
+    float m, s, g = 0.f;                 // g: kXeDx: the factor of the row's gradient
+    bool counts = false;                 // the row's token has a target
 
     __device__ __forceinline__ Epilogue(const XeArgs& args, int index, const TcWarp& warp, MmCursor<1>&)
         : a(args), w(warp), at(locate(args, index)) {}
@@ -278,8 +281,7 @@ struct XeOp {
     __device__ __forceinline__ void begin() {
       const int kind = at.seg->kind;
       row = (long long)at.m * kXeTile + w.row + w.lane;
-      g = a.scale;
-      if (kind == kXeDx && row < a.T) g = factor(a, row);
+      if (kind == kXeDx && row < a.T) counts = xe_factor(a.targets, a.target64, a.V, a.weights, a.scale, row, &g);
       if (kind <= kXeProb) {
         word = -1;
         m = __int_as_float(0xff800000);
@@ -292,10 +294,6 @@ struct XeOp {
           if (kind == kXeProb && counts) m = a.lse[row];
         }
       }
-    }
-
-    static __device__ __forceinline__ float factor(const XeArgs& a, long long row) {
-      return xe_factor(a.targets, a.target64, a.V, a.weights, a.scale, row);
     }
 
     __device__ __forceinline__ void columns(float (&v)[32], int c) {
@@ -388,7 +386,7 @@ struct XeOp {
       }
       if (at.seg->finish) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] *= g;
+        for (int i = 0; i < 32; ++i) v[i] = counts ? v[i] * g : 0.f;
         xe_store(a.dx + (size_t)row0 * (size_t)a.ld_dx + (size_t)col, a.ld_dx, v, w.lane, rows, cols, a.dx_align);
       } else {
 #pragma unroll
@@ -505,7 +503,8 @@ ps_xent_slices_kernel(const __grid_constant__ XeSum q) {
   for (long long i = (long long)blockIdx.x * kXeCopyThreads + threadIdx.x; i < units; i += stride) {
     const long long r = i / per, c = (i - r * per) * 4;
     if (c >= q.cols) continue;
-    const float g = q.targets ? xe_factor(q.targets, q.target64, q.V, q.weights, q.scale, r) : q.scale;
+    float g = q.scale;
+    const bool counts = !q.targets || xe_factor(q.targets, q.target64, q.V, q.weights, q.scale, r, &g);
     const float* p = q.sums + (size_t)r * (size_t)q.pitch + (size_t)c;
     float4 v = *reinterpret_cast<const float4*>(p);
 #pragma unroll 8
@@ -515,6 +514,10 @@ ps_xent_slices_kernel(const __grid_constant__ XeSum q) {
       v.y += t.y;
       v.z += t.z;
       v.w += t.w;
+    }
+    if (!counts) {
+      v = make_float4(0.f, 0.f, 0.f, 0.f);
+      g = 1.f;
     }
     const float e[4] = {v.x * g, v.y * g, v.z * g, v.w * g};
     const size_t o = (size_t)r * (size_t)q.ld + (size_t)c;

@@ -189,6 +189,25 @@ def test_what_ignored_rows_hold_does_not_matter():
 
 
 @gpu
+@pytest.mark.parametrize("T,V,D", [(200, 700, 64), (300, 700, 37), (40, 40000, 128), (40, 40000, 77), (5000, 7000, 64)])
+def test_what_w_holds_does_not_reach_ignored_rows(T, V, D):
+    """One slice, many, several pieces; results along the rows and not.  An infinity or a NaN in w makes NaNs of every
+    other token's gradient."""
+    x, w, t = inputs(T, V, D, ignored=0.3)
+    w[7, 0], w[V - 1, D - 1] = float("inf"), float("nan")
+    gone = t < 0
+    ce = B.CrossEntropy(T, V, D)
+    loss, lse = ce.forward(x, w, t)
+    ts = torch.where(gone, float("nan"), 0.5)
+    dx = torch.full((T, D), 7.0, device="cuda", dtype=BF)
+    ce.backward(x, w, t, lse, dx, None, scale=0.25, token_scale=ts)
+    assert gone.any() and not gone.all()
+    for z in (loss, lse, dx):
+        assert bool((z[gone] == 0).all())
+    assert dx[~gone].isnan().any(1).all()
+
+
+@gpu
 def test_nan_and_infinities_stay_in_their_rows():
     T, V, D = 70, 600, 64
     x, w, t = inputs(T, V, D, ignored=0.0)
