@@ -798,7 +798,10 @@ def _load_ops():
         """Losses and gradients of up to `tokens` tokens over a vocabulary (ps_xent_*), with the workspace they need.
         x is tokens x dim and w vocab x dim (bfloat16, any row stride), targets int32 or int64; all tensors on this
         object's device, which has to be the current one.  `aligned`: whether x's and w's rows start on 16-byte
-        boundaries (default: whether rows of dim elements do).  Calls of one object must not overlap on the GPU."""
+        boundaries (default: whether rows of dim elements do).  Calls of one object must not overlap on the GPU.  An
+        object may be dropped while its calls still run: torch's allocator is told of the streams they were given as
+        torch streams, and where one was given as a number, dropping the object waits for the device.  (A captured graph's
+        replays need the object to be kept.)"""
 
         def __new__(cls, tokens: int, vocab: int, dim: int, device=None, aligned: bool | None = None):
             return super().__new__(cls)
@@ -809,22 +812,65 @@ def _load_ops():
             self.workspace = torch.empty(sizes[0 if (dim % 8 == 0 if aligned is None else aligned) else 1],
                                          dtype=torch.uint8, device=device or "cuda")
             self.device = self.workspace.get_device()
+            # The workspace's memory follows the stream that is current now.  Another stream's first call waits for what
+            # that one has been given before, whose memory it may have been, and the allocator is told of that stream.
+            made_on = torch.cuda.current_stream(self.device)
+            self._streams, self._made, self._waits = {made_on.cuda_stream}, made_on.record_event(), False
+            self._last = made_on                                     # (the stream of the call before is not looked at again)
             super().__init__(tokens, vocab, dim, self.workspace.data_ptr(), self.workspace.numel(), self.device)
+
+        def _torch_stream(self, handle):
+            return torch.cuda.ExternalStream(handle, self.device) if handle else torch.cuda.default_stream(self.device)
+
+        def _uses(self, stream):
+            handle = _stream_ptr(stream)
+            if handle not in self._streams:
+                if not torch.cuda.is_current_stream_capturing():     # (a capture begins when all of that is done)
+                    self._torch_stream(handle).wait_event(self._made)
+                if handle == 0 or isinstance(stream, torch.cuda.Stream):
+                    self.workspace.record_stream(stream if handle else torch.cuda.default_stream(self.device))
+                else:
+                    self._waits = True                               # (that stream may be gone when the object is)
+                self._streams.add(handle)
+            self._last = stream
+
+        def _result(self, n, stream):
+            """n floats that a call on `stream` writes: memory in that stream's order, which the current stream, where the
+            caller goes on, may use as well."""
+            handle = _stream_ptr(stream)
+            current = torch.cuda.current_stream(self.device)
+            if current.cuda_stream == handle:
+                return torch.empty(n, dtype=torch.float32, device=self.workspace.device)
+            with torch.cuda.stream(self._torch_stream(handle)):
+                out = torch.empty(n, dtype=torch.float32, device=self.workspace.device)
+            out.record_stream(current)
+            return out
 
         def forward(self, x, w, targets, loss=None, lse=None, stream=None):
             """Returns (loss, lse): one float32 per token, in the tensors given or in new ones."""
+            if stream is not self._last:
+                self._uses(stream)
             if loss is None:
-                loss = torch.empty(len(x), dtype=torch.float32, device=x.device)
+                loss = self._result(len(x), stream)
             if lse is None:
-                lse = torch.empty(len(x), dtype=torch.float32, device=x.device)
+                lse = self._result(len(x), stream)
             self._forward(x, w, targets, loss, lse, stream)
             return loss, lse
 
         def backward(self, x, w, targets, lse, dx=None, dw=None, scale: float = 1.0, token_scale=None, stream=None):
             """dx (bfloat16) and dw (bfloat16 or float32), either of them None: the gradients of
             sum(scale * token_scale * loss), written to the tensors given."""
+            if stream is not self._last:
+                self._uses(stream)
             self._backward(x, w, targets, lse, dx, dw, scale, token_scale, stream)
             return dx, dw
+
+        def __del__(self):
+            try:
+                if self._waits:
+                    torch.cuda.synchronize(self.device)
+            except Exception:
+                pass
 
     MxTensor.__qualname__ = "MxTensor"
     CrossEntropy.__qualname__ = "CrossEntropy"

@@ -351,6 +351,158 @@ def test_on_another_stream_and_captured():
         assert torch.equal(a, b)
 
 
+def on_a_busy_stream(stream, call, fill, ms=200):
+    """`call` behind work that keeps `stream` busy; then the current stream writes over `fill` bytes of freed memory, many
+    times, in allocations of every size that could be served from what `call` released."""
+    for busy in (0, ms):                                    # (first without: a kernel's first launch may wait for the device)
+        with torch.cuda.stream(stream):
+            torch.cuda._sleep(int(busy * 1.9e6) + 1)
+        made = call()
+        held = []
+        for n in fill:
+            held += [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for _ in range(4)]
+        if busy == 0:
+            del held, made[:]
+            torch.cuda.synchronize()
+    torch.cuda.current_stream().synchronize()
+    assert not stream.query()                               # (it was busy all the while)
+    stream.synchronize()
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["torch", "number"])
+@pytest.mark.parametrize("T,V,D", [(300, 5000, 64), (300, 5000, 61)])
+def test_dropped_and_fresh_results_while_the_calls_wait(kind, T, V, D):
+    """An object dropped right after its calls on another stream, results of its own making, and results dropped at once:
+    none of their memory is the current stream's before the calls are done."""
+    x, w, t = inputs(T, V, D)
+    ref = run(T, V, D)
+    stream = torch.cuda.Stream()
+    given = stream if kind == "torch" else stream.cuda_stream
+    dx, dw = torch.empty(T, D, device="cuda", dtype=BF), torch.empty(V, D, device="cuda", dtype=BF)
+    torch.cuda.synchronize()
+    out = []
+
+    def call():
+        junk = torch.full((B.ps_xent_sizes(T, V, D)[1],), 3, dtype=torch.uint8, device="cuda")
+        torch.cuda._sleep(2_000_000)
+        junk.fill_(9)                                       # (still to run when the workspace takes the memory over)
+        del junk
+        ce = B.CrossEntropy(T, V, D)
+        loss, lse = ce.forward(x, w, t, stream=given)
+        ce.backward(x, w, t, lse, dx, dw, stream=given)
+        gone = ce.forward(x, w, t, stream=given)
+        out.extend((loss, lse, dx, dw))
+        if kind == "torch":
+            del ce, gone
+        else:
+            out.append((ce, gone))                          # (dropping it waits, which is looked at below)
+        return out
+
+    on_a_busy_stream(stream, call, (T * 4, 1 << 20, *B.ps_xent_sizes(T, V, D)))
+    for a, b in zip(out[:4], ref):
+        assert torch.equal(a, b)
+    if kind == "number":
+        ce, _ = out.pop()
+        with torch.cuda.stream(stream):
+            torch.cuda._sleep(20_000_000)
+        ce.forward(x, w, t, stream=given)
+        del ce, _
+        assert stream.query()
+
+
+@gpu
+def test_results_made_on_the_default_stream_beside_a_current_one():
+    """No stream given is the default one, whatever is current."""
+    T, V, D = 200, 700, 64
+    x, w, t = inputs(T, V, D)
+    ref = run(T, V, D)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        ce = B.CrossEntropy(T, V, D)
+        loss, lse = ce.forward(x, w, t)
+        torch.cuda.default_stream().synchronize()
+        assert torch.equal(loss, ref[0]) and torch.equal(lse, ref[1])
+
+
+def test_memory_of_calls_on_other_streams_is_the_allocators_business(monkeypatch):
+    """On made-up streams: the workspace is reported once for each torch stream, results come from the call's stream, and a
+    stream given as a number makes the drop wait."""
+    ops_ready = B.CrossEntropy                              # (loads the extension)
+    log, now = [], []
+
+    class Stream:
+        def __init__(self, handle):
+            self.cuda_stream = handle
+
+        def record_event(self):
+            return "made on %d" % self.cuda_stream
+
+        def wait_event(self, e):
+            log.append(("wait", self.cuda_stream, e))
+
+    class Entered:
+        def __init__(self, s):
+            self.s = s
+
+        def __enter__(self):
+            now.append(self.s)
+
+        def __exit__(self, *a):
+            now.pop()
+
+    class Memory:
+        device = "cuda:0"
+
+        def __init__(self, n):
+            self.n, self.on = n, now[-1].cuda_stream
+
+        def record_stream(self, s):
+            log.append(("record", self.n, self.on, s.cuda_stream))
+
+        data_ptr, numel, get_device = lambda self: 256, lambda self: self.n, lambda self: 0
+
+    class Loss(ops_ready):
+        def _forward(self, *a):
+            log.append(("forward", a[3].on, a[4].on, a[5]))
+
+        def _backward(self, *a):
+            log.append(("backward",))
+
+    now.append(Stream(0))
+    monkeypatch.setattr(torch.cuda, "Stream", Stream)
+    monkeypatch.setattr(torch, "empty", lambda n, **kw: Memory(n))
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: now[-1])
+    monkeypatch.setattr(torch.cuda, "default_stream", lambda device=None: Stream(0))
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle, device=None: Stream(handle))
+    monkeypatch.setattr(torch.cuda, "stream", Entered)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda device=None: log.append("synchronize"))
+    size = B.ps_xent_sizes(10, 20, 8)[0]
+    class Tokens(list):
+        device = "cuda:0"
+
+    x = Tokens(range(10))
+    ce, side = Loss(10, 20, 8), Stream(5)
+    ce.forward(x, None, None)
+    assert log == [("forward", 0, 0, None)]
+    for k in range(2):
+        del log[:]
+        ce.forward(x, None, None, stream=side)
+        results = [("record", 10, 5, 0)] * 2
+        assert log == ([("wait", 5, "made on 0"), ("record", size, 0, 5)] if k == 0 else []) + results + [("forward", 5, 5, side)]
+    del log[:]
+    ce.backward(x, None, None, None, stream=side)
+    assert log == [("backward",)]
+    del ce
+    assert log == [("backward",)]
+    ce = Loss(10, 20, 8)
+    ce.backward(x, None, None, None, stream=7)
+    assert log[1:] == [("wait", 7, "made on 0"), ("backward",)]
+    del ce
+    assert log[-1] == "synchronize"
+
+
 @gpu
 def test_the_binding_refuses():
     ce = B.CrossEntropy(10, 100, 16)
