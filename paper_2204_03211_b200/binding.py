@@ -786,8 +786,8 @@ def _load_ops():
         def __init__(self, rows: int, cols: int, device=None):
             n, m = C.c_size_t(), C.c_size_t()
             _check_op(load().ps_mx_sizes(rows, cols, C.byref(n), C.byref(m)), "ps_mx_sizes")
-            self.codes = torch.empty(n.value, dtype=torch.uint8, device=device or "cuda")
-            self.scales = torch.empty(m.value, dtype=torch.uint8, device=device or "cuda")
+            self.codes = torch.empty(n.value, dtype=torch.uint8, device="cuda" if device is None else device)
+            self.scales = torch.empty(m.value, dtype=torch.uint8, device="cuda" if device is None else device)
             super().__init__(self.codes.data_ptr(), self.scales.data_ptr(), rows, cols, self.codes.get_device())
 
         @property
@@ -810,7 +810,7 @@ def _load_ops():
             sizes = ps_xent_sizes(tokens, vocab, dim)
             self.tokens, self.vocab, self.dim = tokens, vocab, dim
             self.workspace = torch.empty(sizes[0 if (dim % 8 == 0 if aligned is None else aligned) else 1],
-                                         dtype=torch.uint8, device=device or "cuda")
+                                         dtype=torch.uint8, device="cuda" if device is None else device)
             self.device = self.workspace.get_device()
             # The workspace's memory follows the stream that is current now.  Another stream's first call waits for what
             # that one has been given before, whose memory it may have been, and the allocator is told of that stream.

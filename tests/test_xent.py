@@ -425,6 +425,26 @@ def test_results_made_on_the_default_stream_beside_a_current_one():
         assert torch.equal(loss, ref[0]) and torch.equal(lse, ref[1])
 
 
+def test_device_zero_is_a_device(monkeypatch):
+    """Given as 0 it is GPU 0, whatever is current; not given it is the current one."""
+    asked = []
+    B.CrossEntropy, B.MxTensor                              # (loads the extension)
+
+    class Asked(Exception):
+        pass
+
+    def empty(*a, device=None, **kw):
+        asked.append(device)
+        raise Asked
+
+    monkeypatch.setattr(torch, "empty", empty)
+    for make in (lambda d: B.CrossEntropy(10, 20, 8, d), lambda d: B.MxTensor(32, 64, d)):
+        for device in (0, 1, "cuda:0", None):
+            with pytest.raises(Asked):
+                make(device)
+    assert asked == [0, 1, "cuda:0", "cuda"] * 2
+
+
 def test_memory_of_calls_on_other_streams_is_the_allocators_business(monkeypatch):
     """On made-up streams: the workspace is reported once for each torch stream, results come from the call's stream, and a
     stream given as a number makes the drop wait."""
