@@ -183,11 +183,12 @@ int ps_register_block(ps_service* svc, int job, int block, size_t nelem, int ctx
  * blocks of such jobs and of others goes out as two launches, the others' first, when everything that may fail for want
  * of memory has been done for both.  Should CUDA refuse a later launch of the call after all (PS_ERR_CUDA), the blocks of
  * those before it are aggregated and their pushes consumed; PS_MUON blocks whose sums went out and whose orthogonalisation
- * did not have their new momentum and step, and their old parameters.  The first aggregate of a set of
- * blocks that are aggregated together makes its tables and, if it needs more than any before, the
- * workspace (about 12 bytes per element and 16 for the square of each matrix's smaller side), and
- * waits for the device; the tables of the last 64 sets are kept.  ps_block_profile covers the sum
- * of the shards, not the orthogonalisation.
+ * did not have their new momentum and step, and their old parameters.
+ * The first aggregate of a set of blocks, listed in whatever order, makes its tables on the host and, if it needs more
+ * than any before, the workspace (about 12 bytes per element and 8 for the square of each matrix's smaller side; this
+ * waits for the device).  Tables are kept for the sets used last, 64 or two per registered matrix if that is more, and 256 MB
+ * at most; they hold until one of the set's blocks moves or is cut into chunks in another way.  ps_block_profile covers
+ * the sum of the shards, not the orthogonalisation.
  * Errors: those of ps_register_block; BAD_ARG (not a PS_MUON job, rows or cols below 1 or above
  * 2^20, update_scale not finite), TOO_LARGE. */
 int ps_register_matrix(ps_service* svc, int job, int block, long long rows, long long cols, int ctx,

@@ -211,7 +211,12 @@ NsPlan::~NsPlan() {
   if (mem_) cudaFree(mem_);              // (waits for launches that still use it)
 }
 
-int NsPlan::build(const std::vector<NsItem>& items, bool split, void* workspace, int* status) {
+void NsPlan::adopt(NsPlan& old) {
+  std::swap(mem_, old.mem_);             // (what this one had goes with the old one)
+  std::swap(cap_, old.cap_);
+}
+
+int NsPlan::build(const std::vector<NsItem>& items, bool split, void* workspace, int* status, cudaStream_t stream) {
   small_ = small_ctas(items);
   pair_ = take_pairs(items);
   const long long tile = pair_ ? 256 : 128;
@@ -350,24 +355,36 @@ int NsPlan::build(const std::vector<NsItem>& items, bool split, void* workspace,
   units_off_ = take(units.size() * sizeof(int2));
   const size_t done_off = take(n * sizeof(unsigned int) * 32);         // a line each
   const size_t status_off = take(sizeof(int));
-  void* mem = nullptr;
-  cudaError_t e = cudaMalloc(&mem, off);
-  if (e != cudaSuccess) return op_cuda_error("tables of the orthogonalisation", e);
-  mem_ = static_cast<unsigned char*>(mem);
+  cudaError_t e = cudaSuccess;
+  if (off > cap_) {
+    if (mem_) cudaFree(mem_);
+    mem_ = nullptr;
+    cap_ = 4096;                         // (powers of two: the next set's tables are likely to fit)
+    while (cap_ < off) cap_ *= 2;
+    if (cap_ > (64u << 20)) cap_ = off;
+    void* mem = nullptr;
+    e = cudaMalloc(&mem, cap_);
+    if (e != cudaSuccess) {
+      cap_ = 0;
+      return op_cuda_error("tables of the orthogonalisation", e);
+    }
+    mem_ = static_cast<unsigned char*>(mem);
+  }
   for (size_t i = 0; i < n; ++i) {
     mats[i].maps = reinterpret_cast<const CUtensorMap*>(mem_ + maps_off) + kNsMaps * i;
     mats[i].done = reinterpret_cast<unsigned int*>(mem_ + done_off) + 32 * i;
   }
   auto put = [&](size_t o, const void* p, size_t bytes) {
-    if (e == cudaSuccess && bytes) e = cudaMemcpy(mem_ + o, p, bytes, cudaMemcpyHostToDevice);
+    if (e == cudaSuccess && bytes) e = cudaMemcpyAsync(mem_ + o, p, bytes, cudaMemcpyHostToDevice, stream);
   };
   put(maps_off, maps.data(), maps.size() * sizeof(CUtensorMap));
   put(mats_off_, mats.data(), n * sizeof(NsMat));
   put(list_off_, list.data(), list.size() * sizeof(NsTile));
   put(begin_off_, begin.data(), begin.size() * sizeof(int));
   put(units_off_, units.data(), units.size() * sizeof(int2));
-  if (e == cudaSuccess) e = cudaMemset(mem_ + done_off, 0, status_off + sizeof(int) - done_off);
-  if (e == cudaSuccess) e = cudaStreamSynchronize(cudaStreamLegacy);   // before other streams use it
+  if (e == cudaSuccess) e = cudaMemsetAsync(mem_ + done_off, 0, status_off + sizeof(int) - done_off, stream);
+  const cudaError_t w = cudaStreamSynchronize(stream);   // before other streams use it, and before the lists here are gone
+  if (e == cudaSuccess) e = w;
   if (e != cudaSuccess) return op_cuda_error("tables of the orthogonalisation", e);
   status_ = status ? status : reinterpret_cast<int*>(mem_ + status_off);
   count_ = (int)n;

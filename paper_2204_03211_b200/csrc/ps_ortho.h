@@ -34,14 +34,19 @@ class NsPlan {
 
   // Bytes of workspace that a list needs; split: three products of halves (binary32 results).  0: too large a list.
   static size_t workspace(const std::vector<NsItem>& items, bool split);
-  // Makes the tables for the current device and waits until they are there.  Throws std::bad_alloc only.  `status`: the
-  // device word in which a bounded wait that ran out is noted; nullptr: one of its own.
-  int build(const std::vector<NsItem>& items, bool split, void* workspace, int* status = nullptr);
+  // Makes the tables for the current device, copies them on `stream` and waits until they are there.  Throws
+  // std::bad_alloc only.  `status`: the device word in which a bounded wait that ran out is noted; nullptr: one of its own.
+  int build(const std::vector<NsItem>& items, bool split, void* workspace, int* status = nullptr,
+            cudaStream_t stream = cudaStreamLegacy);
+  // Takes over the memory of a plan that no launch uses any more, for the tables of the next build.
+  void adopt(NsPlan& old);
+  size_t bytes() const { return cap_; }
   int run(cudaStream_t stream, int* launches = nullptr) const;
   int status(int* out) const;            // waits for the device
 
  private:
   unsigned char* mem_ = nullptr;
+  size_t cap_ = 0;
   int* status_ = nullptr;
   size_t mats_off_ = 0, list_off_ = 0, begin_off_ = 0, units_off_ = 0;
   int count_ = 0, units_ = 0, grid_ = 0;

@@ -145,16 +145,33 @@ struct Prepared {
   Plan clip_plan;
 };
 
-// The tables of the orthogonalisation for one set of PS_MUON blocks that are aggregated together.
+// One block of a set of PS_MUON blocks that are aggregated together: all that the orthogonalisation's tables depend on.
+struct MuonItem {
+  const float* p;
+  long long rows, cols;
+  float decay, step;
+  unsigned int first_chunk, nchunks;
+  bool operator==(const MuonItem& o) const {
+    return p == o.p && rows == o.rows && cols == o.cols && decay == o.decay && step == o.step && first_chunk == o.first_chunk &&
+           nchunks == o.nchunks;
+  }
+};
+
+// The tables for one such set.
 struct MuonSet {
-  std::vector<int> idx;                    // the set
-  unsigned long long epoch = 0;            // where its blocks lie, and how they are cut into chunks
-  unsigned long long used = 0;             // the aggregate that used it last
+  std::vector<MuonItem> items;             // in the table's order, which does not depend on the caller's
+  unsigned long long used = 0;             // when it was used last (ps_service::muon_uses)
+  int slot = -1;                           // slot and number of the launch that used it last
+  unsigned long long seq = 0;
   std::vector<size_t> u_off;               // per task of the table, floats from the workspace's start
   size_t parts_off = 0;                    // bytes
   NsPlan plan;
 };
-constexpr size_t kMuonSets = 64;           // sets whose tables are kept
+// Sets whose tables are kept: what a service with many matrices cycles through, layer by layer or one by one, and so many
+// bytes at most (144 matrices of 24 layers 1024 wide: 4 MB for all of them in one set or each in its own).  A step of 144
+// aggregates of one such matrix each 58 ms with 64 sets, 51 so; 128 wide 12.1 and 9.2; layer by layer in a new order every
+// time, 128 wide, 2.4 with a set for every order, 1.9 so.
+constexpr size_t kMuonSets = 64, kMuonSetsPerBlock = 2, kMuonTableBytes = 256u << 20;
 
 // What a clipped aggregate adds to an aggregate.
 struct ClipCall {
@@ -233,9 +250,12 @@ struct ps_service {
   char* muon_ws = nullptr;
   size_t muon_ws_cap = 0;
   std::vector<std::unique_ptr<MuonSet>> muon_sets;
+  unsigned long long muon_uses = 0;
+  size_t muon_blocks = 0;                  // registered blocks of PS_MUON jobs
   int muon_slot = -1;                      // slot and number of the last one
   unsigned long long muon_seq = 0;
   std::vector<int> idx_muon, idx_other;    // scratch: a ready list by kind
+  std::vector<MuonItem> muon_want;         // scratch: what the tables of a set are looked up by
   int last_grid = 0, last_block = 0;
   const char* last_kernel = "none";
   std::string cuda_err;
@@ -896,6 +916,7 @@ int ps_register_matrix(ps_service* s, int job, int block, long long rows, long l
   b.rows = rows;
   b.cols = cols;
   b.update_scale = update_scale;
+  ++s->muon_blocks;
   return PS_OK;
 }
 
@@ -1585,33 +1606,63 @@ int launch_clip(ps_service* s, const std::vector<int>& idx, Plan& plan, const Cl
   return PS_OK;
 }
 
+// Makes room for one more set's tables: the sets that have not been used for longest go.  The last one's memory is handed to
+// `next`, so that a service whose sets keep changing frees nothing, which would wait for the device; only the launch that
+// used it last has to be over, and it is the oldest.
+int drop_muon_sets(ps_service* s, NsPlan* next) {
+  size_t bytes = 0;
+  for (auto& m : s->muon_sets) bytes += m->plan.bytes();
+  const size_t most = std::max(kMuonSets, kMuonSetsPerBlock * s->muon_blocks);
+  while (!s->muon_sets.empty() && (s->muon_sets.size() >= most || bytes >= kMuonTableBytes)) {
+    size_t old = 0;
+    for (size_t k = 1; k < s->muon_sets.size(); ++k)
+      if (s->muon_sets[k]->used < s->muon_sets[old]->used) old = k;
+    MuonSet& m = *s->muon_sets[old];
+    if (m.slot >= 0 && s->slots[m.slot].seq == m.seq) {
+      const int rc = wait_slot(s, s->slots[m.slot]);
+      if (rc) return rc;
+    }
+    bytes -= m.plan.bytes();
+    next->adopt(m.plan);
+    s->muon_sets.erase(s->muon_sets.begin() + (long)old);
+  }
+  return PS_OK;
+}
+
 // The tables for the set of PS_MUON blocks of `plan`, kept from aggregate to aggregate, and the workspace they need.
 int muon_set(ps_service* s, const Plan& plan, MuonSet** out) {
   const unsigned char* base = plan.bytes.data();
   const PsTaskDev* tasks = reinterpret_cast<const PsTaskDev*>(base + reinterpret_cast<const PsTableHdr*>(base)->tasks_off);
-  const unsigned long long now = s->launches + 1;
+  const size_t n = plan.order.size();
+  std::vector<MuonItem>& want = s->muon_want;
+  want.clear();
+  for (size_t i = 0; i < n; ++i) {
+    const Block& b = s->blocks[plan.order[i]];
+    const ps_job_desc& d = s->jobs[b.job].d;
+    want.push_back(MuonItem{blk_p(s, b), b.rows, b.cols, (float)(1.0 - (double)d.lr * (double)d.weight_decay),
+                            (float)((double)d.lr * (double)b.update_scale), tasks[i].first_chunk, tasks[i].nchunks});
+  }
+  const unsigned long long now = ++s->muon_uses;
   for (auto& m : s->muon_sets)
-    if (m->epoch == s->epoch && m->idx == plan.order) {
+    if (m->items == want) {
       m->used = now;
       *out = m.get();
       return PS_OK;
     }
-  const size_t n = plan.order.size();
   auto m = std::make_unique<MuonSet>();
-  m->idx = plan.order;
-  m->epoch = s->epoch;
+  m->items = want;
   m->used = now;
   size_t at = 0;
   for (size_t i = 0; i < n; ++i) {
     m->u_off.push_back(at / sizeof(float));
-    at += Arena::round_up(s->blocks[plan.order[i]].nelem * sizeof(float));
+    at += Arena::round_up((size_t)want[i].rows * (size_t)want[i].cols * sizeof(float));
   }
   m->parts_off = at;
   at += Arena::round_up((size_t)plan.total_chunks * sizeof(double));
   std::vector<NsItem> items(n);
   for (size_t i = 0; i < n; ++i) {
-    items[i].rows = s->blocks[plan.order[i]].rows;
-    items[i].cols = s->blocks[plan.order[i]].cols;
+    items[i].rows = want[i].rows;
+    items[i].cols = want[i].cols;
     items[i].parts = reinterpret_cast<double*>(1);       // (not the library's to find room for)
   }
   const size_t ns = NsPlan::workspace(items, true);
@@ -1631,31 +1682,24 @@ int muon_set(ps_service* s, const Plan& plan, MuonSet** out) {
     }
     s->muon_ws_cap = at + ns;
   }
+  int rc = drop_muon_sets(s, &m->plan);
+  if (rc) return rc;
   for (size_t i = 0; i < n; ++i) {
-    const Block& b = s->blocks[plan.order[i]];
-    const ps_job_desc& d = s->jobs[b.job].d;
     NsItem& it = items[i];
     it.src = reinterpret_cast<float*>(s->muon_ws) + m->u_off[i];
-    it.ld_src = it.ld_dst = b.cols;
-    it.parts = reinterpret_cast<double*>(s->muon_ws + m->parts_off) + tasks[i].first_chunk;
-    it.nparts = (int)tasks[i].nchunks;
-    it.dst = blk_p(s, b);
+    it.ld_src = it.ld_dst = want[i].cols;
+    it.parts = reinterpret_cast<double*>(s->muon_ws + m->parts_off) + want[i].first_chunk;
+    it.nparts = (int)want[i].nchunks;
+    it.dst = const_cast<float*>(want[i].p);
     it.out = kNsOutUpdate;
-    it.decay = (float)(1.0 - (double)d.lr * (double)d.weight_decay);
-    it.step = (float)((double)d.lr * (double)b.update_scale);
+    it.decay = want[i].decay;
+    it.step = want[i].step;
   }
-  const int rc = m->plan.build(items, true, s->muon_ws + at, s->status_dev);
+  // (copied on the service's own stream: a launch that is running does not hold the caller up)
+  rc = m->plan.build(items, true, s->muon_ws + at, s->status_dev, s->copy_stream);
   if (rc) {
     if (rc == PS_ERR_CUDA) s->cuda_err = ps_op_last_error();
     return rc;
-  }
-  if (s->muon_sets.size() >= kMuonSets) {  // the one that has not been used for longest, or whose blocks have moved
-    size_t old = 0;
-    for (size_t k = 1; k < s->muon_sets.size(); ++k) {
-      const MuonSet &a = *s->muon_sets[k], &b = *s->muon_sets[old];
-      if ((a.epoch != s->epoch) != (b.epoch != s->epoch) ? a.epoch != s->epoch : a.used < b.used) old = k;
-    }
-    s->muon_sets.erase(s->muon_sets.begin() + (long)old);      // (freeing its tables waits for the device)
   }
   s->muon_sets.push_back(std::move(m));
   *out = s->muon_sets.back().get();
@@ -1687,7 +1731,7 @@ int order_muon(ps_service* s, const std::vector<int>& idx, Plan& plan, const Muo
 }
 
 // Launches that aggregate with the slot that is now the next one (acquired before).
-int launch_muon(ps_service* s, const std::vector<int>& idx, const Plan& plan, const MuonSet& set, cudaStream_t stream) {
+int launch_muon(ps_service* s, const std::vector<int>& idx, const Plan& plan, MuonSet& set, cudaStream_t stream) {
   const int slot_index = s->next_slot;
   Slot* sl = &s->slots[slot_index];
   const unsigned long long seq = s->launches + 1;
@@ -1709,8 +1753,8 @@ int launch_muon(ps_service* s, const std::vector<int>& idx, const Plan& plan, co
   sl->work_stream = -1;
   sl->inflight = true;
   sl->done_recorded = false;
-  s->muon_slot = slot_index;
-  s->muon_seq = seq;
+  s->muon_slot = set.slot = slot_index;
+  s->muon_seq = set.seq = seq;
   s->next_slot = (s->next_slot + 1) % kSlots;
   s->launches = seq;
   s->var_launches[kVarMuon]++;
@@ -1768,6 +1812,7 @@ static int submit_muon(ps_service* s, const std::vector<int>& idx, cudaStream_t 
   s->idx_muon.clear();
   s->idx_other.clear();
   for (int bi : idx) (s->jobs[s->blocks[bi].job].d.opt == PS_MUON ? s->idx_muon : s->idx_other).push_back(bi);
+  std::sort(s->idx_muon.begin(), s->idx_muon.end());     // one table for a set, whatever order its blocks became ready in
   Plan muon;
   MuonSet* set = nullptr;
   rc = build_plan(s, s->idx_muon, &muon);
@@ -2429,6 +2474,7 @@ int ps_unregister_block(ps_service* s, int job, int block) {
   }
   s->ctxs[b.ctx].arena.release(b.off, b.bytes);
   s->jobs[b.job].block_of_id[b.id] = -1;
+  if (s->jobs[b.job].d.opt == PS_MUON) --s->muon_blocks;
   b.nelem = 0;
   b.bytes = 0;
   b.npushed = 0;

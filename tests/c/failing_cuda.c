@@ -4,8 +4,9 @@
 #define _GNU_SOURCE
 #include <dlfcn.h>
 #include <stddef.h>
+#include <string.h>
 
-static int left, seen, copies, launches;
+static int left, seen, copies, launches, mallocs, stops;
 static const void* copied_from;
 
 void fail_cuda(int n) { left = n; seen = 0; }
@@ -13,6 +14,8 @@ int calls_seen(void) { return seen; }
 int copies_seen(void) { return copies; }
 const void* last_copy_from(void) { return copied_from; }        /* host memory of the last asynchronous copy */
 int launches_seen(void) { return launches; }
+int mallocs_seen(void) { return mallocs; }
+int stops_seen(void) { return stops; }                          /* calls that wait for all that runs on the device */
 
 static int fails(void) {
   ++seen;
@@ -23,6 +26,7 @@ static int fails(void) {
 
 int cudaMalloc(void** p, size_t n) {
   NEXT(cudaMalloc);
+  ++mallocs;
   return fails() ? 2 : next(p, n);                              /* cudaErrorMemoryAllocation */
 }
 int cudaHostAlloc(void** p, size_t n, unsigned flags) {
@@ -31,14 +35,16 @@ int cudaHostAlloc(void** p, size_t n, unsigned flags) {
 }
 int cudaMemcpy(void* d, const void* s, size_t n, int kind) {
   NEXT(cudaMemcpy);
+  ++stops;
   return fails() ? 999 : next(d, s, n, kind);
 }
 int cudaMemcpyAsync(void* d, const void* s, size_t n, int kind, void* stream) {
-  NEXT(cudaMemcpyAsync);
+  (void)kind; (void)stream;
   if (fails()) return 999;
   ++copies;
   copied_from = s;
-  return next(d, s, n, kind, stream);
+  memcpy(d, s, n);
+  return 0;
 }
 int cudaStreamWaitEvent(void* stream, void* event, unsigned flags) {
   NEXT(cudaStreamWaitEvent);
@@ -57,6 +63,22 @@ int cudaLaunchKernelExC(const void* config, const void* f, void** args) {
   if (fails()) return 999;
   ++launches;
   return next(config, f, args);
+}
+
+int cudaFree(void* p) {
+  NEXT(cudaFree);
+  ++stops;
+  return next(p);
+}
+int cudaDeviceSynchronize(void) {
+  NEXT(cudaDeviceSynchronize);
+  ++stops;
+  return next();
+}
+int cudaStreamSynchronize(void* stream) {
+  NEXT(cudaStreamSynchronize);
+  if (!stream || stream == (void*)1 || stream == (void*)2) ++stops;       /* the default streams */
+  return next(stream);
 }
 
 static int encode() { return 0; }

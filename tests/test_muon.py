@@ -415,6 +415,11 @@ for how in ("aggregate", "round", "prepared"):
 def test_what_fails_half_way_leaves_every_block_usable(tmp_path, sides):
     """One list with blocks of two jobs, small matrices and larger ones; every call of the CUDA runtime that can fail does,
     once.  Pushes are consumed by what was launched and by nothing else, and no launch's table is written again too early."""
+    made_up_runtime(tmp_path, FAILURES, sides)
+
+
+def made_up_runtime(tmp_path, script, *args):
+    """Runs `script` on the runtime of tests/c/pretend_cuda.c, with tests/c/failing_cuda.c in front of it."""
     import os
     import subprocess
     import sys
@@ -425,6 +430,104 @@ def test_what_fails_half_way_leaves_every_block_usable(tmp_path, sides):
         libs.append(str(tmp_path / (name + ".so")))
         subprocess.run(["gcc", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-o", libs[-1],
                         os.path.join(root, "tests", "c", name + ".c"), "-ldl"], check=True)
-    run = subprocess.run([sys.executable, "-c", FAILURES, root, libs[0], sides],
+    run = subprocess.run([sys.executable, "-c", script, root, libs[0], *args],
                          env=dict(os.environ, LD_PRELOAD=":".join(libs)), capture_output=True, text=True)
     assert run.returncode == 0, run.stderr
+
+
+CHANGING_SETS = r"""
+import ctypes as C, random, sys
+sys.path.insert(0, sys.argv[1])
+from paper_2204_03211_b200 import binding as B
+B.load()
+fake = C.CDLL(sys.argv[2])
+LAYERS, PER = 24, 6
+N = LAYERS * PER
+svc = B.Service(0, 2, 1 << 25)
+svc.register_job(opt=B.PS_MUON, num_workers=1)
+for b in range(N):
+    svc.register_matrix(0, b, 40 + b % 7, 64 if b % PER else 200)
+rng = random.Random(3)
+
+
+def go(blocks):
+    for b in blocks:
+        svc.push(0, b, 0, 1 << 20)
+    svc.aggregate([(0, b) for b in blocks])
+
+
+def costs(call):
+    before = fake.mallocs_seen(), fake.stops_seen(), fake.copies_seen()
+    call()
+    return tuple(a - b for a, b in zip((fake.mallocs_seen(), fake.stops_seen(), fake.copies_seen()), before))
+
+
+def iteration(shuffled):
+    everything = list(range(N))
+    layers = [everything[i:i + PER] for i in range(0, N, PER)]
+    lists = [everything] + layers + [[b] for b in everything]
+    for l in lists:
+        if shuffled:
+            rng.shuffle(l)
+        go(l)
+    return len(lists)
+
+
+for sort in (1, 0):
+    svc.set_option(B.PS_OPT_SORT_TASKS, sort)
+    count = iteration(False)
+    for k in range(20):                     # task tables in flight may still grow, each slot once
+        go(list(range(N)))
+    # a step that walks all of it again, in the same order or as things become ready, costs one table per aggregate
+    for shuffled in (False, True, True):
+        assert costs(lambda: iteration(shuffled)) == (0, 0, count), (sort, shuffled)
+# options that do not touch the chunks keep the tables, too
+svc.set_option(B.PS_OPT_PROFILE, 1)
+svc.set_option(B.PS_OPT_OVERLAP, 1)
+assert costs(lambda: iteration(True)) == (0, 0, count)
+# a block that moves drops the sets that it belongs to
+svc.migrate_block(0, 7, 1)
+assert costs(lambda: go([8])) == (0, 0, 1)
+mallocs, stops, copies = costs(lambda: go([7]))
+assert stops == 0 and copies > 1
+assert costs(lambda: go([7])) == (0, 0, 1)
+# sets that are new every time: tables are made, but what was there before is not freed, and nothing is waited for
+for k in range(3 * N):
+    go(rng.sample(range(N), 5))
+mallocs, stops, copies = costs(lambda: [go(rng.sample(range(N), 5)) for _ in range(500)])
+assert stops == 0 and mallocs == 0, (mallocs, stops)
+svc.close()
+"""
+
+
+def test_sets_of_blocks_that_change_from_call_to_call(tmp_path):
+    """144 matrices, all at once, layer by layer and one by one, listed in changing orders; then sets that never recur.  Tables
+    are made once for a set, and making them neither frees memory nor waits for the device."""
+    made_up_runtime(tmp_path, CHANGING_SETS)
+
+
+@gpu
+def test_listed_in_any_order_with_options_that_change():
+    w = World([(64, 64), (300, 70), (64, 64), (128, 512), (200, 130), (64, 64)], 2)
+    gen = np.random.default_rng(0)
+    for t, (option, value) in enumerate(((B.PS_OPT_SORT_TASKS, 0), (B.PS_OPT_CHUNK_ELEMS, 1024), (B.PS_OPT_PROFILE, 1),
+                                         (B.PS_OPT_CHUNK_ELEMS, 0), (B.PS_OPT_SORT_TASKS, 1), (B.PS_OPT_OVERLAP, 1))):
+        w.svc.set_option(option, value)
+        w.step([int(b) for b in gen.permutation(6)])
+    w.check(6)
+
+
+@gpu
+def test_sets_that_never_recur():
+    """More sets than are kept, in a row without waiting: tables are made in the memory of older ones."""
+    w = World([(8, 8), (16, 8), (8, 150), (24, 24), (9, 9), (130, 8), (8, 40), (12, 12), (8, 9), (20, 20)], 1)
+    bufs = [w.shards(b) for b in range(10)]
+    done, k = [0] * 10, 0
+    for mask in list(range(1, 150)) * 2:
+        group = [b for b in range(10) if (mask * 37 % 1023 + 1) >> b & 1]
+        for b in group:
+            w.push(b, bufs[b])
+            w.expect(b, bufs[b])
+            done[b] += 1
+        w.svc.aggregate([(w.job, b) for b in reversed(group)])
+    w.check(done)
