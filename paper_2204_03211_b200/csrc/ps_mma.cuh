@@ -98,6 +98,10 @@ __device__ __forceinline__ unsigned long long mm_desc_codes(unsigned int addr) {
   return (unsigned long long)((addr & 0x3ffffu) >> 4) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
 }
 
+// Instructions that are `.aligned` want all lanes of the warp at once.  What comes before them here are waits in which each
+// lane spins by itself and branches that some lanes take: mm_load, mm_store16 and mm_cluster_sync bring the lanes together
+// first.
+
 // 32 or 16 columns of this warp's 32 lanes, without waiting for them.
 __device__ __forceinline__ void mm_load32(unsigned int tmem, float* v) {
   unsigned int* u = reinterpret_cast<unsigned int*>(v);
@@ -113,6 +117,7 @@ __device__ __forceinline__ void mm_load32(unsigned int tmem, float* v) {
 }
 __device__ __forceinline__ void mm_store16(unsigned int tmem, const float* v) {      // without waiting
   const unsigned int* u = reinterpret_cast<const unsigned int*>(v);
+  __syncwarp();
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
       "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(tmem),
@@ -131,6 +136,7 @@ __device__ __forceinline__ void mm_load16(unsigned int tmem, float* v) {
 }
 template <int N>
 __device__ __forceinline__ void mm_load(unsigned int tmem, float (&v)[N]) {
+  __syncwarp();
   if constexpr (N == 16) {
     mm_load16(tmem, v);
   } else {
@@ -147,6 +153,7 @@ __device__ __forceinline__ unsigned int mm_bf16x2(float lo, float hi) {
 }
 
 __device__ __forceinline__ void mm_cluster_sync() {
+  __syncwarp();
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
