@@ -350,7 +350,7 @@ ps_tc_kernel(const __grid_constant__ typename Op::Args args) {
           if (warp == 2) {
             TcTile t;
             Op::tile(args, item, &t);
-            if (!tc_wait_ready(t, args.status)) break;
+            if (!tc_wait_ready(t, args.status)) { ok = false; break; }       // (the copies below are waited for then)
             for (int e = 0; ok && e < max(entries[0], entries[1]); ++e)
 #pragma unroll
               for (int h = 0; h < 2; ++h)
