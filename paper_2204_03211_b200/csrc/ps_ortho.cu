@@ -179,13 +179,14 @@ static int small_ctas(const std::vector<NsItem>& items) {
     for (; s != srcs.end() && s->first < d.end; ++s)
       if (s->of != d.of && s->end > d.first) return 0;
   }
-  // One CTA where it can hold a matrix.  Else 128 columns each rather than 256: what every CTA does for itself gets shorter,
-  // adding up A does not get longer (four of 128 x 512: 81 us on two CTAs each, 66 on four).  Seven clusters of sixteen run
-  // at a time; for more than two turns the general form is as fast or faster (12 | 16 | 32 of 128 x 4096 to bf16: 155 | 232 |
-  // 389 us here, 191 | 218 | 341 there), and for 2048 columns clusters of eight (20 to fp32: 193 us, on sixteen 258).
+  // One CTA where it can hold a matrix.  Else 128 columns each rather than 256, so four CTAs at least: what every CTA does for
+  // itself gets shorter, adding up A does not get longer (four of 128 x 512: 81 us on two CTAs each, 66 on four).  Seven
+  // clusters of sixteen run at a time; for more than two turns the general form is as fast or faster (12 | 16 | 32 of
+  // 128 x 4096 to bf16: 155 | 232 | 389 us here, 191 | 218 | 341 there), and for 2048 columns clusters of eight (20 to fp32:
+  // 193 us, on sixteen 258).
   if (widest <= kSoCols) return 1;
   if (widest > kSoCtas / 2 * kSoCols) return srcs.size() <= 14 ? kSoCtas : 0;
-  int ctas = 2;
+  int ctas = 4;
   while (ctas < kSoCtas / 2 && ctas * (kSoCols / 2) < widest) ctas *= 2;
   return ctas;
 }

@@ -4,7 +4,7 @@
 // tile to the next through L2: 6 to 8 us, fifteen times.  Here a CTA keeps 128 rows by up to 256 columns of X (two
 // halves, 128 KB) and A or B (two halves, 64 KB) in shared memory, in the swizzled layout in which the tensor cores take
 // operands: X is an operand along its rows in X X^T and across them in B X, from the same bytes.  Wider matrices are cut
-// into columns over a cluster of 2 to 16 CTAs; only A is a sum over all of them, which they add up through each
+// into columns over a cluster of 4 to 16 CTAs; only A is a sum over all of them, which they add up through each
 // other's shared memory, a share of the rows each, in rank order.  One launch does it all: norm, scaling, steps, result.
 //
 // Measured to fp32 | bf16: 8 of 64 x 256 46 | 32 us (general form 120), 4 of 128 x 512 64 | 48, 4 of 128 x 2048 95 | 69,
@@ -42,7 +42,7 @@ static_assert(sizeof(SoControl) <= 2048 && kSoSmem <= 227 * 1024, "does not fit"
 struct SoArgs {
   const NsMat* mats;
   int* status;
-  int ctas;                                              // of a cluster: 1, 2, 4, 8 or 16
+  int ctas;                                              // of a cluster: 1, 4, 8 or 16
 };
 
 // Byte offset of 16-byte piece `piece` (8 columns) of a row, in planes of 64-column blocks.
@@ -348,8 +348,7 @@ ps_ortho_small_kernel(const __grid_constant__ SoArgs args) {
 #pragma unroll
         for (int k = 0; k < 32; k += 4)
           *reinterpret_cast<float4*>(es + so_float4(row, part * 8 + k / 4)) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
-        if (ctas == 2) add_up(std::integral_constant<int, 2>());
-        else if (ctas == 4) add_up(std::integral_constant<int, 4>());
+        if (ctas == 4) add_up(std::integral_constant<int, 4>());
         else if (ctas == 8) add_up(std::integral_constant<int, 8>());
         else add_up(std::integral_constant<int, 16>());
       }
