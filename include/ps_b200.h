@@ -133,8 +133,9 @@ enum {
   PS_OPT_WORK_STREAMS = 9, /* with PS_OPT_OVERLAP: launches rotate over this many service-owned streams
                               (1..8, default 4) */
   PS_OPT_PROFILE = 5,      /* 1: aggregates record per-task device time (see ps_block_profile);
-                              costs a few atomics per chunk; direct-load kernels and clipped
-                              aggregates (both passes); default 0 */
+                              costs a few atomics per chunk; direct-load kernels, clipped
+                              aggregates (both passes) and aggregates of PS_MUON blocks (sums and
+                              orthogonalisation); default 0 */
   PS_OPT_KERNEL = 4        /* kernel variant: 0 = automatic (direct loads), 1 = direct loads,
                               2 = bulk-copy ring (shards staged through shared memory by the TMA
                               unit); results are identical except for the rounding of the
@@ -187,8 +188,7 @@ int ps_register_block(ps_service* svc, int job, int block, size_t nelem, int ctx
  * The first aggregate of a set of blocks, listed in whatever order, makes its tables on the host and, if it needs more
  * than any before, the workspace (about 12 bytes per element and 8 for the square of each matrix's smaller side; this
  * waits for the device).  Tables are kept for the sets used last, 64 or two per registered matrix if that is more, and 256 MB
- * at most; they hold until one of the set's blocks moves or is cut into chunks in another way.  ps_block_profile covers
- * the sum of the shards, not the orthogonalisation.
+ * at most; they hold until one of the set's blocks moves or is cut into chunks in another way.
  * Errors: those of ps_register_block; BAD_ARG (not a PS_MUON job, rows or cols below 1 or above
  * 2^20, update_scale not finite), TOO_LARGE. */
 int ps_register_matrix(ps_service* svc, int job, int block, long long rows, long long cols, int ctx,
@@ -408,7 +408,9 @@ int ps_block_stats(ps_service* svc, int job, int block, double* grad_sqnorm_out,
  * chunks of the time a CTA spent on the chunk (CTA-microseconds; chunks of one
  * task run concurrently on many CTAs); span = last chunk end - first chunk
  * start.  Timer: the GPU's %globaltimer (resolution is device dependent, up to
- * about 1 us).  Waits for the block's last aggregate.  Out pointers may be NULL. */
+ * about 1 us).  The orthogonalisation of a PS_MUON block counts with what its tiles took on their CTAs, each of which has an
+ * SM to itself and so counts four times (an SM holds four CTAs of the other aggregates).  Waits for the block's last
+ * aggregate.  Out pointers may be NULL. */
 int ps_block_profile(ps_service* svc, int job, int block, double* busy_us_out, double* span_us_out);
 
 /* The same over all blocks of a job (each block's last aggregate): summed busy

@@ -265,6 +265,7 @@ int NsPlan::build(const std::vector<NsItem>& items, bool split, void* workspace,
     M.wide = !M.flip && (reinterpret_cast<uintptr_t>(it.dst) & 31u) == 0 && it.ld_dst * (long long)es % 32 == 0;
     M.decay = it.decay;
     M.step = it.step;
+    M.stat = it.stat;
     if (small_) continue;
     const NsLayout l = layout(it, split, at);
     at = l.end;
@@ -394,25 +395,23 @@ int NsPlan::build(const std::vector<NsItem>& items, bool split, void* workspace,
   return PS_OK;
 }
 
-int NsPlan::run(cudaStream_t stream, int* launches) const {
-  if (launches) *launches = 0;
+int NsPlan::run(cudaStream_t stream, PsStat* stats) const {
   if (!count_) return PS_OK;
   const NsMat* mats = reinterpret_cast<const NsMat*>(mem_ + mats_off_);
   const int2* units = reinterpret_cast<const int2*>(mem_ + units_off_);
-  if (small_) {
-    if (launches) *launches = 1;
+  if (small_)
     return op_launch("orthogonalisation", split_ ? ps_ortho_small_kernel<2> : ps_ortho_small_kernel<1>, (unsigned)(count_ * small_),
-                     kSoThreads, kSoSmem, small_, stream, SoArgs{mats, status_, small_});
-  }
+                     kSoThreads, kSoSmem, small_, stream, SoArgs{mats, status_, small_, stats});
   int rc = PS_OK;
   if (norms_) rc = op_launch("orthogonalisation", ps_ortho_norm_kernel, (unsigned)units_, kNsThreads, 0, 1, stream, mats, units);
-  if (!rc) rc = op_launch("orthogonalisation", ps_ortho_prepare_kernel, (unsigned)units_, kNsThreads, 0, 1, stream, mats, units);
+  if (!rc) rc = op_launch("orthogonalisation", ps_ortho_prepare_kernel, (unsigned)units_, kNsThreads, 0, 1, stream, mats, units, stats);
   if (rc) return rc;
   NsArgs a;
   a.status = status_;
   a.mats = mats;
   a.list = reinterpret_cast<const NsTile*>(mem_ + list_off_);
   a.begin = reinterpret_cast<const int*>(mem_ + begin_off_);
+  a.stats = stats;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)grid_);
   cfg.blockDim = dim3(TcCfg<NsOp<1, false>>::kThreads);
@@ -426,7 +425,6 @@ int NsPlan::run(cudaStream_t stream, int* launches) const {
   cfg.numAttrs = 1;
   const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel.fn, a);
   if (e != cudaSuccess) return op_cuda_error("orthogonalisation", e);
-  if (launches) *launches = norms_ ? 3 : 2;
   return PS_OK;
 }
 

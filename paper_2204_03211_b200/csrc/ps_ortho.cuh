@@ -67,6 +67,7 @@ struct NsMat {                           // one matrix, in its working orientati
   float decay, step;                     // kNsOutUpdate: dst = dst * decay - step * O
   int parts_s, parts_x;                  // what `done` counts in a symmetric product and in the last one
   unsigned int* done;                    // CTAs' finished parts of tiles (those that have rows of the matrix)
+  unsigned int stat;                     // its record of device times
 };
 
 struct NsTile {                          // one tile of the list
@@ -80,7 +81,21 @@ struct NsArgs {
   const NsMat* mats;
   const NsTile* list;                    // CTA after CTA (or pair), each with its tiles in their common order
   const int* begin;                      // where each one's start, and the end
+  PsStat* stats;                         // nullptr: no device times
 };
+
+// Adds the time since t0 to a matrix's record.  The unit is the time of one of four CTAs on an SM, as in the aggregates of
+// other blocks, so that tasks of all kinds can be weighed against each other: a CTA that has an SM to itself counts four times.
+constexpr unsigned int kNsWholeSm = 4;
+__device__ __forceinline__ unsigned long long ns_now() {
+  unsigned long long t;
+  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+  return t;
+}
+__device__ __forceinline__ void ns_charge(PsStat* stats, const NsMat& M, unsigned long long t0, unsigned long long t1, unsigned int units) {
+  atomicAdd(&stats[M.stat].busy_ns, (t1 - t0) * units);
+  atomicMax(&stats[M.stat].t_last, t1);
+}
 
 // c + a and c - a for the lower and the upper of two fp16 numbers: mixed-precision additions widen as they add.
 __device__ __forceinline__ float2 ns_add(unsigned int a, float2 c) {
@@ -282,9 +297,10 @@ struct NsOp {
     MmCursor<kSlots>& slot;
     int i, j0, width_;                   // this lane's row; the warp's first column, and where the columns end
     bool live, last;
+    PsStat* const stats;
 
     __device__ __forceinline__ Epilogue(const NsArgs& a, const NsTile& item, TcWarp& warp, MmCursor<kSlots>& cursor)
-        : at(item), M(a.mats[item.mat]), w(warp), slot(cursor) {}
+        : at(item), M(a.mats[item.mat]), w(warp), slot(cursor), stats(a.stats) {}
 
     __device__ __forceinline__ void begin() {
       const int i0 = at.ti * kTile + w.row;
@@ -292,6 +308,7 @@ struct NsOp {
       j0 = at.tj * kTile + w.col;
       width_ = width(M, at);
       live = (i0 & ~127) < M.m;                            // (as entries(): the CTA's rows hold something)
+      if (stats && w.mark == 0) w.mark = ns_now();
       last = at.step == kNsSteps - 1;
     }
 
@@ -426,7 +443,14 @@ struct NsOp {
       if (i - w.lane < M.m) ns_result(M, v, i - w.lane, w.lane, j, min(32, M.n - j));
     }
 
-    __device__ __forceinline__ void end() {}
+    // (the CTA's time from tile to tile, waiting included, is the later one's)
+    __device__ __forceinline__ void end() {
+      if (stats && live && w.lane == 0 && w.col == 0 && (w.row & 127) == 0) {
+        const unsigned long long now = ns_now();
+        ns_charge(stats, M, w.mark, now, kNsWholeSm);
+        w.mark = now;
+      }
+    }
   };
 };
 
@@ -522,9 +546,10 @@ __device__ __forceinline__ void ns_put8(const NsMat& M, int r, int c, const floa
 
 // One unit of X, scaled, as two planes.
 __global__ void __launch_bounds__(kNsThreads)
-ps_ortho_prepare_kernel(const NsMat* __restrict__ mats, const int2* __restrict__ units) {
+ps_ortho_prepare_kernel(const NsMat* __restrict__ mats, const int2* __restrict__ units, PsStat* __restrict__ stats) {
   __shared__ float tile[64][65];
   mm_pdl();
+  const unsigned long long t0 = stats ? ns_now() : 0ull;
   const int2 u = units[blockIdx.x];
   const NsMat& M = mats[u.x];
   double total = 0.0;
@@ -537,6 +562,7 @@ ps_ortho_prepare_kernel(const NsMat* __restrict__ mats, const int2* __restrict__
   const int r0 = u.y / across * kNsUnitRows, c0 = u.y % across * kNsUnitCols;
   if (!M.flip) {
     ns_each_piece(M, r0, c0, rows, cols, [&](int r, int c, const float (&v)[8]) { ns_put8(M, r, c, v, scale); });
+    if (stats && threadIdx.x == 0) ns_charge(stats, M, t0, ns_now(), 1);
     return;
   }
   // transposed, 64 x 64 at a time: pieces along the source's rows in, along its columns out
@@ -571,6 +597,7 @@ ps_ortho_prepare_kernel(const NsMat* __restrict__ mats, const int2* __restrict__
       }
     }
   }
+  if (stats && threadIdx.x == 0) ns_charge(stats, M, t0, ns_now(), 1);
 }
 
 }  // namespace psb

@@ -6,6 +6,7 @@
 #include <vector>
 
 #include "ps_op.h"
+#include "ps_types.cuh"
 
 namespace psb {
 
@@ -22,6 +23,7 @@ struct NsItem {                          // one matrix, rows x cols with strides
   float decay = 1.f, step = 1.f;         // kNsOutUpdate: dst = dst * decay - step * O
   double* parts = nullptr;               // partial sums of src's squares that are there already; nullptr: computed here
   int nparts = 0;
+  unsigned int stat = 0;                 // its record among the `stats` of a run
 };
 
 // The device tables of one list.  The workspace is its owner's; runs that share one must not overlap on the GPU.
@@ -41,7 +43,8 @@ class NsPlan {
   // Takes over the memory of a plan that no launch uses any more, for the tables of the next build.
   void adopt(NsPlan& old);
   size_t bytes() const { return cap_; }
-  int run(cudaStream_t stream, int* launches = nullptr) const;
+  // stats (device), unless NULL: the matrices' records, to whose device times what the run takes is added.
+  int run(cudaStream_t stream, PsStat* stats = nullptr) const;
   int status(int* out) const;            // waits for the device
 
  private:

@@ -43,6 +43,7 @@ struct SoArgs {
   const NsMat* mats;
   int* status;
   int ctas;                                              // of a cluster: 1, 4, 8 or 16
+  PsStat* stats;                                         // nullptr: no device times
 };
 
 // Byte offset of 16-byte piece `piece` (8 columns) of a row, in planes of 64-column blocks.
@@ -84,6 +85,7 @@ ps_ortho_small_kernel(const __grid_constant__ SoArgs args) {
   }
   if (ctas > 1) mm_cluster_sync();                       // all of them run: their shared memory may be written
   mm_pdl();
+  const unsigned long long t0 = args.stats ? ns_now() : 0ull;
 
   // ---- norm, and X0 as two planes (rows from m on and columns from `cols` on are zeros)
   // (pieces of eight columns of a row; neighbouring lanes take neighbours along the source's rows)
@@ -447,6 +449,7 @@ ps_ortho_small_kernel(const __grid_constant__ SoArgs args) {
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   }
+  if (args.stats && tid == 0) ns_charge(args.stats, M, t0, ns_now(), kNsWholeSm);
   if (ctas > 1) mm_cluster_sync();                       // nobody leaves while its shared memory may be read
   if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 256;" ::"r"(tmem) : "memory");
 }

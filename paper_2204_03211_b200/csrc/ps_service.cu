@@ -150,10 +150,10 @@ struct MuonItem {
   const float* p;
   long long rows, cols;
   float decay, step;
-  unsigned int first_chunk, nchunks;
+  unsigned int first_chunk, nchunks, stat;
   bool operator==(const MuonItem& o) const {
     return p == o.p && rows == o.rows && cols == o.cols && decay == o.decay && step == o.step && first_chunk == o.first_chunk &&
-           nchunks == o.nchunks;
+           nchunks == o.nchunks && stat == o.stat;
   }
 };
 
@@ -1640,7 +1640,7 @@ int muon_set(ps_service* s, const Plan& plan, MuonSet** out) {
     const Block& b = s->blocks[plan.order[i]];
     const ps_job_desc& d = s->jobs[b.job].d;
     want.push_back(MuonItem{blk_p(s, b), b.rows, b.cols, (float)(1.0 - (double)d.lr * (double)d.weight_decay),
-                            (float)((double)d.lr * (double)b.update_scale), tasks[i].first_chunk, tasks[i].nchunks});
+                            (float)((double)d.lr * (double)b.update_scale), tasks[i].first_chunk, tasks[i].nchunks, b.stat_idx});
   }
   const unsigned long long now = ++s->muon_uses;
   for (auto& m : s->muon_sets)
@@ -1694,6 +1694,7 @@ int muon_set(ps_service* s, const Plan& plan, MuonSet** out) {
     it.out = kNsOutUpdate;
     it.decay = want[i].decay;
     it.step = want[i].step;
+    it.stat = want[i].stat;
   }
   // (copied on the service's own stream: a launch that is running does not hold the caller up)
   rc = m->plan.build(items, true, s->muon_ws + at, s->status_dev, s->copy_stream);
@@ -1763,7 +1764,7 @@ int launch_muon(ps_service* s, const std::vector<int>& idx, const Plan& plan, Mu
   s->last_block = kThreads;
   s->last_kernel = "muon";
   consume_pushes(s, idx, slot_index, sl->gen);
-  const int rc = set.plan.run(stream);
+  const int rc = set.plan.run(stream, s->opt_profile ? s->stats_dev : nullptr);
   ce = cudaEventRecord(sl->done, stream);
   sl->done_recorded = ce == cudaSuccess;
   if (rc || ce != cudaSuccess) s->cuda_err = rc ? ps_op_last_error() : cudaGetErrorString(ce);

@@ -189,6 +189,7 @@ struct TcWarp {
   unsigned int staged, filled;           // barriers of slot 0
   int lane, row, col;                    // the warp's first row and column in the tile
   int* status;
+  unsigned long long mark = 0;           // the epilogue's: when the tile before was done
 };
 
 // Op:

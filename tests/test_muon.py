@@ -531,3 +531,55 @@ def test_sets_that_never_recur():
             done[b] += 1
         w.svc.aggregate([(w.job, b) for b in reversed(group)])
     w.check(done)
+
+
+def work(shape):
+    m, n = min(shape), max(shape)
+    return 5.0 * (3 * m * m * n + m ** 3)
+
+
+@gpu
+@pytest.mark.parametrize("shapes", [[(1024, 1024), (512, 512), (512, 2048), (1536, 700)],       # the general form
+                                    [(64, 256), (128, 128), (128, 900), (100, 256)]])           # the small one
+def test_device_times_cover_the_orthogonalisation(shapes):
+    """What the planner weighs tasks by: a span as long as the call takes on the GPU, not as the sums alone do, and CTA-time
+    that fits into it, four units per SM; results are untouched."""
+    w = World(shapes, 2)
+    w.step()                                                # (tables)
+    w.svc.set_option(B.PS_OPT_PROFILE, 1)
+    e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    for b in range(len(shapes)):
+        s = w.shards(b)
+        w.push(b, s)
+        w.expect(b, s)
+    torch.cuda.synchronize()
+    e0.record()
+    w.svc.aggregate([(w.job, b) for b in range(len(shapes))])
+    e1.record()
+    torch.cuda.synchronize()
+    wall = e0.elapsed_time(e1) * 1e3
+    busy, span, blocks = w.svc.job_profile(w.job)
+    assert blocks == len(shapes)
+    # (the clock that kernels read ticks once a microsecond or so; the events enclose the launches of three kernels)
+    assert 0.5 * wall - 20.0 <= span <= wall * 1.05 + 5.0
+    each = [w.svc.block_profile(w.job, b) for b in range(len(shapes))]
+    assert abs(sum(b for b, _ in each) - busy) <= 1e-6 * busy and max(s for _, s in each) <= span + 1e-6
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    assert busy <= 4 * sms * (wall * 1.05 + 5.0) * 2        # (the CTAs before the products are more than four on an SM)
+    w.check(2)
+    w.svc.set_option(B.PS_OPT_PROFILE, 0)
+    w.step()
+    torch.cuda.synchronize()
+    assert w.svc.job_profile(w.job) == (0.0, 0.0, 0)
+    w.check(3)
+    # alone, the sums take a part of it that can be told: the larger product has the longer time
+    if shapes[0] == (1024, 1024):
+        w.svc.set_option(B.PS_OPT_PROFILE, 1)
+        alone = []
+        for b in range(len(shapes)):
+            for _ in range(2):
+                w.step([b])
+            torch.cuda.synchronize()
+            alone.append(w.svc.block_profile(w.job, b)[0])
+        order = sorted(range(len(shapes)), key=lambda b: work(shapes[b]))
+        assert alone[order[0]] < alone[order[-1]]
