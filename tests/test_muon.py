@@ -583,3 +583,40 @@ def test_device_times_cover_the_orthogonalisation(shapes):
             alone.append(w.svc.block_profile(w.job, b)[0])
         order = sorted(range(len(shapes)), key=lambda b: work(shapes[b]))
         assert alone[order[0]] < alone[order[-1]]
+
+
+@gpu
+def test_rounds_from_several_host_threads():
+    """One service, a job, a stream and a thread each, lists that share nothing but the workspace."""
+    import threading
+    svc = B.Service(0, 1, 1 << 26)
+    worlds = [World(shapes, 2, seed=k, svc=svc) for k, shapes in
+              enumerate(([(64, 64), (300, 70)], [(128, 512)], [(200, 130), (33, 50), (8, 8)], [(513, 260)]))]
+    bufs = [[w.shards(b) for b in range(len(w.shapes))] for w in worlds]
+    torch.cuda.synchronize()
+    errors, ROUNDS = [], 12
+
+    def work(k):
+        try:
+            torch.cuda.set_device(0)
+            w, stream = worlds[k], torch.cuda.Stream()
+            for t in range(ROUNDS):
+                ready = list(range(len(w.shapes)))
+                for b in ready:
+                    for r in range(w.W):
+                        svc.push(w.job, b, r, bufs[k][b][r])
+                svc.aggregate([(w.job, b) for b in (ready if t % 2 else ready[::-1])], stream)
+        except Exception as e:      # noqa: BLE001
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(len(worlds))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors
+    for k, w in enumerate(worlds):
+        for _ in range(ROUNDS):
+            for b in range(len(w.shapes)):
+                w.expect(b, bufs[k][b])
+        w.check(ROUNDS)

@@ -265,3 +265,44 @@ def test_refusals():
     for call in (lambda: lib.ps_ortho_run(None, None), lambda: lib.ps_ortho_status(None, None), lambda: lib.ps_ortho_destroy(None)):
         assert call() == B.PS_ERR_BAD_HANDLE
     assert not h.value
+
+
+@gpu
+def test_handles_from_several_host_threads():
+    """One thread, stream and list each, made and run at the same time: results as on one thread, to the bit."""
+    import threading
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    lists = [[torch.randn(s, device="cuda", generator=gen) for s in shapes] for shapes in
+             ([(64, 256)] * 5, [(777, 300), (130, 130)], [(128, 1000)] * 3, [(700, 900)] * 4, [(40, 2000), (2000, 40)])]
+    alone = []
+    for l in lists:
+        outs = [torch.empty_like(t) for t in l]
+        o = B.Ortho(l, outs)
+        o.run()
+        torch.cuda.synchronize()
+        o.close()
+        alone.append(outs)
+    errors = []
+
+    def work(k):
+        try:
+            torch.cuda.set_device(0)
+            stream = torch.cuda.Stream()
+            for it in range(20):
+                with torch.cuda.stream(stream):
+                    outs = [torch.zeros_like(t) for t in lists[k]]
+                o = B.Ortho(lists[k], outs)
+                for _ in range(3):
+                    o.run(stream)
+                stream.synchronize()
+                assert o.status() == 0 and all(torch.equal(a, b) for a, b in zip(outs, alone[k]))
+                o.close()
+        except Exception as e:      # noqa: BLE001
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(len(lists))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors

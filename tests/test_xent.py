@@ -524,6 +524,40 @@ def test_memory_of_calls_on_other_streams_is_the_allocators_business(monkeypatch
 
 
 @gpu
+def test_objects_from_several_host_threads():
+    """One thread, stream and object each, results as on one thread, to the bit."""
+    import threading
+    sizes = [(300, 1000, 64), (37, 5000, 61), (1000, 300, 136), (5000, 7000, 64)]
+    data = [inputs(*s, seed=k) for k, s in enumerate(sizes)]
+    refs = [run(*s, seed=k) for k, s in enumerate(sizes)]
+    torch.cuda.synchronize()
+    errors = []
+
+    def work(k):
+        try:
+            torch.cuda.set_device(0)
+            stream, (T, V, D) = torch.cuda.Stream(), sizes[k]
+            for it in range(20):
+                with torch.cuda.stream(stream):
+                    ce = B.CrossEntropy(T, V, D)
+                    dx, dw = torch.empty(T, D, device="cuda", dtype=BF), torch.empty(V, D, device="cuda", dtype=BF)
+                loss, lse = ce.forward(*data[k], stream=stream)
+                ce.backward(*data[k], lse, dx, dw, stream=stream)
+                stream.synchronize()
+                assert all(torch.equal(a, b) for a, b in zip((loss, lse, dx, dw), refs[k]))
+        except Exception as e:      # noqa: BLE001
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(len(sizes))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors
+    assert B.ps_xent_status() == 0
+
+
+@gpu
 def test_the_binding_refuses():
     ce = B.CrossEntropy(10, 100, 16)
     x, w, t = inputs(10, 100, 16)
