@@ -801,13 +801,13 @@ int ps_ortho_destroy(ps_ortho* o);
  * a language model, and the gradients of its input and its weight, without the tokens x
  * vocab scores ever being stored.  (The paper has no counterpart: it leaves the workers'
  * arithmetic to the training framework.)
- *     s[t][v] = sum_d x[t][d] * w[v][d]          products exact, summed in binary32
+ *     s[t][v] = sum_d x[t][d] * w[v][d]          products exact, summed in binary32 (additions that cut off)
  *     lse[t] = log(sum_v exp(s[t][v])),  loss[t] = lse[t] - s[t][target[t]]
  *     e[t][v] = g[t] * (exp(s[t][v] - lse[t]) - [v == target[t]]),  g[t] = scale * token_scale[t]
  *     dx[t] = sum_v e[t][v] * w[v],  dw[v] = sum_t e[t][v] * x[t]
  * x and w are bf16.  A token whose target lies outside [0, vocab) (-100, say) is ignored:
  * its loss, lse and row of dx are zeros, and nothing of its row of x reaches dw, NaN
- * included.  exp(s - lse) - [...] is rounded to bf16, the sums over it are binary32; token_scale
+ * included.  exp(s - lse) - [...] is rounded to bf16, also where dw is fp32, the sums over it are binary32; token_scale
  * is applied to dx's sums, and for dw to x, rounded to bf16.  A score that is a NaN or
  * +infinity makes its token's loss and gradients NaN.
  * dx and dw must not overlap the inputs or each other.

@@ -11,7 +11,7 @@
 // outnumber the CTAs only those on and below the diagonal are computed, and stored twice.
 //
 // Measured: 24 of 1024 x 4096 to bf16 1.85 ms cool (1 PFLOP/s, tensor cores 65 % busy; X in two halves, 400 MB, comes from
-// HBM for every product, 6.4 GB in all), 2.2 ms in a row under the power cap, to fp32 4.4 to 4.8 ms; 24 of 512 x 512 to bf16
+// HBM for every product, 6.4 GB in all), 2.2 to 2.5 ms in a row under the power cap, to fp32 4.4 to 4.8 ms; 24 of 512 x 512 to bf16
 // 165 us and 3 of 777 x 300 to fp32 187 us, bound by the latency of fifteen products in a row.
 //
 // Arithmetic.  Operands are fp16 (11 bits) scaled by powers of two, sums are binary32.

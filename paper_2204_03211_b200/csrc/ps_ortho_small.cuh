@@ -8,8 +8,10 @@
 // other's shared memory, a share of the rows each, in rank order.  One launch does it all: norm, scaling, steps, result.
 //
 // Measured to fp32 | bf16: 8 of 64 x 256 46 | 32 us (general form 120), 4 of 128 x 512 64 | 48, 4 of 128 x 2048 95 | 69,
-// 4 of 128 x 4096 106 | 78 (general form 290 | 154).  Bound by the chain: 7.7 us per step on one CTA, of which 1.6 are the
-// MMAs of X X^T and 2 the epilogue of X; over a cluster 4 us more for adding up A.
+// 4 of 128 x 4096 106 | 78 (general form 290 | 154).  Bound by the chain.  Cycles of one CTA, from product to product and
+// epilogue to epilogue, 64 x 256 to fp32 | bf16: A 3740 + 2000 | 1500 + 1600, B 1300 + 1390 | 600 + 1050, X 1920 + 3200 |
+// 820 + 3330, 13 600 | 8900 a step (6.9 | 4.5 us), 10 600 before the first (norm, halves) and 4200 | 2200 more for the
+// result.  Over a cluster (128 x 512) A's epilogue, which adds up the parts, takes 9300.
 //
 // Sixteen warps read the sums (row = lane, 32 columns at a time); thread 0 issues the products.  Arithmetic as in
 // ps_ortho.cuh, with the small products of a pair of halves first and the long sums of A in two parts, so that few of

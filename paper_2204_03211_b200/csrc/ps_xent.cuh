@@ -9,11 +9,14 @@
 // so that what each launch ends with is covered by work that does not depend on it.  A piece of d takes up to
 // 40 MB and so stays in L2 between its writing and its reading.
 //
-// Bound by the tensor cores, and in a row by power, where the width is 1024 and more: losses of 8192 x 30522 x 1024 in 318 us
-// (1.6 PFLOP/s), both gradients in 1317 us (three products of 2 T V D, 1.17 PFLOP/s); by the epilogues of the scores and
-// the ends of launches below (2048 x 33278 x 512: 67 us and 200 us); by its launches where everything is small (37 x 500 x 64: 21 us for four).
+// Bound by the tensor cores, and in a row by power, where the width is 1024 and more: losses of 8192 x 30522 x 1024 in 318 to 331 us
+// (1.55 to 1.6 PFLOP/s), both gradients in 1317 to 1340 us (three products of 2 T V D, 1.15 PFLOP/s); by the epilogues of the
+// scores and the ends of launches below (2048 x 33278 x 512: 61 us, tensor cores 62 % busy, and 202 us, 34 to 54 %); by
+// its launches where everything is small (37 x 500 x 64: 21 us for four).
 //
-// Roundings: products of bf16 values are exact and summed in binary32; maxima, sums, lse and losses are binary32.  What is
+// Roundings: products of bf16 values are exact and summed in binary32 by the tensor cores, whose additions cut off rather
+// than round: losses and lse of 1024 wide x are off by 3.4e-7 of themselves (5e-8 with rounded additions), 512 wide by
+// 1.7e-7.  Maxima, sums of exponentials, lse and losses are binary32.  What is
 // stored of d is exp(s - lse) - [v = target], rounded to bf16 (it is an operand, and x and w are bf16, which one MMA wants
 // of both): at most 2^-8 of each entry, of either sign, and none where it matters most, at the target of an unlikely word,
 // whose -1 is exact.  The factor g_t stays out of it, because its own rounding would be the same for all of a token's
