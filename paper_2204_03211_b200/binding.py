@@ -815,7 +815,9 @@ def _load_ops():
             # The workspace's memory follows the stream that is current now.  Another stream's first call waits for what
             # that one has been given before, whose memory it may have been, and the allocator is told of that stream.
             made_on = torch.cuda.current_stream(self.device)
-            self._streams, self._made, self._waits = {made_on.cuda_stream}, made_on.record_event(), False
+            self._streams, self._waits = {made_on.cuda_stream}, False
+            # (a capture begins when all earlier work is done, and its events are no others' to wait for)
+            self._made = None if torch.cuda.is_current_stream_capturing() else made_on.record_event()
             self._last = made_on                                     # (the stream of the call before is not looked at again)
             super().__init__(tokens, vocab, dim, self.workspace.data_ptr(), self.workspace.numel(), self.device)
 
@@ -825,7 +827,7 @@ def _load_ops():
         def _uses(self, stream):
             handle = _stream_ptr(stream)
             if handle not in self._streams:
-                if not torch.cuda.is_current_stream_capturing():     # (a capture begins when all of that is done)
+                if self._made is not None and not torch.cuda.is_current_stream_capturing():
                     self._torch_stream(handle).wait_event(self._made)
                 if handle == 0 or isinstance(stream, torch.cuda.Stream):
                     self.workspace.record_stream(stream if handle else torch.cuda.default_stream(self.device))

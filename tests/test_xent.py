@@ -412,6 +412,29 @@ def test_dropped_and_fresh_results_while_the_calls_wait(kind, T, V, D):
 
 
 @gpu
+def test_made_inside_a_capture():
+    """Workspace and results from the graph's memory; afterwards the object serves calls outside the graph as well."""
+    T, V, D = 300, 1000, 64
+    x, w, t = inputs(T, V, D)
+    ref = run(T, V, D)
+    dx, dw = torch.empty(T, D, device="cuda", dtype=BF), torch.empty(V, D, device="cuda", dtype=BF)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ce = B.CrossEntropy(T, V, D)
+        stream = torch.cuda.current_stream()
+        loss, lse = ce.forward(x, w, t, stream=stream)
+        ce.backward(x, w, t, lse, dx, dw, stream=stream)
+    graph.replay()
+    torch.cuda.synchronize()
+    for a, b in zip((loss, lse, dx, dw), ref):
+        assert torch.equal(a, b)
+    for other in (None, torch.cuda.Stream()):
+        again = ce.forward(x, w, t, stream=other)
+        torch.cuda.synchronize()
+        assert torch.equal(again[0], ref[0]) and torch.equal(again[1], ref[1])
+
+
+@gpu
 def test_results_made_on_the_default_stream_beside_a_current_one():
     """No stream given is the default one, whatever is current."""
     T, V, D = 200, 700, 64
