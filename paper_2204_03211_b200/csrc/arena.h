@@ -30,8 +30,8 @@ class Arena {
     for (auto it = free_.begin(); it != free_.end(); ++it) {
       if (it->second >= need) {
         const size_t off = it->first, len = it->second;
+        if (len > need) free_[off + need] = len - need;        // (this may throw: nothing is taken yet)
         free_.erase(it);
-        if (len > need) free_[off + need] = len - need;
         used_ += need;
         return off;
       }

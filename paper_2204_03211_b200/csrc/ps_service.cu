@@ -889,27 +889,25 @@ int ps_register_job(ps_service* s, const ps_job_desc* d, int* job_out) {
 
 static int register_locked(ps_service* s, int job, int block, size_t nelem, int ctx, const float* init);
 
-int ps_register_block(ps_service* s, int job, int block, size_t nelem, int ctx, const float* init) {
+int ps_register_block(ps_service* s, int job, int block, size_t nelem, int ctx, const float* init) try {
   if (!alive(s)) return PS_ERR_BAD_HANDLE;
   std::lock_guard<std::mutex> lk(s->mu);
   if (job < 0 || job >= (int)s->jobs.size() || s->jobs[job].d.opt == PS_MUON) return PS_ERR_BAD_ARG;
   return register_locked(s, job, block, nelem, ctx, init);
+} catch (const std::bad_alloc&) {
+  return PS_ERR_NOMEM;
 }
 
 int ps_register_matrix(ps_service* s, int job, int block, long long rows, long long cols, int ctx, const float* init,
-                       float update_scale) {
+                       float update_scale) try {
   if (!alive(s)) return PS_ERR_BAD_HANDLE;
   std::lock_guard<std::mutex> lk(s->mu);
   if (job < 0 || job >= (int)s->jobs.size() || s->jobs[job].d.opt != PS_MUON) return PS_ERR_BAD_ARG;
   if (rows < 1 || cols < 1 || rows > kMuonMaxDim || cols > kMuonMaxDim || !(std::fabs(update_scale) <= 3.4e38f)) return PS_ERR_BAD_ARG;
-  try {
-    NsItem one;                            // (a matrix that no aggregate could work on is refused here)
-    one.rows = rows;
-    one.cols = cols;
-    if (!NsPlan::workspace({one}, true)) return PS_ERR_TOO_LARGE;
-  } catch (const std::bad_alloc&) {
-    return PS_ERR_NOMEM;
-  }
+  NsItem one;                              // (a matrix that no aggregate could work on is refused here)
+  one.rows = rows;
+  one.cols = cols;
+  if (!NsPlan::workspace({one}, true)) return PS_ERR_TOO_LARGE;
   const int rc = register_locked(s, job, block, (size_t)rows * (size_t)cols, ctx, init);
   if (rc) return rc;
   Block& b = s->blocks[s->jobs[job].block_of_id[block]];
@@ -918,6 +916,8 @@ int ps_register_matrix(ps_service* s, int job, int block, long long rows, long l
   b.update_scale = update_scale;
   ++s->muon_blocks;
   return PS_OK;
+} catch (const std::bad_alloc&) {
+  return PS_ERR_NOMEM;
 }
 
 static int register_locked(ps_service* s, int job, int block, size_t nelem, int ctx, const float* init) {
@@ -937,6 +937,9 @@ static int register_locked(ps_service* s, int job, int block, size_t nelem, int 
   const bool reuse = !s->free_blocks.empty();
   const size_t bi_new = reuse ? (size_t)s->free_blocks.back() : s->blocks.size();
   b.stat_idx = (unsigned int)bi_new;
+  // (what throws for want of host memory comes before anything changes)
+  if (block >= (int)j.block_of_id.size()) j.block_of_id.resize(block + 1, -1);
+  if (!reuse && s->blocks.size() == s->blocks.capacity()) s->blocks.reserve(std::max<size_t>(16, 2 * s->blocks.size()));
   if (has_device(s)) PS_CUDA(s, cudaSetDevice(s->device));
   int rc = arena_alloc(s, ctx, b.bytes, &b.off);
   if (rc) return rc;
@@ -955,7 +958,6 @@ static int register_locked(ps_service* s, int job, int block, size_t nelem, int 
     }
     if (rc) { s->ctxs[ctx].arena.release(b.off, b.bytes); return rc; }
   }
-  if (block >= (int)j.block_of_id.size()) j.block_of_id.resize(block + 1, -1);
   j.block_of_id[block] = (int)bi_new;
   if (reuse) {
     s->free_blocks.pop_back();

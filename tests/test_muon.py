@@ -418,18 +418,18 @@ def test_what_fails_half_way_leaves_every_block_usable(tmp_path, sides):
     made_up_runtime(tmp_path, FAILURES, sides)
 
 
-def made_up_runtime(tmp_path, script, *args):
-    """Runs `script` on the runtime of tests/c/pretend_cuda.c, with tests/c/failing_cuda.c in front of it."""
+def made_up_runtime(tmp_path, script, *args, front="failing_cuda.c"):
+    """Runs `script` on the runtime of tests/c/pretend_cuda.c, with another of those files in front of it."""
     import os
     import subprocess
     import sys
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     B.load()
     libs = []
-    for name in ("failing_cuda", "pretend_cuda"):
+    for name in (front, "pretend_cuda.c"):
         libs.append(str(tmp_path / (name + ".so")))
-        subprocess.run(["gcc", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-o", libs[-1],
-                        os.path.join(root, "tests", "c", name + ".c"), "-ldl"], check=True)
+        subprocess.run(["g++" if name.endswith("pp") else "gcc", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-o", libs[-1],
+                        os.path.join(root, "tests", "c", name), "-ldl"], check=True)
     run = subprocess.run([sys.executable, "-c", script, root, libs[0], *args],
                          env=dict(os.environ, LD_PRELOAD=":".join(libs)), capture_output=True, text=True)
     assert run.returncode == 0, run.stderr
@@ -620,3 +620,33 @@ def test_rounds_from_several_host_threads():
             for b in range(len(w.shapes)):
                 w.expect(b, bufs[k][b])
         w.check(ROUNDS)
+
+
+NOMEM = r"""
+import ctypes as C, sys
+sys.path.insert(0, sys.argv[1])
+from paper_2204_03211_b200 import binding as B
+lib, new = B.load(), C.CDLL(sys.argv[2])
+svc = B.Service(0, 1, 1 << 22)
+muon, sgd = svc.register_job(opt=B.PS_MUON, num_workers=2), svc.register_job(num_workers=2)
+used = 0
+for block in range(40):                         # (growth of the tables is among them)
+    for call in (lambda: lib.ps_register_matrix(svc.handle, muon, block, 8, 8, 0, None, 1.0),
+                 lambda: lib.ps_register_block(svc.handle, sgd, block, 64, 0, None)):
+        k = rc = 0
+        while k == 0 or rc != B.PS_OK:
+            k += 1
+            new.fail_new(k)
+            rc = call()
+            new.fail_new(0)
+            assert rc in (B.PS_OK, B.PS_ERR_NOMEM), rc
+            assert svc.arena_info(0)[0] == used + (512 if rc == B.PS_OK else 0), (block, k)
+        assert k > 3 and call() == B.PS_ERR_DUPLICATE
+        used += 512
+svc.close()
+"""
+
+
+def test_registration_that_runs_out_of_memory(tmp_path):
+    """Every allocation of a registration fails once: NOMEM, nothing is taken, and the next attempt succeeds."""
+    made_up_runtime(tmp_path, NOMEM, front="failing_new.cpp")
