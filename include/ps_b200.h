@@ -272,7 +272,8 @@ int ps_push_host_batch(ps_service* svc, int n, const int* jobs, const int* block
  * no-op.  If a listed block is under migration the launch is ordered after the
  * copy (Appendix B, "Data Consistency").
  * Errors (nothing launched, nothing changed): BAD_ARG, DUPLICATE, NOT_READY,
- * NO_DEVICE, NOMEM, CUDA. */
+ * NO_DEVICE, NOMEM, CUDA.  (Where CUDA fails only after a launch is out, that launch's
+ * blocks have consumed their pushes.) */
 int ps_aggregate(ps_service* svc, const ps_task* ready, int n_ready, void* stream);
 
 /* Makes `stream` wait for every ps_aggregate launch enqueued so far that it has
