@@ -1304,7 +1304,10 @@ static int launch_plan(ps_service* s, const std::vector<int>& idx, Plan& plan, c
   s->last_block = bulk ? kBulkThreads : kThreads;
   s->last_kernel = inl ? "inline" : bulk ? "bulk" : "ldg";
   consume_pushes(s, idx, slot_index, sl->gen);
-  PS_CUDA(s, re);
+  if (re != cudaSuccess) {
+    s->cuda_err = std::string("event of a launch: ") + cudaGetErrorString(re);
+    return PS_ERR_CUDA;
+  }
   return PS_OK;
 }
 
@@ -1604,7 +1607,10 @@ int launch_clip(ps_service* s, const std::vector<int>& idx, Plan& plan, const Cl
   s->last_block = kThreads;
   s->last_kernel = inl ? "clip_inline" : "clip";
   consume_pushes(s, idx, slot_index, sl->gen);
-  PS_CUDA(s, re);
+  if (re != cudaSuccess) {
+    s->cuda_err = std::string("event of a launch: ") + cudaGetErrorString(re);
+    return PS_ERR_CUDA;
+  }
   return PS_OK;
 }
 
